@@ -286,6 +286,71 @@ eco_status_t eco_bandwidth_probe(int32_t kind, void *codes, void *scales, const 
 eco_status_t eco_arith_selftest(int32_t kind, float numerator, uint32_t bits_lo, uint32_t bits_hi, uint64_t *mismatches,
                                 void *stream);
 
+/*
+ * The losses at the output projection ("head") of a language model, and their gradients: what makes the bf16 gradient that
+ * eco_step reads for the matrix with the vocabulary's rows.  With h_t a row of hidden states and w_v a row of weights
+ * (dec(code) * scale for the quantized formats), z_tv = h_t . w_v:
+ *     cross entropy      ce_t = lse_t - z_t,label(t),                lse_t  = ln sum_v exp z_tv
+ *     distillation       kd_t = tau^2 sum_j q_tj (ln q_tj - (z_t,id(t,j) / tau - lse'_t)),  lse'_t = ln sum_v exp(z_tv / tau)
+ *                        q_tj = softmax over the present entries j of the teacher's logits l_tj / tau
+ *     gradients          g_tv = a_t (exp(z_tv - lse_t) - [v = label(t)])
+ *                               + b_t tau (exp(z_tv / tau - lse'_t) - sum over j with id(t,j) = v of q_tj)
+ *                        grad_hidden = g W,  grad_weights = g^T hidden;  a = dL/dce, b = dL/dkd
+ * The logits are never kept: the forward pass reduces them tile by tile to a maximum and a sum of exponentials, the backward
+ * pass computes them again by pieces of the vocabulary.
+ *
+ * Masks.  A label outside [0, vocab) (-100, say) is none.  An entry of the teacher whose id lies outside [0, vocab) is absent,
+ * one whose logit is -inf has no weight (0 ln 0 = 0), and an id may come up more than once.  A row without a label has ce = 0, one without an entry that has weight
+ * kd = 0, and a row with neither takes no part: its grad_hidden is 0 and nothing of it reaches grad_weights, whatever its
+ * hidden states hold (infinities and NaN too).  In rows that take part a hidden state, weight or present teacher's logit that is not
+ * finite (but for that -inf) makes results that depend on it NaN or infinite.
+ *
+ * Precision.  Products are sums in fp32 of exact products of bf16 values: fp32 operands enter as three bf16 terms each, quantized
+ * weights as two (a relative 2^-17 of the weight).  Statistics, losses and grad_hidden's sums over the vocabulary are fp32.  g is rounded to bf16 where
+ * both gradients are bf16, else it enters as three terms.  Every output is rounded once.  No atomics: the same call on
+ * the same arrays gives the same bits.
+ */
+typedef struct eco_head {
+  const void *hidden;         /* rows x dim values of hidden_dtype, aligned to their size                                          */
+  const void *weights;        /* vocab x dim in the format fmt, laid out as in eco_tensor_t, 16-byte aligned                       */
+  const void *scales;         /* quantized formats: as in eco_tensor_t; else ignored                                               */
+  const int64_t *labels;      /* rows; NULL: no cross entropy                                                                      */
+  const int32_t *top_ids;     /* rows x top_k ids of the teacher's entries; read if top_k > 0                                      */
+  const void *top_logits;     /* rows x top_k logits of top_dtype                                                                  */
+  const float *grad_ce;       /* backward: rows, dL/dce; NULL: that loss has no gradient                                           */
+  const float *grad_kd;       /* backward: rows, dL/dkd; NULL: the same                                                            */
+  float *ce;                  /* forward output, rows; ignored without labels                                                      */
+  float *kd;                  /* forward output, rows; ignored without a teacher                                                   */
+  float *lse;                 /* rows, lse_t: written by the forward pass and read by the backward; ignored without labels. In rows that take no part 0 */
+  float *lse_tau;             /* rows, lse'_t; ignored without a teacher                                                           */
+  float *picked;              /* rows x (1 + top_k): the logits at the label and at the teacher's entries (0 where there is none);
+                                 written by the forward pass and read by the backward                                              */
+  void *grad_hidden;          /* backward output, rows x dim of hidden_dtype                                                       */
+  void *grad_weights;         /* backward output, vocab x dim of grad_weights_dtype (bf16: what eco_step reads), 16-byte aligned   */
+  uint64_t rows, vocab, dim;  /* at most 2^23, 2^24, 2^16                                                                          */
+  uint64_t hidden_stride;     /* elements from one row to the next, 0: packed; so with the other strides                           */
+  uint64_t weight_stride;     /* quantized weights are packed                                                                      */
+  uint64_t top_stride;        /* of top_ids and of top_logits                                                                      */
+  uint64_t grad_hidden_stride, grad_weights_stride;
+  uint64_t group_size;        /* quantized formats: elements per scale, as in eco_tensor_t, not 0                                  */
+  double temperature;         /* tau, in [2^-20, 2^20]; read if top_k > 0                                                          */
+  uint32_t top_k;             /* the teacher's entries a row, at most 1024; 0: no distillation                                     */
+  int32_t fmt;                /* eco_format_t of the weights                                                                       */
+  int32_t scale_dtype, hidden_dtype, top_dtype, grad_weights_dtype;      /* eco_dtype_t                                            */
+} eco_head_t;
+
+/* eco_head_loss_workspace — host only: bytes of device memory that eco_head_loss (backward = 0) or eco_head_loss_backward (1) needs for
+ * this descriptor.  It depends on rows, vocab, dim, top_k, temperature, the formats, types and weight_stride, and on which losses are there. */
+eco_status_t eco_head_loss_workspace(const eco_head_t *head, int32_t backward, size_t *bytes);
+
+/* eco_head_loss — the losses of every row, with lse, lse_tau and picked.  `workspace`: device memory, 256-byte aligned, of at least the size above;
+ * its contents need not be kept between calls.  Asynchronous on `stream`; allocates nothing, and may be captured into a graph. */
+eco_status_t eco_head_loss(const eco_head_t *head, void *workspace, size_t workspace_bytes, void *stream);
+
+/* eco_head_loss_backward — grad_hidden and grad_weights (both written, not added to) of sum_t grad_ce_t ce_t + grad_kd_t kd_t, from the same inputs and
+ * what the forward pass wrote to lse, lse_tau and picked.  Otherwise as eco_head_loss. */
+eco_status_t eco_head_loss_backward(const eco_head_t *head, void *workspace, size_t workspace_bytes, void *stream);
+
 /* eco_step_constants — host only: validates hp as eco_step does and writes the derived fp32 constants. */
 eco_status_t eco_step_constants(const eco_hparams_t *hp, eco_constants_t *out);
 

@@ -40,6 +40,15 @@ class eco_constants_t(C.Structure):
                                          "wd", "inv_lr", "inv_lr_beta")]
 
 
+class eco_head_t(C.Structure):
+    _fields_ = ([(n, C.c_void_p) for n in ("hidden", "weights", "scales", "labels", "top_ids", "top_logits", "grad_ce", "grad_kd", "ce", "kd",
+                                           "lse", "lse_tau", "picked", "grad_hidden", "grad_weights")]
+                + [(n, C.c_uint64) for n in ("rows", "vocab", "dim", "hidden_stride", "weight_stride", "top_stride", "grad_hidden_stride",
+                                             "grad_weights_stride", "group_size")]
+                + [("temperature", C.c_double), ("top_k", C.c_uint32)]
+                + [(n, C.c_int32) for n in ("fmt", "scale_dtype", "hidden_dtype", "top_dtype", "grad_weights_dtype")])
+
+
 class EcoError(RuntimeError):
     def __init__(self, status: int, message: str):
         super().__init__(f"eco status {status}: {message}")
@@ -65,8 +74,12 @@ def _load() -> C.CDLL:
     lib.eco_philox_fill.argtypes = [u64, u64, u32, u64, u64, vp, vp]
     lib.eco_step_constants.argtypes = [C.POINTER(eco_hparams_t), C.POINTER(eco_constants_t)]
     lib.eco_set_option.argtypes = [i32, C.c_int64]
+    lib.eco_head_loss_workspace.argtypes = [C.POINTER(eco_head_t), i32, C.POINTER(C.c_size_t)]
+    lib.eco_head_loss.argtypes = [C.POINTER(eco_head_t), vp, C.c_size_t, vp]
+    lib.eco_head_loss_backward.argtypes = [C.POINTER(eco_head_t), vp, C.c_size_t, vp]
     for name in ("eco_plan_create", "eco_plan_destroy", "eco_step", "eco_step_tensors", "eco_step_tensors_noalloc", "eco_quantize_init",
-                 "eco_dequantize", "eco_quantize_error", "eco_bandwidth_probe", "eco_arith_selftest", "eco_philox_fill", "eco_step_constants", "eco_set_option", "eco_version"):
+                 "eco_dequantize", "eco_quantize_error", "eco_bandwidth_probe", "eco_arith_selftest", "eco_philox_fill", "eco_step_constants", "eco_set_option", "eco_version",
+                 "eco_head_loss_workspace", "eco_head_loss", "eco_head_loss_backward"):
         getattr(lib, name).restype = C.c_int
     lib.eco_status_string.argtypes = [C.c_int]
     lib.eco_status_string.restype = C.c_char_p
@@ -235,6 +248,30 @@ def eco_arith_selftest(kind: int, numerator: float, bits_lo: int, bits_hi: int, 
 
 def eco_philox_fill(seed: int, step: int, tensor_id: int, first_word: int, n_words: int, dst, stream=None) -> None:
     _check(lib.eco_philox_fill(seed & (2 ** 64 - 1), step, tensor_id, first_word, n_words, _ptr(dst), _stream(stream)))
+
+
+def make_head(*, rows: int, vocab: int, dim: int, hidden=None, weights=None, scales=None, labels=None, top_ids=None, top_logits=None, grad_ce=None,
+              grad_kd=None, ce=None, kd=None, lse=None, lse_tau=None, picked=None, grad_hidden=None, grad_weights=None, hidden_stride=0,
+              weight_stride=0, top_stride=0, grad_hidden_stride=0, grad_weights_stride=0, group_size=0, temperature=1.0, top_k=0,
+              fmt=ECO_FMT_BF16_PLAIN, scale_dtype=ECO_DT_FP32, hidden_dtype=ECO_DT_BF16, top_dtype=ECO_DT_FP32,
+              grad_weights_dtype=ECO_DT_BF16) -> eco_head_t:
+    return eco_head_t(*map(_ptr, (hidden, weights, scales, labels, top_ids, top_logits, grad_ce, grad_kd, ce, kd, lse, lse_tau, picked, grad_hidden,
+                                  grad_weights)), rows, vocab, dim, hidden_stride, weight_stride, top_stride, grad_hidden_stride,
+                      grad_weights_stride, group_size, temperature, top_k, fmt, scale_dtype, hidden_dtype, top_dtype, grad_weights_dtype)
+
+
+def eco_head_loss_workspace(head: eco_head_t, backward: bool) -> int:
+    out = C.c_size_t()
+    _check(lib.eco_head_loss_workspace(C.byref(head), int(backward), C.byref(out)))
+    return out.value
+
+
+def eco_head_loss(head: eco_head_t, workspace, workspace_bytes: int, stream=None) -> None:
+    _check(lib.eco_head_loss(C.byref(head), _ptr(workspace), workspace_bytes, _stream(stream)))
+
+
+def eco_head_loss_backward(head: eco_head_t, workspace, workspace_bytes: int, stream=None) -> None:
+    _check(lib.eco_head_loss_backward(C.byref(head), _ptr(workspace), workspace_bytes, _stream(stream)))
 
 
 class Plan:

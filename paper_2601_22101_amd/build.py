@@ -23,6 +23,8 @@ SOURCES = [
     "eco_step_fp8_bf16.hip",
     "eco_step_int4_f32.hip",
     "eco_step_int4_bf16.hip",
+    "eco_head_api.cpp",
+    "eco_head_kernels.hip",
 ]
 
 # -ffp-contract=off: the kernels spell every fused multiply-add explicitly, so that their fp32

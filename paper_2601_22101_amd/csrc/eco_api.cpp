@@ -587,6 +587,10 @@ void make_small(const SmallItem *items, size_t n, const eco_hparams_t *layout, e
 
 }  // namespace
 
+namespace eco {
+void set_last_error(const char *text) { g_last_error = text; }
+}  // namespace eco
+
 extern "C" {
 
 const char *eco_status_string(int s) {

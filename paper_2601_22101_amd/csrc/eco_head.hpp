@@ -1,0 +1,81 @@
+// Host/device shared declarations of the losses at the output projection (eco_head_loss and its backward): what the host
+// works out from a descriptor, the arrays of a workspace, and the launcher entry points.
+#pragma once
+#include <hip/hip_runtime_api.h>
+#include <stdint.h>
+
+namespace eco {
+
+constexpr uint64_t HEAD_MOST_ROWS = 1ull << 23, HEAD_MOST_VOCAB = 1ull << 24, HEAD_MOST_DIM = 1ull << 16;
+constexpr uint32_t HEAD_MOST_TOP_K = 1024;
+constexpr uint32_t HEAD_ROW_PAD = 256;            // compact rows are laid out in whole row tiles, zero past the last one that takes part
+constexpr uint32_t HEAD_K_STEP = 32;              // the products go over their inner axis in steps of 32
+
+constexpr uint64_t head_round_up(uint64_t x, uint64_t k) { return (x + k - 1) / k * k; }
+
+// A weight or a hidden state enters the products as a sum of bfloat16 planes: one where it is a bfloat16, three where it is an fp32
+// (8 + 8 + 8 bits of significand: exact unless the last plane underflows), two where it is a code times a scale (16 bits: a
+// relative 2^-17, beside a bf16's 2^-8; a logit of a thousand such terms is off by a relative 2^-22).
+constexpr int head_weight_planes(int fmt) { return fmt == 2 ? 1 : fmt == 3 ? 3 : 2; }
+constexpr int head_hidden_planes(int dtype_bf16) { return dtype_bf16 ? 1 : 3; }
+
+struct HeadWeights {                              // where a row of weights comes from
+  const void *data, *scales;
+  uint64_t stride, group;                         // elements between rows (unquantized); elements per scale
+  int32_t fmt, scale_bf16;
+};
+
+// The products' operands are bf16 planes.  The inner axis of a "row" operand is contiguous (element (n, k) at n * ld + k), of a
+// "column" operand the outer one is ((n, k) at k * ld + n).
+struct HeadOperand {
+  const void *data;
+  uint64_t plane;                                 // elements between planes
+  uint32_t ld, planes;
+};
+
+struct HeadRows {                                 // a forward or backward call's inputs, as its small kernels take them
+  const void *hidden;
+  const int64_t *labels;
+  const int32_t *top_ids;
+  const void *top_logits;
+  uint64_t hidden_stride, top_stride;
+  uint32_t rows, vocab, dim, top_k;
+  int32_t hidden_bf16, top_bf16;
+  float tau;
+  // workspace: number of rows that take part, compact row -> row, row -> compact row or -1
+  int32_t *count, *order, *place;
+};
+
+struct HeadStats {                                // the logits' statistics by row and tile of the vocabulary
+  float *max, *sum, *sum_tau;                     // [rows][tiles]; sum_tau only where the temperature needs its own
+  uint32_t tiles;
+};
+
+hipError_t launch_head_rows(const HeadRows &, void *compact, uint32_t padded_rows, uint32_t padded_dim, hipStream_t);
+hipError_t launch_head_convert(const HeadWeights &, uint64_t first, uint32_t rows, uint32_t dim, void *planes, uint32_t ld, uint64_t plane, hipStream_t);
+// logits' statistics of vocabulary rows first .. first + n - 1, whose tiles begin at `tile`
+hipError_t launch_head_stats(const HeadOperand &w, const HeadOperand &h, uint32_t n, uint32_t rows, uint32_t dim, const int32_t *count, float inv_tau,
+                             const HeadStats &, uint32_t tile, hipStream_t);
+hipError_t launch_head_finish(const HeadRows &, const HeadWeights &, const HeadStats &, float *ce, float *kd, float *lse, float *lse_tau, float *picked,
+                              hipStream_t);
+
+struct HeadRowConst { float lse2, a, lse2_tau, b; };      // of a compact row: log2(e) lse, dL/dce, log2(e) lse_tau, tau dL/dkd
+
+// entries: ids [rows][top_k + 1] (-1: none) and the gradient of the logit at each, over compact rows; consts: the padded rows
+hipError_t launch_head_entries(const HeadRows &, uint32_t padded_rows, const float *grad_ce, const float *grad_kd, const float *lse, const float *lse_tau,
+                               const float *picked, int merged, int32_t *ids, float *values, HeadRowConst *consts, hipStream_t);
+// g[row][v] of a piece: planes of [padded rows][ld]
+hipError_t launch_head_grad(const HeadOperand &w, const HeadOperand &h, uint32_t n, uint32_t rows, uint32_t dim, const int32_t *count, float inv_tau, int two,
+                            const HeadRowConst *, void *g, uint32_t g_ld, uint64_t g_plane, uint32_t g_planes, hipStream_t);
+hipError_t launch_head_scatter(const int32_t *ids, const float *values, uint32_t rows, uint32_t entries, const int32_t *count, uint64_t first, uint32_t n, void *g,
+                               uint32_t g_ld, uint64_t g_plane, uint32_t g_planes, hipStream_t);
+// partial[s][compact row][dim] (+)= g w over a piece, s the split of the piece's vocabulary
+hipError_t launch_head_grad_hidden(const HeadOperand &w, const HeadOperand &g, uint32_t n, uint32_t rows, uint32_t dim, const int32_t *count, uint32_t splits,
+                                   float *partial, uint32_t partial_ld, uint64_t partial_stride, int add, hipStream_t);
+hipError_t launch_head_grad_hidden_finish(const float *partial, uint32_t splits, uint32_t partial_ld, uint64_t partial_stride, const HeadRows &, void *out,
+                                          uint64_t out_stride, hipStream_t);
+hipError_t launch_head_grad_weights(const HeadOperand &h, const HeadOperand &g, uint32_t n, uint32_t dim, const int32_t *count, void *out, uint64_t out_stride,
+                                    int out_bf16, hipStream_t);
+uint32_t head_vocab_tile(uint32_t rows);          // vocabulary rows to a tile of the statistics
+
+}  // namespace eco

@@ -1,0 +1,274 @@
+// C ABI of the losses at the output projection (eco_head_* in include/eco.h): argument checks, the layout of the caller's
+// workspace, and the order of the launches.
+#include <hip/hip_runtime.h>
+
+#include <cmath>
+#include <cstdarg>
+#include <cstdio>
+#include <cstring>
+
+#include "../../include/eco.h"
+#include "eco_head.hpp"
+#include "eco_internal.hpp"
+
+namespace {
+
+eco_status_t fail(eco_status_t st, const char *fmt, ...) {
+  char buf[512];
+  va_list ap;
+  va_start(ap, fmt);
+  vsnprintf(buf, sizeof buf, fmt, ap);
+  va_end(ap);
+  eco::set_last_error(buf);
+  return st;
+}
+
+bool aligned(const void *p, uintptr_t to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) == 0; }
+bool is_dtype(int32_t d) { return d == ECO_DT_FP32 || d == ECO_DT_BF16; }
+uintptr_t size_of(int32_t dtype) { return dtype == ECO_DT_BF16 ? 2 : 4; }
+bool quantized(int32_t fmt) { return fmt == ECO_FMT_FP8_E4M3 || fmt == ECO_FMT_INT4; }
+uint64_t stride_or(uint64_t stride, uint64_t packed) { return stride ? stride : packed; }
+
+// What both directions read.
+eco_status_t check_head(const eco_head_t *h) {
+  if (!h) return fail(ECO_EINVAL, "head: null pointer");
+  if (h->rows == 0 || h->vocab == 0 || h->dim == 0) return fail(ECO_EINVAL, "head: rows, vocab and dim must be positive");
+  if (h->rows > eco::HEAD_MOST_ROWS || h->vocab > eco::HEAD_MOST_VOCAB || h->dim > eco::HEAD_MOST_DIM)
+    return fail(ECO_EUNSUPPORTED, "head: at most 2^23 rows, a vocabulary of 2^24 and 2^16 dimensions");
+  if (h->fmt < ECO_FMT_FP8_E4M3 || h->fmt > ECO_FMT_FP32_IDENTITY) return fail(ECO_EINVAL, "head: unknown weight format %d", h->fmt);
+  if (!is_dtype(h->hidden_dtype)) return fail(ECO_EINVAL, "head: unknown hidden dtype");
+  if (!h->hidden || !h->weights) return fail(ECO_EINVAL, "head: null hidden or weights");
+  if (!h->labels && h->top_k == 0) return fail(ECO_EINVAL, "head: neither labels nor a teacher's entries: there is no loss to compute");
+  if (!aligned(h->hidden, size_of(h->hidden_dtype))) return fail(ECO_EALIGN, "head: hidden is not aligned to its elements");
+  if (!aligned(h->weights, 16)) return fail(ECO_EALIGN, "head: weights must be 16-byte aligned");
+  if (!aligned(h->labels, 8)) return fail(ECO_EALIGN, "head: labels are not aligned to their elements");
+  if (h->hidden_stride && h->hidden_stride < h->dim) return fail(ECO_EINVAL, "head: hidden_stride is less than dim");
+  if (quantized(h->fmt)) {
+    if (!h->scales) return fail(ECO_EINVAL, "head: quantized format needs scales");
+    if (!is_dtype(h->scale_dtype)) return fail(ECO_EINVAL, "head: unknown scale dtype");
+    if (!aligned(h->scales, 16)) return fail(ECO_EALIGN, "head: scales must be 16-byte aligned");
+    if (h->weight_stride && h->weight_stride != h->dim) return fail(ECO_EUNSUPPORTED, "head: the rows of quantized weights are packed");
+    if (h->group_size == 0) return fail(ECO_EINVAL, "head: group_size must be positive");
+    if (eco::classify_group(h->group_size, h->vocab * h->dim) == eco::GROUP_UNSUPPORTED)
+      return fail(ECO_EUNSUPPORTED, "head: scale group of %llu elements: supported are powers of two in [32, 512], multiples of 8 up to 8192, "
+                  "and the whole tensor", (unsigned long long)h->group_size);
+  } else if (h->weight_stride && h->weight_stride < h->dim) {
+    return fail(ECO_EINVAL, "head: weight_stride is less than dim");
+  }
+  if (h->top_k) {
+    if (h->top_k > eco::HEAD_MOST_TOP_K) return fail(ECO_EUNSUPPORTED, "head: at most %u teacher entries a row", eco::HEAD_MOST_TOP_K);
+    if (!h->top_ids || !h->top_logits) return fail(ECO_EINVAL, "head: null top_ids or top_logits");
+    if (!is_dtype(h->top_dtype)) return fail(ECO_EINVAL, "head: unknown dtype of the teacher's logits");
+    if (!aligned(h->top_ids, 4) || !aligned(h->top_logits, size_of(h->top_dtype))) return fail(ECO_EALIGN, "head: top_ids or top_logits are not aligned to their elements");
+    if (h->top_stride && h->top_stride < h->top_k) return fail(ECO_EINVAL, "head: top_stride is less than top_k");
+    const float tau = static_cast<float>(h->temperature);
+    if (!(tau >= 0x1p-20f && tau <= 0x1p20f)) return fail(ECO_EINVAL, "head: temperature must lie in [2^-20, 2^20]");
+  }
+  if (!h->picked || (h->labels && !h->lse) || (h->top_k && !h->lse_tau)) return fail(ECO_EINVAL, "head: null lse, lse_tau or picked");
+  if (!aligned(h->picked, 4) || !aligned(h->lse, 4) || !aligned(h->lse_tau, 4)) return fail(ECO_EALIGN, "head: lse, lse_tau or picked are not aligned to their elements");
+  return ECO_OK;
+}
+
+eco_status_t check_forward(const eco_head_t *h) {
+  if ((h->labels && !h->ce) || (h->top_k && !h->kd)) return fail(ECO_EINVAL, "head: null ce or kd");
+  if (!aligned(h->ce, 4) || !aligned(h->kd, 4)) return fail(ECO_EALIGN, "head: ce or kd are not aligned to their elements");
+  return ECO_OK;
+}
+
+eco_status_t check_backward(const eco_head_t *h) {
+  if (!h->grad_hidden || !h->grad_weights) return fail(ECO_EINVAL, "head: null grad_hidden or grad_weights");
+  if (!((h->labels && h->grad_ce) || (h->top_k && h->grad_kd))) return fail(ECO_EINVAL, "head: neither loss that is there has an upstream gradient");
+  if (!is_dtype(h->grad_weights_dtype)) return fail(ECO_EINVAL, "head: unknown dtype of grad_weights");
+  if (!aligned(h->grad_ce, 4) || !aligned(h->grad_kd, 4) || !aligned(h->grad_hidden, size_of(h->hidden_dtype)))
+    return fail(ECO_EALIGN, "head: grad_ce, grad_kd or grad_hidden are not aligned to their elements");
+  if (!aligned(h->grad_weights, 16)) return fail(ECO_EALIGN, "head: grad_weights must be 16-byte aligned");
+  if (h->grad_hidden_stride && h->grad_hidden_stride < h->dim) return fail(ECO_EINVAL, "head: grad_hidden_stride is less than dim");
+  if (h->grad_weights_stride && h->grad_weights_stride < h->dim) return fail(ECO_EINVAL, "head: grad_weights_stride is less than dim");
+  return ECO_OK;
+}
+
+// The arrays of a workspace and the pieces of the vocabulary that a call goes by.
+struct Layout {
+  uint32_t padded_rows, padded_dim, entries, piece, hidden_planes, weight_planes, grad_planes, tiles, splits;
+  bool in_place, two;
+  uint64_t count, order, place, compact, planes, max, sum, sum_tau, ids, values, consts, g, partial, bytes;
+};
+
+// Bytes that the converted weights and the logits' gradient of a piece of the vocabulary may take each: what the 256 MB cache in
+// front of HBM holds of them between the product that writes a piece and those that read it.
+constexpr uint64_t PIECE_BYTES = 256ull << 20;
+
+bool two_softmaxes(const eco_head_t *h) { return h->labels && h->top_k && static_cast<float>(h->temperature) != 1.0f; }
+
+Layout layout_of(const eco_head_t *h, bool backward) {
+  Layout l;
+  std::memset(&l, 0, sizeof l);
+  l.padded_rows = static_cast<uint32_t>(eco::head_round_up(h->rows, eco::HEAD_ROW_PAD));
+  l.padded_dim = static_cast<uint32_t>(eco::head_round_up(h->dim, eco::HEAD_K_STEP));
+  l.entries = h->top_k + 1;
+  l.hidden_planes = static_cast<uint32_t>(eco::head_hidden_planes(h->hidden_dtype == ECO_DT_BF16));
+  l.weight_planes = static_cast<uint32_t>(eco::head_weight_planes(h->fmt));
+  l.grad_planes = h->hidden_dtype == ECO_DT_BF16 && h->grad_weights_dtype == ECO_DT_BF16 ? 1 : 3;
+  l.two = two_softmaxes(h);
+  // bf16 weights are read where they lie if 16-byte pieces of their rows are whole
+  const uint64_t stride = stride_or(h->weight_stride, h->dim);
+  l.in_place = h->fmt == ECO_FMT_BF16_PLAIN && h->dim % 8 == 0 && stride % 8 == 0 && stride <= (1u << 22);
+  const uint32_t tile = eco::head_vocab_tile(static_cast<uint32_t>(h->rows));
+  uint64_t piece = eco::head_round_up(h->vocab, 256);
+  const auto limit = [&](uint64_t row_bytes) {
+    const uint64_t most = PIECE_BYTES / row_bytes / 256 * 256;
+    if (piece > most) piece = most < 1024 ? 1024 : most;
+  };
+  if (!l.in_place) limit(2ull * l.padded_dim * l.weight_planes);
+  if (backward) limit(2ull * l.padded_rows * l.grad_planes);
+  l.piece = static_cast<uint32_t>(piece);
+  l.tiles = static_cast<uint32_t>((h->vocab + tile - 1) / tile);
+  uint64_t at = 0;
+  const auto take = [&at](uint64_t bytes) { const uint64_t here = at; at += eco::head_round_up(bytes, 256); return here; };
+  l.count = take(4);
+  l.order = take(4 * h->rows);
+  l.place = take(4 * h->rows);
+  l.compact = take(2ull * l.hidden_planes * l.padded_rows * l.padded_dim);
+  if (!l.in_place) l.planes = take(2ull * l.weight_planes * piece * l.padded_dim);
+  if (!backward) {
+    l.max = take(4ull * h->rows * l.tiles);
+    l.sum = take(4ull * h->rows * l.tiles);
+    if (l.two) l.sum_tau = take(4ull * h->rows * l.tiles);
+  } else {
+    l.ids = take(4ull * h->rows * l.entries);
+    l.values = take(4ull * h->rows * l.entries);
+    l.consts = take(sizeof(eco::HeadRowConst) * l.padded_rows);
+    l.g = take(2ull * l.grad_planes * l.padded_rows * piece);
+    l.splits = 1;
+    l.partial = take(4ull * l.splits * l.padded_rows * l.padded_dim);
+  }
+  l.bytes = at;
+  return l;
+}
+
+eco_status_t check_workspace(const Layout &l, void *workspace, size_t bytes) {
+  if (!workspace) return fail(ECO_EINVAL, "head: null workspace");
+  if (!aligned(workspace, 256)) return fail(ECO_EALIGN, "head: the workspace must be 256-byte aligned");
+  if (bytes < l.bytes) return fail(ECO_EINVAL, "head: a workspace of %llu bytes is needed, this one has %llu", (unsigned long long)l.bytes, (unsigned long long)bytes);
+  return ECO_OK;
+}
+
+eco::HeadRows rows_of(const eco_head_t *h, const Layout &l, char *ws) {
+  eco::HeadRows r;
+  std::memset(&r, 0, sizeof r);
+  r.hidden = h->hidden; r.labels = h->labels; r.hidden_stride = stride_or(h->hidden_stride, h->dim);
+  if (h->top_k) { r.top_ids = h->top_ids; r.top_logits = h->top_logits; r.top_stride = stride_or(h->top_stride, h->top_k); }
+  r.rows = static_cast<uint32_t>(h->rows); r.vocab = static_cast<uint32_t>(h->vocab); r.dim = static_cast<uint32_t>(h->dim); r.top_k = h->top_k;
+  r.hidden_bf16 = h->hidden_dtype == ECO_DT_BF16; r.top_bf16 = h->top_dtype == ECO_DT_BF16;
+  r.tau = h->top_k ? static_cast<float>(h->temperature) : 1.0f;
+  r.count = reinterpret_cast<int32_t *>(ws + l.count);
+  r.order = reinterpret_cast<int32_t *>(ws + l.order);
+  r.place = reinterpret_cast<int32_t *>(ws + l.place);
+  return r;
+}
+
+eco::HeadWeights weights_of(const eco_head_t *h) {
+  return {h->weights, h->scales, stride_or(h->weight_stride, h->dim), h->group_size, h->fmt, h->scale_dtype == ECO_DT_BF16};
+}
+
+eco::HeadOperand hidden_operand(const Layout &l, char *ws) {
+  return {ws + l.compact, static_cast<uint64_t>(l.padded_rows) * l.padded_dim, l.padded_dim, l.hidden_planes};
+}
+
+// Weights first .. first + n - 1 as an operand: where they lie, or converted into the workspace.
+hipError_t weight_operand(const eco_head_t *h, const Layout &l, char *ws, uint64_t first, uint32_t n, hipStream_t s, eco::HeadOperand *out) {
+  const eco::HeadWeights w = weights_of(h);
+  if (l.in_place) {
+    *out = {static_cast<const uint16_t *>(h->weights) + first * w.stride, 0, static_cast<uint32_t>(w.stride), 1};
+    return hipSuccess;
+  }
+  const uint64_t plane = static_cast<uint64_t>(l.piece) * l.padded_dim;
+  *out = {ws + l.planes, plane, l.padded_dim, l.weight_planes};
+  return eco::launch_head_convert(w, first, n, static_cast<uint32_t>(h->dim), ws + l.planes, l.padded_dim, plane, s);
+}
+
+}  // namespace
+
+#define HEAD_LAUNCH(call)                                                                                 \
+  do {                                                                                                    \
+    const hipError_t e_ = (call);                                                                         \
+    if (e_ != hipSuccess) return fail(ECO_EHIP, "head kernel launch: %s", hipGetErrorString(e_));        \
+  } while (0)
+
+extern "C" {
+
+eco_status_t eco_head_loss_workspace(const eco_head_t *head, int32_t backward, size_t *bytes) {
+  eco_status_t st = check_head(head);
+  if (st != ECO_OK) return st;
+  if (!bytes) return fail(ECO_EINVAL, "head: null size");
+  if (backward && !is_dtype(head->grad_weights_dtype)) return fail(ECO_EINVAL, "head: unknown dtype of grad_weights");
+  *bytes = static_cast<size_t>(layout_of(head, backward != 0).bytes);
+  return ECO_OK;
+}
+
+eco_status_t eco_head_loss(const eco_head_t *head, void *workspace, size_t workspace_bytes, void *stream) {
+  eco_status_t st = check_head(head);
+  if (st == ECO_OK) st = check_forward(head);
+  if (st != ECO_OK) return st;
+  const Layout l = layout_of(head, false);
+  st = check_workspace(l, workspace, workspace_bytes);
+  if (st != ECO_OK) return st;
+  (void)hipGetLastError();
+  char *ws = static_cast<char *>(workspace);
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  const eco::HeadRows r = rows_of(head, l, ws);
+  HEAD_LAUNCH(eco::launch_head_rows(r, ws + l.compact, l.padded_rows, l.padded_dim, s));
+  const eco::HeadStats stats = {reinterpret_cast<float *>(ws + l.max), reinterpret_cast<float *>(ws + l.sum),
+                                l.two ? reinterpret_cast<float *>(ws + l.sum_tau) : nullptr, l.tiles};
+  const uint32_t tile = eco::head_vocab_tile(r.rows);
+  for (uint64_t first = 0; first < head->vocab; first += l.piece) {
+    const uint32_t n = static_cast<uint32_t>(head->vocab - first < l.piece ? head->vocab - first : l.piece);
+    eco::HeadOperand w;
+    HEAD_LAUNCH(weight_operand(head, l, ws, first, n, s, &w));
+    HEAD_LAUNCH(eco::launch_head_stats(w, hidden_operand(l, ws), n, r.rows, r.dim, r.count, 1.0f / r.tau, stats, static_cast<uint32_t>(first / tile), s));
+  }
+  HEAD_LAUNCH(eco::launch_head_finish(r, weights_of(head), stats, head->labels ? head->ce : nullptr, head->top_k ? head->kd : nullptr,
+                                      head->labels ? head->lse : nullptr, head->top_k ? head->lse_tau : nullptr, head->picked, s));
+  return ECO_OK;
+}
+
+eco_status_t eco_head_loss_backward(const eco_head_t *head, void *workspace, size_t workspace_bytes, void *stream) {
+  eco_status_t st = check_head(head);
+  if (st == ECO_OK) st = check_backward(head);
+  if (st != ECO_OK) return st;
+  const Layout l = layout_of(head, true);
+  st = check_workspace(l, workspace, workspace_bytes);
+  if (st != ECO_OK) return st;
+  (void)hipGetLastError();
+  char *ws = static_cast<char *>(workspace);
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  const eco::HeadRows r = rows_of(head, l, ws);
+  HEAD_LAUNCH(eco::launch_head_rows(r, ws + l.compact, l.padded_rows, l.padded_dim, s));
+  const float *grad_ce = head->labels ? head->grad_ce : nullptr, *grad_kd = head->top_k ? head->grad_kd : nullptr;
+  // which softmaxes the logits' gradient has: the labels' (0), both (1), the teacher's (2); at a temperature of 1 the two are one
+  const bool merged = grad_ce && grad_kd && !l.two;
+  const int two = grad_ce && grad_kd ? l.two : grad_ce ? 0 : 2;
+  int32_t *ids = reinterpret_cast<int32_t *>(ws + l.ids);
+  float *values = reinterpret_cast<float *>(ws + l.values), *partial = reinterpret_cast<float *>(ws + l.partial);
+  eco::HeadRowConst *consts = reinterpret_cast<eco::HeadRowConst *>(ws + l.consts);
+  HEAD_LAUNCH(eco::launch_head_entries(r, l.padded_rows, grad_ce, grad_kd, head->labels ? head->lse : nullptr, head->top_k ? head->lse_tau : nullptr, head->picked,
+                                       merged, ids, values, consts, s));
+  const uint64_t g_plane = static_cast<uint64_t>(l.padded_rows) * l.piece, partial_stride = static_cast<uint64_t>(l.padded_rows) * l.padded_dim;
+  const eco::HeadOperand g = {ws + l.g, g_plane, l.piece, l.grad_planes}, hidden = hidden_operand(l, ws);
+  const uint64_t out_stride = stride_or(head->grad_weights_stride, head->dim);
+  for (uint64_t first = 0; first < head->vocab; first += l.piece) {
+    const uint32_t n = static_cast<uint32_t>(head->vocab - first < l.piece ? head->vocab - first : l.piece);
+    eco::HeadOperand w;
+    HEAD_LAUNCH(weight_operand(head, l, ws, first, n, s, &w));
+    HEAD_LAUNCH(eco::launch_head_grad(w, hidden, n, r.rows, r.dim, r.count, 1.0f / r.tau, two, consts, ws + l.g, l.piece, g_plane, l.grad_planes, s));
+    HEAD_LAUNCH(eco::launch_head_scatter(ids, values, r.rows, l.entries, r.count, first, n, ws + l.g, l.piece, g_plane, l.grad_planes, s));
+    HEAD_LAUNCH(eco::launch_head_grad_hidden(w, g, n, r.rows, r.dim, r.count, l.splits, partial, l.padded_dim, partial_stride, first != 0, s));
+    char *out = static_cast<char *>(head->grad_weights) + first * out_stride * size_of(head->grad_weights_dtype);
+    HEAD_LAUNCH(eco::launch_head_grad_weights(hidden, g, n, r.dim, r.count, out, out_stride, head->grad_weights_dtype == ECO_DT_BF16, s));
+  }
+  HEAD_LAUNCH(eco::launch_head_grad_hidden_finish(partial, l.splits, l.padded_dim, partial_stride, r, head->grad_hidden,
+                                                  stride_or(head->grad_hidden_stride, head->dim), s));
+  return ECO_OK;
+}
+
+}  // extern "C"

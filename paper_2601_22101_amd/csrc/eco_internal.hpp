@@ -498,6 +498,9 @@ inline int log2_exact(uint64_t x) { return x && !(x & (x - 1)) ? __builtin_ctzll
 hipError_t launch_philox_fill(uint64_t seed, uint64_t step, uint32_t tensor_id, uint64_t first_word, uint64_t n_words,
                               uint32_t *dst, hipStream_t stream);
 
+// sets the calling thread's eco_last_error()
+void set_last_error(const char *text);
+
 // per-(fmt, state) translation units of the quantized step kernel
 hipError_t launch_step_fp8_f32(const KernelVariant &, const StepLaunch &, hipStream_t);
 hipError_t launch_step_fp8_bf16(const KernelVariant &, const StepLaunch &, hipStream_t);

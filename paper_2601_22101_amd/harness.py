@@ -443,3 +443,93 @@ class DeviceWorkload:
         self.plan.close()
         for p in self.plans:
             p.close()
+
+
+_DTYPE = {torch.float32: eco.ECO_DT_FP32, torch.bfloat16: eco.ECO_DT_BF16}
+
+
+class HeadLoss:
+    """The losses at an output projection and their gradients (eco_head_loss, eco_head_loss_backward) with the memory that a training
+    loop keeps between its steps: the outputs and one workspace for both directions.
+
+    ``weights`` (with ``scales`` and ``group_size`` if quantized) are the arrays that the step updates in place, vocab x dim in the
+    storage format ``fmt``; unquantized ones may have a row stride.  The tensors that forward() and backward() return are the object's own and
+    are written again by its next call; both run on the current stream, or on ``stream``.
+    """
+
+    def __init__(self, rows: int, vocab: int, dim: int, *, weights: torch.Tensor, fmt: int, scales: Optional[torch.Tensor] = None, group_size: int = 0,
+                 hidden_dtype: torch.dtype = torch.bfloat16, labels: bool = True, top_k: int = 0, temperature: float = 1.0, training: bool = True,
+                 grad_weights_dtype: torch.dtype = torch.bfloat16):
+        dev = weights.device
+        f32 = lambda *shape: torch.empty(*shape, dtype=torch.float32, device=dev)     # noqa: E731
+        self.rows, self.vocab, self.dim, self.top_k, self.labels = rows, vocab, dim, top_k, labels
+        self.hidden_dtype, self.device = hidden_dtype, dev
+        self.weights, self.scales = weights, scales
+        quantized = fmt in (eco.ECO_FMT_FP8_E4M3, eco.ECO_FMT_INT4)
+        if quantized:
+            need = vocab * dim if fmt == eco.ECO_FMT_FP8_E4M3 else (vocab * dim + 1) // 2
+            if weights.dtype != torch.uint8 or weights.numel() < need or not weights.is_contiguous():
+                raise ValueError(f"weights: {need} contiguous bytes of codes are needed")
+            if scales is None or not scales.is_contiguous() or group_size <= 0 or scales.numel() < -(-vocab * dim // group_size):
+                raise ValueError("scales: one for each scale group is needed, contiguous")
+        else:
+            want = torch.bfloat16 if fmt == eco.ECO_FMT_BF16_PLAIN else torch.float32
+            if weights.dtype != want or weights.shape != (vocab, dim) or (dim > 1 and weights.stride(1) != 1) or (vocab > 1 and weights.stride(0) < dim):
+                raise ValueError(f"weights: {vocab} x {dim} of {want} with contiguous rows are needed")
+        self.ce = f32(rows) if labels else None
+        self.kd = f32(rows) if top_k else None
+        self.lse = f32(rows) if labels else None
+        self.lse_tau = f32(rows) if top_k else None
+        self.picked = f32(rows, 1 + top_k)
+        self.grad_hidden = torch.empty(rows, dim, dtype=hidden_dtype, device=dev) if training else None
+        self.grad_weights = torch.empty(vocab, dim, dtype=grad_weights_dtype, device=dev) if training else None
+        # the descriptor refuses null inputs: the addresses of a call take the place of these
+        some = self.picked
+        self.head = eco.make_head(rows=rows, vocab=vocab, dim=dim, hidden=some, weights=weights, scales=scales, labels=some if labels else None,
+                                  top_ids=some if top_k else None, top_logits=some if top_k else None, ce=self.ce, kd=self.kd, lse=self.lse,
+                                  lse_tau=self.lse_tau, picked=self.picked, grad_hidden=self.grad_hidden, grad_weights=self.grad_weights,
+                                  weight_stride=0 if quantized else weights.stride(0) if vocab > 1 else 0, group_size=group_size, temperature=temperature, top_k=top_k,
+                                  fmt=fmt, scale_dtype=_DTYPE[scales.dtype] if quantized else eco.ECO_DT_FP32, hidden_dtype=_DTYPE[hidden_dtype],
+                                  grad_weights_dtype=_DTYPE[grad_weights_dtype])
+        self.workspace_bytes = max(eco.eco_head_loss_workspace(self.head, b) for b in ([False, True] if training else [False]))
+        self.workspace = torch.empty(self.workspace_bytes, dtype=torch.uint8, device=dev)
+
+    def _takes(self, name: str, t: torch.Tensor, shape, dtypes) -> None:
+        if t is None or t.shape != shape or t.dtype not in dtypes or t.device != self.device:
+            raise ValueError(f"{name}: {tuple(shape)} of {' or '.join(map(str, dtypes))} on {self.device} is needed")
+        if t.dim() > 1 and t.shape[1] > 1 and t.stride(1) != 1 or t.dim() == 1 and t.shape[0] > 1 and t.stride(0) != 1:
+            raise ValueError(f"{name}: rows must be contiguous")
+        if t.dim() > 1 and t.shape[0] > 1 and t.stride(0) < t.shape[1]:
+            raise ValueError(f"{name}: rows must not overlap")
+
+    def forward(self, hidden: torch.Tensor, labels: Optional[torch.Tensor] = None, top_ids: Optional[torch.Tensor] = None,
+                top_logits: Optional[torch.Tensor] = None, stream=None):
+        """(ce, kd) of every row; None for a loss that is not there.  The inputs are kept for backward()."""
+        h = self.head
+        self._takes("hidden", hidden, (self.rows, self.dim), (self.hidden_dtype,))
+        h.hidden, h.hidden_stride = hidden.data_ptr(), hidden.stride(0) if self.rows > 1 else 0
+        if self.labels:
+            self._takes("labels", labels, (self.rows,), (torch.int64,))
+            h.labels = labels.data_ptr()
+        if self.top_k:
+            self._takes("top_ids", top_ids, (self.rows, self.top_k), (torch.int32,))
+            self._takes("top_logits", top_logits, (self.rows, self.top_k), (torch.float32, torch.bfloat16))
+            stride = top_ids.stride(0) if self.rows > 1 else 0
+            if self.rows > 1 and top_logits.stride(0) != stride:
+                raise ValueError("top_ids and top_logits need the same stride")
+            h.top_ids, h.top_logits, h.top_stride, h.top_dtype = top_ids.data_ptr(), top_logits.data_ptr(), stride, _DTYPE[top_logits.dtype]
+        self._inputs = hidden, labels, top_ids, top_logits
+        eco.eco_head_loss(h, self.workspace, self.workspace_bytes, stream)
+        return self.ce, self.kd
+
+    def backward(self, grad_ce: Optional[torch.Tensor] = None, grad_kd: Optional[torch.Tensor] = None, stream=None):
+        """(grad_hidden, grad_weights) for the inputs of the last forward(), from dL/dce and dL/dkd of every row."""
+        if self.grad_hidden is None:
+            raise RuntimeError("this HeadLoss was made without training=True")
+        h = self.head
+        for name, g in (("grad_ce", grad_ce), ("grad_kd", grad_kd)):
+            if g is not None:
+                self._takes(name, g, (self.rows,), (torch.float32,))
+            setattr(h, name, g.data_ptr() if g is not None else None)
+        eco.eco_head_loss_backward(h, self.workspace, self.workspace_bytes, stream)
+        return self.grad_hidden, self.grad_weights
