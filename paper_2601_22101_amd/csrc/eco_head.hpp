@@ -8,7 +8,6 @@ namespace eco {
 
 constexpr uint64_t HEAD_MOST_ROWS = 1ull << 23, HEAD_MOST_VOCAB = 1ull << 24, HEAD_MOST_DIM = 1ull << 16;
 constexpr uint32_t HEAD_MOST_TOP_K = 1024;
-constexpr uint32_t HEAD_ROW_PAD = 256;            // compact rows are laid out in whole row tiles, zero past the last one that takes part
 constexpr uint32_t HEAD_K_STEP = 32;              // the products go over their inner axis in steps of 32
 
 constexpr uint64_t head_round_up(uint64_t x, uint64_t k) { return (x + k - 1) / k * k; }
@@ -74,8 +73,10 @@ hipError_t launch_head_grad_hidden(const HeadOperand &w, const HeadOperand &g, u
                                    float *partial, uint32_t partial_ld, uint64_t partial_stride, int add, hipStream_t);
 hipError_t launch_head_grad_hidden_finish(const float *partial, uint32_t splits, uint32_t partial_ld, uint64_t partial_stride, const HeadRows &, void *out,
                                           uint64_t out_stride, hipStream_t);
-hipError_t launch_head_grad_weights(const HeadOperand &h, const HeadOperand &g, uint32_t n, uint32_t dim, const int32_t *count, void *out, uint64_t out_stride,
+hipError_t launch_head_grad_weights(const HeadOperand &h, const HeadOperand &g, uint32_t n, uint32_t rows, uint32_t dim, const int32_t *count, void *out, uint64_t out_stride,
                                     int out_bf16, hipStream_t);
-uint32_t head_vocab_tile(uint32_t rows);          // vocabulary rows to a tile of the statistics
+struct HeadTiles { uint32_t vocab, rows; };       // a tile of the logits
+HeadTiles head_tiles(uint64_t rows);
+uint32_t head_splits(uint64_t rows, uint64_t dim, uint64_t piece);      // parts of a piece of the vocabulary that grad_hidden's product sums apart
 
 }  // namespace eco

@@ -103,7 +103,8 @@ bool two_softmaxes(const eco_head_t *h) { return h->labels && h->top_k && static
 Layout layout_of(const eco_head_t *h, bool backward) {
   Layout l;
   std::memset(&l, 0, sizeof l);
-  l.padded_rows = static_cast<uint32_t>(eco::head_round_up(h->rows, eco::HEAD_ROW_PAD));
+  const eco::HeadTiles tile = eco::head_tiles(h->rows);
+  l.padded_rows = static_cast<uint32_t>(eco::head_round_up(h->rows, tile.rows));      // compact rows: whole tiles, zero past the last one that takes part
   l.padded_dim = static_cast<uint32_t>(eco::head_round_up(h->dim, eco::HEAD_K_STEP));
   l.entries = h->top_k + 1;
   l.hidden_planes = static_cast<uint32_t>(eco::head_hidden_planes(h->hidden_dtype == ECO_DT_BF16));
@@ -113,7 +114,6 @@ Layout layout_of(const eco_head_t *h, bool backward) {
   // bf16 weights are read where they lie if 16-byte pieces of their rows are whole
   const uint64_t stride = stride_or(h->weight_stride, h->dim);
   l.in_place = h->fmt == ECO_FMT_BF16_PLAIN && h->dim % 8 == 0 && stride % 8 == 0 && stride <= (1u << 22);
-  const uint32_t tile = eco::head_vocab_tile(static_cast<uint32_t>(h->rows));
   uint64_t piece = eco::head_round_up(h->vocab, 256);
   const auto limit = [&](uint64_t row_bytes) {
     const uint64_t most = PIECE_BYTES / row_bytes / 256 * 256;
@@ -122,7 +122,7 @@ Layout layout_of(const eco_head_t *h, bool backward) {
   if (!l.in_place) limit(2ull * l.padded_dim * l.weight_planes);
   if (backward) limit(2ull * l.padded_rows * l.grad_planes);
   l.piece = static_cast<uint32_t>(piece);
-  l.tiles = static_cast<uint32_t>((h->vocab + tile - 1) / tile);
+  l.tiles = static_cast<uint32_t>((h->vocab + tile.vocab - 1) / tile.vocab);
   uint64_t at = 0;
   const auto take = [&at](uint64_t bytes) { const uint64_t here = at; at += eco::head_round_up(bytes, 256); return here; };
   l.count = take(4);
@@ -139,7 +139,7 @@ Layout layout_of(const eco_head_t *h, bool backward) {
     l.values = take(4ull * h->rows * l.entries);
     l.consts = take(sizeof(eco::HeadRowConst) * l.padded_rows);
     l.g = take(2ull * l.grad_planes * l.padded_rows * piece);
-    l.splits = 1;
+    l.splits = eco::head_splits(h->rows, h->dim, piece);
     l.partial = take(4ull * l.splits * l.padded_rows * l.padded_dim);
   }
   l.bytes = at;
@@ -220,7 +220,7 @@ eco_status_t eco_head_loss(const eco_head_t *head, void *workspace, size_t works
   HEAD_LAUNCH(eco::launch_head_rows(r, ws + l.compact, l.padded_rows, l.padded_dim, s));
   const eco::HeadStats stats = {reinterpret_cast<float *>(ws + l.max), reinterpret_cast<float *>(ws + l.sum),
                                 l.two ? reinterpret_cast<float *>(ws + l.sum_tau) : nullptr, l.tiles};
-  const uint32_t tile = eco::head_vocab_tile(r.rows);
+  const uint32_t tile = eco::head_tiles(r.rows).vocab;
   for (uint64_t first = 0; first < head->vocab; first += l.piece) {
     const uint32_t n = static_cast<uint32_t>(head->vocab - first < l.piece ? head->vocab - first : l.piece);
     eco::HeadOperand w;
@@ -264,7 +264,7 @@ eco_status_t eco_head_loss_backward(const eco_head_t *head, void *workspace, siz
     HEAD_LAUNCH(eco::launch_head_scatter(ids, values, r.rows, l.entries, r.count, first, n, ws + l.g, l.piece, g_plane, l.grad_planes, s));
     HEAD_LAUNCH(eco::launch_head_grad_hidden(w, g, n, r.rows, r.dim, r.count, l.splits, partial, l.padded_dim, partial_stride, first != 0, s));
     char *out = static_cast<char *>(head->grad_weights) + first * out_stride * size_of(head->grad_weights_dtype);
-    HEAD_LAUNCH(eco::launch_head_grad_weights(hidden, g, n, r.dim, r.count, out, out_stride, head->grad_weights_dtype == ECO_DT_BF16, s));
+    HEAD_LAUNCH(eco::launch_head_grad_weights(hidden, g, n, r.rows, r.dim, r.count, out, out_stride, head->grad_weights_dtype == ECO_DT_BF16, s));
   }
   HEAD_LAUNCH(eco::launch_head_grad_hidden_finish(partial, l.splits, l.padded_dim, partial_stride, r, head->grad_hidden,
                                                   stride_or(head->grad_hidden_stride, head->dim), s));

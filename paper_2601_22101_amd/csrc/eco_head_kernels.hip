@@ -142,6 +142,8 @@ __global__ __launch_bounds__(256) void eco_head_convert_kernel(HeadWeights w, ui
 //   GRAD   the same product again: g[y][x] as bf16 planes
 //   DH     x hidden dimension, y rows, k vocabulary: partial sums in fp32
 //   DW     x hidden dimension, y vocabulary, k rows: the gradient of the weights
+// With x along a lane's registers, four neighbours in each group, a row's softmax is a reduction over registers and every end stores
+// neighbours together.
 enum : int { STATS = 0, GRAD = 1, DH = 2, DW = 3 };
 
 struct ProductArgs {
@@ -154,178 +156,357 @@ struct ProductArgs {
   float *out_f32;
   void *out;
   uint64_t out_ld, out_plane;
-  uint32_t out_planes, tiles, tile0, splits;
+  uint32_t out_planes, tiles, tile0, splits, tiles_x, tiles_y;
   int32_t two, out_bf16, add;
   float *sum, *sum_tau;
   const HeadRowConst *consts;
 };
 
-constexpr int TILE = 128, KSTEP = HEAD_K_STEP, LDS_LD = KSTEP + 8;
+constexpr int KSTEP = HEAD_K_STEP;
 
-// 8 elements of an operand along its contiguous axis, or zeros
-__device__ __forceinline__ uint4 load8(const uint16_t *p, bool in) { return in ? *reinterpret_cast<const uint4 *>(p) : make_uint4(0, 0, 0, 0); }
+// 16 bytes a lane from global memory to LDS, past the registers: lane i's go to `lds` + 16 i.  The compiler does not see these
+// writes; wait_loads() and barrier() order them.
+__device__ __forceinline__ void load_to_lds(uint32_t lds, const void *base, uint32_t offset) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds), "v"(offset), "s"(base) : "memory");
+}
+template <int LEFT>
+__device__ __forceinline__ void wait_loads() {
+  asm volatile("s_waitcnt vmcnt(%0)" ::"n"(LEFT) : "memory");
+}
+__device__ __forceinline__ void barrier() {
+  __builtin_amdgcn_sched_barrier(0);
+  asm volatile("s_barrier" ::: "memory");
+  __builtin_amdgcn_sched_barrier(0);
+}
 
-template <bool COLUMN>
-__device__ __forceinline__ void stage(uint16_t (*lds)[LDS_LD], const uint16_t *p, uint32_t ld, uint32_t n0, uint32_t n, uint32_t k0, uint32_t k) {
-#pragma unroll
-  for (int i = 0; i < TILE * KSTEP / 8 / 256; ++i) {
-    const uint32_t c = threadIdx.x + 256 * i;
-    if (COLUMN) {
-      const uint32_t kk = c / (TILE / 8), nn = c % (TILE / 8) * 8;
-      const uint4 v = load8(p + static_cast<uint64_t>(k0 + kk) * ld + n0 + nn, k0 + kk < k && n0 + nn < n);
-      const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-      for (int j = 0; j < 8; ++j) lds[nn + j][kk] = static_cast<uint16_t>(w[j / 2] >> (16 * (j & 1)));
-    } else {
-      const uint32_t nn = c / (KSTEP / 8), kk = c % (KSTEP / 8) * 8;
-      *reinterpret_cast<uint4 *>(&lds[nn][kk]) = load8(p + static_cast<uint64_t>(n0 + nn) * ld + k0 + kk, n0 + nn < n && k0 + kk < k);
-    }
+// A tile of BX x BY by WX x WY waves of 32 x 32 blocks.  The inner axis goes by in steps of 32 through DEPTH places in LDS: while
+// one step is multiplied, the next one is there and DEPTH - 2 are under way.
+template <int BX_, int BY_, int WX_, int WY_, int DEPTH_>
+struct Tile {
+  static constexpr int BX = BX_, BY = BY_, WX = WX_, WY = WY_, DEPTH = DEPTH_;
+  static constexpr int THREADS = WX * WY * 64, NI = BX / WX / 32, NJ = BY / WY / 32;
+  static constexpr int X_BYTES = BX * KSTEP * 2, Y_BYTES = BY * KSTEP * 2, STEP_BYTES = X_BYTES + Y_BYTES;
+  static constexpr int X_LOADS = X_BYTES / 16 / THREADS, Y_LOADS = Y_BYTES / 16 / THREADS, LOADS = X_LOADS + Y_LOADS;
+  static_assert(X_LOADS * THREADS * 16 == X_BYTES && Y_LOADS * THREADS * 16 == Y_BYTES, "whole loads");
+};
+
+// Where the 16-byte piece `c` of a step's operand comes from.  A row operand's step is rows of 64 bytes, a column operand's 32 rows of
+// N elements; the pieces of a row are exchanged so that the lanes which read together find theirs in different banks.
+__device__ __forceinline__ void row_piece(uint32_t c, uint32_t &n, uint32_t &k) {
+  n = c >> 2;
+  k = 8 * ((c & 3) ^ ((n >> 1) & 3));
+}
+__device__ __forceinline__ constexpr uint32_t column_swap(uint32_t k) { return 2 * ((k & 3) | ((k >> 3) & 1) << 2); }
+template <int N>
+__device__ __forceinline__ void column_piece(uint32_t c, uint32_t &n, uint32_t &k) {
+  static_assert(N >= 128, "column_swap exchanges 16 pieces");
+  k = c / (N / 8);
+  n = 8 * ((c % (N / 8)) ^ column_swap(k));
+}
+
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) char lds_char;
+
+// The matrix core's operand for 32 rows of an operand from row n0 on, half `kk` of a step.
+template <int N, bool COLUMN>
+__device__ __forceinline__ bf16x8 fragment(const lds_char *step, int n0, int kk, int lane) {
+  if constexpr (COLUMN) {
+    // a transposing read hands lane i of sixteen the elements n0 + i of four rows of k; lane i brings the address of a quarter of one row
+    const int i = lane & 15, k = 16 * kk + 8 * (lane >> 5) + (i >> 2), n = n0 + 16 * ((lane >> 4) & 1) + 4 * (i & 3);
+    const lds_char *p = step + (k * N + 8 * ((n >> 3) ^ static_cast<int>(column_swap(k))) + (n & 7)) * 2;
+    struct { s16x4 a, b; } v = {__builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4 *)p),
+                                __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4 *)(p + 8 * N))};
+    return __builtin_bit_cast(bf16x8, v);
+  } else {
+    const int n = n0 + (lane & 31), piece = 2 * kk + (lane >> 5);
+    return *(const __attribute__((address_space(3))) bf16x8 *)(step + n * (KSTEP * 2) + 16 * (piece ^ ((n >> 1) & 3)));
   }
 }
 
-template <int MODE>
-__global__ __launch_bounds__(256) void eco_head_product_kernel(ProductArgs a) {
-  __shared__ __attribute__((aligned(16))) uint16_t xs[TILE][LDS_LD], ys[TILE][LDS_LD];
-  __shared__ float red[2][TILE];
+// The tile of the workgroup: the hardware hands workgroups to the eight XCDs in turn, so each XCD takes a run of neighbouring tiles,
+// whose operands its L2 then holds once.
+__device__ __forceinline__ uint32_t xcd_run(uint32_t id, uint32_t all) {
+  const uint32_t each = all / 8, more = all % 8, xcd = id % 8, nth = id / 8;
+  return xcd * each + min(xcd, more) + nth;
+}
+
+template <int MODE, class T>
+__global__ __launch_bounds__(T::THREADS) void eco_head_product_kernel(ProductArgs a) {
   constexpr bool X_COLUMN = MODE == DH || MODE == DW, Y_COLUMN = MODE == DW;
+  constexpr int NI = T::NI, NJ = T::NJ;
+  __shared__ __attribute__((aligned(1024))) char smem[T::DEPTH * T::STEP_BYTES];
   const uint32_t count = static_cast<uint32_t>(*a.count);
   const uint32_t ny = MODE == DW ? a.ny : count;
-  uint32_t k_end = MODE == DW ? (count + KSTEP - 1) / KSTEP * KSTEP : a.k, k_begin = 0;
-  const uint32_t x0 = blockIdx.x * TILE, y0 = blockIdx.y * TILE;
-  if (y0 >= ny) return;
-  if (MODE == DH) {
-    const uint32_t steps = (a.k + KSTEP - 1) / KSTEP, each = (steps + a.splits - 1) / a.splits;
-    k_begin = min(a.k, blockIdx.z * each * KSTEP);
-    k_end = min(a.k, (blockIdx.z + 1) * each * KSTEP);
+  uint32_t tile = xcd_run(blockIdx.x, gridDim.x), split = 0, tx, ty;
+  if (MODE == STATS || MODE == GRAD) {
+    // eight tiles of rows beside each other, then the next of the vocabulary
+    const uint32_t run = 8 * a.tiles_x, band = tile / run, high = min(8u, a.tiles_y - band * 8), in = tile - band * run;
+    tx = in / high; ty = band * 8 + in % high;
+  } else {
+    if (MODE == DH) { split = tile / (a.tiles_x * a.tiles_y); tile -= split * a.tiles_x * a.tiles_y; }
+    ty = tile / a.tiles_x; tx = tile % a.tiles_x;
   }
-  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, wx = (wave & 1) * 64, wy = (wave >> 1) * 64;
-  f32x16 acc[2][2] = {};
-  for (uint32_t px = 0; px < a.x_planes; ++px)
-    for (uint32_t py = 0; py < a.y_planes && px + py <= 2; ++py)
-      for (uint32_t k0 = k_begin; k0 < k_end; k0 += KSTEP) {
-        // columns of X past nx are left out at the end
-        stage<X_COLUMN>(xs, a.x + px * a.x_plane, a.ldx, x0, X_COLUMN ? (a.nx + 7) / 8 * 8 : a.nx, k0, k_end);
-        stage<Y_COLUMN>(ys, a.y + py * a.y_plane, a.ldy, y0, Y_COLUMN ? a.ldy : ny, k0, k_end);
-        __syncthreads();
+  const uint32_t x0 = tx * T::BX, y0 = ty * T::BY;
+  if (y0 >= ny) return;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int wx = wave % T::WX * (NI * 32), wy = wave / T::WX * (NJ * 32);
+  const uint32_t all_steps = MODE == DW ? (count + KSTEP - 1) / KSTEP : (a.k + KSTEP - 1) / KSTEP;
+  uint32_t first = 0, steps = all_steps;
+  if (MODE == DH) {
+    const uint32_t each = (all_steps + a.splits - 1) / a.splits;
+    first = min(all_steps, split * each);
+    steps = min(all_steps, first + each) - first;
+  }
+  // the last step's end: past it pieces repeat valid ones of their row, or rows the last one, against zeros of the other operand
+  const uint32_t tail = MODE == DW ? 0 : a.k % KSTEP;
+
+  uint32_t off_x[T::X_LOADS], off_y[T::Y_LOADS];
 #pragma unroll
-        for (int kk = 0; kk < KSTEP; kk += 16) {
-          bf16x8 fx[2], fy[2];
+  for (int i = 0; i < T::X_LOADS; ++i) {
+    uint32_t n, k;
+    if constexpr (X_COLUMN) {
+      column_piece<T::BX>(threadIdx.x + i * T::THREADS, n, k);
+      off_x[i] = (k * a.ldx + min(x0 + n, (a.nx + 7) / 8 * 8 - 8) - x0) * 2;
+    } else {
+      row_piece(threadIdx.x + i * T::THREADS, n, k);
+      off_x[i] = ((min(x0 + n, a.nx - 1) - x0) * a.ldx + k) * 2;
+    }
+  }
 #pragma unroll
-          for (int i = 0; i < 2; ++i) {
-            fx[i] = *reinterpret_cast<const bf16x8 *>(&xs[wx + 32 * i + (lane & 31)][kk + 8 * (lane >> 5)]);
-            fy[i] = *reinterpret_cast<const bf16x8 *>(&ys[wy + 32 * i + (lane & 31)][kk + 8 * (lane >> 5)]);
-          }
+  for (int i = 0; i < T::Y_LOADS; ++i) {
+    uint32_t n, k;
+    if constexpr (Y_COLUMN) column_piece<T::BY>(threadIdx.x + i * T::THREADS, n, k);
+    else row_piece(threadIdx.x + i * T::THREADS, n, k);
+    off_y[i] = (Y_COLUMN ? k * a.ldy + n : n * a.ldy + k) * 2;
+  }
+  const uint64_t step_x = X_COLUMN ? static_cast<uint64_t>(KSTEP) * a.ldx : KSTEP, step_y = Y_COLUMN ? static_cast<uint64_t>(KSTEP) * a.ldy : KSTEP;
+  const uint16_t *const begin_x = a.x + (X_COLUMN ? x0 : static_cast<uint64_t>(x0) * a.ldx) + first * step_x;
+  const uint16_t *const begin_y = a.y + (Y_COLUMN ? y0 : static_cast<uint64_t>(y0) * a.ldy) + first * step_y;
+
+  // pairs of planes whose product counts: the sum of their places is at most 2
+  uint32_t pairs = 0;
+  for (uint32_t px = 0; px < a.x_planes; ++px) pairs += min(a.y_planes, 3 - px);
+  const uint32_t total = steps * pairs;
+  const uint16_t *from_x = begin_x, *from_y = begin_y;
+  uint32_t px = 0, py = 0, in_pair = 0, issued = 0, place = 0;
+  const uint32_t lds0 = static_cast<uint32_t>(reinterpret_cast<uintptr_t>((lds_char *)smem));
+  const auto issue = [&]() {
+    const uint32_t lds = lds0 + place * T::STEP_BYTES + wave * 1024;
+    const bool end = tail && first + in_pair + 1 == all_steps;
 #pragma unroll
-          for (int i = 0; i < 2; ++i)
-#pragma unroll
-            for (int j = 0; j < 2; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fx[i], fy[j], acc[i][j], 0, 0, 0);
+    for (int i = 0; i < T::X_LOADS; ++i) {
+      uint32_t off = off_x[i];
+      if (MODE != DW && end) {
+        uint32_t n, k;
+        if constexpr (X_COLUMN) {
+          column_piece<T::BX>(threadIdx.x + i * T::THREADS, n, k);
+          if (k >= tail) off -= (k - (tail - 1)) * a.ldx * 2;
+        } else {
+          row_piece(threadIdx.x + i * T::THREADS, n, k);
+          if (k >= tail) off -= k * 2;
         }
-        __syncthreads();
       }
+      load_to_lds(lds + i * T::THREADS * 16, from_x, off);
+    }
+#pragma unroll
+    for (int i = 0; i < T::Y_LOADS; ++i) load_to_lds(lds + T::X_BYTES + i * T::THREADS * 16, from_y, off_y[i]);
+    place = place + 1 == T::DEPTH ? 0 : place + 1;
+    ++issued;
+    if (++in_pair == steps) {
+      in_pair = 0;
+      if (++py == a.y_planes || px + py > 2) { py = 0; ++px; }
+      from_x = begin_x + px * a.x_plane;
+      from_y = begin_y + py * a.y_plane;
+    } else {
+      from_x += step_x;
+      from_y += step_y;
+    }
+  };
+
+  f32x16 acc[NI][NJ] = {};
+  if (total) {
+    bf16x8 ax[NI], ay[NJ], bx[NI], by[NJ];
+    for (int i = 0; i < T::DEPTH - 1; ++i)
+      if (issued < total) issue();
+    if (total >= T::DEPTH - 1) wait_loads<(T::DEPTH - 2) * T::LOADS>();
+    else wait_loads<0>();
+    barrier();
+    uint32_t at = 0;
+    const lds_char *step = (const lds_char *)smem;
+#pragma unroll
+    for (int i = 0; i < NI; ++i) ax[i] = fragment<T::BX, X_COLUMN>(step, wx + 32 * i, 0, lane);
+#pragma unroll
+    for (int j = 0; j < NJ; ++j) ay[j] = fragment<T::BY, Y_COLUMN>(step + T::X_BYTES, wy + 32 * j, 0, lane);
+    for (uint32_t s = 0; s < total; ++s) {
+#pragma unroll
+      for (int i = 0; i < NI; ++i) bx[i] = fragment<T::BX, X_COLUMN>(step, wx + 32 * i, 1, lane);
+#pragma unroll
+      for (int j = 0; j < NJ; ++j) by[j] = fragment<T::BY, Y_COLUMN>(step + T::X_BYTES, wy + 32 * j, 1, lane);
+#pragma unroll
+      for (int i = 0; i < NI; ++i)
+#pragma unroll
+        for (int j = 0; j < NJ; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ax[i], ay[j], acc[i][j], 0, 0, 0);
+      // the next step is there once every wave's loads of it are; the place of the step before this one is free once every
+      // wave has multiplied it
+      if (s + T::DEPTH - 2 < total) wait_loads<(T::DEPTH - 3) * T::LOADS>();
+      else wait_loads<0>();
+      barrier();
+      if (issued < total) issue();
+      at = at + 1 == T::DEPTH ? 0 : at + 1;
+      step = (const lds_char *)smem + at * T::STEP_BYTES;
+      if (s + 1 < total) {
+#pragma unroll
+        for (int i = 0; i < NI; ++i) ax[i] = fragment<T::BX, X_COLUMN>(step, wx + 32 * i, 0, lane);
+#pragma unroll
+        for (int j = 0; j < NJ; ++j) ay[j] = fragment<T::BY, Y_COLUMN>(step + T::X_BYTES, wy + 32 * j, 0, lane);
+      }
+#pragma unroll
+      for (int i = 0; i < NI; ++i)
+#pragma unroll
+        for (int j = 0; j < NJ; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(bx[i], by[j], acc[i][j], 0, 0, 0);
+    }
+  }
 
   // acc[i][j][r]: x = x0 + wx + 32 i + (r & 3) + 8 (r >> 2) + 4 (lane >> 5), y = y0 + wy + 32 j + (lane & 31)
   const auto x_of = [&](int i, int r) { return x0 + wx + 32 * i + (r & 3) + 8 * (r >> 2) + 4 * (lane >> 5); };
-  if (MODE == STATS) {
-    float m[2], s[2], st[2];
+  if constexpr (MODE == STATS) {
+    float *red = reinterpret_cast<float *>(smem);              // [WX][BY], the loads' places are free now
+    const auto across = [&](float (&v)[NJ], auto join) {       // over a tile's x: the other half's registers, then the other waves
+      barrier();
 #pragma unroll
-    for (int j = 0; j < 2; ++j) {
+      for (int j = 0; j < NJ; ++j) {
+        v[j] = join(v[j], __shfl_xor(v[j], 32));
+        if (lane < 32) red[wave % T::WX * T::BY + wy + 32 * j + lane] = v[j];
+      }
+      __syncthreads();
+#pragma unroll
+      for (int j = 0; j < NJ; ++j) {
+        v[j] = red[wy + 32 * j + (lane & 31)];
+#pragma unroll
+        for (int w = 1; w < T::WX; ++w) v[j] = join(v[j], red[w * T::BY + wy + 32 * j + (lane & 31)]);
+      }
+    };
+    float m[NJ], s[NJ];
+    if (x0 + T::BX > a.nx)
+#pragma unroll
+      for (int i = 0; i < NI; ++i)
+#pragma unroll
+        for (int r = 0; r < 16; ++r)
+          if (x_of(i, r) >= a.nx)
+#pragma unroll
+            for (int j = 0; j < NJ; ++j) acc[i][j][r] = -INFINITY;
+#pragma unroll
+    for (int j = 0; j < NJ; ++j) {
       m[j] = -INFINITY;
 #pragma unroll
-      for (int i = 0; i < 2; ++i)
+      for (int i = 0; i < NI; ++i)
 #pragma unroll
-        for (int r = 0; r < 16; ++r) {
-          if (x_of(i, r) >= a.nx) acc[i][j][r] = -INFINITY;
-          m[j] = fmaxf(m[j], acc[i][j][r]);
-        }
-      m[j] = fmaxf(m[j], __shfl_xor(m[j], 32));
-      if (lane < 32) red[wave & 1][wy + 32 * j + lane] = m[j];
+        for (int r = 0; r < 16; ++r) m[j] = fmaxf(m[j], acc[i][j][r]);
     }
-    __syncthreads();
+    across(m, [](float p, float q) { return fmaxf(p, q); });
+    const auto sums = [&](float c) {
 #pragma unroll
-    for (int j = 0; j < 2; ++j) m[j] = fmaxf(red[0][wy + 32 * j + (lane & 31)], red[1][wy + 32 * j + (lane & 31)]);
-    __syncthreads();
-    for (int pass = 0; pass < (a.two ? 2 : 1); ++pass) {
-      const float c = pass ? a.scale2_tau : a.scale2;
+      for (int j = 0; j < NJ; ++j) {
+        const float base = m[j] == -INFINITY ? 0.0f : -m[j] * c;
+        s[j] = 0.0f;
 #pragma unroll
-      for (int j = 0; j < 2; ++j) {
-        const float base = m[j] == -INFINITY ? 0.0f : m[j];
-        float sum = 0.0f;
+        for (int i = 0; i < NI; ++i)
 #pragma unroll
-        for (int i = 0; i < 2; ++i)
-#pragma unroll
-          for (int r = 0; r < 16; ++r) sum += exp2_fast((acc[i][j][r] - base) * c);
-        sum += __shfl_xor(sum, 32);
-        if (lane < 32) red[wave & 1][wy + 32 * j + lane] = sum;
+          for (int r = 0; r < 16; ++r) s[j] += exp2_fast(fmaf(acc[i][j][r], c, base));
       }
       __syncthreads();
+      across(s, [](float p, float q) { return p + q; });
+    };
+    const auto store = [&](float *out, const float (&v)[NJ]) {
+      if (wave % T::WX == 0 && lane < 32)
 #pragma unroll
-      for (int j = 0; j < 2; ++j) (pass ? st : s)[j] = red[0][wy + 32 * j + (lane & 31)] + red[1][wy + 32 * j + (lane & 31)];
-      __syncthreads();
-    }
-    if ((wave & 1) == 0 && lane < 32) {
-#pragma unroll
-      for (int j = 0; j < 2; ++j) {
-        const uint32_t y = y0 + wy + 32 * j + lane;
-        if (y < ny) {
-          const uint64_t at = static_cast<uint64_t>(y) * a.tiles + a.tile0 + blockIdx.x;
-          a.out_f32[at] = m[j];
-          a.sum[at] = s[j];
-          if (a.two) a.sum_tau[at] = st[j];
+        for (int j = 0; j < NJ; ++j) {
+          const uint32_t y = y0 + wy + 32 * j + lane;
+          if (y < ny) out[static_cast<uint64_t>(y) * a.tiles + a.tile0 + tx] = v[j];
         }
-      }
+    };
+    store(a.out_f32, m);
+    sums(a.scale2);
+    store(a.sum, s);
+    if (a.two) {
+      sums(a.scale2_tau);
+      store(a.sum_tau, s);
     }
   }
-  if (MODE == GRAD) {
+  if constexpr (MODE == GRAD) {
 #pragma unroll
-    for (int j = 0; j < 2; ++j) {
+    for (int j = 0; j < NJ; ++j) {
       const uint32_t y = y0 + wy + 32 * j + (lane & 31);
       const HeadRowConst rc = a.consts[y];
       uint16_t *out = static_cast<uint16_t *>(a.out) + static_cast<uint64_t>(y) * a.out_ld;
 #pragma unroll
-      for (int i = 0; i < 2; ++i)
+      for (int i = 0; i < NI; ++i)
 #pragma unroll
-        for (int r = 0; r < 16; ++r) {
-          const uint32_t x = x_of(i, r);
-          float g = 0.0f;
-          if (x < a.nx && y < ny) {
-            if (a.two != 2) g = rc.a * exp2_fast(fmaf(acc[i][j][r], a.scale2, -rc.lse2));
-            if (a.two) g = fmaf(rc.b, exp2_fast(fmaf(acc[i][j][r], a.scale2_tau, -rc.lse2_tau)), g);
+        for (int q = 0; q < 4; ++q) {
+          const uint32_t x = x_of(i, 4 * q);
+          float g[4];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const float z = acc[i][j][4 * q + e];
+            g[e] = 0.0f;
+            if (a.two != 2) g[e] = rc.a * exp2_fast(fmaf(z, a.scale2, -rc.lse2));
+            if (a.two) g[e] = fmaf(rc.b, exp2_fast(fmaf(z, a.scale2_tau, -rc.lse2_tau)), g[e]);
+            if (x + e >= a.nx || y >= ny) g[e] = 0.0f;
           }
           for (uint32_t p = 0; p < a.out_planes; ++p) {
-            uint32_t bits;
-            next_plane(g, bits);
-            out[p * a.out_plane + x] = static_cast<uint16_t>(bits);
+            uint32_t b[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) next_plane(g[e], b[e]);
+            *reinterpret_cast<uint2 *>(out + p * a.out_plane + x) = make_uint2(b[0] | b[1] << 16, b[2] | b[3] << 16);
           }
         }
     }
   }
-  if (MODE == DH) {
+  if constexpr (MODE == DH) {
 #pragma unroll
-    for (int j = 0; j < 2; ++j) {
+    for (int j = 0; j < NJ; ++j) {
       const uint32_t y = y0 + wy + 32 * j + (lane & 31);
-      float *out = a.out_f32 + blockIdx.z * a.out_plane + static_cast<uint64_t>(y) * a.out_ld;
+      float *out = a.out_f32 + split * a.out_plane + static_cast<uint64_t>(y) * a.out_ld;
+      if (y < ny)
 #pragma unroll
-      for (int i = 0; i < 2; ++i)
+        for (int i = 0; i < NI; ++i)
 #pragma unroll
-        for (int r = 0; r < 16; ++r) {
-          const uint32_t x = x_of(i, r);
-          if (x < a.nx && y < ny) out[x] = a.add ? out[x] + acc[i][j][r] : acc[i][j][r];
-        }
+          for (int q = 0; q < 4; ++q) {
+            const uint32_t x = x_of(i, 4 * q);
+            if (x >= a.out_ld) continue;          // whole fours: out_ld is the padded dimension
+            float4 v = make_float4(acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]);
+            float4 *to = reinterpret_cast<float4 *>(out + x);
+            if (a.add) { const float4 o = *to; v.x += o.x; v.y += o.y; v.z += o.z; v.w += o.w; }
+            *to = v;
+          }
     }
   }
-  if (MODE == DW) {
+  if constexpr (MODE == DW) {
 #pragma unroll
-    for (int j = 0; j < 2; ++j) {
+    for (int j = 0; j < NJ; ++j) {
       const uint32_t y = y0 + wy + 32 * j + (lane & 31);
+      if (y >= ny) continue;
       const uint64_t row = static_cast<uint64_t>(y) * a.out_ld;
 #pragma unroll
-      for (int i = 0; i < 2; ++i)
+      for (int i = 0; i < NI; ++i)
 #pragma unroll
-        for (int r = 0; r < 16; ++r) {
-          const uint32_t x = x_of(i, r);
-          if (x >= a.nx || y >= ny) continue;
-          if (a.out_bf16) static_cast<uint16_t *>(a.out)[row + x] = static_cast<uint16_t>(f32x2_to_bf16x2_rne(acc[i][j][r], 0.0f));
-          else static_cast<float *>(a.out)[row + x] = acc[i][j][r];
+        for (int q = 0; q < 4; ++q) {
+          const uint32_t x = x_of(i, 4 * q);
+          if (x + 4 <= a.nx && a.out_ld % 4 == 0) {
+            if (a.out_bf16)
+              *reinterpret_cast<uint2 *>(static_cast<uint16_t *>(a.out) + row + x) =
+                  make_uint2(f32x2_to_bf16x2_rne(acc[i][j][4 * q], acc[i][j][4 * q + 1]), f32x2_to_bf16x2_rne(acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]));
+            else
+              *reinterpret_cast<float4 *>(static_cast<float *>(a.out) + row + x) =
+                  make_float4(acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]);
+          } else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              if (x + e < a.nx) {
+                if (a.out_bf16) static_cast<uint16_t *>(a.out)[row + x + e] = static_cast<uint16_t>(f32x2_to_bf16x2_rne(acc[i][j][4 * q + e], 0.0f));
+                else static_cast<float *>(a.out)[row + x + e] = acc[i][j][4 * q + e];
+              }
+          }
         }
     }
   }
@@ -520,6 +701,29 @@ __global__ __launch_bounds__(256) void eco_head_grad_hidden_finish_kernel(const 
 
 uint32_t blocks_for(uint64_t work) { return static_cast<uint32_t>(work < 256 * 8192 ? (work + 255) / 256 : 8192); }
 
+// Tiles by the number of rows.
+using Large = Tile<256, 256, 2, 4, 4>;
+using Medium = Tile<256, 128, 4, 2, 3>;
+using Small = Tile<128, 64, 4, 1, 4>;
+enum Shape { SMALL, MEDIUM, LARGE };
+Shape shape_for(uint64_t rows) { return rows <= 64 ? SMALL : rows <= 1024 ? MEDIUM : LARGE; }
+
+template <int MODE, class T>
+hipError_t launch_tiles(ProductArgs a, uint32_t x, uint32_t y, hipStream_t s) {
+  a.tiles_x = (x + T::BX - 1) / T::BX;
+  a.tiles_y = (y + T::BY - 1) / T::BY;
+  hipLaunchKernelGGL((eco_head_product_kernel<MODE, T>), dim3(a.tiles_x * a.tiles_y * a.splits), dim3(T::THREADS), 0, s, a);
+  return hipGetLastError();
+}
+template <int MODE>
+hipError_t launch_product(const ProductArgs &a, uint64_t rows, uint32_t x, uint32_t y, hipStream_t s) {
+  switch (shape_for(rows)) {
+    case SMALL: return launch_tiles<MODE, Small>(a, x, y, s);
+    case MEDIUM: return launch_tiles<MODE, Medium>(a, x, y, s);
+    default: return launch_tiles<MODE, Large>(a, x, y, s);
+  }
+}
+
 ProductArgs product(const HeadOperand &x, const HeadOperand &y) {
   ProductArgs a = {};
   a.x = static_cast<const uint16_t *>(x.data); a.y = static_cast<const uint16_t *>(y.data);
@@ -530,7 +734,24 @@ ProductArgs product(const HeadOperand &x, const HeadOperand &y) {
 
 }  // namespace
 
-uint32_t head_vocab_tile(uint32_t) { return TILE; }
+HeadTiles head_tiles(uint64_t rows) {
+  switch (shape_for(rows)) {
+    case SMALL: return {Small::BX, Small::BY};
+    case MEDIUM: return {Medium::BX, Medium::BY};
+    default: return {Large::BX, Large::BY};
+  }
+}
+
+uint32_t head_splits(uint64_t rows, uint64_t dim, uint64_t piece) {
+  const Shape shape = shape_for(rows);
+  const HeadTiles t = head_tiles(rows);
+  const uint64_t tiles = (dim + t.vocab - 1) / t.vocab * ((rows + t.rows - 1) / t.rows);
+  const uint64_t wanted = shape == SMALL ? 768 : shape == MEDIUM ? 512 : 256;
+  uint64_t splits = (wanted + tiles - 1) / tiles;
+  const uint64_t most = (piece + 511) / 512;
+  if (splits > most) splits = most;
+  return static_cast<uint32_t>(splits ? splits : 1);
+}
 
 hipError_t launch_head_rows(const HeadRows &r, void *compact, uint32_t padded_rows, uint32_t padded_dim, hipStream_t s) {
   hipLaunchKernelGGL(eco_head_rows_kernel, dim3(1), dim3(1024), 0, s, r);
@@ -555,8 +776,7 @@ hipError_t launch_head_stats(const HeadOperand &w, const HeadOperand &h, uint32_
   a.scale2 = a.two ? LOG2E : LOG2E * inv_tau;
   a.scale2_tau = LOG2E * inv_tau;
   a.out_f32 = st.max; a.sum = st.sum; a.sum_tau = st.sum_tau; a.tiles = st.tiles; a.tile0 = tile;
-  hipLaunchKernelGGL(eco_head_product_kernel<STATS>, dim3((n + TILE - 1) / TILE, (rows + TILE - 1) / TILE), dim3(256), 0, s, a);
-  return hipGetLastError();
+  return launch_product<STATS>(a, rows, n, rows, s);
 }
 
 hipError_t launch_head_finish(const HeadRows &r, const HeadWeights &w, const HeadStats &st, float *ce, float *kd, float *lse, float *lse_tau, float *picked,
@@ -577,8 +797,7 @@ hipError_t launch_head_grad(const HeadOperand &w, const HeadOperand &h, uint32_t
   a.nx = n; a.k = dim; a.count = count; a.two = two;
   a.scale2 = LOG2E; a.scale2_tau = LOG2E * inv_tau;
   a.consts = consts; a.out = g; a.out_ld = g_ld; a.out_plane = g_plane; a.out_planes = g_planes;
-  hipLaunchKernelGGL(eco_head_product_kernel<GRAD>, dim3((n + TILE - 1) / TILE, (rows + TILE - 1) / TILE), dim3(256), 0, s, a);
-  return hipGetLastError();
+  return launch_product<GRAD>(a, rows, n, rows, s);
 }
 
 hipError_t launch_head_scatter(const int32_t *ids, const float *values, uint32_t rows, uint32_t entries, const int32_t *count, uint64_t first, uint32_t n, void *g,
@@ -593,8 +812,7 @@ hipError_t launch_head_grad_hidden(const HeadOperand &w, const HeadOperand &g, u
   ProductArgs a = product(w, g);
   a.nx = dim; a.k = n; a.count = count; a.splits = splits;
   a.out_f32 = partial; a.out_ld = partial_ld; a.out_plane = partial_stride; a.add = add;
-  hipLaunchKernelGGL(eco_head_product_kernel<DH>, dim3((dim + TILE - 1) / TILE, (rows + TILE - 1) / TILE, splits), dim3(256), 0, s, a);
-  return hipGetLastError();
+  return launch_product<DH>(a, rows, dim, rows, s);
 }
 
 hipError_t launch_head_grad_hidden_finish(const float *partial, uint32_t splits, uint32_t partial_ld, uint64_t partial_stride, const HeadRows &r, void *out,
@@ -604,13 +822,12 @@ hipError_t launch_head_grad_hidden_finish(const float *partial, uint32_t splits,
   return hipGetLastError();
 }
 
-hipError_t launch_head_grad_weights(const HeadOperand &h, const HeadOperand &g, uint32_t n, uint32_t dim, const int32_t *count, void *out, uint64_t out_stride,
+hipError_t launch_head_grad_weights(const HeadOperand &h, const HeadOperand &g, uint32_t n, uint32_t rows, uint32_t dim, const int32_t *count, void *out, uint64_t out_stride,
                                     int out_bf16, hipStream_t s) {
   ProductArgs a = product(h, g);
   a.nx = dim; a.ny = n; a.count = count;
   a.out = out; a.out_ld = out_stride; a.out_bf16 = out_bf16;
-  hipLaunchKernelGGL(eco_head_product_kernel<DW>, dim3((dim + TILE - 1) / TILE, (n + TILE - 1) / TILE), dim3(256), 0, s, a);
-  return hipGetLastError();
+  return rows <= 1024 ? launch_tiles<DW, Medium>(a, dim, n, s) : launch_tiles<DW, Large>(a, dim, n, s);
 }
 
 }  // namespace eco
