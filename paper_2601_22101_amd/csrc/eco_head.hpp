@@ -8,7 +8,7 @@ namespace eco {
 
 constexpr uint64_t HEAD_MOST_ROWS = 1ull << 23, HEAD_MOST_VOCAB = 1ull << 24, HEAD_MOST_DIM = 1ull << 16;
 constexpr uint32_t HEAD_MOST_TOP_K = 1024;
-constexpr uint32_t HEAD_K_STEP = 32;              // the products go over their inner axis in steps of 32
+constexpr uint32_t HEAD_K_STEP = 64;              // the products go over their inner axis in steps of 64
 
 constexpr uint64_t head_round_up(uint64_t x, uint64_t k) { return (x + k - 1) / k * k; }
 

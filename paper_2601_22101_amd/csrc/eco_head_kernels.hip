@@ -156,7 +156,7 @@ struct ProductArgs {
   float *out_f32;
   void *out;
   uint64_t out_ld, out_plane;
-  uint32_t out_planes, tiles, tile0, splits, tiles_x, tiles_y;
+  uint32_t out_planes, tiles, tile0, splits, tiles_x;
   int32_t two, out_bf16, add;
   float *sum, *sum_tau;
   const HeadRowConst *consts;
@@ -173,16 +173,23 @@ template <int LEFT>
 __device__ __forceinline__ void wait_loads() {
   asm volatile("s_waitcnt vmcnt(%0)" ::"n"(LEFT) : "memory");
 }
+template <int LEFT>
+__device__ __forceinline__ void wait_all_but() {               // the reads of LDS as well
+  __builtin_amdgcn_sched_barrier(0);
+  asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(LEFT) : "memory");
+}
 __device__ __forceinline__ void barrier() {
   __builtin_amdgcn_sched_barrier(0);
   asm volatile("s_barrier" ::: "memory");
   __builtin_amdgcn_sched_barrier(0);
 }
 
-// A tile of BX x BY by WX x WY waves of 32 x 32 blocks.  The inner axis goes by in steps of 32 through DEPTH places in LDS: while
-// one step is multiplied, the next one is there and DEPTH - 2 are under way.
+// A tile of BX x BY by WX x WY waves of 32 x 32 blocks.  The inner axis goes by in steps of 64, 128 bytes of a row: a whole line of
+// memory, half of which took the caches as long (256 x 256 tiles of 8192 x 1152 x 262144, losses: 4.46 ms in steps of 32).  There are DEPTH places
+// for steps in LDS.
 template <int BX_, int BY_, int WX_, int WY_, int DEPTH_>
 struct Tile {
+  static_assert(KSTEP == 64, "row_piece and fragment go by rows of 128 bytes");
   static constexpr int BX = BX_, BY = BY_, WX = WX_, WY = WY_, DEPTH = DEPTH_;
   static constexpr int THREADS = WX * WY * 64, NI = BX / WX / 32, NJ = BY / WY / 32;
   static constexpr int X_BYTES = BX * KSTEP * 2, Y_BYTES = BY * KSTEP * 2, STEP_BYTES = X_BYTES + Y_BYTES;
@@ -190,13 +197,14 @@ struct Tile {
   static_assert(X_LOADS * THREADS * 16 == X_BYTES && Y_LOADS * THREADS * 16 == Y_BYTES, "whole loads");
 };
 
-// Where the 16-byte piece `c` of a step's operand comes from.  A row operand's step is rows of 64 bytes, a column operand's 32 rows of
-// N elements; the pieces of a row are exchanged so that the lanes which read together find theirs in different banks.
+// Where the 16-byte piece `c` of a step's operand comes from.  A row operand's step is rows of 128 bytes, a column operand's 64 rows of
+// N elements; the pieces of a row are exchanged so that lanes which read together, sixteen of 16 bytes or half a wave of 8, find theirs in
+// different ones of the 64 banks.
 __device__ __forceinline__ void row_piece(uint32_t c, uint32_t &n, uint32_t &k) {
-  n = c >> 2;
-  k = 8 * ((c & 3) ^ ((n >> 1) & 3));
+  n = c >> 3;
+  k = 8 * ((c & 7) ^ ((n >> 1) & 7));
 }
-__device__ __forceinline__ constexpr uint32_t column_swap(uint32_t k) { return 2 * ((k & 3) | ((k >> 3) & 1) << 2); }
+__device__ __forceinline__ constexpr uint32_t column_swap(uint32_t k) { return 4 * (k & 3) | 2 * ((k >> 3) & 1); }
 template <int N>
 __device__ __forceinline__ void column_piece(uint32_t c, uint32_t &n, uint32_t &k) {
   static_assert(N >= 128, "column_swap exchanges 16 pieces");
@@ -207,7 +215,7 @@ __device__ __forceinline__ void column_piece(uint32_t c, uint32_t &n, uint32_t &
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) char lds_char;
 
-// The matrix core's operand for 32 rows of an operand from row n0 on, half `kk` of a step.
+// The matrix core's operand for 32 rows of an operand from row n0 on, quarter `kk` of a step.
 template <int N, bool COLUMN>
 __device__ __forceinline__ bf16x8 fragment(const lds_char *step, int n0, int kk, int lane) {
   if constexpr (COLUMN) {
@@ -219,7 +227,7 @@ __device__ __forceinline__ bf16x8 fragment(const lds_char *step, int n0, int kk,
     return __builtin_bit_cast(bf16x8, v);
   } else {
     const int n = n0 + (lane & 31), piece = 2 * kk + (lane >> 5);
-    return *(const __attribute__((address_space(3))) bf16x8 *)(step + n * (KSTEP * 2) + 16 * (piece ^ ((n >> 1) & 3)));
+    return *(const __attribute__((address_space(3))) bf16x8 *)(step + n * (KSTEP * 2) + 16 * (piece ^ ((n >> 1) & 7)));
   }
 }
 
@@ -237,17 +245,19 @@ __global__ __launch_bounds__(T::THREADS) void eco_head_product_kernel(ProductArg
   __shared__ __attribute__((aligned(1024))) char smem[T::DEPTH * T::STEP_BYTES];
   const uint32_t count = static_cast<uint32_t>(*a.count);
   const uint32_t ny = MODE == DW ? a.ny : count;
-  uint32_t tile = xcd_run(blockIdx.x, gridDim.x), split = 0, tx, ty;
+  // the grid is made for all rows: the tiles that there are, evenly over the XCDs
+  const uint32_t tiles_y = (ny + T::BY - 1) / T::BY, all_tiles = a.tiles_x * tiles_y * a.splits;
+  if (blockIdx.x >= all_tiles) return;
+  uint32_t tile = xcd_run(blockIdx.x, all_tiles), split = 0, tx, ty;
   if (MODE == STATS || MODE == GRAD) {
     // eight tiles of rows beside each other, then the next of the vocabulary
-    const uint32_t run = 8 * a.tiles_x, band = tile / run, high = min(8u, a.tiles_y - band * 8), in = tile - band * run;
+    const uint32_t run = 8 * a.tiles_x, band = tile / run, high = min(8u, tiles_y - band * 8), in = tile - band * run;
     tx = in / high; ty = band * 8 + in % high;
   } else {
-    if (MODE == DH) { split = tile / (a.tiles_x * a.tiles_y); tile -= split * a.tiles_x * a.tiles_y; }
+    if (MODE == DH) { split = tile / (a.tiles_x * tiles_y); tile -= split * a.tiles_x * tiles_y; }
     ty = tile / a.tiles_x; tx = tile % a.tiles_x;
   }
   const uint32_t x0 = tx * T::BX, y0 = ty * T::BY;
-  if (y0 >= ny) return;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wx = wave % T::WX * (NI * 32), wy = wave / T::WX * (NJ * 32);
   const uint32_t all_steps = MODE == DW ? (count + KSTEP - 1) / KSTEP : (a.k + KSTEP - 1) / KSTEP;
@@ -325,45 +335,49 @@ __global__ __launch_bounds__(T::THREADS) void eco_head_product_kernel(ProductArg
 
   f32x16 acc[NI][NJ] = {};
   if (total) {
-    bf16x8 ax[NI], ay[NJ], bx[NI], by[NJ];
-    for (int i = 0; i < T::DEPTH - 1; ++i)
+    constexpr int QUARTERS = KSTEP / 16;
+    bf16x8 fx[2][NI], fy[2][NJ];                               // the quarter at hand and the next one
+    const auto read = [&](const lds_char *step, int kk, bf16x8 (&x)[NI], bf16x8 (&y)[NJ]) {
+#pragma unroll
+      for (int j = 0; j < NJ; ++j) y[j] = fragment<T::BY, Y_COLUMN>(step + T::X_BYTES, wy + 32 * j, kk, lane);
+#pragma unroll
+      for (int i = 0; i < NI; ++i) x[i] = fragment<T::BX, X_COLUMN>(step, wx + 32 * i, kk, lane);
+    };
+    for (int i = 0; i < T::DEPTH; ++i)
       if (issued < total) issue();
-    if (total >= T::DEPTH - 1) wait_loads<(T::DEPTH - 2) * T::LOADS>();
+    if (total >= T::DEPTH) wait_loads<(T::DEPTH - 1) * T::LOADS>();
     else wait_loads<0>();
     barrier();
     uint32_t at = 0;
     const lds_char *step = (const lds_char *)smem;
-#pragma unroll
-    for (int i = 0; i < NI; ++i) ax[i] = fragment<T::BX, X_COLUMN>(step, wx + 32 * i, 0, lane);
-#pragma unroll
-    for (int j = 0; j < NJ; ++j) ay[j] = fragment<T::BY, Y_COLUMN>(step + T::X_BYTES, wy + 32 * j, 0, lane);
+    read(step, 0, fx[0], fy[0]);
     for (uint32_t s = 0; s < total; ++s) {
 #pragma unroll
-      for (int i = 0; i < NI; ++i) bx[i] = fragment<T::BX, X_COLUMN>(step, wx + 32 * i, 1, lane);
+      for (int kk = 0; kk < QUARTERS - 1; ++kk) {
+        read(step, kk + 1, fx[(kk + 1) & 1], fy[(kk + 1) & 1]);
 #pragma unroll
-      for (int j = 0; j < NJ; ++j) by[j] = fragment<T::BY, Y_COLUMN>(step + T::X_BYTES, wy + 32 * j, 1, lane);
+        for (int i = 0; i < NI; ++i)
 #pragma unroll
-      for (int i = 0; i < NI; ++i)
-#pragma unroll
-        for (int j = 0; j < NJ; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ax[i], ay[j], acc[i][j], 0, 0, 0);
-      // the next step is there once every wave's loads of it are; the place of the step before this one is free once every
-      // wave has multiplied it
-      if (s + T::DEPTH - 2 < total) wait_loads<(T::DEPTH - 3) * T::LOADS>();
-      else wait_loads<0>();
+          for (int j = 0; j < NJ; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fx[kk & 1][i], fy[kk & 1][j], acc[i][j], 0, 0, 0);
+      }
+      // the next step is there once every wave's loads of it are, and this one's place is free once every wave has read it
+      if (s + T::DEPTH <= total) wait_all_but<(T::DEPTH - 2) * T::LOADS>();
+      else wait_all_but<0>();
       barrier();
-      if (issued < total) issue();
       at = at + 1 == T::DEPTH ? 0 : at + 1;
       step = (const lds_char *)smem + at * T::STEP_BYTES;
-      if (s + 1 < total) {
+      read(step, 0, fx[0], fy[0]);                             // (after the last step nothing uses these: a branch would make the products wait)
 #pragma unroll
-        for (int i = 0; i < NI; ++i) ax[i] = fragment<T::BX, X_COLUMN>(step, wx + 32 * i, 0, lane);
+      for (int i = 0; i < NI; ++i) {
 #pragma unroll
-        for (int j = 0; j < NJ; ++j) ay[j] = fragment<T::BY, Y_COLUMN>(step + T::X_BYTES, wy + 32 * j, 0, lane);
+        for (int j = 0; j < NJ; ++j)
+          acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fx[(QUARTERS - 1) & 1][i], fy[(QUARTERS - 1) & 1][j], acc[i][j], 0, 0, 0);
+        if (i == 0) {
+          __builtin_amdgcn_sched_barrier(0);
+          if (issued < total) issue();
+          __builtin_amdgcn_sched_barrier(0);
+        }
       }
-#pragma unroll
-      for (int i = 0; i < NI; ++i)
-#pragma unroll
-        for (int j = 0; j < NJ; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(bx[i], by[j], acc[i][j], 0, 0, 0);
     }
   }
 
@@ -702,17 +716,16 @@ __global__ __launch_bounds__(256) void eco_head_grad_hidden_finish_kernel(const 
 uint32_t blocks_for(uint64_t work) { return static_cast<uint32_t>(work < 256 * 8192 ? (work + 255) / 256 : 8192); }
 
 // Tiles by the number of rows.
-using Large = Tile<256, 256, 2, 4, 4>;
+using Large = Tile<256, 256, 2, 4, 2>;
 using Medium = Tile<256, 128, 4, 2, 3>;
-using Small = Tile<128, 64, 4, 1, 4>;
+using Small = Tile<128, 64, 4, 1, 3>;
 enum Shape { SMALL, MEDIUM, LARGE };
 Shape shape_for(uint64_t rows) { return rows <= 64 ? SMALL : rows <= 1024 ? MEDIUM : LARGE; }
 
 template <int MODE, class T>
 hipError_t launch_tiles(ProductArgs a, uint32_t x, uint32_t y, hipStream_t s) {
   a.tiles_x = (x + T::BX - 1) / T::BX;
-  a.tiles_y = (y + T::BY - 1) / T::BY;
-  hipLaunchKernelGGL((eco_head_product_kernel<MODE, T>), dim3(a.tiles_x * a.tiles_y * a.splits), dim3(T::THREADS), 0, s, a);
+  hipLaunchKernelGGL((eco_head_product_kernel<MODE, T>), dim3(a.tiles_x * ((y + T::BY - 1) / T::BY) * a.splits), dim3(T::THREADS), 0, s, a);
   return hipGetLastError();
 }
 template <int MODE>
