@@ -231,6 +231,40 @@ __device__ __forceinline__ bf16x8 fragment(const lds_char *step, int n0, int kk,
   }
 }
 
+// A wave's results on their way out: 32 rows y of its NI * 32 columns x pass through its own part of LDS, so that whole lines are
+// stored; the registers hold four columns of a row, and storing those took the 8192 x 256 tiles of the logits' gradient 1.4 times as long as their
+// product.  16-byte pieces of a row are exchanged by row, against bank conflicts.  A wave's own reads and writes of LDS are in order.
+template <int NI>
+__device__ __forceinline__ void put_bf16(lds_char *own, int lane, int i, int q, uint32_t lo, uint32_t hi) {
+  constexpr int PIECES = NI * 4;
+  const int row = lane & 31;
+  *(__attribute__((address_space(3))) uint64_t *)(own + row * PIECES * 16 + 16 * ((4 * i + q) ^ (row & (PIECES - 1))) + 8 * (lane >> 5)) =
+      static_cast<uint64_t>(hi) << 32 | lo;
+}
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+template <int NI, int NJ>
+__device__ __forceinline__ void put_f32(lds_char *own, int lane, const f32x16 (&acc)[NI][NJ], int j) {
+  constexpr int PIECES = NI * 8;
+  const int row = lane & 31;
+#pragma unroll
+  for (int i = 0; i < NI; ++i)
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      const f32x4 v = {acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]};
+      *(__attribute__((address_space(3))) f32x4 *)(own + row * PIECES * 16 + 16 * ((8 * i + 2 * q + (lane >> 5)) ^ (row & (PIECES - 1)))) = v;
+    }
+}
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+template <int PIECES, class F>
+__device__ __forceinline__ void take(const lds_char *own, int lane, F store) {
+#pragma unroll
+  for (int t = 0; t < 32 * PIECES / 64; ++t) {
+    const int at = t * 64 + lane, row = at / PIECES, piece = at % PIECES;
+    const u32x4 v = *(const __attribute__((address_space(3))) u32x4 *)(own + row * PIECES * 16 + 16 * (piece ^ (row & (PIECES - 1))));
+    store(row, piece, make_uint4(v.x, v.y, v.z, v.w));
+  }
+}
+
 // The tile of the workgroup: the hardware hands workgroups to the eight XCDs in turn, so each XCD takes a run of neighbouring tiles,
 // whose operands its L2 then holds once.
 __device__ __forceinline__ uint32_t xcd_run(uint32_t id, uint32_t all) {
@@ -447,81 +481,98 @@ __global__ __launch_bounds__(T::THREADS) void eco_head_product_kernel(ProductArg
       store(a.sum_tau, s);
     }
   }
-  if constexpr (MODE == GRAD) {
+  if constexpr (MODE != STATS) {
+    barrier();                                                 // every wave has read its operands: LDS is free
+    lds_char *const own = (lds_char *)smem + wave * (32 * NI * 32 * 4);
+    if constexpr (MODE == GRAD) {
+      uint16_t *const out = static_cast<uint16_t *>(a.out);
 #pragma unroll
-    for (int j = 0; j < NJ; ++j) {
-      const uint32_t y = y0 + wy + 32 * j + (lane & 31);
-      const HeadRowConst rc = a.consts[y];
-      uint16_t *out = static_cast<uint16_t *>(a.out) + static_cast<uint64_t>(y) * a.out_ld;
-#pragma unroll
-      for (int i = 0; i < NI; ++i)
-#pragma unroll
-        for (int q = 0; q < 4; ++q) {
-          const uint32_t x = x_of(i, 4 * q);
-          float g[4];
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const float z = acc[i][j][4 * q + e];
-            g[e] = 0.0f;
-            if (a.two != 2) g[e] = rc.a * exp2_fast(fmaf(z, a.scale2, -rc.lse2));
-            if (a.two) g[e] = fmaf(rc.b, exp2_fast(fmaf(z, a.scale2_tau, -rc.lse2_tau)), g[e]);
-            if (x + e >= a.nx || y >= ny) g[e] = 0.0f;
-          }
-          for (uint32_t p = 0; p < a.out_planes; ++p) {
-            uint32_t b[4];
-#pragma unroll
-            for (int e = 0; e < 4; ++e) next_plane(g[e], b[e]);
-            *reinterpret_cast<uint2 *>(out + p * a.out_plane + x) = make_uint2(b[0] | b[1] << 16, b[2] | b[3] << 16);
-          }
-        }
-    }
-  }
-  if constexpr (MODE == DH) {
-#pragma unroll
-    for (int j = 0; j < NJ; ++j) {
-      const uint32_t y = y0 + wy + 32 * j + (lane & 31);
-      float *out = a.out_f32 + split * a.out_plane + static_cast<uint64_t>(y) * a.out_ld;
-      if (y < ny)
+      for (int j = 0; j < NJ; ++j) {
+        const uint32_t y = y0 + wy + 32 * j + (lane & 31);
+        const HeadRowConst rc = a.consts[y];
 #pragma unroll
         for (int i = 0; i < NI; ++i)
 #pragma unroll
-          for (int q = 0; q < 4; ++q) {
-            const uint32_t x = x_of(i, 4 * q);
-            if (x >= a.out_ld) continue;          // whole fours: out_ld is the padded dimension
-            float4 v = make_float4(acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]);
-            float4 *to = reinterpret_cast<float4 *>(out + x);
-            if (a.add) { const float4 o = *to; v.x += o.x; v.y += o.y; v.z += o.z; v.w += o.w; }
-            *to = v;
+          for (int r = 0; r < 16; ++r) {
+            const float z = acc[i][j][r];
+            float g = 0.0f;
+            if (a.two != 2) g = rc.a * exp2_fast(fmaf(z, a.scale2, -rc.lse2));
+            if (a.two) g = fmaf(rc.b, exp2_fast(fmaf(z, a.scale2_tau, -rc.lse2_tau)), g);
+            acc[i][j][r] = x_of(i, r) < a.nx && y < ny ? g : 0.0f;
           }
-    }
-  }
-  if constexpr (MODE == DW) {
+        for (uint32_t p = 0; p < a.out_planes; ++p) {
 #pragma unroll
-    for (int j = 0; j < NJ; ++j) {
-      const uint32_t y = y0 + wy + 32 * j + (lane & 31);
-      if (y >= ny) continue;
-      const uint64_t row = static_cast<uint64_t>(y) * a.out_ld;
+          for (int i = 0; i < NI; ++i)
 #pragma unroll
-      for (int i = 0; i < NI; ++i)
+            for (int q = 0; q < 4; ++q) {
+              uint32_t b[4];
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
-          const uint32_t x = x_of(i, 4 * q);
-          if (x + 4 <= a.nx && a.out_ld % 4 == 0) {
-            if (a.out_bf16)
-              *reinterpret_cast<uint2 *>(static_cast<uint16_t *>(a.out) + row + x) =
-                  make_uint2(f32x2_to_bf16x2_rne(acc[i][j][4 * q], acc[i][j][4 * q + 1]), f32x2_to_bf16x2_rne(acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]));
-            else
-              *reinterpret_cast<float4 *>(static_cast<float *>(a.out) + row + x) =
-                  make_float4(acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]);
-          } else {
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-              if (x + e < a.nx) {
-                if (a.out_bf16) static_cast<uint16_t *>(a.out)[row + x + e] = static_cast<uint16_t>(f32x2_to_bf16x2_rne(acc[i][j][4 * q + e], 0.0f));
-                else static_cast<float *>(a.out)[row + x + e] = acc[i][j][4 * q + e];
-              }
-          }
+              for (int e = 0; e < 4; ++e) { float rest = acc[i][j][4 * q + e]; next_plane(rest, b[e]); acc[i][j][4 * q + e] = rest; }
+              put_bf16<NI>(own, lane, i, q, b[0] | b[1] << 16, b[2] | b[3] << 16);
+            }
+          // (columns and rows of the padded piece: nothing to check)
+          take<NI * 4>(own, lane, [&](uint32_t row, uint32_t piece, uint4 v) {
+            *reinterpret_cast<uint4 *>(out + p * a.out_plane + static_cast<uint64_t>(y0 + wy + 32 * j + row) * a.out_ld + x0 + wx + 8 * piece) = v;
+          });
         }
+      }
+    }
+    if constexpr (MODE == DH) {
+      float *const out = a.out_f32 + split * a.out_plane;
+#pragma unroll
+      for (int j = 0; j < NJ; ++j) {
+        put_f32<NI>(own, lane, acc, j);
+        take<NI * 8>(own, lane, [&](uint32_t row, uint32_t piece, uint4 v) {
+          const uint32_t y = y0 + wy + 32 * j + row, x = x0 + wx + 4 * piece;
+          if (y >= ny || x >= a.out_ld) return;                // whole fours: out_ld is the padded dimension
+          float4 *to = reinterpret_cast<float4 *>(out + static_cast<uint64_t>(y) * a.out_ld + x), f = __builtin_bit_cast(float4, v);
+          if (a.add) { const float4 o = *to; f.x += o.x; f.y += o.y; f.z += o.z; f.w += o.w; }
+          *to = f;
+        });
+      }
+    }
+    if constexpr (MODE == DW) {
+      if (a.out_bf16) {
+        uint16_t *const out = static_cast<uint16_t *>(a.out);
+        const bool whole = a.out_ld % 8 == 0;
+#pragma unroll
+        for (int j = 0; j < NJ; ++j) {
+#pragma unroll
+          for (int i = 0; i < NI; ++i)
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
+              put_bf16<NI>(own, lane, i, q, f32x2_to_bf16x2_rne(acc[i][j][4 * q], acc[i][j][4 * q + 1]), f32x2_to_bf16x2_rne(acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]));
+          take<NI * 4>(own, lane, [&](uint32_t row, uint32_t piece, uint4 v) {
+            const uint32_t y = y0 + wy + 32 * j + row, x = x0 + wx + 8 * piece;
+            if (y >= ny || x >= a.nx) return;
+            uint16_t *to = out + static_cast<uint64_t>(y) * a.out_ld + x;
+            const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+            if (whole && x + 8 <= a.nx) *reinterpret_cast<uint4 *>(to) = v;
+            else
+#pragma unroll
+              for (int e = 0; e < 8; ++e)
+                if (x + e < a.nx) to[e] = static_cast<uint16_t>(w[e / 2] >> (16 * (e & 1)));
+          });
+        }
+      } else {
+        float *const out = static_cast<float *>(a.out);
+        const bool whole = a.out_ld % 4 == 0;
+#pragma unroll
+        for (int j = 0; j < NJ; ++j) {
+          put_f32<NI>(own, lane, acc, j);
+          take<NI * 8>(own, lane, [&](uint32_t row, uint32_t piece, uint4 v) {
+            const uint32_t y = y0 + wy + 32 * j + row, x = x0 + wx + 4 * piece;
+            if (y >= ny || x >= a.nx) return;
+            float *to = out + static_cast<uint64_t>(y) * a.out_ld + x;
+            const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+            if (whole && x + 4 <= a.nx) *reinterpret_cast<uint4 *>(to) = v;
+            else
+#pragma unroll
+              for (int e = 0; e < 4; ++e)
+                if (x + e < a.nx) to[e] = u2f(w[e]);
+          });
+        }
+      }
     }
   }
 }
