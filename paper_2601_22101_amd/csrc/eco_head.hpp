@@ -58,13 +58,16 @@ hipError_t launch_head_stats(const HeadOperand &w, const HeadOperand &h, uint32_
 hipError_t launch_head_finish(const HeadRows &, const HeadWeights &, const HeadStats &, float *ce, float *kd, float *lse, float *lse_tau, float *picked,
                               hipStream_t);
 
-struct HeadRowConst { float lse2, a, lse2_tau, b; };      // of a compact row: log2(e) lse, dL/dce, log2(e) lse_tau, tau dL/dkd
+// Which softmaxes the logits' gradient is made of: the labels', both, the teacher's, or both where a temperature of 1 makes them the same.
+enum : int { HEAD_LABELS = 0, HEAD_BOTH = 1, HEAD_TEACHER = 2, HEAD_SAME = 3 };
+// of a compact row: log2(e) lse, dL/dce, log2(e) lse_tau, tau dL/dkd; where there is but one softmax, its own first
+struct HeadRowConst { float lse2, a, lse2_tau, b; };
 
 // entries: ids [rows][top_k + 1] (-1: none) and the gradient of the logit at each, over compact rows; consts: the padded rows
 hipError_t launch_head_entries(const HeadRows &, uint32_t padded_rows, const float *grad_ce, const float *grad_kd, const float *lse, const float *lse_tau,
-                               const float *picked, int merged, int32_t *ids, float *values, HeadRowConst *consts, hipStream_t);
+                               const float *picked, int softmaxes, int32_t *ids, float *values, HeadRowConst *consts, hipStream_t);
 // g[row][v] of a piece: planes of [padded rows][ld]
-hipError_t launch_head_grad(const HeadOperand &w, const HeadOperand &h, uint32_t n, uint32_t rows, uint32_t dim, const int32_t *count, float inv_tau, int two,
+hipError_t launch_head_grad(const HeadOperand &w, const HeadOperand &h, uint32_t n, uint32_t rows, uint32_t dim, const int32_t *count, float inv_tau, int softmaxes,
                             const HeadRowConst *, void *g, uint32_t g_ld, uint64_t g_plane, uint32_t g_planes, hipStream_t);
 hipError_t launch_head_scatter(const int32_t *ids, const float *values, uint32_t rows, uint32_t entries, const int32_t *count, uint64_t first, uint32_t n, void *g,
                                uint32_t g_ld, uint64_t g_plane, uint32_t g_planes, hipStream_t);
@@ -77,6 +80,7 @@ hipError_t launch_head_grad_weights(const HeadOperand &h, const HeadOperand &g, 
                                     int out_bf16, hipStream_t);
 struct HeadTiles { uint32_t vocab, rows; };       // a tile of the logits
 HeadTiles head_tiles(uint64_t rows);
+uint64_t head_piece(uint64_t rows, uint64_t dim, uint64_t vocab, uint64_t most);          // vocabulary to a piece of the backward pass
 uint32_t head_splits(uint64_t rows, uint64_t dim, uint64_t piece);      // parts of a piece of the vocabulary that grad_hidden's product sums apart
 
 }  // namespace eco

@@ -144,7 +144,8 @@ __global__ __launch_bounds__(256) void eco_head_convert_kernel(HeadWeights w, ui
 //   DW     x hidden dimension, y vocabulary, k rows: the gradient of the weights
 // With x along a lane's registers, four neighbours in each group, a row's softmax is a reduction over registers and every end stores
 // neighbours together.
-enum : int { STATS = 0, GRAD = 1, DH = 2, DW = 3 };
+// GRAD_PLANES is GRAD with g in several planes.
+enum : int { STATS = 0, GRAD = 1, DH = 2, DW = 3, GRAD_PLANES = 4 };
 
 struct ProductArgs {
   const uint16_t *x, *y;
@@ -283,7 +284,7 @@ __global__ __launch_bounds__(T::THREADS) void eco_head_product_kernel(ProductArg
   const uint32_t tiles_y = (ny + T::BY - 1) / T::BY, all_tiles = a.tiles_x * tiles_y * a.splits;
   if (blockIdx.x >= all_tiles) return;
   uint32_t tile = xcd_run(blockIdx.x, all_tiles), split = 0, tx, ty;
-  if (MODE == STATS || MODE == GRAD) {
+  if (MODE == STATS || MODE == GRAD || MODE == GRAD_PLANES) {
     // eight tiles of rows beside each other, then the next of the vocabulary
     const uint32_t run = 8 * a.tiles_x, band = tile / run, high = min(8u, tiles_y - band * 8), in = tile - band * run;
     tx = in / high; ty = band * 8 + in % high;
@@ -484,37 +485,50 @@ __global__ __launch_bounds__(T::THREADS) void eco_head_product_kernel(ProductArg
   if constexpr (MODE != STATS) {
     barrier();                                                 // every wave has read its operands: LDS is free
     lds_char *const own = (lds_char *)smem + wave * (32 * NI * 32 * 4);
-    if constexpr (MODE == GRAD) {
+    if constexpr (MODE == GRAD || MODE == GRAD_PLANES) {
       uint16_t *const out = static_cast<uint16_t *>(a.out);
+      const bool edge = x0 + T::BX > a.nx;
 #pragma unroll
       for (int j = 0; j < NJ; ++j) {
-        const uint32_t y = y0 + wy + 32 * j + (lane & 31);
-        const HeadRowConst rc = a.consts[y];
+        // (rows past the last one that takes part have a = b = 0)
+        const HeadRowConst rc = a.consts[y0 + wy + 32 * j + (lane & 31)];
 #pragma unroll
-        for (int i = 0; i < NI; ++i)
+        for (int i = 0; i < NI; ++i) {
+          if (a.two == 1) {
 #pragma unroll
-          for (int r = 0; r < 16; ++r) {
-            const float z = acc[i][j][r];
-            float g = 0.0f;
-            if (a.two != 2) g = rc.a * exp2_fast(fmaf(z, a.scale2, -rc.lse2));
-            if (a.two) g = fmaf(rc.b, exp2_fast(fmaf(z, a.scale2_tau, -rc.lse2_tau)), g);
-            acc[i][j][r] = x_of(i, r) < a.nx && y < ny ? g : 0.0f;
+            for (int r = 0; r < 16; ++r)
+              acc[i][j][r] = fmaf(rc.b, exp2_fast(fmaf(acc[i][j][r], a.scale2_tau, -rc.lse2_tau)), rc.a * exp2_fast(fmaf(acc[i][j][r], a.scale2, -rc.lse2)));
+          } else {
+#pragma unroll
+            for (int r = 0; r < 16; ++r) acc[i][j][r] = rc.a * exp2_fast(fmaf(acc[i][j][r], a.scale2, -rc.lse2));
           }
-        for (uint32_t p = 0; p < a.out_planes; ++p) {
+          if (edge)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) acc[i][j][r] = x_of(i, r) < a.nx ? acc[i][j][r] : 0.0f;
+        }
+        const auto put_and_take = [&](uint32_t p, auto two_of) {
 #pragma unroll
           for (int i = 0; i < NI; ++i)
 #pragma unroll
-            for (int q = 0; q < 4; ++q) {
-              uint32_t b[4];
-#pragma unroll
-              for (int e = 0; e < 4; ++e) { float rest = acc[i][j][4 * q + e]; next_plane(rest, b[e]); acc[i][j][4 * q + e] = rest; }
-              put_bf16<NI>(own, lane, i, q, b[0] | b[1] << 16, b[2] | b[3] << 16);
-            }
+            for (int q = 0; q < 4; ++q) put_bf16<NI>(own, lane, i, q, two_of(i, 4 * q), two_of(i, 4 * q + 2));
           // (columns and rows of the padded piece: nothing to check)
           take<NI * 4>(own, lane, [&](uint32_t row, uint32_t piece, uint4 v) {
             *reinterpret_cast<uint4 *>(out + p * a.out_plane + static_cast<uint64_t>(y0 + wy + 32 * j + row) * a.out_ld + x0 + wx + 8 * piece) = v;
           });
-        }
+        };
+        if constexpr (MODE == GRAD)
+          put_and_take(0, [&](int i, int r) { return f32x2_to_bf16x2_rne(acc[i][j][r], acc[i][j][r + 1]); });
+        else
+          for (uint32_t p = 0; p < a.out_planes; ++p)
+            put_and_take(p, [&](int i, int r) {
+              uint32_t lo, hi;
+              float rest = acc[i][j][r], next = acc[i][j][r + 1];
+              next_plane(rest, lo);
+              next_plane(next, hi);
+              acc[i][j][r] = rest;
+              acc[i][j][r + 1] = next;
+              return lo | hi << 16;
+            });
       }
     }
     if constexpr (MODE == DH) {
@@ -690,7 +704,7 @@ __global__ __launch_bounds__(256) void eco_head_finish_kernel(HeadRows r, HeadWe
 // For each compact row: the constants of its softmax, and the gradient of the logit at the label and at each of the teacher's
 // entries, which replaces what the product's end writes there.  An id that comes up again in its row is left to the first one.
 __global__ __launch_bounds__(64) void eco_head_entries_kernel(HeadRows r, const float *grad_ce, const float *grad_kd, const float *lse, const float *lse_tau,
-                                                              const float *picked, int merged, int32_t *ids, float *values, HeadRowConst *consts) {
+                                                              const float *picked, int softmaxes, int32_t *ids, float *values, HeadRowConst *consts) {
   __shared__ int32_t id_of[HEAD_MOST_TOP_K + 1];
   __shared__ float q_of[HEAD_MOST_TOP_K + 1];
   const uint32_t c = blockIdx.x, entries = r.top_k + 1;
@@ -707,7 +721,10 @@ __global__ __launch_bounds__(64) void eco_head_entries_kernel(HeadRows r, const 
   const bool taught = q.sum != 0.0f;
   const float a = label >= 0 && grad_ce ? grad_ce[row] : 0.0f, b = taught && grad_kd ? grad_kd[row] * r.tau : 0.0f;
   const float l1 = lse ? lse[row] : 0.0f, lt = lse_tau ? lse_tau[row] : 0.0f;
-  if (lane == 0) consts[c] = {l1 * LOG2E, merged ? a + b : a, lt * LOG2E, b};      // at a temperature of 1 the two softmaxes are one
+  if (lane == 0) {
+    if (softmaxes == HEAD_TEACHER) consts[c] = {lt * LOG2E, b, 0.0f, 0.0f};
+    else consts[c] = {l1 * LOG2E, softmaxes == HEAD_SAME ? a + b : a, lt * LOG2E, b};
+  }
   for (uint32_t j = lane; j < entries; j += 64) {
     id_of[j] = j == 0 ? label : taught ? teacher_id(r, row, j - 1) : -1;
     q_of[j] = j == 0 || id_of[j] < 0 ? 0.0f : exp2_fast((teacher_logit(r, row, j - 1) * it - q.max) * LOG2E) / q.sum;
@@ -806,15 +823,48 @@ HeadTiles head_tiles(uint64_t rows) {
   }
 }
 
+// Tiles run a compute unit's worth at a time: what part of the last round is busy.
+constexpr uint64_t UNITS = 256;
+double rounds(uint64_t tiles) { return static_cast<double>((tiles + UNITS - 1) / UNITS); }
+uint64_t ceil_div(uint64_t a, uint64_t b) { return (a + b - 1) / b; }
+
+// The piece of the vocabulary, at most `most`, whose tiles of the logits' gradient and of the weights' gradient take the least time in
+// rounds (with the inner axes' steps, and about eight steps of a tile's own at either end).  Tiles of one compute unit each.
+uint64_t head_piece(uint64_t rows, uint64_t dim, uint64_t vocab, uint64_t most) {
+  if (shape_for(rows) != LARGE) return most;
+  const uint64_t all = ceil_div(vocab, 256), row_tiles = ceil_div(rows, 256), dim_tiles = ceil_div(dim, 256);
+  const uint64_t fewest = ceil_div(all, most / 256);
+  double best = 0.0;
+  uint64_t piece = most;
+  for (uint64_t pieces = fewest; pieces <= 2 * fewest && pieces <= all && pieces < fewest + 64; ++pieces) {
+    const uint64_t tiles = ceil_div(all, pieces), last = all - tiles * (ceil_div(all, tiles) - 1);
+    double cost = 0.0;
+    for (const uint64_t n : {tiles, last})
+      cost += (n == tiles ? static_cast<double>(ceil_div(all, tiles) - 1) : 1.0) *
+              (rounds(n * row_tiles) * (static_cast<double>(dim) / KSTEP + 8) + rounds(n * dim_tiles) * (static_cast<double>(rows) / KSTEP + 8));
+    if (pieces == fewest || cost < 0.99 * best) { best = cost; piece = tiles * 256; }
+  }
+  return piece;
+}
+
+// Parts of a piece of the vocabulary that grad_hidden's product sums apart, so that its tiles fill the compute units; each costs a
+// reading and a writing of its sums.
 uint32_t head_splits(uint64_t rows, uint64_t dim, uint64_t piece) {
   const Shape shape = shape_for(rows);
   const HeadTiles t = head_tiles(rows);
-  const uint64_t tiles = (dim + t.vocab - 1) / t.vocab * ((rows + t.rows - 1) / t.rows);
-  const uint64_t wanted = shape == SMALL ? 768 : shape == MEDIUM ? 512 : 256;
-  uint64_t splits = (wanted + tiles - 1) / tiles;
-  const uint64_t most = (piece + 511) / 512;
-  if (splits > most) splits = most;
-  return static_cast<uint32_t>(splits ? splits : 1);
+  const uint64_t tiles = ceil_div(dim, t.vocab) * ceil_div(rows, t.rows), most = ceil_div(piece, 512);
+  uint64_t splits = 1;
+  if (shape == LARGE) {
+    double best = 0.0;
+    for (uint64_t n = 1; n <= 16 && n <= most; ++n) {
+      const double cost = rounds(tiles * n) * (static_cast<double>(ceil_div(ceil_div(piece, KSTEP), n)) + 12);
+      if (n == 1 || cost < 0.97 * best) { best = cost; splits = n; }
+    }
+  } else {
+    splits = ceil_div(shape == SMALL ? 768 : 512, tiles);
+    if (splits > most) splits = most;
+  }
+  return static_cast<uint32_t>(splits);
 }
 
 hipError_t launch_head_rows(const HeadRows &r, void *compact, uint32_t padded_rows, uint32_t padded_dim, hipStream_t s) {
@@ -850,18 +900,18 @@ hipError_t launch_head_finish(const HeadRows &r, const HeadWeights &w, const Hea
 }
 
 hipError_t launch_head_entries(const HeadRows &r, uint32_t padded_rows, const float *grad_ce, const float *grad_kd, const float *lse, const float *lse_tau,
-                               const float *picked, int merged, int32_t *ids, float *values, HeadRowConst *consts, hipStream_t s) {
-  hipLaunchKernelGGL(eco_head_entries_kernel, dim3(padded_rows), dim3(64), 0, s, r, grad_ce, grad_kd, lse, lse_tau, picked, merged, ids, values, consts);
+                               const float *picked, int softmaxes, int32_t *ids, float *values, HeadRowConst *consts, hipStream_t s) {
+  hipLaunchKernelGGL(eco_head_entries_kernel, dim3(padded_rows), dim3(64), 0, s, r, grad_ce, grad_kd, lse, lse_tau, picked, softmaxes, ids, values, consts);
   return hipGetLastError();
 }
 
-hipError_t launch_head_grad(const HeadOperand &w, const HeadOperand &h, uint32_t n, uint32_t rows, uint32_t dim, const int32_t *count, float inv_tau, int two,
+hipError_t launch_head_grad(const HeadOperand &w, const HeadOperand &h, uint32_t n, uint32_t rows, uint32_t dim, const int32_t *count, float inv_tau, int softmaxes,
                             const HeadRowConst *consts, void *g, uint32_t g_ld, uint64_t g_plane, uint32_t g_planes, hipStream_t s) {
   ProductArgs a = product(w, h);
-  a.nx = n; a.k = dim; a.count = count; a.two = two;
-  a.scale2 = LOG2E; a.scale2_tau = LOG2E * inv_tau;
+  a.nx = n; a.k = dim; a.count = count; a.two = softmaxes == HEAD_BOTH;
+  a.scale2 = softmaxes == HEAD_TEACHER ? LOG2E * inv_tau : LOG2E; a.scale2_tau = LOG2E * inv_tau;
   a.consts = consts; a.out = g; a.out_ld = g_ld; a.out_plane = g_plane; a.out_planes = g_planes;
-  return launch_product<GRAD>(a, rows, n, rows, s);
+  return g_planes == 1 ? launch_product<GRAD>(a, rows, n, rows, s) : launch_product<GRAD_PLANES>(a, rows, n, rows, s);
 }
 
 hipError_t launch_head_scatter(const int32_t *ids, const float *values, uint32_t rows, uint32_t entries, const int32_t *count, uint64_t first, uint32_t n, void *g,
