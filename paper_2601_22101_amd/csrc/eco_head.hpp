@@ -21,7 +21,7 @@ constexpr int head_hidden_planes(int dtype_bf16) { return dtype_bf16 ? 1 : 3; }
 struct HeadWeights {                              // where a row of weights comes from
   const void *data, *scales;
   uint64_t stride, group;                         // elements between rows (unquantized); elements per scale
-  int32_t fmt, scale_bf16;
+  int32_t fmt, scale_bf16, group_shift;           // log2(group), or -1
 };
 
 // The products' operands are bf16 planes.  The inner axis of a "row" operand is contiguous (element (n, k) at n * ld + k), of a
@@ -39,10 +39,11 @@ struct HeadRows {                                 // a forward or backward call'
   const void *top_logits;
   uint64_t hidden_stride, top_stride;
   uint32_t rows, vocab, dim, top_k;
-  int32_t hidden_bf16, top_bf16;
+  int32_t hidden_bf16, top_bf16, hidden_whole;    // hidden_whole: pieces of eight elements of a row are aligned
   float tau;
   // workspace: number of rows that take part, compact row -> row, row -> compact row or -1
   int32_t *count, *order, *place;
+  uint8_t *flags;                                 // which rows take part, where a teacher's entries have to be looked through
 };
 
 struct HeadStats {                                // the logits' statistics by row and tile of the vocabulary

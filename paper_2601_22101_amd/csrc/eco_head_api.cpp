@@ -91,7 +91,7 @@ eco_status_t check_backward(const eco_head_t *h) {
 struct Layout {
   uint32_t padded_rows, padded_dim, entries, piece, hidden_planes, weight_planes, grad_planes, tiles, splits;
   bool in_place, two;
-  uint64_t count, order, place, compact, planes, max, sum, sum_tau, ids, values, consts, g, partial, bytes;
+  uint64_t count, order, place, flags, compact, planes, max, sum, sum_tau, ids, values, consts, g, partial, bytes;
 };
 
 // Bytes that the converted weights and the logits' gradient of a piece of the vocabulary may take each.  Whether the 256 MB cache in front
@@ -130,6 +130,7 @@ Layout layout_of(const eco_head_t *h, bool backward) {
   l.count = take(4);
   l.order = take(4 * h->rows);
   l.place = take(4 * h->rows);
+  l.flags = take(h->top_k ? h->rows : 0);
   l.compact = take(2ull * l.hidden_planes * l.padded_rows * l.padded_dim);
   if (!l.in_place) l.planes = take(2ull * l.weight_planes * piece * l.padded_dim);
   if (!backward) {
@@ -166,11 +167,15 @@ eco::HeadRows rows_of(const eco_head_t *h, const Layout &l, char *ws) {
   r.count = reinterpret_cast<int32_t *>(ws + l.count);
   r.order = reinterpret_cast<int32_t *>(ws + l.order);
   r.place = reinterpret_cast<int32_t *>(ws + l.place);
+  r.flags = reinterpret_cast<uint8_t *>(ws + l.flags);
+  r.hidden_whole = r.dim % 8 == 0 && r.hidden_stride % (r.hidden_bf16 ? 8 : 4) == 0 && aligned(h->hidden, 16);
   return r;
 }
 
 eco::HeadWeights weights_of(const eco_head_t *h) {
-  return {h->weights, h->scales, stride_or(h->weight_stride, h->dim), h->group_size, h->fmt, h->scale_dtype == ECO_DT_BF16};
+  // a group that holds the whole tensor has the one scale
+  const uint64_t all = h->vocab * h->dim, group = h->group_size < all ? h->group_size : eco::HEAD_MOST_VOCAB * eco::HEAD_MOST_DIM;
+  return {h->weights, h->scales, stride_or(h->weight_stride, h->dim), group, h->fmt, h->scale_dtype == ECO_DT_BF16, eco::log2_exact(group)};
 }
 
 eco::HeadOperand hidden_operand(const Layout &l, char *ws) {

@@ -6,6 +6,8 @@
 #include <hip/hip_runtime.h>
 #include <math.h>
 
+#include <type_traits>
+
 #include "eco_device.hpp"
 #include "eco_head.hpp"
 
@@ -36,32 +38,51 @@ __device__ __forceinline__ int32_t label_of(const HeadRows &r, uint64_t row) {
   const int64_t y = r.labels[row];
   return y >= 0 && y < static_cast<int64_t>(r.vocab) ? static_cast<int32_t>(y) : -1;
 }
-__device__ bool takes_part(const HeadRows &r, uint64_t row) {
-  if (label_of(r, row) >= 0) return true;
-  for (uint32_t j = 0; j < r.top_k; ++j)
-    if (teacher_id(r, row, j) >= 0 && teacher_logit(r, row, j) != -INFINITY) return true;
-  return false;
+constexpr int ROWS_LANES = 16, ROWS_BLOCK = 256, SCAN_THREADS = 1024, SCAN_ROWS = 8;
+
+// Whether each row takes part: a label, or an entry of the teacher with weight, looked for by sixteen lanes a row.
+__global__ __launch_bounds__(ROWS_BLOCK) void eco_head_flags_kernel(HeadRows r) {
+  const uint32_t row = blockIdx.x * (ROWS_BLOCK / ROWS_LANES) + threadIdx.x / ROWS_LANES, lane = threadIdx.x % ROWS_LANES;
+  bool in = row < r.rows && label_of(r, row) >= 0;
+  if (row < r.rows && !in)
+    for (uint32_t j = lane; j < r.top_k && !in; j += ROWS_LANES) in = teacher_id(r, row, j) >= 0 && teacher_logit(r, row, j) != -INFINITY;
+  const uint64_t any = __ballot(in) >> (threadIdx.x % 64 / ROWS_LANES * ROWS_LANES) & ((1u << ROWS_LANES) - 1);
+  if (row < r.rows && lane == 0) r.flags[row] = any != 0;
 }
 
-// Which rows take part, in their order: one workgroup, an ordered count over 1024 rows at a time.
-__global__ __launch_bounds__(1024) void eco_head_rows_kernel(HeadRows r) {
-  __shared__ uint32_t wave_sum[16];
+// The rows that take part, in their order: one workgroup counts through 8192 rows at a time.
+__global__ __launch_bounds__(SCAN_THREADS) void eco_head_rows_kernel(HeadRows r) {
+  __shared__ uint32_t wave_sum[SCAN_THREADS / 64];
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
   uint32_t base = 0;
-  for (uint32_t first = 0; first < r.rows; first += 1024) {
-    const uint32_t row = first + threadIdx.x;
-    const bool in = row < r.rows && takes_part(r, row);
-    const uint64_t mask = __ballot(in);
-    if ((threadIdx.x & 63) == 0) wave_sum[threadIdx.x >> 6] = __popcll(mask);
+  for (uint32_t first = 0; first < r.rows; first += SCAN_THREADS * SCAN_ROWS) {
+    const uint32_t row0 = first + threadIdx.x * SCAN_ROWS;
+    uint32_t in = 0;
+#pragma unroll
+    for (int i = 0; i < SCAN_ROWS; ++i)
+      if (row0 + i < r.rows && (r.top_k ? r.flags[row0 + i] != 0 : label_of(r, row0 + i) >= 0)) in |= 1u << i;
+    uint32_t before = __popc(in);
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+      const uint32_t other = __shfl_up(before, d);
+      if (lane >= d) before += other;
+    }
+    if (lane == 63) wave_sum[wave] = before;
     __syncthreads();
-    uint32_t before = 0, all = 0;
-    for (uint32_t w = 0; w < 16; ++w) {
-      if (w < threadIdx.x >> 6) before += wave_sum[w];
+    uint32_t at = base + before - __popc(in), all = 0;
+#pragma unroll
+    for (int w = 0; w < SCAN_THREADS / 64; ++w) {
+      if (w < wave) at += wave_sum[w];
       all += wave_sum[w];
     }
     __syncthreads();
-    const uint32_t at = base + before + __popcll(mask & ((1ull << (threadIdx.x & 63)) - 1));
-    if (in) r.order[at] = static_cast<int32_t>(row);
-    if (row < r.rows) r.place[row] = in ? static_cast<int32_t>(at) : -1;
+#pragma unroll
+    for (int i = 0; i < SCAN_ROWS; ++i)
+      if (row0 + i < r.rows) {
+        const bool here = in >> i & 1;
+        r.place[row0 + i] = here ? static_cast<int32_t>(at) : -1;
+        if (here) r.order[at++] = static_cast<int32_t>(row0 + i);
+      }
     base += all;
   }
   if (threadIdx.x == 0) *r.count = static_cast<int32_t>(base);
@@ -90,6 +111,27 @@ __device__ __forceinline__ void store_planes(const float (&v)[8], uint16_t *dst,
   }
 }
 
+// Eight hidden states of a row from element k on, those past dim 0.
+__device__ __forceinline__ void hidden8(const HeadRows &r, uint64_t row, uint32_t k, float (&v)[8]) {
+  const uint64_t at = row * r.hidden_stride + k;
+  if (r.hidden_whole) {
+    if (r.hidden_bf16) {
+      const uint4 u = *reinterpret_cast<const uint4 *>(static_cast<const uint16_t *>(r.hidden) + at);
+      const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[j] = (j & 1) ? bf16_hi(w[j / 2]) : bf16_lo(w[j / 2]);
+    } else {
+      const float4 *p = reinterpret_cast<const float4 *>(static_cast<const float *>(r.hidden) + at);
+      const float4 a = p[0], b = p[1];
+      v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+    }
+    return;
+  }
+#pragma unroll
+  for (int j = 0; j < 8; ++j)
+    v[j] = k + j >= r.dim ? 0.0f : r.hidden_bf16 ? u2f(static_cast<uint32_t>(static_cast<const uint16_t *>(r.hidden)[at + j]) << 16) : static_cast<const float *>(r.hidden)[at + j];
+}
+
 // Hidden states of the rows that take part, one after the other, as bf16 planes of `ld` columns; zeros in the columns past dim and
 // in the rows past the last one that takes part, so that nothing which is not a number gets into a product from there.
 __global__ __launch_bounds__(256) void eco_head_gather_kernel(HeadRows r, uint16_t *compact, uint32_t padded, uint32_t ld, uint32_t planes) {
@@ -97,41 +139,69 @@ __global__ __launch_bounds__(256) void eco_head_gather_kernel(HeadRows r, uint16
   const uint64_t work = static_cast<uint64_t>(padded) * chunks, step = static_cast<uint64_t>(gridDim.x) * 256;
   const uint32_t count = static_cast<uint32_t>(*r.count);
   for (uint64_t i = static_cast<uint64_t>(blockIdx.x) * 256 + threadIdx.x; i < work; i += step) {
-    const uint32_t c = static_cast<uint32_t>(i / chunks), k = static_cast<uint32_t>(i % chunks) * 8;
+    const uint32_t c = i >> 32 ? static_cast<uint32_t>(i / chunks) : static_cast<uint32_t>(i) / chunks, k = static_cast<uint32_t>(i - static_cast<uint64_t>(c) * chunks) * 8;
     float v[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-    if (c < count) {
-      const uint64_t at = static_cast<uint64_t>(r.order[c]) * r.hidden_stride + k;
-#pragma unroll
-      for (int j = 0; j < 8; ++j)
-        if (k + j < r.dim) v[j] = r.hidden_bf16 ? u2f(static_cast<uint32_t>(static_cast<const uint16_t *>(r.hidden)[at + j]) << 16) : static_cast<const float *>(r.hidden)[at + j];
-    }
+    if (c < count && k < r.dim) hidden8(r, r.order[c], k, v);
     store_planes(v, compact + static_cast<uint64_t>(c) * ld + k, static_cast<uint64_t>(padded) * ld, planes);
   }
 }
 
 // ------------------------------------------------------------------------------------------------ weights
 
+__device__ __forceinline__ float scale_at(const HeadWeights &w, uint64_t i) {
+  const uint64_t g = w.group_shift >= 0 ? i >> w.group_shift : i >> 32 ? i / w.group : static_cast<uint32_t>(i) / static_cast<uint32_t>(w.group);
+  return w.scale_bf16 ? u2f(static_cast<uint32_t>(static_cast<const uint16_t *>(w.scales)[g]) << 16) : static_cast<const float *>(w.scales)[g];
+}
+template <int FMT>
 __device__ __forceinline__ float weight_at(const HeadWeights &w, uint64_t row, uint32_t dim, uint32_t k) {
-  if (w.fmt == FMT_BF16_PLAIN) return u2f(static_cast<uint32_t>(static_cast<const uint16_t *>(w.data)[row * w.stride + k]) << 16);
-  if (w.fmt == FMT_FP32_ID) return static_cast<const float *>(w.data)[row * w.stride + k];
-  const uint64_t i = row * dim + k, g = i / w.group;
-  const float s = w.scale_bf16 ? u2f(static_cast<uint32_t>(static_cast<const uint16_t *>(w.scales)[g]) << 16) : static_cast<const float *>(w.scales)[g];
-  if (w.fmt == FMT_FP8) return e4m3_decode<0>(static_cast<const uint8_t *>(w.data)[i]) * s;
+  if constexpr (FMT == FMT_BF16_PLAIN) return u2f(static_cast<uint32_t>(static_cast<const uint16_t *>(w.data)[row * w.stride + k]) << 16);
+  if constexpr (FMT == FMT_FP32_ID) return static_cast<const float *>(w.data)[row * w.stride + k];
+  const uint64_t i = row * dim + k;
+  if constexpr (FMT == FMT_FP8) return e4m3_decode<0>(static_cast<const uint8_t *>(w.data)[i]) * scale_at(w, i);
   const int32_t byte = static_cast<const int8_t *>(w.data)[i >> 1];
-  return static_cast<float>((i & 1) ? byte >> 4 : static_cast<int32_t>(static_cast<uint32_t>(byte) << 28) >> 28) * s;
+  return static_cast<float>((i & 1) ? byte >> 4 : static_cast<int32_t>(static_cast<uint32_t>(byte) << 28) >> 28) * scale_at(w, i);
 }
 
-__global__ __launch_bounds__(256) void eco_head_convert_kernel(HeadWeights w, uint64_t first, uint32_t rows, uint32_t dim, uint16_t *dst, uint32_t ld, uint64_t plane,
-                                                               uint32_t planes) {
+// Eight weights of a row from element k (a multiple of 8) on, those past dim 0.  WHOLE: rows are whole pieces of eight, which then lie in one
+// scale group and are one aligned load.
+template <int FMT, bool WHOLE>
+__device__ __forceinline__ void weights8(const HeadWeights &w, uint64_t row, uint32_t dim, uint32_t k, float (&v)[8]) {
+  if constexpr (!WHOLE) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = k + j < dim ? weight_at<FMT>(w, row, dim, k + j) : 0.0f;
+  } else if constexpr (FMT == FMT_BF16_PLAIN) {
+    const uint4 u = *reinterpret_cast<const uint4 *>(static_cast<const uint16_t *>(w.data) + row * w.stride + k);
+    const uint32_t x[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = (j & 1) ? bf16_hi(x[j / 2]) : bf16_lo(x[j / 2]);
+  } else if constexpr (FMT == FMT_FP32_ID) {
+    const float4 *p = reinterpret_cast<const float4 *>(static_cast<const float *>(w.data) + row * w.stride + k);
+    const float4 a = p[0], b = p[1];
+    v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+  } else {
+    const uint64_t i = row * dim + k;
+    const float s = scale_at(w, i);
+    if constexpr (FMT == FMT_FP8) {
+      const uint2 u = *reinterpret_cast<const uint2 *>(static_cast<const uint8_t *>(w.data) + i);
+      v[0] = e4m3_decode<0>(u.x) * s; v[1] = e4m3_decode<1>(u.x) * s; v[2] = e4m3_decode<2>(u.x) * s; v[3] = e4m3_decode<3>(u.x) * s;
+      v[4] = e4m3_decode<0>(u.y) * s; v[5] = e4m3_decode<1>(u.y) * s; v[6] = e4m3_decode<2>(u.y) * s; v[7] = e4m3_decode<3>(u.y) * s;
+    } else {
+      const uint32_t u = *reinterpret_cast<const uint32_t *>(static_cast<const uint8_t *>(w.data) + (i >> 1));
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[j] = static_cast<float>(static_cast<int32_t>(u << (28 - 4 * j)) >> 28) * s;
+    }
+  }
+}
+
+template <int FMT, bool WHOLE>
+__global__ __launch_bounds__(256) void eco_head_convert_kernel(HeadWeights w, uint64_t first, uint32_t rows, uint32_t dim, uint16_t *dst, uint32_t ld, uint64_t plane) {
   const uint32_t chunks = ld / 8;
   const uint64_t work = static_cast<uint64_t>(rows) * chunks, step = static_cast<uint64_t>(gridDim.x) * 256;
   for (uint64_t i = static_cast<uint64_t>(blockIdx.x) * 256 + threadIdx.x; i < work; i += step) {
-    const uint64_t row = i / chunks;
-    const uint32_t k = static_cast<uint32_t>(i % chunks) * 8;
-    float v[8];
-#pragma unroll
-    for (int j = 0; j < 8; ++j) v[j] = k + j < dim ? weight_at(w, first + row, dim, k + j) : 0.0f;
-    store_planes(v, dst + row * ld + k, plane, planes);
+    const uint32_t row = i >> 32 ? static_cast<uint32_t>(i / chunks) : static_cast<uint32_t>(i) / chunks, k = static_cast<uint32_t>(i - static_cast<uint64_t>(row) * chunks) * 8;
+    float v[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+    if (k < dim) weights8<FMT, WHOLE>(w, first + row, dim, k, v);
+    store_planes(v, dst + static_cast<uint64_t>(row) * ld + k, plane, head_weight_planes(FMT));
   }
 }
 
@@ -622,8 +692,11 @@ __device__ Teacher teacher_of(const HeadRows &r, uint64_t row, int lane) {
 }
 
 // A row's losses: the logits at the label and at the teacher's entries as dot products of their own (in fp32, from the weights as
-// they are stored), the tiles' statistics joined, and the sums over the teacher's entries.
+// they are stored), the tiles' statistics joined, and the sums over the teacher's entries.  The dot products are bound by the latency of rows of
+// weights that lie anywhere: a wave has the loads of DOTS rows under way.
+template <int FMT, bool WHOLE>
 __global__ __launch_bounds__(256) void eco_head_finish_kernel(HeadRows r, HeadWeights w, HeadStats st, float *ce, float *kd, float *lse, float *lse_tau, float *picked) {
+  constexpr int DOTS = 8;
   __shared__ float z[HEAD_MOST_TOP_K + 1], red[4][3];
   const uint32_t row = blockIdx.x;
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
@@ -640,17 +713,31 @@ __global__ __launch_bounds__(256) void eco_head_finish_kernel(HeadRows r, HeadWe
     return;
   }
   const int32_t label = label_of(r, row);
-  for (uint32_t j = wave; j < entries; j += 4) {
-    const int32_t id = j == 0 ? label : teacher_id(r, row, j - 1);
-    float sum = 0.0f;
-    if (id >= 0)
-      for (uint32_t k = lane; k < r.dim; k += 64) {
-        const uint64_t at = row * r.hidden_stride + k;
-        const float h = r.hidden_bf16 ? u2f(static_cast<uint32_t>(static_cast<const uint16_t *>(r.hidden)[at]) << 16) : static_cast<const float *>(r.hidden)[at];
-        sum = fmaf(h, weight_at(w, id, r.dim, k), sum);
+  for (uint32_t j0 = wave * DOTS; j0 < entries; j0 += 4 * DOTS) {
+    int32_t id[DOTS];
+    float sum[DOTS];
+#pragma unroll
+    for (int e = 0; e < DOTS; ++e) {
+      id[e] = j0 + e >= entries ? -1 : j0 + e == 0 ? label : teacher_id(r, row, j0 + e - 1);
+      sum[e] = 0.0f;
+    }
+    for (uint32_t k = lane * 8; k < r.dim; k += 512) {
+      float h[8];
+      hidden8(r, row, k, h);
+#pragma unroll
+      for (int e = 0; e < DOTS; ++e) {
+        if (id[e] < 0) continue;
+        float v[8];
+        weights8<FMT, WHOLE>(w, id[e], r.dim, k, v);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) sum[e] = fmaf(h[i], v[i], sum[e]);
       }
-    sum = wave_sum(sum);
-    if (lane == 0) z[j] = sum;
+    }
+#pragma unroll
+    for (int e = 0; e < DOTS; ++e) {
+      sum[e] = wave_sum(sum[e]);
+      if (lane == 0 && j0 + e < entries) z[j0 + e] = sum[e];
+    }
   }
   // the tiles' statistics
   const uint64_t at = static_cast<uint64_t>(c) * st.tiles;
@@ -767,17 +854,37 @@ __global__ __launch_bounds__(256) void eco_head_scatter_kernel(const int32_t *id
   }
 }
 
+// The gradient of the hidden states: each row's parts summed in their order, four columns to a thread; zeros where a row takes no part.
 __global__ __launch_bounds__(256) void eco_head_grad_hidden_finish_kernel(const float *partial, uint32_t splits, uint32_t ld, uint64_t stride, HeadRows r, void *out,
                                                                           uint64_t out_stride) {
-  const uint64_t work = static_cast<uint64_t>(r.rows) * r.dim, step = static_cast<uint64_t>(gridDim.x) * 256;
+  const uint32_t chunks = (r.dim + 3) / 4;
+  const uint64_t work = static_cast<uint64_t>(r.rows) * chunks, step = static_cast<uint64_t>(gridDim.x) * 256;
+  const bool whole = out_stride % 4 == 0 && r.dim % 4 == 0 && (reinterpret_cast<uintptr_t>(out) & 15) == 0;
   for (uint64_t i = static_cast<uint64_t>(blockIdx.x) * 256 + threadIdx.x; i < work; i += step) {
-    const uint64_t row = i / r.dim, k = i % r.dim;
+    const uint32_t row = i >> 32 ? static_cast<uint32_t>(i / chunks) : static_cast<uint32_t>(i) / chunks, k = static_cast<uint32_t>(i - static_cast<uint64_t>(row) * chunks) * 4;
     const int32_t c = r.place[row];
-    float sum = 0.0f;
-    if (c >= 0)
-      for (uint32_t s = 0; s < splits; ++s) sum += partial[s * stride + static_cast<uint64_t>(c) * ld + k];
-    if (r.hidden_bf16) static_cast<uint16_t *>(out)[row * out_stride + k] = static_cast<uint16_t>(f32x2_to_bf16x2_rne(sum, 0.0f));
-    else static_cast<float *>(out)[row * out_stride + k] = sum;
+    float4 sum = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    if (c >= 0) {
+      const float *p = partial + static_cast<uint64_t>(c) * ld + k;
+#pragma unroll 8
+      for (uint32_t s = 0; s < splits; ++s) {
+        const float4 v = *reinterpret_cast<const float4 *>(p + s * stride);
+        sum.x += v.x; sum.y += v.y; sum.z += v.z; sum.w += v.w;
+      }
+    }
+    const uint64_t at = row * out_stride + k;
+    const float v[4] = {sum.x, sum.y, sum.z, sum.w};
+    if (whole) {
+      if (r.hidden_bf16) *reinterpret_cast<uint2 *>(static_cast<uint16_t *>(out) + at) = make_uint2(f32x2_to_bf16x2_rne(v[0], v[1]), f32x2_to_bf16x2_rne(v[2], v[3]));
+      else *reinterpret_cast<float4 *>(static_cast<float *>(out) + at) = sum;
+    } else {
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        if (k + j < r.dim) {
+          if (r.hidden_bf16) static_cast<uint16_t *>(out)[at + j] = static_cast<uint16_t>(f32x2_to_bf16x2_rne(v[j], 0.0f));
+          else static_cast<float *>(out)[at + j] = v[j];
+        }
+    }
   }
 }
 
@@ -867,8 +974,31 @@ uint32_t head_splits(uint64_t rows, uint64_t dim, uint64_t piece) {
   return static_cast<uint32_t>(splits);
 }
 
+template <class F>
+hipError_t by_format(const HeadWeights &w, uint32_t dim, F launch) {
+  // whole: pieces of eight elements of a row are aligned
+  const bool whole = dim % 8 == 0 && (w.fmt == FMT_FP8 || w.fmt == FMT_INT4 || w.stride % (w.fmt == FMT_BF16_PLAIN ? 8 : 4) == 0);
+  const auto of = [&](auto fmt) {
+    if (whole) launch(fmt, std::true_type{});
+    else launch(fmt, std::false_type{});
+  };
+  switch (w.fmt) {
+    case FMT_FP8: of(std::integral_constant<int, FMT_FP8>{}); break;
+    case FMT_INT4: of(std::integral_constant<int, FMT_INT4>{}); break;
+    case FMT_BF16_PLAIN: of(std::integral_constant<int, FMT_BF16_PLAIN>{}); break;
+    default: of(std::integral_constant<int, FMT_FP32_ID>{}); break;
+  }
+  return hipGetLastError();
+}
+
 hipError_t launch_head_rows(const HeadRows &r, void *compact, uint32_t padded_rows, uint32_t padded_dim, hipStream_t s) {
-  hipLaunchKernelGGL(eco_head_rows_kernel, dim3(1), dim3(1024), 0, s, r);
+  if (r.top_k) {
+    constexpr uint32_t each = ROWS_BLOCK / ROWS_LANES;
+    hipLaunchKernelGGL(eco_head_flags_kernel, dim3((r.rows + each - 1) / each), dim3(ROWS_BLOCK), 0, s, r);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  hipLaunchKernelGGL(eco_head_rows_kernel, dim3(1), dim3(SCAN_THREADS), 0, s, r);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   hipLaunchKernelGGL(eco_head_gather_kernel, dim3(blocks_for(static_cast<uint64_t>(padded_rows) * padded_dim / 8)), dim3(256), 0, s, r,
@@ -877,9 +1007,10 @@ hipError_t launch_head_rows(const HeadRows &r, void *compact, uint32_t padded_ro
 }
 
 hipError_t launch_head_convert(const HeadWeights &w, uint64_t first, uint32_t rows, uint32_t dim, void *planes, uint32_t ld, uint64_t plane, hipStream_t s) {
-  hipLaunchKernelGGL(eco_head_convert_kernel, dim3(blocks_for(static_cast<uint64_t>(rows) * ld / 8)), dim3(256), 0, s, w, first, rows, dim,
-                     static_cast<uint16_t *>(planes), ld, plane, static_cast<uint32_t>(head_weight_planes(w.fmt)));
-  return hipGetLastError();
+  return by_format(w, dim, [&](auto fmt, auto whole) {
+    hipLaunchKernelGGL((eco_head_convert_kernel<fmt.value, whole.value>), dim3(blocks_for(static_cast<uint64_t>(rows) * ld / 8)), dim3(256), 0, s, w, first, rows, dim,
+                       static_cast<uint16_t *>(planes), ld, plane);
+  });
 }
 
 hipError_t launch_head_stats(const HeadOperand &w, const HeadOperand &h, uint32_t n, uint32_t rows, uint32_t dim, const int32_t *count, float inv_tau,
@@ -895,8 +1026,9 @@ hipError_t launch_head_stats(const HeadOperand &w, const HeadOperand &h, uint32_
 
 hipError_t launch_head_finish(const HeadRows &r, const HeadWeights &w, const HeadStats &st, float *ce, float *kd, float *lse, float *lse_tau, float *picked,
                               hipStream_t s) {
-  hipLaunchKernelGGL(eco_head_finish_kernel, dim3(r.rows), dim3(256), 0, s, r, w, st, ce, kd, lse, lse_tau, picked);
-  return hipGetLastError();
+  return by_format(w, r.dim, [&](auto fmt, auto whole) {
+    hipLaunchKernelGGL((eco_head_finish_kernel<fmt.value, whole.value>), dim3(r.rows), dim3(256), 0, s, r, w, st, ce, kd, lse, lse_tau, picked);
+  });
 }
 
 hipError_t launch_head_entries(const HeadRows &r, uint32_t padded_rows, const float *grad_ce, const float *grad_kd, const float *lse, const float *lse_tau,
@@ -931,7 +1063,7 @@ hipError_t launch_head_grad_hidden(const HeadOperand &w, const HeadOperand &g, u
 
 hipError_t launch_head_grad_hidden_finish(const float *partial, uint32_t splits, uint32_t partial_ld, uint64_t partial_stride, const HeadRows &r, void *out,
                                           uint64_t out_stride, hipStream_t s) {
-  hipLaunchKernelGGL(eco_head_grad_hidden_finish_kernel, dim3(blocks_for(static_cast<uint64_t>(r.rows) * r.dim)), dim3(256), 0, s, partial, splits, partial_ld,
+  hipLaunchKernelGGL(eco_head_grad_hidden_finish_kernel, dim3(blocks_for(static_cast<uint64_t>(r.rows) * ((r.dim + 3) / 4))), dim3(256), 0, s, partial, splits, partial_ld,
                      partial_stride, r, out, out_stride);
   return hipGetLastError();
 }
