@@ -227,7 +227,7 @@ struct ProductArgs {
   float *out_f32;
   void *out;
   uint64_t out_ld, out_plane;
-  uint32_t out_planes, tiles, tile0, splits, tiles_x;
+  uint32_t out_planes, tiles, tile0, splits, split_steps, tiles_x;
   int32_t two, out_bf16, add;
   float *sum, *sum_tau;
   const HeadRowConst *consts;
@@ -256,8 +256,8 @@ __device__ __forceinline__ void barrier() {
 }
 
 // A tile of BX x BY by WX x WY waves of 32 x 32 blocks.  The inner axis goes by in steps of 64, 128 bytes of a row: a whole line of
-// memory, half of which took the caches as long (256 x 256 tiles of 8192 x 1152 x 262144, losses: 4.46 ms in steps of 32).  There are DEPTH places
-// for steps in LDS.
+// memory, half of which took the caches as long (256 x 256 tiles of 8192 x 1152 x 262144, losses: 4.46 ms in steps of 32, 4.08 of 64).  There are
+// DEPTH places for steps in LDS, and a part of each wave's own for its results on their way out.
 template <int BX_, int BY_, int WX_, int WY_, int DEPTH_>
 struct Tile {
   static_assert(KSTEP == 64, "row_piece and fragment go by rows of 128 bytes");
@@ -267,6 +267,11 @@ struct Tile {
   static constexpr int X_LOADS = X_BYTES / 16 / THREADS, Y_LOADS = Y_BYTES / 16 / THREADS, LOADS = X_LOADS + Y_LOADS;
   static_assert(X_LOADS * THREADS * 16 == X_BYTES && Y_LOADS * THREADS * 16 == Y_BYTES, "whole loads");
 };
+// Bytes of LDS past the steps: of the statistics three arrays [WX][BY], else 32 rows of 64 bf16 or 32 fp32 (of 32 bf16 where a wave has no more) to a wave
+template <int MODE, class T>
+constexpr int own_bytes() { return (MODE == GRAD || MODE == GRAD_PLANES) && T::NI == 1 ? 2048 : 4096; }
+template <int MODE, class T>
+constexpr int extra_bytes() { return MODE == STATS ? 3 * T::WX * T::BY * 4 : T::WX * T::WY * own_bytes<MODE, T>(); }
 
 // Where the 16-byte piece `c` of a step's operand comes from.  A row operand's step is rows of 128 bytes, a column operand's 64 rows of
 // N elements; the pieces of a row are exchanged so that lanes which read together, sixteen of 16 bytes or half a wave of 8, find theirs in
@@ -302,28 +307,23 @@ __device__ __forceinline__ bf16x8 fragment(const lds_char *step, int n0, int kk,
   }
 }
 
-// A wave's results on their way out: 32 rows y of its NI * 32 columns x pass through its own part of LDS, so that whole lines are
-// stored; the registers hold four columns of a row, and storing those took the 8192 x 256 tiles of the logits' gradient 1.4 times as long as their
-// product.  16-byte pieces of a row are exchanged by row, against bank conflicts.  A wave's own reads and writes of LDS are in order.
-template <int NI>
+// A wave's results on their way out: 32 rows y of up to 64 (bf16) or 32 (fp32) columns x pass through its own part of LDS, so that whole lines are
+// stored; the registers hold four columns of a row.  16-byte pieces of a row are exchanged by row, against bank conflicts.  A wave's own
+// reads and writes of LDS are in order.
+template <int PIECES>
 __device__ __forceinline__ void put_bf16(lds_char *own, int lane, int i, int q, uint32_t lo, uint32_t hi) {
-  constexpr int PIECES = NI * 4;
   const int row = lane & 31;
   *(__attribute__((address_space(3))) uint64_t *)(own + row * PIECES * 16 + 16 * ((4 * i + q) ^ (row & (PIECES - 1))) + 8 * (lane >> 5)) =
       static_cast<uint64_t>(hi) << 32 | lo;
 }
 typedef float f32x4 __attribute__((ext_vector_type(4)));
-template <int NI, int NJ>
-__device__ __forceinline__ void put_f32(lds_char *own, int lane, const f32x16 (&acc)[NI][NJ], int j) {
-  constexpr int PIECES = NI * 8;
+__device__ __forceinline__ void put_f32(lds_char *own, int lane, const f32x16 &acc) {
   const int row = lane & 31;
 #pragma unroll
-  for (int i = 0; i < NI; ++i)
-#pragma unroll
-    for (int q = 0; q < 4; ++q) {
-      const f32x4 v = {acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]};
-      *(__attribute__((address_space(3))) f32x4 *)(own + row * PIECES * 16 + 16 * ((8 * i + 2 * q + (lane >> 5)) ^ (row & (PIECES - 1)))) = v;
-    }
+  for (int q = 0; q < 4; ++q) {
+    const f32x4 v = {acc[4 * q], acc[4 * q + 1], acc[4 * q + 2], acc[4 * q + 3]};
+    *(__attribute__((address_space(3))) f32x4 *)(own + row * 128 + 16 * ((2 * q + (lane >> 5)) ^ (row & 7))) = v;
+  }
 }
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 template <int PIECES, class F>
@@ -343,50 +343,56 @@ __device__ __forceinline__ uint32_t xcd_run(uint32_t id, uint32_t all) {
   return xcd * each + min(xcd, more) + nth;
 }
 
+// A workgroup goes through tiles gridDim.x apart.  Its loads do not stop between them: while a tile's results leave, the next tile's
+// first steps are on their way.
 template <int MODE, class T>
 __global__ __launch_bounds__(T::THREADS) void eco_head_product_kernel(ProductArgs a) {
-  constexpr bool X_COLUMN = MODE == DH || MODE == DW, Y_COLUMN = MODE == DW;
-  constexpr int NI = T::NI, NJ = T::NJ;
-  __shared__ __attribute__((aligned(1024))) char smem[T::DEPTH * T::STEP_BYTES];
+  constexpr bool X_COLUMN = MODE == DH || MODE == DW, Y_COLUMN = MODE == DW, LOGITS = MODE == STATS || MODE == GRAD || MODE == GRAD_PLANES;
+  constexpr int NI = T::NI, NJ = T::NJ, QUARTERS = KSTEP / 16;
+  __shared__ __attribute__((aligned(1024))) char smem[T::DEPTH * T::STEP_BYTES + extra_bytes<MODE, T>()];
+  static_assert(sizeof smem <= 163840, "a compute unit's LDS");
   const uint32_t count = static_cast<uint32_t>(*a.count);
   const uint32_t ny = MODE == DW ? a.ny : count;
   // the grid is made for all rows: the tiles that there are, evenly over the XCDs
   const uint32_t tiles_y = (ny + T::BY - 1) / T::BY, all_tiles = a.tiles_x * tiles_y * a.splits;
   if (blockIdx.x >= all_tiles) return;
-  uint32_t tile = xcd_run(blockIdx.x, all_tiles), split = 0, tx, ty;
-  if (MODE == STATS || MODE == GRAD || MODE == GRAD_PLANES) {
-    // eight tiles of rows beside each other, then the next of the vocabulary
-    const uint32_t run = 8 * a.tiles_x, band = tile / run, high = min(8u, tiles_y - band * 8), in = tile - band * run;
-    tx = in / high; ty = band * 8 + in % high;
-  } else {
-    if (MODE == DH) { split = tile / (a.tiles_x * tiles_y); tile -= split * a.tiles_x * tiles_y; }
-    ty = tile / a.tiles_x; tx = tile % a.tiles_x;
-  }
-  const uint32_t x0 = tx * T::BX, y0 = ty * T::BY;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wx = wave % T::WX * (NI * 32), wy = wave / T::WX * (NJ * 32);
   const uint32_t all_steps = MODE == DW ? (count + KSTEP - 1) / KSTEP : (a.k + KSTEP - 1) / KSTEP;
-  uint32_t first = 0, steps = all_steps;
-  if (MODE == DH) {
-    const uint32_t each = (all_steps + a.splits - 1) / a.splits;
-    first = min(all_steps, split * each);
-    steps = min(all_steps, first + each) - first;
-  }
   // the last step's end: past it pieces repeat valid ones of their row, or rows the last one, against zeros of the other operand
   const uint32_t tail = MODE == DW ? 0 : a.k % KSTEP;
+  const uint64_t step_x = X_COLUMN ? static_cast<uint64_t>(KSTEP) * a.ldx : KSTEP, step_y = Y_COLUMN ? static_cast<uint64_t>(KSTEP) * a.ldy : KSTEP;
 
-  uint32_t off_x[T::X_LOADS], off_y[T::Y_LOADS];
-#pragma unroll
-  for (int i = 0; i < T::X_LOADS; ++i) {
-    uint32_t n, k;
-    if constexpr (X_COLUMN) {
-      column_piece<T::BX>(threadIdx.x + i * T::THREADS, n, k);
-      off_x[i] = (k * a.ldx + min(x0 + n, (a.nx + 7) / 8 * 8 - 8) - x0) * 2;
+  struct Where { uint32_t x0, y0, split, first, steps; };
+  const auto where = [&](uint32_t id) {
+    uint32_t tile = xcd_run(id, all_tiles), tx, ty;
+    Where w = {0, 0, 0, 0, all_steps};
+    if (LOGITS) {
+      // eight tiles of rows beside each other, then the next of the vocabulary
+      const uint32_t run = 8 * a.tiles_x, band = tile / run, high = min(8u, tiles_y - band * 8), in = tile - band * run;
+      tx = in / high; ty = band * 8 + in % high;
     } else {
-      row_piece(threadIdx.x + i * T::THREADS, n, k);
-      off_x[i] = ((min(x0 + n, a.nx - 1) - x0) * a.ldx + k) * 2;
+      if (MODE == DH) {
+        w.split = tile / (a.tiles_x * tiles_y);
+        tile -= w.split * a.tiles_x * tiles_y;
+        w.first = w.split * a.split_steps;
+        w.steps = min(a.split_steps, all_steps - w.first);
+      }
+      ty = tile / a.tiles_x; tx = tile % a.tiles_x;
     }
-  }
+    w.x0 = tx * T::BX; w.y0 = ty * T::BY;
+    return w;
+  };
+
+  // pairs of planes whose product counts: the sum of their places is at most 2
+  uint32_t pairs = 0;
+  for (uint32_t px = 0; px < a.x_planes; ++px) pairs += min(a.y_planes, 3 - px);
+
+  // ---- the loads' place in the work
+  uint32_t load_id = blockIdx.x, load_first, load_steps, in_pair, px, py, issued = 0, place = 0;
+  uint32_t off_x[T::X_LOADS], off_y[T::Y_LOADS];
+  const uint16_t *begin_x, *begin_y, *from_x, *from_y;
+  const uint32_t lds0 = static_cast<uint32_t>(reinterpret_cast<uintptr_t>((lds_char *)smem));
 #pragma unroll
   for (int i = 0; i < T::Y_LOADS; ++i) {
     uint32_t n, k;
@@ -394,20 +400,29 @@ __global__ __launch_bounds__(T::THREADS) void eco_head_product_kernel(ProductArg
     else row_piece(threadIdx.x + i * T::THREADS, n, k);
     off_y[i] = (Y_COLUMN ? k * a.ldy + n : n * a.ldy + k) * 2;
   }
-  const uint64_t step_x = X_COLUMN ? static_cast<uint64_t>(KSTEP) * a.ldx : KSTEP, step_y = Y_COLUMN ? static_cast<uint64_t>(KSTEP) * a.ldy : KSTEP;
-  const uint16_t *const begin_x = a.x + (X_COLUMN ? x0 : static_cast<uint64_t>(x0) * a.ldx) + first * step_x;
-  const uint16_t *const begin_y = a.y + (Y_COLUMN ? y0 : static_cast<uint64_t>(y0) * a.ldy) + first * step_y;
-
-  // pairs of planes whose product counts: the sum of their places is at most 2
-  uint32_t pairs = 0;
-  for (uint32_t px = 0; px < a.x_planes; ++px) pairs += min(a.y_planes, 3 - px);
-  const uint32_t total = steps * pairs;
-  const uint16_t *from_x = begin_x, *from_y = begin_y;
-  uint32_t px = 0, py = 0, in_pair = 0, issued = 0, place = 0;
-  const uint32_t lds0 = static_cast<uint32_t>(reinterpret_cast<uintptr_t>((lds_char *)smem));
+  const auto load_tile = [&]() {
+    const Where w = where(load_id);
+#pragma unroll
+    for (int i = 0; i < T::X_LOADS; ++i) {
+      uint32_t n, k;
+      if constexpr (X_COLUMN) {
+        column_piece<T::BX>(threadIdx.x + i * T::THREADS, n, k);
+        off_x[i] = (k * a.ldx + min(w.x0 + n, (a.nx + 7) / 8 * 8 - 8) - w.x0) * 2;
+      } else {
+        row_piece(threadIdx.x + i * T::THREADS, n, k);
+        off_x[i] = ((min(w.x0 + n, a.nx - 1) - w.x0) * a.ldx + k) * 2;
+      }
+    }
+    load_first = w.first;
+    load_steps = w.steps;
+    from_x = begin_x = a.x + (X_COLUMN ? w.x0 : static_cast<uint64_t>(w.x0) * a.ldx) + w.first * step_x;
+    from_y = begin_y = a.y + (Y_COLUMN ? w.y0 : static_cast<uint64_t>(w.y0) * a.ldy) + w.first * step_y;
+    in_pair = px = py = 0;
+  };
   const auto issue = [&]() {
+    if (load_id >= all_tiles) return;
     const uint32_t lds = lds0 + place * T::STEP_BYTES + wave * 1024;
-    const bool end = tail && first + in_pair + 1 == all_steps;
+    const bool end = tail && load_first + in_pair + 1 == all_steps;
 #pragma unroll
     for (int i = 0; i < T::X_LOADS; ++i) {
       uint32_t off = off_x[i];
@@ -427,35 +442,45 @@ __global__ __launch_bounds__(T::THREADS) void eco_head_product_kernel(ProductArg
     for (int i = 0; i < T::Y_LOADS; ++i) load_to_lds(lds + T::X_BYTES + i * T::THREADS * 16, from_y, off_y[i]);
     place = place + 1 == T::DEPTH ? 0 : place + 1;
     ++issued;
-    if (++in_pair == steps) {
+    if (++in_pair == load_steps) {
       in_pair = 0;
       if (++py == a.y_planes || px + py > 2) { py = 0; ++px; }
-      from_x = begin_x + px * a.x_plane;
-      from_y = begin_y + py * a.y_plane;
+      if (px == a.x_planes) {
+        load_id += gridDim.x;
+        if (load_id < all_tiles) load_tile();
+      } else {
+        from_x = begin_x + px * a.x_plane;
+        from_y = begin_y + py * a.y_plane;
+      }
     } else {
       from_x += step_x;
       from_y += step_y;
     }
   };
 
-  f32x16 acc[NI][NJ] = {};
-  if (total) {
-    constexpr int QUARTERS = KSTEP / 16;
-    bf16x8 fx[2][NI], fy[2][NJ];                               // the quarter at hand and the next one
-    const auto read = [&](const lds_char *step, int kk, bf16x8 (&x)[NI], bf16x8 (&y)[NJ]) {
+  // ---- the products' place
+  bf16x8 fx[2][NI], fy[2][NJ];                                 // the quarter of a step at hand and the next one
+  const auto read = [&](const lds_char *step, int kk, bf16x8 (&x)[NI], bf16x8 (&y)[NJ]) {
 #pragma unroll
-      for (int j = 0; j < NJ; ++j) y[j] = fragment<T::BY, Y_COLUMN>(step + T::X_BYTES, wy + 32 * j, kk, lane);
+    for (int j = 0; j < NJ; ++j) y[j] = fragment<T::BY, Y_COLUMN>(step + T::X_BYTES, wy + 32 * j, kk, lane);
 #pragma unroll
-      for (int i = 0; i < NI; ++i) x[i] = fragment<T::BX, X_COLUMN>(step, wx + 32 * i, kk, lane);
-    };
-    for (int i = 0; i < T::DEPTH; ++i)
-      if (issued < total) issue();
-    if (total >= T::DEPTH) wait_loads<(T::DEPTH - 1) * T::LOADS>();
+    for (int i = 0; i < NI; ++i) x[i] = fragment<T::BX, X_COLUMN>(step, wx + 32 * i, kk, lane);
+  };
+  uint32_t at = 0, done = 0;
+  const lds_char *step = (const lds_char *)smem;
+  if (all_steps) {                                             // (0: the gradient of the weights where no row takes part)
+    load_tile();
+    for (int i = 0; i < T::DEPTH; ++i) issue();
+    if (issued == T::DEPTH) wait_loads<(T::DEPTH - 1) * T::LOADS>();
     else wait_loads<0>();
     barrier();
-    uint32_t at = 0;
-    const lds_char *step = (const lds_char *)smem;
     read(step, 0, fx[0], fy[0]);
+  }
+
+  for (uint32_t id = blockIdx.x; id < all_tiles; id += gridDim.x) {
+    const Where w = where(id);
+    const uint32_t x0 = w.x0, y0 = w.y0, total = w.steps * pairs;
+    f32x16 acc[NI][NJ] = {};
     for (uint32_t s = 0; s < total; ++s) {
 #pragma unroll
       for (int kk = 0; kk < QUARTERS - 1; ++kk) {
@@ -466,9 +491,10 @@ __global__ __launch_bounds__(T::THREADS) void eco_head_product_kernel(ProductArg
           for (int j = 0; j < NJ; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fx[kk & 1][i], fy[kk & 1][j], acc[i][j], 0, 0, 0);
       }
       // the next step is there once every wave's loads of it are, and this one's place is free once every wave has read it
-      if (s + T::DEPTH <= total) wait_all_but<(T::DEPTH - 2) * T::LOADS>();
+      if (issued - done >= T::DEPTH) wait_all_but<(T::DEPTH - 2) * T::LOADS>();
       else wait_all_but<0>();
       barrier();
+      ++done;
       at = at + 1 == T::DEPTH ? 0 : at + 1;
       step = (const lds_char *)smem + at * T::STEP_BYTES;
       read(step, 0, fx[0], fy[0]);                             // (after the last step nothing uses these: a branch would make the products wait)
@@ -479,92 +505,90 @@ __global__ __launch_bounds__(T::THREADS) void eco_head_product_kernel(ProductArg
           acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fx[(QUARTERS - 1) & 1][i], fy[(QUARTERS - 1) & 1][j], acc[i][j], 0, 0, 0);
         if (i == 0) {
           __builtin_amdgcn_sched_barrier(0);
-          if (issued < total) issue();
+          issue();
           __builtin_amdgcn_sched_barrier(0);
         }
       }
     }
-  }
 
-  // acc[i][j][r]: x = x0 + wx + 32 i + (r & 3) + 8 (r >> 2) + 4 (lane >> 5), y = y0 + wy + 32 j + (lane & 31)
-  const auto x_of = [&](int i, int r) { return x0 + wx + 32 * i + (r & 3) + 8 * (r >> 2) + 4 * (lane >> 5); };
-  if constexpr (MODE == STATS) {
-    float *red = reinterpret_cast<float *>(smem);              // [WX][BY], the loads' places are free now
-    const auto across = [&](float (&v)[NJ], auto join) {       // over a tile's x: the other half's registers, then the other waves
-      barrier();
+    // acc[i][j][r]: x = x0 + wx + 32 i + (r & 3) + 8 (r >> 2) + 4 (lane >> 5), y = y0 + wy + 32 j + (lane & 31)
+    const auto x_of = [&](int i, int r) { return x0 + wx + 32 * i + (r & 3) + 8 * (r >> 2) + 4 * (lane >> 5); };
+    lds_char *const extra = (lds_char *)smem + T::DEPTH * T::STEP_BYTES;
+    lds_char *const own = extra + wave * own_bytes<MODE, T>();
+    if constexpr (MODE == STATS) {
+      typedef __attribute__((address_space(3))) float lds_float;
+      const auto across = [&](float (&v)[NJ], int which, auto join) {      // over a tile's x: the other half's registers, then the other waves
+        lds_float *red = (lds_float *)extra + which * T::WX * T::BY;
 #pragma unroll
-      for (int j = 0; j < NJ; ++j) {
-        v[j] = join(v[j], __shfl_xor(v[j], 32));
-        if (lane < 32) red[wave % T::WX * T::BY + wy + 32 * j + lane] = v[j];
-      }
-      __syncthreads();
+        for (int j = 0; j < NJ; ++j) {
+          v[j] = join(v[j], __shfl_xor(v[j], 32));
+          if (lane < 32) red[wave % T::WX * T::BY + wy + 32 * j + lane] = v[j];
+        }
+        __syncthreads();
 #pragma unroll
-      for (int j = 0; j < NJ; ++j) {
-        v[j] = red[wy + 32 * j + (lane & 31)];
+        for (int j = 0; j < NJ; ++j) {
+          v[j] = red[wy + 32 * j + (lane & 31)];
 #pragma unroll
-        for (int w = 1; w < T::WX; ++w) v[j] = join(v[j], red[w * T::BY + wy + 32 * j + (lane & 31)]);
-      }
-    };
-    float m[NJ], s[NJ];
-    if (x0 + T::BX > a.nx)
-#pragma unroll
-      for (int i = 0; i < NI; ++i)
-#pragma unroll
-        for (int r = 0; r < 16; ++r)
-          if (x_of(i, r) >= a.nx)
-#pragma unroll
-            for (int j = 0; j < NJ; ++j) acc[i][j][r] = -INFINITY;
-#pragma unroll
-    for (int j = 0; j < NJ; ++j) {
-      m[j] = -INFINITY;
-#pragma unroll
-      for (int i = 0; i < NI; ++i)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) m[j] = fmaxf(m[j], acc[i][j][r]);
-    }
-    across(m, [](float p, float q) { return fmaxf(p, q); });
-    const auto sums = [&](float c) {
-#pragma unroll
-      for (int j = 0; j < NJ; ++j) {
-        const float base = m[j] == -INFINITY ? 0.0f : -m[j] * c;
-        s[j] = 0.0f;
+          for (int q = 1; q < T::WX; ++q) v[j] = join(v[j], red[q * T::BY + wy + 32 * j + (lane & 31)]);
+        }
+      };
+      float m[NJ], sum[NJ];
+      if (x0 + T::BX > a.nx)
 #pragma unroll
         for (int i = 0; i < NI; ++i)
 #pragma unroll
-          for (int r = 0; r < 16; ++r) s[j] += exp2_fast(fmaf(acc[i][j][r], c, base));
+          for (int r = 0; r < 16; ++r)
+            if (x_of(i, r) >= a.nx)
+#pragma unroll
+              for (int j = 0; j < NJ; ++j) acc[i][j][r] = -INFINITY;
+#pragma unroll
+      for (int j = 0; j < NJ; ++j) {
+        m[j] = -INFINITY;
+#pragma unroll
+        for (int i = 0; i < NI; ++i)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) m[j] = fmaxf(m[j], acc[i][j][r]);
       }
-      __syncthreads();
-      across(s, [](float p, float q) { return p + q; });
-    };
-    const auto store = [&](float *out, const float (&v)[NJ]) {
-      if (wave % T::WX == 0 && lane < 32)
+      across(m, 0, [](float p, float q) { return fmaxf(p, q); });
+      const auto sums = [&](float c, int which) {
 #pragma unroll
         for (int j = 0; j < NJ; ++j) {
-          const uint32_t y = y0 + wy + 32 * j + lane;
-          if (y < ny) out[static_cast<uint64_t>(y) * a.tiles + a.tile0 + tx] = v[j];
+          const float base = m[j] == -INFINITY ? 0.0f : -m[j] * c;
+          sum[j] = 0.0f;
+#pragma unroll
+          for (int i = 0; i < NI; ++i)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) sum[j] += exp2_fast(fmaf(acc[i][j][r], c, base));
         }
-    };
-    store(a.out_f32, m);
-    sums(a.scale2);
-    store(a.sum, s);
-    if (a.two) {
-      sums(a.scale2_tau);
-      store(a.sum_tau, s);
+        across(sum, which, [](float p, float q) { return p + q; });
+      };
+      const auto store = [&](float *out, const float (&v)[NJ]) {
+        if (wave % T::WX == 0 && lane < 32)
+#pragma unroll
+          for (int j = 0; j < NJ; ++j) {
+            const uint32_t y = y0 + wy + 32 * j + lane;
+            if (y < ny) out[static_cast<uint64_t>(y) * a.tiles + a.tile0 + x0 / T::BX] = v[j];
+          }
+      };
+      store(a.out_f32, m);
+      sums(a.scale2, 1);
+      store(a.sum, sum);
+      if (a.two) {
+        sums(a.scale2_tau, 2);
+        store(a.sum_tau, sum);
+      }
     }
-  }
-  if constexpr (MODE != STATS) {
-    barrier();                                                 // every wave has read its operands: LDS is free
-    lds_char *const own = (lds_char *)smem + wave * (32 * NI * 32 * 4);
     if constexpr (MODE == GRAD || MODE == GRAD_PLANES) {
       uint16_t *const out = static_cast<uint16_t *>(a.out);
       const bool edge = x0 + T::BX > a.nx;
+      constexpr int WIDE = NI == 1 ? 1 : 2;
 #pragma unroll
       for (int j = 0; j < NJ; ++j) {
         // (rows past the last one that takes part have a = b = 0)
         const HeadRowConst rc = a.consts[y0 + wy + 32 * j + (lane & 31)];
 #pragma unroll
         for (int i = 0; i < NI; ++i) {
-          if (a.two == 1) {
+          if (a.two) {
 #pragma unroll
             for (int r = 0; r < 16; ++r)
               acc[i][j][r] = fmaf(rc.b, exp2_fast(fmaf(acc[i][j][r], a.scale2_tau, -rc.lse2_tau)), rc.a * exp2_fast(fmaf(acc[i][j][r], a.scale2, -rc.lse2)));
@@ -578,13 +602,16 @@ __global__ __launch_bounds__(T::THREADS) void eco_head_product_kernel(ProductArg
         }
         const auto put_and_take = [&](uint32_t p, auto two_of) {
 #pragma unroll
-          for (int i = 0; i < NI; ++i)
+          for (int i0 = 0; i0 < NI; i0 += WIDE) {
 #pragma unroll
-            for (int q = 0; q < 4; ++q) put_bf16<NI>(own, lane, i, q, two_of(i, 4 * q), two_of(i, 4 * q + 2));
-          // (columns and rows of the padded piece: nothing to check)
-          take<NI * 4>(own, lane, [&](uint32_t row, uint32_t piece, uint4 v) {
-            *reinterpret_cast<uint4 *>(out + p * a.out_plane + static_cast<uint64_t>(y0 + wy + 32 * j + row) * a.out_ld + x0 + wx + 8 * piece) = v;
-          });
+            for (int i = 0; i < WIDE; ++i)
+#pragma unroll
+              for (int q = 0; q < 4; ++q) put_bf16<4 * WIDE>(own, lane, i, q, two_of(i0 + i, 4 * q), two_of(i0 + i, 4 * q + 2));
+            // (columns and rows of the padded piece: nothing to check)
+            take<4 * WIDE>(own, lane, [&](uint32_t row, uint32_t piece, uint4 v) {
+              *reinterpret_cast<uint4 *>(out + p * a.out_plane + static_cast<uint64_t>(y0 + wy + 32 * j + row) * a.out_ld + x0 + wx + 32 * i0 + 8 * piece) = v;
+            });
+          }
         };
         if constexpr (MODE == GRAD)
           put_and_take(0, [&](int i, int r) { return f32x2_to_bf16x2_rne(acc[i][j][r], acc[i][j][r + 1]); });
@@ -602,60 +629,68 @@ __global__ __launch_bounds__(T::THREADS) void eco_head_product_kernel(ProductArg
       }
     }
     if constexpr (MODE == DH) {
-      float *const out = a.out_f32 + split * a.out_plane;
+      float *const out = a.out_f32 + w.split * a.out_plane;
 #pragma unroll
-      for (int j = 0; j < NJ; ++j) {
-        put_f32<NI>(own, lane, acc, j);
-        take<NI * 8>(own, lane, [&](uint32_t row, uint32_t piece, uint4 v) {
-          const uint32_t y = y0 + wy + 32 * j + row, x = x0 + wx + 4 * piece;
-          if (y >= ny || x >= a.out_ld) return;                // whole fours: out_ld is the padded dimension
-          float4 *to = reinterpret_cast<float4 *>(out + static_cast<uint64_t>(y) * a.out_ld + x), f = __builtin_bit_cast(float4, v);
-          if (a.add) { const float4 o = *to; f.x += o.x; f.y += o.y; f.z += o.z; f.w += o.w; }
-          *to = f;
-        });
-      }
+      for (int j = 0; j < NJ; ++j)
+#pragma unroll
+        for (int i = 0; i < NI; ++i) {
+          put_f32(own, lane, acc[i][j]);
+          take<8>(own, lane, [&](uint32_t row, uint32_t piece, uint4 v) {
+            const uint32_t y = y0 + wy + 32 * j + row, x = x0 + wx + 32 * i + 4 * piece;
+            if (y >= ny || x >= a.out_ld) return;              // whole fours: out_ld is the padded dimension
+            float4 *to = reinterpret_cast<float4 *>(out + static_cast<uint64_t>(y) * a.out_ld + x), f = __builtin_bit_cast(float4, v);
+            if (a.add) { const float4 o = *to; f.x += o.x; f.y += o.y; f.z += o.z; f.w += o.w; }
+            *to = f;
+          });
+        }
     }
     if constexpr (MODE == DW) {
       if (a.out_bf16) {
         uint16_t *const out = static_cast<uint16_t *>(a.out);
         const bool whole = a.out_ld % 8 == 0;
+        static_assert(MODE != DW || NI % 2 == 0, "two blocks at a time");
 #pragma unroll
-        for (int j = 0; j < NJ; ++j) {
+        for (int j = 0; j < NJ; ++j)
 #pragma unroll
-          for (int i = 0; i < NI; ++i)
+          for (int i0 = 0; i0 < NI; i0 += 2) {
 #pragma unroll
-            for (int q = 0; q < 4; ++q)
-              put_bf16<NI>(own, lane, i, q, f32x2_to_bf16x2_rne(acc[i][j][4 * q], acc[i][j][4 * q + 1]), f32x2_to_bf16x2_rne(acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]));
-          take<NI * 4>(own, lane, [&](uint32_t row, uint32_t piece, uint4 v) {
-            const uint32_t y = y0 + wy + 32 * j + row, x = x0 + wx + 8 * piece;
-            if (y >= ny || x >= a.nx) return;
-            uint16_t *to = out + static_cast<uint64_t>(y) * a.out_ld + x;
-            const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-            if (whole && x + 8 <= a.nx) *reinterpret_cast<uint4 *>(to) = v;
-            else
+            for (int i = 0; i < 2; ++i)
 #pragma unroll
-              for (int e = 0; e < 8; ++e)
-                if (x + e < a.nx) to[e] = static_cast<uint16_t>(w[e / 2] >> (16 * (e & 1)));
-          });
-        }
+              for (int q = 0; q < 4; ++q)
+                put_bf16<8>(own, lane, i, q, f32x2_to_bf16x2_rne(acc[i0 + i][j][4 * q], acc[i0 + i][j][4 * q + 1]),
+                            f32x2_to_bf16x2_rne(acc[i0 + i][j][4 * q + 2], acc[i0 + i][j][4 * q + 3]));
+            take<8>(own, lane, [&](uint32_t row, uint32_t piece, uint4 v) {
+              const uint32_t y = y0 + wy + 32 * j + row, x = x0 + wx + 32 * i0 + 8 * piece;
+              if (y >= ny || x >= a.nx) return;
+              uint16_t *to = out + static_cast<uint64_t>(y) * a.out_ld + x;
+              const uint32_t h[4] = {v.x, v.y, v.z, v.w};
+              if (whole && x + 8 <= a.nx) *reinterpret_cast<uint4 *>(to) = v;
+              else
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                  if (x + e < a.nx) to[e] = static_cast<uint16_t>(h[e / 2] >> (16 * (e & 1)));
+            });
+          }
       } else {
         float *const out = static_cast<float *>(a.out);
         const bool whole = a.out_ld % 4 == 0;
 #pragma unroll
-        for (int j = 0; j < NJ; ++j) {
-          put_f32<NI>(own, lane, acc, j);
-          take<NI * 8>(own, lane, [&](uint32_t row, uint32_t piece, uint4 v) {
-            const uint32_t y = y0 + wy + 32 * j + row, x = x0 + wx + 4 * piece;
-            if (y >= ny || x >= a.nx) return;
-            float *to = out + static_cast<uint64_t>(y) * a.out_ld + x;
-            const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-            if (whole && x + 4 <= a.nx) *reinterpret_cast<uint4 *>(to) = v;
-            else
+        for (int j = 0; j < NJ; ++j)
 #pragma unroll
-              for (int e = 0; e < 4; ++e)
-                if (x + e < a.nx) to[e] = u2f(w[e]);
-          });
-        }
+          for (int i = 0; i < NI; ++i) {
+            put_f32(own, lane, acc[i][j]);
+            take<8>(own, lane, [&](uint32_t row, uint32_t piece, uint4 v) {
+              const uint32_t y = y0 + wy + 32 * j + row, x = x0 + wx + 32 * i + 4 * piece;
+              if (y >= ny || x >= a.nx) return;
+              float *to = out + static_cast<uint64_t>(y) * a.out_ld + x;
+              const uint32_t h[4] = {v.x, v.y, v.z, v.w};
+              if (whole && x + 4 <= a.nx) *reinterpret_cast<uint4 *>(to) = v;
+              else
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                  if (x + e < a.nx) to[e] = u2f(h[e]);
+            });
+          }
       }
     }
   }
@@ -892,21 +927,27 @@ uint32_t blocks_for(uint64_t work) { return static_cast<uint32_t>(work < 256 * 8
 
 // Tiles by the number of rows.
 using Large = Tile<256, 256, 2, 4, 2>;
-using Medium = Tile<256, 128, 4, 2, 3>;
+using Medium = Tile<128, 128, 2, 2, 2>;
 using Small = Tile<128, 64, 4, 1, 3>;
+using SmallF32 = Tile<128, 64, 4, 1, 2>;
 enum Shape { SMALL, MEDIUM, LARGE };
 Shape shape_for(uint64_t rows) { return rows <= 64 ? SMALL : rows <= 1024 ? MEDIUM : LARGE; }
+
+constexpr uint32_t UNITS = 256;                   // compute units
 
 template <int MODE, class T>
 hipError_t launch_tiles(ProductArgs a, uint32_t x, uint32_t y, hipStream_t s) {
   a.tiles_x = (x + T::BX - 1) / T::BX;
-  hipLaunchKernelGGL((eco_head_product_kernel<MODE, T>), dim3(a.tiles_x * ((y + T::BY - 1) / T::BY) * a.splits), dim3(T::THREADS), 0, s, a);
+  // as many workgroups as the chip holds, by their LDS
+  constexpr uint32_t resident = UNITS * (163840 / (T::DEPTH * T::STEP_BYTES + extra_bytes<MODE, T>()));
+  const uint64_t tiles = static_cast<uint64_t>(a.tiles_x) * ((y + T::BY - 1) / T::BY) * a.splits;
+  hipLaunchKernelGGL((eco_head_product_kernel<MODE, T>), dim3(static_cast<uint32_t>(tiles < resident ? tiles : resident)), dim3(T::THREADS), 0, s, a);
   return hipGetLastError();
 }
 template <int MODE>
 hipError_t launch_product(const ProductArgs &a, uint64_t rows, uint32_t x, uint32_t y, hipStream_t s) {
   switch (shape_for(rows)) {
-    case SMALL: return launch_tiles<MODE, Small>(a, x, y, s);
+    case SMALL: return launch_tiles<MODE, std::conditional_t<MODE == DH, SmallF32, Small>>(a, x, y, s);
     case MEDIUM: return launch_tiles<MODE, Medium>(a, x, y, s);
     default: return launch_tiles<MODE, Large>(a, x, y, s);
   }
@@ -931,7 +972,6 @@ HeadTiles head_tiles(uint64_t rows) {
 }
 
 // Tiles run a compute unit's worth at a time: what part of the last round is busy.
-constexpr uint64_t UNITS = 256;
 double rounds(uint64_t tiles) { return static_cast<double>((tiles + UNITS - 1) / UNITS); }
 uint64_t ceil_div(uint64_t a, uint64_t b) { return (a + b - 1) / b; }
 
@@ -971,7 +1011,8 @@ uint32_t head_splits(uint64_t rows, uint64_t dim, uint64_t piece) {
     splits = ceil_div(shape == SMALL ? 768 : 512, tiles);
     if (splits > most) splits = most;
   }
-  return static_cast<uint32_t>(splits);
+  const uint64_t steps = ceil_div(piece, KSTEP);             // (every part of the first piece has a step)
+  return static_cast<uint32_t>(ceil_div(steps, ceil_div(steps, splits)));
 }
 
 template <class F>
@@ -1056,7 +1097,11 @@ hipError_t launch_head_scatter(const int32_t *ids, const float *values, uint32_t
 hipError_t launch_head_grad_hidden(const HeadOperand &w, const HeadOperand &g, uint32_t n, uint32_t rows, uint32_t dim, const int32_t *count, uint32_t splits,
                                    float *partial, uint32_t partial_ld, uint64_t partial_stride, int add, hipStream_t s) {
   ProductArgs a = product(w, g);
-  a.nx = dim; a.k = n; a.count = count; a.splits = splits;
+  a.nx = dim; a.k = n; a.count = count;
+  // no part is empty: a last, shorter piece of the vocabulary may make do with fewer
+  const uint32_t steps = (n + KSTEP - 1) / KSTEP;
+  a.split_steps = (steps + splits - 1) / splits;
+  a.splits = (steps + a.split_steps - 1) / a.split_steps;
   a.out_f32 = partial; a.out_ld = partial_ld; a.out_plane = partial_stride; a.add = add;
   return launch_product<DH>(a, rows, dim, rows, s);
 }
