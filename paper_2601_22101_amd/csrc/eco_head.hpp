@@ -53,9 +53,12 @@ struct HeadStats {                                // the logits' statistics by r
 
 hipError_t launch_head_rows(const HeadRows &, void *compact, uint32_t padded_rows, uint32_t padded_dim, hipStream_t);
 hipError_t launch_head_convert(const HeadWeights &, uint64_t first, uint32_t rows, uint32_t dim, void *planes, uint32_t ld, uint64_t plane, hipStream_t);
-// logits' statistics of vocabulary rows first .. first + n - 1, whose tiles begin at `tile`
-hipError_t launch_head_stats(const HeadOperand &w, const HeadOperand &h, uint32_t n, uint32_t rows, uint32_t dim, const int32_t *count, float inv_tau,
-                             const HeadStats &, uint32_t tile, hipStream_t);
+// Workgroups of the kernel for few rows over `vocab` rows of weights, which reads them as they are stored; 0: it does not take the call.
+uint32_t head_few(const HeadWeights &, int hidden_bf16, uint64_t rows, uint64_t dim, uint64_t vocab);
+// logits' statistics of vocabulary rows first .. first + n - 1, whose tiles begin at `tile`; `few`: the weights for that kernel, then one tile to a
+// workgroup, or null
+hipError_t launch_head_stats(const HeadOperand &w, const HeadWeights *few, uint64_t first, const HeadOperand &h, uint32_t n, uint32_t rows, uint32_t dim,
+                             const int32_t *count, float inv_tau, const HeadStats &, uint32_t tile, hipStream_t);
 hipError_t launch_head_finish(const HeadRows &, const HeadWeights &, const HeadStats &, float *ce, float *kd, float *lse, float *lse_tau, float *picked,
                               hipStream_t);
 
@@ -68,7 +71,7 @@ struct HeadRowConst { float lse2, a, lse2_tau, b; };
 hipError_t launch_head_entries(const HeadRows &, uint32_t padded_rows, const float *grad_ce, const float *grad_kd, const float *lse, const float *lse_tau,
                                const float *picked, int softmaxes, int32_t *ids, float *values, HeadRowConst *consts, hipStream_t);
 // g[row][v] of a piece: planes of [padded rows][ld]
-hipError_t launch_head_grad(const HeadOperand &w, const HeadOperand &h, uint32_t n, uint32_t rows, uint32_t dim, const int32_t *count, float inv_tau, int softmaxes,
+hipError_t launch_head_grad(const HeadOperand &w, const HeadWeights *few, uint64_t first, const HeadOperand &h, uint32_t n, uint32_t rows, uint32_t dim, const int32_t *count, float inv_tau, int softmaxes,
                             const HeadRowConst *, void *g, uint32_t g_ld, uint64_t g_plane, uint32_t g_planes, hipStream_t);
 hipError_t launch_head_scatter(const int32_t *ids, const float *values, uint32_t rows, uint32_t entries, const int32_t *count, uint64_t first, uint32_t n, void *g,
                                uint32_t g_ld, uint64_t g_plane, uint32_t g_planes, hipStream_t);

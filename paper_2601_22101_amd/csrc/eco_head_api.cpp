@@ -87,9 +87,15 @@ eco_status_t check_backward(const eco_head_t *h) {
   return ECO_OK;
 }
 
+eco::HeadWeights weights_of(const eco_head_t *h) {
+  // a group that holds the whole tensor has the one scale
+  const uint64_t all = h->vocab * h->dim, group = h->group_size < all ? h->group_size : eco::HEAD_MOST_VOCAB * eco::HEAD_MOST_DIM;
+  return {h->weights, h->scales, stride_or(h->weight_stride, h->dim), group, h->fmt, h->scale_dtype == ECO_DT_BF16, eco::log2_exact(group)};
+}
+
 // The arrays of a workspace and the pieces of the vocabulary that a call goes by.
 struct Layout {
-  uint32_t padded_rows, padded_dim, entries, piece, hidden_planes, weight_planes, grad_planes, tiles, splits;
+  uint32_t padded_rows, padded_dim, entries, piece, hidden_planes, weight_planes, grad_planes, tiles, splits, few;
   bool in_place, two;
   uint64_t count, order, place, flags, compact, planes, max, sum, sum_tau, ids, values, consts, g, partial, bytes;
 };
@@ -120,11 +126,14 @@ Layout layout_of(const eco_head_t *h, bool backward) {
     const uint64_t most = PIECE_BYTES / row_bytes / 256 * 256;
     if (piece > most) piece = most < 1024 ? 1024 : most;
   };
-  if (!l.in_place) limit(2ull * l.padded_dim * l.weight_planes);
+  // few rows: the logits' kernel of the forward pass reads any format where it lies
+  l.few = eco::head_few(weights_of(h), h->hidden_dtype == ECO_DT_BF16, h->rows, h->dim, h->vocab);
+  const bool converts = !l.in_place && (backward || !l.few);
+  if (converts) limit(2ull * l.padded_dim * l.weight_planes);
   if (backward) limit(2ull * l.padded_rows * l.grad_planes);
   if (backward) piece = eco::head_piece(h->rows, h->dim, h->vocab, piece);
   l.piece = static_cast<uint32_t>(piece);
-  l.tiles = static_cast<uint32_t>((h->vocab + tile.vocab - 1) / tile.vocab);
+  l.tiles = l.few ? l.few : static_cast<uint32_t>((h->vocab + tile.vocab - 1) / tile.vocab);
   uint64_t at = 0;
   const auto take = [&at](uint64_t bytes) { const uint64_t here = at; at += eco::head_round_up(bytes, 256); return here; };
   l.count = take(4);
@@ -132,7 +141,7 @@ Layout layout_of(const eco_head_t *h, bool backward) {
   l.place = take(4 * h->rows);
   l.flags = take(h->top_k ? h->rows : 0);
   l.compact = take(2ull * l.hidden_planes * l.padded_rows * l.padded_dim);
-  if (!l.in_place) l.planes = take(2ull * l.weight_planes * piece * l.padded_dim);
+  if (converts) l.planes = take(2ull * l.weight_planes * piece * l.padded_dim);
   if (!backward) {
     l.max = take(4ull * h->rows * l.tiles);
     l.sum = take(4ull * h->rows * l.tiles);
@@ -170,12 +179,6 @@ eco::HeadRows rows_of(const eco_head_t *h, const Layout &l, char *ws) {
   r.flags = reinterpret_cast<uint8_t *>(ws + l.flags);
   r.hidden_whole = r.dim % 8 == 0 && r.hidden_stride % (r.hidden_bf16 ? 8 : 4) == 0 && aligned(h->hidden, 16);
   return r;
-}
-
-eco::HeadWeights weights_of(const eco_head_t *h) {
-  // a group that holds the whole tensor has the one scale
-  const uint64_t all = h->vocab * h->dim, group = h->group_size < all ? h->group_size : eco::HEAD_MOST_VOCAB * eco::HEAD_MOST_DIM;
-  return {h->weights, h->scales, stride_or(h->weight_stride, h->dim), group, h->fmt, h->scale_dtype == ECO_DT_BF16, eco::log2_exact(group)};
 }
 
 eco::HeadOperand hidden_operand(const Layout &l, char *ws) {
@@ -228,13 +231,14 @@ eco_status_t eco_head_loss(const eco_head_t *head, void *workspace, size_t works
   const eco::HeadStats stats = {reinterpret_cast<float *>(ws + l.max), reinterpret_cast<float *>(ws + l.sum),
                                 l.two ? reinterpret_cast<float *>(ws + l.sum_tau) : nullptr, l.tiles};
   const uint32_t tile = eco::head_tiles(r.rows).vocab;
+  const eco::HeadWeights weights = weights_of(head);
   for (uint64_t first = 0; first < head->vocab; first += l.piece) {
     const uint32_t n = static_cast<uint32_t>(head->vocab - first < l.piece ? head->vocab - first : l.piece);
-    eco::HeadOperand w;
-    HEAD_LAUNCH(weight_operand(head, l, ws, first, n, s, &w));
-    HEAD_LAUNCH(eco::launch_head_stats(w, hidden_operand(l, ws), n, r.rows, r.dim, r.count, 1.0f / r.tau, stats, static_cast<uint32_t>(first / tile), s));
+    eco::HeadOperand w = {};
+    if (!l.few) HEAD_LAUNCH(weight_operand(head, l, ws, first, n, s, &w));
+    HEAD_LAUNCH(eco::launch_head_stats(w, l.few ? &weights : nullptr, first, hidden_operand(l, ws), n, r.rows, r.dim, r.count, 1.0f / r.tau, stats, static_cast<uint32_t>(first / tile), s));
   }
-  HEAD_LAUNCH(eco::launch_head_finish(r, weights_of(head), stats, head->labels ? head->ce : nullptr, head->top_k ? head->kd : nullptr,
+  HEAD_LAUNCH(eco::launch_head_finish(r, weights, stats, head->labels ? head->ce : nullptr, head->top_k ? head->kd : nullptr,
                                       head->labels ? head->lse : nullptr, head->top_k ? head->lse_tau : nullptr, head->picked, s));
   return ECO_OK;
 }
@@ -261,11 +265,12 @@ eco_status_t eco_head_loss_backward(const eco_head_t *head, void *workspace, siz
   const uint64_t g_plane = static_cast<uint64_t>(l.padded_rows) * l.piece, partial_stride = static_cast<uint64_t>(l.padded_rows) * l.padded_dim;
   const eco::HeadOperand g = {ws + l.g, g_plane, l.piece, l.grad_planes}, hidden = hidden_operand(l, ws);
   const uint64_t out_stride = stride_or(head->grad_weights_stride, head->dim);
+  const eco::HeadWeights weights = weights_of(head);
   for (uint64_t first = 0; first < head->vocab; first += l.piece) {
     const uint32_t n = static_cast<uint32_t>(head->vocab - first < l.piece ? head->vocab - first : l.piece);
     eco::HeadOperand w;
     HEAD_LAUNCH(weight_operand(head, l, ws, first, n, s, &w));
-    HEAD_LAUNCH(eco::launch_head_grad(w, hidden, n, r.rows, r.dim, r.count, 1.0f / r.tau, softmaxes, consts, ws + l.g, l.piece, g_plane, l.grad_planes, s));
+    HEAD_LAUNCH(eco::launch_head_grad(w, l.few ? &weights : nullptr, first, hidden, n, r.rows, r.dim, r.count, 1.0f / r.tau, softmaxes, consts, ws + l.g, l.piece, g_plane, l.grad_planes, s));
     HEAD_LAUNCH(eco::launch_head_scatter(ids, values, r.rows, l.entries, r.count, first, n, ws + l.g, l.piece, g_plane, l.grad_planes, s));
     HEAD_LAUNCH(eco::launch_head_grad_hidden(w, g, n, r.rows, r.dim, r.count, l.splits, partial, l.padded_dim, partial_stride, first != 0, s));
     char *out = static_cast<char *>(head->grad_weights) + first * out_stride * size_of(head->grad_weights_dtype);

@@ -360,7 +360,7 @@ __global__ __launch_bounds__(T::THREADS) void eco_head_product_kernel(ProductArg
   const int wx = wave % T::WX * (NI * 32), wy = wave / T::WX * (NJ * 32);
   const uint32_t all_steps = MODE == DW ? (count + KSTEP - 1) / KSTEP : (a.k + KSTEP - 1) / KSTEP;
   // the last step's end: past it pieces repeat valid ones of their row, or rows the last one, against zeros of the other operand
-  const uint32_t tail = MODE == DW ? 0 : a.k % KSTEP;
+  const uint32_t tail = (MODE == DW ? count : a.k) % KSTEP;
   const uint64_t step_x = X_COLUMN ? static_cast<uint64_t>(KSTEP) * a.ldx : KSTEP, step_y = Y_COLUMN ? static_cast<uint64_t>(KSTEP) * a.ldy : KSTEP;
 
   struct Where { uint32_t x0, y0, split, first, steps; };
@@ -439,7 +439,16 @@ __global__ __launch_bounds__(T::THREADS) void eco_head_product_kernel(ProductArg
       load_to_lds(lds + i * T::THREADS * 16, from_x, off);
     }
 #pragma unroll
-    for (int i = 0; i < T::Y_LOADS; ++i) load_to_lds(lds + T::X_BYTES + i * T::THREADS * 16, from_y, off_y[i]);
+    for (int i = 0; i < T::Y_LOADS; ++i) {
+      uint32_t off = off_y[i];
+      if constexpr (MODE == DW)
+        if (end) {
+          uint32_t n, k;
+          column_piece<T::BY>(threadIdx.x + i * T::THREADS, n, k);
+          if (k >= tail) off -= (k - (tail - 1)) * a.ldy * 2;
+        }
+      load_to_lds(lds + T::X_BYTES + i * T::THREADS * 16, from_y, off);
+    }
     place = place + 1 == T::DEPTH ? 0 : place + 1;
     ++issued;
     if (++in_pair == load_steps) {
@@ -699,6 +708,215 @@ __global__ __launch_bounds__(T::THREADS) void eco_head_product_kernel(ProductArg
             });
           }
       }
+    }
+  }
+}
+
+// ------------------------------------------------------------------------------------------------ few rows
+
+// The logits of up to 64 rows are bound by the reading of the weights, which the tiles above do at 4 TB/s: a barrier a step keeps too little
+// under way (the memory answers after 2 us at that rate).  Here each wave reads rows of weights by itself, straight into the registers in which the
+// matrix core takes them, AHEAD pieces of every row ahead of the one that it multiplies, and decodes quantized ones there; the hidden states are in LDS as a
+// whole.  FORMAT's piece is 16 bytes a lane: PIECE elements, of which 4 lanes of a row read 4 PIECE next to each other.
+template <int FMT>
+struct Piece {
+  static constexpr int ELEMS = FMT == FMT_INT4 ? 32 : FMT == FMT_FP8 ? 16 : 8;
+  static constexpr int LOADS = FMT == FMT_FP32_ID ? 2 : 1;
+  static constexpr int UNIT = 4 * ELEMS;                       // along a row, of one load of a wave
+  static constexpr int AHEAD = FMT == FMT_BF16_PLAIN ? 8 : 4;
+};
+template <int BLOCKS> constexpr int few_rows_of_blocks() { return BLOCKS <= 2 ? 1 : 2; }
+constexpr int FEW_WAVES = 8;
+typedef float f32x4_t __attribute__((ext_vector_type(4)));
+
+// A row of hidden states in LDS: whole units, and 16 bytes so that rows begin in different banks.
+template <int FMT>
+constexpr uint32_t few_row_elems(uint32_t dim) { return (dim + Piece<FMT>::UNIT - 1) / Piece<FMT>::UNIT * Piece<FMT>::UNIT + 8; }
+
+template <int MODE, int FMT, int BLOCKS>
+__global__ __launch_bounds__(FEW_WAVES * 64) void eco_head_few_kernel(ProductArgs a, HeadWeights w, uint64_t first, uint32_t dim, uint32_t lds_row) {
+  using P = Piece<FMT>;
+  constexpr int AHEAD = P::AHEAD, R = few_rows_of_blocks<BLOCKS>(), PLANES = FMT == FMT_BF16_PLAIN ? 1 : FMT == FMT_FP32_ID ? 3 : 2;
+  extern __shared__ __attribute__((aligned(16))) uint16_t few_lds[];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), of_four = lane >> 4, n = lane & 15;
+  // (g has zeros up to a whole step of the products that read it)
+  constexpr uint32_t rows_each = 16 * R, whole = MODE == STATS ? rows_each : KSTEP;
+  const uint32_t groups = (a.nx + whole - 1) / whole * (whole / rows_each), units = (lds_row - 8) / P::UNIT, ahead_units = (units + AHEAD - 1) / AHEAD * AHEAD, stride = gridDim.x * FEW_WAVES;
+  const uint64_t row_bytes = FMT == FMT_BF16_PLAIN ? w.stride * 2 : FMT == FMT_FP32_ID ? w.stride * 4 : FMT == FMT_FP8 ? dim : dim / 2;
+  uint4 ahead[AHEAD][R][P::LOADS];
+  float scale[AHEAD][R];
+  // (rows past the last repeat it and are left out below; pieces past the row's end repeat its first against zeros of the hidden states)
+  const auto load = [&](int p, uint32_t group, uint32_t unit) {
+    const uint32_t at = unit * P::UNIT + of_four * P::ELEMS, k = at < dim ? at : 0;
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      const uint64_t row = first + min(group * rows_each + 16 * r + n, a.nx - 1);
+      const char *from = static_cast<const char *>(w.data) + row * row_bytes + static_cast<uint64_t>(k) * 16 * P::LOADS / P::ELEMS;
+#pragma unroll
+      for (int l = 0; l < P::LOADS; ++l) ahead[p][r][l] = *reinterpret_cast<const uint4 *>(from + 16 * l);
+      if constexpr (FMT == FMT_FP8 || FMT == FMT_INT4) scale[p][r] = scale_at(w, row * dim + k);
+    }
+  };
+  uint32_t group = blockIdx.x * FEW_WAVES + wave;
+  float m[BLOCKS], s[BLOCKS], s_tau[BLOCKS];
+#pragma unroll
+  for (int b = 0; b < BLOCKS; ++b) { m[b] = -INFINITY; s[b] = s_tau[b] = 0.0f; }
+  if (group < groups) {
+#pragma unroll
+    for (int p = 0; p < AHEAD; ++p) load(p, group, p);
+  }
+  const uint32_t count = static_cast<uint32_t>(*a.count);
+  if (count == 0) return;
+  for (uint32_t i = threadIdx.x; i < BLOCKS * 16 * (lds_row / 8); i += FEW_WAVES * 64) {
+    const uint32_t row = i / (lds_row / 8), k = i % (lds_row / 8) * 8;
+    *reinterpret_cast<uint4 *>(few_lds + row * lds_row + k) = k < a.ldy ? *reinterpret_cast<const uint4 *>(a.y + static_cast<uint64_t>(row) * a.ldy + k) : make_uint4(0, 0, 0, 0);
+  }
+  __syncthreads();
+  for (; group < groups; group += stride) {
+    f32x4_t acc[R][BLOCKS] = {};
+    const uint32_t next = min(group + stride, groups - 1);
+    for (uint32_t u = 0; u < ahead_units; u += AHEAD) {
+      const bool last = u + AHEAD >= ahead_units;
+#pragma unroll
+      for (int p = 0; p < AHEAD; ++p) {
+        if (u + p < units)
+#pragma unroll
+        for (int e = 0; e < P::ELEMS / 8; ++e) {
+          bf16x8 h[BLOCKS], x[R][PLANES];
+#pragma unroll
+          for (int b = 0; b < BLOCKS; ++b)
+            h[b] = *reinterpret_cast<const bf16x8 *>(few_lds + (16 * b + n) * lds_row + (u + p) * P::UNIT + of_four * P::ELEMS + 8 * e);
+#pragma unroll
+          for (int r = 0; r < R; ++r) {
+            if constexpr (FMT == FMT_BF16_PLAIN) x[r][0] = __builtin_bit_cast(bf16x8, ahead[p][r][0]);
+            else {
+              float v[8];
+              const uint32_t word[8] = {ahead[p][r][0].x, ahead[p][r][0].y, ahead[p][r][0].z, ahead[p][r][0].w,
+                                        ahead[p][r][P::LOADS - 1].x, ahead[p][r][P::LOADS - 1].y, ahead[p][r][P::LOADS - 1].z, ahead[p][r][P::LOADS - 1].w};
+              if constexpr (FMT == FMT_FP32_ID) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) v[i] = u2f(word[i]);
+              } else if constexpr (FMT == FMT_FP8) {
+                const uint32_t lo = word[2 * e], hi = word[2 * e + 1];
+                v[0] = e4m3_decode<0>(lo); v[1] = e4m3_decode<1>(lo); v[2] = e4m3_decode<2>(lo); v[3] = e4m3_decode<3>(lo);
+                v[4] = e4m3_decode<0>(hi); v[5] = e4m3_decode<1>(hi); v[6] = e4m3_decode<2>(hi); v[7] = e4m3_decode<3>(hi);
+              } else {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) v[i] = static_cast<float>(static_cast<int32_t>(word[e] << (28 - 4 * i)) >> 28);
+              }
+              if constexpr (FMT != FMT_FP32_ID)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) v[i] *= scale[p][r];
+#pragma unroll
+              for (int q = 0; q < PLANES; ++q) {
+                uint32_t two[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                  two[i] = f32x2_to_bf16x2_rne(v[2 * i], v[2 * i + 1]);
+                  v[2 * i] -= bf16_lo(two[i]);
+                  v[2 * i + 1] -= bf16_hi(two[i]);
+                }
+                x[r][q] = __builtin_bit_cast(bf16x8, make_uint4(two[0], two[1], two[2], two[3]));
+              }
+            }
+          }
+#pragma unroll
+          for (int q = 0; q < PLANES; ++q)
+#pragma unroll
+            for (int r = 0; r < R; ++r)
+#pragma unroll
+              for (int b = 0; b < BLOCKS; ++b) acc[r][b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x[r][q], h[b], acc[r][b], 0, 0, 0);
+        }
+        load(p, last ? next : group, last ? p : u + p + AHEAD);
+      }
+    }
+    // acc[r][b][i]: vocabulary 16 r + 4 of_four + i of the group, row 16 b + n
+    const uint32_t v0 = group * rows_each + 4 * of_four;
+#pragma unroll
+    for (int b = 0; b < BLOCKS; ++b) {
+      if constexpr (MODE == STATS) {
+        float best = m[b];
+#pragma unroll
+        for (int r = 0; r < R; ++r)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            if (v0 + 16 * r + i >= a.nx) acc[r][b][i] = -INFINITY;
+            best = fmaxf(best, acc[r][b][i]);
+          }
+        const float base = best == -INFINITY ? 0.0f : best;
+        const auto add = [&](float &sum, float c) {
+          sum *= exp2_fast((m[b] - base) * c);
+#pragma unroll
+          for (int r = 0; r < R; ++r)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) sum += exp2_fast((acc[r][b][i] - base) * c);
+        };
+        add(s[b], a.scale2);
+        if (a.two) add(s_tau[b], a.scale2_tau);
+        m[b] = best;
+      } else {
+        const uint32_t y = 16 * b + n;
+        const HeadRowConst rc = a.consts[y];
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+          const uint32_t x = v0 + 16 * r;
+          float g[4];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            g[i] = rc.a * exp2_fast(fmaf(acc[r][b][i], a.scale2, -rc.lse2));
+            if (a.two) g[i] = fmaf(rc.b, exp2_fast(fmaf(acc[r][b][i], a.scale2_tau, -rc.lse2_tau)), g[i]);
+            if (x + i >= a.nx) g[i] = 0.0f;
+          }
+          uint16_t *out = static_cast<uint16_t *>(a.out) + static_cast<uint64_t>(y) * a.out_ld + x;
+          if (y < count)
+            for (uint32_t p = 0; p < a.out_planes; ++p) {
+              uint32_t two[4];
+#pragma unroll
+              for (int i = 0; i < 4; ++i) next_plane(g[i], two[i]);
+              *reinterpret_cast<uint2 *>(out + p * a.out_plane) = make_uint2(two[0] | two[1] << 16, two[2] | two[3] << 16);
+            }
+        }
+      }
+    }
+  }
+  if constexpr (MODE == STATS) {
+    // a workgroup's statistics are one tile's: its lanes' joined, then its waves'
+    __syncthreads();
+    float *red = reinterpret_cast<float *>(few_lds);           // [3][wave][row]
+#pragma unroll
+    for (int b = 0; b < BLOCKS; ++b) {
+      float best = fmaxf(m[b], __shfl_xor(m[b], 16));
+      best = fmaxf(best, __shfl_xor(best, 32));
+      const float base = best == -INFINITY ? 0.0f : best;
+      s[b] *= exp2_fast((m[b] - base) * a.scale2);
+      s[b] += __shfl_xor(s[b], 16);
+      s[b] += __shfl_xor(s[b], 32);
+      s_tau[b] *= exp2_fast((m[b] - base) * a.scale2_tau);
+      s_tau[b] += __shfl_xor(s_tau[b], 16);
+      s_tau[b] += __shfl_xor(s_tau[b], 32);
+      if (of_four == 0) {
+        red[wave * BLOCKS * 16 + 16 * b + n] = best;
+        red[(FEW_WAVES + wave) * BLOCKS * 16 + 16 * b + n] = s[b];
+        red[(2 * FEW_WAVES + wave) * BLOCKS * 16 + 16 * b + n] = s_tau[b];
+      }
+    }
+    __syncthreads();
+    const uint32_t y = threadIdx.x;
+    if (y < BLOCKS * 16 && y < count) {
+      float best = -INFINITY, sum = 0.0f, sum_tau = 0.0f;
+#pragma unroll
+      for (int q = 0; q < FEW_WAVES; ++q) best = fmaxf(best, red[q * BLOCKS * 16 + y]);
+      const float base = best == -INFINITY ? 0.0f : best;
+#pragma unroll
+      for (int q = 0; q < FEW_WAVES; ++q) {
+        const float d = red[q * BLOCKS * 16 + y] - base;
+        sum = fmaf(red[(FEW_WAVES + q) * BLOCKS * 16 + y], exp2_fast(d * a.scale2), sum);
+        sum_tau = fmaf(red[(2 * FEW_WAVES + q) * BLOCKS * 16 + y], exp2_fast(d * a.scale2_tau), sum_tau);
+      }
+      const uint64_t to = static_cast<uint64_t>(y) * a.tiles + blockIdx.x;
+      a.out_f32[to] = best;
+      a.sum[to] = sum;
+      if (a.two) a.sum_tau[to] = sum_tau;
     }
   }
 }
@@ -1061,15 +1279,62 @@ hipError_t launch_head_convert(const HeadWeights &w, uint64_t first, uint32_t ro
   });
 }
 
-hipError_t launch_head_stats(const HeadOperand &w, const HeadOperand &h, uint32_t n, uint32_t rows, uint32_t dim, const int32_t *count, float inv_tau,
-                             const HeadStats &st, uint32_t tile, hipStream_t s) {
+// Whether the kernel for few rows takes a call: its hidden states fit LDS, and its pieces are whole and have one scale each.
+template <int FMT>
+uint32_t few_lds(const HeadWeights &w, uint64_t rows, uint64_t dim) {
+  using P = Piece<FMT>;
+  const bool quantized = FMT == FMT_FP8 || FMT == FMT_INT4;
+  if (dim % P::ELEMS || (quantized ? w.group % P::ELEMS : w.stride * (FMT == FMT_BF16_PLAIN ? 2 : 4) % 16)) return 0;
+  const uint64_t blocks = rows <= 16 ? 1 : rows <= 32 ? 2 : 4, bytes = blocks * 16 * 2 * few_row_elems<FMT>(static_cast<uint32_t>(dim));
+  const uint64_t joined = blocks * 16 * FEW_WAVES * 3 * 4;                // the waves' statistics take the place of the hidden states at the end
+  return bytes <= 163840 ? static_cast<uint32_t>(bytes > joined ? bytes : joined) : 0;
+}
+uint32_t few_lds(const HeadWeights &w, uint64_t rows, uint64_t dim) {
+  switch (w.fmt) {
+    case FMT_FP8: return few_lds<FMT_FP8>(w, rows, dim);
+    case FMT_INT4: return few_lds<FMT_INT4>(w, rows, dim);
+    case FMT_BF16_PLAIN: return few_lds<FMT_BF16_PLAIN>(w, rows, dim);
+    default: return few_lds<FMT_FP32_ID>(w, rows, dim);
+  }
+}
+uint32_t head_few(const HeadWeights &w, int hidden_bf16, uint64_t rows, uint64_t dim, uint64_t vocab) {
+  const uint32_t lds = hidden_bf16 && rows <= 64 ? few_lds(w, rows, dim) : 0;
+  if (!lds) return 0;
+  const uint64_t each = 16 * (rows <= 32 ? 1 : 2) * FEW_WAVES, groups = ceil_div(vocab, each), most = UNITS * (lds <= 81920 ? 2 : 1);
+  return static_cast<uint32_t>(groups < most ? groups : most);
+}
+
+template <int MODE, int FMT>
+hipError_t launch_few(const ProductArgs &a, const HeadWeights &w, uint64_t first, uint32_t rows, uint32_t dim, hipStream_t s) {
+  const uint32_t lds_row = few_row_elems<FMT>(dim), lds = few_lds<FMT>(w, rows, dim);
+  const auto go = [&](auto blocks) {
+    const auto kernel = eco_head_few_kernel<MODE, FMT, blocks.value>;
+    const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, 163840);
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL(kernel, dim3(head_few(w, 1, rows, dim, a.nx)), dim3(FEW_WAVES * 64), lds, s, a, w, first, dim, lds_row);
+    return hipGetLastError();
+  };
+  return rows <= 16 ? go(std::integral_constant<int, 1>{}) : rows <= 32 ? go(std::integral_constant<int, 2>{}) : go(std::integral_constant<int, 4>{});
+}
+template <int MODE>
+hipError_t launch_few(const ProductArgs &a, const HeadWeights &w, uint64_t first, uint32_t rows, uint32_t dim, hipStream_t s) {
+  switch (w.fmt) {
+    case FMT_FP8: return launch_few<MODE, FMT_FP8>(a, w, first, rows, dim, s);
+    case FMT_INT4: return launch_few<MODE, FMT_INT4>(a, w, first, rows, dim, s);
+    case FMT_BF16_PLAIN: return launch_few<MODE, FMT_BF16_PLAIN>(a, w, first, rows, dim, s);
+    default: return launch_few<MODE, FMT_FP32_ID>(a, w, first, rows, dim, s);
+  }
+}
+
+hipError_t launch_head_stats(const HeadOperand &w, const HeadWeights *few, uint64_t first, const HeadOperand &h, uint32_t n, uint32_t rows, uint32_t dim,
+                             const int32_t *count, float inv_tau, const HeadStats &st, uint32_t tile, hipStream_t s) {
   ProductArgs a = product(w, h);
   a.nx = n; a.k = dim; a.count = count;
   a.two = st.sum_tau != nullptr;
   a.scale2 = a.two ? LOG2E : LOG2E * inv_tau;
   a.scale2_tau = LOG2E * inv_tau;
   a.out_f32 = st.max; a.sum = st.sum; a.sum_tau = st.sum_tau; a.tiles = st.tiles; a.tile0 = tile;
-  return launch_product<STATS>(a, rows, n, rows, s);
+  return few ? launch_few<STATS>(a, *few, first, rows, dim, s) : launch_product<STATS>(a, rows, n, rows, s);
 }
 
 hipError_t launch_head_finish(const HeadRows &r, const HeadWeights &w, const HeadStats &st, float *ce, float *kd, float *lse, float *lse_tau, float *picked,
@@ -1085,12 +1350,13 @@ hipError_t launch_head_entries(const HeadRows &r, uint32_t padded_rows, const fl
   return hipGetLastError();
 }
 
-hipError_t launch_head_grad(const HeadOperand &w, const HeadOperand &h, uint32_t n, uint32_t rows, uint32_t dim, const int32_t *count, float inv_tau, int softmaxes,
+hipError_t launch_head_grad(const HeadOperand &w, const HeadWeights *few, uint64_t first, const HeadOperand &h, uint32_t n, uint32_t rows, uint32_t dim, const int32_t *count, float inv_tau, int softmaxes,
                             const HeadRowConst *consts, void *g, uint32_t g_ld, uint64_t g_plane, uint32_t g_planes, hipStream_t s) {
   ProductArgs a = product(w, h);
   a.nx = n; a.k = dim; a.count = count; a.two = softmaxes == HEAD_BOTH;
   a.scale2 = softmaxes == HEAD_TEACHER ? LOG2E * inv_tau : LOG2E; a.scale2_tau = LOG2E * inv_tau;
   a.consts = consts; a.out = g; a.out_ld = g_ld; a.out_plane = g_plane; a.out_planes = g_planes;
+  if (few) return launch_few<GRAD>(a, *few, first, rows, dim, s);
   return g_planes == 1 ? launch_product<GRAD>(a, rows, n, rows, s) : launch_product<GRAD_PLANES>(a, rows, n, rows, s);
 }
 
