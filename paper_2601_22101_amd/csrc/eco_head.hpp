@@ -59,7 +59,8 @@ uint32_t head_few(const HeadWeights &, int hidden_bf16, uint64_t rows, uint64_t 
 // workgroup, or null
 hipError_t launch_head_stats(const HeadOperand &w, const HeadWeights *few, uint64_t first, const HeadOperand &h, uint32_t n, uint32_t rows, uint32_t dim,
                              const int32_t *count, float inv_tau, const HeadStats &, uint32_t tile, hipStream_t);
-hipError_t launch_head_finish(const HeadRows &, const HeadWeights &, const HeadStats &, float *ce, float *kd, float *lse, float *lse_tau, float *picked,
+// `dotted`: the logits at the entries are in `picked` already
+hipError_t launch_head_finish(const HeadRows &, const HeadWeights &, const HeadStats &, int dotted, float *ce, float *kd, float *lse, float *lse_tau, float *picked,
                               hipStream_t);
 
 // Which softmaxes the logits' gradient is made of: the labels', both, the teacher's, or both where a temperature of 1 makes them the same.
@@ -70,6 +71,11 @@ struct HeadRowConst { float lse2, a, lse2_tau, b; };
 // entries: ids [rows][top_k + 1] (-1: none) and the gradient of the logit at each, over compact rows; consts: the padded rows
 hipError_t launch_head_entries(const HeadRows &, uint32_t padded_rows, const float *grad_ce, const float *grad_kd, const float *lse, const float *lse_tau,
                                const float *picked, int softmaxes, int32_t *ids, float *values, HeadRowConst *consts, hipStream_t);
+// At most 64 rows: launch_head_rows with the logits at the entries, or with launch_head_entries, in one launch.
+constexpr uint32_t HEAD_FEW_ROWS = 64;
+hipError_t launch_head_few_rows(const HeadRows &, const HeadWeights &, void *compact, uint32_t padded_rows, uint32_t padded_dim, float *picked, hipStream_t);
+hipError_t launch_head_few_rows_backward(const HeadRows &, void *compact, uint32_t padded_rows, uint32_t padded_dim, const float *grad_ce, const float *grad_kd, const float *lse,
+                                         const float *lse_tau, const float *picked, int softmaxes, int32_t *ids, float *values, HeadRowConst *consts, hipStream_t);
 // g[row][v] of a piece: planes of [padded rows][ld]
 hipError_t launch_head_grad(const HeadOperand &w, const HeadWeights *few, uint64_t first, const HeadOperand &h, uint32_t n, uint32_t rows, uint32_t dim, const int32_t *count, float inv_tau, int softmaxes,
                             const HeadRowConst *, void *g, uint32_t g_ld, uint64_t g_plane, uint32_t g_planes, hipStream_t);

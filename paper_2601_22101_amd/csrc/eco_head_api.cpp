@@ -227,18 +227,20 @@ eco_status_t eco_head_loss(const eco_head_t *head, void *workspace, size_t works
   char *ws = static_cast<char *>(workspace);
   hipStream_t s = static_cast<hipStream_t>(stream);
   const eco::HeadRows r = rows_of(head, l, ws);
-  HEAD_LAUNCH(eco::launch_head_rows(r, ws + l.compact, l.padded_rows, l.padded_dim, s));
+  const eco::HeadWeights weights = weights_of(head);
+  const bool few = r.rows <= eco::HEAD_FEW_ROWS;
+  if (few) HEAD_LAUNCH(eco::launch_head_few_rows(r, weights, ws + l.compact, l.padded_rows, l.padded_dim, head->picked, s));
+  else HEAD_LAUNCH(eco::launch_head_rows(r, ws + l.compact, l.padded_rows, l.padded_dim, s));
   const eco::HeadStats stats = {reinterpret_cast<float *>(ws + l.max), reinterpret_cast<float *>(ws + l.sum),
                                 l.two ? reinterpret_cast<float *>(ws + l.sum_tau) : nullptr, l.tiles};
   const uint32_t tile = eco::head_tiles(r.rows).vocab;
-  const eco::HeadWeights weights = weights_of(head);
   for (uint64_t first = 0; first < head->vocab; first += l.piece) {
     const uint32_t n = static_cast<uint32_t>(head->vocab - first < l.piece ? head->vocab - first : l.piece);
     eco::HeadOperand w = {};
     if (!l.few) HEAD_LAUNCH(weight_operand(head, l, ws, first, n, s, &w));
     HEAD_LAUNCH(eco::launch_head_stats(w, l.few ? &weights : nullptr, first, hidden_operand(l, ws), n, r.rows, r.dim, r.count, 1.0f / r.tau, stats, static_cast<uint32_t>(first / tile), s));
   }
-  HEAD_LAUNCH(eco::launch_head_finish(r, weights, stats, head->labels ? head->ce : nullptr, head->top_k ? head->kd : nullptr,
+  HEAD_LAUNCH(eco::launch_head_finish(r, weights, stats, few, head->labels ? head->ce : nullptr, head->top_k ? head->kd : nullptr,
                                       head->labels ? head->lse : nullptr, head->top_k ? head->lse_tau : nullptr, head->picked, s));
   return ECO_OK;
 }
@@ -254,14 +256,19 @@ eco_status_t eco_head_loss_backward(const eco_head_t *head, void *workspace, siz
   char *ws = static_cast<char *>(workspace);
   hipStream_t s = static_cast<hipStream_t>(stream);
   const eco::HeadRows r = rows_of(head, l, ws);
-  HEAD_LAUNCH(eco::launch_head_rows(r, ws + l.compact, l.padded_rows, l.padded_dim, s));
   const float *grad_ce = head->labels ? head->grad_ce : nullptr, *grad_kd = head->top_k ? head->grad_kd : nullptr;
   const int softmaxes = grad_ce && grad_kd ? (l.two ? eco::HEAD_BOTH : eco::HEAD_SAME) : grad_ce ? eco::HEAD_LABELS : eco::HEAD_TEACHER;
   int32_t *ids = reinterpret_cast<int32_t *>(ws + l.ids);
   float *values = reinterpret_cast<float *>(ws + l.values), *partial = reinterpret_cast<float *>(ws + l.partial);
   eco::HeadRowConst *consts = reinterpret_cast<eco::HeadRowConst *>(ws + l.consts);
-  HEAD_LAUNCH(eco::launch_head_entries(r, l.padded_rows, grad_ce, grad_kd, head->labels ? head->lse : nullptr, head->top_k ? head->lse_tau : nullptr, head->picked,
-                                       softmaxes, ids, values, consts, s));
+  const float *lse = head->labels ? head->lse : nullptr, *lse_tau = head->top_k ? head->lse_tau : nullptr;
+  if (r.rows <= eco::HEAD_FEW_ROWS) {
+    HEAD_LAUNCH(eco::launch_head_few_rows_backward(r, ws + l.compact, l.padded_rows, l.padded_dim, grad_ce, grad_kd, lse, lse_tau, head->picked, softmaxes, ids, values,
+                                                   consts, s));
+  } else {
+    HEAD_LAUNCH(eco::launch_head_rows(r, ws + l.compact, l.padded_rows, l.padded_dim, s));
+    HEAD_LAUNCH(eco::launch_head_entries(r, l.padded_rows, grad_ce, grad_kd, lse, lse_tau, head->picked, softmaxes, ids, values, consts, s));
+  }
   const uint64_t g_plane = static_cast<uint64_t>(l.padded_rows) * l.piece, partial_stride = static_cast<uint64_t>(l.padded_rows) * l.padded_dim;
   const eco::HeadOperand g = {ws + l.g, g_plane, l.piece, l.grad_planes}, hidden = hidden_operand(l, ws);
   const uint64_t out_stride = stride_or(head->grad_weights_stride, head->dim);

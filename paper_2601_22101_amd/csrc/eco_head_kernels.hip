@@ -951,11 +951,36 @@ __device__ Teacher teacher_of(const HeadRows &r, uint64_t row, int lane) {
   return {m, wave_sum(s)};
 }
 
-// A row's losses: the logits at the label and at the teacher's entries as dot products of their own (in fp32, from the weights as
-// they are stored), the tiles' statistics joined, and the sums over the teacher's entries.  The dot products are bound by the latency of rows of
-// weights that lie anywhere: a wave has the loads of DOTS rows under way.
+// The logits at COUNT of a row's entries (0 is the label, then the teacher's) from the j0th on, as dot products of their own: in fp32, from the weights as
+// they are stored.  They are bound by the latency of rows of weights that lie anywhere: a wave has the loads of COUNT rows under way.
+template <int FMT, bool WHOLE, int COUNT>
+__device__ __forceinline__ void dots(const HeadRows &r, const HeadWeights &w, uint32_t row, int32_t label, uint32_t j0, int lane, float (&sum)[COUNT]) {
+  int32_t id[COUNT];
+#pragma unroll
+  for (int e = 0; e < COUNT; ++e) {
+    id[e] = j0 + e > r.top_k ? -1 : j0 + e == 0 ? label : teacher_id(r, row, j0 + e - 1);
+    sum[e] = 0.0f;
+  }
+  for (uint32_t k = lane * 8; k < r.dim; k += 512) {
+    float h[8];
+    hidden8(r, row, k, h);
+#pragma unroll
+    for (int e = 0; e < COUNT; ++e) {
+      if (id[e] < 0) continue;
+      float v[8];
+      weights8<FMT, WHOLE>(w, id[e], r.dim, k, v);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) sum[e] = fmaf(h[i], v[i], sum[e]);
+    }
+  }
+#pragma unroll
+  for (int e = 0; e < COUNT; ++e) sum[e] = wave_sum(sum[e]);
+}
+
+// A row's losses: the logits at its entries (`dotted`: they are in `picked` already), the tiles' statistics joined, and the sums over the
+// teacher's entries.
 template <int FMT, bool WHOLE>
-__global__ __launch_bounds__(256) void eco_head_finish_kernel(HeadRows r, HeadWeights w, HeadStats st, float *ce, float *kd, float *lse, float *lse_tau, float *picked) {
+__global__ __launch_bounds__(256) void eco_head_finish_kernel(HeadRows r, HeadWeights w, HeadStats st, int dotted, float *ce, float *kd, float *lse, float *lse_tau, float *picked) {
   constexpr int DOTS = 8;
   __shared__ float z[HEAD_MOST_TOP_K + 1], red[4][3];
   const uint32_t row = blockIdx.x;
@@ -973,30 +998,15 @@ __global__ __launch_bounds__(256) void eco_head_finish_kernel(HeadRows r, HeadWe
     return;
   }
   const int32_t label = label_of(r, row);
-  for (uint32_t j0 = wave * DOTS; j0 < entries; j0 += 4 * DOTS) {
-    int32_t id[DOTS];
-    float sum[DOTS];
+  if (dotted) {
+    for (uint32_t j = threadIdx.x; j < entries; j += 256) z[j] = picked[static_cast<uint64_t>(row) * entries + j];
+  } else {
+    for (uint32_t j0 = wave * DOTS; j0 < entries; j0 += 4 * DOTS) {
+      float sum[DOTS];
+      dots<FMT, WHOLE>(r, w, row, label, j0, lane, sum);
 #pragma unroll
-    for (int e = 0; e < DOTS; ++e) {
-      id[e] = j0 + e >= entries ? -1 : j0 + e == 0 ? label : teacher_id(r, row, j0 + e - 1);
-      sum[e] = 0.0f;
-    }
-    for (uint32_t k = lane * 8; k < r.dim; k += 512) {
-      float h[8];
-      hidden8(r, row, k, h);
-#pragma unroll
-      for (int e = 0; e < DOTS; ++e) {
-        if (id[e] < 0) continue;
-        float v[8];
-        weights8<FMT, WHOLE>(w, id[e], r.dim, k, v);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) sum[e] = fmaf(h[i], v[i], sum[e]);
-      }
-    }
-#pragma unroll
-    for (int e = 0; e < DOTS; ++e) {
-      sum[e] = wave_sum(sum[e]);
-      if (lane == 0 && j0 + e < entries) z[j0 + e] = sum[e];
+      for (int e = 0; e < DOTS; ++e)
+        if (lane == 0 && j0 + e < entries) z[j0 + e] = sum[e];
     }
   }
   // the tiles' statistics
@@ -1019,7 +1029,8 @@ __global__ __launch_bounds__(256) void eco_head_finish_kernel(HeadRows r, HeadWe
   s_tau = wave_sum(s_tau);
   if (lane == 0) { red[wave][1] = s; red[wave][2] = s_tau; }
   __syncthreads();
-  for (uint32_t j = threadIdx.x; j < entries; j += 256) picked[static_cast<uint64_t>(row) * entries + j] = z[j];
+  if (!dotted)
+    for (uint32_t j = threadIdx.x; j < entries; j += 256) picked[static_cast<uint64_t>(row) * entries + j] = z[j];
   if (wave) return;
   s = red[0][1] + red[1][1] + red[2][1] + red[3][1];
   s_tau = red[0][2] + red[1][2] + red[2][2] + red[3][2];
@@ -1048,29 +1059,31 @@ __global__ __launch_bounds__(256) void eco_head_finish_kernel(HeadRows r, HeadWe
 
 // ------------------------------------------------------------------------------------------------ gradients beside the products
 
-// For each compact row: the constants of its softmax, and the gradient of the logit at the label and at each of the teacher's
-// entries, which replaces what the product's end writes there.  An id that comes up again in its row is left to the first one.
-__global__ __launch_bounds__(64) void eco_head_entries_kernel(HeadRows r, const float *grad_ce, const float *grad_kd, const float *lse, const float *lse_tau,
-                                                              const float *picked, int softmaxes, int32_t *ids, float *values, HeadRowConst *consts) {
-  __shared__ int32_t id_of[HEAD_MOST_TOP_K + 1];
-  __shared__ float q_of[HEAD_MOST_TOP_K + 1];
-  const uint32_t c = blockIdx.x, entries = r.top_k + 1;
-  const int lane = threadIdx.x;
-  if (c >= static_cast<uint32_t>(*r.count)) {
-    if (lane == 0) consts[c] = {0.0f, 0.0f, 0.0f, 0.0f};
+struct EntryArgs {
+  const float *grad_ce, *grad_kd, *lse, *lse_tau, *picked;
+  int32_t softmaxes, *ids;
+  float *values;
+  HeadRowConst *consts;
+};
+
+// For compact row c, which is `row` (-1: none): the constants of its softmax, and the gradient of the logit at the label and at each of the teacher's
+// entries, which replaces what the product's end writes there.  An id that comes up again in its row is left to the first one.  By one wave.
+__device__ void entries_of(const HeadRows &r, const EntryArgs &a, uint32_t c, int64_t row, int lane, int32_t *id_of, float *q_of) {
+  const uint32_t entries = r.top_k + 1;
+  if (row < 0) {
+    if (lane == 0) a.consts[c] = {0.0f, 0.0f, 0.0f, 0.0f};
     return;
   }
-  const uint64_t row = static_cast<uint64_t>(r.order[c]);
   const int32_t label = label_of(r, row);
   const float it = 1.0f / r.tau;
   Teacher q = {-INFINITY, 0.0f};
   if (r.top_k) q = teacher_of(r, row, lane);
   const bool taught = q.sum != 0.0f;
-  const float a = label >= 0 && grad_ce ? grad_ce[row] : 0.0f, b = taught && grad_kd ? grad_kd[row] * r.tau : 0.0f;
-  const float l1 = lse ? lse[row] : 0.0f, lt = lse_tau ? lse_tau[row] : 0.0f;
+  const float ga = label >= 0 && a.grad_ce ? a.grad_ce[row] : 0.0f, gb = taught && a.grad_kd ? a.grad_kd[row] * r.tau : 0.0f;
+  const float l1 = a.lse ? a.lse[row] : 0.0f, lt = a.lse_tau ? a.lse_tau[row] : 0.0f;
   if (lane == 0) {
-    if (softmaxes == HEAD_TEACHER) consts[c] = {lt * LOG2E, b, 0.0f, 0.0f};
-    else consts[c] = {l1 * LOG2E, softmaxes == HEAD_SAME ? a + b : a, lt * LOG2E, b};
+    if (a.softmaxes == HEAD_TEACHER) a.consts[c] = {lt * LOG2E, gb, 0.0f, 0.0f};
+    else a.consts[c] = {l1 * LOG2E, a.softmaxes == HEAD_SAME ? ga + gb : ga, lt * LOG2E, gb};
   }
   for (uint32_t j = lane; j < entries; j += 64) {
     id_of[j] = j == 0 ? label : taught ? teacher_id(r, row, j - 1) : -1;
@@ -1088,14 +1101,73 @@ __global__ __launch_bounds__(64) void eco_head_entries_kernel(HeadRows r, const 
           if (i < j) first = false;
           weight += q_of[i];
         }
-    ids[at] = first ? id : -1;
+    a.ids[at] = first ? id : -1;
     if (!first) continue;
-    const float z = picked[row * entries + j];
+    const float z = a.picked[row * entries + j];
     float g = 0.0f;
-    if (a != 0.0f) g = a * (exp2_fast((z - l1) * LOG2E) - (id == label ? 1.0f : 0.0f));
-    if (b != 0.0f) g = fmaf(b, exp2_fast((z * it - lt) * LOG2E) - weight, g);
-    values[at] = g;
+    if (ga != 0.0f) g = ga * (exp2_fast((z - l1) * LOG2E) - (id == label ? 1.0f : 0.0f));
+    if (gb != 0.0f) g = fmaf(gb, exp2_fast((z * it - lt) * LOG2E) - weight, g);
+    a.values[at] = g;
   }
+}
+
+__global__ __launch_bounds__(64) void eco_head_entries_kernel(HeadRows r, EntryArgs a) {
+  __shared__ int32_t id_of[HEAD_MOST_TOP_K + 1];
+  __shared__ float q_of[HEAD_MOST_TOP_K + 1];
+  const uint32_t c = blockIdx.x;
+  entries_of(r, a, c, c < static_cast<uint32_t>(*r.count) ? r.order[c] : -1, threadIdx.x, id_of, q_of);
+}
+
+// Few rows (at most 64): all that comes before the products in one launch of one-wave workgroups.  Each works out by itself which rows take part; the
+// first `padded` lay out a compact row each, and with `backward` its entries; in a forward pass the rest take a dot product each.
+template <int FMT, bool WHOLE>
+__global__ __launch_bounds__(64) void eco_head_few_rows_kernel(HeadRows r, HeadWeights w, EntryArgs a, uint16_t *compact, uint32_t padded, uint32_t ld, int backward,
+                                                               float *picked) {
+  __shared__ int32_t id_of[HEAD_MOST_TOP_K + 1];
+  __shared__ float q_of[HEAD_MOST_TOP_K + 1];
+  const int lane = threadIdx.x;
+  const auto takes_part = [&](uint32_t row) {
+    bool in = lane == 0 && label_of(r, row) >= 0;
+    for (uint32_t j = lane; j < r.top_k; j += 64) in = in || (teacher_id(r, row, j) >= 0 && teacher_logit(r, row, j) != -INFINITY);
+    return __ballot(in) != 0;
+  };
+  if (blockIdx.x >= padded) {
+    const uint32_t at = blockIdx.x - padded, entries = r.top_k + 1, row = at / entries;
+    float sum[1] = {0.0f};
+    if (takes_part(row)) dots<FMT, WHOLE>(r, w, row, label_of(r, row), at % entries, lane, sum);
+    if (lane == 0) picked[at] = sum[0];
+    return;
+  }
+  // a row a lane by its label and its first entry, which decide most, then the others one by one
+  const uint32_t mine = lane;
+  bool in = mine < r.rows && label_of(r, mine) >= 0;
+  if (mine < r.rows && r.top_k && !in) in = teacher_id(r, mine, 0) >= 0 && teacher_logit(r, mine, 0) != -INFINITY;
+  uint64_t part = __ballot(in);
+  if (r.top_k > 1)
+    for (uint64_t open = __ballot(mine < r.rows && !in); open; open &= open - 1) {
+      const uint32_t row = __ffsll(static_cast<unsigned long long>(open)) - 1;
+      part |= static_cast<uint64_t>(takes_part(row)) << row;
+    }
+  const uint32_t c = blockIdx.x, count = __popcll(part);
+  if (c == 0) {
+    const bool here = part >> lane & 1;
+    const int32_t at = __popcll(part & ((1ull << lane) - 1));
+    if (mine < r.rows) r.place[lane] = here ? at : -1;
+    if (here) r.order[at] = lane;
+    if (lane == 0) *r.count = static_cast<int32_t>(count);
+  }
+  int64_t row = -1;                                            // the cth that takes part
+  if (c < count) {
+    uint64_t rest = part;
+    for (uint32_t i = 0; i < c; ++i) rest &= rest - 1;
+    row = __ffsll(static_cast<unsigned long long>(rest)) - 1;
+  }
+  for (uint32_t k = lane * 8; k < ld; k += 512) {
+    float v[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+    if (row >= 0 && k < r.dim) hidden8(r, row, k, v);
+    store_planes(v, compact + static_cast<uint64_t>(c) * ld + k, static_cast<uint64_t>(padded) * ld, head_hidden_planes(r.hidden_bf16));
+  }
+  if (backward) entries_of(r, a, c, row, lane, id_of, q_of);
 }
 
 __global__ __launch_bounds__(256) void eco_head_scatter_kernel(const int32_t *ids, const float *values, uint32_t entries, const int32_t *count, uint64_t first, uint32_t n,
@@ -1337,16 +1409,32 @@ hipError_t launch_head_stats(const HeadOperand &w, const HeadWeights *few, uint6
   return few ? launch_few<STATS>(a, *few, first, rows, dim, s) : launch_product<STATS>(a, rows, n, rows, s);
 }
 
-hipError_t launch_head_finish(const HeadRows &r, const HeadWeights &w, const HeadStats &st, float *ce, float *kd, float *lse, float *lse_tau, float *picked,
+hipError_t launch_head_finish(const HeadRows &r, const HeadWeights &w, const HeadStats &st, int dotted, float *ce, float *kd, float *lse, float *lse_tau, float *picked,
                               hipStream_t s) {
   return by_format(w, r.dim, [&](auto fmt, auto whole) {
-    hipLaunchKernelGGL((eco_head_finish_kernel<fmt.value, whole.value>), dim3(r.rows), dim3(256), 0, s, r, w, st, ce, kd, lse, lse_tau, picked);
+    hipLaunchKernelGGL((eco_head_finish_kernel<fmt.value, whole.value>), dim3(r.rows), dim3(256), 0, s, r, w, st, dotted, ce, kd, lse, lse_tau, picked);
   });
 }
 
 hipError_t launch_head_entries(const HeadRows &r, uint32_t padded_rows, const float *grad_ce, const float *grad_kd, const float *lse, const float *lse_tau,
                                const float *picked, int softmaxes, int32_t *ids, float *values, HeadRowConst *consts, hipStream_t s) {
-  hipLaunchKernelGGL(eco_head_entries_kernel, dim3(padded_rows), dim3(64), 0, s, r, grad_ce, grad_kd, lse, lse_tau, picked, softmaxes, ids, values, consts);
+  const EntryArgs a = {grad_ce, grad_kd, lse, lse_tau, picked, softmaxes, ids, values, consts};
+  hipLaunchKernelGGL(eco_head_entries_kernel, dim3(padded_rows), dim3(64), 0, s, r, a);
+  return hipGetLastError();
+}
+
+hipError_t launch_head_few_rows(const HeadRows &r, const HeadWeights &w, void *compact, uint32_t padded_rows, uint32_t padded_dim, float *picked, hipStream_t s) {
+  return by_format(w, r.dim, [&](auto fmt, auto whole) {
+    hipLaunchKernelGGL((eco_head_few_rows_kernel<fmt.value, whole.value>), dim3(padded_rows + r.rows * (r.top_k + 1)), dim3(64), 0, s, r, w, EntryArgs{},
+                       static_cast<uint16_t *>(compact), padded_rows, padded_dim, 0, picked);
+  });
+}
+hipError_t launch_head_few_rows_backward(const HeadRows &r, void *compact, uint32_t padded_rows, uint32_t padded_dim, const float *grad_ce, const float *grad_kd, const float *lse,
+                                         const float *lse_tau, const float *picked, int softmaxes, int32_t *ids, float *values, HeadRowConst *consts, hipStream_t s) {
+  const EntryArgs a = {grad_ce, grad_kd, lse, lse_tau, picked, softmaxes, ids, values, consts};
+  // (no dot products: the format does not matter)
+  hipLaunchKernelGGL((eco_head_few_rows_kernel<FMT_BF16_PLAIN, true>), dim3(padded_rows), dim3(64), 0, s, r, HeadWeights{}, a, static_cast<uint16_t *>(compact), padded_rows,
+                     padded_dim, 1, static_cast<float *>(nullptr));
   return hipGetLastError();
 }
 
