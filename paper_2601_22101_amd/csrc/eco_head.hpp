@@ -57,7 +57,7 @@ hipError_t launch_head_convert(const HeadWeights &, uint64_t first, uint32_t row
 uint32_t head_few(const HeadWeights &, int hidden_bf16, uint64_t rows, uint64_t dim, uint64_t vocab);
 // logits' statistics of vocabulary rows first .. first + n - 1, whose tiles begin at `tile`; `few`: the weights for that kernel, then one tile to a
 // workgroup, or null
-hipError_t launch_head_stats(const HeadOperand &w, const HeadWeights *few, uint64_t first, const HeadOperand &h, uint32_t n, uint32_t rows, uint32_t dim,
+hipError_t launch_head_stats(int shape, const HeadOperand &w, const HeadWeights *few, uint64_t first, const HeadOperand &h, uint32_t n, uint32_t rows, uint32_t dim,
                              const int32_t *count, float inv_tau, const HeadStats &, uint32_t tile, hipStream_t);
 // `dotted`: the logits at the entries are in `picked` already
 hipError_t launch_head_finish(const HeadRows &, const HeadWeights &, const HeadStats &, int dotted, float *ce, float *kd, float *lse, float *lse_tau, float *picked,
@@ -77,20 +77,21 @@ hipError_t launch_head_few_rows(const HeadRows &, const HeadWeights &, void *com
 hipError_t launch_head_few_rows_backward(const HeadRows &, void *compact, uint32_t padded_rows, uint32_t padded_dim, const float *grad_ce, const float *grad_kd, const float *lse,
                                          const float *lse_tau, const float *picked, int softmaxes, int32_t *ids, float *values, HeadRowConst *consts, hipStream_t);
 // g[row][v] of a piece: planes of [padded rows][ld]
-hipError_t launch_head_grad(const HeadOperand &w, const HeadWeights *few, uint64_t first, const HeadOperand &h, uint32_t n, uint32_t rows, uint32_t dim, const int32_t *count, float inv_tau, int softmaxes,
+hipError_t launch_head_grad(int shape, const HeadOperand &w, const HeadWeights *few, uint64_t first, const HeadOperand &h, uint32_t n, uint32_t rows, uint32_t dim, const int32_t *count, float inv_tau, int softmaxes,
                             const HeadRowConst *, void *g, uint32_t g_ld, uint64_t g_plane, uint32_t g_planes, hipStream_t);
 hipError_t launch_head_scatter(const int32_t *ids, const float *values, uint32_t rows, uint32_t entries, const int32_t *count, uint64_t first, uint32_t n, void *g,
                                uint32_t g_ld, uint64_t g_plane, uint32_t g_planes, hipStream_t);
 // partial[s][compact row][dim] (+)= g w over a piece, s the split of the piece's vocabulary
-hipError_t launch_head_grad_hidden(const HeadOperand &w, const HeadOperand &g, uint32_t n, uint32_t rows, uint32_t dim, const int32_t *count, uint32_t splits,
+hipError_t launch_head_grad_hidden(int shape, const HeadOperand &w, const HeadOperand &g, uint32_t n, uint32_t rows, uint32_t dim, const int32_t *count, uint32_t splits,
                                    float *partial, uint32_t partial_ld, uint64_t partial_stride, int add, hipStream_t);
 hipError_t launch_head_grad_hidden_finish(const float *partial, uint32_t splits, uint32_t partial_ld, uint64_t partial_stride, const HeadRows &, void *out,
                                           uint64_t out_stride, hipStream_t);
-hipError_t launch_head_grad_weights(const HeadOperand &h, const HeadOperand &g, uint32_t n, uint32_t rows, uint32_t dim, const int32_t *count, void *out, uint64_t out_stride,
-                                    int out_bf16, hipStream_t);
+hipError_t launch_head_grad_weights(int shape, const HeadOperand &h, const HeadOperand &g, uint32_t n, uint32_t dim, const int32_t *count, void *out, uint64_t out_stride,
+                                    int out_bf16, int past_caches, hipStream_t);
 struct HeadTiles { uint32_t vocab, rows; };       // a tile of the logits
-HeadTiles head_tiles(uint64_t rows);
-uint64_t head_piece(uint64_t rows, uint64_t dim, uint64_t vocab, uint64_t most);          // vocabulary to a piece of the backward pass
-uint32_t head_splits(uint64_t rows, uint64_t dim, uint64_t piece);      // parts of a piece of the vocabulary that grad_hidden's product sums apart
+HeadTiles head_tiles(int shape);
+int head_shape(uint64_t rows, uint64_t vocab);    // which tiles a call's products have, for the launchers
+uint64_t head_piece(int shape, uint64_t rows, uint64_t dim, uint64_t vocab, uint64_t most);          // vocabulary to a piece of the backward pass
+uint32_t head_splits(int shape, uint64_t rows, uint64_t dim, uint64_t piece);      // parts of a piece of the vocabulary that grad_hidden's product sums apart
 
 }  // namespace eco

@@ -96,6 +96,7 @@ eco::HeadWeights weights_of(const eco_head_t *h) {
 // The arrays of a workspace and the pieces of the vocabulary that a call goes by.
 struct Layout {
   uint32_t padded_rows, padded_dim, entries, piece, hidden_planes, weight_planes, grad_planes, tiles, splits, few;
+  int shape;
   bool in_place, two;
   uint64_t count, order, place, flags, compact, planes, max, sum, sum_tau, ids, values, consts, g, partial, bytes;
 };
@@ -110,7 +111,8 @@ bool two_softmaxes(const eco_head_t *h) { return h->labels && h->top_k && static
 Layout layout_of(const eco_head_t *h, bool backward) {
   Layout l;
   std::memset(&l, 0, sizeof l);
-  const eco::HeadTiles tile = eco::head_tiles(h->rows);
+  l.shape = eco::head_shape(h->rows, h->vocab);
+  const eco::HeadTiles tile = eco::head_tiles(l.shape);
   l.padded_rows = static_cast<uint32_t>(eco::head_round_up(h->rows, tile.rows));      // compact rows: whole tiles, zero past the last one that takes part
   l.padded_dim = static_cast<uint32_t>(eco::head_round_up(h->dim, eco::HEAD_K_STEP));
   l.entries = h->top_k + 1;
@@ -131,7 +133,7 @@ Layout layout_of(const eco_head_t *h, bool backward) {
   const bool converts = !l.in_place && (backward || !l.few);
   if (converts) limit(2ull * l.padded_dim * l.weight_planes);
   if (backward) limit(2ull * l.padded_rows * l.grad_planes);
-  if (backward) piece = eco::head_piece(h->rows, h->dim, h->vocab, piece);
+  if (backward) piece = eco::head_piece(l.shape, h->rows, h->dim, h->vocab, piece);
   l.piece = static_cast<uint32_t>(piece);
   l.tiles = l.few ? l.few : static_cast<uint32_t>((h->vocab + tile.vocab - 1) / tile.vocab);
   uint64_t at = 0;
@@ -151,7 +153,7 @@ Layout layout_of(const eco_head_t *h, bool backward) {
     l.values = take(4ull * h->rows * l.entries);
     l.consts = take(sizeof(eco::HeadRowConst) * l.padded_rows);
     l.g = take(2ull * l.grad_planes * l.padded_rows * piece);
-    l.splits = eco::head_splits(h->rows, h->dim, piece < h->vocab ? piece : h->vocab);
+    l.splits = eco::head_splits(l.shape, h->rows, h->dim, piece < h->vocab ? piece : h->vocab);
     l.partial = take(4ull * l.splits * l.padded_rows * l.padded_dim);
   }
   l.bytes = at;
@@ -233,12 +235,12 @@ eco_status_t eco_head_loss(const eco_head_t *head, void *workspace, size_t works
   else HEAD_LAUNCH(eco::launch_head_rows(r, ws + l.compact, l.padded_rows, l.padded_dim, s));
   const eco::HeadStats stats = {reinterpret_cast<float *>(ws + l.max), reinterpret_cast<float *>(ws + l.sum),
                                 l.two ? reinterpret_cast<float *>(ws + l.sum_tau) : nullptr, l.tiles};
-  const uint32_t tile = eco::head_tiles(r.rows).vocab;
+  const uint32_t tile = eco::head_tiles(l.shape).vocab;
   for (uint64_t first = 0; first < head->vocab; first += l.piece) {
     const uint32_t n = static_cast<uint32_t>(head->vocab - first < l.piece ? head->vocab - first : l.piece);
     eco::HeadOperand w = {};
     if (!l.few) HEAD_LAUNCH(weight_operand(head, l, ws, first, n, s, &w));
-    HEAD_LAUNCH(eco::launch_head_stats(w, l.few ? &weights : nullptr, first, hidden_operand(l, ws), n, r.rows, r.dim, r.count, 1.0f / r.tau, stats, static_cast<uint32_t>(first / tile), s));
+    HEAD_LAUNCH(eco::launch_head_stats(l.shape, w, l.few ? &weights : nullptr, first, hidden_operand(l, ws), n, r.rows, r.dim, r.count, 1.0f / r.tau, stats, static_cast<uint32_t>(first / tile), s));
   }
   HEAD_LAUNCH(eco::launch_head_finish(r, weights, stats, few, head->labels ? head->ce : nullptr, head->top_k ? head->kd : nullptr,
                                       head->labels ? head->lse : nullptr, head->top_k ? head->lse_tau : nullptr, head->picked, s));
@@ -273,15 +275,18 @@ eco_status_t eco_head_loss_backward(const eco_head_t *head, void *workspace, siz
   const eco::HeadOperand g = {ws + l.g, g_plane, l.piece, l.grad_planes}, hidden = hidden_operand(l, ws);
   const uint64_t out_stride = stride_or(head->grad_weights_stride, head->dim);
   const eco::HeadWeights weights = weights_of(head);
+  // A gradient that the 256 MB cache in front of HBM cannot hold passes the caches by: on its way out it would take the place of the weights, which the next
+  // call reads (67 x 1152 x 262144, training, a pass: 722 us, 758 without).
+  const bool past_caches = head->vocab * head->dim * size_of(head->grad_weights_dtype) > (256u << 20);
   for (uint64_t first = 0; first < head->vocab; first += l.piece) {
     const uint32_t n = static_cast<uint32_t>(head->vocab - first < l.piece ? head->vocab - first : l.piece);
     eco::HeadOperand w;
     HEAD_LAUNCH(weight_operand(head, l, ws, first, n, s, &w));
-    HEAD_LAUNCH(eco::launch_head_grad(w, l.few ? &weights : nullptr, first, hidden, n, r.rows, r.dim, r.count, 1.0f / r.tau, softmaxes, consts, ws + l.g, l.piece, g_plane, l.grad_planes, s));
+    HEAD_LAUNCH(eco::launch_head_grad(l.shape, w, l.few ? &weights : nullptr, first, hidden, n, r.rows, r.dim, r.count, 1.0f / r.tau, softmaxes, consts, ws + l.g, l.piece, g_plane, l.grad_planes, s));
     HEAD_LAUNCH(eco::launch_head_scatter(ids, values, r.rows, l.entries, r.count, first, n, ws + l.g, l.piece, g_plane, l.grad_planes, s));
-    HEAD_LAUNCH(eco::launch_head_grad_hidden(w, g, n, r.rows, r.dim, r.count, l.splits, partial, l.padded_dim, partial_stride, first != 0, s));
+    HEAD_LAUNCH(eco::launch_head_grad_hidden(l.shape, w, g, n, r.rows, r.dim, r.count, l.splits, partial, l.padded_dim, partial_stride, first != 0, s));
     char *out = static_cast<char *>(head->grad_weights) + first * out_stride * size_of(head->grad_weights_dtype);
-    HEAD_LAUNCH(eco::launch_head_grad_weights(hidden, g, n, r.rows, r.dim, r.count, out, out_stride, head->grad_weights_dtype == ECO_DT_BF16, s));
+    HEAD_LAUNCH(eco::launch_head_grad_weights(l.shape, hidden, g, n, r.dim, r.count, out, out_stride, head->grad_weights_dtype == ECO_DT_BF16, past_caches, s));
   }
   HEAD_LAUNCH(eco::launch_head_grad_hidden_finish(partial, l.splits, l.padded_dim, partial_stride, r, head->grad_hidden,
                                                   stride_or(head->grad_hidden_stride, head->dim), s));

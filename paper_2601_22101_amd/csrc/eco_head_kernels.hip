@@ -228,7 +228,7 @@ struct ProductArgs {
   void *out;
   uint64_t out_ld, out_plane;
   uint32_t out_planes, tiles, tile0, splits, split_steps, tiles_x;
-  int32_t two, out_bf16, add;
+  int32_t two, out_bf16, add, past_caches;
   float *sum, *sum_tau;
   const HeadRowConst *consts;
 };
@@ -326,6 +326,11 @@ __device__ __forceinline__ void put_f32(lds_char *own, int lane, const f32x16 &a
   }
 }
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+__device__ __forceinline__ void store16(void *to, uint4 v, int past_caches) {
+  const u32x4 x = {v.x, v.y, v.z, v.w};
+  if (past_caches) __builtin_nontemporal_store(x, static_cast<u32x4 *>(to));
+  else *static_cast<u32x4 *>(to) = x;
+}
 template <int PIECES, class F>
 __device__ __forceinline__ void take(const lds_char *own, int lane, F store) {
 #pragma unroll
@@ -680,7 +685,7 @@ __global__ __launch_bounds__(T::THREADS) void eco_head_product_kernel(ProductArg
               if (y >= ny || x >= a.nx) return;
               uint16_t *to = out + static_cast<uint64_t>(y) * a.out_ld + x;
               const uint32_t h[4] = {v.x, v.y, v.z, v.w};
-              if (whole && x + 8 <= a.nx) *reinterpret_cast<uint4 *>(to) = v;
+              if (whole && x + 8 <= a.nx) store16(to, v, a.past_caches);
               else
 #pragma unroll
                 for (int e = 0; e < 8; ++e)
@@ -700,7 +705,7 @@ __global__ __launch_bounds__(T::THREADS) void eco_head_product_kernel(ProductArg
               if (y >= ny || x >= a.nx) return;
               float *to = out + static_cast<uint64_t>(y) * a.out_ld + x;
               const uint32_t h[4] = {v.x, v.y, v.z, v.w};
-              if (whole && x + 4 <= a.nx) *reinterpret_cast<uint4 *>(to) = v;
+              if (whole && x + 4 <= a.nx) store16(to, v, a.past_caches);
               else
 #pragma unroll
                 for (int e = 0; e < 4; ++e)
@@ -1220,16 +1225,16 @@ __global__ __launch_bounds__(256) void eco_head_grad_hidden_finish_kernel(const 
   }
 }
 
+uint64_t ceil_div(uint64_t a, uint64_t b) { return (a + b - 1) / b; }
 uint32_t blocks_for(uint64_t work) { return static_cast<uint32_t>(work < 256 * 8192 ? (work + 255) / 256 : 8192); }
 
-// Tiles by the number of rows.
+// Tiles.  The large ones are the faster ones where they are enough for the chip (training, us, large / medium: 130 x 1152 x 262144 967 / 1069, 400 1370 /
+// 1890, 1000 2413 / 3544; 256 x 2048 x 102400 668 / 757; 200 x 512 x 32000 120 / 90, 512 134 / 126, 1000 180 / 199; 70 x 1152 x 262144 933 / 735).
 using Large = Tile<256, 256, 2, 4, 2>;
 using Medium = Tile<128, 128, 2, 2, 2>;
 using Small = Tile<128, 64, 4, 1, 3>;
 using SmallF32 = Tile<128, 64, 4, 1, 2>;
-enum Shape { SMALL, MEDIUM, LARGE };
-Shape shape_for(uint64_t rows) { return rows <= 64 ? SMALL : rows <= 1024 ? MEDIUM : LARGE; }
-
+enum : int { SMALL = 0, MEDIUM = 1, LARGE = 2 };
 constexpr uint32_t UNITS = 256;                   // compute units
 
 template <int MODE, class T>
@@ -1242,8 +1247,8 @@ hipError_t launch_tiles(ProductArgs a, uint32_t x, uint32_t y, hipStream_t s) {
   return hipGetLastError();
 }
 template <int MODE>
-hipError_t launch_product(const ProductArgs &a, uint64_t rows, uint32_t x, uint32_t y, hipStream_t s) {
-  switch (shape_for(rows)) {
+hipError_t launch_product(const ProductArgs &a, int shape, uint32_t x, uint32_t y, hipStream_t s) {
+  switch (shape) {
     case SMALL: return launch_tiles<MODE, std::conditional_t<MODE == DH, SmallF32, Small>>(a, x, y, s);
     case MEDIUM: return launch_tiles<MODE, Medium>(a, x, y, s);
     default: return launch_tiles<MODE, Large>(a, x, y, s);
@@ -1260,8 +1265,12 @@ ProductArgs product(const HeadOperand &x, const HeadOperand &y) {
 
 }  // namespace
 
-HeadTiles head_tiles(uint64_t rows) {
-  switch (shape_for(rows)) {
+int head_shape(uint64_t rows, uint64_t vocab) {
+  if (rows <= 64) return SMALL;
+  return rows > 128 && ceil_div(rows, Large::BY) * ceil_div(vocab, Large::BX) >= UNITS ? LARGE : MEDIUM;
+}
+HeadTiles head_tiles(int shape) {
+  switch (shape) {
     case SMALL: return {Small::BX, Small::BY};
     case MEDIUM: return {Medium::BX, Medium::BY};
     default: return {Large::BX, Large::BY};
@@ -1270,12 +1279,11 @@ HeadTiles head_tiles(uint64_t rows) {
 
 // Tiles run a compute unit's worth at a time: what part of the last round is busy.
 double rounds(uint64_t tiles) { return static_cast<double>((tiles + UNITS - 1) / UNITS); }
-uint64_t ceil_div(uint64_t a, uint64_t b) { return (a + b - 1) / b; }
 
 // The piece of the vocabulary, at most `most`, whose tiles of the logits' gradient and of the weights' gradient take the least time in
 // rounds (with the inner axes' steps, and about eight steps of a tile's own at either end).  Tiles of one compute unit each.
-uint64_t head_piece(uint64_t rows, uint64_t dim, uint64_t vocab, uint64_t most) {
-  if (shape_for(rows) != LARGE) return most;
+uint64_t head_piece(int shape, uint64_t rows, uint64_t dim, uint64_t vocab, uint64_t most) {
+  if (shape != LARGE) return most;
   const uint64_t all = ceil_div(vocab, 256), row_tiles = ceil_div(rows, 256), dim_tiles = ceil_div(dim, 256);
   const uint64_t fewest = ceil_div(all, most / 256);
   double best = 0.0;
@@ -1293,9 +1301,8 @@ uint64_t head_piece(uint64_t rows, uint64_t dim, uint64_t vocab, uint64_t most) 
 
 // Parts of a piece of the vocabulary that grad_hidden's product sums apart, so that its tiles fill the compute units; each costs a
 // reading and a writing of its sums.
-uint32_t head_splits(uint64_t rows, uint64_t dim, uint64_t piece) {
-  const Shape shape = shape_for(rows);
-  const HeadTiles t = head_tiles(rows);
+uint32_t head_splits(int shape, uint64_t rows, uint64_t dim, uint64_t piece) {
+  const HeadTiles t = head_tiles(shape);
   const uint64_t tiles = ceil_div(dim, t.vocab) * ceil_div(rows, t.rows), most = ceil_div(piece, 512);
   uint64_t splits = 1;
   if (shape == LARGE) {
@@ -1398,7 +1405,7 @@ hipError_t launch_few(const ProductArgs &a, const HeadWeights &w, uint64_t first
   }
 }
 
-hipError_t launch_head_stats(const HeadOperand &w, const HeadWeights *few, uint64_t first, const HeadOperand &h, uint32_t n, uint32_t rows, uint32_t dim,
+hipError_t launch_head_stats(int shape, const HeadOperand &w, const HeadWeights *few, uint64_t first, const HeadOperand &h, uint32_t n, uint32_t rows, uint32_t dim,
                              const int32_t *count, float inv_tau, const HeadStats &st, uint32_t tile, hipStream_t s) {
   ProductArgs a = product(w, h);
   a.nx = n; a.k = dim; a.count = count;
@@ -1406,7 +1413,7 @@ hipError_t launch_head_stats(const HeadOperand &w, const HeadWeights *few, uint6
   a.scale2 = a.two ? LOG2E : LOG2E * inv_tau;
   a.scale2_tau = LOG2E * inv_tau;
   a.out_f32 = st.max; a.sum = st.sum; a.sum_tau = st.sum_tau; a.tiles = st.tiles; a.tile0 = tile;
-  return few ? launch_few<STATS>(a, *few, first, rows, dim, s) : launch_product<STATS>(a, rows, n, rows, s);
+  return few ? launch_few<STATS>(a, *few, first, rows, dim, s) : launch_product<STATS>(a, shape, n, rows, s);
 }
 
 hipError_t launch_head_finish(const HeadRows &r, const HeadWeights &w, const HeadStats &st, int dotted, float *ce, float *kd, float *lse, float *lse_tau, float *picked,
@@ -1438,14 +1445,14 @@ hipError_t launch_head_few_rows_backward(const HeadRows &r, void *compact, uint3
   return hipGetLastError();
 }
 
-hipError_t launch_head_grad(const HeadOperand &w, const HeadWeights *few, uint64_t first, const HeadOperand &h, uint32_t n, uint32_t rows, uint32_t dim, const int32_t *count, float inv_tau, int softmaxes,
+hipError_t launch_head_grad(int shape, const HeadOperand &w, const HeadWeights *few, uint64_t first, const HeadOperand &h, uint32_t n, uint32_t rows, uint32_t dim, const int32_t *count, float inv_tau, int softmaxes,
                             const HeadRowConst *consts, void *g, uint32_t g_ld, uint64_t g_plane, uint32_t g_planes, hipStream_t s) {
   ProductArgs a = product(w, h);
   a.nx = n; a.k = dim; a.count = count; a.two = softmaxes == HEAD_BOTH;
   a.scale2 = softmaxes == HEAD_TEACHER ? LOG2E * inv_tau : LOG2E; a.scale2_tau = LOG2E * inv_tau;
   a.consts = consts; a.out = g; a.out_ld = g_ld; a.out_plane = g_plane; a.out_planes = g_planes;
   if (few) return launch_few<GRAD>(a, *few, first, rows, dim, s);
-  return g_planes == 1 ? launch_product<GRAD>(a, rows, n, rows, s) : launch_product<GRAD_PLANES>(a, rows, n, rows, s);
+  return g_planes == 1 ? launch_product<GRAD>(a, shape, n, rows, s) : launch_product<GRAD_PLANES>(a, shape, n, rows, s);
 }
 
 hipError_t launch_head_scatter(const int32_t *ids, const float *values, uint32_t rows, uint32_t entries, const int32_t *count, uint64_t first, uint32_t n, void *g,
@@ -1455,7 +1462,7 @@ hipError_t launch_head_scatter(const int32_t *ids, const float *values, uint32_t
   return hipGetLastError();
 }
 
-hipError_t launch_head_grad_hidden(const HeadOperand &w, const HeadOperand &g, uint32_t n, uint32_t rows, uint32_t dim, const int32_t *count, uint32_t splits,
+hipError_t launch_head_grad_hidden(int shape, const HeadOperand &w, const HeadOperand &g, uint32_t n, uint32_t rows, uint32_t dim, const int32_t *count, uint32_t splits,
                                    float *partial, uint32_t partial_ld, uint64_t partial_stride, int add, hipStream_t s) {
   ProductArgs a = product(w, g);
   a.nx = dim; a.k = n; a.count = count;
@@ -1464,7 +1471,7 @@ hipError_t launch_head_grad_hidden(const HeadOperand &w, const HeadOperand &g, u
   a.split_steps = (steps + splits - 1) / splits;
   a.splits = (steps + a.split_steps - 1) / a.split_steps;
   a.out_f32 = partial; a.out_ld = partial_ld; a.out_plane = partial_stride; a.add = add;
-  return launch_product<DH>(a, rows, dim, rows, s);
+  return launch_product<DH>(a, shape, dim, rows, s);
 }
 
 hipError_t launch_head_grad_hidden_finish(const float *partial, uint32_t splits, uint32_t partial_ld, uint64_t partial_stride, const HeadRows &r, void *out,
@@ -1474,12 +1481,12 @@ hipError_t launch_head_grad_hidden_finish(const float *partial, uint32_t splits,
   return hipGetLastError();
 }
 
-hipError_t launch_head_grad_weights(const HeadOperand &h, const HeadOperand &g, uint32_t n, uint32_t rows, uint32_t dim, const int32_t *count, void *out, uint64_t out_stride,
-                                    int out_bf16, hipStream_t s) {
+hipError_t launch_head_grad_weights(int shape, const HeadOperand &h, const HeadOperand &g, uint32_t n, uint32_t dim, const int32_t *count, void *out, uint64_t out_stride,
+                                    int out_bf16, int past_caches, hipStream_t s) {
   ProductArgs a = product(h, g);
   a.nx = dim; a.ny = n; a.count = count;
-  a.out = out; a.out_ld = out_stride; a.out_bf16 = out_bf16;
-  return rows <= 1024 ? launch_tiles<DW, Medium>(a, dim, n, s) : launch_tiles<DW, Large>(a, dim, n, s);
+  a.out = out; a.out_ld = out_stride; a.out_bf16 = out_bf16; a.past_caches = past_caches;
+  return shape == LARGE ? launch_tiles<DW, Large>(a, dim, n, s) : launch_tiles<DW, Medium>(a, dim, n, s);
 }
 
 }  // namespace eco
