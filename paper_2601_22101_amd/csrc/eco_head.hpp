@@ -18,6 +18,13 @@ constexpr uint64_t head_round_up(uint64_t x, uint64_t k) { return (x + k - 1) / 
 constexpr int head_weight_planes(int fmt) { return fmt == 2 ? 1 : fmt == 3 ? 3 : 2; }
 constexpr int head_hidden_planes(int dtype_bf16) { return dtype_bf16 ? 1 : 3; }
 
+// Pairs of two operands' planes whose product counts: the sum of their places is at most 2, what is left out is below a relative 2^-22.
+constexpr uint32_t head_pairs(uint32_t x, uint32_t y) {
+  uint32_t n = 0;
+  for (uint32_t i = 0; i < x; ++i) n += y < 3 - i ? y : 3 - i;
+  return n;
+}
+
 struct HeadWeights {                              // where a row of weights comes from
   const void *data, *scales;
   uint64_t stride, group;                         // elements between rows (unquantized); elements per scale
@@ -92,6 +99,6 @@ struct HeadTiles { uint32_t vocab, rows; };       // a tile of the logits
 HeadTiles head_tiles(int shape);
 int head_shape(uint64_t rows, uint64_t vocab);    // which tiles a call's products have, for the launchers
 uint64_t head_piece(int shape, uint64_t rows, uint64_t dim, uint64_t vocab, uint64_t most);          // vocabulary to a piece of the backward pass
-uint32_t head_splits(int shape, uint64_t rows, uint64_t dim, uint64_t piece);      // parts of a piece of the vocabulary that grad_hidden's product sums apart
+uint32_t head_splits(int shape, uint64_t rows, uint64_t dim, uint64_t piece, uint32_t pairs);      // parts of a piece of the vocabulary that grad_hidden's product sums apart
 
 }  // namespace eco

@@ -153,7 +153,7 @@ Layout layout_of(const eco_head_t *h, bool backward) {
     l.values = take(4ull * h->rows * l.entries);
     l.consts = take(sizeof(eco::HeadRowConst) * l.padded_rows);
     l.g = take(2ull * l.grad_planes * l.padded_rows * piece);
-    l.splits = eco::head_splits(l.shape, h->rows, h->dim, piece < h->vocab ? piece : h->vocab);
+    l.splits = eco::head_splits(l.shape, h->rows, h->dim, piece < h->vocab ? piece : h->vocab, eco::head_pairs(l.weight_planes, l.grad_planes));
     l.partial = take(4ull * l.splits * l.padded_rows * l.padded_dim);
   }
   l.bytes = at;

@@ -280,12 +280,23 @@ __device__ __forceinline__ void row_piece(uint32_t c, uint32_t &n, uint32_t &k) 
   n = c >> 3;
   k = 8 * ((c & 7) ^ ((n >> 1) & 7));
 }
-__device__ __forceinline__ constexpr uint32_t column_swap(uint32_t k) { return 4 * (k & 3) | 2 * ((k >> 3) & 1); }
+// (Of a column operand whose rows are no power of two, rotated instead of exchanged: 192 elements are one and a half times the banks.)
+template <int N>
+__device__ __forceinline__ constexpr uint32_t column_place(uint32_t piece, uint32_t k) {
+  static_assert(N >= 128, "pieces go to places among 16");
+  if constexpr ((N & (N - 1)) == 0) return piece ^ (4 * (k & 3) | 2 * ((k >> 3) & 1));
+  const uint32_t at = piece + (12 * k & 12) + 2 * ((k >> 3) & 1);
+  return at < N / 8 ? at : at - N / 8;
+}
 template <int N>
 __device__ __forceinline__ void column_piece(uint32_t c, uint32_t &n, uint32_t &k) {
-  static_assert(N >= 128, "column_swap exchanges 16 pieces");
   k = c / (N / 8);
-  n = 8 * ((c % (N / 8)) ^ column_swap(k));
+  const uint32_t place = c % (N / 8);
+  if constexpr ((N & (N - 1)) == 0) n = 8 * column_place<N>(place, k);
+  else {
+    const uint32_t turn = (12 * k & 12) + 2 * ((k >> 3) & 1);
+    n = 8 * (place >= turn ? place - turn : place + N / 8 - turn);
+  }
 }
 
 typedef short s16x4 __attribute__((ext_vector_type(4)));
@@ -297,7 +308,7 @@ __device__ __forceinline__ bf16x8 fragment(const lds_char *step, int n0, int kk,
   if constexpr (COLUMN) {
     // a transposing read hands lane i of sixteen the elements n0 + i of four rows of k; lane i brings the address of a quarter of one row
     const int i = lane & 15, k = 16 * kk + 8 * (lane >> 5) + (i >> 2), n = n0 + 16 * ((lane >> 4) & 1) + 4 * (i & 3);
-    const lds_char *p = step + (k * N + 8 * ((n >> 3) ^ static_cast<int>(column_swap(k))) + (n & 7)) * 2;
+    const lds_char *p = step + (k * N + 8 * static_cast<int>(column_place<N>(n >> 3, k)) + (n & 7)) * 2;
     struct { s16x4 a, b; } v = {__builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4 *)p),
                                 __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4 *)(p + 8 * N))};
     return __builtin_bit_cast(bf16x8, v);
@@ -389,9 +400,7 @@ __global__ __launch_bounds__(T::THREADS) void eco_head_product_kernel(ProductArg
     return w;
   };
 
-  // pairs of planes whose product counts: the sum of their places is at most 2
-  uint32_t pairs = 0;
-  for (uint32_t px = 0; px < a.x_planes; ++px) pairs += min(a.y_planes, 3 - px);
+  const uint32_t pairs = head_pairs(a.x_planes, a.y_planes);
 
   // ---- the loads' place in the work
   uint32_t load_id = blockIdx.x, load_first, load_steps, in_pair, px, py, issued = 0, place = 0;
@@ -669,29 +678,32 @@ __global__ __launch_bounds__(T::THREADS) void eco_head_product_kernel(ProductArg
       if (a.out_bf16) {
         uint16_t *const out = static_cast<uint16_t *>(a.out);
         const bool whole = a.out_ld % 8 == 0;
-        static_assert(MODE != DW || NI % 2 == 0, "two blocks at a time");
+        const auto two_blocks = [&](int j, int i0, auto wide) {
+          constexpr int WIDE = decltype(wide)::value;
+#pragma unroll
+          for (int i = 0; i < WIDE; ++i)
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
+              put_bf16<4 * WIDE>(own, lane, i, q, f32x2_to_bf16x2_rne(acc[i0 + i][j][4 * q], acc[i0 + i][j][4 * q + 1]),
+                                 f32x2_to_bf16x2_rne(acc[i0 + i][j][4 * q + 2], acc[i0 + i][j][4 * q + 3]));
+          take<4 * WIDE>(own, lane, [&](uint32_t row, uint32_t piece, uint4 v) {
+            const uint32_t y = y0 + wy + 32 * j + row, x = x0 + wx + 32 * i0 + 8 * piece;
+            if (y >= ny || x >= a.nx) return;
+            uint16_t *to = out + static_cast<uint64_t>(y) * a.out_ld + x;
+            const uint32_t h[4] = {v.x, v.y, v.z, v.w};
+            if (whole && x + 8 <= a.nx) store16(to, v, a.past_caches);
+            else
+#pragma unroll
+              for (int e = 0; e < 8; ++e)
+                if (x + e < a.nx) to[e] = static_cast<uint16_t>(h[e / 2] >> (16 * (e & 1)));
+          });
+        };
 #pragma unroll
         for (int j = 0; j < NJ; ++j)
 #pragma unroll
-          for (int i0 = 0; i0 < NI; i0 += 2) {
-#pragma unroll
-            for (int i = 0; i < 2; ++i)
-#pragma unroll
-              for (int q = 0; q < 4; ++q)
-                put_bf16<8>(own, lane, i, q, f32x2_to_bf16x2_rne(acc[i0 + i][j][4 * q], acc[i0 + i][j][4 * q + 1]),
-                            f32x2_to_bf16x2_rne(acc[i0 + i][j][4 * q + 2], acc[i0 + i][j][4 * q + 3]));
-            take<8>(own, lane, [&](uint32_t row, uint32_t piece, uint4 v) {
-              const uint32_t y = y0 + wy + 32 * j + row, x = x0 + wx + 32 * i0 + 8 * piece;
-              if (y >= ny || x >= a.nx) return;
-              uint16_t *to = out + static_cast<uint64_t>(y) * a.out_ld + x;
-              const uint32_t h[4] = {v.x, v.y, v.z, v.w};
-              if (whole && x + 8 <= a.nx) store16(to, v, a.past_caches);
-              else
-#pragma unroll
-                for (int e = 0; e < 8; ++e)
-                  if (x + e < a.nx) to[e] = static_cast<uint16_t>(h[e / 2] >> (16 * (e & 1)));
-            });
-          }
+          for (int i0 = 0; i0 < NI; i0 += 2)
+            if (i0 + 1 < NI) two_blocks(j, i0, std::integral_constant<int, 2>{});
+            else two_blocks(j, i0, std::integral_constant<int, 1>{});
       } else {
         float *const out = static_cast<float *>(a.out);
         const bool whole = a.out_ld % 4 == 0;
@@ -1231,6 +1243,7 @@ uint32_t blocks_for(uint64_t work) { return static_cast<uint32_t>(work < 256 * 8
 // Tiles.  The large ones are the faster ones where they are enough for the chip (training, us, large / medium: 130 x 1152 x 262144 967 / 1069, 400 1370 /
 // 1890, 1000 2413 / 3544; 256 x 2048 x 102400 668 / 757; 200 x 512 x 32000 120 / 90, 512 134 / 126, 1000 180 / 199; 70 x 1152 x 262144 933 / 735).
 using Large = Tile<256, 256, 2, 4, 2>;
+using Large192 = Tile<192, 256, 2, 4, 2>;         // across the hidden dimension, where the others would be a quarter empty (1229 x 576 x 32128, both gradients 150 -> 119 us)
 using Medium = Tile<128, 128, 2, 2, 2>;
 using Small = Tile<128, 64, 4, 1, 3>;
 using SmallF32 = Tile<128, 64, 4, 1, 2>;
@@ -1269,6 +1282,12 @@ int head_shape(uint64_t rows, uint64_t vocab) {
   if (rows <= 64) return SMALL;
   return rows > 128 && ceil_div(rows, Large::BY) * ceil_div(vocab, Large::BX) >= UNITS ? LARGE : MEDIUM;
 }
+// A tile of the gradients across the hidden dimension.
+uint64_t dim_tile(int shape, uint64_t dim) {
+  if (shape != LARGE) return Medium::BX;
+  // (the narrower tile takes 1.17 times the loads for each product: 8192 x 1152 x 262144, 1152 of 1280 columns there, 9.7 ms with it and without)
+  return ceil_div(dim, Large192::BX) * Large192::BX * 115 < ceil_div(dim, Large::BX) * Large::BX * 100 ? Large192::BX : Large::BX;
+}
 HeadTiles head_tiles(int shape) {
   switch (shape) {
     case SMALL: return {Small::BX, Small::BY};
@@ -1284,7 +1303,7 @@ double rounds(uint64_t tiles) { return static_cast<double>((tiles + UNITS - 1) /
 // rounds (with the inner axes' steps, and about eight steps of a tile's own at either end).  Tiles of one compute unit each.
 uint64_t head_piece(int shape, uint64_t rows, uint64_t dim, uint64_t vocab, uint64_t most) {
   if (shape != LARGE) return most;
-  const uint64_t all = ceil_div(vocab, 256), row_tiles = ceil_div(rows, 256), dim_tiles = ceil_div(dim, 256);
+  const uint64_t all = ceil_div(vocab, 256), row_tiles = ceil_div(rows, 256), dim_tiles = ceil_div(dim, dim_tile(shape, dim));
   const uint64_t fewest = ceil_div(all, most / 256);
   double best = 0.0;
   uint64_t piece = most;
@@ -1293,30 +1312,31 @@ uint64_t head_piece(int shape, uint64_t rows, uint64_t dim, uint64_t vocab, uint
     double cost = 0.0;
     for (const uint64_t n : {tiles, last})
       cost += (n == tiles ? static_cast<double>(ceil_div(all, tiles) - 1) : 1.0) *
-              (rounds(n * row_tiles) * (static_cast<double>(dim) / KSTEP + 8) + rounds(n * dim_tiles) * (static_cast<double>(rows) / KSTEP + 8));
+              (rounds(n * row_tiles) * (static_cast<double>(dim) / KSTEP + 8) +
+               rounds(n * dim_tiles) * (static_cast<double>(rows) / KSTEP + 8) * static_cast<double>(dim_tile(shape, dim)) / 256);
     if (pieces == fewest || cost < 0.99 * best) { best = cost; piece = tiles * 256; }
   }
   return piece;
 }
 
-// Parts of a piece of the vocabulary that grad_hidden's product sums apart, so that its tiles fill the compute units; each costs a
-// reading and a writing of its sums.
-uint32_t head_splits(int shape, uint64_t rows, uint64_t dim, uint64_t piece) {
+// Parts of a piece of the vocabulary that grad_hidden's product sums apart, so that its tiles fill the compute units: in steps of 64 (about a
+// microsecond) with a dozen at a tile's ends, and with the writing and reading of the parts' sums at 5 TB/s, half of which the products hide.
+uint32_t head_splits(int shape, uint64_t rows, uint64_t dim, uint64_t piece, uint32_t pairs) {
   const HeadTiles t = head_tiles(shape);
-  const uint64_t tiles = ceil_div(dim, t.vocab) * ceil_div(rows, t.rows), most = ceil_div(piece, 512);
+  const uint64_t tiles = ceil_div(dim, dim_tile(shape, dim)) * ceil_div(rows, t.rows), steps = ceil_div(piece, KSTEP);
+  const uint64_t most = ceil_div(steps, 8) < 64 ? ceil_div(steps, 8) : 64;
   uint64_t splits = 1;
   if (shape == LARGE) {
     double best = 0.0;
-    for (uint64_t n = 1; n <= 16 && n <= most; ++n) {
-      const double cost = rounds(tiles * n) * (static_cast<double>(ceil_div(ceil_div(piece, KSTEP), n)) + 12);
-      if (n == 1 || cost < 0.97 * best) { best = cost; splits = n; }
+    for (uint64_t n = 1; n <= most; ++n) {
+      const double cost = rounds(tiles * n) * (static_cast<double>(ceil_div(steps, n) * pairs) + 12) + 0.5 * static_cast<double>(n * rows * dim) * 12 / 5e6;
+      if (n == 1 || cost < 0.98 * best) { best = cost; splits = n; }
     }
   } else {
-    splits = ceil_div(shape == SMALL ? 768 : 512, tiles);
-    if (splits > most) splits = most;
+    const uint64_t wanted = ceil_div(shape == SMALL ? 768 : 512, tiles);
+    splits = wanted < ceil_div(steps, 8) ? wanted : ceil_div(steps, 8);
   }
-  const uint64_t steps = ceil_div(piece, KSTEP);             // (every part of the first piece has a step)
-  return static_cast<uint32_t>(ceil_div(steps, ceil_div(steps, splits)));
+  return static_cast<uint32_t>(ceil_div(steps, ceil_div(steps, splits)));      // every part of the first piece has a step
 }
 
 template <class F>
@@ -1471,7 +1491,7 @@ hipError_t launch_head_grad_hidden(int shape, const HeadOperand &w, const HeadOp
   a.split_steps = (steps + splits - 1) / splits;
   a.splits = (steps + a.split_steps - 1) / a.split_steps;
   a.out_f32 = partial; a.out_ld = partial_ld; a.out_plane = partial_stride; a.add = add;
-  return launch_product<DH>(a, shape, dim, rows, s);
+  return dim_tile(shape, dim) == Large192::BX ? launch_tiles<DH, Large192>(a, dim, rows, s) : launch_product<DH>(a, shape, dim, rows, s);
 }
 
 hipError_t launch_head_grad_hidden_finish(const float *partial, uint32_t splits, uint32_t partial_ld, uint64_t partial_stride, const HeadRows &r, void *out,
@@ -1486,7 +1506,8 @@ hipError_t launch_head_grad_weights(int shape, const HeadOperand &h, const HeadO
   ProductArgs a = product(h, g);
   a.nx = dim; a.ny = n; a.count = count;
   a.out = out; a.out_ld = out_stride; a.out_bf16 = out_bf16; a.past_caches = past_caches;
-  return shape == LARGE ? launch_tiles<DW, Large>(a, dim, n, s) : launch_tiles<DW, Medium>(a, dim, n, s);
+  if (shape != LARGE) return launch_tiles<DW, Medium>(a, dim, n, s);
+  return dim_tile(shape, dim) == Large192::BX ? launch_tiles<DW, Large192>(a, dim, n, s) : launch_tiles<DW, Large>(a, dim, n, s);
 }
 
 }  // namespace eco
