@@ -214,8 +214,9 @@ __global__ __launch_bounds__(256) void eco_head_convert_kernel(HeadWeights w, ui
 //   DW     x hidden dimension, y vocabulary, k rows: the gradient of the weights
 // With x along a lane's registers, four neighbours in each group, a row's softmax is a reduction over registers and every end stores
 // neighbours together.
-// GRAD_PLANES is GRAD with g in several planes.
-enum : int { STATS = 0, GRAD = 1, DH = 2, DW = 3, GRAD_PLANES = 4 };
+// GRAD_PLANES is GRAD with g in several planes, DW_PAST is DW with stores past the caches.
+enum : int { STATS = 0, GRAD = 1, DH = 2, DW = 3, GRAD_PLANES = 4, DW_PAST = 5 };
+constexpr bool is_dw(int mode) { return mode == DW || mode == DW_PAST; }
 
 struct ProductArgs {
   const uint16_t *x, *y;
@@ -228,7 +229,7 @@ struct ProductArgs {
   void *out;
   uint64_t out_ld, out_plane;
   uint32_t out_planes, tiles, tile0, splits, split_steps, tiles_x;
-  int32_t two, out_bf16, add, past_caches;
+  int32_t two, out_bf16, add;
   float *sum, *sum_tau;
   const HeadRowConst *consts;
 };
@@ -337,9 +338,10 @@ __device__ __forceinline__ void put_f32(lds_char *own, int lane, const f32x16 &a
   }
 }
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
-__device__ __forceinline__ void store16(void *to, uint4 v, int past_caches) {
+template <bool PAST>
+__device__ __forceinline__ void store16(void *to, uint4 v) {
   const u32x4 x = {v.x, v.y, v.z, v.w};
-  if (past_caches) __builtin_nontemporal_store(x, static_cast<u32x4 *>(to));
+  if constexpr (PAST) __builtin_nontemporal_store(x, static_cast<u32x4 *>(to));
   else *static_cast<u32x4 *>(to) = x;
 }
 template <int PIECES, class F>
@@ -363,20 +365,20 @@ __device__ __forceinline__ uint32_t xcd_run(uint32_t id, uint32_t all) {
 // first steps are on their way.
 template <int MODE, class T>
 __global__ __launch_bounds__(T::THREADS) void eco_head_product_kernel(ProductArgs a) {
-  constexpr bool X_COLUMN = MODE == DH || MODE == DW, Y_COLUMN = MODE == DW, LOGITS = MODE == STATS || MODE == GRAD || MODE == GRAD_PLANES;
+  constexpr bool X_COLUMN = MODE == DH || is_dw(MODE), Y_COLUMN = is_dw(MODE), LOGITS = MODE == STATS || MODE == GRAD || MODE == GRAD_PLANES;
   constexpr int NI = T::NI, NJ = T::NJ, QUARTERS = KSTEP / 16;
   __shared__ __attribute__((aligned(1024))) char smem[T::DEPTH * T::STEP_BYTES + extra_bytes<MODE, T>()];
   static_assert(sizeof smem <= 163840, "a compute unit's LDS");
   const uint32_t count = static_cast<uint32_t>(*a.count);
-  const uint32_t ny = MODE == DW ? a.ny : count;
+  const uint32_t ny = is_dw(MODE) ? a.ny : count;
   // the grid is made for all rows: the tiles that there are, evenly over the XCDs
   const uint32_t tiles_y = (ny + T::BY - 1) / T::BY, all_tiles = a.tiles_x * tiles_y * a.splits;
   if (blockIdx.x >= all_tiles) return;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wx = wave % T::WX * (NI * 32), wy = wave / T::WX * (NJ * 32);
-  const uint32_t all_steps = MODE == DW ? (count + KSTEP - 1) / KSTEP : (a.k + KSTEP - 1) / KSTEP;
+  const uint32_t all_steps = is_dw(MODE) ? (count + KSTEP - 1) / KSTEP : (a.k + KSTEP - 1) / KSTEP;
   // the last step's end: past it pieces repeat valid ones of their row, or rows the last one, against zeros of the other operand
-  const uint32_t tail = (MODE == DW ? count : a.k) % KSTEP;
+  const uint32_t tail = (is_dw(MODE) ? count : a.k) % KSTEP;
   const uint64_t step_x = X_COLUMN ? static_cast<uint64_t>(KSTEP) * a.ldx : KSTEP, step_y = Y_COLUMN ? static_cast<uint64_t>(KSTEP) * a.ldy : KSTEP;
 
   struct Where { uint32_t x0, y0, split, first, steps; };
@@ -440,7 +442,7 @@ __global__ __launch_bounds__(T::THREADS) void eco_head_product_kernel(ProductArg
 #pragma unroll
     for (int i = 0; i < T::X_LOADS; ++i) {
       uint32_t off = off_x[i];
-      if (MODE != DW && end) {
+      if (!is_dw(MODE) && end) {
         uint32_t n, k;
         if constexpr (X_COLUMN) {
           column_piece<T::BX>(threadIdx.x + i * T::THREADS, n, k);
@@ -455,7 +457,7 @@ __global__ __launch_bounds__(T::THREADS) void eco_head_product_kernel(ProductArg
 #pragma unroll
     for (int i = 0; i < T::Y_LOADS; ++i) {
       uint32_t off = off_y[i];
-      if constexpr (MODE == DW)
+      if constexpr (is_dw(MODE))
         if (end) {
           uint32_t n, k;
           column_piece<T::BY>(threadIdx.x + i * T::THREADS, n, k);
@@ -637,9 +639,10 @@ __global__ __launch_bounds__(T::THREADS) void eco_head_product_kernel(ProductArg
             for (int i = 0; i < WIDE; ++i)
 #pragma unroll
               for (int q = 0; q < 4; ++q) put_bf16<4 * WIDE>(own, lane, i, q, two_of(i0 + i, 4 * q), two_of(i0 + i, 4 * q + 2));
-            // (columns and rows of the padded piece: nothing to check)
+            // (the columns are a padded piece's; of the rows past the last one that takes part nothing is read)
             take<4 * WIDE>(own, lane, [&](uint32_t row, uint32_t piece, uint4 v) {
-              *reinterpret_cast<uint4 *>(out + p * a.out_plane + static_cast<uint64_t>(y0 + wy + 32 * j + row) * a.out_ld + x0 + wx + 32 * i0 + 8 * piece) = v;
+              const uint32_t y = y0 + wy + 32 * j + row;
+              if (y < ny) *reinterpret_cast<uint4 *>(out + p * a.out_plane + static_cast<uint64_t>(y) * a.out_ld + x0 + wx + 32 * i0 + 8 * piece) = v;
             });
           }
         };
@@ -674,7 +677,7 @@ __global__ __launch_bounds__(T::THREADS) void eco_head_product_kernel(ProductArg
           });
         }
     }
-    if constexpr (MODE == DW) {
+    if constexpr (is_dw(MODE)) {
       if (a.out_bf16) {
         uint16_t *const out = static_cast<uint16_t *>(a.out);
         const bool whole = a.out_ld % 8 == 0;
@@ -691,7 +694,7 @@ __global__ __launch_bounds__(T::THREADS) void eco_head_product_kernel(ProductArg
             if (y >= ny || x >= a.nx) return;
             uint16_t *to = out + static_cast<uint64_t>(y) * a.out_ld + x;
             const uint32_t h[4] = {v.x, v.y, v.z, v.w};
-            if (whole && x + 8 <= a.nx) store16(to, v, a.past_caches);
+            if (whole && x + 8 <= a.nx) store16<MODE == DW_PAST>(to, v);
             else
 #pragma unroll
               for (int e = 0; e < 8; ++e)
@@ -717,7 +720,7 @@ __global__ __launch_bounds__(T::THREADS) void eco_head_product_kernel(ProductArg
               if (y >= ny || x >= a.nx) return;
               float *to = out + static_cast<uint64_t>(y) * a.out_ld + x;
               const uint32_t h[4] = {v.x, v.y, v.z, v.w};
-              if (whole && x + 4 <= a.nx) store16(to, v, a.past_caches);
+              if (whole && x + 4 <= a.nx) store16<MODE == DW_PAST>(to, v);
               else
 #pragma unroll
                 for (int e = 0; e < 4; ++e)
@@ -1505,9 +1508,12 @@ hipError_t launch_head_grad_weights(int shape, const HeadOperand &h, const HeadO
                                     int out_bf16, int past_caches, hipStream_t s) {
   ProductArgs a = product(h, g);
   a.nx = dim; a.ny = n; a.count = count;
-  a.out = out; a.out_ld = out_stride; a.out_bf16 = out_bf16; a.past_caches = past_caches;
-  if (shape != LARGE) return launch_tiles<DW, Medium>(a, dim, n, s);
-  return dim_tile(shape, dim) == Large192::BX ? launch_tiles<DW, Large192>(a, dim, n, s) : launch_tiles<DW, Large>(a, dim, n, s);
+  a.out = out; a.out_ld = out_stride; a.out_bf16 = out_bf16;
+  const auto go = [&](auto mode) {
+    if (shape != LARGE) return launch_tiles<mode.value, Medium>(a, dim, n, s);
+    return dim_tile(shape, dim) == Large192::BX ? launch_tiles<mode.value, Large192>(a, dim, n, s) : launch_tiles<mode.value, Large>(a, dim, n, s);
+  };
+  return past_caches ? go(std::integral_constant<int, DW_PAST>{}) : go(std::integral_constant<int, DW>{});
 }
 
 }  // namespace eco
