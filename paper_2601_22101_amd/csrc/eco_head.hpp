@@ -18,10 +18,11 @@ constexpr uint64_t head_round_up(uint64_t x, uint64_t k) { return (x + k - 1) / 
 constexpr int head_weight_planes(int fmt) { return fmt == 2 ? 1 : fmt == 3 ? 3 : 2; }
 constexpr int head_hidden_planes(int dtype_bf16) { return dtype_bf16 ? 1 : 3; }
 
-// Pairs of two operands' planes whose product counts: the sum of their places is at most 2, what is left out is below a relative 2^-22.
-constexpr uint32_t head_pairs(uint32_t x, uint32_t y) {
+// Pairs of two operands' planes whose product counts: the sum of their places is at most `order`.  2 leaves out less than a relative 2^-22 of a
+// product, 1 less than 2^-15, which is what a result that ends as a bf16 needs.
+constexpr uint32_t head_pairs(uint32_t x, uint32_t y, uint32_t order) {
   uint32_t n = 0;
-  for (uint32_t i = 0; i < x; ++i) n += y < 3 - i ? y : 3 - i;
+  for (uint32_t i = 0; i < x && i <= order; ++i) n += y < order + 1 - i ? y : order + 1 - i;
   return n;
 }
 
@@ -74,6 +75,8 @@ hipError_t launch_head_finish(const HeadRows &, const HeadWeights &, const HeadS
 enum : int { HEAD_LABELS = 0, HEAD_BOTH = 1, HEAD_TEACHER = 2, HEAD_SAME = 3 };
 // of a compact row: log2(e) lse, dL/dce, log2(e) lse_tau, tau dL/dkd; where there is but one softmax, its own first
 struct HeadRowConst { float lse2, a, lse2_tau, b; };
+// The logits' gradient is kept divided by the first row's upstream gradient, and both products are multiplied by it again: where all rows have the same, 1 / n, say, its
+// significand would put the same error into every rounding of g to bf16.
 
 // entries: ids [rows][top_k + 1] (-1: none) and the gradient of the logit at each, over compact rows; consts: the padded rows
 hipError_t launch_head_entries(const HeadRows &, uint32_t padded_rows, const float *grad_ce, const float *grad_kd, const float *lse, const float *lse_tau,
@@ -85,19 +88,20 @@ hipError_t launch_head_few_rows_backward(const HeadRows &, void *compact, uint32
                                          const float *lse_tau, const float *picked, int softmaxes, int32_t *ids, float *values, HeadRowConst *consts, hipStream_t);
 // g[row][v] of a piece: planes of [padded rows][ld]
 hipError_t launch_head_grad(int shape, const HeadOperand &w, const HeadWeights *few, uint64_t first, const HeadOperand &h, uint32_t n, uint32_t rows, uint32_t dim, const int32_t *count, float inv_tau, int softmaxes,
-                            const HeadRowConst *, void *g, uint32_t g_ld, uint64_t g_plane, uint32_t g_planes, hipStream_t);
-hipError_t launch_head_scatter(const int32_t *ids, const float *values, uint32_t rows, uint32_t entries, const int32_t *count, uint64_t first, uint32_t n, void *g,
+                            uint32_t order, const HeadRowConst *, void *g, uint32_t g_ld, uint64_t g_plane, uint32_t g_planes, hipStream_t);
+hipError_t launch_head_scatter(const int32_t *ids, const float *values, const HeadRowConst *, uint32_t rows, uint32_t entries, const int32_t *count, uint64_t first, uint32_t n, void *g,
                                uint32_t g_ld, uint64_t g_plane, uint32_t g_planes, hipStream_t);
 // partial[s][compact row][dim] (+)= g w over a piece, s the split of the piece's vocabulary
-hipError_t launch_head_grad_hidden(int shape, const HeadOperand &w, const HeadOperand &g, uint32_t n, uint32_t rows, uint32_t dim, const int32_t *count, uint32_t splits,
-                                   float *partial, uint32_t partial_ld, uint64_t partial_stride, int add, hipStream_t);
-hipError_t launch_head_grad_hidden_finish(const float *partial, uint32_t splits, uint32_t partial_ld, uint64_t partial_stride, const HeadRows &, void *out,
+hipError_t launch_head_grad_hidden(int shape, const HeadOperand &w, const HeadOperand &g, uint32_t n, uint32_t rows, uint32_t dim, const int32_t *count, uint32_t order,
+                                   uint32_t splits, float *partial, uint32_t partial_ld, uint64_t partial_stride, int add, hipStream_t);
+hipError_t launch_head_grad_hidden_finish(const HeadRowConst *, const float *partial, uint32_t splits, uint32_t partial_ld, uint64_t partial_stride, const HeadRows &, void *out,
                                           uint64_t out_stride, hipStream_t);
-hipError_t launch_head_grad_weights(int shape, const HeadOperand &h, const HeadOperand &g, uint32_t n, uint32_t dim, const int32_t *count, void *out, uint64_t out_stride,
-                                    int out_bf16, int past_caches, hipStream_t);
+hipError_t launch_head_grad_weights(int shape, const HeadOperand &h, const HeadOperand &g, uint32_t n, uint32_t dim, const int32_t *count, uint32_t order,
+                                    const HeadRowConst *, void *out, uint64_t out_stride, int out_bf16, int past_caches, hipStream_t);
 struct HeadTiles { uint32_t vocab, rows; };       // a tile of the logits
 HeadTiles head_tiles(int shape);
-int head_shape(uint64_t rows, uint64_t vocab);    // which tiles a call's products have, for the launchers
+enum : int { HEAD_SMALL = 0, HEAD_MEDIUM = 1, HEAD_LARGE = 2 };
+int head_shape(uint64_t rows, uint64_t vocab);    // which tiles a call's products have
 uint64_t head_piece(int shape, uint64_t rows, uint64_t dim, uint64_t vocab, uint64_t most);          // vocabulary to a piece of the backward pass
 uint32_t head_splits(int shape, uint64_t rows, uint64_t dim, uint64_t piece, uint32_t pairs);      // parts of a piece of the vocabulary that grad_hidden's product sums apart
 

@@ -95,7 +95,7 @@ eco::HeadWeights weights_of(const eco_head_t *h) {
 
 // The arrays of a workspace and the pieces of the vocabulary that a call goes by.
 struct Layout {
-  uint32_t padded_rows, padded_dim, entries, piece, hidden_planes, weight_planes, grad_planes, tiles, splits, few;
+  uint32_t padded_rows, padded_dim, entries, piece, hidden_planes, weight_planes, grad_planes, tiles, splits, few, pair_order;
   int shape;
   bool in_place, two;
   uint64_t count, order, place, flags, compact, planes, max, sum, sum_tau, ids, values, consts, g, partial, bytes;
@@ -112,13 +112,17 @@ Layout layout_of(const eco_head_t *h, bool backward) {
   Layout l;
   std::memset(&l, 0, sizeof l);
   l.shape = eco::head_shape(h->rows, h->vocab);
+  // Where both gradients are bf16 they are made of products of order 1 (see head_pairs), and the logits' gradient is rounded to bf16: to one, or to
+  // two of up to 64 rows, of which too few average its rounding.
+  const bool both_bf16 = h->hidden_dtype == ECO_DT_BF16 && h->grad_weights_dtype == ECO_DT_BF16;
+  l.pair_order = both_bf16 ? 1 : 2;
+  l.grad_planes = !both_bf16 ? 3 : h->rows <= eco::HEAD_FEW_ROWS ? 2 : 1;
   const eco::HeadTiles tile = eco::head_tiles(l.shape);
   l.padded_rows = static_cast<uint32_t>(eco::head_round_up(h->rows, tile.rows));      // compact rows: whole tiles, zero past the last one that takes part
   l.padded_dim = static_cast<uint32_t>(eco::head_round_up(h->dim, eco::HEAD_K_STEP));
   l.entries = h->top_k + 1;
   l.hidden_planes = static_cast<uint32_t>(eco::head_hidden_planes(h->hidden_dtype == ECO_DT_BF16));
   l.weight_planes = static_cast<uint32_t>(eco::head_weight_planes(h->fmt));
-  l.grad_planes = h->hidden_dtype == ECO_DT_BF16 && h->grad_weights_dtype == ECO_DT_BF16 ? 1 : 3;
   l.two = two_softmaxes(h);
   // bf16 weights are read where they lie if 16-byte pieces of their rows are whole
   const uint64_t stride = stride_or(h->weight_stride, h->dim);
@@ -153,7 +157,7 @@ Layout layout_of(const eco_head_t *h, bool backward) {
     l.values = take(4ull * h->rows * l.entries);
     l.consts = take(sizeof(eco::HeadRowConst) * l.padded_rows);
     l.g = take(2ull * l.grad_planes * l.padded_rows * piece);
-    l.splits = eco::head_splits(l.shape, h->rows, h->dim, piece < h->vocab ? piece : h->vocab, eco::head_pairs(l.weight_planes, l.grad_planes));
+    l.splits = eco::head_splits(l.shape, h->rows, h->dim, piece < h->vocab ? piece : h->vocab, eco::head_pairs(l.weight_planes, l.grad_planes, l.pair_order));
     l.partial = take(4ull * l.splits * l.padded_rows * l.padded_dim);
   }
   l.bytes = at;
@@ -272,7 +276,8 @@ eco_status_t eco_head_loss_backward(const eco_head_t *head, void *workspace, siz
     HEAD_LAUNCH(eco::launch_head_entries(r, l.padded_rows, grad_ce, grad_kd, lse, lse_tau, head->picked, softmaxes, ids, values, consts, s));
   }
   const uint64_t g_plane = static_cast<uint64_t>(l.padded_rows) * l.piece, partial_stride = static_cast<uint64_t>(l.padded_rows) * l.padded_dim;
-  const eco::HeadOperand g = {ws + l.g, g_plane, l.piece, l.grad_planes}, hidden = hidden_operand(l, ws);
+  const eco::HeadOperand hidden = hidden_operand(l, ws);
+  const eco::HeadOperand g = {ws + l.g, g_plane, l.piece, l.grad_planes};
   const uint64_t out_stride = stride_or(head->grad_weights_stride, head->dim);
   const eco::HeadWeights weights = weights_of(head);
   // A gradient that the 256 MB cache in front of HBM cannot hold passes the caches by: on its way out it would take the place of the weights, which the next
@@ -282,13 +287,14 @@ eco_status_t eco_head_loss_backward(const eco_head_t *head, void *workspace, siz
     const uint32_t n = static_cast<uint32_t>(head->vocab - first < l.piece ? head->vocab - first : l.piece);
     eco::HeadOperand w;
     HEAD_LAUNCH(weight_operand(head, l, ws, first, n, s, &w));
-    HEAD_LAUNCH(eco::launch_head_grad(l.shape, w, l.few ? &weights : nullptr, first, hidden, n, r.rows, r.dim, r.count, 1.0f / r.tau, softmaxes, consts, ws + l.g, l.piece, g_plane, l.grad_planes, s));
-    HEAD_LAUNCH(eco::launch_head_scatter(ids, values, r.rows, l.entries, r.count, first, n, ws + l.g, l.piece, g_plane, l.grad_planes, s));
-    HEAD_LAUNCH(eco::launch_head_grad_hidden(l.shape, w, g, n, r.rows, r.dim, r.count, l.splits, partial, l.padded_dim, partial_stride, first != 0, s));
+    HEAD_LAUNCH(eco::launch_head_grad(l.shape, w, l.few ? &weights : nullptr, first, hidden, n, r.rows, r.dim, r.count, 1.0f / r.tau, softmaxes,
+                                      l.pair_order, consts, ws + l.g, l.piece, g_plane, l.grad_planes, s));
+    HEAD_LAUNCH(eco::launch_head_scatter(ids, values, consts, r.rows, l.entries, r.count, first, n, ws + l.g, l.piece, g_plane, l.grad_planes, s));
+    HEAD_LAUNCH(eco::launch_head_grad_hidden(l.shape, w, g, n, r.rows, r.dim, r.count, l.pair_order, l.splits, partial, l.padded_dim, partial_stride, first != 0, s));
     char *out = static_cast<char *>(head->grad_weights) + first * out_stride * size_of(head->grad_weights_dtype);
-    HEAD_LAUNCH(eco::launch_head_grad_weights(l.shape, hidden, g, n, r.dim, r.count, out, out_stride, head->grad_weights_dtype == ECO_DT_BF16, past_caches, s));
+    HEAD_LAUNCH(eco::launch_head_grad_weights(l.shape, hidden, g, n, r.dim, r.count, l.pair_order, consts, out, out_stride, head->grad_weights_dtype == ECO_DT_BF16, past_caches, s));
   }
-  HEAD_LAUNCH(eco::launch_head_grad_hidden_finish(partial, l.splits, l.padded_dim, partial_stride, r, head->grad_hidden,
+  HEAD_LAUNCH(eco::launch_head_grad_hidden_finish(consts, partial, l.splits, l.padded_dim, partial_stride, r, head->grad_hidden,
                                                   stride_or(head->grad_hidden_stride, head->dim), s));
   return ECO_OK;
 }

@@ -207,6 +207,13 @@ __global__ __launch_bounds__(256) void eco_head_convert_kernel(HeadWeights w, ui
 
 // ------------------------------------------------------------------------------------------------ products
 
+// What the logits' gradient is divided by, see HeadRowConst.
+__device__ __forceinline__ float grad_unit(const HeadRowConst *consts) {
+  const HeadRowConst c = consts[0];
+  const float u = c.a != 0.0f ? fabsf(c.a) : fabsf(c.b);
+  return u > 0x1p-60f && u < 0x1p60f ? u : 1.0f;
+}
+
 // One product kernel, D[x][y] = sum_k X[x][k] Y[y][k], with four ends:
 //   STATS  x vocabulary, y rows: max and sum of exponentials over the tile's x, for each y
 //   GRAD   the same product again: g[y][x] as bf16 planes
@@ -221,7 +228,7 @@ constexpr bool is_dw(int mode) { return mode == DW || mode == DW_PAST; }
 struct ProductArgs {
   const uint16_t *x, *y;
   uint64_t x_plane, y_plane;
-  uint32_t ldx, ldy, x_planes, y_planes;
+  uint32_t ldx, ldy, x_planes, y_planes, order;
   uint32_t nx, ny, k;                             // ny, or k in DW, at most *count
   const int32_t *count;
   float scale2, scale2_tau;                       // log2(e), log2(e) / tau
@@ -402,7 +409,7 @@ __global__ __launch_bounds__(T::THREADS) void eco_head_product_kernel(ProductArg
     return w;
   };
 
-  const uint32_t pairs = head_pairs(a.x_planes, a.y_planes);
+  const uint32_t pairs = head_pairs(a.x_planes, a.y_planes, a.order), x_planes = min(a.x_planes, a.order + 1);
 
   // ---- the loads' place in the work
   uint32_t load_id = blockIdx.x, load_first, load_steps, in_pair, px, py, issued = 0, place = 0;
@@ -469,8 +476,8 @@ __global__ __launch_bounds__(T::THREADS) void eco_head_product_kernel(ProductArg
     ++issued;
     if (++in_pair == load_steps) {
       in_pair = 0;
-      if (++py == a.y_planes || px + py > 2) { py = 0; ++px; }
-      if (px == a.x_planes) {
+      if (++py == a.y_planes || px + py > a.order) { py = 0; ++px; }
+      if (px == x_planes) {
         load_id += gridDim.x;
         if (load_id < all_tiles) load_tile();
       } else {
@@ -613,11 +620,14 @@ __global__ __launch_bounds__(T::THREADS) void eco_head_product_kernel(ProductArg
     if constexpr (MODE == GRAD || MODE == GRAD_PLANES) {
       uint16_t *const out = static_cast<uint16_t *>(a.out);
       const bool edge = x0 + T::BX > a.nx;
+      const float per_unit = 1.0f / grad_unit(a.consts);
       constexpr int WIDE = NI == 1 ? 1 : 2;
 #pragma unroll
       for (int j = 0; j < NJ; ++j) {
         // (rows past the last one that takes part have a = b = 0)
-        const HeadRowConst rc = a.consts[y0 + wy + 32 * j + (lane & 31)];
+        HeadRowConst rc = a.consts[y0 + wy + 32 * j + (lane & 31)];
+        rc.a *= per_unit;
+        rc.b *= per_unit;
 #pragma unroll
         for (int i = 0; i < NI; ++i) {
           if (a.two) {
@@ -678,6 +688,13 @@ __global__ __launch_bounds__(T::THREADS) void eco_head_product_kernel(ProductArg
         }
     }
     if constexpr (is_dw(MODE)) {
+      const float unit = grad_unit(a.consts);
+#pragma unroll
+      for (int i = 0; i < NI; ++i)
+#pragma unroll
+        for (int j = 0; j < NJ; ++j)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) acc[i][j][r] *= unit;
       if (a.out_bf16) {
         uint16_t *const out = static_cast<uint16_t *>(a.out);
         const bool whole = a.out_ld % 8 == 0;
@@ -792,6 +809,8 @@ __global__ __launch_bounds__(FEW_WAVES * 64) void eco_head_few_kernel(ProductArg
     *reinterpret_cast<uint4 *>(few_lds + row * lds_row + k) = k < a.ldy ? *reinterpret_cast<const uint4 *>(a.y + static_cast<uint64_t>(row) * a.ldy + k) : make_uint4(0, 0, 0, 0);
   }
   __syncthreads();
+  float per_unit = 1.0f;
+  if constexpr (MODE != STATS) per_unit = 1.0f / grad_unit(a.consts);
   for (; group < groups; group += stride) {
     f32x4_t acc[R][BLOCKS] = {};
     const uint32_t next = min(group + stride, groups - 1);
@@ -876,7 +895,9 @@ __global__ __launch_bounds__(FEW_WAVES * 64) void eco_head_few_kernel(ProductArg
         m[b] = best;
       } else {
         const uint32_t y = 16 * b + n;
-        const HeadRowConst rc = a.consts[y];
+        HeadRowConst rc = a.consts[y];
+        rc.a *= per_unit;
+        rc.b *= per_unit;
 #pragma unroll
         for (int r = 0; r < R; ++r) {
           const uint32_t x = v0 + 16 * r;
@@ -1190,14 +1211,15 @@ __global__ __launch_bounds__(64) void eco_head_few_rows_kernel(HeadRows r, HeadW
   if (backward) entries_of(r, a, c, row, lane, id_of, q_of);
 }
 
-__global__ __launch_bounds__(256) void eco_head_scatter_kernel(const int32_t *ids, const float *values, uint32_t entries, const int32_t *count, uint64_t first, uint32_t n,
+__global__ __launch_bounds__(256) void eco_head_scatter_kernel(const int32_t *ids, const float *values, const HeadRowConst *consts, uint32_t entries, const int32_t *count, uint64_t first, uint32_t n,
                                                                uint16_t *g, uint32_t ld, uint64_t plane, uint32_t planes) {
   const uint64_t work = static_cast<uint64_t>(*count) * entries, step = static_cast<uint64_t>(gridDim.x) * 256;
+  const float per_unit = 1.0f / grad_unit(consts);
   for (uint64_t i = static_cast<uint64_t>(blockIdx.x) * 256 + threadIdx.x; i < work; i += step) {
     const int64_t v = static_cast<int64_t>(ids[i]) - static_cast<int64_t>(first);
     if (ids[i] < 0 || v < 0 || v >= static_cast<int64_t>(n)) continue;
     uint16_t *to = g + i / entries * ld + static_cast<uint64_t>(v);
-    float rest = values[i];
+    float rest = values[i] * per_unit;
     for (uint32_t p = 0; p < planes; ++p) {
       uint32_t bits;
       next_plane(rest, bits);
@@ -1207,10 +1229,11 @@ __global__ __launch_bounds__(256) void eco_head_scatter_kernel(const int32_t *id
 }
 
 // The gradient of the hidden states: each row's parts summed in their order, four columns to a thread; zeros where a row takes no part.
-__global__ __launch_bounds__(256) void eco_head_grad_hidden_finish_kernel(const float *partial, uint32_t splits, uint32_t ld, uint64_t stride, HeadRows r, void *out,
+__global__ __launch_bounds__(256) void eco_head_grad_hidden_finish_kernel(const HeadRowConst *consts, const float *partial, uint32_t splits, uint32_t ld, uint64_t stride, HeadRows r, void *out,
                                                                           uint64_t out_stride) {
   const uint32_t chunks = (r.dim + 3) / 4;
   const uint64_t work = static_cast<uint64_t>(r.rows) * chunks, step = static_cast<uint64_t>(gridDim.x) * 256;
+  const float unit = grad_unit(consts);
   const bool whole = out_stride % 4 == 0 && r.dim % 4 == 0 && (reinterpret_cast<uintptr_t>(out) & 15) == 0;
   for (uint64_t i = static_cast<uint64_t>(blockIdx.x) * 256 + threadIdx.x; i < work; i += step) {
     const uint32_t row = i >> 32 ? static_cast<uint32_t>(i / chunks) : static_cast<uint32_t>(i) / chunks, k = static_cast<uint32_t>(i - static_cast<uint64_t>(row) * chunks) * 4;
@@ -1224,6 +1247,7 @@ __global__ __launch_bounds__(256) void eco_head_grad_hidden_finish_kernel(const 
         sum.x += v.x; sum.y += v.y; sum.z += v.z; sum.w += v.w;
       }
     }
+    sum.x *= unit; sum.y *= unit; sum.z *= unit; sum.w *= unit;
     const uint64_t at = row * out_stride + k;
     const float v[4] = {sum.x, sum.y, sum.z, sum.w};
     if (whole) {
@@ -1248,9 +1272,9 @@ uint32_t blocks_for(uint64_t work) { return static_cast<uint32_t>(work < 256 * 8
 using Large = Tile<256, 256, 2, 4, 2>;
 using Large192 = Tile<192, 256, 2, 4, 2>;         // across the hidden dimension, where the others would be a quarter empty (1229 x 576 x 32128, both gradients 150 -> 119 us)
 using Medium = Tile<128, 128, 2, 2, 2>;
+using MediumWide = Tile<256, 128, 4, 2, 2>;
 using Small = Tile<128, 64, 4, 1, 3>;
 using SmallF32 = Tile<128, 64, 4, 1, 2>;
-enum : int { SMALL = 0, MEDIUM = 1, LARGE = 2 };
 constexpr uint32_t UNITS = 256;                   // compute units
 
 template <int MODE, class T>
@@ -1265,8 +1289,12 @@ hipError_t launch_tiles(ProductArgs a, uint32_t x, uint32_t y, hipStream_t s) {
 template <int MODE>
 hipError_t launch_product(const ProductArgs &a, int shape, uint32_t x, uint32_t y, hipStream_t s) {
   switch (shape) {
-    case SMALL: return launch_tiles<MODE, std::conditional_t<MODE == DH, SmallF32, Small>>(a, x, y, s);
-    case MEDIUM: return launch_tiles<MODE, Medium>(a, x, y, s);
+    case HEAD_SMALL: return launch_tiles<MODE, std::conditional_t<MODE == DH, SmallF32, Small>>(a, x, y, s);
+    case HEAD_MEDIUM:
+      // (the logits' gradient of 67 x 1152 x 262144: 143 us in wide tiles, 171)
+      if constexpr (MODE == GRAD || MODE == GRAD_PLANES)
+        if (ceil_div(x, MediumWide::BX) * ceil_div(y, MediumWide::BY) >= 2 * UNITS) return launch_tiles<MODE, MediumWide>(a, x, y, s);
+      return launch_tiles<MODE, Medium>(a, x, y, s);
     default: return launch_tiles<MODE, Large>(a, x, y, s);
   }
 }
@@ -1276,25 +1304,26 @@ ProductArgs product(const HeadOperand &x, const HeadOperand &y) {
   a.x = static_cast<const uint16_t *>(x.data); a.y = static_cast<const uint16_t *>(y.data);
   a.x_plane = x.plane; a.y_plane = y.plane; a.ldx = x.ld; a.ldy = y.ld; a.x_planes = x.planes; a.y_planes = y.planes;
   a.splits = 1;
+  a.order = 2;
   return a;
 }
 
 }  // namespace
 
 int head_shape(uint64_t rows, uint64_t vocab) {
-  if (rows <= 64) return SMALL;
-  return rows > 128 && ceil_div(rows, Large::BY) * ceil_div(vocab, Large::BX) >= UNITS ? LARGE : MEDIUM;
+  if (rows <= 64) return HEAD_SMALL;
+  return rows > 128 && ceil_div(rows, Large::BY) * ceil_div(vocab, Large::BX) >= UNITS ? HEAD_LARGE : HEAD_MEDIUM;
 }
 // A tile of the gradients across the hidden dimension.
 uint64_t dim_tile(int shape, uint64_t dim) {
-  if (shape != LARGE) return Medium::BX;
+  if (shape != HEAD_LARGE) return Medium::BX;
   // (the narrower tile takes 1.17 times the loads for each product: 8192 x 1152 x 262144, 1152 of 1280 columns there, 9.7 ms with it and without)
   return ceil_div(dim, Large192::BX) * Large192::BX * 115 < ceil_div(dim, Large::BX) * Large::BX * 100 ? Large192::BX : Large::BX;
 }
 HeadTiles head_tiles(int shape) {
   switch (shape) {
-    case SMALL: return {Small::BX, Small::BY};
-    case MEDIUM: return {Medium::BX, Medium::BY};
+    case HEAD_SMALL: return {Small::BX, Small::BY};
+    case HEAD_MEDIUM: return {Medium::BX, Medium::BY};
     default: return {Large::BX, Large::BY};
   }
 }
@@ -1305,7 +1334,7 @@ double rounds(uint64_t tiles) { return static_cast<double>((tiles + UNITS - 1) /
 // The piece of the vocabulary, at most `most`, whose tiles of the logits' gradient and of the weights' gradient take the least time in
 // rounds (with the inner axes' steps, and about eight steps of a tile's own at either end).  Tiles of one compute unit each.
 uint64_t head_piece(int shape, uint64_t rows, uint64_t dim, uint64_t vocab, uint64_t most) {
-  if (shape != LARGE) return most;
+  if (shape != HEAD_LARGE) return most;
   const uint64_t all = ceil_div(vocab, 256), row_tiles = ceil_div(rows, 256), dim_tiles = ceil_div(dim, dim_tile(shape, dim));
   const uint64_t fewest = ceil_div(all, most / 256);
   double best = 0.0;
@@ -1327,17 +1356,18 @@ uint64_t head_piece(int shape, uint64_t rows, uint64_t dim, uint64_t vocab, uint
 uint32_t head_splits(int shape, uint64_t rows, uint64_t dim, uint64_t piece, uint32_t pairs) {
   const HeadTiles t = head_tiles(shape);
   const uint64_t tiles = ceil_div(dim, dim_tile(shape, dim)) * ceil_div(rows, t.rows), steps = ceil_div(piece, KSTEP);
-  const uint64_t most = ceil_div(steps, 8) < 64 ? ceil_div(steps, 8) : 64;
+  const uint64_t each_eight = ceil_div(steps * pairs, 8), most = each_eight < 64 ? each_eight : 64;
   uint64_t splits = 1;
-  if (shape == LARGE) {
+  if (shape == HEAD_LARGE) {
     double best = 0.0;
-    for (uint64_t n = 1; n <= most; ++n) {
+    for (uint64_t n = 1; n <= most && n <= steps; ++n) {
       const double cost = rounds(tiles * n) * (static_cast<double>(ceil_div(steps, n) * pairs) + 12) + 0.5 * static_cast<double>(n * rows * dim) * 12 / 5e6;
       if (n == 1 || cost < 0.98 * best) { best = cost; splits = n; }
     }
   } else {
-    const uint64_t wanted = ceil_div(shape == SMALL ? 768 : 512, tiles);
-    splits = wanted < ceil_div(steps, 8) ? wanted : ceil_div(steps, 8);
+    const uint64_t wanted = ceil_div(shape == HEAD_SMALL ? 768 : 512, tiles);
+    splits = wanted < each_eight ? wanted : each_eight;
+    if (splits > steps) splits = steps;
   }
   return static_cast<uint32_t>(ceil_div(steps, ceil_div(steps, splits)));      // every part of the first piece has a step
 }
@@ -1469,26 +1499,26 @@ hipError_t launch_head_few_rows_backward(const HeadRows &r, void *compact, uint3
 }
 
 hipError_t launch_head_grad(int shape, const HeadOperand &w, const HeadWeights *few, uint64_t first, const HeadOperand &h, uint32_t n, uint32_t rows, uint32_t dim, const int32_t *count, float inv_tau, int softmaxes,
-                            const HeadRowConst *consts, void *g, uint32_t g_ld, uint64_t g_plane, uint32_t g_planes, hipStream_t s) {
+                            uint32_t order, const HeadRowConst *consts, void *g, uint32_t g_ld, uint64_t g_plane, uint32_t g_planes, hipStream_t s) {
   ProductArgs a = product(w, h);
-  a.nx = n; a.k = dim; a.count = count; a.two = softmaxes == HEAD_BOTH;
+  a.nx = n; a.k = dim; a.count = count; a.order = order; a.two = softmaxes == HEAD_BOTH;
   a.scale2 = softmaxes == HEAD_TEACHER ? LOG2E * inv_tau : LOG2E; a.scale2_tau = LOG2E * inv_tau;
   a.consts = consts; a.out = g; a.out_ld = g_ld; a.out_plane = g_plane; a.out_planes = g_planes;
   if (few) return launch_few<GRAD>(a, *few, first, rows, dim, s);
   return g_planes == 1 ? launch_product<GRAD>(a, shape, n, rows, s) : launch_product<GRAD_PLANES>(a, shape, n, rows, s);
 }
 
-hipError_t launch_head_scatter(const int32_t *ids, const float *values, uint32_t rows, uint32_t entries, const int32_t *count, uint64_t first, uint32_t n, void *g,
+hipError_t launch_head_scatter(const int32_t *ids, const float *values, const HeadRowConst *consts, uint32_t rows, uint32_t entries, const int32_t *count, uint64_t first, uint32_t n, void *g,
                                uint32_t g_ld, uint64_t g_plane, uint32_t g_planes, hipStream_t s) {
-  hipLaunchKernelGGL(eco_head_scatter_kernel, dim3(blocks_for(static_cast<uint64_t>(rows) * entries)), dim3(256), 0, s, ids, values, entries, count, first, n,
+  hipLaunchKernelGGL(eco_head_scatter_kernel, dim3(blocks_for(static_cast<uint64_t>(rows) * entries)), dim3(256), 0, s, ids, values, consts, entries, count, first, n,
                      static_cast<uint16_t *>(g), g_ld, g_plane, g_planes);
   return hipGetLastError();
 }
 
-hipError_t launch_head_grad_hidden(int shape, const HeadOperand &w, const HeadOperand &g, uint32_t n, uint32_t rows, uint32_t dim, const int32_t *count, uint32_t splits,
-                                   float *partial, uint32_t partial_ld, uint64_t partial_stride, int add, hipStream_t s) {
+hipError_t launch_head_grad_hidden(int shape, const HeadOperand &w, const HeadOperand &g, uint32_t n, uint32_t rows, uint32_t dim, const int32_t *count, uint32_t order,
+                                   uint32_t splits, float *partial, uint32_t partial_ld, uint64_t partial_stride, int add, hipStream_t s) {
   ProductArgs a = product(w, g);
-  a.nx = dim; a.k = n; a.count = count;
+  a.nx = dim; a.k = n; a.count = count; a.order = order;
   // no part is empty: a last, shorter piece of the vocabulary may make do with fewer
   const uint32_t steps = (n + KSTEP - 1) / KSTEP;
   a.split_steps = (steps + splits - 1) / splits;
@@ -1497,20 +1527,23 @@ hipError_t launch_head_grad_hidden(int shape, const HeadOperand &w, const HeadOp
   return dim_tile(shape, dim) == Large192::BX ? launch_tiles<DH, Large192>(a, dim, rows, s) : launch_product<DH>(a, shape, dim, rows, s);
 }
 
-hipError_t launch_head_grad_hidden_finish(const float *partial, uint32_t splits, uint32_t partial_ld, uint64_t partial_stride, const HeadRows &r, void *out,
+hipError_t launch_head_grad_hidden_finish(const HeadRowConst *consts, const float *partial, uint32_t splits, uint32_t partial_ld, uint64_t partial_stride, const HeadRows &r, void *out,
                                           uint64_t out_stride, hipStream_t s) {
-  hipLaunchKernelGGL(eco_head_grad_hidden_finish_kernel, dim3(blocks_for(static_cast<uint64_t>(r.rows) * ((r.dim + 3) / 4))), dim3(256), 0, s, partial, splits, partial_ld,
+  hipLaunchKernelGGL(eco_head_grad_hidden_finish_kernel, dim3(blocks_for(static_cast<uint64_t>(r.rows) * ((r.dim + 3) / 4))), dim3(256), 0, s, consts, partial, splits, partial_ld,
                      partial_stride, r, out, out_stride);
   return hipGetLastError();
 }
 
-hipError_t launch_head_grad_weights(int shape, const HeadOperand &h, const HeadOperand &g, uint32_t n, uint32_t dim, const int32_t *count, void *out, uint64_t out_stride,
-                                    int out_bf16, int past_caches, hipStream_t s) {
+hipError_t launch_head_grad_weights(int shape, const HeadOperand &h, const HeadOperand &g, uint32_t n, uint32_t dim, const int32_t *count, uint32_t order,
+                                    const HeadRowConst *consts, void *out, uint64_t out_stride, int out_bf16, int past_caches, hipStream_t s) {
   ProductArgs a = product(h, g);
-  a.nx = dim; a.ny = n; a.count = count;
+  a.nx = dim; a.ny = n; a.count = count; a.order = order; a.consts = consts;
   a.out = out; a.out_ld = out_stride; a.out_bf16 = out_bf16;
   const auto go = [&](auto mode) {
-    if (shape != LARGE) return launch_tiles<mode.value, Medium>(a, dim, n, s);
+    // (few rows: the tiles are all stores, and twice a chip's worth of large ones are the faster ones, 67 x 1152 x 262144 149 / 188 us, 32 rows 115 / 140; 1 x
+    // 576 x 32128, 378 of them, 13.1 / 12.3)
+    if (shape != HEAD_LARGE)
+      return ceil_div(dim, Large::BX) * ceil_div(n, Large::BY) >= 2 * UNITS ? launch_tiles<mode.value, Large>(a, dim, n, s) : launch_tiles<mode.value, Medium>(a, dim, n, s);
     return dim_tile(shape, dim) == Large192::BX ? launch_tiles<mode.value, Large192>(a, dim, n, s) : launch_tiles<mode.value, Large>(a, dim, n, s);
   };
   return past_caches ? go(std::integral_constant<int, DW_PAST>{}) : go(std::integral_constant<int, DW>{});
