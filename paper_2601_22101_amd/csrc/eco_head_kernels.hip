@@ -412,7 +412,7 @@ __global__ __launch_bounds__(T::THREADS) void eco_head_product_kernel(ProductArg
   const uint32_t pairs = head_pairs(a.x_planes, a.y_planes, a.order), x_planes = min(a.x_planes, a.order + 1);
 
   // ---- the loads' place in the work
-  uint32_t load_id = blockIdx.x, load_first, load_steps, in_pair, px, py, issued = 0, place = 0;
+  uint32_t load_id = blockIdx.x, load_first, load_steps, at_step, px, py, issued = 0, place = 0;
   uint32_t off_x[T::X_LOADS], off_y[T::Y_LOADS];
   const uint16_t *begin_x, *begin_y, *from_x, *from_y;
   const uint32_t lds0 = static_cast<uint32_t>(reinterpret_cast<uintptr_t>((lds_char *)smem));
@@ -440,12 +440,12 @@ __global__ __launch_bounds__(T::THREADS) void eco_head_product_kernel(ProductArg
     load_steps = w.steps;
     from_x = begin_x = a.x + (X_COLUMN ? w.x0 : static_cast<uint64_t>(w.x0) * a.ldx) + w.first * step_x;
     from_y = begin_y = a.y + (Y_COLUMN ? w.y0 : static_cast<uint64_t>(w.y0) * a.ldy) + w.first * step_y;
-    in_pair = px = py = 0;
+    at_step = px = py = 0;
   };
   const auto issue = [&]() {
     if (load_id >= all_tiles) return;
     const uint32_t lds = lds0 + place * T::STEP_BYTES + wave * 1024;
-    const bool end = tail && load_first + in_pair + 1 == all_steps;
+    const bool end = tail && load_first + at_step + 1 == all_steps;
 #pragma unroll
     for (int i = 0; i < T::X_LOADS; ++i) {
       uint32_t off = off_x[i];
@@ -474,20 +474,20 @@ __global__ __launch_bounds__(T::THREADS) void eco_head_product_kernel(ProductArg
     }
     place = place + 1 == T::DEPTH ? 0 : place + 1;
     ++issued;
-    if (++in_pair == load_steps) {
-      in_pair = 0;
-      if (++py == a.y_planes || px + py > a.order) { py = 0; ++px; }
-      if (px == x_planes) {
+    // the pairs of planes of a step, then the next step: a plane that comes again is still in the caches
+    if (++py == a.y_planes || px + py > a.order) { py = 0; ++px; }
+    if (px == x_planes) {
+      px = 0;
+      if (++at_step == load_steps) {
         load_id += gridDim.x;
         if (load_id < all_tiles) load_tile();
-      } else {
-        from_x = begin_x + px * a.x_plane;
-        from_y = begin_y + py * a.y_plane;
+        return;
       }
-    } else {
-      from_x += step_x;
-      from_y += step_y;
+      begin_x += step_x;
+      begin_y += step_y;
     }
+    from_x = begin_x + px * a.x_plane;
+    from_y = begin_y + py * a.y_plane;
   };
 
   // ---- the products' place
