@@ -81,10 +81,13 @@ struct HeadRowConst { float lse2, a, lse2_tau, b; };
 // entries: ids [rows][top_k + 1] (-1: none) and the gradient of the logit at each, over compact rows; consts: the padded rows
 hipError_t launch_head_entries(const HeadRows &, uint32_t padded_rows, const float *grad_ce, const float *grad_kd, const float *lse, const float *lse_tau,
                                const float *picked, int softmaxes, int32_t *ids, float *values, HeadRowConst *consts, hipStream_t);
+// Up to 32 rows with g in two planes: the second plane's rows come 32 after the first one's, and the hidden states' once more 32 after themselves, so that the
+// two planes are one product: rows of their own of grad_hidden's, whose parts are added in the end, and one step of the inner axis of grad_weights'.
+constexpr uint32_t HEAD_STACK = 32;
 // At most 64 rows: launch_head_rows with the logits at the entries, or with launch_head_entries, in one launch.
 constexpr uint32_t HEAD_FEW_ROWS = 64;
 hipError_t launch_head_few_rows(const HeadRows &, const HeadWeights &, void *compact, uint32_t padded_rows, uint32_t padded_dim, float *picked, hipStream_t);
-hipError_t launch_head_few_rows_backward(const HeadRows &, void *compact, uint32_t padded_rows, uint32_t padded_dim, const float *grad_ce, const float *grad_kd, const float *lse,
+hipError_t launch_head_few_rows_backward(const HeadRows &, uint32_t stack, void *compact, uint32_t padded_rows, uint32_t padded_dim, const float *grad_ce, const float *grad_kd, const float *lse,
                                          const float *lse_tau, const float *picked, int softmaxes, int32_t *ids, float *values, HeadRowConst *consts, hipStream_t);
 // g[row][v] of a piece: planes of [padded rows][ld]
 hipError_t launch_head_grad(int shape, const HeadOperand &w, const HeadWeights *few, uint64_t first, const HeadOperand &h, uint32_t n, uint32_t rows, uint32_t dim, const int32_t *count, float inv_tau, int softmaxes,
@@ -92,11 +95,11 @@ hipError_t launch_head_grad(int shape, const HeadOperand &w, const HeadWeights *
 hipError_t launch_head_scatter(const int32_t *ids, const float *values, const HeadRowConst *, uint32_t rows, uint32_t entries, const int32_t *count, uint64_t first, uint32_t n, void *g,
                                uint32_t g_ld, uint64_t g_plane, uint32_t g_planes, hipStream_t);
 // partial[s][compact row][dim] (+)= g w over a piece, s the split of the piece's vocabulary
-hipError_t launch_head_grad_hidden(int shape, const HeadOperand &w, const HeadOperand &g, uint32_t n, uint32_t rows, uint32_t dim, const int32_t *count, uint32_t order,
+hipError_t launch_head_grad_hidden(int shape, uint32_t stack, const HeadOperand &w, const HeadOperand &g, uint32_t n, uint32_t rows, uint32_t dim, const int32_t *count, uint32_t order,
                                    uint32_t splits, float *partial, uint32_t partial_ld, uint64_t partial_stride, int add, hipStream_t);
-hipError_t launch_head_grad_hidden_finish(const HeadRowConst *, const float *partial, uint32_t splits, uint32_t partial_ld, uint64_t partial_stride, const HeadRows &, void *out,
+hipError_t launch_head_grad_hidden_finish(const HeadRowConst *, const float *partial, uint32_t splits, uint32_t partial_ld, uint64_t partial_stride, uint32_t stack, const HeadRows &, void *out,
                                           uint64_t out_stride, hipStream_t);
-hipError_t launch_head_grad_weights(int shape, const HeadOperand &h, const HeadOperand &g, uint32_t n, uint32_t dim, const int32_t *count, uint32_t order,
+hipError_t launch_head_grad_weights(int shape, uint32_t stack, const HeadOperand &h, const HeadOperand &g, uint32_t n, uint32_t dim, const int32_t *count, uint32_t order,
                                     const HeadRowConst *, void *out, uint64_t out_stride, int out_bf16, int past_caches, hipStream_t);
 struct HeadTiles { uint32_t vocab, rows; };       // a tile of the logits
 HeadTiles head_tiles(int shape);

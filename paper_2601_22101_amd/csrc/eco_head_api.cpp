@@ -95,7 +95,7 @@ eco::HeadWeights weights_of(const eco_head_t *h) {
 
 // The arrays of a workspace and the pieces of the vocabulary that a call goes by.
 struct Layout {
-  uint32_t padded_rows, padded_dim, entries, piece, hidden_planes, weight_planes, grad_planes, tiles, splits, few, pair_order;
+  uint32_t padded_rows, padded_dim, entries, piece, hidden_planes, weight_planes, grad_planes, tiles, splits, few, pair_order, stack;
   int shape;
   bool in_place, two;
   uint64_t count, order, place, flags, compact, planes, max, sum, sum_tau, ids, values, consts, g, partial, bytes;
@@ -117,6 +117,7 @@ Layout layout_of(const eco_head_t *h, bool backward) {
   const bool both_bf16 = h->hidden_dtype == ECO_DT_BF16 && h->grad_weights_dtype == ECO_DT_BF16;
   l.pair_order = both_bf16 ? 1 : 2;
   l.grad_planes = !both_bf16 ? 3 : h->rows <= eco::HEAD_FEW_ROWS ? 2 : 1;
+  l.stack = l.grad_planes == 2 && h->rows <= eco::HEAD_STACK ? eco::HEAD_STACK : 0;
   const eco::HeadTiles tile = eco::head_tiles(l.shape);
   l.padded_rows = static_cast<uint32_t>(eco::head_round_up(h->rows, tile.rows));      // compact rows: whole tiles, zero past the last one that takes part
   l.padded_dim = static_cast<uint32_t>(eco::head_round_up(h->dim, eco::HEAD_K_STEP));
@@ -157,7 +158,7 @@ Layout layout_of(const eco_head_t *h, bool backward) {
     l.values = take(4ull * h->rows * l.entries);
     l.consts = take(sizeof(eco::HeadRowConst) * l.padded_rows);
     l.g = take(2ull * l.grad_planes * l.padded_rows * piece);
-    l.splits = eco::head_splits(l.shape, h->rows, h->dim, piece < h->vocab ? piece : h->vocab, eco::head_pairs(l.weight_planes, l.grad_planes, l.pair_order));
+    l.splits = eco::head_splits(l.shape, h->rows, h->dim, piece < h->vocab ? piece : h->vocab, eco::head_pairs(l.weight_planes, l.stack ? 1 : l.grad_planes, l.pair_order));
     l.partial = take(4ull * l.splits * l.padded_rows * l.padded_dim);
   }
   l.bytes = at;
@@ -269,15 +270,15 @@ eco_status_t eco_head_loss_backward(const eco_head_t *head, void *workspace, siz
   eco::HeadRowConst *consts = reinterpret_cast<eco::HeadRowConst *>(ws + l.consts);
   const float *lse = head->labels ? head->lse : nullptr, *lse_tau = head->top_k ? head->lse_tau : nullptr;
   if (r.rows <= eco::HEAD_FEW_ROWS) {
-    HEAD_LAUNCH(eco::launch_head_few_rows_backward(r, ws + l.compact, l.padded_rows, l.padded_dim, grad_ce, grad_kd, lse, lse_tau, head->picked, softmaxes, ids, values,
+    HEAD_LAUNCH(eco::launch_head_few_rows_backward(r, l.stack, ws + l.compact, l.padded_rows, l.padded_dim, grad_ce, grad_kd, lse, lse_tau, head->picked, softmaxes, ids, values,
                                                    consts, s));
   } else {
     HEAD_LAUNCH(eco::launch_head_rows(r, ws + l.compact, l.padded_rows, l.padded_dim, s));
     HEAD_LAUNCH(eco::launch_head_entries(r, l.padded_rows, grad_ce, grad_kd, lse, lse_tau, head->picked, softmaxes, ids, values, consts, s));
   }
-  const uint64_t g_plane = static_cast<uint64_t>(l.padded_rows) * l.piece, partial_stride = static_cast<uint64_t>(l.padded_rows) * l.padded_dim;
+  const uint64_t g_plane = static_cast<uint64_t>(l.stack ? l.stack : l.padded_rows) * l.piece, partial_stride = static_cast<uint64_t>(l.padded_rows) * l.padded_dim;
   const eco::HeadOperand hidden = hidden_operand(l, ws);
-  const eco::HeadOperand g = {ws + l.g, g_plane, l.piece, l.grad_planes};
+  const eco::HeadOperand g = {ws + l.g, g_plane, l.piece, l.stack ? 1 : l.grad_planes};
   const uint64_t out_stride = stride_or(head->grad_weights_stride, head->dim);
   const eco::HeadWeights weights = weights_of(head);
   // A gradient that the 256 MB cache in front of HBM cannot hold passes the caches by: on its way out it would take the place of the weights, which the next
@@ -290,11 +291,11 @@ eco_status_t eco_head_loss_backward(const eco_head_t *head, void *workspace, siz
     HEAD_LAUNCH(eco::launch_head_grad(l.shape, w, l.few ? &weights : nullptr, first, hidden, n, r.rows, r.dim, r.count, 1.0f / r.tau, softmaxes,
                                       l.pair_order, consts, ws + l.g, l.piece, g_plane, l.grad_planes, s));
     HEAD_LAUNCH(eco::launch_head_scatter(ids, values, consts, r.rows, l.entries, r.count, first, n, ws + l.g, l.piece, g_plane, l.grad_planes, s));
-    HEAD_LAUNCH(eco::launch_head_grad_hidden(l.shape, w, g, n, r.rows, r.dim, r.count, l.pair_order, l.splits, partial, l.padded_dim, partial_stride, first != 0, s));
+    HEAD_LAUNCH(eco::launch_head_grad_hidden(l.shape, l.stack, w, g, n, r.rows, r.dim, r.count, l.pair_order, l.splits, partial, l.padded_dim, partial_stride, first != 0, s));
     char *out = static_cast<char *>(head->grad_weights) + first * out_stride * size_of(head->grad_weights_dtype);
-    HEAD_LAUNCH(eco::launch_head_grad_weights(l.shape, hidden, g, n, r.dim, r.count, l.pair_order, consts, out, out_stride, head->grad_weights_dtype == ECO_DT_BF16, past_caches, s));
+    HEAD_LAUNCH(eco::launch_head_grad_weights(l.shape, l.stack, hidden, g, n, r.dim, r.count, l.pair_order, consts, out, out_stride, head->grad_weights_dtype == ECO_DT_BF16, past_caches, s));
   }
-  HEAD_LAUNCH(eco::launch_head_grad_hidden_finish(consts, partial, l.splits, l.padded_dim, partial_stride, r, head->grad_hidden,
+  HEAD_LAUNCH(eco::launch_head_grad_hidden_finish(consts, partial, l.splits, l.padded_dim, partial_stride, l.stack, r, head->grad_hidden,
                                                   stride_or(head->grad_hidden_stride, head->dim), s));
   return ECO_OK;
 }

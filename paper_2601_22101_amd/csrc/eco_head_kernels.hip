@@ -230,6 +230,7 @@ struct ProductArgs {
   uint64_t x_plane, y_plane;
   uint32_t ldx, ldy, x_planes, y_planes, order;
   uint32_t nx, ny, k;                             // ny, or k in DW, at most *count
+  uint32_t stack;                                 // of up to 32 rows: g's second plane is rows 32 and on of its first, see HEAD_STACK
   const int32_t *count;
   float scale2, scale2_tau;                       // log2(e), log2(e) / tau
   float *out_f32;
@@ -377,13 +378,13 @@ __global__ __launch_bounds__(T::THREADS) void eco_head_product_kernel(ProductArg
   __shared__ __attribute__((aligned(1024))) char smem[T::DEPTH * T::STEP_BYTES + extra_bytes<MODE, T>()];
   static_assert(sizeof smem <= 163840, "a compute unit's LDS");
   const uint32_t count = static_cast<uint32_t>(*a.count);
-  const uint32_t ny = is_dw(MODE) ? a.ny : count;
+  const uint32_t ny = is_dw(MODE) ? a.ny : MODE == DH ? count + a.stack : count;
   // the grid is made for all rows: the tiles that there are, evenly over the XCDs
   const uint32_t tiles_y = (ny + T::BY - 1) / T::BY, all_tiles = a.tiles_x * tiles_y * a.splits;
   if (blockIdx.x >= all_tiles) return;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wx = wave % T::WX * (NI * 32), wy = wave / T::WX * (NJ * 32);
-  const uint32_t all_steps = is_dw(MODE) ? (count + KSTEP - 1) / KSTEP : (a.k + KSTEP - 1) / KSTEP;
+  const uint32_t all_steps = is_dw(MODE) ? (count + KSTEP - 1) / KSTEP : (a.k + KSTEP - 1) / KSTEP;      // (stacked rows are one step of DW)
   // the last step's end: past it pieces repeat valid ones of their row, or rows the last one, against zeros of the other operand
   const uint32_t tail = (is_dw(MODE) ? count : a.k) % KSTEP;
   const uint64_t step_x = X_COLUMN ? static_cast<uint64_t>(KSTEP) * a.ldx : KSTEP, step_y = Y_COLUMN ? static_cast<uint64_t>(KSTEP) * a.ldy : KSTEP;
@@ -468,6 +469,7 @@ __global__ __launch_bounds__(T::THREADS) void eco_head_product_kernel(ProductArg
         if (end) {
           uint32_t n, k;
           column_piece<T::BY>(threadIdx.x + i * T::THREADS, n, k);
+          if (a.stack) k %= HEAD_STACK;
           if (k >= tail) off -= (k - (tail - 1)) * a.ldy * 2;
         }
       load_to_lds(lds + T::X_BYTES + i * T::THREADS * 16, from_y, off);
@@ -550,8 +552,11 @@ __global__ __launch_bounds__(T::THREADS) void eco_head_product_kernel(ProductArg
       }
     }
 
-    // acc[i][j][r]: x = x0 + wx + 32 i + (r & 3) + 8 (r >> 2) + 4 (lane >> 5), y = y0 + wy + 32 j + (lane & 31)
-    const auto x_of = [&](int i, int r) { return x0 + wx + 32 * i + (r & 3) + 8 * (r >> 2) + 4 * (lane >> 5); };
+    // acc[i][j][r]: x = x0 + wx + 32 i + (r & 3) + 8 (r >> 2) + 4 (end_lane >> 5), y = y0 + wy + 32 j + (end_lane & 31)
+    // (a lane that the compiler does not know: addresses of the tile's end would otherwise hold registers through the products, and spill others)
+    int end_lane = lane;
+    asm volatile("" : "+v"(end_lane));
+    const auto x_of = [&](int i, int r) { return x0 + wx + 32 * i + (r & 3) + 8 * (r >> 2) + 4 * (end_lane >> 5); };
     lds_char *const extra = (lds_char *)smem + T::DEPTH * T::STEP_BYTES;
     lds_char *const own = extra + wave * own_bytes<MODE, T>();
     if constexpr (MODE == STATS) {
@@ -561,14 +566,14 @@ __global__ __launch_bounds__(T::THREADS) void eco_head_product_kernel(ProductArg
 #pragma unroll
         for (int j = 0; j < NJ; ++j) {
           v[j] = join(v[j], __shfl_xor(v[j], 32));
-          if (lane < 32) red[wave % T::WX * T::BY + wy + 32 * j + lane] = v[j];
+          if (end_lane < 32) red[wave % T::WX * T::BY + wy + 32 * j + end_lane] = v[j];
         }
         __syncthreads();
 #pragma unroll
         for (int j = 0; j < NJ; ++j) {
-          v[j] = red[wy + 32 * j + (lane & 31)];
+          v[j] = red[wy + 32 * j + (end_lane & 31)];
 #pragma unroll
-          for (int q = 1; q < T::WX; ++q) v[j] = join(v[j], red[q * T::BY + wy + 32 * j + (lane & 31)]);
+          for (int q = 1; q < T::WX; ++q) v[j] = join(v[j], red[q * T::BY + wy + 32 * j + (end_lane & 31)]);
         }
       };
       float m[NJ], sum[NJ];
@@ -602,10 +607,10 @@ __global__ __launch_bounds__(T::THREADS) void eco_head_product_kernel(ProductArg
         across(sum, which, [](float p, float q) { return p + q; });
       };
       const auto store = [&](float *out, const float (&v)[NJ]) {
-        if (wave % T::WX == 0 && lane < 32)
+        if (wave % T::WX == 0 && end_lane < 32)
 #pragma unroll
           for (int j = 0; j < NJ; ++j) {
-            const uint32_t y = y0 + wy + 32 * j + lane;
+            const uint32_t y = y0 + wy + 32 * j + end_lane;
             if (y < ny) out[static_cast<uint64_t>(y) * a.tiles + a.tile0 + x0 / T::BX] = v[j];
           }
       };
@@ -625,7 +630,7 @@ __global__ __launch_bounds__(T::THREADS) void eco_head_product_kernel(ProductArg
 #pragma unroll
       for (int j = 0; j < NJ; ++j) {
         // (rows past the last one that takes part have a = b = 0)
-        HeadRowConst rc = a.consts[y0 + wy + 32 * j + (lane & 31)];
+        HeadRowConst rc = a.consts[y0 + wy + 32 * j + (end_lane & 31)];
         rc.a *= per_unit;
         rc.b *= per_unit;
 #pragma unroll
@@ -642,33 +647,33 @@ __global__ __launch_bounds__(T::THREADS) void eco_head_product_kernel(ProductArg
 #pragma unroll
             for (int r = 0; r < 16; ++r) acc[i][j][r] = x_of(i, r) < a.nx ? acc[i][j][r] : 0.0f;
         }
-        const auto put_and_take = [&](uint32_t p, auto two_of) {
+        const auto put_and_take = [&](int i0, uint32_t p, auto two_of) {
 #pragma unroll
-          for (int i0 = 0; i0 < NI; i0 += WIDE) {
+          for (int i = 0; i < WIDE; ++i)
 #pragma unroll
-            for (int i = 0; i < WIDE; ++i)
-#pragma unroll
-              for (int q = 0; q < 4; ++q) put_bf16<4 * WIDE>(own, lane, i, q, two_of(i0 + i, 4 * q), two_of(i0 + i, 4 * q + 2));
-            // (the columns are a padded piece's; of the rows past the last one that takes part nothing is read)
-            take<4 * WIDE>(own, lane, [&](uint32_t row, uint32_t piece, uint4 v) {
-              const uint32_t y = y0 + wy + 32 * j + row;
-              if (y < ny) *reinterpret_cast<uint4 *>(out + p * a.out_plane + static_cast<uint64_t>(y) * a.out_ld + x0 + wx + 32 * i0 + 8 * piece) = v;
-            });
-          }
+            for (int q = 0; q < 4; ++q) put_bf16<4 * WIDE>(own, end_lane, i, q, two_of(i0 + i, 4 * q), two_of(i0 + i, 4 * q + 2));
+          // (the columns are a padded piece's; of the rows past the last one that takes part nothing is read)
+          take<4 * WIDE>(own, end_lane, [&](uint32_t row, uint32_t piece, uint4 v) {
+            const uint32_t y = y0 + wy + 32 * j + row;
+            if (y < ny) *reinterpret_cast<uint4 *>(out + p * a.out_plane + static_cast<uint64_t>(y) * a.out_ld + x0 + wx + 32 * i0 + 8 * piece) = v;
+          });
         };
-        if constexpr (MODE == GRAD)
-          put_and_take(0, [&](int i, int r) { return f32x2_to_bf16x2_rne(acc[i][j][r], acc[i][j][r + 1]); });
-        else
-          for (uint32_t p = 0; p < a.out_planes; ++p)
-            put_and_take(p, [&](int i, int r) {
-              uint32_t lo, hi;
-              float rest = acc[i][j][r], next = acc[i][j][r + 1];
-              next_plane(rest, lo);
-              next_plane(next, hi);
-              acc[i][j][r] = rest;
-              acc[i][j][r + 1] = next;
-              return lo | hi << 16;
-            });
+#pragma unroll
+        for (int i0 = 0; i0 < NI; i0 += WIDE) {
+          if constexpr (MODE == GRAD) {
+            put_and_take(i0, 0, [&](int i, int r) { return f32x2_to_bf16x2_rne(acc[i][j][r], acc[i][j][r + 1]); });
+          } else {
+            // (nothing here is past the range of a bf16: |g| is below the rows' largest upstream gradient over the first's)
+#pragma unroll
+            for (uint32_t p = 0; p < 3; ++p)
+              if (p < a.out_planes) put_and_take(i0, p, [&](int i, int r) {
+                const uint32_t two = f32x2_to_bf16x2_rne(acc[i][j][r], acc[i][j][r + 1]);
+                acc[i][j][r] -= bf16_lo(two);
+                acc[i][j][r + 1] -= bf16_hi(two);
+                return two;
+              });
+          }
+        }
       }
     }
     if constexpr (MODE == DH) {
@@ -677,8 +682,8 @@ __global__ __launch_bounds__(T::THREADS) void eco_head_product_kernel(ProductArg
       for (int j = 0; j < NJ; ++j)
 #pragma unroll
         for (int i = 0; i < NI; ++i) {
-          put_f32(own, lane, acc[i][j]);
-          take<8>(own, lane, [&](uint32_t row, uint32_t piece, uint4 v) {
+          put_f32(own, end_lane, acc[i][j]);
+          take<8>(own, end_lane, [&](uint32_t row, uint32_t piece, uint4 v) {
             const uint32_t y = y0 + wy + 32 * j + row, x = x0 + wx + 32 * i + 4 * piece;
             if (y >= ny || x >= a.out_ld) return;              // whole fours: out_ld is the padded dimension
             float4 *to = reinterpret_cast<float4 *>(out + static_cast<uint64_t>(y) * a.out_ld + x), f = __builtin_bit_cast(float4, v);
@@ -704,9 +709,9 @@ __global__ __launch_bounds__(T::THREADS) void eco_head_product_kernel(ProductArg
           for (int i = 0; i < WIDE; ++i)
 #pragma unroll
             for (int q = 0; q < 4; ++q)
-              put_bf16<4 * WIDE>(own, lane, i, q, f32x2_to_bf16x2_rne(acc[i0 + i][j][4 * q], acc[i0 + i][j][4 * q + 1]),
+              put_bf16<4 * WIDE>(own, end_lane, i, q, f32x2_to_bf16x2_rne(acc[i0 + i][j][4 * q], acc[i0 + i][j][4 * q + 1]),
                                  f32x2_to_bf16x2_rne(acc[i0 + i][j][4 * q + 2], acc[i0 + i][j][4 * q + 3]));
-          take<4 * WIDE>(own, lane, [&](uint32_t row, uint32_t piece, uint4 v) {
+          take<4 * WIDE>(own, end_lane, [&](uint32_t row, uint32_t piece, uint4 v) {
             const uint32_t y = y0 + wy + 32 * j + row, x = x0 + wx + 32 * i0 + 8 * piece;
             if (y >= ny || x >= a.nx) return;
             uint16_t *to = out + static_cast<uint64_t>(y) * a.out_ld + x;
@@ -731,8 +736,8 @@ __global__ __launch_bounds__(T::THREADS) void eco_head_product_kernel(ProductArg
         for (int j = 0; j < NJ; ++j)
 #pragma unroll
           for (int i = 0; i < NI; ++i) {
-            put_f32(own, lane, acc[i][j]);
-            take<8>(own, lane, [&](uint32_t row, uint32_t piece, uint4 v) {
+            put_f32(own, end_lane, acc[i][j]);
+            take<8>(own, end_lane, [&](uint32_t row, uint32_t piece, uint4 v) {
               const uint32_t y = y0 + wy + 32 * j + row, x = x0 + wx + 32 * i + 4 * piece;
               if (y >= ny || x >= a.nx) return;
               float *to = out + static_cast<uint64_t>(y) * a.out_ld + x;
@@ -1163,7 +1168,7 @@ __global__ __launch_bounds__(64) void eco_head_entries_kernel(HeadRows r, EntryA
 // first `padded` lay out a compact row each, and with `backward` its entries; in a forward pass the rest take a dot product each.
 template <int FMT, bool WHOLE>
 __global__ __launch_bounds__(64) void eco_head_few_rows_kernel(HeadRows r, HeadWeights w, EntryArgs a, uint16_t *compact, uint32_t padded, uint32_t ld, int backward,
-                                                               float *picked) {
+                                                               uint32_t stack, float *picked) {
   __shared__ int32_t id_of[HEAD_MOST_TOP_K + 1];
   __shared__ float q_of[HEAD_MOST_TOP_K + 1];
   const int lane = threadIdx.x;
@@ -1197,10 +1202,11 @@ __global__ __launch_bounds__(64) void eco_head_few_rows_kernel(HeadRows r, HeadW
     if (here) r.order[at] = lane;
     if (lane == 0) *r.count = static_cast<int32_t>(count);
   }
-  int64_t row = -1;                                            // the cth that takes part
-  if (c < count) {
+  int64_t row = -1;                                            // the cth that takes part; stacked, once more for g's second plane
+  const uint32_t nth = stack ? c % HEAD_STACK : c;
+  if (nth < count) {
     uint64_t rest = part;
-    for (uint32_t i = 0; i < c; ++i) rest &= rest - 1;
+    for (uint32_t i = 0; i < nth; ++i) rest &= rest - 1;
     row = __ffsll(static_cast<unsigned long long>(rest)) - 1;
   }
   for (uint32_t k = lane * 8; k < ld; k += 512) {
@@ -1208,7 +1214,7 @@ __global__ __launch_bounds__(64) void eco_head_few_rows_kernel(HeadRows r, HeadW
     if (row >= 0 && k < r.dim) hidden8(r, row, k, v);
     store_planes(v, compact + static_cast<uint64_t>(c) * ld + k, static_cast<uint64_t>(padded) * ld, head_hidden_planes(r.hidden_bf16));
   }
-  if (backward) entries_of(r, a, c, row, lane, id_of, q_of);
+  if (backward) entries_of(r, a, c, c == nth ? row : -1, lane, id_of, q_of);
 }
 
 __global__ __launch_bounds__(256) void eco_head_scatter_kernel(const int32_t *ids, const float *values, const HeadRowConst *consts, uint32_t entries, const int32_t *count, uint64_t first, uint32_t n,
@@ -1228,25 +1234,43 @@ __global__ __launch_bounds__(256) void eco_head_scatter_kernel(const int32_t *id
   }
 }
 
-// The gradient of the hidden states: each row's parts summed in their order, four columns to a thread; zeros where a row takes no part.
-__global__ __launch_bounds__(256) void eco_head_grad_hidden_finish_kernel(const HeadRowConst *consts, const float *partial, uint32_t splits, uint32_t ld, uint64_t stride, HeadRows r, void *out,
-                                                                          uint64_t out_stride) {
-  const uint32_t chunks = (r.dim + 3) / 4;
-  const uint64_t work = static_cast<uint64_t>(r.rows) * chunks, step = static_cast<uint64_t>(gridDim.x) * 256;
+// The gradient of the hidden states: each row's parts summed, four columns to a thread; zeros where a row takes no part.  WAYS threads take every WAYSth part
+// each where there are many, and their sums are added in order.
+template <int WAYS>
+__global__ __launch_bounds__(256) void eco_head_grad_hidden_finish_kernel(const HeadRowConst *consts, const float *partial, uint32_t splits, uint32_t ld, uint64_t stride, uint32_t stack,
+                                                                          HeadRows r, void *out, uint64_t out_stride) {
+  constexpr uint32_t EACH = 256 / WAYS;
+  __shared__ float4 sums[WAYS > 1 ? 256 : 1];
+  const uint32_t chunks = (r.dim + 3) / 4, way = threadIdx.x / EACH;
+  const uint64_t work = static_cast<uint64_t>(r.rows) * chunks, step = static_cast<uint64_t>(gridDim.x) * EACH;
   const float unit = grad_unit(consts);
   const bool whole = out_stride % 4 == 0 && r.dim % 4 == 0 && (reinterpret_cast<uintptr_t>(out) & 15) == 0;
-  for (uint64_t i = static_cast<uint64_t>(blockIdx.x) * 256 + threadIdx.x; i < work; i += step) {
+  for (uint64_t begin = static_cast<uint64_t>(blockIdx.x) * EACH; begin < work; begin += step) {
+    const uint64_t i = begin + threadIdx.x % EACH < work ? begin + threadIdx.x % EACH : work - 1;
     const uint32_t row = i >> 32 ? static_cast<uint32_t>(i / chunks) : static_cast<uint32_t>(i) / chunks, k = static_cast<uint32_t>(i - static_cast<uint64_t>(row) * chunks) * 4;
     const int32_t c = r.place[row];
     float4 sum = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
     if (c >= 0) {
       const float *p = partial + static_cast<uint64_t>(c) * ld + k;
+      for (uint32_t rows = 0; rows <= stack; rows += HEAD_STACK, p += HEAD_STACK * static_cast<uint64_t>(ld))
 #pragma unroll 8
-      for (uint32_t s = 0; s < splits; ++s) {
-        const float4 v = *reinterpret_cast<const float4 *>(p + s * stride);
-        sum.x += v.x; sum.y += v.y; sum.z += v.z; sum.w += v.w;
-      }
+        for (uint32_t s = way; s < splits; s += WAYS) {
+          const float4 v = *reinterpret_cast<const float4 *>(p + s * stride);
+          sum.x += v.x; sum.y += v.y; sum.z += v.z; sum.w += v.w;
+        }
     }
+    if constexpr (WAYS > 1) {
+      sums[threadIdx.x] = sum;
+      __syncthreads();
+      if (way == 0)
+#pragma unroll
+        for (int q = 1; q < WAYS; ++q) {
+          const float4 v = sums[q * EACH + threadIdx.x];
+          sum.x += v.x; sum.y += v.y; sum.z += v.z; sum.w += v.w;
+        }
+      __syncthreads();
+    }
+    if (way != 0 || begin + threadIdx.x >= work) continue;
     sum.x *= unit; sum.y *= unit; sum.z *= unit; sum.w *= unit;
     const uint64_t at = row * out_stride + k;
     const float v[4] = {sum.x, sum.y, sum.z, sum.w};
@@ -1486,15 +1510,15 @@ hipError_t launch_head_entries(const HeadRows &r, uint32_t padded_rows, const fl
 hipError_t launch_head_few_rows(const HeadRows &r, const HeadWeights &w, void *compact, uint32_t padded_rows, uint32_t padded_dim, float *picked, hipStream_t s) {
   return by_format(w, r.dim, [&](auto fmt, auto whole) {
     hipLaunchKernelGGL((eco_head_few_rows_kernel<fmt.value, whole.value>), dim3(padded_rows + r.rows * (r.top_k + 1)), dim3(64), 0, s, r, w, EntryArgs{},
-                       static_cast<uint16_t *>(compact), padded_rows, padded_dim, 0, picked);
+                       static_cast<uint16_t *>(compact), padded_rows, padded_dim, 0, 0u, picked);
   });
 }
-hipError_t launch_head_few_rows_backward(const HeadRows &r, void *compact, uint32_t padded_rows, uint32_t padded_dim, const float *grad_ce, const float *grad_kd, const float *lse,
+hipError_t launch_head_few_rows_backward(const HeadRows &r, uint32_t stack, void *compact, uint32_t padded_rows, uint32_t padded_dim, const float *grad_ce, const float *grad_kd, const float *lse,
                                          const float *lse_tau, const float *picked, int softmaxes, int32_t *ids, float *values, HeadRowConst *consts, hipStream_t s) {
   const EntryArgs a = {grad_ce, grad_kd, lse, lse_tau, picked, softmaxes, ids, values, consts};
   // (no dot products: the format does not matter)
   hipLaunchKernelGGL((eco_head_few_rows_kernel<FMT_BF16_PLAIN, true>), dim3(padded_rows), dim3(64), 0, s, r, HeadWeights{}, a, static_cast<uint16_t *>(compact), padded_rows,
-                     padded_dim, 1, static_cast<float *>(nullptr));
+                     padded_dim, 1, stack, static_cast<float *>(nullptr));
   return hipGetLastError();
 }
 
@@ -1515,29 +1539,33 @@ hipError_t launch_head_scatter(const int32_t *ids, const float *values, const He
   return hipGetLastError();
 }
 
-hipError_t launch_head_grad_hidden(int shape, const HeadOperand &w, const HeadOperand &g, uint32_t n, uint32_t rows, uint32_t dim, const int32_t *count, uint32_t order,
+hipError_t launch_head_grad_hidden(int shape, uint32_t stack, const HeadOperand &w, const HeadOperand &g, uint32_t n, uint32_t rows, uint32_t dim, const int32_t *count, uint32_t order,
                                    uint32_t splits, float *partial, uint32_t partial_ld, uint64_t partial_stride, int add, hipStream_t s) {
   ProductArgs a = product(w, g);
-  a.nx = dim; a.k = n; a.count = count; a.order = order;
+  a.nx = dim; a.k = n; a.count = count; a.order = order; a.stack = stack;
   // no part is empty: a last, shorter piece of the vocabulary may make do with fewer
   const uint32_t steps = (n + KSTEP - 1) / KSTEP;
   a.split_steps = (steps + splits - 1) / splits;
   a.splits = (steps + a.split_steps - 1) / a.split_steps;
   a.out_f32 = partial; a.out_ld = partial_ld; a.out_plane = partial_stride; a.add = add;
-  return dim_tile(shape, dim) == Large192::BX ? launch_tiles<DH, Large192>(a, dim, rows, s) : launch_product<DH>(a, shape, dim, rows, s);
+  return dim_tile(shape, dim) == Large192::BX ? launch_tiles<DH, Large192>(a, dim, rows, s) : launch_product<DH>(a, shape, dim, rows + stack, s);
 }
 
-hipError_t launch_head_grad_hidden_finish(const HeadRowConst *consts, const float *partial, uint32_t splits, uint32_t partial_ld, uint64_t partial_stride, const HeadRows &r, void *out,
+hipError_t launch_head_grad_hidden_finish(const HeadRowConst *consts, const float *partial, uint32_t splits, uint32_t partial_ld, uint64_t partial_stride, uint32_t stack, const HeadRows &r, void *out,
                                           uint64_t out_stride, hipStream_t s) {
-  hipLaunchKernelGGL(eco_head_grad_hidden_finish_kernel, dim3(blocks_for(static_cast<uint64_t>(r.rows) * ((r.dim + 3) / 4))), dim3(256), 0, s, consts, partial, splits, partial_ld,
-                     partial_stride, r, out, out_stride);
+  const uint64_t work = static_cast<uint64_t>(r.rows) * ((r.dim + 3) / 4);
+  if (splits >= 16)
+    hipLaunchKernelGGL(eco_head_grad_hidden_finish_kernel<8>, dim3(blocks_for(8 * work)), dim3(256), 0, s, consts, partial, splits, partial_ld, partial_stride, stack, r, out, out_stride);
+  else
+    hipLaunchKernelGGL(eco_head_grad_hidden_finish_kernel<1>, dim3(blocks_for(work)), dim3(256), 0, s, consts, partial, splits, partial_ld,
+                     partial_stride, stack, r, out, out_stride);
   return hipGetLastError();
 }
 
-hipError_t launch_head_grad_weights(int shape, const HeadOperand &h, const HeadOperand &g, uint32_t n, uint32_t dim, const int32_t *count, uint32_t order,
+hipError_t launch_head_grad_weights(int shape, uint32_t stack, const HeadOperand &h, const HeadOperand &g, uint32_t n, uint32_t dim, const int32_t *count, uint32_t order,
                                     const HeadRowConst *consts, void *out, uint64_t out_stride, int out_bf16, int past_caches, hipStream_t s) {
   ProductArgs a = product(h, g);
-  a.nx = dim; a.ny = n; a.count = count; a.order = order; a.consts = consts;
+  a.nx = dim; a.ny = n; a.count = count; a.order = order; a.consts = consts; a.stack = stack;
   a.out = out; a.out_ld = out_stride; a.out_bf16 = out_bf16;
   const auto go = [&](auto mode) {
     // (few rows: the tiles are all stores, and twice a chip's worth of large ones are the faster ones, 67 x 1152 x 262144 149 / 188 us, 32 rows 115 / 140; 1 x
