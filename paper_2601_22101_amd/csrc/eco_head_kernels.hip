@@ -111,20 +111,38 @@ __device__ __forceinline__ void store_planes(const float (&v)[8], uint16_t *dst,
   }
 }
 
+// A value at an address of any alignment.
+template <class V>
+__device__ __forceinline__ V loose(const void *p) {
+  V v;
+  __builtin_memcpy(&v, p, sizeof v);
+  return v;
+}
+__device__ __forceinline__ void bf16_values(uint4 u, float (&v)[8]) {
+  const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+  for (int j = 0; j < 8; ++j) v[j] = (j & 1) ? bf16_hi(w[j / 2]) : bf16_lo(w[j / 2]);
+}
+__device__ __forceinline__ void fp32_values(const float *p, float (&v)[8]) {
+  const float4 a = loose<float4>(p), b = loose<float4>(p + 4);
+  v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+}
+
 // Eight hidden states of a row from element k on, those past dim 0.
 __device__ __forceinline__ void hidden8(const HeadRows &r, uint64_t row, uint32_t k, float (&v)[8]) {
   const uint64_t at = row * r.hidden_stride + k;
   if (r.hidden_whole) {
-    if (r.hidden_bf16) {
-      const uint4 u = *reinterpret_cast<const uint4 *>(static_cast<const uint16_t *>(r.hidden) + at);
-      const uint32_t w[4] = {u.x, u.y, u.z, u.w};
-#pragma unroll
-      for (int j = 0; j < 8; ++j) v[j] = (j & 1) ? bf16_hi(w[j / 2]) : bf16_lo(w[j / 2]);
-    } else {
+    if (r.hidden_bf16) bf16_values(*reinterpret_cast<const uint4 *>(static_cast<const uint16_t *>(r.hidden) + at), v);
+    else {
       const float4 *p = reinterpret_cast<const float4 *>(static_cast<const float *>(r.hidden) + at);
       const float4 a = p[0], b = p[1];
       v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
     }
+    return;
+  }
+  if (k + 8 <= r.dim) {
+    if (r.hidden_bf16) bf16_values(loose<uint4>(static_cast<const uint16_t *>(r.hidden) + at), v);
+    else fp32_values(static_cast<const float *>(r.hidden) + at, v);
     return;
   }
 #pragma unroll
@@ -163,33 +181,37 @@ __device__ __forceinline__ float weight_at(const HeadWeights &w, uint64_t row, u
 }
 
 // Eight weights of a row from element k (a multiple of 8) on, those past dim 0.  WHOLE: rows are whole pieces of eight, which then lie in one
-// scale group and are one aligned load.
+// scale group and are one aligned load; else a piece may lie at any address and in two groups.
 template <int FMT, bool WHOLE>
 __device__ __forceinline__ void weights8(const HeadWeights &w, uint64_t row, uint32_t dim, uint32_t k, float (&v)[8]) {
-  if constexpr (!WHOLE) {
+  const uint64_t i = row * dim + k;
+  // (an odd nibble to begin with is left to the single elements)
+  if (!WHOLE && (k + 8 > dim || (FMT == FMT_INT4 && (i & 1)))) {
 #pragma unroll
     for (int j = 0; j < 8; ++j) v[j] = k + j < dim ? weight_at<FMT>(w, row, dim, k + j) : 0.0f;
-  } else if constexpr (FMT == FMT_BF16_PLAIN) {
-    const uint4 u = *reinterpret_cast<const uint4 *>(static_cast<const uint16_t *>(w.data) + row * w.stride + k);
-    const uint32_t x[4] = {u.x, u.y, u.z, u.w};
-#pragma unroll
-    for (int j = 0; j < 8; ++j) v[j] = (j & 1) ? bf16_hi(x[j / 2]) : bf16_lo(x[j / 2]);
+    return;
+  }
+  if constexpr (FMT == FMT_BF16_PLAIN) {
+    const uint16_t *p = static_cast<const uint16_t *>(w.data) + row * w.stride + k;
+    bf16_values(WHOLE ? *reinterpret_cast<const uint4 *>(p) : loose<uint4>(p), v);
   } else if constexpr (FMT == FMT_FP32_ID) {
-    const float4 *p = reinterpret_cast<const float4 *>(static_cast<const float *>(w.data) + row * w.stride + k);
-    const float4 a = p[0], b = p[1];
-    v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+    fp32_values(static_cast<const float *>(w.data) + row * w.stride + k, v);
   } else {
-    const uint64_t i = row * dim + k;
-    const float s = scale_at(w, i);
     if constexpr (FMT == FMT_FP8) {
-      const uint2 u = *reinterpret_cast<const uint2 *>(static_cast<const uint8_t *>(w.data) + i);
-      v[0] = e4m3_decode<0>(u.x) * s; v[1] = e4m3_decode<1>(u.x) * s; v[2] = e4m3_decode<2>(u.x) * s; v[3] = e4m3_decode<3>(u.x) * s;
-      v[4] = e4m3_decode<0>(u.y) * s; v[5] = e4m3_decode<1>(u.y) * s; v[6] = e4m3_decode<2>(u.y) * s; v[7] = e4m3_decode<3>(u.y) * s;
+      const uint8_t *p = static_cast<const uint8_t *>(w.data) + i;
+      const uint2 u = WHOLE ? *reinterpret_cast<const uint2 *>(p) : loose<uint2>(p);
+      v[0] = e4m3_decode<0>(u.x); v[1] = e4m3_decode<1>(u.x); v[2] = e4m3_decode<2>(u.x); v[3] = e4m3_decode<3>(u.x);
+      v[4] = e4m3_decode<0>(u.y); v[5] = e4m3_decode<1>(u.y); v[6] = e4m3_decode<2>(u.y); v[7] = e4m3_decode<3>(u.y);
     } else {
-      const uint32_t u = *reinterpret_cast<const uint32_t *>(static_cast<const uint8_t *>(w.data) + (i >> 1));
+      const uint8_t *p = static_cast<const uint8_t *>(w.data) + (i >> 1);
+      const uint32_t u = WHOLE ? *reinterpret_cast<const uint32_t *>(p) : loose<uint32_t>(p);
 #pragma unroll
-      for (int j = 0; j < 8; ++j) v[j] = static_cast<float>(static_cast<int32_t>(u << (28 - 4 * j)) >> 28) * s;
+      for (int j = 0; j < 8; ++j) v[j] = static_cast<float>(static_cast<int32_t>(u << (28 - 4 * j)) >> 28);
     }
+    const float s = scale_at(w, i), s7 = WHOLE ? s : scale_at(w, i + 7);
+    const uint64_t in = WHOLE || w.group_shift >= 40 ? 0 : w.group_shift >= 0 ? i & ((1ull << w.group_shift) - 1) : i % w.group;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] *= WHOLE || in + j < w.group ? s : s7;
   }
 }
 
