@@ -17,6 +17,7 @@ constexpr uint64_t head_round_up(uint64_t x, uint64_t k) { return (x + k - 1) / 
 // relative 2^-17, beside a bf16's 2^-8; a logit of a thousand such terms is off by a relative 2^-22).
 constexpr int head_weight_planes(int fmt) { return fmt == 2 ? 1 : fmt == 3 ? 3 : 2; }
 constexpr int head_hidden_planes(int dtype_bf16) { return dtype_bf16 ? 1 : 3; }
+constexpr int head_hidden_half_planes(int dtype_bf16) { return dtype_bf16 ? 1 : 2; }      // as fp16 planes of a scaled row; weights: 2
 
 // Pairs of two operands' planes whose product counts: the sum of their places is at most `order`.  2 leaves out less than a relative 2^-22 of a
 // product, 1 less than 2^-15, which is what a result that ends as a bf16 needs.
@@ -38,6 +39,7 @@ struct HeadOperand {
   const void *data;
   uint64_t plane;                                 // elements between planes
   uint32_t ld, planes;
+  const int32_t *back;                            // fp16 planes: the power of two that each row is multiplied by in the end; null: bf16 planes
 };
 
 struct HeadRows {                                 // a forward or backward call's inputs, as its small kernels take them
@@ -61,6 +63,9 @@ struct HeadStats {                                // the logits' statistics by r
 
 hipError_t launch_head_rows(const HeadRows &, void *compact, uint32_t padded_rows, uint32_t padded_dim, hipStream_t);
 hipError_t launch_head_convert(const HeadWeights &, uint64_t first, uint32_t rows, uint32_t dim, void *planes, uint32_t ld, uint64_t plane, hipStream_t);
+// fp16 planes of scaled rows
+hipError_t launch_head_convert_half(const HeadWeights &, uint64_t first, uint32_t rows, uint32_t dim, void *planes, uint32_t ld, uint64_t plane, int32_t *back, hipStream_t);
+hipError_t launch_head_gather_half(const HeadRows &, void *compact, uint32_t padded_rows, uint32_t padded_dim, int32_t *back, hipStream_t);
 // Workgroups of the kernel for few rows over `vocab` rows of weights, which reads them as they are stored; 0: it does not take the call.
 uint32_t head_few(const HeadWeights &, int hidden_bf16, uint64_t rows, uint64_t dim, uint64_t vocab);
 // logits' statistics of vocabulary rows first .. first + n - 1, whose tiles begin at `tile`; `few`: the weights for that kernel, then one tile to a

@@ -97,7 +97,8 @@ eco::HeadWeights weights_of(const eco_head_t *h) {
 struct Layout {
   uint32_t padded_rows, padded_dim, entries, piece, hidden_planes, weight_planes, grad_planes, tiles, splits, few, pair_order, stack;
   int shape;
-  bool in_place, two;
+  bool in_place, two, half;
+  uint64_t half_planes, half_compact, half_back, half_rows_back;
   uint64_t count, order, place, flags, compact, planes, max, sum, sum_tau, ids, values, consts, g, partial, bytes;
 };
 
@@ -135,8 +136,15 @@ Layout layout_of(const eco_head_t *h, bool backward) {
   };
   // few rows: the logits' kernel of the forward pass reads any format where it lies
   l.few = eco::head_few(weights_of(h), h->hidden_dtype == ECO_DT_BF16, h->rows, h->dim, h->vocab);
-  const bool converts = !l.in_place && (backward || !l.few);
-  if (converts) limit(2ull * l.padded_dim * l.weight_planes);
+  // Weights that are no bf16 make the logits of fp16 planes (see half_exponent): in the losses always, where those take fewer products, fewer bytes, or are
+  // the more exact ones.  The gradients need the bf16 planes too, and making and reading others takes as long as one of the logits' products of 750 rows
+  // (training, us in the kernels, with and without: fp32 30 x 1024 x 50304 582 505, which saves three products; bf16 and fp32 700 x 1024 x 50304 1516
+  // 1502, one; fp32 and FP8 of the same sizes 1675 1753, two).
+  const uint32_t half_pairs = eco::head_pairs(2, eco::head_hidden_half_planes(h->hidden_dtype == ECO_DT_BF16), 1);
+  const uint32_t saved = eco::head_pairs(l.weight_planes, l.hidden_planes, backward ? l.pair_order : 2) - half_pairs;
+  l.half = !l.few && h->fmt != ECO_FMT_BF16_PLAIN && (!backward || saved * h->rows >= 1024);
+  const bool converts = !l.in_place && (backward || (!l.few && !l.half));
+  if (converts || l.half) limit(2ull * l.padded_dim * l.weight_planes);
   if (backward) limit(2ull * l.padded_rows * l.grad_planes);
   if (backward) piece = eco::head_piece(l.shape, h->rows, h->dim, h->vocab, piece);
   l.piece = static_cast<uint32_t>(piece);
@@ -148,6 +156,12 @@ Layout layout_of(const eco_head_t *h, bool backward) {
   l.place = take(4 * h->rows);
   l.flags = take(h->top_k ? h->rows : 0);
   l.compact = take(2ull * l.hidden_planes * l.padded_rows * l.padded_dim);
+  if (l.half) {
+    l.half_planes = take(4ull * piece * l.padded_dim);
+    l.half_compact = take(4ull * l.padded_rows * l.padded_dim);
+    l.half_back = take(4ull * (piece + 256));               // (a tile reads all of its rows')
+    l.half_rows_back = take(4ull * l.padded_rows);
+  }
   if (converts) l.planes = take(2ull * l.weight_planes * piece * l.padded_dim);
   if (!backward) {
     l.max = take(4ull * h->rows * l.tiles);
@@ -189,19 +203,32 @@ eco::HeadRows rows_of(const eco_head_t *h, const Layout &l, char *ws) {
 }
 
 eco::HeadOperand hidden_operand(const Layout &l, char *ws) {
-  return {ws + l.compact, static_cast<uint64_t>(l.padded_rows) * l.padded_dim, l.padded_dim, l.hidden_planes};
+  return {ws + l.compact, static_cast<uint64_t>(l.padded_rows) * l.padded_dim, l.padded_dim, l.hidden_planes, nullptr};
 }
 
 // Weights first .. first + n - 1 as an operand: where they lie, or converted into the workspace.
 hipError_t weight_operand(const eco_head_t *h, const Layout &l, char *ws, uint64_t first, uint32_t n, hipStream_t s, eco::HeadOperand *out) {
   const eco::HeadWeights w = weights_of(h);
   if (l.in_place) {
-    *out = {static_cast<const uint16_t *>(h->weights) + first * w.stride, 0, static_cast<uint32_t>(w.stride), 1};
+    *out = {static_cast<const uint16_t *>(h->weights) + first * w.stride, 0, static_cast<uint32_t>(w.stride), 1, nullptr};
     return hipSuccess;
   }
   const uint64_t plane = static_cast<uint64_t>(l.piece) * l.padded_dim;
-  *out = {ws + l.planes, plane, l.padded_dim, l.weight_planes};
+  *out = {ws + l.planes, plane, l.padded_dim, l.weight_planes, nullptr};
   return eco::launch_head_convert(w, first, n, static_cast<uint32_t>(h->dim), ws + l.planes, l.padded_dim, plane, s);
+}
+
+// The same as fp16 planes of scaled rows, and the hidden states so.
+hipError_t half_weight_operand(const eco_head_t *h, const Layout &l, char *ws, uint64_t first, uint32_t n, hipStream_t s, eco::HeadOperand *out) {
+  const uint64_t plane = static_cast<uint64_t>(l.piece) * l.padded_dim;
+  int32_t *back = reinterpret_cast<int32_t *>(ws + l.half_back);
+  *out = {ws + l.half_planes, plane, l.padded_dim, 2, back};
+  return eco::launch_head_convert_half(weights_of(h), first, n, static_cast<uint32_t>(h->dim), ws + l.half_planes, l.padded_dim, plane, back, s);
+}
+hipError_t half_hidden_operand(const eco::HeadRows &r, const Layout &l, char *ws, hipStream_t s, eco::HeadOperand *out) {
+  int32_t *back = reinterpret_cast<int32_t *>(ws + l.half_rows_back);
+  *out = {ws + l.half_compact, static_cast<uint64_t>(l.padded_rows) * l.padded_dim, l.padded_dim, static_cast<uint32_t>(eco::head_hidden_half_planes(r.hidden_bf16)), back};
+  return eco::launch_head_gather_half(r, ws + l.half_compact, l.padded_rows, l.padded_dim, back, s);
 }
 
 }  // namespace
@@ -241,11 +268,14 @@ eco_status_t eco_head_loss(const eco_head_t *head, void *workspace, size_t works
   const eco::HeadStats stats = {reinterpret_cast<float *>(ws + l.max), reinterpret_cast<float *>(ws + l.sum),
                                 l.two ? reinterpret_cast<float *>(ws + l.sum_tau) : nullptr, l.tiles};
   const uint32_t tile = eco::head_tiles(l.shape).vocab;
+  eco::HeadOperand hidden = hidden_operand(l, ws);
+  if (l.half) HEAD_LAUNCH(half_hidden_operand(r, l, ws, s, &hidden));
   for (uint64_t first = 0; first < head->vocab; first += l.piece) {
     const uint32_t n = static_cast<uint32_t>(head->vocab - first < l.piece ? head->vocab - first : l.piece);
     eco::HeadOperand w = {};
-    if (!l.few) HEAD_LAUNCH(weight_operand(head, l, ws, first, n, s, &w));
-    HEAD_LAUNCH(eco::launch_head_stats(l.shape, w, l.few ? &weights : nullptr, first, hidden_operand(l, ws), n, r.rows, r.dim, r.count, 1.0f / r.tau, stats, static_cast<uint32_t>(first / tile), s));
+    if (l.half) HEAD_LAUNCH(half_weight_operand(head, l, ws, first, n, s, &w));
+    else if (!l.few) HEAD_LAUNCH(weight_operand(head, l, ws, first, n, s, &w));
+    HEAD_LAUNCH(eco::launch_head_stats(l.shape, w, l.few ? &weights : nullptr, first, hidden, n, r.rows, r.dim, r.count, 1.0f / r.tau, stats, static_cast<uint32_t>(first / tile), s));
   }
   HEAD_LAUNCH(eco::launch_head_finish(r, weights, stats, few, head->labels ? head->ce : nullptr, head->top_k ? head->kd : nullptr,
                                       head->labels ? head->lse : nullptr, head->top_k ? head->lse_tau : nullptr, head->picked, s));
@@ -278,7 +308,9 @@ eco_status_t eco_head_loss_backward(const eco_head_t *head, void *workspace, siz
   }
   const uint64_t g_plane = static_cast<uint64_t>(l.stack ? l.stack : l.padded_rows) * l.piece, partial_stride = static_cast<uint64_t>(l.padded_rows) * l.padded_dim;
   const eco::HeadOperand hidden = hidden_operand(l, ws);
-  const eco::HeadOperand g = {ws + l.g, g_plane, l.piece, l.stack ? 1 : l.grad_planes};
+  eco::HeadOperand half_hidden = {}, half_w = {};
+  if (l.half) HEAD_LAUNCH(half_hidden_operand(r, l, ws, s, &half_hidden));
+  const eco::HeadOperand g = {ws + l.g, g_plane, l.piece, l.stack ? 1 : l.grad_planes, nullptr};
   const uint64_t out_stride = stride_or(head->grad_weights_stride, head->dim);
   const eco::HeadWeights weights = weights_of(head);
   // A gradient that the 256 MB cache in front of HBM cannot hold passes the caches by: on its way out it would take the place of the weights, which the next
@@ -288,7 +320,8 @@ eco_status_t eco_head_loss_backward(const eco_head_t *head, void *workspace, siz
     const uint32_t n = static_cast<uint32_t>(head->vocab - first < l.piece ? head->vocab - first : l.piece);
     eco::HeadOperand w;
     HEAD_LAUNCH(weight_operand(head, l, ws, first, n, s, &w));
-    HEAD_LAUNCH(eco::launch_head_grad(l.shape, w, l.few ? &weights : nullptr, first, hidden, n, r.rows, r.dim, r.count, 1.0f / r.tau, softmaxes,
+    if (l.half) HEAD_LAUNCH(half_weight_operand(head, l, ws, first, n, s, &half_w));
+    HEAD_LAUNCH(eco::launch_head_grad(l.shape, l.half ? half_w : w, l.few ? &weights : nullptr, first, l.half ? half_hidden : hidden, n, r.rows, r.dim, r.count, 1.0f / r.tau, softmaxes,
                                       l.pair_order, consts, ws + l.g, l.piece, g_plane, l.grad_planes, s));
     HEAD_LAUNCH(eco::launch_head_scatter(ids, values, consts, r.rows, l.entries, r.count, first, n, ws + l.g, l.piece, g_plane, l.grad_planes, s));
     HEAD_LAUNCH(eco::launch_head_grad_hidden(l.shape, l.stack, w, g, n, r.rows, r.dim, r.count, l.pair_order, l.splits, partial, l.padded_dim, partial_stride, first != 0, s));

@@ -227,6 +227,74 @@ __global__ __launch_bounds__(256) void eco_head_convert_kernel(HeadWeights w, ui
   }
 }
 
+// ------------------------------------------------------------------------------------------------ fp16 planes
+
+// Logits of fp32 operands in three products instead of six: a row scaled by a power of two to a largest value in [2^14, 2^15) is two fp16 terms of 11 bits
+// of significand each, a bf16 row one.  What that leaves of a value is below 2^-24 of it, and 2^-39 of the row's largest where a term falls among fp16's
+// subnormal numbers, which a sum over the row does not see; the logits' gradient, whose single values count, stays in bf16 terms.
+__device__ __forceinline__ int half_exponent(float largest) {
+  const int exponent = static_cast<int>(f2u(largest) >> 23) - 127;
+  return largest == 0.0f ? 0 : exponent < -86 ? 100 : 14 - exponent;
+}
+typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ void store_half_planes(const float (&v)[8], float scale, uint16_t *dst, uint64_t plane, uint32_t planes) {
+  float rest[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) rest[i] = v[i] * scale;
+  for (uint32_t p = 0; p < planes; ++p) {
+    uint32_t two[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const eco_f32x2_t x = {rest[2 * i], rest[2 * i + 1]};
+      const f16x2 h = __builtin_convertvector(x, f16x2);
+      two[i] = __builtin_bit_cast(uint32_t, h);
+      const float lo = static_cast<float>(h.x), hi = static_cast<float>(h.y);
+      rest[2 * i] = fabsf(lo) < INFINITY ? rest[2 * i] - lo : 0.0f;
+      rest[2 * i + 1] = fabsf(hi) < INFINITY ? rest[2 * i + 1] - hi : 0.0f;
+    }
+    *reinterpret_cast<uint4 *>(dst + p * plane) = make_uint4(two[0], two[1], two[2], two[3]);
+  }
+}
+__device__ __forceinline__ float wave_max(float x) {
+#pragma unroll
+  for (int d = 32; d; d >>= 1) x = fmaxf(x, __shfl_xor(x, d));
+  return x;
+}
+// A row by one wave, `get(k, v)` its eight values from k on.
+template <class F>
+__device__ __forceinline__ void half_row(uint32_t dim, uint32_t ld, int lane, F get, uint16_t *dst, uint64_t plane, uint32_t planes, int32_t *back) {
+  float largest = 0.0f, v[8];
+  for (uint32_t k = lane * 8; k < dim; k += 512) {
+    get(k, v);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) largest = fmaxf(largest, fabsf(v[i]) < INFINITY ? fabsf(v[i]) : 0.0f);
+  }
+  const int up = half_exponent(wave_max(largest));
+  const float scale = u2f(static_cast<uint32_t>(127 + up) << 23);
+  if (lane == 0) *back = -up;
+  for (uint32_t k = lane * 8; k < ld; k += 512) {
+    if (k < dim) get(k, v);
+    else
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[i] = 0.0f;
+    store_half_planes(v, scale, dst + k, plane, planes);
+  }
+}
+template <int FMT, bool WHOLE>
+__global__ __launch_bounds__(256) void eco_head_convert_half_kernel(HeadWeights w, uint64_t first, uint32_t rows, uint32_t dim, uint16_t *dst, uint32_t ld, uint64_t plane, int32_t *back) {
+  const int lane = threadIdx.x & 63;
+  for (uint32_t row = blockIdx.x * 4 + (threadIdx.x >> 6); row < rows; row += gridDim.x * 4)
+    half_row(dim, ld, lane, [&](uint32_t k, float (&v)[8]) { weights8<FMT, WHOLE>(w, first + row, dim, k, v); }, dst + static_cast<uint64_t>(row) * ld, plane, 2, back + row);
+}
+__global__ __launch_bounds__(256) void eco_head_gather_half_kernel(HeadRows r, uint16_t *compact, uint32_t padded, uint32_t ld, uint32_t planes, int32_t *back) {
+  const int lane = threadIdx.x & 63;
+  const uint32_t c = blockIdx.x * 4 + (threadIdx.x >> 6), count = static_cast<uint32_t>(*r.count);
+  if (c >= padded) return;
+  const int64_t row = c < count ? r.order[c] : -1;
+  half_row(row < 0 ? 0 : r.dim, ld, lane, [&](uint32_t k, float (&v)[8]) { hidden8(r, row, k, v); }, compact + static_cast<uint64_t>(c) * ld, static_cast<uint64_t>(padded) * ld,
+           planes, back + c);
+}
+
 // ------------------------------------------------------------------------------------------------ products
 
 // What the logits' gradient is divided by, see HeadRowConst.
@@ -243,8 +311,11 @@ __device__ __forceinline__ float grad_unit(const HeadRowConst *consts) {
 //   DW     x hidden dimension, y vocabulary, k rows: the gradient of the weights
 // With x along a lane's registers, four neighbours in each group, a row's softmax is a reduction over registers and every end stores
 // neighbours together.
-// GRAD_PLANES is GRAD with g in several planes, DW_PAST is DW with stores past the caches.
-enum : int { STATS = 0, GRAD = 1, DH = 2, DW = 3, GRAD_PLANES = 4, DW_PAST = 5 };
+// GRAD_PLANES is GRAD with g in several planes, DW_PAST is DW with stores past the caches.  The HALF ones multiply fp16 planes of scaled rows.
+enum : int { STATS = 0, GRAD = 1, DH = 2, DW = 3, GRAD_PLANES = 4, DW_PAST = 5, STATS_HALF = 6, GRAD_HALF = 7 };
+constexpr bool is_half(int mode) { return mode == STATS_HALF || mode == GRAD_HALF; }
+constexpr bool is_stats(int mode) { return mode == STATS || mode == STATS_HALF; }
+constexpr bool is_grad(int mode) { return mode == GRAD || mode == GRAD_PLANES || mode == GRAD_HALF; }
 constexpr bool is_dw(int mode) { return mode == DW || mode == DW_PAST; }
 
 struct ProductArgs {
@@ -262,6 +333,7 @@ struct ProductArgs {
   int32_t two, out_bf16, add;
   float *sum, *sum_tau;
   const HeadRowConst *consts;
+  const int32_t *x_back, *y_back;                 // exponents of the rows of fp16 operands
 };
 
 constexpr int KSTEP = HEAD_K_STEP;
@@ -300,9 +372,9 @@ struct Tile {
 };
 // Bytes of LDS past the steps: of the statistics three arrays [WX][BY], else 32 rows of 64 bf16 or 32 fp32 (of 32 bf16 where a wave has no more) to a wave
 template <int MODE, class T>
-constexpr int own_bytes() { return (MODE == GRAD || MODE == GRAD_PLANES) && T::NI == 1 ? 2048 : 4096; }
+constexpr int own_bytes() { return is_grad(MODE) && T::NI == 1 ? 2048 : 4096; }
 template <int MODE, class T>
-constexpr int extra_bytes() { return MODE == STATS ? 3 * T::WX * T::BY * 4 : T::WX * T::WY * own_bytes<MODE, T>(); }
+constexpr int extra_bytes() { return is_stats(MODE) ? 3 * T::WX * T::BY * 4 : T::WX * T::WY * own_bytes<MODE, T>(); }
 
 // Where the 16-byte piece `c` of a step's operand comes from.  A row operand's step is rows of 128 bytes, a column operand's 64 rows of
 // N elements; the pieces of a row are exchanged so that lanes which read together, sixteen of 16 bytes or half a wave of 8, find theirs in
@@ -391,11 +463,18 @@ __device__ __forceinline__ uint32_t xcd_run(uint32_t id, uint32_t all) {
   return xcd * each + min(xcd, more) + nth;
 }
 
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+template <bool HALF>
+__device__ __forceinline__ f32x16 multiply(bf16x8 x, bf16x8 y, f32x16 acc) {
+  if constexpr (HALF) return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, x), __builtin_bit_cast(f16x8, y), acc, 0, 0, 0);
+  else return __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, y, acc, 0, 0, 0);
+}
+
 // A workgroup goes through tiles gridDim.x apart.  Its loads do not stop between them: while a tile's results leave, the next tile's
 // first steps are on their way.
 template <int MODE, class T>
 __global__ __launch_bounds__(T::THREADS) void eco_head_product_kernel(ProductArgs a) {
-  constexpr bool X_COLUMN = MODE == DH || is_dw(MODE), Y_COLUMN = is_dw(MODE), LOGITS = MODE == STATS || MODE == GRAD || MODE == GRAD_PLANES;
+  constexpr bool X_COLUMN = MODE == DH || is_dw(MODE), Y_COLUMN = is_dw(MODE), LOGITS = is_stats(MODE) || is_grad(MODE);
   constexpr int NI = T::NI, NJ = T::NJ, QUARTERS = KSTEP / 16;
   __shared__ __attribute__((aligned(1024))) char smem[T::DEPTH * T::STEP_BYTES + extra_bytes<MODE, T>()];
   static_assert(sizeof smem <= 163840, "a compute unit's LDS");
@@ -544,7 +623,7 @@ __global__ __launch_bounds__(T::THREADS) void eco_head_product_kernel(ProductArg
 #pragma unroll
         for (int i = 0; i < NI; ++i)
 #pragma unroll
-          for (int j = 0; j < NJ; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fx[kk & 1][i], fy[kk & 1][j], acc[i][j], 0, 0, 0);
+          for (int j = 0; j < NJ; ++j) acc[i][j] = multiply<is_half(MODE)>(fx[kk & 1][i], fy[kk & 1][j], acc[i][j]);
         // a read of LDS or two, then a product, and so on: the products hide the reads (8192 x 2048 x 65536, training, 7.43 -> 7.28 ms)
         constexpr int READS = NI * (X_COLUMN ? 2 : 1) + NJ * (Y_COLUMN ? 2 : 1), EACH = (READS + NI * NJ - 1) / (NI * NJ);
 #pragma unroll
@@ -565,7 +644,7 @@ __global__ __launch_bounds__(T::THREADS) void eco_head_product_kernel(ProductArg
       for (int i = 0; i < NI; ++i) {
 #pragma unroll
         for (int j = 0; j < NJ; ++j)
-          acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fx[(QUARTERS - 1) & 1][i], fy[(QUARTERS - 1) & 1][j], acc[i][j], 0, 0, 0);
+          acc[i][j] = multiply<is_half(MODE)>(fx[(QUARTERS - 1) & 1][i], fy[(QUARTERS - 1) & 1][j], acc[i][j]);
         if (i == 0) {
           __builtin_amdgcn_sched_barrier(0);
           issue();
@@ -579,9 +658,26 @@ __global__ __launch_bounds__(T::THREADS) void eco_head_product_kernel(ProductArg
     int end_lane = lane;
     asm volatile("" : "+v"(end_lane));
     const auto x_of = [&](int i, int r) { return x0 + wx + 32 * i + (r & 3) + 8 * (r >> 2) + 4 * (end_lane >> 5); };
+    const auto unscale = [&](int i, int j) {                   // of fp16 planes (the exponents of all of a tile's rows are there to be read)
+      const int of_row = a.y_back[y0 + wy + 32 * j + (end_lane & 31)];
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const int4 v = *reinterpret_cast<const int4 *>(a.x_back + x_of(i, 4 * q));
+        acc[i][j][4 * q] = ldexpf(acc[i][j][4 * q], v.x + of_row);
+        acc[i][j][4 * q + 1] = ldexpf(acc[i][j][4 * q + 1], v.y + of_row);
+        acc[i][j][4 * q + 2] = ldexpf(acc[i][j][4 * q + 2], v.z + of_row);
+        acc[i][j][4 * q + 3] = ldexpf(acc[i][j][4 * q + 3], v.w + of_row);
+      }
+      __builtin_amdgcn_sched_barrier(0);                       // (all exponents at once would spill)
+    };
     lds_char *const extra = (lds_char *)smem + T::DEPTH * T::STEP_BYTES;
     lds_char *const own = extra + wave * own_bytes<MODE, T>();
-    if constexpr (MODE == STATS) {
+    if constexpr (is_stats(MODE)) {
+      if constexpr (is_half(MODE))
+#pragma unroll
+        for (int j = 0; j < NJ; ++j)
+#pragma unroll
+          for (int i = 0; i < NI; ++i) unscale(i, j);
       typedef __attribute__((address_space(3))) float lds_float;
       const auto across = [&](float (&v)[NJ], int which, auto join) {      // over a tile's x: the other half's registers, then the other waves
         lds_float *red = (lds_float *)extra + which * T::WX * T::BY;
@@ -644,7 +740,7 @@ __global__ __launch_bounds__(T::THREADS) void eco_head_product_kernel(ProductArg
         store(a.sum_tau, sum);
       }
     }
-    if constexpr (MODE == GRAD || MODE == GRAD_PLANES) {
+    if constexpr (is_grad(MODE)) {
       uint16_t *const out = static_cast<uint16_t *>(a.out);
       const bool edge = x0 + T::BX > a.nx;
       const float per_unit = 1.0f / grad_unit(a.consts);
@@ -657,6 +753,7 @@ __global__ __launch_bounds__(T::THREADS) void eco_head_product_kernel(ProductArg
         rc.b *= per_unit;
 #pragma unroll
         for (int i = 0; i < NI; ++i) {
+          if constexpr (is_half(MODE)) unscale(i, j);
           if (a.two) {
 #pragma unroll
             for (int r = 0; r < 16; ++r)
@@ -996,11 +1093,6 @@ __device__ __forceinline__ float wave_sum(float x) {
   for (int d = 32; d; d >>= 1) x += __shfl_xor(x, d);
   return x;
 }
-__device__ __forceinline__ float wave_max(float x) {
-#pragma unroll
-  for (int d = 32; d; d >>= 1) x = fmaxf(x, __shfl_xor(x, d));
-  return x;
-}
 
 struct Teacher { float max, sum; };               // of a row's present logits over tau: q_j = exp(l_j / tau - max) / sum
 __device__ Teacher teacher_of(const HeadRows &r, uint64_t row, int lane) {
@@ -1105,7 +1197,10 @@ __global__ __launch_bounds__(256) void eco_head_finish_kernel(HeadRows r, HeadWe
   const float l1 = fmaf(log2_fast(s), LN2, only_tau ? base * it : base);
   const float lt = st.sum_tau ? fmaf(log2_fast(s_tau), LN2, base * it) : l1;
   if (lane == 0) {
-    if (ce) ce[row] = label >= 0 ? l1 - z[0] : 0.0f;
+    if (ce) {                                     // (neither loss is below zero, which their rounding may be; a NaN stays)
+      const float loss = l1 - z[0];
+      ce[row] = label < 0 || loss < 0.0f ? 0.0f : loss;
+    }
     if (lse) lse[row] = l1;
     if (lse_tau) lse_tau[row] = lt;
   }
@@ -1122,7 +1217,7 @@ __global__ __launch_bounds__(256) void eco_head_finish_kernel(HeadRows r, HeadWe
     }
   }
   sum = wave_sum(sum);
-  if (lane == 0) kd[row] = r.tau * r.tau * sum;
+  if (lane == 0) kd[row] = sum < 0.0f ? 0.0f : r.tau * r.tau * sum;
 }
 
 // ------------------------------------------------------------------------------------------------ gradients beside the products
@@ -1338,7 +1433,7 @@ hipError_t launch_product(const ProductArgs &a, int shape, uint32_t x, uint32_t 
     case HEAD_SMALL: return launch_tiles<MODE, std::conditional_t<MODE == DH, SmallF32, Small>>(a, x, y, s);
     case HEAD_MEDIUM:
       // (the logits' gradient of 67 x 1152 x 262144: 143 us in wide tiles, 171)
-      if constexpr (MODE == GRAD || MODE == GRAD_PLANES)
+      if constexpr (is_grad(MODE))
         if (ceil_div(x, MediumWide::BX) * ceil_div(y, MediumWide::BY) >= 2 * UNITS) return launch_tiles<MODE, MediumWide>(a, x, y, s);
       return launch_tiles<MODE, Medium>(a, x, y, s);
     default: return launch_tiles<MODE, Large>(a, x, y, s);
@@ -1504,6 +1599,18 @@ hipError_t launch_few(const ProductArgs &a, const HeadWeights &w, uint64_t first
   }
 }
 
+hipError_t launch_head_convert_half(const HeadWeights &w, uint64_t first, uint32_t rows, uint32_t dim, void *planes, uint32_t ld, uint64_t plane, int32_t *back, hipStream_t s) {
+  return by_format(w, dim, [&](auto fmt, auto whole) {
+    hipLaunchKernelGGL((eco_head_convert_half_kernel<fmt.value, whole.value>), dim3(rows < 4 * 8192 ? (rows + 3) / 4 : 8192), dim3(256), 0, s, w, first, rows, dim,
+                       static_cast<uint16_t *>(planes), ld, plane, back);
+  });
+}
+hipError_t launch_head_gather_half(const HeadRows &r, void *compact, uint32_t padded_rows, uint32_t padded_dim, int32_t *back, hipStream_t s) {
+  hipLaunchKernelGGL(eco_head_gather_half_kernel, dim3((padded_rows + 3) / 4), dim3(256), 0, s, r, static_cast<uint16_t *>(compact), padded_rows, padded_dim,
+                     static_cast<uint32_t>(head_hidden_half_planes(r.hidden_bf16)), back);
+  return hipGetLastError();
+}
+
 hipError_t launch_head_stats(int shape, const HeadOperand &w, const HeadWeights *few, uint64_t first, const HeadOperand &h, uint32_t n, uint32_t rows, uint32_t dim,
                              const int32_t *count, float inv_tau, const HeadStats &st, uint32_t tile, hipStream_t s) {
   ProductArgs a = product(w, h);
@@ -1512,7 +1619,10 @@ hipError_t launch_head_stats(int shape, const HeadOperand &w, const HeadWeights 
   a.scale2 = a.two ? LOG2E : LOG2E * inv_tau;
   a.scale2_tau = LOG2E * inv_tau;
   a.out_f32 = st.max; a.sum = st.sum; a.sum_tau = st.sum_tau; a.tiles = st.tiles; a.tile0 = tile;
-  return few ? launch_few<STATS>(a, *few, first, rows, dim, s) : launch_product<STATS>(a, shape, n, rows, s);
+  if (few) return launch_few<STATS>(a, *few, first, rows, dim, s);
+  if (!w.back) return launch_product<STATS>(a, shape, n, rows, s);
+  a.order = 1; a.x_back = w.back; a.y_back = h.back;
+  return launch_product<STATS_HALF>(a, shape, n, rows, s);
 }
 
 hipError_t launch_head_finish(const HeadRows &r, const HeadWeights &w, const HeadStats &st, int dotted, float *ce, float *kd, float *lse, float *lse_tau, float *picked,
@@ -1551,6 +1661,10 @@ hipError_t launch_head_grad(int shape, const HeadOperand &w, const HeadWeights *
   a.scale2 = softmaxes == HEAD_TEACHER ? LOG2E * inv_tau : LOG2E; a.scale2_tau = LOG2E * inv_tau;
   a.consts = consts; a.out = g; a.out_ld = g_ld; a.out_plane = g_plane; a.out_planes = g_planes;
   if (few) return launch_few<GRAD>(a, *few, first, rows, dim, s);
+  if (w.back) {
+    a.order = 1; a.x_back = w.back; a.y_back = h.back;
+    return launch_product<GRAD_HALF>(a, shape, n, rows, s);
+  }
   return g_planes == 1 ? launch_product<GRAD>(a, shape, n, rows, s) : launch_product<GRAD_PLANES>(a, shape, n, rows, s);
 }
 
