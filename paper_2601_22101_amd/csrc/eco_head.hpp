@@ -94,6 +94,11 @@ constexpr uint32_t HEAD_FEW_ROWS = 64;
 hipError_t launch_head_few_rows(const HeadRows &, const HeadWeights &, void *compact, uint32_t padded_rows, uint32_t padded_dim, float *picked, hipStream_t);
 hipError_t launch_head_few_rows_backward(const HeadRows &, uint32_t stack, void *compact, uint32_t padded_rows, uint32_t padded_dim, const float *grad_ce, const float *grad_kd, const float *lse,
                                          const float *lse_tau, const float *picked, int softmaxes, int32_t *ids, float *values, HeadRowConst *consts, hipStream_t);
+// Parts of the vocabulary that the kernel of few rows' grad_hidden goes by, which reads weights that are no bf16 as they are stored; 0: it does not take the
+// call.  Its partial sums take the place of launch_head_grad_hidden's, without a stack.
+uint32_t head_few_hidden(const HeadWeights &, uint64_t rows, uint64_t dim, uint64_t vocab);
+hipError_t launch_head_few_hidden(const HeadWeights &, uint64_t first, const void *g, uint32_t g_ld, uint64_t g_plane, uint32_t g_planes, uint32_t n, uint32_t rows, uint32_t dim,
+                                  const int32_t *count, uint32_t splits, float *partial, uint32_t partial_ld, uint64_t partial_stride, int add, hipStream_t);
 // g[row][v] of a piece: planes of [padded rows][ld]
 hipError_t launch_head_grad(int shape, const HeadOperand &w, const HeadWeights *few, uint64_t first, const HeadOperand &h, uint32_t n, uint32_t rows, uint32_t dim, const int32_t *count, float inv_tau, int softmaxes,
                             uint32_t order, const HeadRowConst *, void *g, uint32_t g_ld, uint64_t g_plane, uint32_t g_planes, hipStream_t);

@@ -95,7 +95,7 @@ eco::HeadWeights weights_of(const eco_head_t *h) {
 
 // The arrays of a workspace and the pieces of the vocabulary that a call goes by.
 struct Layout {
-  uint32_t padded_rows, padded_dim, entries, piece, hidden_planes, weight_planes, grad_planes, tiles, splits, few, pair_order, stack;
+  uint32_t padded_rows, padded_dim, entries, piece, hidden_planes, weight_planes, grad_planes, tiles, splits, few, few_hidden, pair_order, stack;
   int shape;
   bool in_place, two, half;
   uint64_t half_planes, half_compact, half_back, half_rows_back;
@@ -140,10 +140,11 @@ Layout layout_of(const eco_head_t *h, bool backward) {
   // the more exact ones.  The gradients need the bf16 planes too, and making and reading others takes as long as one of the logits' products of 750 rows
   // (training, us in the kernels, with and without: fp32 30 x 1024 x 50304 582 505, which saves three products; bf16 and fp32 700 x 1024 x 50304 1516
   // 1502, one; fp32 and FP8 of the same sizes 1675 1753, two).
+  l.few_hidden = backward ? eco::head_few_hidden(weights_of(h), h->rows, h->dim, h->vocab) : 0;
   const uint32_t half_pairs = eco::head_pairs(2, eco::head_hidden_half_planes(h->hidden_dtype == ECO_DT_BF16), 1);
   const uint32_t saved = eco::head_pairs(l.weight_planes, l.hidden_planes, backward ? l.pair_order : 2) - half_pairs;
-  l.half = !l.few && h->fmt != ECO_FMT_BF16_PLAIN && (!backward || saved * h->rows >= 1024);
-  const bool converts = !l.in_place && (backward || (!l.few && !l.half));
+  l.half = !l.few && h->fmt != ECO_FMT_BF16_PLAIN && (!backward || l.few_hidden || saved * h->rows >= 1024);
+  const bool converts = !l.in_place && (backward ? !l.few_hidden : !l.few && !l.half);
   if (converts || l.half) limit(2ull * l.padded_dim * l.weight_planes);
   if (backward) limit(2ull * l.padded_rows * l.grad_planes);
   if (backward) piece = eco::head_piece(l.shape, h->rows, h->dim, h->vocab, piece);
@@ -172,7 +173,8 @@ Layout layout_of(const eco_head_t *h, bool backward) {
     l.values = take(4ull * h->rows * l.entries);
     l.consts = take(sizeof(eco::HeadRowConst) * l.padded_rows);
     l.g = take(2ull * l.grad_planes * l.padded_rows * piece);
-    l.splits = eco::head_splits(l.shape, h->rows, h->dim, piece < h->vocab ? piece : h->vocab, eco::head_pairs(l.weight_planes, l.stack ? 1 : l.grad_planes, l.pair_order));
+    l.splits = l.few_hidden ? eco::head_few_hidden(weights_of(h), h->rows, h->dim, piece < h->vocab ? piece : h->vocab)
+                            : eco::head_splits(l.shape, h->rows, h->dim, piece < h->vocab ? piece : h->vocab, eco::head_pairs(l.weight_planes, l.stack ? 1 : l.grad_planes, l.pair_order));
     l.partial = take(4ull * l.splits * l.padded_rows * l.padded_dim);
   }
   l.bytes = at;
@@ -318,17 +320,21 @@ eco_status_t eco_head_loss_backward(const eco_head_t *head, void *workspace, siz
   const bool past_caches = head->vocab * head->dim * size_of(head->grad_weights_dtype) > (256u << 20);
   for (uint64_t first = 0; first < head->vocab; first += l.piece) {
     const uint32_t n = static_cast<uint32_t>(head->vocab - first < l.piece ? head->vocab - first : l.piece);
-    eco::HeadOperand w;
-    HEAD_LAUNCH(weight_operand(head, l, ws, first, n, s, &w));
+    eco::HeadOperand w = {};
+    if (!l.few_hidden) HEAD_LAUNCH(weight_operand(head, l, ws, first, n, s, &w));
     if (l.half) HEAD_LAUNCH(half_weight_operand(head, l, ws, first, n, s, &half_w));
     HEAD_LAUNCH(eco::launch_head_grad(l.shape, l.half ? half_w : w, l.few ? &weights : nullptr, first, l.half ? half_hidden : hidden, n, r.rows, r.dim, r.count, 1.0f / r.tau, softmaxes,
                                       l.pair_order, consts, ws + l.g, l.piece, g_plane, l.grad_planes, s));
     HEAD_LAUNCH(eco::launch_head_scatter(ids, values, consts, r.rows, l.entries, r.count, first, n, ws + l.g, l.piece, g_plane, l.grad_planes, s));
-    HEAD_LAUNCH(eco::launch_head_grad_hidden(l.shape, l.stack, w, g, n, r.rows, r.dim, r.count, l.pair_order, l.splits, partial, l.padded_dim, partial_stride, first != 0, s));
+    if (l.few_hidden)
+      HEAD_LAUNCH(eco::launch_head_few_hidden(weights, first, ws + l.g, l.piece, g_plane, l.grad_planes, n, r.rows, r.dim, r.count, l.splits, partial, l.padded_dim, partial_stride,
+                                              first != 0, s));
+    else
+      HEAD_LAUNCH(eco::launch_head_grad_hidden(l.shape, l.stack, w, g, n, r.rows, r.dim, r.count, l.pair_order, l.splits, partial, l.padded_dim, partial_stride, first != 0, s));
     char *out = static_cast<char *>(head->grad_weights) + first * out_stride * size_of(head->grad_weights_dtype);
     HEAD_LAUNCH(eco::launch_head_grad_weights(l.shape, l.stack, hidden, g, n, r.dim, r.count, l.pair_order, consts, out, out_stride, head->grad_weights_dtype == ECO_DT_BF16, past_caches, s));
   }
-  HEAD_LAUNCH(eco::launch_head_grad_hidden_finish(consts, partial, l.splits, l.padded_dim, partial_stride, l.stack, r, head->grad_hidden,
+  HEAD_LAUNCH(eco::launch_head_grad_hidden_finish(consts, partial, l.splits, l.padded_dim, partial_stride, l.few_hidden ? 0 : l.stack, r, head->grad_hidden,
                                                   stride_or(head->grad_hidden_stride, head->dim), s));
   return ECO_OK;
 }

@@ -166,8 +166,11 @@ __global__ __launch_bounds__(256) void eco_head_gather_kernel(HeadRows r, uint16
 
 // ------------------------------------------------------------------------------------------------ weights
 
+__device__ __forceinline__ uint64_t scale_place(const HeadWeights &w, uint64_t i) {
+  return w.group_shift >= 0 ? i >> w.group_shift : i >> 32 ? i / w.group : static_cast<uint32_t>(i) / static_cast<uint32_t>(w.group);
+}
 __device__ __forceinline__ float scale_at(const HeadWeights &w, uint64_t i) {
-  const uint64_t g = w.group_shift >= 0 ? i >> w.group_shift : i >> 32 ? i / w.group : static_cast<uint32_t>(i) / static_cast<uint32_t>(w.group);
+  const uint64_t g = scale_place(w, i);
   return w.scale_bf16 ? u2f(static_cast<uint32_t>(static_cast<const uint16_t *>(w.scales)[g]) << 16) : static_cast<const float *>(w.scales)[g];
 }
 template <int FMT>
@@ -1086,6 +1089,120 @@ __global__ __launch_bounds__(FEW_WAVES * 64) void eco_head_few_kernel(ProductArg
   }
 }
 
+// grad_hidden of up to 64 rows, g W of weights that are no bf16: bound by the reading of the weights as well, so they are read where they lie, once, and
+// become planes in the registers of the wave that multiplies them.  A wave takes 128 columns, four next to each other to a lane, of 16 rows of weights at a
+// time, and is two such steps ahead with its loads; lane n, h holds columns 4 n .. 4 n + 3 of rows 8 h .. 8 h + 7, which is a quarter of each of four operands of
+// every fourth column.  The rows of g come from the caches: by LDS, with a barrier every 64 of the vocabulary, the waves wait for each other (60 x 1024 x 50304,
+// fp32, 100 us, 73 without).  Measured beside planes in memory and the tiles above, us: 2 x 2048 x 102400 of fp32 162 (5.2 TB/s) and 717, 30 x 1152 x 262144 of
+// FP8 176 and 585, of INT4 190 and 633, 6 x 576 x 32128 of FP8 21 and 33.
+template <int FMT, int GP, int BLOCKS>
+__global__ __launch_bounds__(256) void eco_head_few_hidden_kernel(ProductArgs a, HeadWeights w, uint64_t first, uint32_t rows_each) {
+  constexpr int PLANES = FMT == FMT_FP32_ID ? GP : 2;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = lane & 31, half = lane >> 5;
+  const uint32_t base = (blockIdx.x * 4 + wave) * 128, begin = blockIdx.y * rows_each, end = min(begin + rows_each, a.k);
+  const uint32_t count = static_cast<uint32_t>(*a.count);
+  if (base >= a.nx || begin >= end || count == 0) return;
+  const uint32_t col = base + 4 * n < a.nx ? base + 4 * n : 0, last = (a.k - 1) / 16 * 16;
+  // (scale groups that divide a row: no division for each)
+  const uint32_t per_row = FMT != FMT_FP32_ID && w.group <= a.nx && a.nx % static_cast<uint32_t>(w.group) == 0 ? a.nx / static_cast<uint32_t>(w.group) : 0,
+                 in_row = per_row ? col / static_cast<uint32_t>(w.group) : 0;
+  uint32_t raw[2][8][FMT == FMT_FP32_ID ? 4 : 1], scale[2][8];
+  const uint32_t scale_shift = w.scale_bf16 ? 16 : 0;
+  bf16x8 g[2][GP][BLOCKS];
+  // (rows past the last repeat it and are left out below; a step past the last repeats that)
+  const auto load = [&](int p, uint32_t v) {
+    v = min(v, last);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const uint64_t row = first + min(v + 8 * half + i, a.k - 1), at = row * a.nx + col;
+      if constexpr (FMT == FMT_FP32_ID) {
+        const uint4 q = *reinterpret_cast<const uint4 *>(static_cast<const float *>(w.data) + row * w.stride + col);
+        raw[p][i][0] = q.x; raw[p][i][1] = q.y; raw[p][i][2] = q.z; raw[p][i][3] = q.w;
+      } else {
+        raw[p][i][0] = FMT == FMT_FP8 ? *reinterpret_cast<const uint32_t *>(static_cast<const uint8_t *>(w.data) + at)
+                                      : *reinterpret_cast<const uint16_t *>(static_cast<const uint8_t *>(w.data) + at / 2);
+      }
+    }
+    if constexpr (FMT != FMT_FP32_ID) {
+      uint64_t at[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const uint64_t row = first + min(v + 8 * half + i, a.k - 1);
+        at[i] = per_row ? row * per_row + in_row : scale_place(w, row * a.nx + col);
+      }
+      // (no use of what is loaded, a shift included, before the step's own: each would be waited for)
+      if (w.scale_bf16)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) scale[p][i] = static_cast<const uint16_t *>(w.scales)[at[i]];
+      else
+#pragma unroll
+        for (int i = 0; i < 8; ++i) scale[p][i] = static_cast<const uint32_t *>(w.scales)[at[i]];
+    }
+#pragma unroll
+    for (int q = 0; q < GP; ++q)
+#pragma unroll
+      for (int b = 0; b < BLOCKS; ++b)
+        g[p][q][b] = *reinterpret_cast<const bf16x8 *>(a.y + q * a.y_plane + static_cast<uint64_t>(32 * b + n) * a.ldy + v + 8 * half);
+  };
+  f32x16 acc[BLOCKS][4] = {};
+  const auto multiply_step = [&](int p, uint32_t v0) {
+#pragma unroll
+    for (int c = 0; c < 4; ++c) {
+      float v[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        if constexpr (FMT == FMT_FP32_ID) v[i] = u2f(raw[p][i][c]);
+        else if constexpr (FMT == FMT_FP8) v[i] = (c == 0 ? e4m3_decode<0>(raw[p][i][0]) : c == 1 ? e4m3_decode<1>(raw[p][i][0]) : c == 2 ? e4m3_decode<2>(raw[p][i][0]) : e4m3_decode<3>(raw[p][i][0])) * u2f(scale[p][i] << scale_shift);
+        else v[i] = static_cast<float>(static_cast<int32_t>(raw[p][i][0] << (28 - 4 * c)) >> 28) * u2f(scale[p][i] << scale_shift);
+      }
+      if (v0 + 16 > a.k)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = v0 + 8 * half + i < a.k ? v[i] : 0.0f;
+      bf16x8 x[PLANES];
+#pragma unroll
+      for (int q = 0; q < PLANES; ++q) {
+        uint32_t two[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          two[i] = f32x2_to_bf16x2_rne(v[2 * i], v[2 * i + 1]);
+          v[2 * i] -= bf16_lo(two[i]);
+          v[2 * i + 1] -= bf16_hi(two[i]);
+        }
+        x[q] = __builtin_bit_cast(bf16x8, make_uint4(two[0], two[1], two[2], two[3]));
+      }
+#pragma unroll
+      for (int q = 0; q < PLANES; ++q)
+#pragma unroll
+        for (int o = 0; o + q < GP; ++o)
+#pragma unroll
+          for (int b = 0; b < BLOCKS; ++b) acc[b][c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x[q], g[p][o][b], acc[b][c], 0, 0, 0);
+    }
+  };
+  load(0, begin);
+  load(1, begin + 16);
+  for (uint32_t v = begin; v < end; v += 32) {
+    multiply_step(0, v);
+    load(0, v + 32);
+    if (v + 16 < end) multiply_step(1, v + 16);
+    load(1, v + 48);
+  }
+  // acc[b][c][r]: row 32 b + n, column base + 4 ((r & 3) + 8 (r >> 2) + 4 half) + c
+#pragma unroll
+  for (int b = 0; b < BLOCKS; ++b)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      const uint32_t y = 32 * b + n, x = base + 4 * ((r & 3) + 8 * (r >> 2) + 4 * half);
+      if (y >= count || x >= a.nx) continue;
+      float4 *to = reinterpret_cast<float4 *>(a.out_f32 + blockIdx.y * a.out_plane + y * a.out_ld + x);
+      float4 sum = make_float4(acc[b][0][r], acc[b][1][r], acc[b][2][r], acc[b][3][r]);
+      if (a.add) {
+        const float4 old = *to;
+        sum.x += old.x; sum.y += old.y; sum.z += old.z; sum.w += old.w;
+      }
+      *to = sum;
+    }
+}
+
 // ------------------------------------------------------------------------------------------------ losses
 
 __device__ __forceinline__ float wave_sum(float x) {
@@ -1673,6 +1790,39 @@ hipError_t launch_head_scatter(const int32_t *ids, const float *values, const He
   hipLaunchKernelGGL(eco_head_scatter_kernel, dim3(blocks_for(static_cast<uint64_t>(rows) * entries)), dim3(256), 0, s, ids, values, consts, entries, count, first, n,
                      static_cast<uint16_t *>(g), g_ld, g_plane, g_planes);
   return hipGetLastError();
+}
+
+uint32_t head_few_hidden(const HeadWeights &w, uint64_t rows, uint64_t dim, uint64_t vocab) {
+  const bool quantized = w.fmt == FMT_FP8 || w.fmt == FMT_INT4;
+  if (rows > HEAD_FEW_ROWS || w.fmt == FMT_BF16_PLAIN || dim % 4 || (quantized ? w.group : w.stride) % 4) return 0;
+  // two workgroups a compute unit, of some 64 rows of weights at the least
+  const uint64_t parts = ceil_div(2 * UNITS, ceil_div(dim, 512)), most = ceil_div(vocab, 64);
+  const uint64_t rows_each = ceil_div(ceil_div(vocab, parts < most ? parts : most), 16) * 16;
+  return static_cast<uint32_t>(ceil_div(vocab, rows_each));
+}
+template <int FMT>
+hipError_t launch_few_hidden(const ProductArgs &a, const HeadWeights &w, uint64_t first, uint32_t g_planes, uint32_t rows, hipStream_t s) {
+  const uint32_t rows_each = static_cast<uint32_t>(ceil_div(ceil_div(a.k, a.splits), 16) * 16);
+  const auto go = [&](auto planes, auto blocks) {
+    hipLaunchKernelGGL((eco_head_few_hidden_kernel<FMT, planes.value, blocks.value>), dim3(static_cast<uint32_t>(ceil_div(a.nx, 512)), a.splits), dim3(256), 0, s, a, w, first, rows_each);
+    return hipGetLastError();
+  };
+  using two = std::integral_constant<int, 2>;
+  using three = std::integral_constant<int, 3>;
+  using one = std::integral_constant<int, 1>;
+  if (rows <= 32) return g_planes == 2 ? go(two{}, one{}) : go(three{}, one{});
+  return g_planes == 2 ? go(two{}, two{}) : go(three{}, two{});
+}
+hipError_t launch_head_few_hidden(const HeadWeights &w, uint64_t first, const void *g, uint32_t g_ld, uint64_t g_plane, uint32_t g_planes, uint32_t n, uint32_t rows, uint32_t dim,
+                                  const int32_t *count, uint32_t splits, float *partial, uint32_t partial_ld, uint64_t partial_stride, int add, hipStream_t s) {
+  ProductArgs a = {};
+  a.y = static_cast<const uint16_t *>(g); a.y_plane = g_plane; a.ldy = g_ld; a.nx = dim; a.k = n; a.count = count; a.splits = splits;
+  a.out_f32 = partial; a.out_ld = partial_ld; a.out_plane = partial_stride; a.add = add;
+  switch (w.fmt) {
+    case FMT_FP8: return launch_few_hidden<FMT_FP8>(a, w, first, g_planes, rows, s);
+    case FMT_INT4: return launch_few_hidden<FMT_INT4>(a, w, first, g_planes, rows, s);
+    default: return launch_few_hidden<FMT_FP32_ID>(a, w, first, g_planes, rows, s);
+  }
 }
 
 hipError_t launch_head_grad_hidden(int shape, uint32_t stack, const HeadOperand &w, const HeadOperand &g, uint32_t n, uint32_t rows, uint32_t dim, const int32_t *count, uint32_t order,
