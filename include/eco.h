@@ -305,10 +305,16 @@ eco_status_t eco_arith_selftest(int32_t kind, float numerator, uint32_t bits_lo,
  * hidden states hold (infinities and NaN too).  In rows that take part a hidden state, weight or present teacher's logit that is not
  * finite (but for that -inf) makes results that depend on it NaN or infinite.
  *
- * Precision.  Products are sums in fp32 of exact products of bf16 values: fp32 operands enter as three bf16 terms each, quantized
- * weights as two (a relative 2^-17 of the weight).  Statistics, losses and grad_hidden's sums over the vocabulary are fp32.  g is rounded to bf16 where
- * both gradients are bf16, else it enters as three terms.  Every output is rounded once.  No atomics: the same call on
- * the same arrays gives the same bits.
+ * Precision.  Products are sums in fp32 of exact products of 16-bit terms.  bf16 operands are one term; fp32 ones three bf16 terms and quantized weights
+ * two (a relative 2^-17 of the weight), or, for logits, either of them two fp16 terms of a row scaled by a power of two (2^-22 of a value, and 2^-39 of the
+ * row's largest).  Products of two terms whose places sum to more than 2 are left out (2^-22), to more than 1 where both gradients are bf16 and it is they that
+ * are computed (2^-15).  Statistics, losses and grad_hidden's sums over the vocabulary are fp32.  g is kept relative to the first row's upstream gradient; where
+ * both gradients are bf16 it is rounded to one bf16, or of up to 64 rows to two bf16 terms, else it enters as three.  Every output is rounded once.  No
+ * atomics: the same call on the same arrays gives the same bits.
+ *
+ * Time (MI355X, bf16 but where noted; rows x dim x vocab): losses 1 x 512 x 32000 16 us, 2048 x 1024 x 50304 0.21 ms, 24 x 2048 x 102400 in INT4 0.10 ms;
+ * losses and gradients 2048 x 1024 x 50304 in FP8 1.6 ms, 4096 x 2048 x 102400 with a quarter of the rows ignored 4.8 ms, 8192 x 1152 x 262144 18.6 ms.  Matrix
+ * cores bound many rows, the reading of the weights few.  fp32 weights with fp32 hidden states are slow for few rows: they are first written as planes.
  */
 typedef struct eco_head {
   const void *hidden;         /* rows x dim values of hidden_dtype, aligned to their size                                          */
