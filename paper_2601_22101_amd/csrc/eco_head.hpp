@@ -107,7 +107,8 @@ hipError_t launch_head_scatter(const int32_t *ids, const float *values, const He
 // partial[s][compact row][dim] (+)= g w over a piece, s the split of the piece's vocabulary
 hipError_t launch_head_grad_hidden(int shape, uint32_t stack, const HeadOperand &w, const HeadOperand &g, uint32_t n, uint32_t rows, uint32_t dim, const int32_t *count, uint32_t order,
                                    uint32_t splits, float *partial, uint32_t partial_ld, uint64_t partial_stride, int add, hipStream_t);
-hipError_t launch_head_grad_hidden_finish(const HeadRowConst *, const float *partial, uint32_t splits, uint32_t partial_ld, uint64_t partial_stride, uint32_t stack, const HeadRows &, void *out,
+// ids, values: of launch_head_entries where g is one bf16, else null
+hipError_t launch_head_grad_hidden_finish(const HeadRowConst *, const float *partial, uint32_t splits, uint32_t partial_ld, uint64_t partial_stride, uint32_t stack, const HeadRows &, const HeadWeights &, const int32_t *ids, const float *values, void *out,
                                           uint64_t out_stride, hipStream_t);
 hipError_t launch_head_grad_weights(int shape, uint32_t stack, const HeadOperand &h, const HeadOperand &g, uint32_t n, uint32_t dim, const int32_t *count, uint32_t order,
                                     const HeadRowConst *, void *out, uint64_t out_stride, int out_bf16, int past_caches, hipStream_t);

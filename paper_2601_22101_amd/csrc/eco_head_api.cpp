@@ -334,7 +334,7 @@ eco_status_t eco_head_loss_backward(const eco_head_t *head, void *workspace, siz
     char *out = static_cast<char *>(head->grad_weights) + first * out_stride * size_of(head->grad_weights_dtype);
     HEAD_LAUNCH(eco::launch_head_grad_weights(l.shape, l.stack, hidden, g, n, r.dim, r.count, l.pair_order, consts, out, out_stride, head->grad_weights_dtype == ECO_DT_BF16, past_caches, s));
   }
-  HEAD_LAUNCH(eco::launch_head_grad_hidden_finish(consts, partial, l.splits, l.padded_dim, partial_stride, l.few_hidden ? 0 : l.stack, r, head->grad_hidden,
+  HEAD_LAUNCH(eco::launch_head_grad_hidden_finish(consts, partial, l.splits, l.padded_dim, partial_stride, l.few_hidden ? 0 : l.stack, r, weights, l.grad_planes == 1 ? ids : nullptr, values, head->grad_hidden,
                                                   stride_or(head->grad_hidden_stride, head->dim), s));
   return ECO_OK;
 }

@@ -183,6 +183,15 @@ __device__ __forceinline__ float weight_at(const HeadWeights &w, uint64_t row, u
   return static_cast<float>((i & 1) ? byte >> 4 : static_cast<int32_t>(static_cast<uint32_t>(byte) << 28) >> 28) * scale_at(w, i);
 }
 
+__device__ __forceinline__ float weight_of(const HeadWeights &w, uint64_t row, uint32_t dim, uint32_t k) {
+  switch (w.fmt) {
+    case FMT_FP8: return weight_at<FMT_FP8>(w, row, dim, k);
+    case FMT_INT4: return weight_at<FMT_INT4>(w, row, dim, k);
+    case FMT_BF16_PLAIN: return weight_at<FMT_BF16_PLAIN>(w, row, dim, k);
+    default: return weight_at<FMT_FP32_ID>(w, row, dim, k);
+  }
+}
+
 // Eight weights of a row from element k (a multiple of 8) on, those past dim 0.  WHOLE: rows are whole pieces of eight, which then lie in one
 // scale group and are one aligned load; else a piece may lie at any address and in two groups.
 template <int FMT, bool WHOLE>
@@ -1472,10 +1481,12 @@ __global__ __launch_bounds__(256) void eco_head_scatter_kernel(const int32_t *id
 }
 
 // The gradient of the hidden states: each row's parts summed, four columns to a thread; zeros where a row takes no part.  WAYS threads take every WAYSth part
-// each where there are many, and their sums are added in order.
+// each where there are many, and their sums are added in order.  `ids`, where g is rounded to one bf16 (else null): what that rounding left of g at the label, most
+// rows' largest value by far, is added here, of one row of weights a row (4096 x 2048 x 102400 with both losses: grad_hidden's error 0.0023 of its norm, 0.0026
+// without, where its own last rounding makes 0.0017).
 template <int WAYS>
 __global__ __launch_bounds__(256) void eco_head_grad_hidden_finish_kernel(const HeadRowConst *consts, const float *partial, uint32_t splits, uint32_t ld, uint64_t stride, uint32_t stack,
-                                                                          HeadRows r, void *out, uint64_t out_stride) {
+                                                                          HeadRows r, HeadWeights w, const int32_t *ids, const float *values, void *out, uint64_t out_stride) {
   constexpr uint32_t EACH = 256 / WAYS;
   __shared__ float4 sums[WAYS > 1 ? 256 : 1];
   const uint32_t chunks = (r.dim + 3) / 4, way = threadIdx.x / EACH;
@@ -1508,6 +1519,18 @@ __global__ __launch_bounds__(256) void eco_head_grad_hidden_finish_kernel(const 
       __syncthreads();
     }
     if (way != 0 || begin + threadIdx.x >= work) continue;
+    if (ids && c >= 0) {
+      const uint64_t at = static_cast<uint64_t>(c) * (r.top_k + 1);
+      const int32_t id = ids[at];
+      if (id >= 0) {
+        float rest = values[at] * (1.0f / unit), v[4];
+        uint32_t bits;
+        next_plane(rest, bits);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) v[j] = k + j < r.dim ? rest * weight_of(w, id, r.dim, k + j) : 0.0f;
+        sum.x += v[0]; sum.y += v[1]; sum.z += v[2]; sum.w += v[3];
+      }
+    }
     sum.x *= unit; sum.y *= unit; sum.z *= unit; sum.w *= unit;
     const uint64_t at = row * out_stride + k;
     const float v[4] = {sum.x, sum.y, sum.z, sum.w};
@@ -1840,14 +1863,14 @@ hipError_t launch_head_grad_hidden(int shape, uint32_t stack, const HeadOperand 
   return dim_tile(shape, dim) == Large192::BX ? launch_tiles<DH, Large192>(a, dim, rows, s) : launch_product<DH>(a, shape, dim, rows + stack, s);
 }
 
-hipError_t launch_head_grad_hidden_finish(const HeadRowConst *consts, const float *partial, uint32_t splits, uint32_t partial_ld, uint64_t partial_stride, uint32_t stack, const HeadRows &r, void *out,
+hipError_t launch_head_grad_hidden_finish(const HeadRowConst *consts, const float *partial, uint32_t splits, uint32_t partial_ld, uint64_t partial_stride, uint32_t stack, const HeadRows &r, const HeadWeights &w, const int32_t *ids, const float *values, void *out,
                                           uint64_t out_stride, hipStream_t s) {
   const uint64_t work = static_cast<uint64_t>(r.rows) * ((r.dim + 3) / 4);
   if (splits >= 16)
-    hipLaunchKernelGGL(eco_head_grad_hidden_finish_kernel<8>, dim3(blocks_for(8 * work)), dim3(256), 0, s, consts, partial, splits, partial_ld, partial_stride, stack, r, out, out_stride);
+    hipLaunchKernelGGL(eco_head_grad_hidden_finish_kernel<8>, dim3(blocks_for(8 * work)), dim3(256), 0, s, consts, partial, splits, partial_ld, partial_stride, stack, r, w, ids, values, out, out_stride);
   else
     hipLaunchKernelGGL(eco_head_grad_hidden_finish_kernel<1>, dim3(blocks_for(work)), dim3(256), 0, s, consts, partial, splits, partial_ld,
-                     partial_stride, stack, r, out, out_stride);
+                     partial_stride, stack, r, w, ids, values, out, out_stride);
   return hipGetLastError();
 }
 
