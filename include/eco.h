@@ -300,10 +300,11 @@ eco_status_t eco_arith_selftest(int32_t kind, float numerator, uint32_t bits_lo,
  * pass computes them again by pieces of the vocabulary.
  *
  * Masks.  A label outside [0, vocab) (-100, say) is none.  An entry of the teacher whose id lies outside [0, vocab) is absent,
- * one whose logit is -inf has no weight (0 ln 0 = 0), and an id may come up more than once.  A row without a label has ce = 0, one without an entry that has weight
- * kd = 0, and a row with neither takes no part: its grad_hidden is 0 and nothing of it reaches grad_weights, whatever its
- * hidden states hold (infinities and NaN too).  In rows that take part a hidden state, weight or present teacher's logit that is not
- * finite (but for that -inf) makes results that depend on it NaN or infinite.
+ * one whose logit is -inf has no weight (0 ln 0 = 0), and an id may come up more than once: each entry counts by itself, so that kd of such a row may be below
+ * zero.  (So may another row's by its rounding; ce is never.)  A row without a label has ce = 0, one without an entry that has weight
+ * kd = 0, and a row with neither takes no part: its grad_hidden is 0 and nothing of it reaches grad_weights, whatever its hidden states hold
+ * (infinities and NaN too).  In rows that take part a hidden state, weight or present teacher's logit that is not finite (but for that -inf) makes
+ * results that depend on it NaN or infinite.
  *
  * Precision.  Products are sums in fp32 of exact products of 16-bit terms.  bf16 operands are one term; fp32 ones three bf16 terms and quantized weights
  * two (a relative 2^-17 of the weight), or, for logits, either of them two fp16 terms of a row scaled by a power of two (2^-22 of a value, and 2^-39 of the

@@ -1326,7 +1326,7 @@ __global__ __launch_bounds__(256) void eco_head_finish_kernel(HeadRows r, HeadWe
   const float l1 = fmaf(log2_fast(s), LN2, only_tau ? base * it : base);
   const float lt = st.sum_tau ? fmaf(log2_fast(s_tau), LN2, base * it) : l1;
   if (lane == 0) {
-    if (ce) {                                     // (neither loss is below zero, which their rounding may be; a NaN stays)
+    if (ce) {                                     // (not below zero, which its rounding may be; a NaN stays)
       const float loss = l1 - z[0];
       ce[row] = label < 0 || loss < 0.0f ? 0.0f : loss;
     }
@@ -1346,7 +1346,7 @@ __global__ __launch_bounds__(256) void eco_head_finish_kernel(HeadRows r, HeadWe
     }
   }
   sum = wave_sum(sum);
-  if (lane == 0) kd[row] = sum < 0.0f ? 0.0f : r.tau * r.tau * sum;
+  if (lane == 0) kd[row] = r.tau * r.tau * sum;    // (below zero where an id that comes up again has more of p than any one of its entries has of q)
 }
 
 // ------------------------------------------------------------------------------------------------ gradients beside the products

@@ -1,0 +1,33 @@
+"""The losses at the output projection where a value is easily lost: losses below zero, teachers whose logits lie at the ends of their type.
+Bounds as in head_util."""
+import pytest
+import torch
+
+from head_util import exact, hold, inputs
+from test_gpu_head import check
+
+pytestmark = pytest.mark.gpu
+
+
+def confident(rows, dim, vocab, height, std=0.05, **kw):
+    """Inputs whose hidden states give the label a logit of about `height`, the others' about 0."""
+    s = inputs(rows, dim, vocab, std=std, **kw)
+    s["hidden"] = (s["w"][s["labels"]] * (height / (dim * std * std))).to(s["hidden"].dtype)
+    return s
+
+
+@pytest.mark.parametrize("rows", [5, 64, 200])
+@pytest.mark.parametrize("tau", [1.0, 2.0])
+@pytest.mark.parametrize("weights", ["bf16", "fp8"])
+def test_a_distillation_loss_below_zero(rows, tau, weights):
+    """An id that comes up k times with equal logits has 1/k of q in each entry: where the student gives it all its weight, kd is -tau^2 ln k."""
+    for k in (2, 7):
+        s = confident(rows, 64, 500, 40.0 * tau, weights=weights, top_k=k, tau=tau, seed=rows + k)
+        s["top_ids"] = s["labels"][:, None].repeat(1, k).int()
+        s["top_logits"] = torch.full((rows, k), 1.5, device="cuda")
+        assert (exact(s)["kd"] < -0.5).all()
+        check(s)
+        # beside an ordinary entry, and in a loss of its own
+        s["top_ids"][:, k - 1] = (s["labels"] + 1).int() % 500
+        check(s)
+        check(dict(s, labels=None, grad_ce=None))
