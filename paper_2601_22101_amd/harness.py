@@ -483,7 +483,7 @@ class HeadLoss:
         self.picked = f32(rows, 1 + top_k)
         self.grad_hidden = torch.empty(rows, dim, dtype=hidden_dtype, device=dev) if training else None
         self.grad_weights = torch.empty(vocab, dim, dtype=grad_weights_dtype, device=dev) if training else None
-        # the descriptor refuses null inputs: the addresses of a call take the place of these
+        # the workspace's size is asked for with inputs in place, which the descriptor needs; a call brings its own
         some = self.picked
         self.head = eco.make_head(rows=rows, vocab=vocab, dim=dim, hidden=some, weights=weights, scales=scales, labels=some if labels else None,
                                   top_ids=some if top_k else None, top_logits=some if top_k else None, ce=self.ce, kd=self.kd, lse=self.lse,
@@ -493,6 +493,8 @@ class HeadLoss:
                                   grad_weights_dtype=_DTYPE[grad_weights_dtype])
         self.workspace_bytes = max(eco.eco_head_loss_workspace(self.head, b) for b in ([False, True] if training else [False]))
         self.workspace = torch.empty(self.workspace_bytes, dtype=torch.uint8, device=dev)
+        self._inputs = None                             # of the last forward()
+        self.head.hidden = self.head.labels = self.head.top_ids = self.head.top_logits = None
 
     def _takes(self, name: str, t: torch.Tensor, shape, dtypes) -> None:
         if t is None or t.shape != shape or t.dtype not in dtypes or t.device != self.device:
@@ -526,6 +528,8 @@ class HeadLoss:
         """(grad_hidden, grad_weights) for the inputs of the last forward(), from dL/dce and dL/dkd of every row."""
         if self.grad_hidden is None:
             raise RuntimeError("this HeadLoss was made without training=True")
+        if self._inputs is None:
+            raise RuntimeError("backward() needs a forward() before it")
         h = self.head
         for name, g in (("grad_ce", grad_ce), ("grad_kd", grad_kd)):
             if g is not None:
