@@ -507,21 +507,24 @@ class HeadLoss:
     def forward(self, hidden: torch.Tensor, labels: Optional[torch.Tensor] = None, top_ids: Optional[torch.Tensor] = None,
                 top_logits: Optional[torch.Tensor] = None, stream=None):
         """(ce, kd) of every row; None for a loss that is not there.  The inputs are kept for backward()."""
-        h = self.head
+        # all of the checks, then the descriptor: after a refusal it still has the last forward()'s inputs
+        h, many = self.head, self.rows > 1
         self._takes("hidden", hidden, (self.rows, self.dim), (self.hidden_dtype,))
-        h.hidden, h.hidden_stride = hidden.data_ptr(), hidden.stride(0) if self.rows > 1 else 0
         if self.labels:
             self._takes("labels", labels, (self.rows,), (torch.int64,))
-            h.labels = labels.data_ptr()
         if self.top_k:
             self._takes("top_ids", top_ids, (self.rows, self.top_k), (torch.int32,))
             self._takes("top_logits", top_logits, (self.rows, self.top_k), (torch.float32, torch.bfloat16))
-            stride = top_ids.stride(0) if self.rows > 1 else 0
-            if self.rows > 1 and top_logits.stride(0) != stride:
+            if many and top_logits.stride(0) != top_ids.stride(0):
                 raise ValueError("top_ids and top_logits need the same stride")
-            h.top_ids, h.top_logits, h.top_stride, h.top_dtype = top_ids.data_ptr(), top_logits.data_ptr(), stride, _DTYPE[top_logits.dtype]
-        self._inputs = hidden, labels, top_ids, top_logits
+        self._inputs = None                             # (a call that fails leaves nothing for backward())
+        h.hidden, h.hidden_stride = hidden.data_ptr(), hidden.stride(0) if many else 0
+        if self.labels:
+            h.labels = labels.data_ptr()
+        if self.top_k:
+            h.top_ids, h.top_logits, h.top_stride, h.top_dtype = top_ids.data_ptr(), top_logits.data_ptr(), top_ids.stride(0) if many else 0, _DTYPE[top_logits.dtype]
         eco.eco_head_loss(h, self.workspace, self.workspace_bytes, stream)
+        self._inputs = hidden, labels, top_ids, top_logits
         return self.ce, self.kd
 
     def backward(self, grad_ce: Optional[torch.Tensor] = None, grad_kd: Optional[torch.Tensor] = None, stream=None):
@@ -534,6 +537,6 @@ class HeadLoss:
         for name, g in (("grad_ce", grad_ce), ("grad_kd", grad_kd)):
             if g is not None:
                 self._takes(name, g, (self.rows,), (torch.float32,))
-            setattr(h, name, g.data_ptr() if g is not None else None)
+        h.grad_ce, h.grad_kd = (g.data_ptr() if g is not None else None for g in (grad_ce, grad_kd))
         eco.eco_head_loss_backward(h, self.workspace, self.workspace_bytes, stream)
         return self.grad_hidden, self.grad_weights

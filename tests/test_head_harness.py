@@ -10,6 +10,7 @@ def calls(monkeypatch):
     """The library's calls as (name, {field: value}) in their order; nothing is launched."""
     from paper_2601_22101_amd import harness
     made = []
+    monkeypatch.setattr(torch.Tensor, "is_cuda", True)          # the tensors here stand for ones on a GPU
 
     def keep(name):
         def call(head, workspace, workspace_bytes, stream=None):
@@ -49,3 +50,49 @@ def test_backward_needs_a_forward(calls, labels, top_k):
     head.forward(**arguments(s))
     head.backward(s["grad_ce"], s["grad_kd"])
     assert [name for name, _ in calls] == ["eco_head_loss", "eco_head_loss_backward"] and calls[1][1]["hidden"] == s["hidden"].data_ptr()
+
+
+def test_a_refused_forward_changes_nothing(calls):
+    """Inputs are looked at before any of them gets into the descriptor: after a refusal backward() has the last forward()'s, all of them."""
+    s, other = inputs(6, 64, 300, top_k=3, device="cpu"), inputs(6, 64, 300, top_k=3, seed=1, device="cpu")
+    head = head_for(s)
+    head.forward(**arguments(s))
+    kept = head._inputs
+    good = arguments(other)
+    for name, bad in (("labels", other["labels"].int()), ("labels", None), ("top_ids", other["top_ids"].long()), ("top_logits", other["top_logits"].half()),
+                      ("top_logits", torch.zeros(6, 5)[:, :3])):
+        with pytest.raises(ValueError):
+            head.forward(**{**good, name: bad})
+        assert all(a is b for a, b in zip(head._inputs, kept))
+    head.backward(s["grad_ce"], s["grad_kd"])
+    for name, t in arguments(s).items():
+        assert calls[-1][1][name] == t.data_ptr(), name
+
+
+def test_a_forward_that_fails_leaves_nothing_to_differentiate(calls, monkeypatch):
+    """A call that the library refuses, or fails, may have written some of what the backward pass reads."""
+    from paper_2601_22101_amd import binding, harness
+    s = inputs(6, 64, 300, device="cpu")
+    head = head_for(s)
+    head.forward(s["hidden"], s["labels"])
+
+    def fails(*args):
+        raise binding.EcoError(binding.ECO_EHIP, "head kernel launch")
+
+    with monkeypatch.context() as m:
+        m.setattr(harness.eco, "eco_head_loss", fails)
+        with pytest.raises(binding.EcoError):
+            head.forward(s["hidden"], s["labels"])
+    with pytest.raises(RuntimeError):
+        head.backward(s["grad_ce"])
+    head.forward(s["hidden"], s["labels"])
+    head.backward(s["grad_ce"])
+
+
+def test_a_refused_gradient_changes_nothing(calls):
+    s = inputs(6, 64, 300, top_k=3, device="cpu")
+    head = head_for(s)
+    head.forward(**arguments(s))
+    with pytest.raises(ValueError):
+        head.backward(s["grad_ce"], s["grad_kd"].double())
+    assert head.head.grad_ce is None and head.head.grad_kd is None
