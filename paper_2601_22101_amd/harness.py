@@ -466,12 +466,16 @@ class HeadLoss:
         self.hidden_dtype, self.device = hidden_dtype, dev
         self.weights, self.scales = weights, scales
         quantized = fmt in (eco.ECO_FMT_FP8_E4M3, eco.ECO_FMT_INT4)
+        if not weights.is_cuda:
+            raise ValueError("weights: memory of a GPU is needed")
         if quantized:
             need = vocab * dim if fmt == eco.ECO_FMT_FP8_E4M3 else (vocab * dim + 1) // 2
             if weights.dtype != torch.uint8 or weights.numel() < need or not weights.is_contiguous():
                 raise ValueError(f"weights: {need} contiguous bytes of codes are needed")
             if scales is None or not scales.is_contiguous() or group_size <= 0 or scales.numel() < -(-vocab * dim // group_size):
                 raise ValueError("scales: one for each scale group is needed, contiguous")
+            if scales.device != dev or scales.dtype not in _DTYPE:
+                raise ValueError(f"scales: {' or '.join(map(str, _DTYPE))} on {dev} is needed")
         else:
             want = torch.bfloat16 if fmt == eco.ECO_FMT_BF16_PLAIN else torch.float32
             if weights.dtype != want or weights.shape != (vocab, dim) or (dim > 1 and weights.stride(1) != 1) or (vocab > 1 and weights.stride(0) < dim):

@@ -96,3 +96,19 @@ def test_a_refused_gradient_changes_nothing(calls):
     with pytest.raises(ValueError):
         head.backward(s["grad_ce"], s["grad_kd"].double())
     assert head.head.grad_ce is None and head.head.grad_kd is None
+
+
+@pytest.mark.parametrize("weights", ["bf16", "fp8"])
+def test_weights_off_the_gpu_are_refused(weights):
+    """Their addresses are no memory of a kernel's."""
+    with pytest.raises(ValueError, match="GPU"):
+        head_for(inputs(6, 64, 300, weights=weights, device="cpu"))
+
+
+def test_scales_off_the_weights_device_are_refused(calls):
+    s = inputs(6, 64, 300, weights="fp8", device="cpu")
+    with pytest.raises(ValueError, match="scales"):
+        head_for(dict(s, scales=s["scales"].to("meta")))
+    with pytest.raises(ValueError, match="scales"):
+        head_for(dict(s, scales=s["scales"].half()))
+    head_for(s)
