@@ -508,6 +508,16 @@ class HeadLoss:
         if t.dim() > 1 and t.shape[0] > 1 and t.stride(0) < t.shape[1]:
             raise ValueError(f"{name}: rows must not overlap")
 
+    def _used_on(self, stream, tensors) -> None:
+        """A call on ``stream`` reads or writes them: their memory is not handed out again before it has ended, whenever they are let go."""
+        if stream is None:
+            return
+        if isinstance(stream, int):
+            stream = torch.cuda.ExternalStream(stream) if stream else torch.cuda.default_stream(self.device)
+        for t in (self.weights, self.scales, self.lse, self.lse_tau, self.picked, self.workspace, *tensors):
+            if t is not None:
+                t.record_stream(stream)
+
     def forward(self, hidden: torch.Tensor, labels: Optional[torch.Tensor] = None, top_ids: Optional[torch.Tensor] = None,
                 top_logits: Optional[torch.Tensor] = None, stream=None):
         """(ce, kd) of every row; None for a loss that is not there.  The inputs are kept for backward()."""
@@ -521,6 +531,8 @@ class HeadLoss:
             self._takes("top_logits", top_logits, (self.rows, self.top_k), (torch.float32, torch.bfloat16))
             if many and top_logits.stride(0) != top_ids.stride(0):
                 raise ValueError("top_ids and top_logits need the same stride")
+        taken = hidden, labels if self.labels else None, top_ids if self.top_k else None, top_logits if self.top_k else None
+        self._used_on(stream, (*taken, self.ce, self.kd))
         self._inputs = None                             # (a call that fails leaves nothing for backward())
         h.hidden, h.hidden_stride = hidden.data_ptr(), hidden.stride(0) if many else 0
         if self.labels:
@@ -528,7 +540,7 @@ class HeadLoss:
         if self.top_k:
             h.top_ids, h.top_logits, h.top_stride, h.top_dtype = top_ids.data_ptr(), top_logits.data_ptr(), top_ids.stride(0) if many else 0, _DTYPE[top_logits.dtype]
         eco.eco_head_loss(h, self.workspace, self.workspace_bytes, stream)
-        self._inputs = hidden, labels, top_ids, top_logits
+        self._inputs = taken
         return self.ce, self.kd
 
     def backward(self, grad_ce: Optional[torch.Tensor] = None, grad_kd: Optional[torch.Tensor] = None, stream=None):
@@ -541,6 +553,7 @@ class HeadLoss:
         for name, g in (("grad_ce", grad_ce), ("grad_kd", grad_kd)):
             if g is not None:
                 self._takes(name, g, (self.rows,), (torch.float32,))
+        self._used_on(stream, (*self._inputs, grad_ce, grad_kd, self.grad_hidden, self.grad_weights))
         h.grad_ce, h.grad_kd = (g.data_ptr() if g is not None else None for g in (grad_ce, grad_kd))
         eco.eco_head_loss_backward(h, self.workspace, self.workspace_bytes, stream)
         return self.grad_hidden, self.grad_weights

@@ -112,3 +112,21 @@ def test_scales_off_the_weights_device_are_refused(calls):
     with pytest.raises(ValueError, match="scales"):
         head_for(dict(s, scales=s["scales"].half()))
     head_for(s)
+
+
+def test_memory_of_a_call_on_another_stream_is_not_handed_out_again(calls, monkeypatch):
+    """Work on `stream` may be under way when a tensor that it reads or writes is let go: the allocator has to know of it."""
+    from types import SimpleNamespace
+    s, stream = inputs(6, 64, 300, weights="fp8", top_k=3, device="cpu"), SimpleNamespace(cuda_stream=0x5000)
+    head = head_for(s)
+    noted = set()
+    monkeypatch.setattr(torch.Tensor, "record_stream", lambda t, on: noted.add((t.data_ptr(), on.cuda_stream)))
+    head.forward(**arguments(s))
+    head.backward(s["grad_ce"], s["grad_kd"])
+    assert not noted                                            # on the current stream, whose allocations follow each other
+    both = [head.weights, head.scales, head.lse, head.lse_tau, head.picked, head.workspace, *arguments(s).values()]
+    head.forward(**arguments(s), stream=stream)
+    assert noted == {(t.data_ptr(), 0x5000) for t in (*both, head.ce, head.kd)}
+    noted.clear()
+    head.backward(s["grad_ce"], s["grad_kd"], stream=stream)
+    assert noted == {(t.data_ptr(), 0x5000) for t in (*both, s["grad_ce"], s["grad_kd"], head.grad_hidden, head.grad_weights)}
