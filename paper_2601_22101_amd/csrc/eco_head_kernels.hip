@@ -1223,7 +1223,7 @@ __device__ __forceinline__ float wave_sum(float x) {
   return x;
 }
 
-struct Teacher { float max, sum; };               // of a row's present logits over tau: q_j = exp(l_j / tau - max) / sum
+struct Teacher { float max, sum; };               // of a row's present logits over tau: q_j = exp(l_j / tau - max) / sum; a sum of 0: none has weight
 __device__ Teacher teacher_of(const HeadRows &r, uint64_t row, int lane) {
   const float it = 1.0f / r.tau;
   float m = -INFINITY;
@@ -1233,10 +1233,10 @@ __device__ Teacher teacher_of(const HeadRows &r, uint64_t row, int lane) {
       m = fmaxf(m, l);
     }
   m = wave_max(m);
+  if (m == -INFINITY) m = 0.0f;                   // (the maximum passes a NaN by, the sum does not)
   float s = 0.0f;
-  if (m != -INFINITY)
-    for (uint32_t j = lane; j < r.top_k; j += 64)
-      if (teacher_id(r, row, j) >= 0) s += exp2_fast((teacher_logit(r, row, j) * it - m) * LOG2E);
+  for (uint32_t j = lane; j < r.top_k; j += 64)
+    if (teacher_id(r, row, j) >= 0) s += exp2_fast((teacher_logit(r, row, j) * it - m) * LOG2E);
   return {m, wave_sum(s)};
 }
 

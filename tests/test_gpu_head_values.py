@@ -4,7 +4,7 @@ import pytest
 import torch
 
 from head_util import exact, hold, inputs
-from test_gpu_head import check
+from test_gpu_head import check, head_for
 
 pytestmark = pytest.mark.gpu
 
@@ -31,3 +31,28 @@ def test_a_distillation_loss_below_zero(rows, tau, weights):
         s["top_ids"][:, k - 1] = (s["labels"] + 1).int() % 500
         check(s)
         check(dict(s, labels=None, grad_ce=None))
+
+
+def rows_of_nan(rows, **kw):
+    """A row whose only entries with a logit are NaN, one with -inf beside it, and one with an ordinary entry."""
+    s = inputs(rows, 64, 500, top_k=3, seed=7, **kw)
+    nan, none = float("nan"), float("-inf")
+    s["top_logits"][1] = nan
+    s["top_logits"][2] = torch.tensor([none, nan, none])
+    s["top_logits"][3] = torch.tensor([1.0, nan, 2.0])
+    s["top_ids"][4], s["top_logits"][4] = -1, nan               # absent: no entry at all
+    return s
+
+
+@pytest.mark.parametrize("rows", [6, 200])
+@pytest.mark.parametrize("tau", [1.0, 2.0])
+def test_a_teacher_of_nan(rows, tau):
+    """A present entry that is no number makes its row's distillation loss none, and its gradient; other rows are as they were."""
+    s = rows_of_nan(rows, tau=tau)
+    head = head_for(s)
+    ce, kd = head.forward(s["hidden"], s["labels"], s["top_ids"], s["top_logits"])
+    gh, _ = head.backward(s["grad_ce"], s["grad_kd"])
+    bad = torch.zeros(rows, dtype=torch.bool, device="cuda")
+    bad[1:4] = True
+    assert torch.isnan(kd[bad]).all() and torch.isnan(gh[bad]).any(1).all()
+    assert torch.isfinite(kd[~bad]).all() and torch.isfinite(gh[~bad]).all() and torch.isfinite(ce).all() and kd[4] == 0
