@@ -1223,20 +1223,18 @@ __device__ __forceinline__ float wave_sum(float x) {
   return x;
 }
 
-struct Teacher { float max, sum; };               // of a row's present logits over tau: q_j = exp(l_j / tau - max) / sum; a sum of 0: none has weight
+// Of a row's present logits: q_j = exp((l_j - max) / tau) / sum; a sum of 0: none has weight.  (By differences: a finite logit over a temperature need not be finite.)
+struct Teacher { float max, sum; };
 __device__ Teacher teacher_of(const HeadRows &r, uint64_t row, int lane) {
-  const float it = 1.0f / r.tau;
   float m = -INFINITY;
   for (uint32_t j = lane; j < r.top_k; j += 64)
-    if (teacher_id(r, row, j) >= 0) {
-      const float l = teacher_logit(r, row, j) * it;
-      m = fmaxf(m, l);
-    }
+    if (teacher_id(r, row, j) >= 0) m = fmaxf(m, teacher_logit(r, row, j));
   m = wave_max(m);
   if (m == -INFINITY) m = 0.0f;                   // (the maximum passes a NaN by, the sum does not)
   float s = 0.0f;
+  const float it = 1.0f / r.tau;
   for (uint32_t j = lane; j < r.top_k; j += 64)
-    if (teacher_id(r, row, j) >= 0) s += exp2_fast((teacher_logit(r, row, j) * it - m) * LOG2E);
+    if (teacher_id(r, row, j) >= 0) s += exp2_fast((teacher_logit(r, row, j) - m) * it * LOG2E);
   return {m, wave_sum(s)};
 }
 
@@ -1340,7 +1338,7 @@ __global__ __launch_bounds__(256) void eco_head_finish_kernel(HeadRows r, HeadWe
     const float log_sum = log2_fast(q.sum) * LN2;
     for (uint32_t j = lane; j < r.top_k; j += 64) {
       if (teacher_id(r, row, j) < 0) continue;
-      const float log_q = teacher_logit(r, row, j) * it - q.max - log_sum;
+      const float log_q = (teacher_logit(r, row, j) - q.max) * it - log_sum;
       const float qj = exp2_fast(log_q * LOG2E);
       if (qj != 0.0f) sum = fmaf(qj, log_q - (z[j + 1] * it - lt), sum);
     }
@@ -1379,7 +1377,7 @@ __device__ void entries_of(const HeadRows &r, const EntryArgs &a, uint32_t c, in
   }
   for (uint32_t j = lane; j < entries; j += 64) {
     id_of[j] = j == 0 ? label : taught ? teacher_id(r, row, j - 1) : -1;
-    q_of[j] = j == 0 || id_of[j] < 0 ? 0.0f : exp2_fast((teacher_logit(r, row, j - 1) * it - q.max) * LOG2E) / q.sum;
+    q_of[j] = j == 0 || id_of[j] < 0 ? 0.0f : exp2_fast((teacher_logit(r, row, j - 1) - q.max) * it * LOG2E) / q.sum;
   }
   __syncthreads();
   for (uint32_t j = lane; j < entries; j += 64) {

@@ -3,7 +3,7 @@ Bounds as in head_util."""
 import pytest
 import torch
 
-from head_util import exact, hold, inputs
+from head_util import DTYPE, exact, inputs
 from test_gpu_head import check, head_for
 
 pytestmark = pytest.mark.gpu
@@ -56,3 +56,19 @@ def test_a_teacher_of_nan(rows, tau):
     bad[1:4] = True
     assert torch.isnan(kd[bad]).all() and torch.isnan(gh[bad]).any(1).all()
     assert torch.isfinite(kd[~bad]).all() and torch.isfinite(gh[~bad]).all() and torch.isfinite(ce).all() and kd[4] == 0
+
+
+@pytest.mark.parametrize("top", ["fp32", "bf16"])
+@pytest.mark.parametrize("tau", [0.25, 0.75, 1.0, 3.0])
+@pytest.mark.parametrize("rows", [8, 130])
+def test_logits_at_the_ends_of_their_type(rows, tau, top):
+    """The lowest value is a mask as -inf is, but in a row of nothing else all entries are alike; large logits count by their differences."""
+    s = inputs(rows, 64, 500, top_k=4, tau=tau, top=top, seed=9)
+    lowest = torch.finfo(DTYPE[top]).min
+    s["top_logits"][1] = lowest
+    s["top_logits"][2, 1:3] = lowest
+    s["top_logits"][3] = -lowest
+    s["top_logits"][4, 0], s["top_logits"][4, 1:] = 2.0 ** 127, lowest
+    s["top_logits"][5] = torch.tensor([lowest, lowest, float("-inf"), float("-inf")])
+    check(s)
+    check(dict(s, labels=None, grad_ce=None))
