@@ -1395,8 +1395,10 @@ __device__ void entries_of(const HeadRows &r, const EntryArgs &a, uint32_t c, in
     if (!first) continue;
     const float z = a.picked[row * entries + j];
     float g = 0.0f;
-    if (ga != 0.0f) g = ga * (exp2_fast((z - l1) * LOG2E) - (id == label ? 1.0f : 0.0f));
-    if (gb != 0.0f) g = fmaf(gb, exp2_fast((z * it - lt) * LOG2E) - weight, g);
+    // (a logit that lies above the logarithm of the sum with it does so by rounding; a NaN stays)
+    const float log_p = z - l1, log_p_tau = z * it - lt;
+    if (ga != 0.0f) g = ga * (exp2_fast(log_p > 0.0f ? 0.0f : log_p * LOG2E) - (id == label ? 1.0f : 0.0f));
+    if (gb != 0.0f) g = fmaf(gb, exp2_fast(log_p_tau > 0.0f ? 0.0f : log_p_tau * LOG2E) - weight, g);
     a.values[at] = g;
   }
 }

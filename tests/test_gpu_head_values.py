@@ -72,3 +72,27 @@ def test_logits_at_the_ends_of_their_type(rows, tau, top):
     s["top_logits"][5] = torch.tensor([lowest, lowest, float("-inf"), float("-inf")])
     check(s)
     check(dict(s, labels=None, grad_ce=None))
+
+
+@pytest.mark.parametrize("rows", [1, 40, 200])
+@pytest.mark.parametrize("weights", ["bf16", "fp32", "fp8", "int4"])
+@pytest.mark.parametrize("loss", ["ce", "kd"])
+def test_no_probability_is_above_one(rows, weights, loss):
+    """The entries' logits and the sum over the vocabulary round apart: where the student is sure, the gradient at the label may come out as
+    nothing, but not with the wrong sign."""
+    s = confident(rows, 512, 3000, 60.0, weights=weights, labels=True, top_k=1, tau=1.0, seed=rows)
+    s["labels"] = torch.randperm(3000, generator=torch.Generator().manual_seed(rows))[:rows].cuda()
+    s["hidden"] = (s["w"][s["labels"]] * (60.0 / (512 * 0.05 ** 2))).bfloat16()
+    s["grad_ce"], s["grad_kd"] = torch.ones(rows, device="cuda"), torch.ones(rows, device="cuda")
+    s["top_ids"] = s["labels"][:, None].int()
+    if loss == "ce":
+        s.update(top_k=0, top_ids=None, top_logits=None, grad_kd=None)
+    label = s["labels"]
+    if loss == "kd":
+        s.update(labels=None, grad_ce=None)
+    head = head_for(s, grad_weights=torch.float32)
+    head.forward(s["hidden"], s["labels"], s["top_ids"], s["top_logits"])
+    _, gw = head.backward(s["grad_ce"], s["grad_kd"])
+    along = (gw[label].double() * s["hidden"].double()).sum(1)
+    # (g h.h, where h.h is above 1000; the other rows' share is below e^-30)
+    assert (along <= 1e-9).all()
