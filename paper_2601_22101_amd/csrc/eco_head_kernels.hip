@@ -1617,19 +1617,21 @@ double rounds(uint64_t tiles) { return static_cast<double>((tiles + UNITS - 1) /
 
 // The piece of the vocabulary, at most `most`, whose tiles of the logits' gradient and of the weights' gradient take the least time in
 // rounds (with the inner axes' steps, and about eight steps of a tile's own at either end).  Tiles of one compute unit each.
+// (Training, us: 8192 x 1024 x 131072 in pieces of 32768 7890, of 26368 8020; 4096 x 1152 x 262144 of 65536 9220, of 37632 9360; 8192 x 512 x 262144, where the
+// model is off, of 32768 9110, of 29184 9030.)
 uint64_t head_piece(int shape, uint64_t rows, uint64_t dim, uint64_t vocab, uint64_t most) {
   if (shape != HEAD_LARGE) return most;
   const uint64_t all = ceil_div(vocab, 256), row_tiles = ceil_div(rows, 256), dim_tiles = ceil_div(dim, dim_tile(shape, dim));
   const uint64_t fewest = ceil_div(all, most / 256);
+  const auto of = [&](uint64_t n) {
+    return rounds(n * row_tiles) * (static_cast<double>(dim) / KSTEP + 8) +
+           rounds(n * dim_tiles) * (static_cast<double>(rows) / KSTEP + 8) * static_cast<double>(dim_tile(shape, dim)) / 256;
+  };
   double best = 0.0;
   uint64_t piece = most;
   for (uint64_t pieces = fewest; pieces <= 2 * fewest && pieces <= all && pieces < fewest + 64; ++pieces) {
-    const uint64_t tiles = ceil_div(all, pieces), last = all - tiles * (ceil_div(all, tiles) - 1);
-    double cost = 0.0;
-    for (const uint64_t n : {tiles, last})
-      cost += (n == tiles ? static_cast<double>(ceil_div(all, tiles) - 1) : 1.0) *
-              (rounds(n * row_tiles) * (static_cast<double>(dim) / KSTEP + 8) +
-               rounds(n * dim_tiles) * (static_cast<double>(rows) / KSTEP + 8) * static_cast<double>(dim_tile(shape, dim)) / 256);
+    const uint64_t tiles = ceil_div(all, pieces), whole = ceil_div(all, tiles) - 1;
+    const double cost = static_cast<double>(whole) * of(tiles) + of(all - whole * tiles);
     if (pieces == fewest || cost < 0.99 * best) { best = cost; piece = tiles * 256; }
   }
   return piece;
