@@ -347,7 +347,7 @@ typedef struct eco_head {
 } eco_head_t;
 
 /* eco_head_loss_workspace — host only: bytes of device memory that eco_head_loss (backward = 0) or eco_head_loss_backward (1) needs for
- * this descriptor.  It depends on rows, vocab, dim, top_k, temperature, the formats, types and weight_stride, and on which losses are there. */
+ * this descriptor.  It depends on rows, vocab, dim, top_k, temperature, the formats, types, group_size and weight_stride, and on which losses are there. */
 eco_status_t eco_head_loss_workspace(const eco_head_t *head, int32_t backward, size_t *bytes);
 
 /* eco_head_loss — the losses of every row, with lse, lse_tau and picked.  `workspace`: device memory, 256-byte aligned, of at least the size above;
