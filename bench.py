@@ -59,12 +59,13 @@ def algorithmic_bytes(wl, variant: str = "adam-sr") -> float:
 
 
 def kernel_source_hash() -> str:
-    """sha256 over the library's kernel and launch sources: what a committed profile was measured on."""
+    """sha256 over the step's kernel and launch sources, those of the losses at the output projection (eco_head*) left out: what a committed
+    profile of it was measured on."""
     import hashlib
     h = hashlib.sha256()
     d = os.path.join(ROOT, "paper_2601_22101_amd", "csrc")
     for fn in sorted(os.listdir(d)):
-        if fn.endswith((".hip", ".hpp", ".cpp")):
+        if fn.endswith((".hip", ".hpp", ".cpp")) and not fn.startswith("eco_head"):
             h.update(fn.encode())
             h.update(open(os.path.join(d, fn), "rb").read())
     return h.hexdigest()[:16]
