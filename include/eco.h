@@ -314,8 +314,8 @@ eco_status_t eco_arith_selftest(int32_t kind, float numerator, uint32_t bits_lo,
  * atomics: the same call on the same arrays gives the same bits.
  *
  * Time (MI355X, bf16 but where noted; rows x dim x vocab): losses 1 x 512 x 32000 16 us, 2048 x 1024 x 50304 0.21 ms, 24 x 2048 x 102400 in INT4 0.10 ms;
- * losses and gradients 2048 x 1024 x 50304 in FP8 1.6 ms, 4096 x 2048 x 102400 with a quarter of the rows ignored 4.8 ms, 8192 x 1152 x 262144 18.6 ms.  Matrix
- * cores bound many rows, the reading of the weights few.  fp32 weights with fp32 hidden states are slow for few rows: they are first written as planes.
+ * losses and gradients 2048 x 1024 x 50304 in FP8 1.6 ms, 4096 x 2048 x 102400 with a quarter of the rows ignored 4.9 ms, 8192 x 1152 x 262144 19.0 ms.  The
+ * products bound many rows, the reading of the weights few.  fp32 weights with fp32 hidden states are slow for few rows: they are first written as planes.
  */
 typedef struct eco_head {
   const void *hidden;         /* rows x dim values of hidden_dtype, aligned to their size                                          */

@@ -454,7 +454,8 @@ class HeadLoss:
 
     ``weights`` (with ``scales`` and ``group_size`` if quantized) are the arrays that the step updates in place, vocab x dim in the
     storage format ``fmt``; unquantized ones may have a row stride.  The tensors that forward() and backward() return are the object's own and
-    are written again by its next call; both run on the current stream, or on ``stream``.
+    are written again by its next call; both run on the current stream, or on ``stream``, whose use of the tensors the allocator is then told of.
+    A call that refuses its arguments (ValueError) leaves the object as it was.
     """
 
     def __init__(self, rows: int, vocab: int, dim: int, *, weights: torch.Tensor, fmt: int, scales: Optional[torch.Tensor] = None, group_size: int = 0,
