@@ -104,7 +104,7 @@ struct Layout {
 
 // Bytes that the converted weights and the logits' gradient of a piece of the vocabulary may take each.  Whether the 256 MB cache in front
 // of HBM holds a piece between the product that writes it and those that read it makes no difference, how many whole rounds of tiles it is
-// does (8192 x 1152 x 262144, training, ms in the kernels: 64 MB 28.2, 128 22.2, 256 22.6, 512 21.2, 1024 21.2).
+// does (8192 x 1152 x 262144, training, ms: 64 MB 26.8, 128 20.8, 256 19.2, 512 18.7, 1024, in twice the memory, 18.2).
 constexpr uint64_t PIECE_BYTES = 512ull << 20;
 
 bool two_softmaxes(const eco_head_t *h) { return h->labels && h->top_k && static_cast<float>(h->temperature) != 1.0f; }
@@ -316,7 +316,7 @@ eco_status_t eco_head_loss_backward(const eco_head_t *head, void *workspace, siz
   const uint64_t out_stride = stride_or(head->grad_weights_stride, head->dim);
   const eco::HeadWeights weights = weights_of(head);
   // A gradient that the 256 MB cache in front of HBM cannot hold passes the caches by: on its way out it would take the place of the weights, which the next
-  // call reads (67 x 1152 x 262144, training, a pass: 722 us, 758 without).
+  // call reads (67 x 1152 x 262144, training, a pass: 639 us, 684 without).
   const bool past_caches = head->vocab * head->dim * size_of(head->grad_weights_dtype) > (256u << 20);
   for (uint64_t first = 0; first < head->vocab; first += l.piece) {
     const uint32_t n = static_cast<uint32_t>(head->vocab - first < l.piece ? head->vocab - first : l.piece);

@@ -1551,8 +1551,8 @@ __global__ __launch_bounds__(256) void eco_head_grad_hidden_finish_kernel(const 
 uint64_t ceil_div(uint64_t a, uint64_t b) { return (a + b - 1) / b; }
 uint32_t blocks_for(uint64_t work) { return static_cast<uint32_t>(work < 256 * 8192 ? (work + 255) / 256 : 8192); }
 
-// Tiles.  The large ones are the faster ones where they are enough for the chip (training, us, large / medium: 130 x 1152 x 262144 967 / 1069, 400 1370 /
-// 1890, 1000 2413 / 3544; 256 x 2048 x 102400 668 / 757; 200 x 512 x 32000 120 / 90, 512 134 / 126, 1000 180 / 199; 70 x 1152 x 262144 933 / 735).
+// Tiles.  The large ones are the faster ones where they are enough for the chip (training, us, large / medium: 130 x 1152 x 262144 721 / 965, 400 1257 /
+// 1772, 1000 2428 / 3277; 256 x 2048 x 102400 586 / 699; 200 x 512 x 32000 104 / 104, 512 128 / 149, 1000 195 / 215; 70 x 1152 x 262144 658 / 642).
 using Large = Tile<256, 256, 2, 4, 2>;
 using Large192 = Tile<192, 256, 2, 4, 2>;         // across the hidden dimension, where the others would be a quarter empty (1229 x 576 x 32128, both gradients 150 -> 119 us)
 using Medium = Tile<128, 128, 2, 2, 2>;
