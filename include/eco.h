@@ -358,6 +358,104 @@ eco_status_t eco_head_loss(const eco_head_t *head, void *workspace, size_t works
  * what the forward pass wrote to lse, lse_tau and picked.  Otherwise as eco_head_loss. */
 eco_status_t eco_head_loss_backward(const eco_head_t *head, void *workspace, size_t workspace_bytes, void *stream);
 
+/*
+ * The feed-forward half of a layer on the weights that eco_step keeps: a norm, the linear product and the gated unit, each with its gradients, which leave as
+ * the bf16 that eco_step reads.  Activations go from one to the next as 8-bit rows:
+ *     a row's blocks of 128 elements (the last one may be shorter) are E4M3 codes times 2^e, e the smallest whole number of [-100, 127] with
+ *     max |block| <= 448 2^e; codes are rounded to nearest, ties to even; the scale is the byte e + 127 (E8M0), rows x ceil(dim / 128) of them, packed.
+ * The power of two goes into the matrix instruction beside the codes and makes a value exact as a bfloat16.  A block that holds a value which is not finite
+ * becomes NaN as a whole (codes 0x7F, scale byte 0xFF).
+ *
+ * Common to these calls: rows may be 0 (an expert that got no token: outputs of rows are left alone, gradients of weights and gains are written as zeros).  A stride
+ * counts elements from one row to the next, 0 stands for packed rows; what lies behind a row's end or behind the last row is neither read nor written.  Pointers are
+ * aligned to their elements, where no more is said.  `workspace`: device memory, 256-byte aligned, of at least the size that the _workspace call gives for
+ * the descriptor, which is enough for as many rows and for fewer (0: NULL will do); nothing in it has to be kept between calls.  All run asynchronously on `stream`, allocate nothing and may be captured into a
+ * graph.  No atomics: the same call on the same arrays gives the same bits.  At most 2^23 rows and 2^16 columns of anything, strides below 2^23.
+ */
+
+/* eco_rows_quantize — rows of src_dtype (ECO_DT_FP32 or ECO_DT_BF16) as 8-bit rows: an attention's output, say, on its way to eco_linear. */
+eco_status_t eco_rows_quantize(const void *src, int32_t src_dtype, uint64_t rows, uint64_t dim, uint64_t src_stride, void *codes, uint64_t codes_stride,
+                               void *scales, void *stream);
+
+/*
+ * Root-mean-square norm with the residual's addition.  For each row:
+ *     s = input + residual, rounded to dtype (the residual stream; s = input where residual is NULL)
+ *     rstd = 1 / sqrt(mean s^2 + eps);  y = s rstd gain, as 8-bit rows or, without scales, rounded to dtype
+ * backward, from grad_out = dL/dy (which passes the rounding to 8 bits straight through) and grad_sum = dL/ds from what else reads s (NULL: none):
+ *     grad_input = rstd (u - s rstd mean(u s rstd)) + grad_sum,  u = grad_out gain     (the gradient of input and of residual alike)
+ *     grad_gain  = sum over the rows of grad_out s rstd
+ * Sums are fp32.  sum may be input or residual, grad_input may be grad_out or grad_sum: a row is read before it is written.
+ */
+typedef struct eco_norm {
+  const void *input;          /* rows x dim of dtype; so residual, sum, grad_out, grad_sum, grad_input                            */
+  const void *residual;       /* or NULL                                                                                          */
+  void *sum;                  /* forward output, there if residual is; the backward pass reads it, and input where it is NULL     */
+  const void *gain;           /* dim of gain_dtype; NULL: ones                                                                    */
+  void *out;                  /* forward output: codes, or rows x dim of dtype where scales is NULL                               */
+  void *scales;               /* forward output: the scale bytes                                                                  */
+  float *rstd;                /* rows: written by the forward pass (NULL: not), read by the backward                              */
+  const void *grad_out, *grad_sum;
+  void *grad_input;           /* backward outputs; either may be NULL                                                             */
+  void *grad_gain;            /* dim of grad_gain_dtype                                                                           */
+  uint64_t rows, dim;
+  uint64_t input_stride, residual_stride, sum_stride, out_stride, grad_out_stride, grad_sum_stride, grad_input_stride;
+  double eps;                 /* > 0 */
+  int32_t dtype, gain_dtype, grad_gain_dtype;                              /* eco_dtype_t */
+} eco_norm_t;
+
+eco_status_t eco_norm(const eco_norm_t *norm, void *stream);
+eco_status_t eco_norm_backward_workspace(const eco_norm_t *norm, size_t *bytes);        /* host only */
+eco_status_t eco_norm_backward(const eco_norm_t *norm, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * Linear product of 8-bit rows with quantized weights:  out = x W^T (+ add), x = code 2^e, W = dec(code) * scale, out_dim x in_dim as eco_step keeps them.
+ * in_dim is a multiple of 16.  Scale groups: the row (group_size = in_dim), the tensor (group_size >= its elements), or a multiple of 128 elements that divides in_dim.
+ * Sums are fp32 of exact products of codes, of 128 at a time where groups are shorter than rows, times the weights' scale; out is rounded once.  INT4 codes are
+ * exact as E4M3.  backward, from grad_out (bf16):
+ *     grad_input = grad_out W   (of the values behind the 8-bit rows; W rounded to bf16, sums fp32, rounded once to bf16)
+ *     grad_weights = grad_out^T x   (exact products, sums fp32, rounded once to bf16: what eco_step reads)
+ */
+typedef struct eco_linear {
+  const void *codes, *code_scales;    /* the input rows, rows x in_dim; codes are 16-byte aligned, codes_stride a multiple of 16    */
+  const void *weights, *scales;       /* laid out as in eco_tensor_t, ECO_FMT_FP8_E4M3 or ECO_FMT_INT4, 16-byte aligned             */
+  const void *add;                    /* rows x out_dim of out_dtype, NULL: nothing; may be out                                     */
+  void *out;                          /* forward output, rows x out_dim of out_dtype                                                */
+  const void *grad_out;               /* rows x out_dim bf16                                                                        */
+  void *grad_input;                   /* backward outputs, rows x in_dim and out_dim x in_dim bf16; either may be NULL; grad_weights is */
+  void *grad_weights;                 /*   packed, and 16-byte aligned                                                              */
+  uint64_t rows, in_dim, out_dim;
+  uint64_t codes_stride, add_stride, out_stride, grad_out_stride, grad_input_stride;
+  uint64_t group_size;
+  int32_t fmt, scale_dtype, out_dtype;
+} eco_linear_t;
+
+eco_status_t eco_linear_workspace(const eco_linear_t *linear, int32_t backward, size_t *bytes);       /* host only */
+eco_status_t eco_linear(const eco_linear_t *linear, void *workspace, size_t workspace_bytes, void *stream);
+eco_status_t eco_linear_backward(const eco_linear_t *linear, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * Gated unit:  h = act(x G^T) * (x U^T) as 8-bit rows, x 8-bit rows, G and U width x in_dim as the weights of eco_linear.  Both projections, the activation, the
+ * product and the rounding to 8 bits are one kernel; nothing else is kept, and the backward pass computes a = x G^T and b = x U^T again.  From grad_out = dL/dh (bf16):
+ *     ga = grad_out b act'(a),  gb = grad_out act(a), each rounded once to bf16
+ *     grad_input = ga G + gb U,  grad_gate = ga^T x,  grad_up = gb^T x     (as those of eco_linear)
+ */
+typedef enum { ECO_ACT_SILU = 0, ECO_ACT_GELU = 1 } eco_act_t;      /* a / (1 + exp(-a));  a (1 + tanh(sqrt(2/pi) (a + 0.044715 a^3))) / 2 */
+typedef struct eco_gated {
+  const void *codes, *code_scales;
+  const void *gate, *gate_scales, *up, *up_scales;
+  void *out, *out_scales;             /* forward output: 8-bit rows, rows x width                                                   */
+  const void *grad_out;               /* rows x width bf16                                                                          */
+  void *grad_input, *grad_gate, *grad_up;     /* backward outputs, bf16; grad_input may be NULL, so may grad_gate and grad_up together */
+  uint64_t rows, in_dim, width;
+  uint64_t codes_stride, out_stride, grad_out_stride, grad_input_stride;
+  uint64_t group_size;
+  int32_t fmt, scale_dtype, act;
+} eco_gated_t;
+
+eco_status_t eco_gated_workspace(const eco_gated_t *gated, int32_t backward, size_t *bytes);          /* host only */
+eco_status_t eco_gated(const eco_gated_t *gated, void *workspace, size_t workspace_bytes, void *stream);
+eco_status_t eco_gated_backward(const eco_gated_t *gated, void *workspace, size_t workspace_bytes, void *stream);
+
 /* eco_step_constants — host only: validates hp as eco_step does and writes the derived fp32 constants. */
 eco_status_t eco_step_constants(const eco_hparams_t *hp, eco_constants_t *out);
 

@@ -19,6 +19,7 @@ ECO_FMT_FP8_E4M3, ECO_FMT_INT4, ECO_FMT_BF16_PLAIN, ECO_FMT_FP32_IDENTITY = 0, 1
 ECO_OPT_ADAM, ECO_OPT_SGDM = 0, 1
 ECO_ROUND_SR, ECO_ROUND_RTN = 0, 1
 ECO_DT_FP32, ECO_DT_BF16 = 0, 1
+ECO_ACT_SILU, ECO_ACT_GELU = 0, 1
 ECO_MODE_NAIVE, ECO_MODE_ECO, ECO_MODE_EXACT, ECO_MODE_MASTER = 0, 1, 2, 3
 
 
@@ -49,6 +50,27 @@ class eco_head_t(C.Structure):
                 + [(n, C.c_int32) for n in ("fmt", "scale_dtype", "hidden_dtype", "top_dtype", "grad_weights_dtype")])
 
 
+class eco_norm_t(C.Structure):
+    _fields_ = ([(n, C.c_void_p) for n in ("input", "residual", "sum", "gain", "out", "scales", "rstd", "grad_out", "grad_sum", "grad_input", "grad_gain")]
+                + [(n, C.c_uint64) for n in ("rows", "dim", "input_stride", "residual_stride", "sum_stride", "out_stride", "grad_out_stride", "grad_sum_stride",
+                                             "grad_input_stride")]
+                + [("eps", C.c_double)] + [(n, C.c_int32) for n in ("dtype", "gain_dtype", "grad_gain_dtype")])
+
+
+class eco_linear_t(C.Structure):
+    _fields_ = ([(n, C.c_void_p) for n in ("codes", "code_scales", "weights", "scales", "add", "out", "grad_out", "grad_input", "grad_weights")]
+                + [(n, C.c_uint64) for n in ("rows", "in_dim", "out_dim", "codes_stride", "add_stride", "out_stride", "grad_out_stride", "grad_input_stride",
+                                             "group_size")]
+                + [(n, C.c_int32) for n in ("fmt", "scale_dtype", "out_dtype")])
+
+
+class eco_gated_t(C.Structure):
+    _fields_ = ([(n, C.c_void_p) for n in ("codes", "code_scales", "gate", "gate_scales", "up", "up_scales", "out", "out_scales", "grad_out", "grad_input",
+                                           "grad_gate", "grad_up")]
+                + [(n, C.c_uint64) for n in ("rows", "in_dim", "width", "codes_stride", "out_stride", "grad_out_stride", "grad_input_stride", "group_size")]
+                + [(n, C.c_int32) for n in ("fmt", "scale_dtype", "act")])
+
+
 class EcoError(RuntimeError):
     def __init__(self, status: int, message: str):
         super().__init__(f"eco status {status}: {message}")
@@ -77,9 +99,18 @@ def _load() -> C.CDLL:
     lib.eco_head_loss_workspace.argtypes = [C.POINTER(eco_head_t), i32, C.POINTER(C.c_size_t)]
     lib.eco_head_loss.argtypes = [C.POINTER(eco_head_t), vp, C.c_size_t, vp]
     lib.eco_head_loss_backward.argtypes = [C.POINTER(eco_head_t), vp, C.c_size_t, vp]
+    lib.eco_rows_quantize.argtypes = [vp, i32, u64, u64, u64, vp, u64, vp, vp]
+    lib.eco_norm.argtypes = [C.POINTER(eco_norm_t), vp]
+    lib.eco_norm_backward_workspace.argtypes = [C.POINTER(eco_norm_t), C.POINTER(C.c_size_t)]
+    lib.eco_norm_backward.argtypes = [C.POINTER(eco_norm_t), vp, C.c_size_t, vp]
+    for name, struct in (("eco_linear", eco_linear_t), ("eco_gated", eco_gated_t)):
+        getattr(lib, name + "_workspace").argtypes = [C.POINTER(struct), i32, C.POINTER(C.c_size_t)]
+        getattr(lib, name).argtypes = getattr(lib, name + "_backward").argtypes = [C.POINTER(struct), vp, C.c_size_t, vp]
     for name in ("eco_plan_create", "eco_plan_destroy", "eco_step", "eco_step_tensors", "eco_step_tensors_noalloc", "eco_quantize_init",
                  "eco_dequantize", "eco_quantize_error", "eco_bandwidth_probe", "eco_arith_selftest", "eco_philox_fill", "eco_step_constants", "eco_set_option", "eco_version",
-                 "eco_head_loss_workspace", "eco_head_loss", "eco_head_loss_backward"):
+                 "eco_head_loss_workspace", "eco_head_loss", "eco_head_loss_backward",
+                 "eco_rows_quantize", "eco_norm", "eco_norm_backward_workspace", "eco_norm_backward", "eco_linear_workspace", "eco_linear", "eco_linear_backward",
+                 "eco_gated_workspace", "eco_gated", "eco_gated_backward"):
         getattr(lib, name).restype = C.c_int
     lib.eco_status_string.argtypes = [C.c_int]
     lib.eco_status_string.restype = C.c_char_p
@@ -272,6 +303,83 @@ def eco_head_loss(head: eco_head_t, workspace, workspace_bytes: int, stream=None
 
 def eco_head_loss_backward(head: eco_head_t, workspace, workspace_bytes: int, stream=None) -> None:
     _check(lib.eco_head_loss_backward(C.byref(head), _ptr(workspace), workspace_bytes, _stream(stream)))
+
+
+def eco_rows_quantize(src, src_dtype: int, rows: int, dim: int, src_stride: int, codes, codes_stride: int, scales, stream=None) -> None:
+    _check(lib.eco_rows_quantize(_ptr(src), src_dtype, rows, dim, src_stride, _ptr(codes), codes_stride, _ptr(scales), _stream(stream)))
+
+
+def _fill(struct, ints, pointers):
+    for name, value in ints.items():
+        setattr(struct, name, value)
+    for name, value in pointers.items():
+        setattr(struct, name, _ptr(value))
+    return struct
+
+
+def make_norm(*, rows: int, dim: int, eps: float, dtype=ECO_DT_BF16, gain_dtype=ECO_DT_BF16, grad_gain_dtype=ECO_DT_BF16, input_stride=0, residual_stride=0,
+              sum_stride=0, out_stride=0, grad_out_stride=0, grad_sum_stride=0, grad_input_stride=0, **pointers) -> eco_norm_t:
+    """`pointers`: input, residual, sum, gain, out, scales, rstd, grad_out, grad_sum, grad_input, grad_gain."""
+    return _fill(eco_norm_t(), dict(rows=rows, dim=dim, eps=eps, dtype=dtype, gain_dtype=gain_dtype, grad_gain_dtype=grad_gain_dtype, input_stride=input_stride,
+                                    residual_stride=residual_stride, sum_stride=sum_stride, out_stride=out_stride, grad_out_stride=grad_out_stride,
+                                    grad_sum_stride=grad_sum_stride, grad_input_stride=grad_input_stride), pointers)
+
+
+def make_linear(*, rows: int, in_dim: int, out_dim: int, group_size: int, fmt=ECO_FMT_FP8_E4M3, scale_dtype=ECO_DT_FP32, out_dtype=ECO_DT_BF16, codes_stride=0,
+                add_stride=0, out_stride=0, grad_out_stride=0, grad_input_stride=0, **pointers) -> eco_linear_t:
+    """`pointers`: codes, code_scales, weights, scales, add, out, grad_out, grad_input, grad_weights."""
+    return _fill(eco_linear_t(), dict(rows=rows, in_dim=in_dim, out_dim=out_dim, group_size=group_size, fmt=fmt, scale_dtype=scale_dtype, out_dtype=out_dtype,
+                                      codes_stride=codes_stride, add_stride=add_stride, out_stride=out_stride, grad_out_stride=grad_out_stride,
+                                      grad_input_stride=grad_input_stride), pointers)
+
+
+def make_gated(*, rows: int, in_dim: int, width: int, group_size: int, fmt=ECO_FMT_FP8_E4M3, scale_dtype=ECO_DT_FP32, act=ECO_ACT_SILU, codes_stride=0, out_stride=0,
+               grad_out_stride=0, grad_input_stride=0, **pointers) -> eco_gated_t:
+    """`pointers`: codes, code_scales, gate, gate_scales, up, up_scales, out, out_scales, grad_out, grad_input, grad_gate, grad_up."""
+    return _fill(eco_gated_t(), dict(rows=rows, in_dim=in_dim, width=width, group_size=group_size, fmt=fmt, scale_dtype=scale_dtype, act=act, codes_stride=codes_stride,
+                                     out_stride=out_stride, grad_out_stride=grad_out_stride, grad_input_stride=grad_input_stride), pointers)
+
+
+def _workspace(call, *args) -> int:
+    out = C.c_size_t()
+    _check(call(*args, C.byref(out)))
+    return out.value
+
+
+def eco_norm(norm: eco_norm_t, stream=None) -> None:
+    _check(lib.eco_norm(C.byref(norm), _stream(stream)))
+
+
+def eco_norm_backward_workspace(norm: eco_norm_t) -> int:
+    return _workspace(lib.eco_norm_backward_workspace, C.byref(norm))
+
+
+def eco_norm_backward(norm: eco_norm_t, workspace, workspace_bytes: int, stream=None) -> None:
+    _check(lib.eco_norm_backward(C.byref(norm), _ptr(workspace), workspace_bytes, _stream(stream)))
+
+
+def eco_linear_workspace(linear: eco_linear_t, backward: bool) -> int:
+    return _workspace(lib.eco_linear_workspace, C.byref(linear), int(backward))
+
+
+def eco_linear(linear: eco_linear_t, workspace, workspace_bytes: int, stream=None) -> None:
+    _check(lib.eco_linear(C.byref(linear), _ptr(workspace), workspace_bytes, _stream(stream)))
+
+
+def eco_linear_backward(linear: eco_linear_t, workspace, workspace_bytes: int, stream=None) -> None:
+    _check(lib.eco_linear_backward(C.byref(linear), _ptr(workspace), workspace_bytes, _stream(stream)))
+
+
+def eco_gated_workspace(gated: eco_gated_t, backward: bool) -> int:
+    return _workspace(lib.eco_gated_workspace, C.byref(gated), int(backward))
+
+
+def eco_gated(gated: eco_gated_t, workspace, workspace_bytes: int, stream=None) -> None:
+    _check(lib.eco_gated(C.byref(gated), _ptr(workspace), workspace_bytes, _stream(stream)))
+
+
+def eco_gated_backward(gated: eco_gated_t, workspace, workspace_bytes: int, stream=None) -> None:
+    _check(lib.eco_gated_backward(C.byref(gated), _ptr(workspace), workspace_bytes, _stream(stream)))
 
 
 class Plan:

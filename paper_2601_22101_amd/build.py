@@ -25,6 +25,10 @@ SOURCES = [
     "eco_step_int4_bf16.hip",
     "eco_head_api.cpp",
     "eco_head_kernels.hip",
+    "eco_norm_kernels.hip",
+    "eco_ffn_api.cpp",
+    "eco_ffn_kernels.hip",
+    "eco_ffn_grad_kernels.hip",
 ]
 
 # -ffp-contract=off: the kernels spell every fused multiply-add explicitly, so that their fp32

@@ -1,0 +1,101 @@
+// Host/device shared declarations of the feed-forward half of a layer (eco_norm, eco_linear, eco_gated and their backward passes): what the host works out
+// from a descriptor, and the launcher entry points.
+#pragma once
+#include <hip/hip_runtime_api.h>
+#include <stdint.h>
+
+namespace eco {
+
+constexpr uint64_t FFN_MOST_ROWS = 1ull << 23, FFN_MOST_DIM = 1ull << 16, FFN_MOST_STRIDE = 1ull << 23;
+constexpr uint32_t FFN_BLOCK = 128;               // elements of a row to a scale: one step of the 8-bit products
+// Parts that a product's inner axis is summed in, and what the parts may take: a workspace is asked for once, for the most rows, and has to hold any call with fewer.
+constexpr uint64_t FFN_MOST_SPLITS = 32;
+constexpr uint64_t FFN_MOST_PARTIAL = 256ull * 64 * 128;       // elements, 8-bit products: they are split where there are less than 256 of the smallest tiles
+constexpr uint64_t FFN_MOST_INPUT_ROWS = 32768;                // rows of all parts of grad_input
+constexpr uint64_t FFN_MOST_WEIGHTS_PARTIAL = 1ull << 26;      // elements of all parts of grad_weights
+
+constexpr uint64_t ffn_round_up(uint64_t x, uint64_t k) { return (x + k - 1) / k * k; }
+
+struct NormRows {
+  const void *input, *residual, *gain;
+  void *sum, *out;
+  uint8_t *scales;
+  float *rstd;
+  uint64_t input_stride, residual_stride, sum_stride, out_stride;
+  uint32_t rows, dim;
+  float eps;
+  int32_t bf16, gain_bf16, norm;                  // norm 0: the rows as they are, to 8 bits
+};
+hipError_t launch_norm(const NormRows &, hipStream_t);
+
+struct NormGrad {
+  const void *s, *gain, *grad_out, *grad_sum;
+  const float *rstd;
+  void *grad_input, *grad_gain;
+  float *partial;                                 // [norm_parts()][dim]: the gain's gradient over the rows of each workgroup
+  uint64_t s_stride, grad_out_stride, grad_sum_stride, grad_input_stride;
+  uint32_t rows, dim;
+  int32_t bf16, gain_bf16, grad_gain_bf16;
+};
+uint32_t norm_parts(uint64_t rows, uint64_t dim);
+hipError_t launch_norm_backward(const NormGrad &, hipStream_t);
+
+// One or two matrices of weights with the same shape and scale groups.  Element (n, k) has the scale n * scale_row + k / (128 * group_blocks), the last term 0 where
+// group_blocks is 0.
+struct FfnWeights {
+  const void *data[2], *scales[2];
+  uint32_t matrices, rows, dim, scale_row, group_blocks;
+  int32_t fmt, scale_bf16;
+};
+
+struct FfnRows8 {
+  const uint8_t *codes, *scales;
+  uint64_t stride;
+  uint32_t rows, dim, blocks;                     // blocks = ceil(dim / 128), scale bytes of a row
+};
+
+// What becomes of the products' sums.
+struct FfnOut {
+  const void *add;                                // linear
+  void *out;
+  uint64_t add_stride, out_stride;
+  float *partial;                                 // linear: [splits][rows][out_dim], joined by launch_ffn_join; null: written at once
+  uint32_t splits, split_steps;
+  int32_t bf16, act;
+  uint8_t *scales;                                // gated: out are codes
+  const uint16_t *grad_out;                       // the gated unit's backward pass: out is [rows][2 half] bf16, ga then gb, with zeros from width to half
+  uint64_t grad_out_stride;
+  uint32_t half;
+};
+enum : int { FFN_LINEAR = 0, FFN_GATED = 1, FFN_GATED_BACK = 2 };
+
+// Tiles of an 8-bit product: rows of x to a tile; 0: the kernel for few rows, which takes weights as they are stored.
+struct FfnPlan { int end, rows_tile, width_tile; uint32_t splits, split_steps; };
+FfnPlan ffn_plan(int end, const FfnWeights &, uint64_t rows);
+hipError_t launch_ffn(const FfnPlan &, const FfnRows8 &, const FfnWeights &, const FfnOut &, hipStream_t);
+hipError_t launch_ffn_join(const FfnOut &, uint32_t rows, uint32_t width, hipStream_t);
+// INT4 codes as the E4M3 codes of the same values (one matrix).
+hipError_t launch_ffn_expand(const void *codes, uint64_t numel, void *out, hipStream_t);
+
+// ---- gradients, of bf16 operands
+// Weights as bf16 rows [matrices][padded rows][ld], zeros in the padding; x the same; a bf16 matrix copied with padding.
+hipError_t launch_ffn_weights_bf16(const FfnWeights &, void *out, uint32_t padded_rows, hipStream_t);
+hipError_t launch_ffn_rows_bf16(const FfnRows8 &, void *out, uint32_t padded_rows, hipStream_t);
+hipError_t launch_ffn_pad(const void *src, uint64_t src_stride, uint32_t rows, uint32_t dim, void *out, uint32_t ld, hipStream_t);
+
+// D[y][x] = sum_k Y X, X a [k][x] array with zeros from k_end to the next multiple of 64; Y [y][k] (rows) or [k][y] (columns, in `matrices` runs of y_offset columns).
+struct FfnProduct {
+  const uint16_t *x, *y;
+  uint32_t ldx, nx, ny, k, y_offset, matrices;
+  uint64_t ldy;
+  void *out[2];                                   // bf16
+  uint64_t out_stride;
+  float *partial;                                 // [splits][matrices][ny][nx]; null: out is written at once
+  uint32_t splits, split_steps;
+};
+struct FfnGradPlan { int shape; uint32_t splits, split_steps; };
+// most_splits: what the workspace has room for.
+FfnGradPlan ffn_grad_plan(uint64_t nx, uint64_t ny, uint64_t k, uint32_t matrices, uint64_t most_splits);
+hipError_t launch_ffn_grad(const FfnGradPlan &, bool columns, const FfnProduct &, hipStream_t);
+
+}  // namespace eco

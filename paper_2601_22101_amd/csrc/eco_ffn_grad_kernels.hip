@@ -1,0 +1,383 @@
+// Kernels of the gradients of the linear product and of the gated unit: the operands as bfloat16, and the two products
+//   grad_input[m][k] = sum_n G[m][n] W[n][k],   grad_weights[n][k] = sum_m G[m][n] x[m][k]
+// with G the gradient of the product's output.  x = code 2^e is exact as a bfloat16; W = code * scale is rounded to one (2^-9 of a weight, whose sum over a row of
+// grad_input averages).  Both products have the inner axis of their X operand, W or x, across memory, which the transposing reads of LDS turn.
+#include <hip/hip_runtime.h>
+
+#include <type_traits>
+
+#include "eco_device.hpp"
+#include "eco_ffn.hpp"
+#include "eco_product.hpp"
+
+namespace eco {
+namespace {
+
+// ------------------------------------------------------------------------------------------------ operands
+
+__device__ __forceinline__ float weight_scale(const FfnWeights &w, int matrix, uint32_t row, uint32_t k) {
+  const uint64_t at = static_cast<uint64_t>(row) * w.scale_row + (w.group_blocks ? k / FFN_BLOCK / w.group_blocks : 0);
+  const void *from = matrix ? w.scales[1] : w.scales[0];
+  return w.scale_bf16 ? u2f(static_cast<uint32_t>(static_cast<const uint16_t *>(from)[at]) << 16) : static_cast<const float *>(from)[at];
+}
+__device__ __forceinline__ void put_bf16x8(uint16_t *to, const float (&v)[8]) {
+  *reinterpret_cast<uint4 *>(to) = make_uint4(f32x2_to_bf16x2_rne(v[0], v[1]), f32x2_to_bf16x2_rne(v[2], v[3]), f32x2_to_bf16x2_rne(v[4], v[5]), f32x2_to_bf16x2_rne(v[6], v[7]));
+}
+__device__ __forceinline__ void fp8_values(uint2 u, float scale, float (&v)[8]) {
+  v[0] = e4m3_decode<0>(u.x); v[1] = e4m3_decode<1>(u.x); v[2] = e4m3_decode<2>(u.x); v[3] = e4m3_decode<3>(u.x);
+  v[4] = e4m3_decode<0>(u.y); v[5] = e4m3_decode<1>(u.y); v[6] = e4m3_decode<2>(u.y); v[7] = e4m3_decode<3>(u.y);
+#pragma unroll
+  for (int j = 0; j < 8; ++j) v[j] *= scale;
+}
+
+// Eight weights a thread; rows are whole sixteens of codes.
+template <int FMT>
+__global__ __launch_bounds__(256) void eco_ffn_weights_kernel(FfnWeights w, uint16_t *out, uint32_t padded_rows) {
+  const uint32_t chunks = w.dim / 8;
+  const uint64_t work = static_cast<uint64_t>(w.matrices) * padded_rows * chunks;
+  for (uint64_t i = static_cast<uint64_t>(blockIdx.x) * 256 + threadIdx.x; i < work; i += static_cast<uint64_t>(gridDim.x) * 256) {
+    const uint32_t all_row = static_cast<uint32_t>(i >> 32 ? i / chunks : static_cast<uint32_t>(i) / chunks), k = static_cast<uint32_t>(i - static_cast<uint64_t>(all_row) * chunks) * 8;
+    const int matrix = all_row >= padded_rows;
+    const uint32_t row = all_row - (matrix ? padded_rows : 0);
+    float v[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+    if (row < w.rows) {
+      const uint64_t at = static_cast<uint64_t>(row) * w.dim + k;
+      const uint8_t *from = static_cast<const uint8_t *>(matrix ? w.data[1] : w.data[0]);
+      const float scale = weight_scale(w, matrix, row, k);
+      if constexpr (FMT == FMT_FP8) fp8_values(*reinterpret_cast<const uint2 *>(from + at), scale, v);
+      else {
+        const uint32_t u = *reinterpret_cast<const uint32_t *>(from + at / 2);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] = static_cast<float>(static_cast<int32_t>(u << (28 - 4 * j)) >> 28) * scale;
+      }
+    }
+    put_bf16x8(out + i * 8, v);
+  }
+}
+
+// 8-bit rows; exact.
+__global__ __launch_bounds__(256) void eco_ffn_rows_kernel(FfnRows8 x, uint16_t *out, uint32_t padded_rows) {
+  const uint32_t chunks = x.dim / 8;
+  const uint64_t work = static_cast<uint64_t>(padded_rows) * chunks;
+  for (uint64_t i = static_cast<uint64_t>(blockIdx.x) * 256 + threadIdx.x; i < work; i += static_cast<uint64_t>(gridDim.x) * 256) {
+    const uint32_t row = static_cast<uint32_t>(i >> 32 ? i / chunks : static_cast<uint32_t>(i) / chunks), k = static_cast<uint32_t>(i - static_cast<uint64_t>(row) * chunks) * 8;
+    float v[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+    if (row < x.rows) {
+      const uint32_t byte = x.scales[static_cast<uint64_t>(row) * x.blocks + k / FFN_BLOCK];
+      fp8_values(*reinterpret_cast<const uint2 *>(x.codes + row * x.stride + k), u2f(byte ? byte << 23 : 0x00400000u), v);
+    }
+    put_bf16x8(out + i * 8, v);
+  }
+}
+
+__global__ __launch_bounds__(256) void eco_ffn_pad_kernel(const uint16_t *src, uint64_t stride, uint32_t rows, uint32_t dim, uint16_t *out, uint32_t ld) {
+  const uint32_t chunks = ld / 8;
+  const uint64_t work = static_cast<uint64_t>(rows) * chunks;
+  for (uint64_t i = static_cast<uint64_t>(blockIdx.x) * 256 + threadIdx.x; i < work; i += static_cast<uint64_t>(gridDim.x) * 256) {
+    const uint64_t row = i / chunks;
+    const uint32_t k = static_cast<uint32_t>(i - row * chunks) * 8;
+    uint32_t v[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = k + j < dim ? src[row * stride + k + j] : 0u;
+    *reinterpret_cast<uint4 *>(out + i * 8) = make_uint4(v[0] | v[1] << 16, v[2] | v[3] << 16, v[4] | v[5] << 16, v[6] | v[7] << 16);
+  }
+}
+
+// ------------------------------------------------------------------------------------------------ products
+
+struct GradArgs {
+  FfnProduct p;
+  uint32_t tiles_x, tiles_y, steps;
+};
+
+// D[y][x] = sum_k Y X.  x runs along a lane's registers, four neighbours in each group.  A workgroup goes through tiles gridDim.x apart; its loads do not stop
+// between them.
+template <bool Y_COLUMN, class T>
+__global__ __launch_bounds__(T::THREADS) void eco_ffn_grad_kernel(GradArgs a) {
+  constexpr int NI = T::NI, NJ = T::NJ, QUARTERS = KSTEP / 16, OWN = 4096;
+  __shared__ __attribute__((aligned(1024))) char smem[T::DEPTH * T::STEP_BYTES + T::WX * T::WY * OWN];
+  static_assert(sizeof smem <= 163840, "a compute unit's LDS");
+  const FfnProduct &p = a.p;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int wx = wave % T::WX * (NI * 32), wy = wave / T::WX * (NJ * 32);
+  const uint32_t all_tiles = a.tiles_x * a.tiles_y * p.matrices * p.splits, tail = p.k % KSTEP;
+  const uint64_t step_x = static_cast<uint64_t>(KSTEP) * p.ldx, step_y = Y_COLUMN ? KSTEP * p.ldy : KSTEP;
+  const uint32_t last_piece_y = (p.ny + 7) / 8 * 8 - 8;
+
+  struct Where { uint32_t x0, y0, matrix, split, first, steps; };
+  const auto where = [&](uint32_t id) {
+    uint32_t tile = xcd_run(id, all_tiles);
+    Where w;
+    const uint32_t each = a.tiles_x * a.tiles_y;
+    w.split = tile / (each * p.matrices);
+    tile -= w.split * each * p.matrices;
+    w.matrix = tile / each;
+    tile -= w.matrix * each;
+    w.y0 = tile / a.tiles_x * T::BY;
+    w.x0 = tile % a.tiles_x * T::BX;
+    w.first = w.split * p.split_steps;
+    w.steps = min(p.split_steps, a.steps - w.first);
+    return w;
+  };
+
+  // ---- the loads' place in the work
+  uint32_t load_id = blockIdx.x, load_first = 0, load_steps = 0, at_step = 0, issued = 0, place = 0;
+  uint32_t off_x[T::X_LOADS], off_y[T::Y_LOADS];
+  const uint16_t *from_x = nullptr, *from_y = nullptr;
+  const uint32_t lds0 = static_cast<uint32_t>(reinterpret_cast<uintptr_t>((lds_char *)smem));
+  const auto load_tile = [&]() {
+    const Where w = where(load_id);
+#pragma unroll
+    for (int i = 0; i < T::X_LOADS; ++i) {
+      uint32_t n, k;
+      column_piece<T::BX>(threadIdx.x + i * T::THREADS, n, k);
+      off_x[i] = (k * p.ldx + min(w.x0 + n, p.nx - 8) - w.x0) * 2;
+    }
+#pragma unroll
+    for (int i = 0; i < T::Y_LOADS; ++i) {
+      uint32_t n, k;
+      if constexpr (Y_COLUMN) {
+        column_piece<T::BY>(threadIdx.x + i * T::THREADS, n, k);
+        off_y[i] = static_cast<uint32_t>(k * p.ldy + min(w.y0 + n, last_piece_y) - w.y0) * 2;
+      } else {
+        row_piece(threadIdx.x + i * T::THREADS, n, k);
+        off_y[i] = static_cast<uint32_t>((min(w.y0 + n, p.ny - 1) - w.y0) * p.ldy + k) * 2;
+      }
+    }
+    load_first = w.first;
+    load_steps = w.steps;
+    from_x = p.x + w.x0 + w.first * step_x;
+    from_y = p.y + static_cast<uint64_t>(w.matrix) * p.y_offset + (Y_COLUMN ? w.y0 : w.y0 * p.ldy) + w.first * step_y;
+    at_step = 0;
+  };
+  const auto issue = [&]() {
+    if (load_id >= all_tiles) return;
+    const uint32_t lds = lds0 + place * T::STEP_BYTES + wave * 1024;
+    // the last step's end: X has zeros there, Y repeats what is there of the row, or the last row
+    const bool end = tail && load_first + at_step + 1 == a.steps;
+#pragma unroll
+    for (int i = 0; i < T::X_LOADS; ++i) load_to_lds(lds + i * T::THREADS * 16, from_x, off_x[i]);
+#pragma unroll
+    for (int i = 0; i < T::Y_LOADS; ++i) {
+      uint32_t off = off_y[i];
+      if (end) {
+        uint32_t n, k;
+        if constexpr (Y_COLUMN) {
+          column_piece<T::BY>(threadIdx.x + i * T::THREADS, n, k);
+          if (k >= tail) off -= static_cast<uint32_t>((k - (tail - 1)) * p.ldy) * 2;
+        } else {
+          row_piece(threadIdx.x + i * T::THREADS, n, k);
+          if (k >= tail) off -= k * 2;
+        }
+      }
+      load_to_lds(lds + T::X_BYTES + i * T::THREADS * 16, from_y, off);
+    }
+    place = place + 1 == T::DEPTH ? 0 : place + 1;
+    ++issued;
+    if (++at_step == load_steps) {
+      load_id += gridDim.x;
+      if (load_id < all_tiles) load_tile();
+      return;
+    }
+    from_x += step_x;
+    from_y += step_y;
+  };
+
+  // ---- the products' place
+  bf16x8 fx[2][NI], fy[2][NJ];                                 // the quarter of a step at hand and the next one
+  const auto read = [&](const lds_char *step, int kk, bf16x8 (&x)[NI], bf16x8 (&y)[NJ]) {
+#pragma unroll
+    for (int j = 0; j < NJ; ++j) y[j] = fragment<T::BY, Y_COLUMN>(step + T::X_BYTES, wy + 32 * j, kk, lane);
+#pragma unroll
+    for (int i = 0; i < NI; ++i) x[i] = fragment<T::BX, true>(step, wx + 32 * i, kk, lane);
+  };
+  uint32_t at = 0, done = 0;
+  const lds_char *step = (const lds_char *)smem;
+  if (a.steps) {                                               // (0: no rows, and gradients of zero)
+    load_tile();
+    for (int i = 0; i < T::DEPTH; ++i) issue();
+    if (issued == T::DEPTH) wait_loads<(T::DEPTH - 1) * T::LOADS>();
+    else wait_loads<0>();
+    barrier();
+    read(step, 0, fx[0], fy[0]);
+  }
+  for (uint32_t id = blockIdx.x; id < all_tiles; id += gridDim.x) {
+    const Where w = where(id);
+    f32x16 acc[NI][NJ] = {};
+    for (uint32_t s = 0; s < w.steps; ++s) {
+#pragma unroll
+      for (int kk = 0; kk < QUARTERS - 1; ++kk) {
+        read(step, kk + 1, fx[(kk + 1) & 1], fy[(kk + 1) & 1]);
+#pragma unroll
+        for (int i = 0; i < NI; ++i)
+#pragma unroll
+          for (int j = 0; j < NJ; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fx[kk & 1][i], fy[kk & 1][j], acc[i][j], 0, 0, 0);
+        constexpr int READS = NI * 2 + NJ * (Y_COLUMN ? 2 : 1), EACH = (READS + NI * NJ - 1) / (NI * NJ);
+#pragma unroll
+        for (int q = 0; q < NI * NJ; ++q) {
+          __builtin_amdgcn_sched_group_barrier(0x100, EACH, 0);
+          __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+        }
+      }
+      // the next step is there once every wave's loads of it are, and this one's place is free once every wave has read it
+      if (issued - done >= T::DEPTH) wait_all_but<(T::DEPTH - 2) * T::LOADS>();
+      else wait_all_but<0>();
+      barrier();
+      ++done;
+      at = at + 1 == T::DEPTH ? 0 : at + 1;
+      step = (const lds_char *)smem + at * T::STEP_BYTES;
+      read(step, 0, fx[0], fy[0]);                             // (after the last step nothing uses these)
+#pragma unroll
+      for (int i = 0; i < NI; ++i) {
+#pragma unroll
+        for (int j = 0; j < NJ; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fx[(QUARTERS - 1) & 1][i], fy[(QUARTERS - 1) & 1][j], acc[i][j], 0, 0, 0);
+        if (i == 0) {
+          __builtin_amdgcn_sched_barrier(0);
+          issue();
+          __builtin_amdgcn_sched_barrier(0);
+        }
+      }
+    }
+
+    // acc[i][j][r]: x = x0 + wx + 32 i + (r & 3) + 8 (r >> 2) + 4 (end_lane >> 5), y = y0 + wy + 32 j + (end_lane & 31)
+    int end_lane = lane;
+    asm volatile("" : "+v"(end_lane));
+    lds_char *const own = (lds_char *)smem + T::DEPTH * T::STEP_BYTES + wave * OWN;
+    if (p.partial) {
+      float *const out = p.partial + (static_cast<uint64_t>(w.split) * p.matrices + w.matrix) * p.ny * p.nx;
+#pragma unroll
+      for (int j = 0; j < NJ; ++j)
+#pragma unroll
+        for (int i = 0; i < NI; ++i) {
+          put_f32(own, end_lane, acc[i][j]);
+          eco::take<8>(own, end_lane, [&](uint32_t row, uint32_t piece, uint4 v) {
+            const uint32_t y = w.y0 + wy + 32 * j + row, x = w.x0 + wx + 32 * i + 4 * piece;
+            if (y < p.ny && x < p.nx) *reinterpret_cast<uint4 *>(out + static_cast<uint64_t>(y) * p.nx + x) = v;      // nx is whole sixteens
+          });
+        }
+    } else {
+      uint16_t *const out = static_cast<uint16_t *>(w.matrix ? p.out[1] : p.out[0]);
+      const bool whole = p.out_stride % 8 == 0 && (reinterpret_cast<uintptr_t>(out) & 15) == 0;
+      const auto two_blocks = [&](int j, int i0, auto wide) {
+        constexpr int WIDE = decltype(wide)::value;
+#pragma unroll
+        for (int i = 0; i < WIDE; ++i)
+#pragma unroll
+          for (int q = 0; q < 4; ++q)
+            put_bf16<4 * WIDE>(own, end_lane, i, q, f32x2_to_bf16x2_rne(acc[i0 + i][j][4 * q], acc[i0 + i][j][4 * q + 1]),
+                               f32x2_to_bf16x2_rne(acc[i0 + i][j][4 * q + 2], acc[i0 + i][j][4 * q + 3]));
+        eco::take<4 * WIDE>(own, end_lane, [&](uint32_t row, uint32_t piece, uint4 v) {
+          const uint32_t y = w.y0 + wy + 32 * j + row, x = w.x0 + wx + 32 * i0 + 8 * piece;
+          if (y >= p.ny || x >= p.nx) return;
+          uint16_t *to = out + y * p.out_stride + x;
+          if (whole) *reinterpret_cast<uint4 *>(to) = v;
+          else {
+            const uint32_t h[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+            for (int e = 0; e < 8; ++e) to[e] = static_cast<uint16_t>(h[e / 2] >> (16 * (e & 1)));
+          }
+        });
+      };
+#pragma unroll
+      for (int j = 0; j < NJ; ++j)
+#pragma unroll
+        for (int i0 = 0; i0 < NI; i0 += 2)
+          if (i0 + 1 < NI) two_blocks(j, i0, std::integral_constant<int, 2>{});
+          else two_blocks(j, i0, std::integral_constant<int, 1>{});
+    }
+  }
+}
+
+// Parts of the sums, added in their order and rounded: eight neighbours a thread.
+__global__ __launch_bounds__(256) void eco_ffn_grad_join_kernel(FfnProduct p) {
+  const uint64_t each = static_cast<uint64_t>(p.ny) * p.nx, all = each * p.matrices;
+  const uint32_t chunks = p.nx / 8;
+  for (uint64_t i = static_cast<uint64_t>(blockIdx.x) * 256 + threadIdx.x; i < all / 8; i += static_cast<uint64_t>(gridDim.x) * 256) {
+    float v[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+    for (uint32_t s = 0; s < p.splits; ++s) {
+      const float4 *from = reinterpret_cast<const float4 *>(p.partial + s * all + i * 8);
+      const float4 u = from[0], t = from[1];
+      v[0] += u.x; v[1] += u.y; v[2] += u.z; v[3] += u.w;
+      v[4] += t.x; v[5] += t.y; v[6] += t.z; v[7] += t.w;
+    }
+    const uint64_t matrix = i >= each / 8, in = i - matrix * (each / 8), y = in / chunks, x = (in - y * chunks) * 8;
+    uint16_t *to = static_cast<uint16_t *>(matrix ? p.out[1] : p.out[0]) + y * p.out_stride + x;
+    const uint32_t w[4] = {f32x2_to_bf16x2_rne(v[0], v[1]), f32x2_to_bf16x2_rne(v[2], v[3]), f32x2_to_bf16x2_rne(v[4], v[5]), f32x2_to_bf16x2_rne(v[6], v[7])};
+    if ((reinterpret_cast<uintptr_t>(to) & 15) == 0) *reinterpret_cast<uint4 *>(to) = make_uint4(w[0], w[1], w[2], w[3]);
+    else
+#pragma unroll
+      for (int e = 0; e < 8; ++e) to[e] = static_cast<uint16_t>(w[e / 2] >> (16 * (e & 1)));
+  }
+}
+
+using Large = Tile<256, 256, 2, 4, 2>;
+using Large192 = Tile<192, 256, 2, 4, 2>;
+using Medium = Tile<128, 128, 2, 2, 2>;
+constexpr uint64_t UNITS = 256;
+
+uint64_t ceil_div(uint64_t a, uint64_t b) { return (a + b - 1) / b; }
+uint32_t grid_of(uint64_t work) { const uint64_t g = ceil_div(work, 256); return static_cast<uint32_t>(g < 1 ? 1 : g < 8192 ? g : 8192); }
+
+struct Shape { uint32_t x, y, at_once; };
+Shape shape_of(int shape) { return shape == 2 ? Shape{256, 256, 1} : shape == 1 ? Shape{192, 256, 1} : Shape{128, 128, 2}; }
+
+template <bool Y_COLUMN, class T>
+hipError_t launch_grad_tiles(const FfnProduct &p, uint32_t at_once, hipStream_t s) {
+  const GradArgs a = {p, static_cast<uint32_t>(ceil_div(p.nx, T::BX)), static_cast<uint32_t>(ceil_div(p.ny, T::BY)), static_cast<uint32_t>(ceil_div(p.k, KSTEP))};
+  const uint64_t tiles = static_cast<uint64_t>(a.tiles_x) * a.tiles_y * p.matrices * p.splits;
+  eco_ffn_grad_kernel<Y_COLUMN, T><<<static_cast<uint32_t>(tiles < UNITS * at_once ? tiles : UNITS * at_once), T::THREADS, 0, s>>>(a);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_ffn_weights_bf16(const FfnWeights &w, void *out, uint32_t padded_rows, hipStream_t s) {
+  const uint32_t grid = grid_of(static_cast<uint64_t>(w.matrices) * padded_rows * (w.dim / 8));
+  if (w.fmt == FMT_FP8) eco_ffn_weights_kernel<FMT_FP8><<<grid, 256, 0, s>>>(w, static_cast<uint16_t *>(out), padded_rows);
+  else eco_ffn_weights_kernel<FMT_INT4><<<grid, 256, 0, s>>>(w, static_cast<uint16_t *>(out), padded_rows);
+  return hipGetLastError();
+}
+hipError_t launch_ffn_rows_bf16(const FfnRows8 &x, void *out, uint32_t padded_rows, hipStream_t s) {
+  if (padded_rows == 0) return hipSuccess;
+  eco_ffn_rows_kernel<<<grid_of(static_cast<uint64_t>(padded_rows) * (x.dim / 8)), 256, 0, s>>>(x, static_cast<uint16_t *>(out), padded_rows);
+  return hipGetLastError();
+}
+hipError_t launch_ffn_pad(const void *src, uint64_t src_stride, uint32_t rows, uint32_t dim, void *out, uint32_t ld, hipStream_t s) {
+  if (rows == 0) return hipSuccess;
+  eco_ffn_pad_kernel<<<grid_of(static_cast<uint64_t>(rows) * (ld / 8)), 256, 0, s>>>(static_cast<const uint16_t *>(src), src_stride, rows, dim, static_cast<uint16_t *>(out), ld);
+  return hipGetLastError();
+}
+
+FfnGradPlan ffn_grad_plan(uint64_t nx, uint64_t ny, uint64_t k, uint32_t matrices, uint64_t most_splits) {
+  const uint64_t steps = ceil_div(k, KSTEP);
+  FfnGradPlan best = {0, 1, static_cast<uint32_t>(steps)};
+  double least = 0;
+  for (int shape = 0; shape <= 2; ++shape) {
+    const Shape t = shape_of(shape);
+    const uint64_t tiles = ceil_div(nx, t.x) * ceil_div(ny, t.y) * matrices;
+    for (uint64_t n = 1; n == 1 || (n <= most_splits && n * 4 <= steps); ++n) {
+      // in steps of a 256 x 256 tile: whole rounds of tiles, with what a tile costs beside its steps, and the parts' way through memory
+      const double each = shape == 0 ? 0.62 : shape == 1 ? 0.78 : 1.0;      // (two of the small ones at once on a compute unit)
+      const double rounds = static_cast<double>(ceil_div(tiles * n, UNITS * t.at_once));
+      const double cost = rounds * (static_cast<double>(ceil_div(steps, n)) * each + 8 * each) + (n > 1 ? 4 + 0.5 * static_cast<double>(n * matrices * nx * ny) * 10 / 5e6 : 0);
+      if ((shape == 0 && n == 1) || cost < 0.98 * least) {
+        least = cost;
+        const uint64_t each_steps = ceil_div(steps, n);
+        best = {shape, static_cast<uint32_t>(each_steps ? ceil_div(steps, each_steps) : 1), static_cast<uint32_t>(each_steps)};
+      }
+    }
+  }
+  return best;
+}
+
+hipError_t launch_ffn_grad(const FfnGradPlan &plan, bool columns, const FfnProduct &p, hipStream_t s) {
+  if (p.ny == 0) return hipSuccess;
+  hipError_t e;
+  if (columns) e = plan.shape == 2 ? launch_grad_tiles<true, Large>(p, 1, s) : plan.shape == 1 ? launch_grad_tiles<true, Large192>(p, 1, s) : launch_grad_tiles<true, Medium>(p, 2, s);
+  else e = plan.shape == 2 ? launch_grad_tiles<false, Large>(p, 1, s) : plan.shape == 1 ? launch_grad_tiles<false, Large192>(p, 1, s) : launch_grad_tiles<false, Medium>(p, 2, s);
+  if (e != hipSuccess || !p.partial) return e;
+  eco_ffn_grad_join_kernel<<<grid_of(static_cast<uint64_t>(p.matrices) * p.ny * (p.nx / 8)), 256, 0, s>>>(p);
+  return hipGetLastError();
+}
+
+}  // namespace eco

@@ -558,3 +558,265 @@ class HeadLoss:
         h.grad_ce, h.grad_kd = (g.data_ptr() if g is not None else None for g in (grad_ce, grad_kd))
         eco.eco_head_loss_backward(h, self.workspace, self.workspace_bytes, stream)
         return self.grad_hidden, self.grad_weights
+
+
+class _RowUnit:
+    """What the units of a layer's feed-forward half have in common: rows of tensors that a call brings, the current stream, and one workspace."""
+
+    def _rows(self, n: int) -> None:
+        if n > self.rows:
+            raise ValueError(f"{n} rows: this one was made for up to {self.rows}")
+
+    def _takes(self, name: str, t: torch.Tensor, n: int, columns: int, dtype: torch.dtype) -> int:
+        """The stride of an input's rows, after its checks."""
+        if t is None or t.shape != (n, columns) or t.dtype != dtype or t.device != self.device:
+            raise ValueError(f"{name}: {n} x {columns} of {dtype} on {self.device} is needed")
+        if n == 0:
+            return 0
+        row, column = t.stride()
+        if column != 1 and columns > 1:
+            raise ValueError(f"{name}: rows must be contiguous")
+        if n == 1:
+            return 0
+        if row < columns:
+            raise ValueError(f"{name}: rows must not overlap")
+        return row
+
+    def _takes_rows8(self, codes: torch.Tensor, scales: torch.Tensor, columns: int) -> int:
+        n = codes.shape[0] if codes is not None and codes.dim() == 2 else -1
+        stride = self._takes("codes", codes, n, columns, torch.uint8)
+        blocks = -(-columns // 128)
+        if self._takes("scales", scales, n, blocks, torch.uint8) not in (0, blocks):
+            raise ValueError("scales: packed rows are needed")
+        self._rows(n)
+        return stride
+
+    def _weights(self, name: str, weights: torch.Tensor, scales: torch.Tensor, columns: int, rows: int) -> None:
+        if not weights.is_cuda:
+            raise ValueError(f"{name}: memory of a GPU is needed")
+        need = rows * columns // (2 if self.fmt == eco.ECO_FMT_INT4 else 1)
+        if weights.dtype != torch.uint8 or weights.numel() < need or not weights.is_contiguous():
+            raise ValueError(f"{name}: {need} contiguous bytes of codes are needed")
+        if scales is None or not scales.is_contiguous() or self.group_size <= 0 or scales.numel() < -(-rows * columns // self.group_size):
+            raise ValueError(f"{name}: one scale for each scale group is needed, contiguous")
+        if scales.device != weights.device or scales.dtype not in _DTYPE:
+            raise ValueError(f"{name}: scales of {' or '.join(map(str, _DTYPE))} on {weights.device} are needed")
+
+    def _run(self, call, descriptor, stream, used, workspace=True) -> None:
+        """`used`: what the call reads or writes; the allocator is told of a stream that is not the current one."""
+        if stream is not None:
+            s = stream
+            if isinstance(s, int):
+                s = torch.cuda.ExternalStream(s) if s else torch.cuda.default_stream(self.device)
+            for t in (*used, self.workspace):
+                if t is not None:
+                    t.record_stream(s)
+        args = (descriptor, self.workspace, self.workspace_bytes, stream) if workspace else (descriptor, stream)
+        if torch.cuda.current_device() == self.device.index:
+            call(*args)
+        else:
+            with torch.cuda.device(self.device):
+                call(*args)
+
+    def _make_workspace(self, sizes) -> None:
+        self.workspace_bytes = max(sizes)
+        self.workspace = torch.empty(self.workspace_bytes, dtype=torch.uint8, device=self.device) if self.workspace_bytes else None
+
+
+def quantize_rows(x: torch.Tensor, codes: Optional[torch.Tensor] = None, scales: Optional[torch.Tensor] = None, stream=None):
+    """(codes, scales) of the rows of ``x`` (fp32 or bf16): 8-bit rows as RowNorm and GatedUnit make them and Linear and GatedUnit take them.
+    Both may be given, as uint8 arrays to write to; else they are new."""
+    if x.dim() != 2 or x.dtype not in _DTYPE or not x.is_cuda:
+        raise ValueError("x: rows of fp32 or bf16 in a GPU's memory are needed")
+    n, columns = x.shape
+    if n and columns > 1 and x.stride(1) != 1 or n > 1 and x.stride(0) < columns:
+        raise ValueError("x: rows must be contiguous and must not overlap")
+    blocks = -(-columns // 128)
+    codes = torch.empty(n, columns, dtype=torch.uint8, device=x.device) if codes is None else codes
+    scales = torch.empty(n, blocks, dtype=torch.uint8, device=x.device) if scales is None else scales
+    for name, t, width in (("codes", codes, columns), ("scales", scales, blocks)):
+        if t.shape != (n, width) or t.dtype != torch.uint8 or t.device != x.device or n and width > 1 and t.stride(1) != 1 or n > 1 and t.stride(0) < width:
+            raise ValueError(f"{name}: {n} x {width} of uint8 on {x.device} with contiguous rows is needed")
+    if n > 1 and scales.stride(0) != blocks:
+        raise ValueError("scales: packed rows are needed")
+    if stream is not None:
+        s = stream if not isinstance(stream, int) else torch.cuda.ExternalStream(stream) if stream else torch.cuda.default_stream(x.device)
+        for t in (x, codes, scales):
+            t.record_stream(s)
+    with torch.cuda.device(x.device):
+        eco.eco_rows_quantize(x, _DTYPE[x.dtype], n, columns, x.stride(0) if n > 1 else 0, codes, codes.stride(0) if n > 1 else 0, scales, stream)
+    return codes, scales
+
+
+class RowNorm(_RowUnit):
+    """Root-mean-square norm with the residual's addition, its rows leaving in 8 bits or, with ``quantize=False``, in ``dtype`` (eco_norm, eco_norm_backward).
+
+    Made for up to ``rows`` rows; a call brings as many or fewer.  The tensors that forward() and backward() return are the object's own, or views of them, and are
+    written again by its next call; both run on the current stream, or on ``stream``.  A call that refuses its arguments (ValueError) leaves the object as it was.
+    """
+
+    def __init__(self, rows: int, dim: int, *, gain: Optional[torch.Tensor] = None, dtype: torch.dtype = torch.bfloat16, eps: float = 1e-6, residual: bool = False,
+                 quantize: bool = True, training: bool = False, grad_gain_dtype: torch.dtype = torch.bfloat16, device=None):
+        self.device = dev = gain.device if gain is not None else torch.device("cuda", torch.cuda.current_device()) if device is None else torch.device(device)
+        if dev.type != "cuda" or dev.index is None:
+            raise ValueError("gain: memory of a GPU is needed")
+        if dtype not in _DTYPE or gain is not None and (gain.shape != (dim,) or gain.dtype not in _DTYPE or not gain.is_contiguous()):
+            raise ValueError(f"dtype and gain: {' or '.join(map(str, _DTYPE))}, and {dim} contiguous gains, are needed")
+        self.rows, self.dim, self.dtype, self.gain, self.has_residual, self.quantize, self.training = rows, dim, dtype, gain, residual, quantize, training
+        self.out = torch.empty(rows, dim, dtype=torch.uint8 if quantize else dtype, device=dev)
+        self.scales = torch.empty(rows, -(-dim // 128), dtype=torch.uint8, device=dev) if quantize else None
+        self.sum = torch.empty(rows, dim, dtype=dtype, device=dev) if residual else None
+        self.rstd = torch.empty(rows, dtype=torch.float32, device=dev) if training else None
+        self.grad_input = torch.empty(rows, dim, dtype=dtype, device=dev) if training else None
+        self.grad_gain = torch.empty(dim, dtype=grad_gain_dtype, device=dev) if training and gain is not None else None
+        self.norm = eco.make_norm(rows=rows, dim=dim, eps=eps, dtype=_DTYPE[dtype], gain_dtype=_DTYPE[gain.dtype] if gain is not None else eco.ECO_DT_BF16,
+                                  grad_gain_dtype=_DTYPE[grad_gain_dtype], gain=gain, out=self.out, scales=self.scales, sum=self.sum, rstd=self.rstd,
+                                  grad_input=self.grad_input, grad_gain=self.grad_gain)
+        self._make_workspace([eco.eco_norm_backward_workspace(self.norm) if training else 0])
+        self._inputs = None                             # of the last forward()
+
+    def forward(self, x: torch.Tensor, residual: Optional[torch.Tensor] = None, stream=None):
+        """(out, scales, sum): the normalised rows, their scale bytes (None unless they are quantized), and the residual stream (None without a residual)."""
+        n = x.shape[0] if x is not None and x.dim() == 2 else -1
+        stride = self._takes("x", x, n, self.dim, self.dtype)
+        if self.has_residual:
+            residual_stride = self._takes("residual", residual, n, self.dim, self.dtype)
+        elif residual is not None:
+            raise ValueError("residual: this RowNorm was made without residual=True")
+        self._rows(n)
+        d = self.norm
+        self._inputs = None
+        d.rows, d.input, d.input_stride = n, x.data_ptr(), stride
+        if self.has_residual:
+            d.residual, d.residual_stride = residual.data_ptr(), residual_stride
+        self._run(eco.eco_norm, d, stream, () if stream is None else (x, residual, self.gain, self.out, self.scales, self.sum, self.rstd), workspace=False)
+        self._inputs = x, n
+        if n == self.rows:
+            return self.out, self.scales, self.sum
+        return self.out[:n], self.scales[:n] if self.quantize else None, self.sum[:n] if self.has_residual else None
+
+    def backward(self, grad_out: torch.Tensor, grad_sum: Optional[torch.Tensor] = None, stream=None):
+        """(grad_input, grad_gain) for the rows of the last forward(): grad_input is that of x and of the residual alike; grad_sum is the gradient of what else reads
+        the residual stream."""
+        if not self.training:
+            raise RuntimeError("this RowNorm was made without training=True")
+        if self._inputs is None:
+            raise RuntimeError("backward() needs a forward() before it")
+        x, n = self._inputs
+        stride = self._takes("grad_out", grad_out, n, self.dim, self.dtype)
+        sum_stride = self._takes("grad_sum", grad_sum, n, self.dim, self.dtype) if grad_sum is not None else 0
+        d = self.norm
+        d.grad_out, d.grad_out_stride = grad_out.data_ptr(), stride
+        d.grad_sum, d.grad_sum_stride = None if grad_sum is None else grad_sum.data_ptr(), sum_stride
+        self._run(eco.eco_norm_backward, d, stream, () if stream is None else (x, grad_out, grad_sum, self.gain, self.sum, self.rstd, self.grad_input, self.grad_gain))
+        return self.grad_input if n == self.rows else self.grad_input[:n], self.grad_gain
+
+
+class Linear(_RowUnit):
+    """The product of 8-bit rows with quantized weights, and its gradients (eco_linear, eco_linear_backward).
+
+    ``weights`` (out_dim x in_dim codes in the storage format ``fmt``) and ``scales`` are the arrays that the step updates in place; grad_weights is the bf16 gradient that
+    it reads.  Rows, streams and returned tensors as of RowNorm.
+    """
+
+    def __init__(self, rows: int, in_dim: int, out_dim: int, *, weights: torch.Tensor, scales: torch.Tensor, fmt: int = eco.ECO_FMT_FP8_E4M3, group_size: int = 128,
+                 out_dtype: torch.dtype = torch.bfloat16, training: bool = False):
+        self.rows, self.in_dim, self.out_dim, self.fmt, self.group_size, self.out_dtype, self.training = rows, in_dim, out_dim, fmt, group_size, out_dtype, training
+        self.device = dev = weights.device
+        self._weights("weights", weights, scales, in_dim, out_dim)
+        if out_dtype not in _DTYPE:
+            raise ValueError(f"out_dtype: {' or '.join(map(str, _DTYPE))} is needed")
+        self.weights, self.scales = weights, scales
+        self.out = torch.empty(rows, out_dim, dtype=out_dtype, device=dev)
+        self.grad_input = torch.empty(rows, in_dim, dtype=torch.bfloat16, device=dev) if training else None
+        self.grad_weights = torch.empty(out_dim, in_dim, dtype=torch.bfloat16, device=dev) if training else None
+        # the workspace's size is asked for with an input in place, which the descriptor needs; a call brings its own
+        self.linear = eco.make_linear(rows=rows, in_dim=in_dim, out_dim=out_dim, group_size=group_size, fmt=fmt, scale_dtype=_DTYPE[scales.dtype], out_dtype=_DTYPE[out_dtype],
+                                      codes=weights, code_scales=scales, weights=weights, scales=scales, out=self.out, grad_input=self.grad_input,
+                                      grad_weights=self.grad_weights)
+        self._make_workspace([eco.eco_linear_workspace(self.linear, b) for b in ([False, True] if training else [False])])
+        self.linear.codes = self.linear.code_scales = None
+        self._inputs = None
+
+    def forward(self, codes: torch.Tensor, scales: torch.Tensor, add: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+        """The product of the rows, plus ``add`` (of the output's type) where it is given."""
+        stride = self._takes_rows8(codes, scales, self.in_dim)
+        n = codes.shape[0]
+        add_stride = self._takes("add", add, n, self.out_dim, self.out_dtype) if add is not None else 0
+        d = self.linear
+        self._inputs = None
+        d.rows, d.codes, d.code_scales, d.codes_stride = n, codes.data_ptr(), scales.data_ptr(), stride
+        d.add, d.add_stride = None if add is None else add.data_ptr(), add_stride
+        self._run(eco.eco_linear, d, stream, () if stream is None else (codes, scales, add, self.weights, self.scales, self.out))
+        self._inputs = codes, scales, n
+        return self.out if n == self.rows else self.out[:n]
+
+    def backward(self, grad_out: torch.Tensor, stream=None):
+        """(grad_input, grad_weights) for the rows of the last forward(), from dL/d(its result) in bf16."""
+        if not self.training:
+            raise RuntimeError("this Linear was made without training=True")
+        if self._inputs is None:
+            raise RuntimeError("backward() needs a forward() before it")
+        codes, scales, n = self._inputs
+        stride = self._takes("grad_out", grad_out, n, self.out_dim, torch.bfloat16)
+        d = self.linear
+        d.grad_out, d.grad_out_stride = grad_out.data_ptr(), stride
+        self._run(eco.eco_linear_backward, d, stream, () if stream is None else (codes, scales, grad_out, self.weights, self.scales, self.grad_input, self.grad_weights))
+        return self.grad_input if n == self.rows else self.grad_input[:n], self.grad_weights
+
+
+class GatedUnit(_RowUnit):
+    """act(x gate^T) * (x up^T) of 8-bit rows as 8-bit rows, and its gradients (eco_gated, eco_gated_backward).
+
+    ``gate`` and ``up`` (width x in_dim codes in the storage format ``fmt``) with their scales are the arrays that the step updates in place; ``act`` is "silu" or "gelu" (its
+    tanh form).  Rows, streams and returned tensors as of RowNorm.
+    """
+
+    ACTS = {"silu": eco.ECO_ACT_SILU, "gelu": eco.ECO_ACT_GELU}
+
+    def __init__(self, rows: int, in_dim: int, width: int, *, gate: torch.Tensor, gate_scales: torch.Tensor, up: torch.Tensor, up_scales: torch.Tensor,
+                 fmt: int = eco.ECO_FMT_FP8_E4M3, group_size: int = 128, act: str = "silu", training: bool = False):
+        self.rows, self.in_dim, self.width, self.fmt, self.group_size, self.training = rows, in_dim, width, fmt, group_size, training
+        self.device = dev = gate.device
+        self._weights("gate", gate, gate_scales, in_dim, width)
+        self._weights("up", up, up_scales, in_dim, width)
+        if up.device != dev or up_scales.dtype != gate_scales.dtype:
+            raise ValueError("gate and up: one device and one type of scales are needed")
+        if act not in self.ACTS:
+            raise ValueError(f"act: {' or '.join(self.ACTS)} is needed")
+        self.gate, self.gate_scales, self.up, self.up_scales = gate, gate_scales, up, up_scales
+        bf16 = lambda *shape: torch.empty(*shape, dtype=torch.bfloat16, device=dev) if training else None     # noqa: E731
+        self.out = torch.empty(rows, width, dtype=torch.uint8, device=dev)
+        self.scales = torch.empty(rows, -(-width // 128), dtype=torch.uint8, device=dev)
+        self.grad_input, self.grad_gate, self.grad_up = bf16(rows, in_dim), bf16(width, in_dim), bf16(width, in_dim)
+        self.gated = eco.make_gated(rows=rows, in_dim=in_dim, width=width, group_size=group_size, fmt=fmt, scale_dtype=_DTYPE[gate_scales.dtype], act=self.ACTS[act],
+                                    codes=gate, code_scales=gate_scales, gate=gate, gate_scales=gate_scales, up=up, up_scales=up_scales, out=self.out,
+                                    out_scales=self.scales, grad_input=self.grad_input, grad_gate=self.grad_gate, grad_up=self.grad_up)
+        self._make_workspace([eco.eco_gated_workspace(self.gated, b) for b in ([False, True] if training else [False])])
+        self.gated.codes = self.gated.code_scales = None
+        self._inputs = None
+
+    def forward(self, codes: torch.Tensor, scales: torch.Tensor, stream=None):
+        """(codes, scales) of the unit's rows."""
+        stride = self._takes_rows8(codes, scales, self.in_dim)
+        n = codes.shape[0]
+        d = self.gated
+        self._inputs = None
+        d.rows, d.codes, d.code_scales, d.codes_stride = n, codes.data_ptr(), scales.data_ptr(), stride
+        self._run(eco.eco_gated, d, stream, () if stream is None else (codes, scales, self.gate, self.gate_scales, self.up, self.up_scales, self.out, self.scales))
+        self._inputs = codes, scales, n
+        return (self.out, self.scales) if n == self.rows else (self.out[:n], self.scales[:n])
+
+    def backward(self, grad_out: torch.Tensor, stream=None):
+        """(grad_input, grad_gate, grad_up) for the rows of the last forward(), from dL/d(its result) in bf16."""
+        if not self.training:
+            raise RuntimeError("this GatedUnit was made without training=True")
+        if self._inputs is None:
+            raise RuntimeError("backward() needs a forward() before it")
+        codes, scales, n = self._inputs
+        stride = self._takes("grad_out", grad_out, n, self.width, torch.bfloat16)
+        d = self.gated
+        d.grad_out, d.grad_out_stride = grad_out.data_ptr(), stride
+        self._run(eco.eco_gated_backward, d, stream, () if stream is None else (codes, scales, grad_out, self.gate, self.gate_scales, self.up, self.up_scales, self.grad_input,
+                                                                             self.grad_gate, self.grad_up))
+        return self.grad_input if n == self.rows else self.grad_input[:n], self.grad_gate, self.grad_up
