@@ -70,8 +70,8 @@ struct FfnOut {
 enum : int { FFN_LINEAR = 0, FFN_GATED = 1, FFN_GATED_BACK = 2 };
 
 // Tiles of an 8-bit product: rows of x to a tile; 0: the kernel for few rows, which takes weights as they are stored.
-struct FfnPlan { int end, rows_tile, width_tile; uint32_t splits, split_steps; };
-FfnPlan ffn_plan(int end, const FfnWeights &, uint64_t rows);
+struct FfnPlan { int end, rows_tile, width_tile; uint32_t splits, split_steps; bool exact; };
+FfnPlan ffn_plan(int end, const FfnWeights &, uint64_t rows, bool exact);      // exact: sums for an output in fp32
 hipError_t launch_ffn(const FfnPlan &, const FfnRows8 &, const FfnWeights &, const FfnOut &, hipStream_t);
 hipError_t launch_ffn_join(const FfnOut &, uint32_t rows, uint32_t width, hipStream_t);
 // INT4 codes as the E4M3 codes of the same values (one matrix).

@@ -151,7 +151,7 @@ struct Forward {
 };
 // MOST: room for any call with up to as many rows, whatever its plan.
 enum Room { EXACT, MOST };
-Forward forward_of(const Unit &u, int end, Room room, Places &p) {
+Forward forward_of(const Unit &u, int end, Room room, Places &p, bool exact = false) {
   Forward f;
   std::memset(&f, 0, sizeof f);
   if (room == MOST) {
@@ -161,7 +161,7 @@ Forward forward_of(const Unit &u, int end, Room room, Places &p) {
     if (end == eco::FFN_LINEAR) (void)p.take(4 * (all < eco::FFN_MOST_PARTIAL ? all : eco::FFN_MOST_PARTIAL));
     return f;
   }
-  f.plan = eco::ffn_plan(end, weights_of(u), u.rows);
+  f.plan = eco::ffn_plan(end, weights_of(u), u.rows, exact);
   f.expands = u.fmt == ECO_FMT_INT4 && f.plan.rows_tile && u.rows;
   if (f.expands)
     for (uint32_t m = 0; m < u.matrices; ++m) f.expanded[m] = p.take(u.width * u.dim);
@@ -376,7 +376,7 @@ eco_status_t eco_linear(const eco_linear_t *l, void *workspace, size_t workspace
   if (l->add) CHECK(check_rows("linear", "add", l->add, l->rows, l->add_stride, l->out_dim, size));
   Places p;
   const Unit u = unit_of(l);
-  const Forward f = forward_of(u, eco::FFN_LINEAR, EXACT, p);
+  const Forward f = forward_of(u, eco::FFN_LINEAR, EXACT, p, l->out_dtype == ECO_DT_FP32);
   CHECK(check_workspace("linear", workspace, workspace_bytes, p.bytes));
   (void)hipGetLastError();
   if (l->rows == 0) return ECO_OK;

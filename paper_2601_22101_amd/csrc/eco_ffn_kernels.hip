@@ -18,11 +18,10 @@ namespace {
 
 typedef int i32x4 __attribute__((ext_vector_type(4)));
 typedef int i32x8 __attribute__((ext_vector_type(8)));
-typedef __attribute__((address_space(3))) float lds_float;
 typedef __attribute__((address_space(3))) uint32_t lds_uint;
 
 constexpr float LOG2E = 1.44269504088896340736f;
-constexpr int STEP = FFN_BLOCK, WAVES_N = 4, WAVES_M = 2, THREADS = WAVES_M * WAVES_N * 64;
+constexpr int STEP = FFN_BLOCK, WAVES_M = 4, WAVES_N = 2, THREADS = WAVES_M * WAVES_N * 64;
 
 // ------------------------------------------------------------------------------------------------ activations
 
@@ -64,393 +63,411 @@ __device__ __forceinline__ void dword_to_lds(uint32_t lds, const void *base, uin
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2" ::"s"(lds), "v"(offset), "s"(base) : "memory");
 }
 
+__device__ const uint4 ffn_zeros = {0, 0, 0, 0};
+// The same as load_to_lds, from an address of each lane's own.
+__device__ __forceinline__ void lane_to_lds(uint32_t lds, const void *from) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds), "v"(from) : "memory");
+}
+
+// Where a lane's first 16 bytes of 16 rows of a step lie, from the first row's (a multiple of 16) on; the others are 64 bytes away, up or down.
+__device__ __forceinline__ uint32_t lane_place(int lane) {
+  const int row = lane & 15;
+  return row * STEP + 16 * ((lane >> 4) ^ ((row >> 1) & 7));
+}
 // 32 bytes a lane of 16 rows of a step: which of a block's bytes are which k does not matter as long as both operands agree.
-__device__ __forceinline__ i32x8 operand(const lds_char *rows, int n, int lane) {
-  const int row = n + (lane & 15), piece = lane >> 4, turn = (row >> 1) & 7;
-  const auto at = [&](int p) { return *(const __attribute__((address_space(3))) i32x4 *)(rows + row * STEP + 16 * (p ^ turn)); };
-  const i32x4 a = at(piece), b = at(piece + 4);
+__device__ __forceinline__ i32x8 operand(const lds_char *first, const lds_char *second, int n) {
+  const i32x4 a = *(const __attribute__((address_space(3))) i32x4 *)(first + n * STEP), b = *(const __attribute__((address_space(3))) i32x4 *)(second + n * STEP);
   return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
 }
 
-// A tile of BM = 32 MI rows by BN = 64 NJ columns, by 2 x 4 waves of (16 MI) x (16 NJ).  Of the gated unit a tile's columns are 128 of the gate's and the same of
-// the other projection's, and a wave has the same ones of both.
+// The same as bf16 operands times a power of two, exact: four of eight elements a lane.
+struct Wide { bf16x8 v[4]; };
+__device__ __forceinline__ Wide widen(i32x8 u, float scale) {
+  Wide w;
+#pragma unroll
+  for (int q = 0; q < 4; ++q) {
+    typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+    const bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(u[2 * q], scale, false), b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(u[2 * q], scale, true);
+    const bf16x2 c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(u[2 * q + 1], scale, false), d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(u[2 * q + 1], scale, true);
+    w.v[q] = bf16x8{a.x, a.y, b.x, b.y, c.x, c.y, d.x, d.y};
+  }
+  return w;
+}
+__device__ __forceinline__ float power_of(uint32_t byte) { return u2f(byte ? byte << 23 : 0x00400000u); }
+__device__ __forceinline__ f32x4 multiply(const Wide &x, const Wide &y, f32x4 c) {
+#pragma unroll
+  for (int q = 0; q < 4; ++q) c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x.v[q], y.v[q], c, 0, 0, 0);
+  return c;
+}
+
+// A tile of BM = 64 MI rows by BN = 32 NJ columns, by 4 x 2 waves of (16 MI) x (16 NJ).  A lane's columns lie beside each other in memory, so that results leave without
+// a way through LDS: fragment j of a wave's columns holds those NJ c + j, c = 0 .. 15, and of the gated unit, where half of the fragments are of each
+// matrix, NJ / 2 c + j of either.  In LDS a fragment's rows lie together.
 template <int MI, int NJ, bool GATED>
 struct Tile8 {
   static constexpr int BM = 16 * MI * WAVES_M, BN = 16 * NJ * WAVES_N, X_BYTES = BM * STEP, W_BYTES = BN * STEP;
-  static constexpr int SCALES = BM + BN < THREADS ? THREADS : BM + BN, STEP_BYTES = X_BYTES + W_BYTES + SCALES * 4;
+  static constexpr int STEP_BYTES = X_BYTES + W_BYTES + THREADS * 4;
   static constexpr int X_LOADS = X_BYTES / 16 / THREADS, W_LOADS = W_BYTES / 16 / THREADS, LOADS = X_LOADS + W_LOADS + 1;
   static constexpr int COLUMNS = GATED ? BN / 2 : BN;          // of the output
-  static_assert(X_LOADS * THREADS * 16 == X_BYTES && W_LOADS * THREADS * 16 == W_BYTES && SCALES == THREADS, "whole loads");
+  static constexpr int RUN = GATED ? NJ / 2 : NJ;              // a lane's columns of a matrix
+  static constexpr int DEPTH = 163840 / (STEP_BYTES + 1024) < 4 ? 163840 / (STEP_BYTES + 1024) : 4;
+  static_assert(X_LOADS * THREADS * 16 == X_BYTES && W_LOADS * THREADS * 16 == W_BYTES && BM + BN <= THREADS, "whole loads");
 };
-constexpr int OWN_ROW = 36, OWN_BYTES = 16 * OWN_ROW * 4;      // 16 rows of 32 fp32 on a wave's way out, rows in different banks
-template <int MI, int NJ, int END>
-constexpr int end_bytes() {
-  return END == FFN_GATED ? WAVES_N * 16 * MI * WAVES_M * 4 + 64 * WAVES_M * 128 : WAVES_M * WAVES_N * OWN_BYTES;
-}
 
-template <int MI, int NJ, int END, bool BY_BLOCK>
+// A workgroup goes through tiles gridDim.x apart; its loads do not stop between them: while a tile's results leave, the next tile's first steps are on their way.
+// EXACT: in bf16, whose instruction adds products as an fp32 sum does.  The one for 8 bits, twice as fast, leaves out of eight neighbouring products what is below 2^-13
+// of the largest of them: 2^-14 of a result of activations with outlying channels, far below its rounding to bf16 or 8 bits, but not to fp32.
+template <int MI, int NJ, int END, bool BY_BLOCK, bool EXACT>
 __global__ __launch_bounds__(THREADS) void eco_ffn_kernel(ProductArgs a) {
   constexpr bool GATED = END != FFN_LINEAR;
   using T = Tile8<MI, NJ, GATED>;
-  __shared__ __attribute__((aligned(1024))) char smem[2 * T::STEP_BYTES + end_bytes<MI, NJ, END>()];
+  constexpr int DEPTH = T::DEPTH, RUN = T::RUN;
+  __shared__ __attribute__((aligned(1024))) char smem[DEPTH * T::STEP_BYTES + (END == FFN_GATED ? WAVES_N * T::BM * 4 : 0)];
   static_assert(sizeof smem <= 163840, "a compute unit's LDS");
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wn = wave % WAVES_N, wm = wave / WAVES_N * 16 * MI;
+  const uint32_t all_tiles = a.tiles_n * a.tiles_m * a.o.splits, tail = a.w.dim % STEP;
 
-  // eight tiles of rows beside each other, then the next columns: neighbours on an XCD share operands
-  uint32_t tile = xcd_run(blockIdx.x, gridDim.x);
-  const uint32_t split = tile / (a.tiles_n * a.tiles_m);
-  tile -= split * a.tiles_n * a.tiles_m;
-  const uint32_t run = 8 * a.tiles_n, band = tile / run, high = min(8u, a.tiles_m - band * 8), in = tile - band * run;
-  const uint32_t m0 = (band * 8 + in % high) * T::BM, n0 = in / high * T::COLUMNS;
-  const uint32_t first = split * a.o.split_steps, steps = min(a.o.split_steps, a.steps - first);
-
-  // ---- loads: rows past the last repeat it, and are not stored
-  const uint32_t lds0 = static_cast<uint32_t>(reinterpret_cast<uintptr_t>((lds_char *)smem));
-  const auto piece_of = [&](int i, uint32_t &row, uint32_t &k) {
-    uint32_t half;
-    row_piece(threadIdx.x + i * THREADS, row, half);
-    k = 2 * half;
+  struct Where { uint32_t m0, n0, split, first, steps; };
+  const auto where = [&](uint32_t id) {
+    // eight tiles of rows beside each other, then the next columns: neighbours on an XCD share operands
+    uint32_t tile = xcd_run(id, all_tiles);
+    Where w;
+    w.split = tile / (a.tiles_n * a.tiles_m);
+    tile -= w.split * a.tiles_n * a.tiles_m;
+    const uint32_t run = 8 * a.tiles_n, band = tile / run, high = min(8u, a.tiles_m - band * 8), in = tile - band * run;
+    w.m0 = (band * 8 + in % high) * T::BM;
+    w.n0 = in / high * T::COLUMNS;
+    w.first = w.split * a.o.split_steps;
+    w.steps = min(a.o.split_steps, a.steps - w.first);
+    return w;
   };
-  // of a column of the tile: the matrix and the row of it (a wave's 16 NJ columns of the gated unit are half gate, half up; in LDS the halves lie apart)
-  const auto matrix_of = [&](uint32_t n) { return GATED ? n / T::COLUMNS : 0u; };
-  const auto row_of = [&](uint32_t n) { return min(n0 + (GATED ? n % T::COLUMNS : n), a.w.rows - 1); };
-  const uint8_t *x_from = a.x.codes + m0 * a.x.stride + first * STEP;
-  const uint8_t *w_from[2] = {static_cast<const uint8_t *>(a.w.data[0]) + static_cast<uint64_t>(n0) * a.w.dim + first * STEP,
-                              GATED ? static_cast<const uint8_t *>(a.w.data[1]) + static_cast<uint64_t>(n0) * a.w.dim + first * STEP : nullptr};
-  uint32_t x_off[T::X_LOADS], w_off[T::W_LOADS];
-#pragma unroll
-  for (int i = 0; i < T::X_LOADS; ++i) {
-    uint32_t row, k;
-    piece_of(i, row, k);
-    x_off[i] = (min(m0 + row, a.x.rows - 1) - m0) * static_cast<uint32_t>(a.x.stride) + k;
-  }
-#pragma unroll
-  for (int i = 0; i < T::W_LOADS; ++i) {
-    uint32_t row, k;
-    piece_of(i, row, k);
-    w_off[i] = (row_of(row) - n0) * a.w.dim + k;
-  }
-  // one scale a thread: of the rows, then of the weights (by waves: 64 is a factor of both)
-  const bool of_x = static_cast<uint32_t>(wave) < T::BM / 64 || !BY_BLOCK;
-  const uint32_t sn = min(threadIdx.x - (of_x ? 0 : T::BM), static_cast<uint32_t>(T::BN) - 1);
-  const uint32_t smat = of_x ? 0 : __builtin_amdgcn_readfirstlane(matrix_of(sn));
-  const uint32_t scale_off = of_x ? (min(m0 + min(threadIdx.x, T::BM - 1u), a.x.rows - 1) - m0) * a.x.blocks : row_of(sn) * a.w.scale_row;
-  const uint8_t *xs_from = a.x.scales + static_cast<uint64_t>(m0) * a.x.blocks;
-  const uint32_t tail = a.w.dim % STEP;
-  uint32_t issued = 0;
-  const auto issue = [&]() {
-    if (issued >= steps) return;
-    const uint32_t lds = lds0 + (issued & 1) * T::STEP_BYTES + wave * 1024, step = first + issued;
-    const bool end = tail && step + 1 == a.steps;              // pieces past the row repeat its block's first, zeros take the place of the weights'
-#pragma unroll
-    for (int i = 0; i < T::X_LOADS; ++i) {
-      uint32_t row, k, off = x_off[i];
-      piece_of(i, row, k);
-      if (end && k >= tail) off -= k;
-      load_to_lds(lds + i * THREADS * 16, x_from, off);
+
+  // ---- loads
+  const uint32_t lds0 = static_cast<uint32_t>(reinterpret_cast<uintptr_t>((lds_char *)smem));
+  // a thread's pieces of 16 bytes are of rows 64 apart, and at the same place of them
+  uint32_t piece_row, piece_k;
+  row_piece(threadIdx.x, piece_row, piece_k);
+  piece_k *= 2;
+  const bool past = tail && piece_k >= tail;
+  // the column of row p of the tile's weights in LDS, and its matrix, which is the same for the eight rows of a wave's load
+  const auto column_of = [&](uint32_t p) { return p / (16 * NJ) * 16 * RUN + RUN * (p % 16) + p / 16 % NJ % RUN; };
+  const auto matrix_of = [&](uint32_t p) { return GATED && p / 16 % NJ >= RUN; };
+  uint32_t load_id = blockIdx.x, step_at = 0, steps_left = 0, place = 0, last_m = 0, last_n = 0, scale_off = 0;
+  const uint32_t piece_column = column_of(piece_row);
+  const uint8_t *x_from = nullptr, *xs_from = nullptr, *w_from[2] = {nullptr, nullptr};
+  // one scale a thread and step: of the rows, then of the weights by matrix (whole waves of each; threads past the last repeat it)
+  const bool of_x = !BY_BLOCK || static_cast<uint32_t>(wave) < T::BM / 64;
+  const uint32_t scale_p = min(threadIdx.x - (of_x ? 0u : T::BM), (of_x ? T::BM : T::BN) - 1u);
+  const bool scale_up = GATED && !of_x && __builtin_amdgcn_readfirstlane(scale_p) >= T::COLUMNS;
+  const char *const scales_from = static_cast<const char *>(scale_up ? a.w.scales[1] : a.w.scales[0]);
+  const auto load_tile = [&]() {
+    const Where w = where(load_id);
+    last_m = a.x.rows - 1 - w.m0;
+    last_n = a.w.rows - 1 - w.n0;
+    if (of_x) scale_off = (min(w.m0 + scale_p, a.x.rows - 1) - w.m0) * a.x.blocks;
+    else {
+      // in LDS by matrix, wave, fragment and lane
+      const uint32_t q = GATED ? scale_p % T::COLUMNS : scale_p, column = q / (16 * RUN) * 16 * RUN + RUN * (q % 16) + q / 16 % RUN;
+      scale_off = min(w.n0 + column, a.w.rows - 1) * a.w.scale_row * (a.w.scale_bf16 ? 2 : 4);
     }
+    step_at = w.first;
+    steps_left = w.steps;
+    x_from = a.x.codes + w.m0 * a.x.stride + w.first * STEP;
+    xs_from = a.x.scales + static_cast<uint64_t>(w.m0) * a.x.blocks + w.first;
+#pragma unroll
+    for (int q = 0; q < (GATED ? 2 : 1); ++q) w_from[q] = static_cast<const uint8_t *>(a.w.data[q]) + static_cast<uint64_t>(w.n0) * a.w.dim + w.first * STEP;
+  };
+  // (after the last tile the last step's loads are repeated, so that their number is the same in every step)
+  const auto issue = [&]() {
+    const uint32_t to = lds0 + place * T::STEP_BYTES, lds = to + wave * 1024;
+    // pieces past the row: of x the block's first, which the weights' zeros take out of the sums
+    const bool zero = past && step_at + 1 == a.steps;
+    const uint32_t x_k = zero ? 0 : piece_k;
+#pragma unroll
+    for (int i = 0; i < T::X_LOADS; ++i)                       // rows past the last repeat it, and are not stored
+      load_to_lds(lds + i * THREADS * 16, x_from, min(piece_row + 64 * i, last_m) * static_cast<uint32_t>(a.x.stride) + x_k);
 #pragma unroll
     for (int i = 0; i < T::W_LOADS; ++i) {
-      uint32_t row, k, off = w_off[i];
-      piece_of(i, row, k);
-      if (end && k >= tail) off -= k;
-      // (a load's rows, 64 of them, are of one matrix)
-      load_to_lds(lds + T::X_BYTES + i * THREADS * 16, w_from[GATED && i * 64 >= T::COLUMNS ? 1 : 0], off);
+      const uint8_t *from = w_from[matrix_of(i * 64 + wave * 8)] + (min(piece_column + column_of(64 * i), last_n) * a.w.dim + piece_k);
+      lane_to_lds(lds + T::X_BYTES + i * THREADS * 16, zero ? reinterpret_cast<const uint8_t *>(&ffn_zeros) : from);
     }
-    const uint32_t to = lds0 + (issued & 1) * T::STEP_BYTES + T::X_BYTES + T::W_BYTES + wave * 256;
-    if (of_x) byte_to_lds(to, xs_from + step, scale_off);
+    const uint32_t to_scale = to + T::X_BYTES + T::W_BYTES + wave * 256;
+    if (of_x) byte_to_lds(to_scale, xs_from, scale_off);
     else {
-      const uint32_t group = a.w.group_blocks ? step / a.w.group_blocks : 0;
-      const void *of_w = GATED && smat ? a.w.scales[1] : a.w.scales[0];
-      if (a.w.scale_bf16) half_to_lds(to, static_cast<const uint16_t *>(of_w) + group, scale_off * 2);
-      else dword_to_lds(to, static_cast<const float *>(of_w) + group, scale_off * 4);
+      const uint32_t group = a.w.group_blocks == 1 ? step_at : step_at / a.w.group_blocks;
+      if (a.w.scale_bf16) half_to_lds(to_scale, scales_from + group * 2, scale_off);
+      else dword_to_lds(to_scale, scales_from + group * 4, scale_off);
     }
+    place = place + 1 == DEPTH ? 0 : place + 1;
+    if (load_id >= all_tiles) return;
+    if (--steps_left == 0) {
+      load_id += gridDim.x;
+      if (load_id < all_tiles) load_tile();
+      return;
+    }
+    ++step_at;
     x_from += STEP;
+    ++xs_from;
     w_from[0] += STEP;
     if (GATED) w_from[1] += STEP;
-    ++issued;
   };
 
-  // columns of the wave's fragment j in the tile
-  const auto column = [&](int j) { return GATED ? (j / (NJ / 2)) * T::COLUMNS + wn * 8 * NJ + 16 * (j % (NJ / 2)) : wn * 16 * NJ + 16 * j; };
-
-  f32x4 acc[MI][NJ] = {};
-  issue();
-  issue();
-  for (uint32_t s = 0; s < steps; ++s) {
-    if (issued - s >= 2) wait_all_but<T::LOADS>();
-    else wait_all_but<0>();
-    barrier();
-    const lds_char *step = (const lds_char *)smem + (s & 1) * T::STEP_BYTES;
-    if (tail && first + s + 1 == a.steps) {
-#pragma unroll
-      for (int i = 0; i < T::W_LOADS; ++i) {
-        uint32_t row, k;
-        piece_of(i, row, k);
-        if (k >= tail) *(__attribute__((address_space(3))) i32x4 *)((lds_char *)step + T::X_BYTES + (threadIdx.x + i * THREADS) * 16) = i32x4{0, 0, 0, 0};
-      }
-      __syncthreads();
+  // ---- the products' place
+  i32x8 fx[EXACT ? 1 : MI], fw[2];
+  Wide gx[EXACT ? MI : 1], gw[2];
+  uint32_t sx[MI];
+  float sw[2];
+  const uint32_t lane_at = lane_place(lane);
+  const lds_char *x_at[2], *w_at[2];
+  const lds_uint *scale_x, *scale_w;
+  const auto go_to = [&](uint32_t place_of) {
+    const lds_char *step = (const lds_char *)smem + place_of * T::STEP_BYTES;
+    x_at[0] = step + wm * STEP + lane_at;
+    x_at[1] = step + wm * STEP + (lane_at ^ 64);
+    w_at[0] = step + T::X_BYTES + wn * 16 * NJ * STEP + lane_at;
+    w_at[1] = step + T::X_BYTES + wn * 16 * NJ * STEP + (lane_at ^ 64);
+    scale_x = (const lds_uint *)(step + T::X_BYTES + T::W_BYTES) + wm + (lane & 15);
+    scale_w = (const lds_uint *)(step + T::X_BYTES + T::W_BYTES) + T::BM + wn * 16 * RUN + (lane & 15);
+  };
+  const auto read_w = [&](int j) {
+    const i32x8 f = operand(w_at[0], w_at[1], 16 * j);
+    if constexpr (EXACT) gw[j & 1] = widen(f, 1.0f);
+    else fw[j & 1] = f;
+    if constexpr (BY_BLOCK) {
+      const uint32_t bits = scale_w[GATED ? j / RUN * T::COLUMNS + 16 * (j % RUN) : 16 * j];
+      sw[j & 1] = u2f(a.w.scale_bf16 ? bits << 16 : bits);
     }
-    const lds_uint *scales = (const lds_uint *)(step + T::X_BYTES + T::W_BYTES);
-    i32x8 fw[NJ];
-    float sw[NJ];
+  };
+  const auto read_x = [&]() {
 #pragma unroll
-    for (int j = 0; j < NJ; ++j) {
-      fw[j] = operand(step + T::X_BYTES, column(j), lane);
-      if constexpr (BY_BLOCK) {
-        const uint32_t bits = scales[T::BM + column(j) + (lane & 15)];
-        sw[j] = u2f(a.w.scale_bf16 ? bits << 16 : bits);
-      }
+    for (int i = 0; i < MI; ++i) {
+      sx[i] = scale_x[16 * i];
+      const i32x8 f = operand(x_at[0], x_at[1], 16 * i);
+      if constexpr (EXACT) gx[i] = widen(f, power_of(sx[i]));
+      else fx[i] = f;
     }
-    i32x8 fx[2];
-    uint32_t sx[2];
-    const auto read = [&](int i) {
-      fx[i & 1] = operand(step, wm + 16 * i, lane);
-      sx[i & 1] = scales[wm + 16 * i + (lane & 15)];
-    };
-    read(0);
-    f32x4 part[2][NJ];
+  };
+  uint32_t at = 0;
+  f32x4 acc[MI][NJ], part[2][MI];
+  const auto products = [&](int j) {
+    const f32x4 zero = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-    for (int i = 0; i < MI + 1; ++i) {
-      if (i + 1 < MI) read(i + 1);
-      if (i < MI) {
-#pragma unroll
-        for (int j = 0; j < NJ; ++j) {
-          const f32x4 zero = {0.0f, 0.0f, 0.0f, 0.0f};
-          const f32x4 v = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(fx[i & 1], fw[j], BY_BLOCK ? zero : acc[i][j], 0, 0, 0, static_cast<int>(sx[i & 1]), 0, 127);
-          if constexpr (BY_BLOCK) part[i & 1][j] = v;
-          else acc[i][j] = v;
-        }
-      }
-      if constexpr (BY_BLOCK) {
-        if (i) {
-#pragma unroll
-          for (int j = 0; j < NJ; ++j)
-#pragma unroll
-            for (int r = 0; r < 4; ++r) acc[i - 1][j][r] = fmaf(part[(i - 1) & 1][j][r], sw[j], acc[i - 1][j][r]);
-        }
-      }
+    for (int i = 0; i < MI; ++i) {
+      const f32x4 c = BY_BLOCK ? zero : acc[i][j];
+      f32x4 v;
+      if constexpr (EXACT) v = multiply(gx[i], gw[j & 1], c);
+      else v = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(fx[i], fw[j & 1], c, 0, 0, 0, static_cast<int>(sx[i]), 0, 127);
+      if constexpr (BY_BLOCK) part[j & 1][i] = v;
+      else acc[i][j] = v;
     }
-    __builtin_amdgcn_sched_barrier(0);
-    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-    barrier();
-    issue();
-  }
-
-  // ---- ends.  acc[i][j][r]: row m0 + wm + 16 i + 4 (lane >> 4) + r, column column(j) + (lane & 15)
-  int end_lane = lane;
-  asm volatile("" : "+v"(end_lane));
-  const int col = end_lane & 15, row4 = 4 * (end_lane >> 4);
-  if constexpr (!BY_BLOCK) {
-#pragma unroll
-    for (int j = 0; j < NJ; ++j) {
-      const uint32_t n = column(j) + col;
-      const void *from = GATED && j >= NJ / 2 ? a.w.scales[1] : a.w.scales[0];
-      const uint64_t at = static_cast<uint64_t>(row_of(n)) * a.w.scale_row;
-      const float s = a.w.scale_bf16 ? u2f(static_cast<uint32_t>(static_cast<const uint16_t *>(from)[at]) << 16) : static_cast<const float *>(from)[at];
+  };
+  const auto add = [&](int j, float s) {
+    if constexpr (BY_BLOCK)
 #pragma unroll
       for (int i = 0; i < MI; ++i)
 #pragma unroll
-        for (int r = 0; r < 4; ++r) acc[i][j][r] *= s;
-    }
-  }
-  char *const extra = smem + 2 * T::STEP_BYTES;
-  lds_char *const own = (lds_char *)extra + wave * OWN_BYTES;
-  // 16 rows of 32 columns through the wave's own part of LDS: from the matrix core's places to a lane's eight neighbours of row end_lane / 4, or back
-  const auto put = [&](int c, f32x4 v) {
-#pragma unroll
-    for (int r = 0; r < 4; ++r) ((lds_float *)own)[(row4 + r) * OWN_ROW + 16 * c + col] = v[r];
-  };
-  const int out_row = end_lane >> 2, out_col = 8 * (end_lane & 3);
-  const auto take = [&](float (&v)[8]) {
-#pragma unroll
-    for (int q = 0; q < 2; ++q) {
-      const f32x4 u = *(const __attribute__((address_space(3))) f32x4 *)(own + (out_row * OWN_ROW + out_col + 4 * q) * 4);
-#pragma unroll
-      for (int r = 0; r < 4; ++r) v[4 * q + r] = u[r];
-    }
+        for (int r = 0; r < 4; ++r) acc[i][j][r] = fmaf(part[j & 1][i][r], s, acc[i][j][r]);
   };
 
-  if constexpr (END == FFN_LINEAR) {
-    const bool to_partial = a.o.partial != nullptr, as_bf16 = a.o.bf16 && !to_partial;
-    const uint64_t stride = to_partial ? a.w.rows : a.o.out_stride;
-    char *const out = to_partial ? reinterpret_cast<char *>(a.o.partial + static_cast<uint64_t>(split) * a.x.rows * a.w.rows) : static_cast<char *>(a.o.out);
-    const bool whole = stride % (as_bf16 ? 8 : 4) == 0 && (reinterpret_cast<uintptr_t>(out) & 15) == 0;
-    const bool whole_add = a.o.add_stride % (as_bf16 ? 8 : 4) == 0 && (reinterpret_cast<uintptr_t>(a.o.add) & 15) == 0;
+  load_tile();
+  for (int i = 0; i < DEPTH - 1; ++i) issue();
+  wait_loads<(DEPTH - 2) * T::LOADS>();
+  barrier();
+  go_to(0);
+  read_x();
+  read_w(0);
+  for (uint32_t id = blockIdx.x; id < all_tiles; id += gridDim.x) {
+    const Where w = where(id);
+    const uint32_t m0 = w.m0, n0 = w.n0;
 #pragma unroll
     for (int i = 0; i < MI; ++i)
 #pragma unroll
-      for (int j = 0; j < NJ; j += 2) {
-        put(0, acc[i][j]);
-        put(1, acc[i][j + 1]);
-        float v[8];
-        take(v);
-        const uint32_t m = m0 + wm + 16 * i + out_row, n = n0 + column(j) + out_col;
-        if (m >= a.x.rows || n >= a.w.rows) continue;
-        const bool all = n + 8 <= a.w.rows;
-        const uint64_t at = m * stride + n;
-        if (a.o.add && !to_partial) {
-          const uint64_t from = m * a.o.add_stride + n;
-          if (as_bf16) {
-            const uint16_t *p = static_cast<const uint16_t *>(a.o.add) + from;
-            if (all && whole_add) {
-              const uint4 u = *reinterpret_cast<const uint4 *>(p);
-              const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+      for (int j = 0; j < NJ; ++j) acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    for (uint32_t s = 0; s < w.steps; ++s) {
+      issue();                                                 // into the last step's place, which every wave has read
+      // (from here on no branch, over which the compiler would carry the products)
+      __builtin_amdgcn_sched_barrier(0);
+      float before = 0.0f;
 #pragma unroll
-              for (int e = 0; e < 8; ++e) v[e] += (e & 1) ? bf16_hi(w[e / 2]) : bf16_lo(w[e / 2]);
-            } else {
+      for (int j = 0; j < NJ - 1; ++j) {
+        const float mine = sw[j & 1];
+        read_w(j + 1);
+        products(j);
+        if (j) add(j - 1, before);
+        before = mine;
+        // reads of LDS first, then a product and its share of the sums, and so on
+        if constexpr (!EXACT) {
+          __builtin_amdgcn_sched_group_barrier(0x100, BY_BLOCK ? 3 : 2, 0);
 #pragma unroll
-              for (int e = 0; e < 8; ++e)
-                if (n + e < a.w.rows) v[e] += u2f(static_cast<uint32_t>(p[e]) << 16);
-            }
-          } else {
-            const float *p = static_cast<const float *>(a.o.add) + from;
-#pragma unroll
-            for (int e = 0; e < 8; ++e)
-              if (n + e < a.w.rows) v[e] += p[e];
-          }
-        }
-        if (as_bf16) {
-          uint32_t w[4];
-#pragma unroll
-          for (int e = 0; e < 4; ++e) w[e] = f32x2_to_bf16x2_rne(v[2 * e], v[2 * e + 1]);
-          uint16_t *to = reinterpret_cast<uint16_t *>(out) + at;
-          if (all && whole) *reinterpret_cast<uint4 *>(to) = make_uint4(w[0], w[1], w[2], w[3]);
-          else
-#pragma unroll
-            for (int e = 0; e < 8; ++e)
-              if (n + e < a.w.rows) to[e] = static_cast<uint16_t>(w[e / 2] >> (16 * (e & 1)));
-        } else {
-          float *to = reinterpret_cast<float *>(out) + at;
-          if (all && whole) {
-            reinterpret_cast<float4 *>(to)[0] = make_float4(v[0], v[1], v[2], v[3]);
-            reinterpret_cast<float4 *>(to)[1] = make_float4(v[4], v[5], v[6], v[7]);
-          } else {
-#pragma unroll
-            for (int e = 0; e < 8; ++e)
-              if (n + e < a.w.rows) to[e] = v[e];
+          for (int i = 0; i < MI; ++i) {
+            __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+            if (BY_BLOCK && j) __builtin_amdgcn_sched_group_barrier(0x002, 4, 0);
           }
         }
       }
-  }
+      const float last = sw[(NJ - 1) & 1];
+      products(NJ - 1);
+      add(NJ - 2, before);
+      // the next step, of this tile or the next, is there once every wave's loads of it are
+      wait_all_but<(DEPTH - 2) * T::LOADS>();
+      barrier();
+      at = at + 1 == DEPTH ? 0 : at + 1;
+      go_to(at);
+      read_x();
+      read_w(0);
+      add(NJ - 1, last);
+    }
 
-  if constexpr (END == FFN_GATED) {
-    // h in the gate's place; the largest of a row over the tile's columns: sixteen lanes, then the four waves beside each other
-    lds_uint *const red = (lds_uint *)(lds_char *)extra;
-    uint8_t *const codes = reinterpret_cast<uint8_t *>(extra + WAVES_N * T::BM * 4);
+    // ---- ends.  acc[i][j][r]: row m0 + wm + 16 i + 4 (end_lane >> 4) + r, column of fragment j and lane c = end_lane & 15 as above
+    int end_lane = lane;
+    asm volatile("" : "+v"(end_lane));
+    const int c = end_lane & 15, row4 = 4 * (end_lane >> 4);
+    const uint32_t n = n0 + wn * 16 * RUN + RUN * c;           // the first of the lane's columns
+    const bool all = n + RUN <= a.w.rows;
+    if constexpr (!BY_BLOCK) {
 #pragma unroll
-    for (int i = 0; i < MI; ++i) {
-      uint32_t largest[4] = {0, 0, 0, 0};
+      for (int j = 0; j < NJ; ++j) {
+        const void *from = GATED && j >= RUN ? a.w.scales[1] : a.w.scales[0];
+        const uint64_t place_of = static_cast<uint64_t>(min(n + j % RUN, a.w.rows - 1)) * a.w.scale_row;
+        const float s = a.w.scale_bf16 ? u2f(static_cast<uint32_t>(static_cast<const uint16_t *>(from)[place_of]) << 16) : static_cast<const float *>(from)[place_of];
 #pragma unroll
-      for (int j = 0; j < NJ / 2; ++j) {
-        const bool there = n0 + column(j) + col < a.w.rows;
+        for (int i = 0; i < MI; ++i)
 #pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          acc[i][j][r] = act_of(acc[i][j][r], a.o.act) * acc[i][j + NJ / 2][r];
-          largest[r] = max(largest[r], there ? f2u(acc[i][j][r]) & 0x7FFFFFFFu : 0u);
-        }
-      }
-#pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        largest[r] = max_of_16(largest[r]);
-        if (col == 0) red[wn * T::BM + wm + 16 * i + row4 + r] = largest[r];
+          for (int r = 0; r < 4; ++r) acc[i][j][r] *= s;
       }
     }
-    __syncthreads();
-    const bool whole = a.o.out_stride % 16 == 0 && (reinterpret_cast<uintptr_t>(a.o.out) & 15) == 0;
-    const uint32_t blocks = (a.w.rows + FFN_BLOCK - 1) / FFN_BLOCK;
-    constexpr int AT_ONCE = MI < 4 ? MI : 4;                   // sixteens of rows of each half of the waves
+
+    if constexpr (END == FFN_LINEAR) {
+      const bool to_partial = a.o.partial != nullptr, as_bf16 = a.o.bf16 && !to_partial;
+      const uint64_t stride = to_partial ? a.w.rows : a.o.out_stride;
+      char *const out = to_partial ? reinterpret_cast<char *>(a.o.partial + static_cast<uint64_t>(w.split) * a.x.rows * a.w.rows) : static_cast<char *>(a.o.out);
+      const bool whole = all && stride % (as_bf16 ? RUN : 4) == 0 && (reinterpret_cast<uintptr_t>(out) & (as_bf16 ? 2 * RUN - 1 : 15)) == 0;
+      const bool whole_add = all && a.o.add_stride % (as_bf16 ? RUN : 4) == 0 && (reinterpret_cast<uintptr_t>(a.o.add) & (as_bf16 ? 2 * RUN - 1 : 15)) == 0;
 #pragma unroll
-    for (int i0 = 0; i0 < MI; i0 += AT_ONCE) {
+      for (int i = 0; i < MI; ++i)
 #pragma unroll
-      for (int i = i0; i < i0 + AT_ONCE; ++i)
+        for (int r = 0; r < 4; ++r) {
+          const uint32_t m = m0 + wm + 16 * i + row4 + r;
+          if (m >= a.x.rows || n >= a.w.rows) continue;
+          if (a.o.add && !to_partial) {
+            const uint64_t from = m * a.o.add_stride + n;
+            if (as_bf16) {
+              const uint16_t *p = static_cast<const uint16_t *>(a.o.add) + from;
+              uint32_t two[RUN / 2];
+              if (whole_add) __builtin_memcpy(two, __builtin_assume_aligned(p, 2 * RUN), sizeof two);
+              else
+#pragma unroll
+                for (int e = 0; e < RUN; e += 2) two[e / 2] = (n + e < a.w.rows ? p[e] : 0u) | (n + e + 1 < a.w.rows ? p[e + 1] : 0u) << 16;
+#pragma unroll
+              for (int e = 0; e < RUN; ++e) acc[i][e][r] += (e & 1) ? bf16_hi(two[e / 2]) : bf16_lo(two[e / 2]);
+            } else {
+              const float *p = static_cast<const float *>(a.o.add) + from;
+              float v[RUN];
+              if (whole_add) __builtin_memcpy(v, __builtin_assume_aligned(p, 16), sizeof v);
+              else
+#pragma unroll
+                for (int e = 0; e < RUN; ++e) v[e] = n + e < a.w.rows ? p[e] : 0.0f;
+#pragma unroll
+              for (int e = 0; e < RUN; ++e) acc[i][e][r] += v[e];
+            }
+          }
+          if (as_bf16) {
+            uint16_t *to = reinterpret_cast<uint16_t *>(out) + m * stride + n;
+            uint32_t two[RUN / 2];
+#pragma unroll
+            for (int e = 0; e < RUN; e += 2) two[e / 2] = f32x2_to_bf16x2_rne(acc[i][e][r], acc[i][e + 1][r]);
+            if (whole) __builtin_memcpy(__builtin_assume_aligned(to, 2 * RUN), two, sizeof two);
+            else
+#pragma unroll
+              for (int e = 0; e < RUN; ++e)
+                if (n + e < a.w.rows) to[e] = static_cast<uint16_t>(two[e / 2] >> (16 * (e & 1)));
+          } else {
+            float *to = reinterpret_cast<float *>(out) + m * stride + n;
+            if (whole)
+#pragma unroll
+              for (int e = 0; e < RUN; e += 4) *reinterpret_cast<float4 *>(to + e) = make_float4(acc[i][e][r], acc[i][e + 1][r], acc[i][e + 2][r], acc[i][e + 3][r]);
+            else
+#pragma unroll
+              for (int e = 0; e < RUN; ++e)
+                if (n + e < a.w.rows) to[e] = acc[i][e][r];
+          }
+        }
+    }
+
+    if constexpr (END == FFN_GATED) {
+      // h in the gate's place; the largest of a row over the tile's columns: a lane's, sixteen lanes', then the two waves' beside each other
+      static_assert(RUN == 4, "a lane's codes are a dword");
+      lds_uint *const red = (lds_uint *)((lds_char *)smem + DEPTH * T::STEP_BYTES);
+#pragma unroll
+      for (int i = 0; i < MI; ++i)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          uint32_t largest = 0;
+#pragma unroll
+          for (int j = 0; j < RUN; ++j) {
+            acc[i][j][r] = act_of(acc[i][j][r], a.o.act) * acc[i][j + RUN][r];
+            if (all || n + j < a.w.rows) largest = max(largest, f2u(acc[i][j][r]) & 0x7FFFFFFFu);
+          }
+          largest = max_of_16(largest);
+          if (c == 0) red[wn * T::BM + wm + 16 * i + row4 + r] = largest;
+        }
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+      barrier();
+      const uint32_t blocks = (a.w.rows + FFN_BLOCK - 1) / FFN_BLOCK;
+      const bool whole = all && a.o.out_stride % 4 == 0 && (reinterpret_cast<uintptr_t>(a.o.out) & 3) == 0;
+#pragma unroll
+      for (int i = 0; i < MI; ++i)
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
           const int row = wm + 16 * i + row4 + r;
-          uint32_t largest = red[row];
-#pragma unroll
-          for (int w = 1; w < WAVES_N; ++w) largest = max(largest, red[w * T::BM + row]);
-          const Rows8Scale s = rows8_scale(largest);
           const uint32_t m = m0 + row;
-          if (wn == 0 && col == 0 && m < a.x.rows) a.o.scales[static_cast<uint64_t>(m) * blocks + n0 / FFN_BLOCK] = s.byte;
-          static_assert(NJ == 4, "two columns' codes at a time");
-          const uint32_t two = rows8_codes(s, acc[i][0][r], acc[i][1][r], 0.0f, 0.0f);
-          uint8_t *to = codes + ((wave / WAVES_N) * 16 * AT_ONCE + 16 * (i - i0) + row4 + r) * 128 + wn * 32 + col;
-          to[0] = static_cast<uint8_t>(two);
-          to[16] = static_cast<uint8_t>(two >> 8);
-        }
-      __syncthreads();
+          const Rows8Scale s = rows8_scale(max(red[row], red[T::BM + row]));
+          const uint32_t codes = rows8_codes(s, acc[i][0][r], acc[i][1][r], acc[i][2][r], acc[i][3][r]);
+          if (m >= a.x.rows || n >= a.w.rows) continue;
+          if (wn == 0 && c == 0) a.o.scales[static_cast<uint64_t>(m) * blocks + n0 / FFN_BLOCK] = s.byte;
+          uint8_t *to = static_cast<uint8_t *>(a.o.out) + m * a.o.out_stride + n;
+          if (whole) *reinterpret_cast<uint32_t *>(to) = codes;
+          else
 #pragma unroll
-      for (int q = 0; q < WAVES_M * 16 * AT_ONCE * 8 / THREADS; ++q) {
-        const int at = threadIdx.x + q * THREADS, row = at / 8, c = at % 8 * 16;
-        const uint32_t m = m0 + row / (16 * AT_ONCE) * 16 * MI + 16 * i0 + row % (16 * AT_ONCE), n = n0 + c;
-        if (m >= a.x.rows || n >= a.w.rows) continue;
-        const uint4 v = *reinterpret_cast<const uint4 *>(codes + row * 128 + c);
-        uint8_t *to = static_cast<uint8_t *>(a.o.out) + m * a.o.out_stride + n;
-        if (whole && n + 16 <= a.w.rows) *reinterpret_cast<uint4 *>(to) = v;
-        else {
-          const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-          for (int e = 0; e < 16; ++e)
-            if (n + e < a.w.rows) to[e] = static_cast<uint8_t>(w[e / 4] >> (8 * (e & 3)));
+            for (int e = 0; e < 4; ++e)
+              if (n + e < a.w.rows) to[e] = static_cast<uint8_t>(codes >> (8 * e));
         }
-      }
-      __syncthreads();
+      // (the next tile's largest are written after barriers of its steps, of which each tile has one at least)
     }
-  }
 
-  if constexpr (END == FFN_GATED_BACK) {
-    const bool whole = a.o.grad_out_stride % 8 == 0 && (reinterpret_cast<uintptr_t>(a.o.grad_out) & 15) == 0;
+    if constexpr (END == FFN_GATED_BACK) {
+      static_assert(RUN == 4, "a lane's gradients are eight bytes");
+      const bool whole = all && a.o.grad_out_stride % 4 == 0 && (reinterpret_cast<uintptr_t>(a.o.grad_out) & 7) == 0;
 #pragma unroll
-    for (int i = 0; i < MI; ++i) {
-      const uint32_t m = m0 + wm + 16 * i + out_row, n = n0 + column(0) + out_col;
-      const bool row_there = m < a.x.rows;
-      float g[8];
-      {
-        const uint16_t *from = a.o.grad_out + m * a.o.grad_out_stride + n;
-        if (row_there && whole && n + 8 <= a.w.rows) {
-          const uint4 u = *reinterpret_cast<const uint4 *>(from);
-          const uint32_t w[4] = {u.x, u.y, u.z, u.w};
-#pragma unroll
-          for (int e = 0; e < 8; ++e) g[e] = (e & 1) ? bf16_hi(w[e / 2]) : bf16_lo(w[e / 2]);
-        } else {
-#pragma unroll
-          for (int e = 0; e < 8; ++e) g[e] = row_there && n + e < a.w.rows ? u2f(static_cast<uint32_t>(from[e]) << 16) : 0.0f;
-        }
-      }
-      // to the matrix core's places
-#pragma unroll
-      for (int q = 0; q < 2; ++q) {
-        const f32x4 u = {g[4 * q], g[4 * q + 1], g[4 * q + 2], g[4 * q + 3]};
-        *(__attribute__((address_space(3))) f32x4 *)(own + (out_row * OWN_ROW + out_col + 4 * q) * 4) = u;
-      }
-#pragma unroll
-      for (int j = 0; j < NJ / 2; ++j)
+      for (int i = 0; i < MI; ++i)
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
-          const float grad = ((const lds_float *)own)[(row4 + r) * OWN_ROW + 16 * j + col];
-          float f, df;
-          act_both(acc[i][j][r], a.o.act, f, df);
-          // (columns past the width are the last one's, and leave as zeros)
-          const bool there = n0 + column(j) + col < a.w.rows;
-          acc[i][j][r] = there ? grad * acc[i][j + NJ / 2][r] * df : 0.0f;
-          acc[i][j + NJ / 2][r] = there ? grad * f : 0.0f;
+          const uint32_t m = m0 + wm + 16 * i + row4 + r;
+          if (m >= a.x.rows || n >= a.o.half) continue;        // (half is whole fours; columns from the width to half leave as zeros)
+          const uint16_t *from = a.o.grad_out + m * a.o.grad_out_stride + n;
+          uint32_t two[2];
+          if (whole) __builtin_memcpy(two, __builtin_assume_aligned(from, 8), sizeof two);
+          else
+#pragma unroll
+            for (int e = 0; e < 4; e += 2) two[e / 2] = (n + e < a.w.rows ? from[e] : 0u) | (n + e + 1 < a.w.rows ? from[e + 1] : 0u) << 16;
+          float ga[4], gb[4];
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const float grad = (j & 1) ? bf16_hi(two[j / 2]) : bf16_lo(two[j / 2]);
+            float f, df;
+            act_both(acc[i][j][r], a.o.act, f, df);
+            const bool there = all || n + j < a.w.rows;
+            ga[j] = there ? grad * acc[i][j + RUN][r] * df : 0.0f;
+            gb[j] = there ? grad * f : 0.0f;
+          }
+          uint16_t *to = static_cast<uint16_t *>(a.o.out) + m * a.o.out_stride + n;
+          *reinterpret_cast<uint2 *>(to) = make_uint2(f32x2_to_bf16x2_rne(ga[0], ga[1]), f32x2_to_bf16x2_rne(ga[2], ga[3]));
+          *reinterpret_cast<uint2 *>(to + a.o.half) = make_uint2(f32x2_to_bf16x2_rne(gb[0], gb[1]), f32x2_to_bf16x2_rne(gb[2], gb[3]));
         }
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-#pragma unroll
-        for (int j = 0; j < NJ / 2; ++j) put(j, acc[i][h * (NJ / 2) + j]);
-        float v[8];
-        take(v);
-        if (!row_there || n >= a.o.half) continue;             // half is whole eights
-        uint32_t w[4];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) w[e] = f32x2_to_bf16x2_rne(v[2 * e], v[2 * e + 1]);
-        *reinterpret_cast<uint4 *>(static_cast<uint16_t *>(a.o.out) + m * a.o.out_stride + h * a.o.half + n) = make_uint4(w[0], w[1], w[2], w[3]);
-      }
     }
   }
+  wait_loads<0>();                                             // (nothing is on its way to LDS when it is given up)
 }
 
 // Parts of sums over the inner axis, added in their order.
@@ -500,29 +517,31 @@ __global__ __launch_bounds__(256) void eco_ffn_expand_kernel(const uint32_t *cod
   for (uint64_t i = static_cast<uint64_t>(blockIdx.x) * 256 + threadIdx.x; i < words; i += static_cast<uint64_t>(gridDim.x) * 256) out[i] = e4m3_of_int4(codes[i]);
 }
 
-template <int MI, int NJ, int END>
+constexpr uint32_t UNITS = 256;                                // compute units
+template <int MI, int NJ, int END, bool EXACT>
 hipError_t launch_tiles(const FfnRows8 &x, const FfnWeights &w, const FfnOut &o, hipStream_t s) {
   using T = Tile8<MI, NJ, END != FFN_LINEAR>;
   const uint32_t tiles_n = (w.rows + T::COLUMNS - 1) / T::COLUMNS, tiles_m = (x.rows + T::BM - 1) / T::BM;
   const ProductArgs a = {x, w, o, tiles_n, tiles_m, x.blocks};
-  const uint32_t grid = tiles_n * tiles_m * o.splits;
-  if (w.group_blocks) eco_ffn_kernel<MI, NJ, END, true><<<grid, THREADS, 0, s>>>(a);
-  else eco_ffn_kernel<MI, NJ, END, false><<<grid, THREADS, 0, s>>>(a);
+  const uint64_t all = static_cast<uint64_t>(tiles_n) * tiles_m * o.splits;
+  const uint32_t grid = static_cast<uint32_t>(all < UNITS ? all : UNITS);
+  if (w.group_blocks) eco_ffn_kernel<MI, NJ, END, true, EXACT><<<grid, THREADS, 0, s>>>(a);
+  else eco_ffn_kernel<MI, NJ, END, false, EXACT><<<grid, THREADS, 0, s>>>(a);
   return hipGetLastError();
 }
 
 }  // namespace
 
-FfnPlan ffn_plan(int end, const FfnWeights &w, uint64_t rows) {
+FfnPlan ffn_plan(int end, const FfnWeights &w, uint64_t rows, bool exact) {
   const uint32_t steps = (w.dim + FFN_BLOCK - 1) / FFN_BLOCK;
-  FfnPlan p = {end, 256, 256, 1, steps};
+  FfnPlan p = {end, 256, 256, 1, steps, exact};
   const auto tiles = [&]() { return (rows + p.rows_tile - 1) / p.rows_tile * ((w.rows + p.width_tile - 1) / p.width_tile); };
   if (end != FFN_LINEAR) {
     p.width_tile = 128;
     while (p.rows_tile > 64 && tiles() < 256) p.rows_tile /= 2;
     return p;
   }
-  if (tiles() < 256) p.width_tile = 128;
+  if (exact || tiles() < 256) p.width_tile = 128;
   while (p.rows_tile > 64 && tiles() < 256) p.rows_tile /= 2;
   const uint64_t t = tiles();
   uint32_t splits = t < 256 ? static_cast<uint32_t>(256 / t) : 1;
@@ -535,19 +554,24 @@ FfnPlan ffn_plan(int end, const FfnWeights &w, uint64_t rows) {
 hipError_t launch_ffn(const FfnPlan &p, const FfnRows8 &x, const FfnWeights &w, const FfnOut &o, hipStream_t s) {
   if (x.rows == 0) return hipSuccess;
   if (p.end == FFN_GATED) {
-    if (p.rows_tile == 256) return launch_tiles<8, 4, FFN_GATED>(x, w, o, s);
-    if (p.rows_tile == 128) return launch_tiles<4, 4, FFN_GATED>(x, w, o, s);
-    return launch_tiles<2, 4, FFN_GATED>(x, w, o, s);
+    if (p.rows_tile == 256) return launch_tiles<4, 8, FFN_GATED, false>(x, w, o, s);
+    if (p.rows_tile == 128) return launch_tiles<2, 8, FFN_GATED, false>(x, w, o, s);
+    return launch_tiles<1, 8, FFN_GATED, false>(x, w, o, s);
   }
   if (p.end == FFN_GATED_BACK) {
-    if (p.rows_tile == 256) return launch_tiles<8, 4, FFN_GATED_BACK>(x, w, o, s);
-    if (p.rows_tile == 128) return launch_tiles<4, 4, FFN_GATED_BACK>(x, w, o, s);
-    return launch_tiles<2, 4, FFN_GATED_BACK>(x, w, o, s);
+    if (p.rows_tile == 256) return launch_tiles<4, 8, FFN_GATED_BACK, false>(x, w, o, s);
+    if (p.rows_tile == 128) return launch_tiles<2, 8, FFN_GATED_BACK, false>(x, w, o, s);
+    return launch_tiles<1, 8, FFN_GATED_BACK, false>(x, w, o, s);
   }
-  if (p.width_tile == 256) return launch_tiles<8, 4, FFN_LINEAR>(x, w, o, s);
-  if (p.rows_tile == 256) return launch_tiles<8, 2, FFN_LINEAR>(x, w, o, s);
-  if (p.rows_tile == 128) return launch_tiles<4, 2, FFN_LINEAR>(x, w, o, s);
-  return launch_tiles<2, 2, FFN_LINEAR>(x, w, o, s);
+  if (p.exact) {
+    if (p.rows_tile == 256) return launch_tiles<4, 4, FFN_LINEAR, true>(x, w, o, s);
+    if (p.rows_tile == 128) return launch_tiles<2, 4, FFN_LINEAR, true>(x, w, o, s);
+    return launch_tiles<1, 4, FFN_LINEAR, true>(x, w, o, s);
+  }
+  if (p.width_tile == 256) return launch_tiles<4, 8, FFN_LINEAR, false>(x, w, o, s);
+  if (p.rows_tile == 256) return launch_tiles<4, 4, FFN_LINEAR, false>(x, w, o, s);
+  if (p.rows_tile == 128) return launch_tiles<2, 4, FFN_LINEAR, false>(x, w, o, s);
+  return launch_tiles<1, 4, FFN_LINEAR, false>(x, w, o, s);
 }
 
 hipError_t launch_ffn_join(const FfnOut &o, uint32_t rows, uint32_t width, hipStream_t s) {
