@@ -306,7 +306,7 @@ eco_status_t eco_norm(const eco_norm_t *n, void *stream) {
   if (n->residual) {
     CHECK(check_rows("norm", "residual", n->residual, n->rows, n->residual_stride, n->dim, size));
     CHECK(check_rows("norm", "sum", n->sum, n->rows, n->sum_stride, n->dim, size));
-  } else if (n->sum) {
+  } else if (n->sum && n->rows) {
     return fail(ECO_EINVAL, "norm: a sum without a residual");
   }
   CHECK(check_rows("norm", "out", n->out, n->rows, n->out_stride, n->dim, n->scales ? 1 : size));

@@ -535,6 +535,7 @@ hipError_t launch_tiles(const FfnRows8 &x, const FfnWeights &w, const FfnOut &o,
 FfnPlan ffn_plan(int end, const FfnWeights &w, uint64_t rows, bool exact) {
   const uint32_t steps = (w.dim + FFN_BLOCK - 1) / FFN_BLOCK;
   FfnPlan p = {end, 256, 256, 1, steps, exact};
+  if (rows == 0) return p;
   const auto tiles = [&]() { return (rows + p.rows_tile - 1) / p.rows_tile * ((w.rows + p.width_tile - 1) / p.width_tile); };
   if (end != FFN_LINEAR) {
     p.width_tile = 128;
