@@ -11,6 +11,7 @@ constexpr uint32_t FFN_BLOCK = 128;               // elements of a row to a scal
 // Parts that a product's inner axis is summed in, and what the parts may take: a workspace is asked for once, for the most rows, and has to hold any call with fewer.
 constexpr uint64_t FFN_MOST_SPLITS = 32;
 constexpr uint64_t FFN_MOST_PARTIAL = 256ull * 64 * 128;       // elements, 8-bit products: they are split where there are less than 256 of the smallest tiles
+constexpr uint64_t FFN_FEW_ROWS = 64;                          // the kernel for few rows; the gated unit's leaves h in fp32 as a partial
 constexpr uint64_t FFN_MOST_INPUT_ROWS = 32768;                // rows of all parts of grad_input
 constexpr uint64_t FFN_MOST_WEIGHTS_PARTIAL = 1ull << 26;      // elements of all parts of grad_weights
 
@@ -59,7 +60,7 @@ struct FfnOut {
   const void *add;                                // linear
   void *out;
   uint64_t add_stride, out_stride;
-  float *partial;                                 // linear: [splits][rows][out_dim], joined by launch_ffn_join; null: written at once
+  float *partial;                                 // linear: [splits][rows][out_dim], joined by launch_ffn_join; null: written at once; gated, few rows: [rows][width]
   uint32_t splits, split_steps;
   int32_t bf16, act;
   uint8_t *scales;                                // gated: out are codes

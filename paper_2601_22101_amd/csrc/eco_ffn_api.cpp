@@ -137,6 +137,8 @@ eco::FfnRows8 rows_of(const Unit &u) {
           static_cast<uint32_t>(u.dim), static_cast<uint32_t>(blocks_of(u.dim))};
 }
 
+uint64_t least(uint64_t a, uint64_t b) { return a < b ? a : b; }
+
 // Arrays of a workspace, one after the other.
 struct Places {
   uint64_t bytes = 0;
@@ -147,7 +149,7 @@ struct Places {
 struct Forward {
   eco::FfnPlan plan;
   uint64_t expanded[2], partial;
-  bool expands;
+  bool expands, joins, rounds;                    // rounds: h in fp32 on its way to 8 bits
 };
 // MOST: room for any call with up to as many rows, whatever its plan.
 enum Room { EXACT, MOST };
@@ -158,6 +160,7 @@ Forward forward_of(const Unit &u, int end, Room room, Places &p, bool exact = fa
     if (u.fmt == ECO_FMT_INT4)
       for (uint32_t m = 0; m < u.matrices; ++m) (void)p.take(u.width * u.dim);
     const uint64_t all = blocks_of(u.dim) / 4 * u.rows * u.width;
+    if (end == eco::FFN_GATED) (void)p.take(4 * least(u.rows, eco::FFN_FEW_ROWS) * u.width);
     if (end == eco::FFN_LINEAR) (void)p.take(4 * (all < eco::FFN_MOST_PARTIAL ? all : eco::FFN_MOST_PARTIAL));
     return f;
   }
@@ -165,7 +168,9 @@ Forward forward_of(const Unit &u, int end, Room room, Places &p, bool exact = fa
   f.expands = u.fmt == ECO_FMT_INT4 && f.plan.rows_tile && u.rows;
   if (f.expands)
     for (uint32_t m = 0; m < u.matrices; ++m) f.expanded[m] = p.take(u.width * u.dim);
-  if (f.plan.splits > 1) f.partial = p.take(4ull * f.plan.splits * u.rows * u.width);
+  f.joins = f.plan.splits > 1;
+  f.rounds = end == eco::FFN_GATED && !f.plan.rows_tile;
+  if (f.joins || f.rounds) f.partial = p.take(4ull * f.plan.splits * u.rows * u.width);
   return f;
 }
 eco_status_t product(const Unit &u, const Forward &f, eco::FfnOut o, char *ws, hipStream_t s) {
@@ -179,9 +184,9 @@ eco_status_t product(const Unit &u, const Forward &f, eco::FfnOut o, char *ws, h
   }
   o.splits = f.plan.splits;
   o.split_steps = f.plan.split_steps;
-  if (f.plan.splits > 1) o.partial = reinterpret_cast<float *>(ws + f.partial);
+  if (f.joins || f.rounds) o.partial = reinterpret_cast<float *>(ws + f.partial);
   LAUNCH(u.what, eco::launch_ffn(f.plan, rows_of(u), w, o, s));
-  if (f.plan.splits > 1) LAUNCH(u.what, eco::launch_ffn_join(o, static_cast<uint32_t>(u.rows), static_cast<uint32_t>(u.width), s));
+  if (f.joins) LAUNCH(u.what, eco::launch_ffn_join(o, static_cast<uint32_t>(u.rows), static_cast<uint32_t>(u.width), s));
   return ECO_OK;
 }
 
@@ -192,7 +197,6 @@ struct Backward {
   uint64_t half, padded_rows, w, x, grad, input_partial, weights_partial;
   bool copies;
 };
-uint64_t least(uint64_t a, uint64_t b) { return a < b ? a : b; }
 Backward backward_of(const Unit &u, bool input, bool weights, bool copies, Room room, Places &p) {
   Backward b;
   std::memset(&b, 0, sizeof b);

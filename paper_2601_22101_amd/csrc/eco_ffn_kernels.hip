@@ -43,6 +43,19 @@ __device__ __forceinline__ void act_both(float a, int act, float &f, float &df) 
   df = q == 0.0f ? p : fmaf(a * dt, q, p);         // (a dt may be infinite there)
 }
 
+// ------------------------------------------------------------------------------------------------ INT4 codes as E4M3
+
+// The E4M3 codes of 0 .. 7 and of -8 .. -1 (the second half's -8 is no code of the library's, and stands for itself).
+__device__ __forceinline__ uint32_t e4m3_of_nibbles(uint32_t n) {        // one nibble in each byte
+  const uint32_t low = __builtin_amdgcn_perm(0x4E4C4A48u, 0x44403800u, n & 0x07070707u);
+  const uint32_t high = __builtin_amdgcn_perm(0xB8C0C4C8u, 0xCACCCED0u, n & 0x07070707u);
+  const uint32_t mask = ((n >> 3) & 0x01010101u) * 255u;
+  return (low & ~mask) | (high & mask);
+}
+__device__ __forceinline__ uint2 e4m3_of_int4(uint32_t eight) {          // eight codes in their order
+  const uint32_t even = e4m3_of_nibbles(eight & 0x0F0F0F0Fu), odd = e4m3_of_nibbles((eight >> 4) & 0x0F0F0F0Fu);
+  return make_uint2(__builtin_amdgcn_perm(odd, even, 0x05010400u), __builtin_amdgcn_perm(odd, even, 0x07030602u));
+}
 // ------------------------------------------------------------------------------------------------ tiles
 
 struct ProductArgs {
@@ -500,19 +513,181 @@ __global__ __launch_bounds__(256) void eco_ffn_join_kernel(FfnOut o, uint32_t ro
   }
 }
 
-// ------------------------------------------------------------------------------------------------ INT4 codes as E4M3
+// ------------------------------------------------------------------------------------------------ few rows
 
-// The E4M3 codes of 0 .. 7 and of -8 .. -1 (the second half's -8 is no code of the library's, and stands for itself).
-__device__ __forceinline__ uint32_t e4m3_of_nibbles(uint32_t n) {        // one nibble in each byte
-  const uint32_t low = __builtin_amdgcn_perm(0x4E4C4A48u, 0x44403800u, n & 0x07070707u);
-  const uint32_t high = __builtin_amdgcn_perm(0xB8C0C4C8u, 0xCACCCED0u, n & 0x07070707u);
-  const uint32_t mask = ((n >> 3) & 0x01010101u) * 255u;
-  return (low & ~mask) | (high & mask);
+// Up to 16 MT rows are bound by the reading of the weights: each wave reads 16 rows of them by itself, straight into the registers in which the matrix core takes
+// them, AHEAD blocks at a time, and INT4 codes become E4M3 there.  Nothing is kept in LDS but sums on their way from wave to wave.  (1 x 6912 x 1152 in FP8: 6.7 us; with
+// 8 or 4 columns to a workgroup, so that there are more of them than the 72, 8.9.)
+
+template <class V>
+__device__ __forceinline__ V loose(const void *p) {            // at an address of any alignment
+  V v;
+  __builtin_memcpy(&v, p, sizeof v);
+  return v;
 }
-__device__ __forceinline__ uint2 e4m3_of_int4(uint32_t eight) {          // eight codes in their order
-  const uint32_t even = e4m3_of_nibbles(eight & 0x0F0F0F0Fu), odd = e4m3_of_nibbles((eight >> 4) & 0x0F0F0F0Fu);
-  return make_uint2(__builtin_amdgcn_perm(odd, even, 0x05010400u), __builtin_amdgcn_perm(odd, even, 0x07030602u));
+
+// A lane's 32 codes of a row's block: of FP8 16 from 16 q and 16 from 64 + 16 q on, of INT4 32 from 32 q on.
+template <int FMT>
+struct Few {
+  static constexpr int SECOND = FMT == FMT_FP8 ? 64 : 16, FIRST = FMT == FMT_FP8 ? 16 : 32;
+  typedef std::conditional_t<FMT == FMT_FP8, i32x8, i32x4> Raw;
+  static __device__ __forceinline__ Raw read(const uint8_t *row, uint32_t k, uint32_t dim) {      // zeros past the row's end
+    Raw v = {};
+    if constexpr (FMT == FMT_FP8) {
+      const i32x4 zero = {0, 0, 0, 0}, a = k < dim ? *reinterpret_cast<const i32x4 *>(row + k) : zero, b = k + SECOND < dim ? *reinterpret_cast<const i32x4 *>(row + k + SECOND) : zero;
+      v = __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
+    } else {
+      if (k + 32 <= dim) v = loose<i32x4>(row + k / 2);
+      else if (k < dim) {
+        const uint2 u = loose<uint2>(row + k / 2);
+        v = i32x4{static_cast<int>(u.x), static_cast<int>(u.y), 0, 0};
+      }
+    }
+    return v;
+  }
+  static __device__ __forceinline__ i32x8 codes(Raw v) {
+    if constexpr (FMT == FMT_FP8) return v;
+    else {
+      i32x8 w;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const uint2 u = e4m3_of_int4(static_cast<uint32_t>(v[i]));
+        w[2 * i] = static_cast<int>(u.x);
+        w[2 * i + 1] = static_cast<int>(u.y);
+      }
+      return w;
+    }
+  }
+};
+
+// The sums of 16 rows of weights from n0 on with all rows of x, over blocks first, first + stride, ...  acc[t][r]: row 16 t + 4 (lane >> 4) + r of x, row n0 + (lane & 15)
+// of the weights.
+template <int FMT, int MT, int MATRICES, int AHEAD, bool EXACT>
+__device__ __forceinline__ void few_sums(const FfnRows8 &x, const FfnWeights &w, uint32_t n0, uint32_t first, uint32_t stride, int lane,
+                                         f32x4 (&acc)[MATRICES][MT]) {
+  using F = Few<FMT>;
+  const uint32_t n = min(n0 + (lane & 15), w.rows - 1), q = lane >> 4;
+  const uint64_t row = static_cast<uint64_t>(n) * w.dim / (FMT == FMT_FP8 ? 1 : 2);
+  const uint64_t scale_row = static_cast<uint64_t>(n) * w.scale_row;
+  const uint8_t *x_row[MT], *x_scale[MT];
+#pragma unroll
+  for (int t = 0; t < MT; ++t) {
+    const uint32_t m = min(16u * t + (lane & 15), x.rows - 1);
+    x_row[t] = x.codes + m * x.stride;
+    x_scale[t] = x.scales + static_cast<uint64_t>(m) * x.blocks;
+#pragma unroll
+    for (int y = 0; y < MATRICES; ++y) acc[y][t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+  }
+  for (uint32_t b0 = first; b0 < x.blocks; b0 += stride * AHEAD) {
+    typename F::Raw raw[MATRICES][AHEAD];
+    i32x8 fx[AHEAD][MT];
+    uint32_t sx[AHEAD][MT];
+    float sw[MATRICES][AHEAD];
+#pragma unroll
+    for (int p = 0; p < AHEAD; ++p) {
+      const uint32_t b = b0 + p * stride, k = b * STEP + q * F::FIRST;      // blocks past the last are all zeros
+      const uint64_t at = scale_row + (w.group_blocks ? min(b, x.blocks - 1) / w.group_blocks : 0);
+#pragma unroll
+      for (int y = 0; y < MATRICES; ++y) {
+        raw[y][p] = F::read(static_cast<const uint8_t *>(w.data[y]) + row, k, w.dim);
+        sw[y][p] = w.scale_bf16 ? u2f(static_cast<uint32_t>(static_cast<const uint16_t *>(w.scales[y])[at]) << 16) : static_cast<const float *>(w.scales[y])[at];
+      }
+#pragma unroll
+      for (int t = 0; t < MT; ++t) {
+        const i32x4 zero = {0, 0, 0, 0}, u = k < w.dim ? *reinterpret_cast<const i32x4 *>(x_row[t] + k) : zero,
+                    v = k + F::SECOND < w.dim ? *reinterpret_cast<const i32x4 *>(x_row[t] + k + F::SECOND) : zero;
+        fx[p][t] = __builtin_shufflevector(u, v, 0, 1, 2, 3, 4, 5, 6, 7);
+        sx[p][t] = x_scale[t][min(b, x.blocks - 1)];
+      }
+    }
+#pragma unroll
+    for (int p = 0; p < AHEAD; ++p) {
+      if (b0 + p * stride >= x.blocks) break;
+#pragma unroll
+      for (int y = 0; y < MATRICES; ++y) {
+        const i32x8 fw = F::codes(raw[y][p]);
+        const f32x4 zero = {0.0f, 0.0f, 0.0f, 0.0f};
+        Wide gw;
+        if constexpr (EXACT) gw = widen(fw, 1.0f);
+#pragma unroll
+        for (int t = 0; t < MT; ++t) {
+          f32x4 v;
+          if constexpr (EXACT) v = multiply(widen(fx[p][t], power_of(sx[p][t])), gw, zero);
+          else v = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(fx[p][t], fw, zero, 0, 0, 0, static_cast<int>(sx[p][t]), 0, 127);
+#pragma unroll
+          for (int r = 0; r < 4; ++r) acc[y][t][r] = fmaf(v[r], sw[y][p], acc[y][t][r]);
+        }
+      }
+    }
+  }
 }
+
+// 16 columns to a workgroup, whose waves have blocks of the inner axis in turn; the waves' sums are added in their order.  Of the gated unit the results are h in
+// fp32, which rows of 8 bits are made of next: a block of 128 is the work of eight workgroups.
+template <int FMT, int MT, int END, int WAVES, bool EXACT>
+__global__ __launch_bounds__(WAVES * 64) void eco_ffn_few_kernel(ProductArgs a) {
+  constexpr int MATRICES = END == FFN_GATED ? 2 : 1, AHEAD = MT == 1 ? 4 / MATRICES : MT == 2 ? 2 : 1;
+  __shared__ float sums[WAVES][MATRICES * MT * 4][64];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const uint32_t n0 = blockIdx.x * 16;
+  f32x4 acc[MATRICES][MT];
+  few_sums<FMT, MT, MATRICES, AHEAD, EXACT>(a.x, a.w, n0, wave, WAVES, lane, acc);
+#pragma unroll
+  for (int y = 0; y < MATRICES; ++y)
+#pragma unroll
+    for (int t = 0; t < MT; ++t)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) sums[wave][(y * MT + t) * 4 + r][lane] = acc[y][t][r];
+  __syncthreads();
+  const uint32_t n = n0 + (lane & 15);
+  for (int at = wave; at < MT * 4; at += WAVES) {
+    float v = 0.0f, u = 0.0f;
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w) {
+      v += sums[w][at][lane];
+      if (MATRICES == 2) u += sums[w][MT * 4 + at][lane];
+    }
+    const uint32_t m = at / 4 * 16 + 4 * (lane >> 4) + at % 4;
+    if (m >= a.x.rows || n >= a.w.rows) continue;
+    if constexpr (END == FFN_GATED) {
+      a.o.partial[static_cast<uint64_t>(m) * a.w.rows + n] = act_of(v, a.o.act) * u;
+    } else {
+      const uint64_t to = m * a.o.out_stride + n, from = m * a.o.add_stride + n;
+      if (a.o.bf16) {
+        if (a.o.add) v += u2f(static_cast<uint32_t>(static_cast<const uint16_t *>(a.o.add)[from]) << 16);
+        static_cast<uint16_t *>(a.o.out)[to] = static_cast<uint16_t>(f32x2_to_bf16x2_rne(v, 0.0f));
+      } else {
+        if (a.o.add) v += static_cast<const float *>(a.o.add)[from];
+        static_cast<float *>(a.o.out)[to] = v;
+      }
+    }
+  }
+}
+
+template <int FMT>
+hipError_t launch_few(const FfnPlan &p, const ProductArgs &a, hipStream_t s) {
+  const uint32_t grid = (a.w.rows + 15) / 16;
+  if (p.end == FFN_GATED) {
+    if (a.x.rows <= 16) eco_ffn_few_kernel<FMT, 1, FFN_GATED, 8, false><<<grid, 8 * 64, 0, s>>>(a);
+    else if (a.x.rows <= 32) eco_ffn_few_kernel<FMT, 2, FFN_GATED, 8, false><<<grid, 8 * 64, 0, s>>>(a);
+    else eco_ffn_few_kernel<FMT, 4, FFN_GATED, 8, false><<<grid, 8 * 64, 0, s>>>(a);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    NormRows r = {};
+    r.input = a.o.partial; r.out = a.o.out; r.scales = a.o.scales; r.input_stride = r.dim = a.w.rows; r.out_stride = a.o.out_stride; r.rows = a.x.rows;
+    return launch_norm(r, s);
+  }
+  const auto go = [&](auto exact) {
+    constexpr bool E = decltype(exact)::value;
+    if (a.x.rows <= 16) eco_ffn_few_kernel<FMT, 1, FFN_LINEAR, 16, E><<<grid, 16 * 64, 0, s>>>(a);
+    else if (a.x.rows <= 32) eco_ffn_few_kernel<FMT, 2, FFN_LINEAR, 16, E><<<grid, 16 * 64, 0, s>>>(a);
+    else eco_ffn_few_kernel<FMT, 4, FFN_LINEAR, 16, E><<<grid, 16 * 64, 0, s>>>(a);
+  };
+  if (p.exact) go(std::true_type{});
+  else go(std::false_type{});
+  return hipGetLastError();
+}
+
 __global__ __launch_bounds__(256) void eco_ffn_expand_kernel(const uint32_t *codes, uint64_t words, uint2 *out) {
   for (uint64_t i = static_cast<uint64_t>(blockIdx.x) * 256 + threadIdx.x; i < words; i += static_cast<uint64_t>(gridDim.x) * 256) out[i] = e4m3_of_int4(codes[i]);
 }
@@ -536,6 +711,10 @@ FfnPlan ffn_plan(int end, const FfnWeights &w, uint64_t rows, bool exact) {
   const uint32_t steps = (w.dim + FFN_BLOCK - 1) / FFN_BLOCK;
   FfnPlan p = {end, 256, 256, 1, steps, exact};
   if (rows == 0) return p;
+  if (end != FFN_GATED_BACK && rows <= FFN_FEW_ROWS) {
+    p.rows_tile = p.width_tile = 0;
+    return p;
+  }
   const auto tiles = [&]() { return (rows + p.rows_tile - 1) / p.rows_tile * ((w.rows + p.width_tile - 1) / p.width_tile); };
   if (end != FFN_LINEAR) {
     p.width_tile = 128;
@@ -554,6 +733,10 @@ FfnPlan ffn_plan(int end, const FfnWeights &w, uint64_t rows, bool exact) {
 
 hipError_t launch_ffn(const FfnPlan &p, const FfnRows8 &x, const FfnWeights &w, const FfnOut &o, hipStream_t s) {
   if (x.rows == 0) return hipSuccess;
+  if (p.rows_tile == 0) {
+    const ProductArgs a = {x, w, o, 0, 0, x.blocks};
+    return w.fmt == FMT_INT4 ? launch_few<FMT_INT4>(p, a, s) : launch_few<FMT_FP8>(p, a, s);
+  }
   if (p.end == FFN_GATED) {
     if (p.rows_tile == 256) return launch_tiles<4, 8, FFN_GATED, false>(x, w, o, s);
     if (p.rows_tile == 128) return launch_tiles<2, 8, FFN_GATED, false>(x, w, o, s);
