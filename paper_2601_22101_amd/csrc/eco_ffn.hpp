@@ -8,12 +8,11 @@ namespace eco {
 
 constexpr uint64_t FFN_MOST_ROWS = 1ull << 23, FFN_MOST_DIM = 1ull << 16, FFN_MOST_STRIDE = 1ull << 23;
 constexpr uint32_t FFN_BLOCK = 128;               // elements of a row to a scale: one step of the 8-bit products
-// Parts that a product's inner axis is summed in, and what the parts may take: a workspace is asked for once, for the most rows, and has to hold any call with fewer.
-constexpr uint64_t FFN_MOST_SPLITS = 32;
-constexpr uint64_t FFN_MOST_PARTIAL = 256ull * 64 * 128;       // elements, 8-bit products: they are split where there are less than 256 of the smallest tiles
+// A product's tiles go out in whole rounds over the compute units; those of the last, partial round are split along the inner axis, and their parts joined by a kernel
+// of their own.  What the parts may take: a workspace is asked for once, for the most rows, and has to hold any call with fewer.
+constexpr uint32_t FFN_UNITS = 256;
+constexpr uint64_t FFN_MOST_SPLITS = 16, FFN_MOST_PARTIAL = 1ull << 24;      // elements
 constexpr uint64_t FFN_FEW_ROWS = 64;                          // the kernel for few rows; the gated unit's leaves h in fp32 as a partial
-constexpr uint64_t FFN_MOST_INPUT_ROWS = 32768;                // rows of all parts of grad_input
-constexpr uint64_t FFN_MOST_WEIGHTS_PARTIAL = 1ull << 26;      // elements of all parts of grad_weights
 
 constexpr uint64_t ffn_round_up(uint64_t x, uint64_t k) { return (x + k - 1) / k * k; }
 
@@ -60,8 +59,8 @@ struct FfnOut {
   const void *add;                                // linear
   void *out;
   uint64_t add_stride, out_stride;
-  float *partial;                                 // linear: [splits][rows][out_dim], joined by launch_ffn_join; null: written at once; gated, few rows: [rows][width]
-  uint32_t splits, split_steps;
+  float *partial;                                 // linear: [splits][tiles from `whole` on][tile], joined by launch_ffn_join; gated, few rows: [rows][width]
+  uint32_t whole, splits, split_steps;            // tiles that are not split, parts of the others
   int32_t bf16, act;
   uint8_t *scales;                                // gated: out are codes
   const uint16_t *grad_out;                       // the gated unit's backward pass: out is [rows][2 half] bf16, ga then gb, with zeros from width to half
@@ -71,10 +70,15 @@ struct FfnOut {
 enum : int { FFN_LINEAR = 0, FFN_GATED = 1, FFN_GATED_BACK = 2 };
 
 // Tiles of an 8-bit product: rows of x to a tile; 0: the kernel for few rows, which takes weights as they are stored.
-struct FfnPlan { int end, rows_tile, width_tile; uint32_t splits, split_steps; bool exact; };
+struct FfnSplit { uint32_t whole, tail, splits, split_steps; uint64_t partial; };      // partial: elements of all parts
+struct FfnPlan { int end, rows_tile, width_tile; bool exact; FfnSplit split; };
 FfnPlan ffn_plan(int end, const FfnWeights &, uint64_t rows, bool exact);      // exact: sums for an output in fp32
 hipError_t launch_ffn(const FfnPlan &, const FfnRows8 &, const FfnWeights &, const FfnOut &, hipStream_t);
-hipError_t launch_ffn_join(const FfnOut &, uint32_t rows, uint32_t width, hipStream_t);
+hipError_t launch_ffn_join(const FfnPlan &, const FfnRows8 &, const FfnWeights &, const FfnOut &, hipStream_t);
+// What a tile costs in microseconds, a step of the inner axis and beside them, for the plans.
+struct FfnTile { uint32_t x, y; double step, tile; };
+// The best split of `tiles` tiles with `steps` steps each over `units` places, and what it costs.
+double ffn_split(uint64_t tiles, uint64_t steps, uint64_t units, uint64_t least_steps, const FfnTile &, FfnSplit *);
 // INT4 codes as the E4M3 codes of the same values (one matrix).
 hipError_t launch_ffn_expand(const void *codes, uint64_t numel, void *out, hipStream_t);
 
@@ -91,12 +95,11 @@ struct FfnProduct {
   uint64_t ldy;
   void *out[2];                                   // bf16
   uint64_t out_stride;
-  float *partial;                                 // [splits][matrices][ny][nx]; null: out is written at once
-  uint32_t splits, split_steps;
+  float *partial;                                 // [splits][tiles from `whole` on][tile]
+  uint32_t whole, splits, split_steps;
 };
-struct FfnGradPlan { int shape; uint32_t splits, split_steps; };
-// most_splits: what the workspace has room for.
-FfnGradPlan ffn_grad_plan(uint64_t nx, uint64_t ny, uint64_t k, uint32_t matrices, uint64_t most_splits);
+struct FfnGradPlan { int shape; FfnSplit split; };
+FfnGradPlan ffn_grad_plan(uint64_t nx, uint64_t ny, uint64_t k, uint32_t matrices);
 hipError_t launch_ffn_grad(const FfnGradPlan &, bool columns, const FfnProduct &, hipStream_t);
 
 }  // namespace eco

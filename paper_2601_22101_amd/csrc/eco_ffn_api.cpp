@@ -145,6 +145,11 @@ struct Places {
   uint64_t take(uint64_t n) { const uint64_t here = bytes; bytes += eco::ffn_round_up(n, 256); return here; }
 };
 
+// What the parts of a product of up to ny x nx results may take: split tiles are at most 256 x 256.
+uint64_t most_partial(uint64_t ny, uint64_t nx, uint64_t matrices) {
+  return least(eco::FFN_MOST_PARTIAL, eco::FFN_MOST_SPLITS * eco::ffn_round_up(ny, 256) * eco::ffn_round_up(nx, 256) * matrices);
+}
+
 // A product in 8 bits: INT4 weights as E4M3, and the parts of sums.
 struct Forward {
   eco::FfnPlan plan;
@@ -157,20 +162,23 @@ Forward forward_of(const Unit &u, int end, Room room, Places &p, bool exact = fa
   Forward f;
   std::memset(&f, 0, sizeof f);
   if (room == MOST) {
+    if (u.rows <= eco::FFN_FEW_ROWS && end != eco::FFN_GATED_BACK) {
+      if (end == eco::FFN_GATED) (void)p.take(4 * u.rows * u.width);
+      return f;
+    }
     if (u.fmt == ECO_FMT_INT4)
       for (uint32_t m = 0; m < u.matrices; ++m) (void)p.take(u.width * u.dim);
-    const uint64_t all = blocks_of(u.dim) / 4 * u.rows * u.width;
-    if (end == eco::FFN_GATED) (void)p.take(4 * least(u.rows, eco::FFN_FEW_ROWS) * u.width);
-    if (end == eco::FFN_LINEAR) (void)p.take(4 * (all < eco::FFN_MOST_PARTIAL ? all : eco::FFN_MOST_PARTIAL));
+    if (end == eco::FFN_GATED) (void)p.take(4 * eco::FFN_FEW_ROWS * u.width);
+    if (end == eco::FFN_LINEAR) (void)p.take(4 * most_partial(u.rows, u.width, 1));
     return f;
   }
   f.plan = eco::ffn_plan(end, weights_of(u), u.rows, exact);
   f.expands = u.fmt == ECO_FMT_INT4 && f.plan.rows_tile && u.rows;
   if (f.expands)
     for (uint32_t m = 0; m < u.matrices; ++m) f.expanded[m] = p.take(u.width * u.dim);
-  f.joins = f.plan.splits > 1;
+  f.joins = f.plan.split.splits > 1;
   f.rounds = end == eco::FFN_GATED && !f.plan.rows_tile;
-  if (f.joins || f.rounds) f.partial = p.take(4ull * f.plan.splits * u.rows * u.width);
+  if (f.joins || f.rounds) f.partial = p.take(4 * (f.joins ? f.plan.split.partial : u.rows * u.width));
   return f;
 }
 eco_status_t product(const Unit &u, const Forward &f, eco::FfnOut o, char *ws, hipStream_t s) {
@@ -182,11 +190,12 @@ eco_status_t product(const Unit &u, const Forward &f, eco::FfnOut o, char *ws, h
     }
     w.fmt = ECO_FMT_FP8_E4M3;
   }
-  o.splits = f.plan.splits;
-  o.split_steps = f.plan.split_steps;
+  o.whole = f.plan.split.whole;
+  o.splits = f.plan.split.splits;
+  o.split_steps = f.plan.split.split_steps;
   if (f.joins || f.rounds) o.partial = reinterpret_cast<float *>(ws + f.partial);
   LAUNCH(u.what, eco::launch_ffn(f.plan, rows_of(u), w, o, s));
-  if (f.joins) LAUNCH(u.what, eco::launch_ffn_join(o, static_cast<uint32_t>(u.rows), static_cast<uint32_t>(u.width), s));
+  if (f.joins) LAUNCH(u.what, eco::launch_ffn_join(f.plan, rows_of(u), w, o, s));
   return ECO_OK;
 }
 
@@ -205,17 +214,16 @@ Backward backward_of(const Unit &u, bool input, bool weights, bool copies, Room 
   b.copies = copies;
   if (copies) b.grad = p.take(2ull * u.rows * b.half * u.matrices);
   if (input && u.rows) {
-    const uint64_t most = least(eco::FFN_MOST_SPLITS, eco::FFN_MOST_INPUT_ROWS / u.rows);
     b.w = p.take(2ull * u.matrices * b.half * u.dim);
-    if (room == EXACT) b.input = eco::ffn_grad_plan(u.dim, u.rows, u.matrices == 2 ? 2 * b.half : u.width, 1, most);
-    if (room == MOST) (void)p.take(4ull * least(eco::FFN_MOST_SPLITS * u.rows, eco::FFN_MOST_INPUT_ROWS) * u.dim);
-    else if (b.input.splits > 1) b.input_partial = p.take(4ull * b.input.splits * u.rows * u.dim);
+    if (room == EXACT) b.input = eco::ffn_grad_plan(u.dim, u.rows, u.matrices == 2 ? 2 * b.half : u.width, 1);
+    const uint64_t parts = room == EXACT ? b.input.split.partial : most_partial(u.rows, u.dim, 1);
+    if (parts) b.input_partial = p.take(4 * parts);
   }
   if (weights) {
-    const uint64_t each = u.matrices * u.width * u.dim, steps = b.padded_rows / GRAD_STEP, most = least(least(eco::FFN_MOST_SPLITS, steps / 4), eco::FFN_MOST_WEIGHTS_PARTIAL / each);
     b.x = p.take(2ull * b.padded_rows * u.dim);
-    if (room == EXACT) b.weights = eco::ffn_grad_plan(u.dim, u.width, u.rows, u.matrices, most);
-    if (room == MOST ? most > 1 : b.weights.splits > 1) b.weights_partial = p.take(4ull * (room == MOST ? most : b.weights.splits) * each);
+    if (room == EXACT) b.weights = eco::ffn_grad_plan(u.dim, u.width, u.rows, u.matrices);
+    const uint64_t parts = room == EXACT ? b.weights.split.partial : b.padded_rows > GRAD_STEP ? most_partial(u.width, u.dim, u.matrices) : 0;
+    if (parts) b.weights_partial = p.take(4 * parts);
   }
   return b;
 }
@@ -230,8 +238,8 @@ eco_status_t gradients(const Unit &u, const Backward &b, const void *grad, uint6
     p.x = reinterpret_cast<const uint16_t *>(ws + b.w); p.y = static_cast<const uint16_t *>(grad);
     p.ldx = p.nx = dim; p.ldy = ldy; p.ny = rows; p.k = u.matrices == 2 ? static_cast<uint32_t>(2 * b.half) : width; p.matrices = 1;
     p.out[0] = grad_input; p.out_stride = stride_or(grad_input_stride, u.dim);
-    p.splits = b.input.splits; p.split_steps = b.input.split_steps;
-    if (p.splits > 1) p.partial = reinterpret_cast<float *>(ws + b.input_partial);
+    p.whole = b.input.split.whole; p.splits = b.input.split.splits; p.split_steps = b.input.split.split_steps;
+    p.partial = reinterpret_cast<float *>(ws + b.input_partial);
     LAUNCH(u.what, eco::launch_ffn_grad(b.input, false, p, s));
   }
   if (grad_weights[0]) {
@@ -241,8 +249,8 @@ eco_status_t gradients(const Unit &u, const Backward &b, const void *grad, uint6
     p.x = reinterpret_cast<const uint16_t *>(ws + b.x); p.y = static_cast<const uint16_t *>(grad);
     p.ldx = p.nx = dim; p.ldy = ldy; p.ny = width; p.k = rows; p.matrices = u.matrices; p.y_offset = static_cast<uint32_t>(b.half);
     p.out[0] = grad_weights[0]; p.out[1] = grad_weights[1]; p.out_stride = u.dim;
-    p.splits = b.weights.splits; p.split_steps = b.weights.split_steps;
-    if (p.splits > 1) p.partial = reinterpret_cast<float *>(ws + b.weights_partial);
+    p.whole = b.weights.split.whole; p.splits = b.weights.split.splits; p.split_steps = b.weights.split.split_steps;
+    p.partial = reinterpret_cast<float *>(ws + b.weights_partial);
     LAUNCH(u.what, eco::launch_ffn_grad(b.weights, true, p, s));
   }
   return ECO_OK;

@@ -100,23 +100,32 @@ __global__ __launch_bounds__(T::THREADS) void eco_ffn_grad_kernel(GradArgs a) {
   const FfnProduct &p = a.p;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wx = wave % T::WX * (NI * 32), wy = wave / T::WX * (NJ * 32);
-  const uint32_t all_tiles = a.tiles_x * a.tiles_y * p.matrices * p.splits, tail = p.k % KSTEP;
+  const uint32_t each = a.tiles_x * a.tiles_y, split_tiles = each * p.matrices - p.whole, all_tiles = p.whole + split_tiles * p.splits, tail = p.k % KSTEP;
   const uint64_t step_x = static_cast<uint64_t>(KSTEP) * p.ldx, step_y = Y_COLUMN ? KSTEP * p.ldy : KSTEP;
   const uint32_t last_piece_y = (p.ny + 7) / 8 * 8 - 8;
 
-  struct Where { uint32_t x0, y0, matrix, split, first, steps; };
+  struct Where { uint32_t x0, y0, matrix, block, first, steps; };
+  constexpr uint32_t NO_BLOCK = ~0u;                           // the place of a split tile's part
   const auto where = [&](uint32_t id) {
-    uint32_t tile = xcd_run(id, all_tiles);
     Where w;
-    const uint32_t each = a.tiles_x * a.tiles_y;
-    w.split = tile / (each * p.matrices);
-    tile -= w.split * each * p.matrices;
+    uint32_t tile;
+    if (id < p.whole) {
+      tile = xcd_run(id, p.whole);
+      w.block = NO_BLOCK;
+      w.first = 0;
+      w.steps = a.steps;
+    } else {
+      w.block = xcd_run(id - p.whole, all_tiles - p.whole);
+      const uint32_t split = w.block / split_tiles;
+      tile = p.whole + w.block - split * split_tiles;
+      w.first = split * p.split_steps;
+      w.steps = min(p.split_steps, a.steps - w.first);
+      if (p.splits == 1) w.block = NO_BLOCK;
+    }
     w.matrix = tile / each;
     tile -= w.matrix * each;
     w.y0 = tile / a.tiles_x * T::BY;
     w.x0 = tile % a.tiles_x * T::BX;
-    w.first = w.split * p.split_steps;
-    w.steps = min(p.split_steps, a.steps - w.first);
     return w;
   };
 
@@ -243,16 +252,15 @@ __global__ __launch_bounds__(T::THREADS) void eco_ffn_grad_kernel(GradArgs a) {
     int end_lane = lane;
     asm volatile("" : "+v"(end_lane));
     lds_char *const own = (lds_char *)smem + T::DEPTH * T::STEP_BYTES + wave * OWN;
-    if (p.partial) {
-      float *const out = p.partial + (static_cast<uint64_t>(w.split) * p.matrices + w.matrix) * p.ny * p.nx;
+    if (w.block != NO_BLOCK) {
+      float *const out = p.partial + static_cast<uint64_t>(w.block) * T::BX * T::BY;
 #pragma unroll
       for (int j = 0; j < NJ; ++j)
 #pragma unroll
         for (int i = 0; i < NI; ++i) {
           put_f32(own, end_lane, acc[i][j]);
           eco::take<8>(own, end_lane, [&](uint32_t row, uint32_t piece, uint4 v) {
-            const uint32_t y = w.y0 + wy + 32 * j + row, x = w.x0 + wx + 32 * i + 4 * piece;
-            if (y < p.ny && x < p.nx) *reinterpret_cast<uint4 *>(out + static_cast<uint64_t>(y) * p.nx + x) = v;      // nx is whole sixteens
+            *reinterpret_cast<uint4 *>(out + (wy + 32 * j + row) * T::BX + wx + 32 * i + 4 * piece) = v;
           });
         }
     } else {
@@ -288,44 +296,52 @@ __global__ __launch_bounds__(T::THREADS) void eco_ffn_grad_kernel(GradArgs a) {
   }
 }
 
-// Parts of the sums, added in their order and rounded: eight neighbours a thread.
-__global__ __launch_bounds__(256) void eco_ffn_grad_join_kernel(FfnProduct p) {
-  const uint64_t each = static_cast<uint64_t>(p.ny) * p.nx, all = each * p.matrices;
-  const uint32_t chunks = p.nx / 8;
-  for (uint64_t i = static_cast<uint64_t>(blockIdx.x) * 256 + threadIdx.x; i < all / 8; i += static_cast<uint64_t>(gridDim.x) * 256) {
-    float v[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-    for (uint32_t s = 0; s < p.splits; ++s) {
-      const float4 *from = reinterpret_cast<const float4 *>(p.partial + s * all + i * 8);
-      const float4 u = from[0], t = from[1];
-      v[0] += u.x; v[1] += u.y; v[2] += u.z; v[3] += u.w;
-      v[4] += t.x; v[5] += t.y; v[6] += t.z; v[7] += t.w;
-    }
-    const uint64_t matrix = i >= each / 8, in = i - matrix * (each / 8), y = in / chunks, x = (in - y * chunks) * 8;
-    uint16_t *to = static_cast<uint16_t *>(matrix ? p.out[1] : p.out[0]) + y * p.out_stride + x;
-    const uint32_t w[4] = {f32x2_to_bf16x2_rne(v[0], v[1]), f32x2_to_bf16x2_rne(v[2], v[3]), f32x2_to_bf16x2_rne(v[4], v[5]), f32x2_to_bf16x2_rne(v[6], v[7])};
-    if ((reinterpret_cast<uintptr_t>(to) & 15) == 0) *reinterpret_cast<uint4 *>(to) = make_uint4(w[0], w[1], w[2], w[3]);
-    else
-#pragma unroll
-      for (int e = 0; e < 8; ++e) to[e] = static_cast<uint16_t>(w[e / 2] >> (16 * (e & 1)));
+// The parts of split tiles, added in their order and rounded: eight neighbours a thread.
+__global__ __launch_bounds__(256) void eco_ffn_grad_join_kernel(GradArgs a, uint32_t bx, uint32_t by) {
+  const FfnProduct &p = a.p;
+  const uint32_t each = a.tiles_x * a.tiles_y, split_tiles = each * p.matrices - p.whole, chunks = bx / 8, per_tile = chunks * by / 256;
+  const uint32_t nth = blockIdx.x / per_tile, in = blockIdx.x % per_tile * 256 + threadIdx.x, row = in / chunks, column = in % chunks * 8;
+  uint32_t tile = p.whole + nth;
+  const uint32_t matrix = tile / each;
+  tile -= matrix * each;
+  const uint32_t y = tile / a.tiles_x * by + row, x = tile % a.tiles_x * bx + column;
+  if (y >= p.ny || x >= p.nx) return;
+  const float *from = p.partial + (static_cast<uint64_t>(nth) * by + row) * bx + column;
+  float v[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+#pragma unroll 4
+  for (uint32_t s = 0; s < p.splits; ++s) {
+    const float4 *at = reinterpret_cast<const float4 *>(from + static_cast<uint64_t>(s) * split_tiles * bx * by);
+    const float4 u = at[0], t = at[1];
+    v[0] += u.x; v[1] += u.y; v[2] += u.z; v[3] += u.w;
+    v[4] += t.x; v[5] += t.y; v[6] += t.z; v[7] += t.w;
   }
+  uint16_t *to = static_cast<uint16_t *>(matrix ? p.out[1] : p.out[0]) + y * p.out_stride + x;
+  const uint32_t w[4] = {f32x2_to_bf16x2_rne(v[0], v[1]), f32x2_to_bf16x2_rne(v[2], v[3]), f32x2_to_bf16x2_rne(v[4], v[5]), f32x2_to_bf16x2_rne(v[6], v[7])};
+  if ((reinterpret_cast<uintptr_t>(to) & 15) == 0) *reinterpret_cast<uint4 *>(to) = make_uint4(w[0], w[1], w[2], w[3]);
+  else
+#pragma unroll
+    for (int e = 0; e < 8; ++e) to[e] = static_cast<uint16_t>(w[e / 2] >> (16 * (e & 1)));
 }
 
 using Large = Tile<256, 256, 2, 4, 2>;
 using Large192 = Tile<192, 256, 2, 4, 2>;
+using Large128 = Tile<128, 256, 2, 4, 2>;
 using Medium = Tile<128, 128, 2, 2, 2>;
-constexpr uint64_t UNITS = 256;
 
 uint64_t ceil_div(uint64_t a, uint64_t b) { return (a + b - 1) / b; }
 uint32_t grid_of(uint64_t work) { const uint64_t g = ceil_div(work, 256); return static_cast<uint32_t>(g < 1 ? 1 : g < 8192 ? g : 8192); }
 
-struct Shape { uint32_t x, y, at_once; };
-Shape shape_of(int shape) { return shape == 2 ? Shape{256, 256, 1} : shape == 1 ? Shape{192, 256, 1} : Shape{128, 128, 2}; }
+// By shape: 128 x 128, of which a compute unit holds two, then 128, 192 and 256 x 256.
+constexpr int SHAPES = 4;
+FfnTile tile_of(int shape) {
+  constexpr FfnTile tiles[SHAPES] = {{128, 128, 1.1, 3.0}, {128, 256, 1.0, 3.0}, {192, 256, 1.43, 4.0}, {256, 256, 1.85, 5.0}};
+  return tiles[shape];
+}
+uint32_t units_of(int shape) { return shape == 0 ? 2 * FFN_UNITS : FFN_UNITS; }
 
 template <bool Y_COLUMN, class T>
-hipError_t launch_grad_tiles(const FfnProduct &p, uint32_t at_once, hipStream_t s) {
-  const GradArgs a = {p, static_cast<uint32_t>(ceil_div(p.nx, T::BX)), static_cast<uint32_t>(ceil_div(p.ny, T::BY)), static_cast<uint32_t>(ceil_div(p.k, KSTEP))};
-  const uint64_t tiles = static_cast<uint64_t>(a.tiles_x) * a.tiles_y * p.matrices * p.splits;
-  eco_ffn_grad_kernel<Y_COLUMN, T><<<static_cast<uint32_t>(tiles < UNITS * at_once ? tiles : UNITS * at_once), T::THREADS, 0, s>>>(a);
+hipError_t launch_grad_tiles(const GradArgs &a, uint64_t items, uint32_t units, hipStream_t s) {
+  eco_ffn_grad_kernel<Y_COLUMN, T><<<static_cast<uint32_t>(items < units ? items : units), T::THREADS, 0, s>>>(a);
   return hipGetLastError();
 }
 
@@ -348,35 +364,36 @@ hipError_t launch_ffn_pad(const void *src, uint64_t src_stride, uint32_t rows, u
   return hipGetLastError();
 }
 
-FfnGradPlan ffn_grad_plan(uint64_t nx, uint64_t ny, uint64_t k, uint32_t matrices, uint64_t most_splits) {
-  const uint64_t steps = ceil_div(k, KSTEP);
-  FfnGradPlan best = {0, 1, static_cast<uint32_t>(steps)};
+FfnGradPlan ffn_grad_plan(uint64_t nx, uint64_t ny, uint64_t k, uint32_t matrices) {
+  FfnGradPlan best = {};
   double least = 0;
-  for (int shape = 0; shape <= 2; ++shape) {
-    const Shape t = shape_of(shape);
-    const uint64_t tiles = ceil_div(nx, t.x) * ceil_div(ny, t.y) * matrices;
-    for (uint64_t n = 1; n == 1 || (n <= most_splits && n * 4 <= steps); ++n) {
-      // in steps of a 256 x 256 tile: whole rounds of tiles, with what a tile costs beside its steps, and the parts' way through memory
-      const double each = shape == 0 ? 0.62 : shape == 1 ? 0.78 : 1.0;      // (two of the small ones at once on a compute unit)
-      const double rounds = static_cast<double>(ceil_div(tiles * n, UNITS * t.at_once));
-      const double cost = rounds * (static_cast<double>(ceil_div(steps, n)) * each + 8 * each) + (n > 1 ? 4 + 0.5 * static_cast<double>(n * matrices * nx * ny) * 10 / 5e6 : 0);
-      if ((shape == 0 && n == 1) || cost < 0.98 * least) {
-        least = cost;
-        const uint64_t each_steps = ceil_div(steps, n);
-        best = {shape, static_cast<uint32_t>(each_steps ? ceil_div(steps, each_steps) : 1), static_cast<uint32_t>(each_steps)};
-      }
-    }
+  for (int shape = 0; shape < SHAPES; ++shape) {
+    const FfnTile t = tile_of(shape);
+    FfnSplit split;
+    const double cost = ffn_split(ceil_div(nx, t.x) * ceil_div(ny, t.y) * matrices, ceil_div(k, KSTEP), units_of(shape), 4, t, &split);
+    if (shape == 0 || cost < least) { least = cost; best = {shape, split}; }
   }
   return best;
 }
 
 hipError_t launch_ffn_grad(const FfnGradPlan &plan, bool columns, const FfnProduct &p, hipStream_t s) {
   if (p.ny == 0) return hipSuccess;
-  hipError_t e;
-  if (columns) e = plan.shape == 2 ? launch_grad_tiles<true, Large>(p, 1, s) : plan.shape == 1 ? launch_grad_tiles<true, Large192>(p, 1, s) : launch_grad_tiles<true, Medium>(p, 2, s);
-  else e = plan.shape == 2 ? launch_grad_tiles<false, Large>(p, 1, s) : plan.shape == 1 ? launch_grad_tiles<false, Large192>(p, 1, s) : launch_grad_tiles<false, Medium>(p, 2, s);
-  if (e != hipSuccess || !p.partial) return e;
-  eco_ffn_grad_join_kernel<<<grid_of(static_cast<uint64_t>(p.matrices) * p.ny * (p.nx / 8)), 256, 0, s>>>(p);
+  const FfnTile t = tile_of(plan.shape);
+  const GradArgs a = {p, static_cast<uint32_t>(ceil_div(p.nx, t.x)), static_cast<uint32_t>(ceil_div(p.ny, t.y)), static_cast<uint32_t>(ceil_div(p.k, KSTEP))};
+  const uint64_t items = plan.split.whole + static_cast<uint64_t>(plan.split.tail) * plan.split.splits;
+  const uint32_t units = units_of(plan.shape);
+  const auto go = [&](auto y_column) {
+    constexpr bool Y = decltype(y_column)::value;
+    switch (plan.shape) {
+      case 0: return launch_grad_tiles<Y, Medium>(a, items, units, s);
+      case 1: return launch_grad_tiles<Y, Large128>(a, items, units, s);
+      case 2: return launch_grad_tiles<Y, Large192>(a, items, units, s);
+      default: return launch_grad_tiles<Y, Large>(a, items, units, s);
+    }
+  };
+  const hipError_t e = columns ? go(std::true_type{}) : go(std::false_type{});
+  if (e != hipSuccess || plan.split.splits == 1) return e;
+  eco_ffn_grad_join_kernel<<<plan.split.tail * (t.x * t.y / 2048), 256, 0, s>>>(a, t.x, t.y);
   return hipGetLastError();
 }
 

@@ -139,20 +139,30 @@ __global__ __launch_bounds__(THREADS) void eco_ffn_kernel(ProductArgs a) {
   static_assert(sizeof smem <= 163840, "a compute unit's LDS");
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wn = wave % WAVES_N, wm = wave / WAVES_N * 16 * MI;
-  const uint32_t all_tiles = a.tiles_n * a.tiles_m * a.o.splits, tail = a.w.dim % STEP;
+  const uint32_t split_tiles = a.tiles_n * a.tiles_m - a.o.whole, all_tiles = a.o.whole + split_tiles * a.o.splits, tail = a.w.dim % STEP;
 
-  struct Where { uint32_t m0, n0, split, first, steps; };
+  struct Where { uint32_t m0, n0, block, first, steps; };
+  constexpr uint32_t NO_BLOCK = ~0u;                           // the place of a split tile's part
   const auto where = [&](uint32_t id) {
-    // eight tiles of rows beside each other, then the next columns: neighbours on an XCD share operands
-    uint32_t tile = xcd_run(id, all_tiles);
     Where w;
-    w.split = tile / (a.tiles_n * a.tiles_m);
-    tile -= w.split * a.tiles_n * a.tiles_m;
+    uint32_t tile;
+    if (id < a.o.whole) {
+      tile = xcd_run(id, a.o.whole);
+      w.block = NO_BLOCK;
+      w.first = 0;
+      w.steps = a.steps;
+    } else {
+      w.block = xcd_run(id - a.o.whole, all_tiles - a.o.whole);
+      const uint32_t split = w.block / split_tiles;
+      tile = a.o.whole + w.block - split * split_tiles;
+      w.first = split * a.o.split_steps;
+      w.steps = min(a.o.split_steps, a.steps - w.first);
+      if (a.o.splits == 1) w.block = NO_BLOCK;
+    }
+    // eight tiles of rows beside each other, then the next columns: neighbours on an XCD share operands
     const uint32_t run = 8 * a.tiles_n, band = tile / run, high = min(8u, a.tiles_m - band * 8), in = tile - band * run;
     w.m0 = (band * 8 + in % high) * T::BM;
     w.n0 = in / high * T::COLUMNS;
-    w.first = w.split * a.o.split_steps;
-    w.steps = min(a.o.split_steps, a.steps - w.first);
     return w;
   };
 
@@ -352,9 +362,20 @@ __global__ __launch_bounds__(THREADS) void eco_ffn_kernel(ProductArgs a) {
     }
 
     if constexpr (END == FFN_LINEAR) {
-      const bool to_partial = a.o.partial != nullptr, as_bf16 = a.o.bf16 && !to_partial;
-      const uint64_t stride = to_partial ? a.w.rows : a.o.out_stride;
-      char *const out = to_partial ? reinterpret_cast<char *>(a.o.partial + static_cast<uint64_t>(w.split) * a.x.rows * a.w.rows) : static_cast<char *>(a.o.out);
+      if (w.block != NO_BLOCK) {
+        float *const to = a.o.partial + static_cast<uint64_t>(w.block) * T::BM * T::BN + (wm + row4) * T::BN + wn * 16 * RUN + RUN * c;
+#pragma unroll
+        for (int i = 0; i < MI; ++i)
+#pragma unroll
+          for (int r = 0; r < 4; ++r)
+#pragma unroll
+            for (int e = 0; e < RUN; e += 4)
+              *reinterpret_cast<float4 *>(to + (16 * i + r) * T::BN + e) = make_float4(acc[i][e][r], acc[i][e + 1][r], acc[i][e + 2][r], acc[i][e + 3][r]);
+        continue;
+      }
+      const bool as_bf16 = a.o.bf16;
+      const uint64_t stride = a.o.out_stride;
+      char *const out = static_cast<char *>(a.o.out);
       const bool whole = all && stride % (as_bf16 ? RUN : 4) == 0 && (reinterpret_cast<uintptr_t>(out) & (as_bf16 ? 2 * RUN - 1 : 15)) == 0;
       const bool whole_add = all && a.o.add_stride % (as_bf16 ? RUN : 4) == 0 && (reinterpret_cast<uintptr_t>(a.o.add) & (as_bf16 ? 2 * RUN - 1 : 15)) == 0;
 #pragma unroll
@@ -363,7 +384,7 @@ __global__ __launch_bounds__(THREADS) void eco_ffn_kernel(ProductArgs a) {
         for (int r = 0; r < 4; ++r) {
           const uint32_t m = m0 + wm + 16 * i + row4 + r;
           if (m >= a.x.rows || n >= a.w.rows) continue;
-          if (a.o.add && !to_partial) {
+          if (a.o.add) {
             const uint64_t from = m * a.o.add_stride + n;
             if (as_bf16) {
               const uint16_t *p = static_cast<const uint16_t *>(a.o.add) + from;
@@ -483,32 +504,42 @@ __global__ __launch_bounds__(THREADS) void eco_ffn_kernel(ProductArgs a) {
   wait_loads<0>();                                             // (nothing is on its way to LDS when it is given up)
 }
 
-// Parts of sums over the inner axis, added in their order.
-__global__ __launch_bounds__(256) void eco_ffn_join_kernel(FfnOut o, uint32_t rows, uint32_t width) {
-  const uint64_t all = static_cast<uint64_t>(rows) * width, step = static_cast<uint64_t>(gridDim.x) * 256 * 4;
-  for (uint64_t i = (static_cast<uint64_t>(blockIdx.x) * 256 + threadIdx.x) * 4; i < all; i += step) {
-    const int n = all - i < 4 ? static_cast<int>(all - i) : 4;
-    float v[4] = {0, 0, 0, 0};
-    if (n == 4 && all % 4 == 0) {
-      for (uint32_t p = 0; p < o.splits; ++p) {
-        const float4 u = *reinterpret_cast<const float4 *>(o.partial + p * all + i);
-        v[0] += u.x; v[1] += u.y; v[2] += u.z; v[3] += u.w;
+// The parts of split tiles, added in their order: four neighbours a thread.
+__global__ __launch_bounds__(256) void eco_ffn_join_kernel(ProductArgs a, uint32_t bm, uint32_t bn) {
+  const FfnOut &o = a.o;
+  const uint32_t split_tiles = a.tiles_n * a.tiles_m - o.whole, chunks = bn / 4, per_tile = chunks * bm / 256;
+  const uint32_t nth = blockIdx.x / per_tile, at = blockIdx.x % per_tile * 256 + threadIdx.x, row = at / chunks, column = at % chunks * 4, tile = o.whole + nth;
+  const uint32_t run = 8 * a.tiles_n, band = tile / run, high = min(8u, a.tiles_m - band * 8), in = tile - band * run;
+  const uint32_t m = (band * 8 + in % high) * bm + row, n = in / high * bn + column;
+  if (m >= a.x.rows || n >= a.w.rows) return;
+  const float *from = o.partial + (static_cast<uint64_t>(nth) * bm + row) * bn + column;
+  float v[4] = {0, 0, 0, 0};
+#pragma unroll 4
+  for (uint32_t p = 0; p < o.splits; ++p) {
+    const float4 u = *reinterpret_cast<const float4 *>(from + static_cast<uint64_t>(p) * split_tiles * bm * bn);
+    v[0] += u.x; v[1] += u.y; v[2] += u.z; v[3] += u.w;
+  }
+  const uint64_t to = m * o.out_stride + n, add = m * o.add_stride + n;
+  if (o.bf16) {
+    uint16_t *out = static_cast<uint16_t *>(o.out) + to;
+    const uint16_t *more = static_cast<const uint16_t *>(o.add) + add;
+    if (n + 4 <= a.w.rows && ((reinterpret_cast<uintptr_t>(out) | (o.add ? reinterpret_cast<uintptr_t>(more) : 0)) & 7) == 0) {
+      if (o.add) {
+        const uint2 u = *reinterpret_cast<const uint2 *>(more);
+        v[0] += bf16_lo(u.x); v[1] += bf16_hi(u.x); v[2] += bf16_lo(u.y); v[3] += bf16_hi(u.y);
       }
+      *reinterpret_cast<uint2 *>(out) = make_uint2(f32x2_to_bf16x2_rne(v[0], v[1]), f32x2_to_bf16x2_rne(v[2], v[3]));
     } else {
-      for (uint32_t p = 0; p < o.splits; ++p)
-        for (int e = 0; e < 4; ++e)
-          if (e < n) v[e] += o.partial[p * all + i + e];
-    }
-    for (int e = 0; e < 4; ++e) {
-      if (e >= n) break;
-      const uint64_t m = (i + e) / width, k = (i + e) % width;
-      if (o.bf16) {
-        if (o.add) v[e] += u2f(static_cast<uint32_t>(static_cast<const uint16_t *>(o.add)[m * o.add_stride + k]) << 16);
-        static_cast<uint16_t *>(o.out)[m * o.out_stride + k] = static_cast<uint16_t>(f32x2_to_bf16x2_rne(v[e], 0.0f));
-      } else {
-        if (o.add) v[e] += static_cast<const float *>(o.add)[m * o.add_stride + k];
-        static_cast<float *>(o.out)[m * o.out_stride + k] = v[e];
+      for (int e = 0; e < 4; ++e) {
+        if (n + e >= a.w.rows) break;
+        if (o.add) v[e] += u2f(static_cast<uint32_t>(more[e]) << 16);
+        out[e] = static_cast<uint16_t>(f32x2_to_bf16x2_rne(v[e], 0.0f));
       }
+    }
+  } else {
+    for (int e = 0; e < 4; ++e) {
+      if (n + e >= a.w.rows) break;
+      static_cast<float *>(o.out)[to + e] = o.add ? v[e] + static_cast<const float *>(o.add)[add + e] : v[e];
     }
   }
 }
@@ -692,76 +723,85 @@ __global__ __launch_bounds__(256) void eco_ffn_expand_kernel(const uint32_t *cod
   for (uint64_t i = static_cast<uint64_t>(blockIdx.x) * 256 + threadIdx.x; i < words; i += static_cast<uint64_t>(gridDim.x) * 256) out[i] = e4m3_of_int4(codes[i]);
 }
 
-constexpr uint32_t UNITS = 256;                                // compute units
 template <int MI, int NJ, int END, bool EXACT>
-hipError_t launch_tiles(const FfnRows8 &x, const FfnWeights &w, const FfnOut &o, hipStream_t s) {
-  using T = Tile8<MI, NJ, END != FFN_LINEAR>;
-  const uint32_t tiles_n = (w.rows + T::COLUMNS - 1) / T::COLUMNS, tiles_m = (x.rows + T::BM - 1) / T::BM;
-  const ProductArgs a = {x, w, o, tiles_n, tiles_m, x.blocks};
-  const uint64_t all = static_cast<uint64_t>(tiles_n) * tiles_m * o.splits;
-  const uint32_t grid = static_cast<uint32_t>(all < UNITS ? all : UNITS);
-  if (w.group_blocks) eco_ffn_kernel<MI, NJ, END, true, EXACT><<<grid, THREADS, 0, s>>>(a);
+hipError_t launch_tiles(const FfnPlan &p, const ProductArgs &a, hipStream_t s) {
+  const uint64_t items = p.split.whole + static_cast<uint64_t>(p.split.tail) * p.split.splits;
+  const uint32_t grid = static_cast<uint32_t>(items < FFN_UNITS ? items : FFN_UNITS);
+  if (a.w.group_blocks) eco_ffn_kernel<MI, NJ, END, true, EXACT><<<grid, THREADS, 0, s>>>(a);
   else eco_ffn_kernel<MI, NJ, END, false, EXACT><<<grid, THREADS, 0, s>>>(a);
   return hipGetLastError();
+}
+uint64_t ceil_div(uint64_t a, uint64_t b) { return (a + b - 1) / b; }
+ProductArgs args_of(const FfnPlan &p, const FfnRows8 &x, const FfnWeights &w, const FfnOut &o) {
+  const uint32_t columns = p.width_tile ? p.width_tile : 1, rows = p.rows_tile ? p.rows_tile : 1;
+  return {x, w, o, static_cast<uint32_t>(ceil_div(w.rows, columns)), static_cast<uint32_t>(ceil_div(x.rows, rows)), x.blocks};
 }
 
 }  // namespace
 
+// Whole rounds, then the rest in as many parts as cost the least: their rounds, and their way through memory and a launch.
+double ffn_split(uint64_t tiles, uint64_t steps, uint64_t units, uint64_t least_steps, const FfnTile &t, FfnSplit *best) {
+  const uint64_t whole = tiles / units * units, tail = tiles - whole, area = static_cast<uint64_t>(t.x) * t.y;
+  const double of_whole = static_cast<double>(tiles / units) * (static_cast<double>(steps) * t.step + t.tile);
+  *best = {static_cast<uint32_t>(whole), static_cast<uint32_t>(tail), 1, static_cast<uint32_t>(steps), 0};
+  double least = tail ? static_cast<double>(steps) * t.step + t.tile : 0.0;
+  for (uint64_t n = 2; tail && n <= FFN_MOST_SPLITS && n * least_steps <= steps && n * tail * area <= FFN_MOST_PARTIAL; ++n) {
+    const uint64_t each = ceil_div(steps, n), parts = ceil_div(steps, each);
+    const double cost = static_cast<double>(ceil_div(tail * parts, units)) * (static_cast<double>(each) * t.step + t.tile) + 4.0 + static_cast<double>(parts * tail * area) * 8 / 5e6;
+    if (parts > 1 && cost < least) {
+      least = cost;
+      *best = {static_cast<uint32_t>(whole), static_cast<uint32_t>(tail), static_cast<uint32_t>(parts), static_cast<uint32_t>(each), parts * tail * area};
+    }
+  }
+  return of_whole + least;
+}
+
+// Microseconds of a step of 128 and of a tile's ends (8192 x 6912 and 8192 x 1024 over widths that are whole rounds: 256 x 256 122 and 26 us, 256 x 128 73 and 18,
+// 128 x 128 46 and 11.5, 64 x 128 33 and 8.9; gated, tiles of 256, 128 and 64 rows, 120 and 27, 75 and 17, 57 and 12).  In bf16 products a step is of twice the work.
 FfnPlan ffn_plan(int end, const FfnWeights &w, uint64_t rows, bool exact) {
   const uint32_t steps = (w.dim + FFN_BLOCK - 1) / FFN_BLOCK;
-  FfnPlan p = {end, 256, 256, 1, steps, exact};
+  FfnPlan p = {end, 256, 256, exact, {0, 0, 1, steps, 0}};
   if (rows == 0) return p;
   if (end != FFN_GATED_BACK && rows <= FFN_FEW_ROWS) {
     p.rows_tile = p.width_tile = 0;
     return p;
   }
-  const auto tiles = [&]() { return (rows + p.rows_tile - 1) / p.rows_tile * ((w.rows + p.width_tile - 1) / p.width_tile); };
-  if (end != FFN_LINEAR) {
-    p.width_tile = 128;
-    while (p.rows_tile > 64 && tiles() < 256) p.rows_tile /= 2;
-    return p;
+  const FfnTile linear[] = {{256, 256, 2.09, 4.5}, {128, 256, 1.2, 3.5}, {128, 128, 0.75, 2.0}, {128, 64, 0.51, 1.5}};
+  const FfnTile gated[] = {{128, 256, 2.04, 5.5}, {128, 128, 1.25, 3.5}, {128, 64, 0.97, 2.0}};
+  const FfnTile in_bf16[] = {{128, 256, 2.4, 3.5}, {128, 128, 1.4, 2.0}, {128, 64, 0.9, 1.5}};
+  const bool product = end == FFN_LINEAR;
+  const FfnTile *tiles = !product ? gated : exact ? in_bf16 : linear;
+  const int n = !product || exact ? 3 : 4;
+  double least = 0;
+  for (int i = 0; i < n; ++i) {
+    FfnSplit split;
+    // (the gated unit's ends want whole sums)
+    const double cost = ffn_split(ceil_div(w.rows, tiles[i].x) * ceil_div(rows, tiles[i].y), steps, FFN_UNITS, product ? 4 : steps + 1, tiles[i], &split);
+    if (i == 0 || cost < least) {
+      least = cost;
+      p.rows_tile = static_cast<int>(tiles[i].y);
+      p.width_tile = static_cast<int>(tiles[i].x);
+      p.split = split;
+    }
   }
-  if (exact || tiles() < 256) p.width_tile = 128;
-  while (p.rows_tile > 64 && tiles() < 256) p.rows_tile /= 2;
-  const uint64_t t = tiles();
-  uint32_t splits = t < 256 ? static_cast<uint32_t>(256 / t) : 1;
-  if (splits > steps / 4) splits = steps / 4 ? steps / 4 : 1;
-  p.split_steps = (steps + splits - 1) / splits;
-  p.splits = (steps + p.split_steps - 1) / p.split_steps;
   return p;
 }
 
 hipError_t launch_ffn(const FfnPlan &p, const FfnRows8 &x, const FfnWeights &w, const FfnOut &o, hipStream_t s) {
   if (x.rows == 0) return hipSuccess;
-  if (p.rows_tile == 0) {
-    const ProductArgs a = {x, w, o, 0, 0, x.blocks};
-    return w.fmt == FMT_INT4 ? launch_few<FMT_INT4>(p, a, s) : launch_few<FMT_FP8>(p, a, s);
-  }
-  if (p.end == FFN_GATED) {
-    if (p.rows_tile == 256) return launch_tiles<4, 8, FFN_GATED, false>(x, w, o, s);
-    if (p.rows_tile == 128) return launch_tiles<2, 8, FFN_GATED, false>(x, w, o, s);
-    return launch_tiles<1, 8, FFN_GATED, false>(x, w, o, s);
-  }
-  if (p.end == FFN_GATED_BACK) {
-    if (p.rows_tile == 256) return launch_tiles<4, 8, FFN_GATED_BACK, false>(x, w, o, s);
-    if (p.rows_tile == 128) return launch_tiles<2, 8, FFN_GATED_BACK, false>(x, w, o, s);
-    return launch_tiles<1, 8, FFN_GATED_BACK, false>(x, w, o, s);
-  }
-  if (p.exact) {
-    if (p.rows_tile == 256) return launch_tiles<4, 4, FFN_LINEAR, true>(x, w, o, s);
-    if (p.rows_tile == 128) return launch_tiles<2, 4, FFN_LINEAR, true>(x, w, o, s);
-    return launch_tiles<1, 4, FFN_LINEAR, true>(x, w, o, s);
-  }
-  if (p.width_tile == 256) return launch_tiles<4, 8, FFN_LINEAR, false>(x, w, o, s);
-  if (p.rows_tile == 256) return launch_tiles<4, 4, FFN_LINEAR, false>(x, w, o, s);
-  if (p.rows_tile == 128) return launch_tiles<2, 4, FFN_LINEAR, false>(x, w, o, s);
-  return launch_tiles<1, 4, FFN_LINEAR, false>(x, w, o, s);
+  const ProductArgs a = args_of(p, x, w, o);
+  if (p.rows_tile == 0) return w.fmt == FMT_INT4 ? launch_few<FMT_INT4>(p, a, s) : launch_few<FMT_FP8>(p, a, s);
+  const auto by_rows = [&](auto of_256, auto of_128, auto of_64) { return p.rows_tile == 256 ? of_256(p, a, s) : p.rows_tile == 128 ? of_128(p, a, s) : of_64(p, a, s); };
+  if (p.end == FFN_GATED) return by_rows(launch_tiles<4, 8, FFN_GATED, false>, launch_tiles<2, 8, FFN_GATED, false>, launch_tiles<1, 8, FFN_GATED, false>);
+  if (p.end == FFN_GATED_BACK)
+    return by_rows(launch_tiles<4, 8, FFN_GATED_BACK, false>, launch_tiles<2, 8, FFN_GATED_BACK, false>, launch_tiles<1, 8, FFN_GATED_BACK, false>);
+  if (p.exact) return by_rows(launch_tiles<4, 4, FFN_LINEAR, true>, launch_tiles<2, 4, FFN_LINEAR, true>, launch_tiles<1, 4, FFN_LINEAR, true>);
+  if (p.width_tile == 256) return launch_tiles<4, 8, FFN_LINEAR, false>(p, a, s);
+  return by_rows(launch_tiles<4, 4, FFN_LINEAR, false>, launch_tiles<2, 4, FFN_LINEAR, false>, launch_tiles<1, 4, FFN_LINEAR, false>);
 }
 
-hipError_t launch_ffn_join(const FfnOut &o, uint32_t rows, uint32_t width, hipStream_t s) {
-  const uint64_t all = (static_cast<uint64_t>(rows) * width + 1023) / 1024;
-  if (all == 0) return hipSuccess;
-  eco_ffn_join_kernel<<<static_cast<uint32_t>(all < 4096 ? all : 4096), 256, 0, s>>>(o, rows, width);
+hipError_t launch_ffn_join(const FfnPlan &p, const FfnRows8 &x, const FfnWeights &w, const FfnOut &o, hipStream_t s) {
+  eco_ffn_join_kernel<<<p.split.tail * (p.rows_tile * p.width_tile / 1024), 256, 0, s>>>(args_of(p, x, w, o), p.rows_tile, p.width_tile);
   return hipGetLastError();
 }
 
