@@ -65,23 +65,25 @@ struct ProductArgs {
   uint32_t tiles_n, tiles_m, steps;
 };
 
-// Past the registers, to LDS: a byte or a 16-bit value a lane as a dword, or a dword.
+// Loads to LDS as load_to_lds has them, which do not hold back the reads of LDS around them: those are of other steps' places, and the barriers between order them.
+__device__ __forceinline__ void step_to_lds(uint32_t lds, const void *base, uint32_t offset) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds), "v"(offset), "s"(base));
+}
+// From an address of each lane's own; a byte or a 16-bit value a lane as a dword, or a dword.
+__device__ __forceinline__ void lane_to_lds(uint32_t lds, const void *from) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds), "v"(from));
+}
 __device__ __forceinline__ void byte_to_lds(uint32_t lds, const void *base, uint32_t offset) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_ubyte %1, %2" ::"s"(lds), "v"(offset), "s"(base) : "memory");
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_ubyte %1, %2" ::"s"(lds), "v"(offset), "s"(base));
 }
 __device__ __forceinline__ void half_to_lds(uint32_t lds, const void *base, uint32_t offset) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_ushort %1, %2" ::"s"(lds), "v"(offset), "s"(base) : "memory");
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_ushort %1, %2" ::"s"(lds), "v"(offset), "s"(base));
 }
 __device__ __forceinline__ void dword_to_lds(uint32_t lds, const void *base, uint32_t offset) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2" ::"s"(lds), "v"(offset), "s"(base) : "memory");
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2" ::"s"(lds), "v"(offset), "s"(base));
 }
 
 __device__ const uint4 ffn_zeros = {0, 0, 0, 0};
-// The same as load_to_lds, from an address of each lane's own.
-__device__ __forceinline__ void lane_to_lds(uint32_t lds, const void *from) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds), "v"(from) : "memory");
-}
-
 // Where a lane's first 16 bytes of 16 rows of a step lie, from the first row's (a multiple of 16) on; the others are 64 bytes away, up or down.
 __device__ __forceinline__ uint32_t lane_place(int lane) {
   const int row = lane & 15;
@@ -130,9 +132,11 @@ struct Tile8 {
 // A workgroup goes through tiles gridDim.x apart; its loads do not stop between them: while a tile's results leave, the next tile's first steps are on their way.
 // EXACT: in bf16, whose instruction adds products as an fp32 sum does.  The one for 8 bits, twice as fast, leaves out of eight neighbouring products what is below 2^-13
 // of the largest of them: 2^-14 of a result of activations with outlying channels, far below its rounding to bf16 or 8 bits, but not to fp32.
-template <int MI, int NJ, int END, bool BY_BLOCK, bool EXACT>
+// SCALES: of the weights, BY_BLOCK, or BY_ROW of rows that are whole blocks, or BY_ROW_CUT of others.
+enum : int { BY_BLOCK = 0, BY_ROW = 1, BY_ROW_CUT = 2 };
+template <int MI, int NJ, int END, int SCALES, bool EXACT>
 __global__ __launch_bounds__(THREADS) void eco_ffn_kernel(ProductArgs a) {
-  constexpr bool GATED = END != FFN_LINEAR;
+  constexpr bool GATED = END != FFN_LINEAR, BLOCKS = SCALES == BY_BLOCK, CUT = SCALES == BY_ROW_CUT;
   using T = Tile8<MI, NJ, GATED>;
   constexpr int DEPTH = T::DEPTH, RUN = T::RUN;
   __shared__ __attribute__((aligned(1024))) char smem[DEPTH * T::STEP_BYTES + (END == FFN_GATED ? WAVES_N * T::BM * 4 : 0)];
@@ -172,15 +176,15 @@ __global__ __launch_bounds__(THREADS) void eco_ffn_kernel(ProductArgs a) {
   uint32_t piece_row, piece_k;
   row_piece(threadIdx.x, piece_row, piece_k);
   piece_k *= 2;
-  const bool past = tail && piece_k >= tail;
+  const bool past = CUT && piece_k >= tail;
   // the column of row p of the tile's weights in LDS, and its matrix, which is the same for the eight rows of a wave's load
   const auto column_of = [&](uint32_t p) { return p / (16 * NJ) * 16 * RUN + RUN * (p % 16) + p / 16 % NJ % RUN; };
   const auto matrix_of = [&](uint32_t p) { return GATED && p / 16 % NJ >= RUN; };
-  uint32_t load_id = blockIdx.x, step_at = 0, steps_left = 0, place = 0, last_m = 0, last_n = 0, scale_off = 0;
+  uint32_t load_id = blockIdx.x, step_at = 0, group = 0, steps_left = 0, place = 0, last_m = 0, last_n = 0, scale_off = 0;
   const uint32_t piece_column = column_of(piece_row);
   const uint8_t *x_from = nullptr, *xs_from = nullptr, *w_from[2] = {nullptr, nullptr};
   // one scale a thread and step: of the rows, then of the weights by matrix (whole waves of each; threads past the last repeat it)
-  const bool of_x = !BY_BLOCK || static_cast<uint32_t>(wave) < T::BM / 64;
+  const bool of_x = !BLOCKS || static_cast<uint32_t>(wave) < T::BM / 64;
   const uint32_t scale_p = min(threadIdx.x - (of_x ? 0u : T::BM), (of_x ? T::BM : T::BN) - 1u);
   const bool scale_up = GATED && !of_x && __builtin_amdgcn_readfirstlane(scale_p) >= T::COLUMNS;
   const char *const scales_from = static_cast<const char *>(scale_up ? a.w.scales[1] : a.w.scales[0]);
@@ -195,33 +199,35 @@ __global__ __launch_bounds__(THREADS) void eco_ffn_kernel(ProductArgs a) {
       scale_off = min(w.n0 + column, a.w.rows - 1) * a.w.scale_row * (a.w.scale_bf16 ? 2 : 4);
     }
     step_at = w.first;
+    group = BLOCKS ? w.first / a.w.group_blocks : 0;
     steps_left = w.steps;
     x_from = a.x.codes + w.m0 * a.x.stride + w.first * STEP;
     xs_from = a.x.scales + static_cast<uint64_t>(w.m0) * a.x.blocks + w.first;
 #pragma unroll
     for (int q = 0; q < (GATED ? 2 : 1); ++q) w_from[q] = static_cast<const uint8_t *>(a.w.data[q]) + static_cast<uint64_t>(w.n0) * a.w.dim + w.first * STEP;
   };
-  // (after the last tile the last step's loads are repeated, so that their number is the same in every step)
-  const auto issue = [&]() {
+  // One load of a step's codes.  (After the last tile the last step's loads are repeated, so that their number is the same in every step.)
+  const auto load = [&](int which) {
     const uint32_t to = lds0 + place * T::STEP_BYTES, lds = to + wave * 1024;
     // pieces past the row: of x the block's first, which the weights' zeros take out of the sums
-    const bool zero = past && step_at + 1 == a.steps;
-    const uint32_t x_k = zero ? 0 : piece_k;
-#pragma unroll
-    for (int i = 0; i < T::X_LOADS; ++i)                       // rows past the last repeat it, and are not stored
-      load_to_lds(lds + i * THREADS * 16, x_from, min(piece_row + 64 * i, last_m) * static_cast<uint32_t>(a.x.stride) + x_k);
-#pragma unroll
-    for (int i = 0; i < T::W_LOADS; ++i) {
-      const uint8_t *from = w_from[matrix_of(i * 64 + wave * 8)] + (min(piece_column + column_of(64 * i), last_n) * a.w.dim + piece_k);
-      lane_to_lds(lds + T::X_BYTES + i * THREADS * 16, zero ? reinterpret_cast<const uint8_t *>(&ffn_zeros) : from);
+    const bool zero = CUT && past && step_at + 1 == a.steps;
+    if (which < T::X_LOADS) {                                  // rows past the last repeat it, and are not stored
+      step_to_lds(lds + which * THREADS * 16, x_from, min(piece_row + 64 * which, last_m) * static_cast<uint32_t>(a.x.stride) + (zero ? 0 : piece_k));
+    } else {
+      const int i = which - T::X_LOADS;
+      const uint8_t *from = w_from[matrix_of(i * 64 + wave * 8)];
+      const uint32_t off = min(piece_column + column_of(64 * i), last_n) * a.w.dim + piece_k;
+      if constexpr (CUT) lane_to_lds(lds + T::X_BYTES + i * THREADS * 16, zero ? reinterpret_cast<const uint8_t *>(&ffn_zeros) : from + off);
+      else step_to_lds(lds + T::X_BYTES + i * THREADS * 16, from, off);
     }
-    const uint32_t to_scale = to + T::X_BYTES + T::W_BYTES + wave * 256;
-    if (of_x) byte_to_lds(to_scale, xs_from, scale_off);
-    else {
-      const uint32_t group = a.w.group_blocks == 1 ? step_at : step_at / a.w.group_blocks;
-      if (a.w.scale_bf16) half_to_lds(to_scale, scales_from + group * 2, scale_off);
-      else dword_to_lds(to_scale, scales_from + group * 4, scale_off);
-    }
+  };
+  const auto load_scale = [&]() {
+    const uint32_t to = lds0 + place * T::STEP_BYTES + T::X_BYTES + T::W_BYTES + wave * 256;
+    if (of_x) byte_to_lds(to, xs_from, scale_off);
+    else if (a.w.scale_bf16) half_to_lds(to, scales_from + group * 2, scale_off);
+    else dword_to_lds(to, scales_from + group * 4, scale_off);
+  };
+  const auto next_step = [&]() {
     place = place + 1 == DEPTH ? 0 : place + 1;
     if (load_id >= all_tiles) return;
     if (--steps_left == 0) {
@@ -234,6 +240,7 @@ __global__ __launch_bounds__(THREADS) void eco_ffn_kernel(ProductArgs a) {
     ++xs_from;
     w_from[0] += STEP;
     if (GATED) w_from[1] += STEP;
+    if (BLOCKS) group = a.w.group_blocks == 1 ? step_at : step_at / a.w.group_blocks;
   };
 
   // ---- the products' place
@@ -257,7 +264,7 @@ __global__ __launch_bounds__(THREADS) void eco_ffn_kernel(ProductArgs a) {
     const i32x8 f = operand(w_at[0], w_at[1], 16 * j);
     if constexpr (EXACT) gw[j & 1] = widen(f, 1.0f);
     else fw[j & 1] = f;
-    if constexpr (BY_BLOCK) {
+    if constexpr (BLOCKS) {
       const uint32_t bits = scale_w[GATED ? j / RUN * T::COLUMNS + 16 * (j % RUN) : 16 * j];
       sw[j & 1] = u2f(a.w.scale_bf16 ? bits << 16 : bits);
     }
@@ -271,22 +278,23 @@ __global__ __launch_bounds__(THREADS) void eco_ffn_kernel(ProductArgs a) {
       else fx[i] = f;
     }
   };
+  constexpr int LOADS_EACH = (T::LOADS + NJ - 2) / (NJ - 1);       // loads beside a fragment's products
   uint32_t at = 0;
   f32x4 acc[MI][NJ], part[2][MI];
   const auto products = [&](int j) {
     const f32x4 zero = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
     for (int i = 0; i < MI; ++i) {
-      const f32x4 c = BY_BLOCK ? zero : acc[i][j];
+      const f32x4 c = BLOCKS ? zero : acc[i][j];
       f32x4 v;
       if constexpr (EXACT) v = multiply(gx[i], gw[j & 1], c);
       else v = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(fx[i], fw[j & 1], c, 0, 0, 0, static_cast<int>(sx[i]), 0, 127);
-      if constexpr (BY_BLOCK) part[j & 1][i] = v;
+      if constexpr (BLOCKS) part[j & 1][i] = v;
       else acc[i][j] = v;
     }
   };
   const auto add = [&](int j, float s) {
-    if constexpr (BY_BLOCK)
+    if constexpr (BLOCKS)
 #pragma unroll
       for (int i = 0; i < MI; ++i)
 #pragma unroll
@@ -294,7 +302,12 @@ __global__ __launch_bounds__(THREADS) void eco_ffn_kernel(ProductArgs a) {
   };
 
   load_tile();
-  for (int i = 0; i < DEPTH - 1; ++i) issue();
+  for (int i = 0; i < DEPTH - 1; ++i) {
+    if (i) next_step();
+    load_scale();
+#pragma unroll
+    for (int l = 0; l < T::LOADS - 1; ++l) load(l);
+  }
   wait_loads<(DEPTH - 2) * T::LOADS>();
   barrier();
   go_to(0);
@@ -308,24 +321,27 @@ __global__ __launch_bounds__(THREADS) void eco_ffn_kernel(ProductArgs a) {
 #pragma unroll
       for (int j = 0; j < NJ; ++j) acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
     for (uint32_t s = 0; s < w.steps; ++s) {
-      issue();                                                 // into the last step's place, which every wave has read
-      // (from here on no branch, over which the compiler would carry the products)
-      __builtin_amdgcn_sched_barrier(0);
+      next_step();                                             // into the last step's place, which every wave has read
+      load_scale();
+      __builtin_amdgcn_sched_barrier(0);                       // (from here on no branch, over which the compiler would carry the products)
       float before = 0.0f;
 #pragma unroll
       for (int j = 0; j < NJ - 1; ++j) {
         const float mine = sw[j & 1];
         read_w(j + 1);
+#pragma unroll
+        for (int l = 0; l < T::LOADS - 1; ++l)
+          if (l / LOADS_EACH == j) load(l);
         products(j);
         if (j) add(j - 1, before);
         before = mine;
         // reads of LDS first, then a product and its share of the sums, and so on
         if constexpr (!EXACT) {
-          __builtin_amdgcn_sched_group_barrier(0x100, BY_BLOCK ? 3 : 2, 0);
+          __builtin_amdgcn_sched_group_barrier(0x100, BLOCKS ? 3 : 2, 0);
 #pragma unroll
           for (int i = 0; i < MI; ++i) {
             __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-            if (BY_BLOCK && j) __builtin_amdgcn_sched_group_barrier(0x002, 4, 0);
+            if (BLOCKS && j) __builtin_amdgcn_sched_group_barrier(0x002, 4, 0);
           }
         }
       }
@@ -348,7 +364,7 @@ __global__ __launch_bounds__(THREADS) void eco_ffn_kernel(ProductArgs a) {
     const int c = end_lane & 15, row4 = 4 * (end_lane >> 4);
     const uint32_t n = n0 + wn * 16 * RUN + RUN * c;           // the first of the lane's columns
     const bool all = n + RUN <= a.w.rows;
-    if constexpr (!BY_BLOCK) {
+    if constexpr (!BLOCKS) {
 #pragma unroll
       for (int j = 0; j < NJ; ++j) {
         const void *from = GATED && j >= RUN ? a.w.scales[1] : a.w.scales[0];
@@ -727,8 +743,9 @@ template <int MI, int NJ, int END, bool EXACT>
 hipError_t launch_tiles(const FfnPlan &p, const ProductArgs &a, hipStream_t s) {
   const uint64_t items = p.split.whole + static_cast<uint64_t>(p.split.tail) * p.split.splits;
   const uint32_t grid = static_cast<uint32_t>(items < FFN_UNITS ? items : FFN_UNITS);
-  if (a.w.group_blocks) eco_ffn_kernel<MI, NJ, END, true, EXACT><<<grid, THREADS, 0, s>>>(a);
-  else eco_ffn_kernel<MI, NJ, END, false, EXACT><<<grid, THREADS, 0, s>>>(a);
+  if (a.w.group_blocks) eco_ffn_kernel<MI, NJ, END, BY_BLOCK, EXACT><<<grid, THREADS, 0, s>>>(a);
+  else if (a.w.dim % STEP == 0) eco_ffn_kernel<MI, NJ, END, BY_ROW, EXACT><<<grid, THREADS, 0, s>>>(a);
+  else eco_ffn_kernel<MI, NJ, END, BY_ROW_CUT, EXACT><<<grid, THREADS, 0, s>>>(a);
   return hipGetLastError();
 }
 uint64_t ceil_div(uint64_t a, uint64_t b) { return (a + b - 1) / b; }
