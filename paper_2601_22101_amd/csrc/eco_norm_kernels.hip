@@ -22,25 +22,55 @@ __device__ __forceinline__ V loose(const void *p) {            // at an address 
 template <class V>
 __device__ __forceinline__ void put_loose(void *p, V v) { __builtin_memcpy(p, &v, sizeof v); }
 
-// Eight elements of a row from k on; those past dim are 0, or not written.
+// Eight elements of a row from k on, those past dim 0, in two halves: a load that no branch holds back, so that all of a row's are under way together, and their
+// values.  A piece that the row's end cuts is loaded from the last eight elements and shifted.
 template <bool BF16>
-__device__ __forceinline__ void read8(const void *row, uint32_t k, uint32_t dim, float (&v)[8]) {
-  if (k + 8 <= dim) {
-    if constexpr (BF16) {
-      const uint4 u = loose<uint4>(static_cast<const uint16_t *>(row) + k);
-      const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+struct Raw { uint4 u[BF16 ? 1 : 2]; };
+// ANY: of rows of less than eight elements too.
+template <bool BF16, bool ANY>
+__device__ __forceinline__ Raw<BF16> load8(const void *row, uint32_t k, uint32_t dim) {
+  constexpr int SIZE = BF16 ? 2 : 4;
+  Raw<BF16> r;
+  if (!ANY || dim >= 8) {
+    const char *from = static_cast<const char *>(row) + static_cast<uint64_t>(min(k, dim - 8)) * SIZE;
 #pragma unroll
-      for (int j = 0; j < 8; ++j) v[j] = (j & 1) ? bf16_hi(w[j / 2]) : bf16_lo(w[j / 2]);
-    } else {
-      const float4 a = loose<float4>(static_cast<const float *>(row) + k), b = loose<float4>(static_cast<const float *>(row) + k + 4);
-      v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+    for (int i = 0; i < (BF16 ? 1 : 2); ++i) r.u[i] = loose<uint4>(from + 16 * i);
+  } else {                                         // (by single elements, as if they were the row's last eight)
+    uint32_t e[8];
+#pragma unroll
+    for (uint32_t j = 0; j < 8; ++j) {
+      const bool there = j + dim >= 8;
+      const uint32_t at = there ? j + dim - 8 : 0;
+      e[j] = !there ? 0u : BF16 ? static_cast<const uint16_t *>(row)[at] : static_cast<const uint32_t *>(row)[at];
     }
-    return;
+    if constexpr (BF16) r.u[0] = make_uint4(e[0] | e[1] << 16, e[2] | e[3] << 16, e[4] | e[5] << 16, e[6] | e[7] << 16);
+    else { r.u[0] = make_uint4(e[0], e[1], e[2], e[3]); r.u[1] = make_uint4(e[4], e[5], e[6], e[7]); }
+  }
+  return r;
+}
+template <bool BF16>
+__device__ __forceinline__ void values8(const Raw<BF16> &r, uint32_t k, uint32_t dim, float (&v)[8]) {
+  if constexpr (BF16) {
+    const uint32_t w[4] = {r.u[0].x, r.u[0].y, r.u[0].z, r.u[0].w};
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = (j & 1) ? bf16_hi(w[j / 2]) : bf16_lo(w[j / 2]);
+  } else {
+    const uint32_t w[8] = {r.u[0].x, r.u[0].y, r.u[0].z, r.u[0].w, r.u[1].x, r.u[1].y, r.u[1].z, r.u[1].w};
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = u2f(w[j]);
+  }
+  if (dim % 8) {
+    const uint32_t shift = k + 8 <= dim ? 0 : k + 8 - dim;
+#pragma unroll
+    for (int bit = 4; bit; bit /= 2)
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[j] = shift & bit ? (j + bit < 8 ? v[j + bit] : 0.0f) : v[j];
   }
 #pragma unroll
-  for (int j = 0; j < 8; ++j)
-    v[j] = k + j >= dim ? 0.0f : BF16 ? u2f(static_cast<uint32_t>(static_cast<const uint16_t *>(row)[k + j]) << 16) : static_cast<const float *>(row)[k + j];
+  for (int j = 0; j < 8; ++j) v[j] = k < dim ? v[j] : 0.0f;
 }
+template <bool BF16, bool ANY>
+__device__ __forceinline__ void read8(const void *row, uint32_t k, uint32_t dim, float (&v)[8]) { values8<BF16>(load8<BF16, ANY>(row, k, dim), k, dim, v); }
 // The values are rounded to the type, and left so in `v`.
 template <bool BF16>
 __device__ __forceinline__ void write8(void *row, uint32_t k, uint32_t dim, float (&v)[8]) {
@@ -70,12 +100,13 @@ __device__ __forceinline__ void write8(void *row, uint32_t k, uint32_t dim, floa
     }
   }
 }
-__device__ __forceinline__ void gain8(const NormRows &a, uint32_t k, float (&v)[8]) {
-  if (!a.gain) {
+template <bool ANY>
+__device__ __forceinline__ void gain8(const void *gain, int gain_bf16, uint32_t k, uint32_t dim, float (&v)[8]) {
+  if (!gain) {
 #pragma unroll
     for (int j = 0; j < 8; ++j) v[j] = 1.0f;
-  } else if (a.gain_bf16) read8<true>(a.gain, k, a.dim, v);
-  else read8<false>(a.gain, k, a.dim, v);
+  } else if (gain_bf16) read8<true, ANY>(gain, k, dim, v);
+  else read8<false, ANY>(gain, k, dim, v);
 }
 __device__ __forceinline__ const char *row_of(const void *base, uint64_t row, uint64_t stride, int size) {
   return static_cast<const char *>(base) + row * stride * size;
@@ -123,9 +154,10 @@ __device__ __forceinline__ void put_y(const NormRows &a, uint64_t row, uint32_t 
 
 constexpr int NORM_THREADS = 256;
 
-// CHUNKS pieces of eight a lane, LANES * 8 columns apart; CHUNKS 0: as many as there are, read again for the second use.
+// CHUNKS pieces of eight a lane, LANES * 8 columns apart; CHUNKS 0: as many as there are, read again for the second use, and rows of less than eight.
 template <bool BF16, int LANES, int CHUNKS>
 __global__ __launch_bounds__(LANES < NORM_THREADS ? NORM_THREADS : LANES) void eco_norm_kernel(NormRows a) {
+  constexpr bool ANY = CHUNKS == 0;
   constexpr int SIZE = BF16 ? 2 : 4, KEEP = CHUNKS ? CHUNKS : 1, EACH = LANES < NORM_THREADS ? NORM_THREADS / LANES : 1;
   __shared__ float red[LANES / 64];
   const uint32_t lane = threadIdx.x % LANES, chunks = CHUNKS ? CHUNKS : (a.dim + LANES * 8 - 1) / (LANES * 8);
@@ -133,15 +165,19 @@ __global__ __launch_bounds__(LANES < NORM_THREADS ? NORM_THREADS : LANES) void e
   for (uint64_t row = static_cast<uint64_t>(blockIdx.x) * EACH + threadIdx.x / LANES; row < a.rows; row += static_cast<uint64_t>(gridDim.x) * EACH) {
   const char *input = row_of(a.input, row, a.input_stride, SIZE), *residual = a.residual ? row_of(a.residual, row, a.residual_stride, SIZE) : nullptr;
   char *sum = const_cast<char *>(row_of(a.sum, row, a.sum_stride, SIZE));
-  float s[KEEP][8], r[KEEP][8], total = 0.0f;
+  float s[KEEP][8], total = 0.0f;
+  Raw<BF16> raw[KEEP], more[KEEP];
   const auto take = [&](int c, uint32_t k) {       // loads first, all of them
-    read8<BF16>(input, k, a.dim, s[c]);
-    if (residual) read8<BF16>(residual, k, a.dim, r[c]);
+    raw[c] = load8<BF16, ANY>(input, k, a.dim);
+    if (residual) more[c] = load8<BF16, ANY>(residual, k, a.dim);
   };
   const auto add = [&](int c, uint32_t k) {
+    values8<BF16>(raw[c], k, a.dim, s[c]);
     if (residual) {
+      float r[8];
+      values8<BF16>(more[c], k, a.dim, r);
 #pragma unroll
-      for (int j = 0; j < 8; ++j) s[c][j] += r[c][j];
+      for (int j = 0; j < 8; ++j) s[c][j] += r[j];
       if (k < a.dim) write8<BF16>(sum, k, a.dim, s[c]);
     }
 #pragma unroll
@@ -167,7 +203,7 @@ __global__ __launch_bounds__(LANES < NORM_THREADS ? NORM_THREADS : LANES) void e
     float y[8];
     if (a.norm) {
       float gain[8];
-      gain8(a, k, gain);
+      gain8<ANY>(a.gain, a.gain_bf16, k, a.dim, gain);
 #pragma unroll
       for (int j = 0; j < 8; ++j) y[j] = s[c][j] * rstd * gain[j];
     } else {
@@ -182,7 +218,7 @@ __global__ __launch_bounds__(LANES < NORM_THREADS ? NORM_THREADS : LANES) void e
   } else {
     for (uint32_t c = 0; c < chunks; ++c) {
       const uint32_t k = (c * LANES + lane) * 8;
-      read8<BF16>(residual ? sum : input, k, a.dim, s[0]);
+      read8<BF16, ANY>(residual ? sum : input, k, a.dim, s[0]);
       leave(0, k);
     }
   }
@@ -192,28 +228,42 @@ __global__ __launch_bounds__(LANES < NORM_THREADS ? NORM_THREADS : LANES) void e
 // A workgroup goes through rows gridDim.x apart (times the rows that it holds at once) and keeps the gain's gradient over them.
 template <bool BF16, int LANES, int CHUNKS>
 __global__ __launch_bounds__(LANES < NORM_THREADS ? NORM_THREADS : LANES) void eco_norm_backward_kernel(NormGrad a) {
+  constexpr bool ANY = CHUNKS == 0;
   constexpr int SIZE = BF16 ? 2 : 4, KEEP = CHUNKS ? CHUNKS : 1, EACH = LANES < NORM_THREADS ? NORM_THREADS / LANES : 1;
   __shared__ float red[LANES / 64];
   __shared__ float joined[EACH > 1 ? (EACH - 1) * KEEP * LANES * 8 : 1];
   const uint32_t lane = threadIdx.x % LANES, part = threadIdx.x / LANES;
   const uint32_t chunks = CHUNKS ? CHUNKS : (a.dim + LANES * 8 - 1) / (LANES * 8);
-  const NormRows of_gain = {nullptr, nullptr, a.gain, nullptr, nullptr, nullptr, nullptr, 0, 0, 0, 0, 0, a.dim, 0.0f, 0, a.gain_bf16, 0};
   float gg[KEEP][8] = {}, s[KEEP][8], g[KEEP][8];
   float *const mine = a.partial + static_cast<uint64_t>(blockIdx.x) * a.dim;
   bool first = true;
-  for (uint64_t row = static_cast<uint64_t>(blockIdx.x) * EACH + part; row < a.rows; row += static_cast<uint64_t>(gridDim.x) * EACH) {
+  Raw<BF16> raw_s[KEEP], raw_g[KEEP], raw_more[KEEP];
+  const auto load = [&](uint64_t row) {            // a row's loads go out before the row in front of it is worked on
+#pragma unroll
+    for (int c = 0; c < CHUNKS; ++c) {
+      const uint32_t k = (c * LANES + lane) * 8;
+      raw_s[c] = load8<BF16, ANY>(row_of(a.s, row, a.s_stride, SIZE), k, a.dim);
+      raw_g[c] = load8<BF16, ANY>(row_of(a.grad_out, row, a.grad_out_stride, SIZE), k, a.dim);
+      if (a.grad_sum) raw_more[c] = load8<BF16, ANY>(row_of(a.grad_sum, row, a.grad_sum_stride, SIZE), k, a.dim);
+    }
+  };
+  const uint64_t step = static_cast<uint64_t>(gridDim.x) * EACH, row0 = static_cast<uint64_t>(blockIdx.x) * EACH + part;
+  float next_rstd = 0.0f;
+  if (CHUNKS != 0 && row0 < a.rows) { load(row0); next_rstd = a.rstd[row0]; }
+  for (uint64_t row = row0; row < a.rows; row += step) {
     const char *from = row_of(a.s, row, a.s_stride, SIZE), *grad = row_of(a.grad_out, row, a.grad_out_stride, SIZE);
     const char *more = a.grad_sum ? row_of(a.grad_sum, row, a.grad_sum_stride, SIZE) : nullptr;
     char *to = const_cast<char *>(row_of(a.grad_input, row, a.grad_input_stride, SIZE));
-    const float rstd = a.rstd[row];
+    const float rstd = CHUNKS != 0 ? next_rstd : a.rstd[row];
     float dot = 0.0f;
+    float d[KEEP][8];
     const auto take = [&](int c, uint32_t k) {
-      read8<BF16>(from, k, a.dim, s[c]);
-      read8<BF16>(grad, k, a.dim, g[c]);
+      read8<BF16, ANY>(from, k, a.dim, s[c]);
+      read8<BF16, ANY>(grad, k, a.dim, g[c]);
     };
     const auto add = [&](int c, uint32_t k) {      // s becomes n, g becomes u
       float gain[8];
-      gain8(of_gain, k, gain);
+      gain8<ANY>(a.gain, a.gain_bf16, k, a.dim, gain);
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
         s[c][j] *= rstd;
@@ -224,7 +274,13 @@ __global__ __launch_bounds__(LANES < NORM_THREADS ? NORM_THREADS : LANES) void e
     };
     if constexpr (CHUNKS != 0) {
 #pragma unroll
-      for (int c = 0; c < CHUNKS; ++c) take(c, (c * LANES + lane) * 8);
+      for (int c = 0; c < CHUNKS; ++c) {
+        const uint32_t k = (c * LANES + lane) * 8;
+        values8<BF16>(raw_s[c], k, a.dim, s[c]);
+        values8<BF16>(raw_g[c], k, a.dim, g[c]);
+        if (more) values8<BF16>(raw_more[c], k, a.dim, d[c]);
+      }
+      if (row + step < a.rows) { load(row + step); next_rstd = a.rstd[row + step]; }
 #pragma unroll
       for (int c = 0; c < CHUNKS; ++c) add(c, (c * LANES + lane) * 8);
     } else {
@@ -236,7 +292,7 @@ __global__ __launch_bounds__(LANES < NORM_THREADS ? NORM_THREADS : LANES) void e
           if (first) {
 #pragma unroll
             for (int j = 0; j < 8; ++j) sums[j] = 0.0f;
-          } else read8<false>(mine, k, a.dim, sums);
+          } else read8<false, ANY>(mine, k, a.dim, sums);
 #pragma unroll
           for (int j = 0; j < 8; ++j) sums[j] = fmaf(g[0][j], s[0][j] * rstd, sums[j]);
           write8<false>(mine, k, a.dim, sums);
@@ -248,14 +304,13 @@ __global__ __launch_bounds__(LANES < NORM_THREADS ? NORM_THREADS : LANES) void e
     if (!a.grad_input) continue;                   // (uniform)
     const float mean = row_sum<LANES>(dot, red) / static_cast<float>(a.dim);
     const auto leave = [&](int c, uint32_t k) {
-      float d[8];
-      if (more) read8<BF16>(more, k, a.dim, d);
+      if (CHUNKS == 0 && more) read8<BF16, ANY>(more, k, a.dim, d[c]);
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
         const float x = rstd * fmaf(-s[c][j], mean, g[c][j]);
-        d[j] = more ? x + d[j] : x;
+        d[c][j] = more ? x + d[c][j] : x;
       }
-      if (k < a.dim) write8<BF16>(to, k, a.dim, d);
+      if (k < a.dim) write8<BF16>(to, k, a.dim, d[c]);
     };
     if constexpr (CHUNKS != 0) {
 #pragma unroll
@@ -265,7 +320,7 @@ __global__ __launch_bounds__(LANES < NORM_THREADS ? NORM_THREADS : LANES) void e
         const uint32_t k = (c * LANES + lane) * 8;
         float gain[8];
         take(0, k);
-        gain8(of_gain, k, gain);
+        gain8<ANY>(a.gain, a.gain_bf16, k, a.dim, gain);
 #pragma unroll
         for (int j = 0; j < 8; ++j) { s[0][j] *= rstd; g[0][j] *= gain[j]; }
         leave(0, k);
@@ -318,6 +373,7 @@ template <class F>
 hipError_t by_width(uint32_t dim, F f) {
   using std::integral_constant;
   const auto go = [&](auto lanes, auto chunks) { return f(lanes, chunks); };
+  if (dim < 8) return go(integral_constant<int, 1024>{}, integral_constant<int, 0>{});
   if (dim <= 512) return go(integral_constant<int, 64>{}, integral_constant<int, 1>{});
   if (dim <= 1024) return go(integral_constant<int, 64>{}, integral_constant<int, 2>{});
   if (dim <= 1536) return go(integral_constant<int, 64>{}, integral_constant<int, 3>{});
@@ -326,7 +382,7 @@ hipError_t by_width(uint32_t dim, F f) {
   if (dim <= 8192) return go(integral_constant<int, 256>{}, integral_constant<int, 4>{});
   return go(integral_constant<int, 1024>{}, integral_constant<int, 0>{});
 }
-uint32_t rows_at_once(uint64_t dim) { return dim <= 2048 ? 4 : 1; }
+uint32_t rows_at_once(uint64_t dim) { return dim >= 8 && dim <= 2048 ? 4 : 1; }
 
 }  // namespace
 
