@@ -152,13 +152,11 @@ __device__ __forceinline__ void put_y(const NormRows &a, uint64_t row, uint32_t 
   else if (k < a.dim) write8<BF16>(const_cast<char *>(row_of(a.out, row, a.out_stride, BF16 ? 2 : 4)), k, a.dim, y);
 }
 
-constexpr int NORM_THREADS = 256;
-
 // CHUNKS pieces of eight a lane, LANES * 8 columns apart; CHUNKS 0: as many as there are, read again for the second use, and rows of less than eight.
 template <bool BF16, int LANES, int CHUNKS>
-__global__ __launch_bounds__(LANES < NORM_THREADS ? NORM_THREADS : LANES) void eco_norm_kernel(NormRows a) {
+__global__ __launch_bounds__(LANES == 64 ? 256 : LANES) void eco_norm_kernel(NormRows a) {
   constexpr bool ANY = CHUNKS == 0;
-  constexpr int SIZE = BF16 ? 2 : 4, KEEP = CHUNKS ? CHUNKS : 1, EACH = LANES < NORM_THREADS ? NORM_THREADS / LANES : 1;
+  constexpr int SIZE = BF16 ? 2 : 4, KEEP = CHUNKS ? CHUNKS : 1, EACH = LANES == 64 ? 4 : 1;
   __shared__ float red[LANES / 64];
   const uint32_t lane = threadIdx.x % LANES, chunks = CHUNKS ? CHUNKS : (a.dim + LANES * 8 - 1) / (LANES * 8);
   // (by whole waves, and by whole workgroups where a row takes more than one; the grid has a workgroup for each row but for dim > 8192)
@@ -227,9 +225,9 @@ __global__ __launch_bounds__(LANES < NORM_THREADS ? NORM_THREADS : LANES) void e
 
 // A workgroup goes through rows gridDim.x apart (times the rows that it holds at once) and keeps the gain's gradient over them.
 template <bool BF16, int LANES, int CHUNKS>
-__global__ __launch_bounds__(LANES < NORM_THREADS ? NORM_THREADS : LANES) void eco_norm_backward_kernel(NormGrad a) {
+__global__ __launch_bounds__(LANES == 64 ? 256 : LANES) void eco_norm_backward_kernel(NormGrad a) {
   constexpr bool ANY = CHUNKS == 0;
-  constexpr int SIZE = BF16 ? 2 : 4, KEEP = CHUNKS ? CHUNKS : 1, EACH = LANES < NORM_THREADS ? NORM_THREADS / LANES : 1;
+  constexpr int SIZE = BF16 ? 2 : 4, KEEP = CHUNKS ? CHUNKS : 1, EACH = LANES == 64 ? 4 : 1;
   __shared__ float red[LANES / 64];
   __shared__ float joined[EACH > 1 ? (EACH - 1) * KEEP * LANES * 8 : 1];
   const uint32_t lane = threadIdx.x % LANES, part = threadIdx.x / LANES;
@@ -375,14 +373,15 @@ hipError_t by_width(uint32_t dim, F f) {
   const auto go = [&](auto lanes, auto chunks) { return f(lanes, chunks); };
   if (dim < 8) return go(integral_constant<int, 1024>{}, integral_constant<int, 0>{});
   if (dim <= 512) return go(integral_constant<int, 64>{}, integral_constant<int, 1>{});
-  if (dim <= 1024) return go(integral_constant<int, 64>{}, integral_constant<int, 2>{});
-  if (dim <= 1536) return go(integral_constant<int, 64>{}, integral_constant<int, 3>{});
-  if (dim <= 2048) return go(integral_constant<int, 64>{}, integral_constant<int, 4>{});
+  if (dim <= 1024) return go(integral_constant<int, 128>{}, integral_constant<int, 1>{});
+  if (dim <= 1536) return go(integral_constant<int, 192>{}, integral_constant<int, 1>{});
+  if (dim <= 2048) return go(integral_constant<int, 256>{}, integral_constant<int, 1>{});
   if (dim <= 4096) return go(integral_constant<int, 256>{}, integral_constant<int, 2>{});
   if (dim <= 8192) return go(integral_constant<int, 256>{}, integral_constant<int, 4>{});
   return go(integral_constant<int, 1024>{}, integral_constant<int, 0>{});
 }
-uint32_t rows_at_once(uint64_t dim) { return dim >= 8 && dim <= 2048 ? 4 : 1; }
+constexpr int threads_of(int lanes) { return lanes == 64 ? 256 : lanes; }
+uint32_t rows_at_once(uint64_t dim) { return dim >= 8 && dim <= 512 ? 4 : 1; }
 
 }  // namespace
 
@@ -390,23 +389,24 @@ hipError_t launch_norm(const NormRows &a, hipStream_t s) {
   if (a.rows == 0) return hipSuccess;
   const uint32_t each = rows_at_once(a.dim), all = (a.rows + each - 1) / each, grid = a.dim > 8192 && all > 65536 ? 65536 : all;
   return by_width(a.dim, [&](auto lanes, auto chunks) {
-    constexpr int L = decltype(lanes)::value, C = decltype(chunks)::value, T = L < NORM_THREADS ? NORM_THREADS : L;
+    constexpr int L = decltype(lanes)::value, C = decltype(chunks)::value, T = threads_of(L);
     if (a.bf16) eco_norm_kernel<true, L, C><<<grid, T, 0, s>>>(a);
     else eco_norm_kernel<false, L, C><<<grid, T, 0, s>>>(a);
     return hipGetLastError();
   });
 }
 
+constexpr uint32_t NORM_PARTS = 1024;
 uint32_t norm_parts(uint64_t rows, uint64_t dim) {
   const uint64_t all = (rows + rows_at_once(dim) - 1) / rows_at_once(dim);
-  return static_cast<uint32_t>(all < 512 ? all : 512);
+  return static_cast<uint32_t>(all < NORM_PARTS ? all : NORM_PARTS);
 }
 
 hipError_t launch_norm_backward(const NormGrad &a, hipStream_t s) {
   const uint32_t parts = norm_parts(a.rows, a.dim);
   if (a.rows) {
     const hipError_t e = by_width(a.dim, [&](auto lanes, auto chunks) {
-      constexpr int L = decltype(lanes)::value, C = decltype(chunks)::value, T = L < NORM_THREADS ? NORM_THREADS : L;
+      constexpr int L = decltype(lanes)::value, C = decltype(chunks)::value, T = threads_of(L);
       if (a.bf16) eco_norm_backward_kernel<true, L, C><<<parts, T, 0, s>>>(a);
       else eco_norm_backward_kernel<false, L, C><<<parts, T, 0, s>>>(a);
       return hipGetLastError();
