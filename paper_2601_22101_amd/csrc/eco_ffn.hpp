@@ -79,14 +79,21 @@ hipError_t launch_ffn_join(const FfnPlan &, const FfnRows8 &, const FfnWeights &
 struct FfnTile { uint32_t x, y; double step, tile; };
 // The best split of `tiles` tiles with `steps` steps each over `units` places, and what it costs.
 double ffn_split(uint64_t tiles, uint64_t steps, uint64_t units, uint64_t least_steps, const FfnTile &, FfnSplit *);
-// INT4 codes as the E4M3 codes of the same values (one matrix).
-hipError_t launch_ffn_expand(const void *codes, uint64_t numel, void *out, hipStream_t);
+// INT4 codes as the E4M3 codes of the same values, of each matrix.
+hipError_t launch_ffn_expand(const FfnWeights &, void *const out[2], hipStream_t);
 
 // ---- gradients, of bf16 operands
-// Weights as bf16 rows [matrices][padded rows][ld], zeros in the padding; x the same; a bf16 matrix copied with padding.
-hipError_t launch_ffn_weights_bf16(const FfnWeights &, void *out, uint32_t padded_rows, hipStream_t);
-hipError_t launch_ffn_rows_bf16(const FfnRows8 &, void *out, uint32_t padded_rows, hipStream_t);
-hipError_t launch_ffn_pad(const void *src, uint64_t src_stride, uint32_t rows, uint32_t dim, void *out, uint32_t ld, hipStream_t);
+// Weights as bf16 rows [matrices][padded_width][dim], zeros in the padding; x [padded_rows][dim] the same; the output's gradient copied to rows of grad_ld, zeros behind
+// them.  Those that are null are not made.
+struct FfnOperands {
+  FfnWeights w;
+  FfnRows8 x;
+  const uint16_t *grad_from;
+  uint64_t grad_stride;
+  uint16_t *weights, *rows, *grad;
+  uint32_t padded_width, padded_rows, grad_ld;
+};
+hipError_t launch_ffn_operands(const FfnOperands &, hipStream_t);
 
 // D[y][x] = sum_k Y X, X a [k][x] array with zeros from k_end to the next multiple of 64; Y [y][k] (rows) or [k][y] (columns, in `matrices` runs of y_offset columns).
 struct FfnProduct {
@@ -98,8 +105,9 @@ struct FfnProduct {
   float *partial;                                 // [splits][tiles from `whole` on][tile]
   uint32_t whole, splits, split_steps;
 };
-struct FfnGradPlan { int shape; FfnSplit split; };
-FfnGradPlan ffn_grad_plan(uint64_t nx, uint64_t ny, uint64_t k, uint32_t matrices);
-hipError_t launch_ffn_grad(const FfnGradPlan &, bool columns, const FfnProduct &, hipStream_t);
+struct FfnGradSize { uint64_t nx, ny, k; uint32_t matrices; };         // ny 0: that gradient is not wanted
+struct FfnGradPlan { int shape; uint32_t of_input; FfnSplit input, weights; };      // of_input: workgroups for grad_input
+FfnGradPlan ffn_grad_plan(const FfnGradSize &input, const FfnGradSize &weights);
+hipError_t launch_ffn_grad(const FfnGradPlan &, const FfnProduct &input, const FfnProduct &weights, hipStream_t);
 
 }  // namespace eco

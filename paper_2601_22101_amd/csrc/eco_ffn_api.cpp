@@ -184,10 +184,9 @@ Forward forward_of(const Unit &u, int end, Room room, Places &p, bool exact = fa
 eco_status_t product(const Unit &u, const Forward &f, eco::FfnOut o, char *ws, hipStream_t s) {
   eco::FfnWeights w = weights_of(u);
   if (f.expands) {
-    for (uint32_t m = 0; m < u.matrices; ++m) {
-      LAUNCH(u.what, eco::launch_ffn_expand(w.data[m], u.width * u.dim, ws + f.expanded[m], s));
-      w.data[m] = ws + f.expanded[m];
-    }
+    void *const codes[2] = {ws + f.expanded[0], ws + f.expanded[1]};
+    LAUNCH(u.what, eco::launch_ffn_expand(w, codes, s));
+    for (uint32_t m = 0; m < u.matrices; ++m) w.data[m] = codes[m];
     w.fmt = ECO_FMT_FP8_E4M3;
   }
   o.whole = f.plan.split.whole;
@@ -200,11 +199,11 @@ eco_status_t product(const Unit &u, const Forward &f, eco::FfnOut o, char *ws, h
 }
 
 // The gradients' operands: `half` columns of the output's gradient for each matrix, whole steps of the inner axis.
-constexpr uint64_t GRAD_STEP = 64, MOST_DIRECT_STRIDE = 1ull << 22;
+constexpr uint64_t GRAD_STEP = 64, LEAST_SPLIT = 8 * GRAD_STEP, MOST_DIRECT_STRIDE = 1ull << 22;      // (parts have four steps at least)
 struct Backward {
-  eco::FfnGradPlan input, weights;
+  eco::FfnGradPlan plan;
   uint64_t half, padded_rows, w, x, grad, input_partial, weights_partial;
-  bool copies;
+  bool copies, input, weights;
 };
 Backward backward_of(const Unit &u, bool input, bool weights, bool copies, Room room, Places &p) {
   Backward b;
@@ -212,47 +211,52 @@ Backward backward_of(const Unit &u, bool input, bool weights, bool copies, Room 
   b.half = eco::ffn_round_up(u.width, GRAD_STEP);
   b.padded_rows = eco::ffn_round_up(u.rows, GRAD_STEP);
   b.copies = copies;
+  b.input = input && u.rows;
+  b.weights = weights;
   if (copies) b.grad = p.take(2ull * u.rows * b.half * u.matrices);
-  if (input && u.rows) {
-    b.w = p.take(2ull * u.matrices * b.half * u.dim);
-    if (room == EXACT) b.input = eco::ffn_grad_plan(u.dim, u.rows, u.matrices == 2 ? 2 * b.half : u.width, 1);
-    const uint64_t parts = room == EXACT ? b.input.split.partial : most_partial(u.rows, u.dim, 1);
-    if (parts) b.input_partial = p.take(4 * parts);
-  }
-  if (weights) {
-    b.x = p.take(2ull * b.padded_rows * u.dim);
-    if (room == EXACT) b.weights = eco::ffn_grad_plan(u.dim, u.width, u.rows, u.matrices);
-    const uint64_t parts = room == EXACT ? b.weights.split.partial : b.padded_rows > GRAD_STEP ? most_partial(u.width, u.dim, u.matrices) : 0;
-    if (parts) b.weights_partial = p.take(4 * parts);
-  }
+  if (b.input) b.w = p.take(2ull * u.matrices * b.half * u.dim);
+  if (b.weights) b.x = p.take(2ull * b.padded_rows * u.dim);
+  if (room == EXACT) b.plan = eco::ffn_grad_plan({u.dim, b.input ? u.rows : 0, u.matrices == 2 ? 2 * b.half : u.width, 1}, {u.dim, b.weights ? u.width : 0, u.rows, u.matrices});
+  const uint64_t of_input = room == EXACT ? b.plan.input.partial : b.input && u.matrices * b.half >= LEAST_SPLIT ? most_partial(u.rows, u.dim, 1) : 0;
+  const uint64_t of_weights = room == EXACT ? b.plan.weights.partial : b.weights && b.padded_rows >= LEAST_SPLIT ? most_partial(u.width, u.dim, u.matrices) : 0;
+  if (of_input) b.input_partial = p.take(4 * of_input);
+  if (of_weights) b.weights_partial = p.take(4 * of_weights);
   return b;
+}
+eco_status_t operands(const Unit &u, const Backward &b, const void *grad, uint64_t grad_stride, char *ws, hipStream_t s) {
+  eco::FfnOperands o;
+  std::memset(&o, 0, sizeof o);
+  o.w = weights_of(u); o.x = rows_of(u);
+  o.padded_width = static_cast<uint32_t>(b.half); o.padded_rows = static_cast<uint32_t>(b.padded_rows);
+  if (b.input) o.weights = reinterpret_cast<uint16_t *>(ws + b.w);
+  if (b.weights) o.rows = reinterpret_cast<uint16_t *>(ws + b.x);
+  if (grad) { o.grad = reinterpret_cast<uint16_t *>(ws + b.grad); o.grad_from = static_cast<const uint16_t *>(grad); o.grad_stride = grad_stride; o.grad_ld = static_cast<uint32_t>(b.half); }
+  LAUNCH(u.what, eco::launch_ffn_operands(o, s));
+  return ECO_OK;
 }
 // From the output's gradient as bf16 rows, `ldy` apart, of each matrix in turn.
 eco_status_t gradients(const Unit &u, const Backward &b, const void *grad, uint64_t ldy, void *grad_input, uint64_t grad_input_stride, void *const grad_weights[2], char *ws,
                        hipStream_t s) {
   const uint32_t dim = static_cast<uint32_t>(u.dim), rows = static_cast<uint32_t>(u.rows), width = static_cast<uint32_t>(u.width);
-  if (grad_input && rows) {
-    LAUNCH(u.what, eco::launch_ffn_weights_bf16(weights_of(u), ws + b.w, static_cast<uint32_t>(b.half), s));
-    eco::FfnProduct p;
-    std::memset(&p, 0, sizeof p);
-    p.x = reinterpret_cast<const uint16_t *>(ws + b.w); p.y = static_cast<const uint16_t *>(grad);
-    p.ldx = p.nx = dim; p.ldy = ldy; p.ny = rows; p.k = u.matrices == 2 ? static_cast<uint32_t>(2 * b.half) : width; p.matrices = 1;
-    p.out[0] = grad_input; p.out_stride = stride_or(grad_input_stride, u.dim);
-    p.whole = b.input.split.whole; p.splits = b.input.split.splits; p.split_steps = b.input.split.split_steps;
-    p.partial = reinterpret_cast<float *>(ws + b.input_partial);
-    LAUNCH(u.what, eco::launch_ffn_grad(b.input, false, p, s));
+  eco::FfnProduct in, of;
+  std::memset(&in, 0, sizeof in);
+  std::memset(&of, 0, sizeof of);
+  const auto split = [](eco::FfnProduct &p, const eco::FfnSplit &f, char *partial) {
+    p.whole = f.whole; p.splits = f.splits; p.split_steps = f.split_steps; p.partial = reinterpret_cast<float *>(partial);
+  };
+  if (b.input) {
+    in.x = reinterpret_cast<const uint16_t *>(ws + b.w); in.y = static_cast<const uint16_t *>(grad);
+    in.ldx = in.nx = dim; in.ldy = ldy; in.ny = rows; in.k = u.matrices == 2 ? static_cast<uint32_t>(2 * b.half) : width; in.matrices = 1;
+    in.out[0] = grad_input; in.out_stride = stride_or(grad_input_stride, u.dim);
+    split(in, b.plan.input, ws + b.input_partial);
   }
-  if (grad_weights[0]) {
-    LAUNCH(u.what, eco::launch_ffn_rows_bf16(rows_of(u), ws + b.x, static_cast<uint32_t>(b.padded_rows), s));
-    eco::FfnProduct p;
-    std::memset(&p, 0, sizeof p);
-    p.x = reinterpret_cast<const uint16_t *>(ws + b.x); p.y = static_cast<const uint16_t *>(grad);
-    p.ldx = p.nx = dim; p.ldy = ldy; p.ny = width; p.k = rows; p.matrices = u.matrices; p.y_offset = static_cast<uint32_t>(b.half);
-    p.out[0] = grad_weights[0]; p.out[1] = grad_weights[1]; p.out_stride = u.dim;
-    p.whole = b.weights.split.whole; p.splits = b.weights.split.splits; p.split_steps = b.weights.split.split_steps;
-    p.partial = reinterpret_cast<float *>(ws + b.weights_partial);
-    LAUNCH(u.what, eco::launch_ffn_grad(b.weights, true, p, s));
+  if (b.weights) {
+    of.x = reinterpret_cast<const uint16_t *>(ws + b.x); of.y = static_cast<const uint16_t *>(grad);
+    of.ldx = of.nx = dim; of.ldy = ldy; of.ny = width; of.k = rows; of.matrices = u.matrices; of.y_offset = static_cast<uint32_t>(b.half);
+    of.out[0] = grad_weights[0]; of.out[1] = grad_weights[1]; of.out_stride = u.dim;
+    split(of, b.plan.weights, ws + b.weights_partial);
   }
+  LAUNCH(u.what, eco::launch_ffn_grad(b.plan, in, of, s));
   return ECO_OK;
 }
 
@@ -412,8 +416,8 @@ eco_status_t eco_linear_backward(const eco_linear_t *l, void *workspace, size_t 
   hipStream_t s = static_cast<hipStream_t>(stream);
   const void *grad = l->grad_out;
   uint64_t ldy = stride_or(l->grad_out_stride, l->out_dim);
+  CHECK(operands(u, b, copies ? grad : nullptr, ldy, ws, s));
   if (copies) {
-    LAUNCH("linear", eco::launch_ffn_pad(grad, ldy, static_cast<uint32_t>(l->rows), static_cast<uint32_t>(l->out_dim), ws + b.grad, static_cast<uint32_t>(b.half), s));
     grad = ws + b.grad;
     ldy = b.half;
   }
@@ -465,6 +469,7 @@ eco_status_t eco_gated_backward(const eco_gated_t *g, void *workspace, size_t wo
     o.grad_out = static_cast<const uint16_t *>(g->grad_out); o.grad_out_stride = stride_or(g->grad_out_stride, g->width);
     CHECK(product(u, f, o, ws, s));
   }
+  CHECK(operands(u, b, nullptr, 0, ws, s));
   void *const to[2] = {g->grad_gate, g->grad_up};
   return gradients(u, b, ws + b.grad, 2 * b.half, g->grad_input, g->grad_input_stride, to, ws, s);
 }

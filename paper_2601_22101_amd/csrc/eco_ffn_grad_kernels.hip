@@ -30,15 +30,17 @@ __device__ __forceinline__ void fp8_values(uint2 u, float scale, float (&v)[8]) 
   for (int j = 0; j < 8; ++j) v[j] *= scale;
 }
 
-// Eight weights a thread; rows are whole sixteens of codes.
+// All operands in one launch, workgroups for each in turn.  Eight weights a thread, whose rows are whole sixteens of codes; 8-bit rows, exact; rows of the output's gradient copied
+// where they lie at addresses that the products cannot read, with zeros behind them.
 template <int FMT>
-__global__ __launch_bounds__(256) void eco_ffn_weights_kernel(FfnWeights w, uint16_t *out, uint32_t padded_rows) {
+__device__ __forceinline__ void weights_bf16(const FfnOperands &a, uint64_t first, uint64_t step) {
+  const FfnWeights &w = a.w;
   const uint32_t chunks = w.dim / 8;
-  const uint64_t work = static_cast<uint64_t>(w.matrices) * padded_rows * chunks;
-  for (uint64_t i = static_cast<uint64_t>(blockIdx.x) * 256 + threadIdx.x; i < work; i += static_cast<uint64_t>(gridDim.x) * 256) {
+  const uint64_t work = static_cast<uint64_t>(w.matrices) * a.padded_width * chunks;
+  for (uint64_t i = first; i < work; i += step) {
     const uint32_t all_row = static_cast<uint32_t>(i >> 32 ? i / chunks : static_cast<uint32_t>(i) / chunks), k = static_cast<uint32_t>(i - static_cast<uint64_t>(all_row) * chunks) * 8;
-    const int matrix = all_row >= padded_rows;
-    const uint32_t row = all_row - (matrix ? padded_rows : 0);
+    const int matrix = all_row >= a.padded_width;
+    const uint32_t row = all_row - (matrix ? a.padded_width : 0);
     float v[8] = {0, 0, 0, 0, 0, 0, 0, 0};
     if (row < w.rows) {
       const uint64_t at = static_cast<uint64_t>(row) * w.dim + k;
@@ -51,35 +53,42 @@ __global__ __launch_bounds__(256) void eco_ffn_weights_kernel(FfnWeights w, uint
         for (int j = 0; j < 8; ++j) v[j] = static_cast<float>(static_cast<int32_t>(u << (28 - 4 * j)) >> 28) * scale;
       }
     }
-    put_bf16x8(out + i * 8, v);
+    put_bf16x8(a.weights + i * 8, v);
   }
 }
-
-// 8-bit rows; exact.
-__global__ __launch_bounds__(256) void eco_ffn_rows_kernel(FfnRows8 x, uint16_t *out, uint32_t padded_rows) {
-  const uint32_t chunks = x.dim / 8;
-  const uint64_t work = static_cast<uint64_t>(padded_rows) * chunks;
-  for (uint64_t i = static_cast<uint64_t>(blockIdx.x) * 256 + threadIdx.x; i < work; i += static_cast<uint64_t>(gridDim.x) * 256) {
-    const uint32_t row = static_cast<uint32_t>(i >> 32 ? i / chunks : static_cast<uint32_t>(i) / chunks), k = static_cast<uint32_t>(i - static_cast<uint64_t>(row) * chunks) * 8;
-    float v[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-    if (row < x.rows) {
-      const uint32_t byte = x.scales[static_cast<uint64_t>(row) * x.blocks + k / FFN_BLOCK];
-      fp8_values(*reinterpret_cast<const uint2 *>(x.codes + row * x.stride + k), u2f(byte ? byte << 23 : 0x00400000u), v);
+template <int FMT>
+__global__ __launch_bounds__(256) void eco_ffn_operands_kernel(FfnOperands a, uint32_t of_weights, uint32_t of_rows) {
+  uint32_t id = blockIdx.x;
+  if (id < of_weights) {
+    weights_bf16<FMT>(a, static_cast<uint64_t>(id) * 256 + threadIdx.x, static_cast<uint64_t>(of_weights) * 256);
+    return;
+  }
+  id -= of_weights;
+  if (id < of_rows) {
+    const FfnRows8 &x = a.x;
+    const uint32_t chunks = x.dim / 8;
+    const uint64_t work = static_cast<uint64_t>(a.padded_rows) * chunks;
+    for (uint64_t i = static_cast<uint64_t>(id) * 256 + threadIdx.x; i < work; i += static_cast<uint64_t>(of_rows) * 256) {
+      const uint32_t row = static_cast<uint32_t>(i >> 32 ? i / chunks : static_cast<uint32_t>(i) / chunks), k = static_cast<uint32_t>(i - static_cast<uint64_t>(row) * chunks) * 8;
+      float v[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+      if (row < x.rows) {
+        const uint32_t byte = x.scales[static_cast<uint64_t>(row) * x.blocks + k / FFN_BLOCK];
+        fp8_values(*reinterpret_cast<const uint2 *>(x.codes + row * x.stride + k), u2f(byte ? byte << 23 : 0x00400000u), v);
+      }
+      put_bf16x8(a.rows + i * 8, v);
     }
-    put_bf16x8(out + i * 8, v);
+    return;
   }
-}
-
-__global__ __launch_bounds__(256) void eco_ffn_pad_kernel(const uint16_t *src, uint64_t stride, uint32_t rows, uint32_t dim, uint16_t *out, uint32_t ld) {
-  const uint32_t chunks = ld / 8;
-  const uint64_t work = static_cast<uint64_t>(rows) * chunks;
-  for (uint64_t i = static_cast<uint64_t>(blockIdx.x) * 256 + threadIdx.x; i < work; i += static_cast<uint64_t>(gridDim.x) * 256) {
+  id -= of_rows;
+  const uint32_t chunks = a.grad_ld / 8;
+  const uint64_t work = static_cast<uint64_t>(a.x.rows) * chunks, step = static_cast<uint64_t>(gridDim.x - of_weights - of_rows) * 256;
+  for (uint64_t i = static_cast<uint64_t>(id) * 256 + threadIdx.x; i < work; i += step) {
     const uint64_t row = i / chunks;
     const uint32_t k = static_cast<uint32_t>(i - row * chunks) * 8;
     uint32_t v[8];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) v[j] = k + j < dim ? src[row * stride + k + j] : 0u;
-    *reinterpret_cast<uint4 *>(out + i * 8) = make_uint4(v[0] | v[1] << 16, v[2] | v[3] << 16, v[4] | v[5] << 16, v[6] | v[7] << 16);
+    for (int j = 0; j < 8; ++j) v[j] = k + j < a.w.rows ? a.grad_from[row * a.grad_stride + k + j] : 0u;
+    *reinterpret_cast<uint4 *>(a.grad + i * 8) = make_uint4(v[0] | v[1] << 16, v[2] | v[3] << 16, v[4] | v[5] << 16, v[6] | v[7] << 16);
   }
 }
 
@@ -90,13 +99,13 @@ struct GradArgs {
   uint32_t tiles_x, tiles_y, steps;
 };
 
-// D[y][x] = sum_k Y X.  x runs along a lane's registers, four neighbours in each group.  A workgroup goes through tiles gridDim.x apart; its loads do not stop
+constexpr int OWN = 4096;                         // of LDS, for a wave's results on their way out
+
+// D[y][x] = sum_k Y X.  x runs along a lane's registers, four neighbours in each group.  Workgroup `me` of `all` goes through tiles `all` apart; its loads do not stop
 // between them.
 template <bool Y_COLUMN, class T>
-__global__ __launch_bounds__(T::THREADS) void eco_ffn_grad_kernel(GradArgs a) {
-  constexpr int NI = T::NI, NJ = T::NJ, QUARTERS = KSTEP / 16, OWN = 4096;
-  __shared__ __attribute__((aligned(1024))) char smem[T::DEPTH * T::STEP_BYTES + T::WX * T::WY * OWN];
-  static_assert(sizeof smem <= 163840, "a compute unit's LDS");
+__device__ __forceinline__ void grad_product(const GradArgs &a, uint32_t me, uint32_t all, char *smem) {
+  constexpr int NI = T::NI, NJ = T::NJ, QUARTERS = KSTEP / 16;
   const FfnProduct &p = a.p;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wx = wave % T::WX * (NI * 32), wy = wave / T::WX * (NJ * 32);
@@ -130,7 +139,7 @@ __global__ __launch_bounds__(T::THREADS) void eco_ffn_grad_kernel(GradArgs a) {
   };
 
   // ---- the loads' place in the work
-  uint32_t load_id = blockIdx.x, load_first = 0, load_steps = 0, at_step = 0, issued = 0, place = 0;
+  uint32_t load_id = me, load_first = 0, load_steps = 0, at_step = 0, issued = 0, place = 0;
   uint32_t off_x[T::X_LOADS], off_y[T::Y_LOADS];
   const uint16_t *from_x = nullptr, *from_y = nullptr;
   const uint32_t lds0 = static_cast<uint32_t>(reinterpret_cast<uintptr_t>((lds_char *)smem));
@@ -184,7 +193,7 @@ __global__ __launch_bounds__(T::THREADS) void eco_ffn_grad_kernel(GradArgs a) {
     place = place + 1 == T::DEPTH ? 0 : place + 1;
     ++issued;
     if (++at_step == load_steps) {
-      load_id += gridDim.x;
+      load_id += all;
       if (load_id < all_tiles) load_tile();
       return;
     }
@@ -210,7 +219,7 @@ __global__ __launch_bounds__(T::THREADS) void eco_ffn_grad_kernel(GradArgs a) {
     barrier();
     read(step, 0, fx[0], fy[0]);
   }
-  for (uint32_t id = blockIdx.x; id < all_tiles; id += gridDim.x) {
+  for (uint32_t id = me; id < all_tiles; id += all) {
     const Where w = where(id);
     f32x16 acc[NI][NJ] = {};
     for (uint32_t s = 0; s < w.steps; ++s) {
@@ -296,11 +305,23 @@ __global__ __launch_bounds__(T::THREADS) void eco_ffn_grad_kernel(GradArgs a) {
   }
 }
 
+// Both products in one launch, so that the chip has no partial round of tiles for each: the first workgroups have grad_input's tiles, the others grad_weights'.
+template <class T>
+__global__ __launch_bounds__(T::THREADS) void eco_ffn_grad_kernel(GradArgs input, GradArgs weights, uint32_t of_input) {
+  __shared__ __attribute__((aligned(1024))) char smem[T::DEPTH * T::STEP_BYTES + T::WX * T::WY * OWN];
+  static_assert(sizeof smem <= 163840, "a compute unit's LDS");
+  if (blockIdx.x < of_input) grad_product<false, T>(input, blockIdx.x, of_input, smem);
+  else grad_product<true, T>(weights, blockIdx.x - of_input, gridDim.x - of_input, smem);
+}
+
 // The parts of split tiles, added in their order and rounded: eight neighbours a thread.
-__global__ __launch_bounds__(256) void eco_ffn_grad_join_kernel(GradArgs a, uint32_t bx, uint32_t by) {
+__global__ __launch_bounds__(256) void eco_ffn_grad_join_kernel(GradArgs input, GradArgs weights, uint32_t of_input, uint32_t bx, uint32_t by) {
+  const bool first = blockIdx.x < of_input;
+  const GradArgs &a = first ? input : weights;
   const FfnProduct &p = a.p;
+  const uint32_t id = blockIdx.x - (first ? 0 : of_input);
   const uint32_t each = a.tiles_x * a.tiles_y, split_tiles = each * p.matrices - p.whole, chunks = bx / 8, per_tile = chunks * by / 256;
-  const uint32_t nth = blockIdx.x / per_tile, in = blockIdx.x % per_tile * 256 + threadIdx.x, row = in / chunks, column = in % chunks * 8;
+  const uint32_t nth = id / per_tile, in = id % per_tile * 256 + threadIdx.x, row = in / chunks, column = in % chunks * 8;
   uint32_t tile = p.whole + nth;
   const uint32_t matrix = tile / each;
   tile -= matrix * each;
@@ -331,69 +352,75 @@ using Medium = Tile<128, 128, 2, 2, 2>;
 uint64_t ceil_div(uint64_t a, uint64_t b) { return (a + b - 1) / b; }
 uint32_t grid_of(uint64_t work) { const uint64_t g = ceil_div(work, 256); return static_cast<uint32_t>(g < 1 ? 1 : g < 8192 ? g : 8192); }
 
-// By shape: 128 x 128, of which a compute unit holds two, then 128, 192 and 256 x 256.
+// By shape: 128 x 128, of which a compute unit holds two, then 128, 192 and 256 x 256.  Microseconds of a step of 64 and of a tile's ends, from products of 8192 rows with 1152 x
+// 6912, 1152 x 13824 and 2048 x 2048 to 8192 weights.
 constexpr int SHAPES = 4;
 FfnTile tile_of(int shape) {
-  constexpr FfnTile tiles[SHAPES] = {{128, 128, 1.1, 3.0}, {128, 256, 1.0, 3.0}, {192, 256, 1.43, 4.0}, {256, 256, 1.85, 5.0}};
+  constexpr FfnTile tiles[SHAPES] = {{128, 128, 1.01, 4.0}, {128, 256, 1.14, 3.0}, {192, 256, 1.26, 4.5}, {256, 256, 1.56, 8.0}};
   return tiles[shape];
 }
 uint32_t units_of(int shape) { return shape == 0 ? 2 * FFN_UNITS : FFN_UNITS; }
 
-template <bool Y_COLUMN, class T>
-hipError_t launch_grad_tiles(const GradArgs &a, uint64_t items, uint32_t units, hipStream_t s) {
-  eco_ffn_grad_kernel<Y_COLUMN, T><<<static_cast<uint32_t>(items < units ? items : units), T::THREADS, 0, s>>>(a);
-  return hipGetLastError();
-}
+uint64_t items_of(const FfnSplit &s) { return s.whole + static_cast<uint64_t>(s.tail) * s.splits; }
 
 }  // namespace
 
-hipError_t launch_ffn_weights_bf16(const FfnWeights &w, void *out, uint32_t padded_rows, hipStream_t s) {
-  const uint32_t grid = grid_of(static_cast<uint64_t>(w.matrices) * padded_rows * (w.dim / 8));
-  if (w.fmt == FMT_FP8) eco_ffn_weights_kernel<FMT_FP8><<<grid, 256, 0, s>>>(w, static_cast<uint16_t *>(out), padded_rows);
-  else eco_ffn_weights_kernel<FMT_INT4><<<grid, 256, 0, s>>>(w, static_cast<uint16_t *>(out), padded_rows);
-  return hipGetLastError();
-}
-hipError_t launch_ffn_rows_bf16(const FfnRows8 &x, void *out, uint32_t padded_rows, hipStream_t s) {
-  if (padded_rows == 0) return hipSuccess;
-  eco_ffn_rows_kernel<<<grid_of(static_cast<uint64_t>(padded_rows) * (x.dim / 8)), 256, 0, s>>>(x, static_cast<uint16_t *>(out), padded_rows);
-  return hipGetLastError();
-}
-hipError_t launch_ffn_pad(const void *src, uint64_t src_stride, uint32_t rows, uint32_t dim, void *out, uint32_t ld, hipStream_t s) {
-  if (rows == 0) return hipSuccess;
-  eco_ffn_pad_kernel<<<grid_of(static_cast<uint64_t>(rows) * (ld / 8)), 256, 0, s>>>(static_cast<const uint16_t *>(src), src_stride, rows, dim, static_cast<uint16_t *>(out), ld);
+hipError_t launch_ffn_operands(const FfnOperands &a, hipStream_t s) {
+  const uint32_t of_weights = a.weights ? grid_of(static_cast<uint64_t>(a.w.matrices) * a.padded_width * (a.w.dim / 8)) : 0;
+  const uint32_t of_rows = a.rows && a.padded_rows ? grid_of(static_cast<uint64_t>(a.padded_rows) * (a.x.dim / 8)) : 0;
+  const uint32_t all = of_weights + of_rows + (a.grad && a.x.rows ? grid_of(static_cast<uint64_t>(a.x.rows) * (a.grad_ld / 8)) : 0);
+  if (all == 0) return hipSuccess;
+  if (a.w.fmt == FMT_FP8) eco_ffn_operands_kernel<FMT_FP8><<<all, 256, 0, s>>>(a, of_weights, of_rows);
+  else eco_ffn_operands_kernel<FMT_INT4><<<all, 256, 0, s>>>(a, of_weights, of_rows);
   return hipGetLastError();
 }
 
-FfnGradPlan ffn_grad_plan(uint64_t nx, uint64_t ny, uint64_t k, uint32_t matrices) {
+// The tile shape, and the compute units' division between the products, that are done the soonest.
+FfnGradPlan ffn_grad_plan(const FfnGradSize &input, const FfnGradSize &weights) {
   FfnGradPlan best = {};
   double least = 0;
+  bool any = false;
   for (int shape = 0; shape < SHAPES; ++shape) {
     const FfnTile t = tile_of(shape);
-    FfnSplit split;
-    const double cost = ffn_split(ceil_div(nx, t.x) * ceil_div(ny, t.y) * matrices, ceil_div(k, KSTEP), units_of(shape), 4, t, &split);
-    if (shape == 0 || cost < least) { least = cost; best = {shape, split}; }
+    const uint32_t units = units_of(shape);
+    const auto tiles = [&](const FfnGradSize &g) { return ceil_div(g.nx, t.x) * ceil_div(g.ny, t.y) * g.matrices; };
+    for (uint32_t eighths = 1; eighths < 8; ++eighths) {
+      const uint32_t of_input = input.ny == 0 ? 0 : weights.ny == 0 ? units : units / 8 * eighths;
+      FfnGradPlan p = {shape, of_input, {}, {}};
+      double cost = 0;
+      if (input.ny) cost = ffn_split(tiles(input), ceil_div(input.k, KSTEP), of_input, 4, t, &p.input);
+      if (weights.ny) {
+        const double other = ffn_split(tiles(weights), ceil_div(weights.k, KSTEP), units - of_input, 4, t, &p.weights);
+        if (other > cost) cost = other;
+      }
+      if (!any || cost < least) { any = true; least = cost; best = p; }
+    }
   }
+  // no more workgroups than there are tiles
+  const uint64_t of_input = items_of(best.input);
+  if (of_input < best.of_input) best.of_input = static_cast<uint32_t>(of_input);
   return best;
 }
 
-hipError_t launch_ffn_grad(const FfnGradPlan &plan, bool columns, const FfnProduct &p, hipStream_t s) {
-  if (p.ny == 0) return hipSuccess;
+hipError_t launch_ffn_grad(const FfnGradPlan &plan, const FfnProduct &input, const FfnProduct &weights, hipStream_t s) {
   const FfnTile t = tile_of(plan.shape);
-  const GradArgs a = {p, static_cast<uint32_t>(ceil_div(p.nx, t.x)), static_cast<uint32_t>(ceil_div(p.ny, t.y)), static_cast<uint32_t>(ceil_div(p.k, KSTEP))};
-  const uint64_t items = plan.split.whole + static_cast<uint64_t>(plan.split.tail) * plan.split.splits;
-  const uint32_t units = units_of(plan.shape);
-  const auto go = [&](auto y_column) {
-    constexpr bool Y = decltype(y_column)::value;
-    switch (plan.shape) {
-      case 0: return launch_grad_tiles<Y, Medium>(a, items, units, s);
-      case 1: return launch_grad_tiles<Y, Large128>(a, items, units, s);
-      case 2: return launch_grad_tiles<Y, Large192>(a, items, units, s);
-      default: return launch_grad_tiles<Y, Large>(a, items, units, s);
-    }
+  const auto args = [&](const FfnProduct &p) {
+    return GradArgs{p, static_cast<uint32_t>(ceil_div(p.nx, t.x)), static_cast<uint32_t>(ceil_div(p.ny, t.y)), static_cast<uint32_t>(ceil_div(p.k, KSTEP))};
   };
-  const hipError_t e = columns ? go(std::true_type{}) : go(std::false_type{});
-  if (e != hipSuccess || plan.split.splits == 1) return e;
-  eco_ffn_grad_join_kernel<<<plan.split.tail * (t.x * t.y / 2048), 256, 0, s>>>(a, t.x, t.y);
+  const GradArgs i = args(input), w = args(weights);
+  const uint64_t of_weights = items_of(plan.weights), room = units_of(plan.shape) - plan.of_input;
+  const uint32_t grid = plan.of_input + static_cast<uint32_t>(of_weights < room ? of_weights : room);
+  if (grid == 0) return hipSuccess;
+  switch (plan.shape) {
+    case 0: eco_ffn_grad_kernel<Medium><<<grid, Medium::THREADS, 0, s>>>(i, w, plan.of_input); break;
+    case 1: eco_ffn_grad_kernel<Large128><<<grid, Large128::THREADS, 0, s>>>(i, w, plan.of_input); break;
+    case 2: eco_ffn_grad_kernel<Large192><<<grid, Large192::THREADS, 0, s>>>(i, w, plan.of_input); break;
+    default: eco_ffn_grad_kernel<Large><<<grid, Large::THREADS, 0, s>>>(i, w, plan.of_input);
+  }
+  const hipError_t e = hipGetLastError();
+  const uint32_t per_tile = t.x * t.y / 2048, join_input = plan.input.splits > 1 ? plan.input.tail * per_tile : 0, join_weights = plan.weights.splits > 1 ? plan.weights.tail * per_tile : 0;
+  if (e != hipSuccess || join_input + join_weights == 0) return e;
+  eco_ffn_grad_join_kernel<<<join_input + join_weights, 256, 0, s>>>(i, w, join_input, t.x, t.y);
   return hipGetLastError();
 }
 

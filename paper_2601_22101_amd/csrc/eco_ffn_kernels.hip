@@ -735,7 +735,10 @@ hipError_t launch_few(const FfnPlan &p, const ProductArgs &a, hipStream_t s) {
   return hipGetLastError();
 }
 
-__global__ __launch_bounds__(256) void eco_ffn_expand_kernel(const uint32_t *codes, uint64_t words, uint2 *out) {
+__global__ __launch_bounds__(256) void eco_ffn_expand_kernel(const uint32_t *first, const uint32_t *second, uint64_t words, uint2 *to_first, uint2 *to_second) {
+  const bool up = blockIdx.y;
+  const uint32_t *codes = up ? second : first;
+  uint2 *out = up ? to_second : to_first;
   for (uint64_t i = static_cast<uint64_t>(blockIdx.x) * 256 + threadIdx.x; i < words; i += static_cast<uint64_t>(gridDim.x) * 256) out[i] = e4m3_of_int4(codes[i]);
 }
 
@@ -822,9 +825,10 @@ hipError_t launch_ffn_join(const FfnPlan &p, const FfnRows8 &x, const FfnWeights
   return hipGetLastError();
 }
 
-hipError_t launch_ffn_expand(const void *codes, uint64_t numel, void *out, hipStream_t s) {
-  const uint64_t words = numel / 8, groups = (words + 255) / 256;      // (rows are multiples of 16 codes)
-  eco_ffn_expand_kernel<<<static_cast<uint32_t>(groups < 4096 ? groups : 4096), 256, 0, s>>>(static_cast<const uint32_t *>(codes), words, static_cast<uint2 *>(out));
+hipError_t launch_ffn_expand(const FfnWeights &w, void *const out[2], hipStream_t s) {
+  const uint64_t words = static_cast<uint64_t>(w.rows) * w.dim / 8, groups = ceil_div(words, 256);      // (rows are multiples of 16 codes)
+  eco_ffn_expand_kernel<<<dim3(static_cast<uint32_t>(groups < 4096 ? groups : 4096), w.matrices), 256, 0, s>>>(
+      static_cast<const uint32_t *>(w.data[0]), static_cast<const uint32_t *>(w.data[1]), words, static_cast<uint2 *>(out[0]), static_cast<uint2 *>(out[1]));
   return hipGetLastError();
 }
 
