@@ -66,21 +66,26 @@ struct ProductArgs {
 };
 
 // Loads to LDS as load_to_lds has them, which do not hold back the reads of LDS around them: those are of other steps' places, and the barriers between order them.
+__device__ __forceinline__ const void *uniform(const void *p) {      // the same in all lanes, and in scalar registers
+  const uint64_t v = reinterpret_cast<uint64_t>(p);
+  const uint32_t lo = __builtin_amdgcn_readfirstlane(static_cast<uint32_t>(v)), hi = __builtin_amdgcn_readfirstlane(static_cast<uint32_t>(v >> 32));
+  return reinterpret_cast<const void *>(static_cast<uint64_t>(hi) << 32 | lo);
+}
 __device__ __forceinline__ void step_to_lds(uint32_t lds, const void *base, uint32_t offset) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds), "v"(offset), "s"(base));
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds), "v"(offset), "s"(uniform(base)));
 }
 // From an address of each lane's own; a byte or a 16-bit value a lane as a dword, or a dword.
 __device__ __forceinline__ void lane_to_lds(uint32_t lds, const void *from) {
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds), "v"(from));
 }
 __device__ __forceinline__ void byte_to_lds(uint32_t lds, const void *base, uint32_t offset) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_ubyte %1, %2" ::"s"(lds), "v"(offset), "s"(base));
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_ubyte %1, %2" ::"s"(lds), "v"(offset), "s"(uniform(base)));
 }
 __device__ __forceinline__ void half_to_lds(uint32_t lds, const void *base, uint32_t offset) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_ushort %1, %2" ::"s"(lds), "v"(offset), "s"(base));
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_ushort %1, %2" ::"s"(lds), "v"(offset), "s"(uniform(base)));
 }
 __device__ __forceinline__ void dword_to_lds(uint32_t lds, const void *base, uint32_t offset) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2" ::"s"(lds), "v"(offset), "s"(base));
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2" ::"s"(lds), "v"(offset), "s"(uniform(base)));
 }
 
 __device__ const uint4 ffn_zeros = {0, 0, 0, 0};
@@ -389,60 +394,61 @@ __global__ __launch_bounds__(THREADS) void eco_ffn_kernel(ProductArgs a) {
               *reinterpret_cast<float4 *>(to + (16 * i + r) * T::BN + e) = make_float4(acc[i][e][r], acc[i][e + 1][r], acc[i][e + 2][r], acc[i][e + 3][r]);
         continue;
       }
-      const bool as_bf16 = a.o.bf16;
-      const uint64_t stride = a.o.out_stride;
-      char *const out = static_cast<char *>(a.o.out);
-      const bool whole = all && stride % (as_bf16 ? RUN : 4) == 0 && (reinterpret_cast<uintptr_t>(out) & (as_bf16 ? 2 * RUN - 1 : 15)) == 0;
-      const bool whole_add = all && a.o.add_stride % (as_bf16 ? RUN : 4) == 0 && (reinterpret_cast<uintptr_t>(a.o.add) & (as_bf16 ? 2 * RUN - 1 : 15)) == 0;
+      // (fp32 results are those of exact products)
+      typedef std::conditional_t<EXACT, float, uint16_t> Out;
+      constexpr int SIZE = sizeof(Out), WORDS = RUN * SIZE / 4, ALIGN = WORDS * 4 < 16 ? WORDS * 4 : 16;
+      Out *const out = static_cast<Out *>(a.o.out);
+      const bool whole = all && a.o.out_stride * SIZE % ALIGN == 0 && (reinterpret_cast<uintptr_t>(out) & (ALIGN - 1)) == 0;
+      // what is added: all of a lane's loads before the first is waited for, or, of wide tiles, which have no registers for them, those of a fragment of rows
+      constexpr int AT_ONCE = NJ == 4 && !EXACT ? MI : 1;
+      uint32_t more[AT_ONCE][4][WORDS];
+      const Out *const from = static_cast<const Out *>(a.o.add);
+      const bool whole_add = all && a.o.add_stride * SIZE % ALIGN == 0 && (reinterpret_cast<uintptr_t>(from) & (ALIGN - 1)) == 0;
+      const auto fetch = [&](int i) {
 #pragma unroll
-      for (int i = 0; i < MI; ++i)
+        for (int r = 0; r < 4; ++r) {
+          const uint32_t m = min(m0 + wm + 16 * i + row4 + r, a.x.rows - 1);
+          const Out *p = from + m * a.o.add_stride + n;
+          if (whole_add) __builtin_memcpy(more[i % AT_ONCE][r], __builtin_assume_aligned(p, ALIGN), sizeof more[0][0]);
+          else
+#pragma unroll
+            for (int e = 0; e < WORDS; ++e) {
+              if constexpr (EXACT) more[i % AT_ONCE][r][e] = n + e < a.w.rows ? f2u(p[e]) : 0u;
+              else more[i % AT_ONCE][r][e] = (n + 2 * e < a.w.rows ? p[2 * e] : 0u) | (n + 2 * e + 1 < a.w.rows ? p[2 * e + 1] : 0u) << 16;
+            }
+        }
+      };
+      if (from && AT_ONCE > 1)
+#pragma unroll
+        for (int i = 0; i < MI; ++i) fetch(i);
+#pragma unroll
+      for (int i = 0; i < MI; ++i) {
+        if (from) {
+          if (AT_ONCE == 1) fetch(i);
+#pragma unroll
+          for (int r = 0; r < 4; ++r)
+#pragma unroll
+            for (int e = 0; e < RUN; ++e)
+              acc[i][e][r] += EXACT ? u2f(more[i % AT_ONCE][r][e % WORDS]) : (e & 1) ? bf16_hi(more[i % AT_ONCE][r][e / 2 % WORDS]) : bf16_lo(more[i % AT_ONCE][r][e / 2 % WORDS]);
+        }
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
           const uint32_t m = m0 + wm + 16 * i + row4 + r;
           if (m >= a.x.rows || n >= a.w.rows) continue;
-          if (a.o.add) {
-            const uint64_t from = m * a.o.add_stride + n;
-            if (as_bf16) {
-              const uint16_t *p = static_cast<const uint16_t *>(a.o.add) + from;
-              uint32_t two[RUN / 2];
-              if (whole_add) __builtin_memcpy(two, __builtin_assume_aligned(p, 2 * RUN), sizeof two);
-              else
+          Out *to = out + m * a.o.out_stride + n;
+          uint32_t w[WORDS];
 #pragma unroll
-                for (int e = 0; e < RUN; e += 2) two[e / 2] = (n + e < a.w.rows ? p[e] : 0u) | (n + e + 1 < a.w.rows ? p[e + 1] : 0u) << 16;
+          for (int e = 0; e < WORDS; ++e) w[e] = EXACT ? f2u(acc[i][e][r]) : f32x2_to_bf16x2_rne(acc[i][2 * e % RUN][r], acc[i][(2 * e + 1) % RUN][r]);
+          if (whole) __builtin_memcpy(__builtin_assume_aligned(to, ALIGN), w, sizeof w);
+          else
 #pragma unroll
-              for (int e = 0; e < RUN; ++e) acc[i][e][r] += (e & 1) ? bf16_hi(two[e / 2]) : bf16_lo(two[e / 2]);
-            } else {
-              const float *p = static_cast<const float *>(a.o.add) + from;
-              float v[RUN];
-              if (whole_add) __builtin_memcpy(v, __builtin_assume_aligned(p, 16), sizeof v);
-              else
-#pragma unroll
-                for (int e = 0; e < RUN; ++e) v[e] = n + e < a.w.rows ? p[e] : 0.0f;
-#pragma unroll
-              for (int e = 0; e < RUN; ++e) acc[i][e][r] += v[e];
-            }
-          }
-          if (as_bf16) {
-            uint16_t *to = reinterpret_cast<uint16_t *>(out) + m * stride + n;
-            uint32_t two[RUN / 2];
-#pragma unroll
-            for (int e = 0; e < RUN; e += 2) two[e / 2] = f32x2_to_bf16x2_rne(acc[i][e][r], acc[i][e + 1][r]);
-            if (whole) __builtin_memcpy(__builtin_assume_aligned(to, 2 * RUN), two, sizeof two);
-            else
-#pragma unroll
-              for (int e = 0; e < RUN; ++e)
-                if (n + e < a.w.rows) to[e] = static_cast<uint16_t>(two[e / 2] >> (16 * (e & 1)));
-          } else {
-            float *to = reinterpret_cast<float *>(out) + m * stride + n;
-            if (whole)
-#pragma unroll
-              for (int e = 0; e < RUN; e += 4) *reinterpret_cast<float4 *>(to + e) = make_float4(acc[i][e][r], acc[i][e + 1][r], acc[i][e + 2][r], acc[i][e + 3][r]);
-            else
-#pragma unroll
-              for (int e = 0; e < RUN; ++e)
-                if (n + e < a.w.rows) to[e] = acc[i][e][r];
-          }
+            for (int e = 0; e < RUN; ++e)
+              if (n + e < a.w.rows) {
+                if constexpr (EXACT) to[e] = u2f(w[e]);
+                else to[e] = static_cast<uint16_t>(w[e / 2] >> (16 * (e & 1)));
+              }
         }
+      }
     }
 
     if constexpr (END == FFN_GATED) {
@@ -489,22 +495,27 @@ __global__ __launch_bounds__(THREADS) void eco_ffn_kernel(ProductArgs a) {
     if constexpr (END == FFN_GATED_BACK) {
       static_assert(RUN == 4, "a lane's gradients are eight bytes");
       const bool whole = all && a.o.grad_out_stride % 4 == 0 && (reinterpret_cast<uintptr_t>(a.o.grad_out) & 7) == 0;
+      uint32_t grads[MI][4][2];                                // all of a lane's on their way before the first is waited for
+#pragma unroll
+      for (int i = 0; i < MI; ++i)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const uint16_t *from = a.o.grad_out + min(m0 + wm + 16 * i + row4 + r, a.x.rows - 1) * a.o.grad_out_stride + n;
+          if (whole) __builtin_memcpy(grads[i][r], __builtin_assume_aligned(from, 8), 8);
+          else
+#pragma unroll
+            for (int e = 0; e < 4; e += 2) grads[i][r][e / 2] = (n + e < a.w.rows ? from[e] : 0u) | (n + e + 1 < a.w.rows ? from[e + 1] : 0u) << 16;
+        }
 #pragma unroll
       for (int i = 0; i < MI; ++i)
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
           const uint32_t m = m0 + wm + 16 * i + row4 + r;
           if (m >= a.x.rows || n >= a.o.half) continue;        // (half is whole fours; columns from the width to half leave as zeros)
-          const uint16_t *from = a.o.grad_out + m * a.o.grad_out_stride + n;
-          uint32_t two[2];
-          if (whole) __builtin_memcpy(two, __builtin_assume_aligned(from, 8), sizeof two);
-          else
-#pragma unroll
-            for (int e = 0; e < 4; e += 2) two[e / 2] = (n + e < a.w.rows ? from[e] : 0u) | (n + e + 1 < a.w.rows ? from[e + 1] : 0u) << 16;
           float ga[4], gb[4];
 #pragma unroll
           for (int j = 0; j < 4; ++j) {
-            const float grad = (j & 1) ? bf16_hi(two[j / 2]) : bf16_lo(two[j / 2]);
+            const float grad = (j & 1) ? bf16_hi(grads[i][r][j / 2]) : bf16_lo(grads[i][r][j / 2]);
             float f, df;
             act_both(acc[i][j][r], a.o.act, f, df);
             const bool there = all || n + j < a.w.rows;
