@@ -612,7 +612,7 @@ class _RowUnit:
                 if t is not None:
                     t.record_stream(s)
         args = (descriptor, self.workspace, self.workspace_bytes, stream) if workspace else (descriptor, stream)
-        if torch.cuda.current_device() == self.device.index:
+        if self.device.index == torch.cuda.current_device():
             call(*args)
         else:
             with torch.cuda.device(self.device):
@@ -657,9 +657,10 @@ class RowNorm(_RowUnit):
 
     def __init__(self, rows: int, dim: int, *, gain: Optional[torch.Tensor] = None, dtype: torch.dtype = torch.bfloat16, eps: float = 1e-6, residual: bool = False,
                  quantize: bool = True, training: bool = False, grad_gain_dtype: torch.dtype = torch.bfloat16, device=None):
-        self.device = dev = gain.device if gain is not None else torch.device("cuda", torch.cuda.current_device()) if device is None else torch.device(device)
-        if dev.type != "cuda" or dev.index is None:
+        dev = gain.device if gain is not None else torch.device("cuda" if device is None else device)
+        if dev.type != "cuda":
             raise ValueError("gain: memory of a GPU is needed")
+        self.device = dev = dev if dev.index is not None else torch.device("cuda", torch.cuda.current_device())
         if dtype not in _DTYPE or gain is not None and (gain.shape != (dim,) or gain.dtype not in _DTYPE or not gain.is_contiguous()):
             raise ValueError(f"dtype and gain: {' or '.join(map(str, _DTYPE))}, and {dim} contiguous gains, are needed")
         self.rows, self.dim, self.dtype, self.gain, self.has_residual, self.quantize, self.training = rows, dim, dtype, gain, residual, quantize, training

@@ -20,10 +20,6 @@ def harness():
     return harness
 
 
-def gen_of(*key):
-    return torch.Generator().manual_seed(hash(key) % (1 << 31))
-
-
 NORMS = [(1, 512), (1, 1), (2, 7), (3, 127), (5, 128), (4, 129), (33, 520), (7, 777), (65, 1152), (9, 1537), (300, 2048), (3, 2049), (5, 4100), (2, 8192), (3, 8200), (2, 20011)]
 
 
@@ -114,6 +110,8 @@ LINEARS = [
     (16, 1024, 1000, 256, "int4", "bf16"), (17, 6912, 257, 128, "fp8", "fp32"), (64, 2304, 129, 2304, "int4", "fp32"), (65, 1408, 2048, 128, "int4", "bf16"),
     (127, 1152, 300, 384, "fp8", "bf16"), (200, 272, 777, 272, "int4", "bf16"), (257, 640, 1153, 128, "fp8", "fp32"), (513, 48, 96, 10 ** 9, "fp8", "fp32"),
     (1025, 1152, 640, 1152, "fp8", "bf16"), (700, 2048, 1408, 2048, "int4", "fp32"),
+    # one step of the inner axis, or a piece of one; tiles that are split along it, with odd widths; whole rounds of tiles and a rest
+    (100, 16, 40, 16, "fp8", "fp32"), (70, 6912, 301, 128, "fp8", "fp32"), (4100, 4096, 1030, 4096, "int4", "fp32"), (8200, 128, 2200, 128, "fp8", "bf16"),
 ]
 
 
@@ -154,6 +152,7 @@ GATED = [
     (16, 1024, 1024, 128, "fp8", "fp32", "silu"), (31, 2048, 1408, 128, "int4", "bf16", "silu"), (64, 320, 255, 320, "fp8", "fp32", "gelu"),
     (65, 512, 2048, 256, "fp8", "bf16", "silu"), (130, 1152, 391, 1152, "int4", "bf16", "gelu"), (300, 1024, 1000, 128, "fp8", "fp32", "silu"),
     (513, 144, 4100, 10 ** 9, "fp8", "fp32", "gelu"), (1030, 384, 640, 384, "fp8", "fp32", "silu"),
+    (4100, 128, 2500, 128, "int4", "fp32", "gelu"), (66, 16, 7, 16, "fp8", "fp32", "silu"), (2100, 2048, 130, 256, "fp8", "bf16", "silu"),
 ]
 
 
@@ -401,3 +400,111 @@ def test_extreme_activations(harness):
             assert abs(v[k, 0].item() / want - 1) <= 2.0 ** -4 and v[k, 2] == v[k, 0]
         grads = unit.backward(torch.full((2, 4), 2.0 ** -20, dtype=torch.bfloat16, device="cuda"))
         assert all(torch.isfinite(g).all() for g in grads)
+
+
+def test_offsets_past_32_bits(harness):
+    """More than 2^32 codes: the last rows come out as they do by themselves."""
+    rows, dim, width = 65600, 65536, 16
+    gen = torch.Generator().manual_seed(5)
+    end = torch.randn(8, dim, generator=gen).bfloat16().cuda()
+    x = torch.zeros(rows, dim, dtype=torch.bfloat16, device="cuda")
+    x[-8:] = end
+    codes, scales = harness.quantize_rows(x)
+    want_codes, want_scales = harness.quantize_rows(end)
+    assert torch.equal(codes[-8:], want_codes) and torch.equal(scales[-8:], want_scales) and not codes[:-8].any()
+    norm = harness.RowNorm(rows, dim, quantize=False)
+    assert torch.equal(norm.forward(x)[0][-8:], harness.RowNorm(8, dim, quantize=False).forward(end)[0])
+    del x, norm
+    w, ws, values = weights(width, dim, "fp8", 128, "fp32", gen)
+    unit = harness.Linear(rows, dim, width, weights=w, scales=ws, training=True)
+    v = rows8_values(want_codes, want_scales)
+    hold(unit.forward(codes, scales)[-8:], v @ values.t(), product_bound(v, values), "out")
+    grad = torch.zeros(rows, width, dtype=torch.bfloat16, device="cuda")
+    grad[-8:] = torch.randn(8, width, generator=gen).bfloat16().cuda()
+    grad_input, grad_weights = unit.backward(grad)
+    g = grad[-8:].double()
+    want = gradients_exact([g], [values], v, [torch.zeros_like(g)])
+    hold(grad_input[-8:], want["grad_input"], want["grad_input_tol"], "grad_input")
+    assert not grad_input[:-8].any()
+    hold(grad_weights, want["grad_0"], want["grad_0_tol"] + 1e-30, "grad_weights")
+
+
+def test_units_at_once_on_two_streams(harness):
+    """Each with its own workspace, and what the allocator is told where a stream is given: the bits of one after the other."""
+    layers = [run_layer(harness, rows) for rows in (300, 500)]
+    want = [{k: v.clone() for k, v in step().items()} for step, _ in layers]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in layers]
+    for _ in range(3):
+        got = []
+        for (step, _), s in zip(layers, streams):
+            with torch.cuda.stream(s):
+                got.append(step())
+        torch.cuda.synchronize()
+        for g, w in zip(got, want):
+            for name, t in g.items():
+                assert torch.equal(t.view(torch.uint8), w[name].view(torch.uint8)), name
+
+
+def test_a_stream_that_is_given(harness):
+    gen, codes, code_scales, x, w, ws, values = make_linear(90, 256, 130, 256, "fp8", "fp32")
+    unit = harness.Linear(90, 256, 130, weights=w, scales=ws, group_size=256, training=True)
+    grad = torch.ones(90, 130, dtype=torch.bfloat16, device="cuda")
+    want = [unit.forward(codes, code_scales).clone(), *(t.clone() for t in unit.backward(grad))]
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    for s in (side, side.cuda_stream):
+        got = [unit.forward(codes, code_scales, stream=s), *unit.backward(grad, stream=s)]
+        side.synchronize()
+        assert all(torch.equal(p, q) for p, q in zip(got, want))
+
+
+def test_refusals(harness):
+    """A refused call leaves the object as it was."""
+    gen, codes, code_scales, x, w, ws, values = make_linear(9, 256, 130, 256, "fp8", "fp32")
+    unit = harness.Linear(9, 256, 130, weights=w, scales=ws, group_size=256, training=True)
+    with pytest.raises(RuntimeError, match="forward"):
+        unit.backward(torch.ones(9, 130, dtype=torch.bfloat16, device="cuda"))
+    first = unit.forward(codes, code_scales).clone()
+    more = torch.zeros(10, 256, dtype=torch.uint8, device="cuda")
+    for bad in ((codes.int(), code_scales), (codes[:, :240], code_scales), (codes, code_scales[:, :1]), (codes.cpu(), code_scales), (codes, code_scales[:5]), (None, code_scales),
+                (codes, None), (more, more[:, :2]), (codes.t().contiguous().t(), code_scales), (codes[0], code_scales)):
+        with pytest.raises(ValueError):
+            unit.forward(*bad)
+    for bad in (torch.ones(9, 130, device="cuda"), torch.ones(9, 130, dtype=torch.bfloat16), torch.ones(8, 130, dtype=torch.bfloat16, device="cuda"), None):
+        with pytest.raises(ValueError):
+            unit.backward(bad)
+    grad = torch.ones(9, 130, dtype=torch.bfloat16, device="cuda")
+    unit.backward(grad)
+    assert torch.equal(unit.forward(codes, code_scales), first)
+    plain = harness.Linear(9, 256, 130, weights=w, scales=ws, group_size=256)
+    plain.forward(codes, code_scales)
+    with pytest.raises(RuntimeError, match="training"):
+        plain.backward(grad)
+    with pytest.raises(ValueError):
+        harness.Linear(9, 256, 130, weights=w[:-1], scales=ws, group_size=256)
+    with pytest.raises(ValueError):
+        harness.Linear(9, 256, 130, weights=w, scales=ws[:-1], group_size=256)
+    with pytest.raises(ValueError):
+        harness.GatedUnit(9, 256, 130, gate=w, gate_scales=ws, up=w, up_scales=ws.bfloat16(), group_size=256)
+    with pytest.raises(ValueError):
+        harness.GatedUnit(9, 256, 130, gate=w, gate_scales=ws, up=w, up_scales=ws, group_size=256, act="relu")
+    norm = harness.RowNorm(9, 256, gain=torch.ones(256, device="cuda"))
+    with pytest.raises(ValueError):
+        norm.forward(torch.ones(9, 256, dtype=torch.bfloat16, device="cuda"), torch.ones(9, 256, dtype=torch.bfloat16, device="cuda"))
+    with pytest.raises(ValueError):
+        harness.RowNorm(9, 256, gain=torch.ones(255, device="cuda"))
+
+
+@pytest.mark.parametrize("fmt,act", [("fp8", "silu"), ("int4", "gelu")])
+def test_the_example_runs(fmt, act):
+    import importlib.util
+    import os
+    path = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples", "train_ffn.py")
+    spec = importlib.util.spec_from_file_location("train_ffn", path)
+    train_ffn = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(train_ffn)
+    losses, layer = train_ffn.train(steps=2, rows=130, fmt=fmt, act=act)
+    assert len(losses) == 2 and all(l > 0 and l == l for l in losses)
+    for m, v in layer.state:
+        assert torch.isfinite(m).all() and m.any() and (v >= 0).all() and v.any()
