@@ -4,6 +4,8 @@
 #include <hip/hip_runtime_api.h>
 #include <stdint.h>
 
+#include "../../include/eco.h"
+
 namespace eco {
 
 constexpr uint64_t FFN_MOST_ROWS = 1ull << 23, FFN_MOST_DIM = 1ull << 16, FFN_MOST_STRIDE = 1ull << 23;
@@ -12,7 +14,11 @@ constexpr uint32_t FFN_BLOCK = 128;               // elements of a row to a scal
 // of their own.  What the parts may take: a workspace is asked for once, for the most rows, and has to hold any call with fewer.
 constexpr uint32_t FFN_UNITS = 256;
 constexpr uint64_t FFN_MOST_SPLITS = 16, FFN_MOST_PARTIAL = 1ull << 24;      // elements
-constexpr uint64_t FFN_FEW_ROWS = 64;                          // the kernel for few rows; the gated unit's leaves h in fp32 as a partial
+// The most rows of the kernel for few rows, whose time grows with them, and those up to which it is always the faster: INT4 weights are wanted as E4M3 by tiles, a pass of its own.
+// us at 16, 32 and 64 rows and, from 17 on, of tiles: FP8 6912 x 1152 9.6, 13.3, 20.3 and 11.0 to 11.7; 14336 x 4096 20.7, 29.9, 44 and 18.1 to 18.6; gated 2048 x 1408 8.9, 10.3, 12.9
+// and 17.3; INT4 4096 x 14336 14.4, 17.8, 25.4 and 18.5 after 15 for the codes.
+constexpr uint64_t FFN_FEW_ROWS = 64;
+constexpr uint64_t ffn_always_few(int fmt) { return fmt == ECO_FMT_INT4 ? FFN_FEW_ROWS : 16; }
 
 constexpr uint64_t ffn_round_up(uint64_t x, uint64_t k) { return (x + k - 1) / k * k; }
 

@@ -162,7 +162,7 @@ Forward forward_of(const Unit &u, int end, Room room, Places &p, bool exact = fa
   Forward f;
   std::memset(&f, 0, sizeof f);
   if (room == MOST) {
-    if (u.rows <= eco::FFN_FEW_ROWS && end != eco::FFN_GATED_BACK) {
+    if (u.rows <= eco::ffn_always_few(u.fmt) && end != eco::FFN_GATED_BACK) {
       if (end == eco::FFN_GATED) (void)p.take(4 * u.rows * u.width);
       return f;
     }

@@ -573,10 +573,9 @@ __global__ __launch_bounds__(256) void eco_ffn_join_kernel(ProductArgs a, uint32
 
 // ------------------------------------------------------------------------------------------------ few rows
 
-// Up to 16 MT rows are bound by the reading of the weights: each wave reads 16 rows of them by itself, straight into the registers in which the matrix core takes
-// them, AHEAD blocks at a time, and INT4 codes become E4M3 there.  Nothing is kept in LDS but sums on their way from wave to wave.  (1 x 6912 x 1152 in FP8: 6.7 us; with
-// 8 or 4 columns to a workgroup, so that there are more of them than the 72, 8.9.)
-
+// Few rows are bound by the reading of the weights: each wave reads 16 NT rows of them by itself, straight into the registers in which the matrix core takes
+// them, AHEAD blocks at a time, and INT4 codes become E4M3 there.  Nothing is kept in LDS but sums on their way from wave to wave.  The products are exact ones in
+// bf16: they cost nothing beside the loads (linear 1 x 6912 x 1152 7.4 us, 7.9 in 8 bits; gated 24 x 1152 x 6912 13.5 and 11.7).
 template <class V>
 __device__ __forceinline__ V loose(const void *p) {            // at an address of any alignment
   V v;
@@ -618,15 +617,20 @@ struct Few {
   }
 };
 
-// The sums of 16 rows of weights from n0 on with all rows of x, over blocks first, first + stride, ...  acc[t][r]: row 16 t + 4 (lane >> 4) + r of x, row n0 + (lane & 15)
-// of the weights.
-template <int FMT, int MT, int MATRICES, int AHEAD, bool EXACT>
+// The sums of 16 NT rows of weights from n0 on with all rows of x, over blocks first, first + stride, ...  acc[t][u][r]: row 16 t + 4 (lane >> 4) + r of x, row
+// n0 + 16 u + (lane & 15) of the weights.
+template <int FMT, int MT, int NT, int MATRICES, int AHEAD>
 __device__ __forceinline__ void few_sums(const FfnRows8 &x, const FfnWeights &w, uint32_t n0, uint32_t first, uint32_t stride, int lane,
-                                         f32x4 (&acc)[MATRICES][MT]) {
+                                         f32x4 (&acc)[MATRICES][MT][NT]) {
   using F = Few<FMT>;
-  const uint32_t n = min(n0 + (lane & 15), w.rows - 1), q = lane >> 4;
-  const uint64_t row = static_cast<uint64_t>(n) * w.dim / (FMT == FMT_FP8 ? 1 : 2);
-  const uint64_t scale_row = static_cast<uint64_t>(n) * w.scale_row;
+  const uint32_t q = lane >> 4;
+  uint64_t row[NT], scale_row[NT];
+#pragma unroll
+  for (int u = 0; u < NT; ++u) {
+    const uint64_t n = min(n0 + 16 * u + (lane & 15), w.rows - 1);
+    row[u] = n * w.dim / (FMT == FMT_FP8 ? 1 : 2);
+    scale_row[u] = n * w.scale_row;
+  }
   const uint8_t *x_row[MT], *x_scale[MT];
 #pragma unroll
   for (int t = 0; t < MT; ++t) {
@@ -634,22 +638,27 @@ __device__ __forceinline__ void few_sums(const FfnRows8 &x, const FfnWeights &w,
     x_row[t] = x.codes + m * x.stride;
     x_scale[t] = x.scales + static_cast<uint64_t>(m) * x.blocks;
 #pragma unroll
-    for (int y = 0; y < MATRICES; ++y) acc[y][t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    for (int y = 0; y < MATRICES; ++y)
+#pragma unroll
+      for (int u = 0; u < NT; ++u) acc[y][t][u] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
   }
   for (uint32_t b0 = first; b0 < x.blocks; b0 += stride * AHEAD) {
-    typename F::Raw raw[MATRICES][AHEAD];
+    typename F::Raw raw[MATRICES][AHEAD][NT];
     i32x8 fx[AHEAD][MT];
     uint32_t sx[AHEAD][MT];
-    float sw[MATRICES][AHEAD];
+    float sw[MATRICES][AHEAD][NT];
 #pragma unroll
     for (int p = 0; p < AHEAD; ++p) {
       const uint32_t b = b0 + p * stride, k = b * STEP + q * F::FIRST;      // blocks past the last are all zeros
-      const uint64_t at = scale_row + (w.group_blocks ? min(b, x.blocks - 1) / w.group_blocks : 0);
+      const uint32_t group = w.group_blocks ? min(b, x.blocks - 1) / w.group_blocks : 0;
 #pragma unroll
-      for (int y = 0; y < MATRICES; ++y) {
-        raw[y][p] = F::read(static_cast<const uint8_t *>(w.data[y]) + row, k, w.dim);
-        sw[y][p] = w.scale_bf16 ? u2f(static_cast<uint32_t>(static_cast<const uint16_t *>(w.scales[y])[at]) << 16) : static_cast<const float *>(w.scales[y])[at];
-      }
+      for (int y = 0; y < MATRICES; ++y)
+#pragma unroll
+        for (int u = 0; u < NT; ++u) {
+          raw[y][p][u] = F::read(static_cast<const uint8_t *>(w.data[y]) + row[u], k, w.dim);
+          const uint64_t at = scale_row[u] + group;
+          sw[y][p][u] = w.scale_bf16 ? u2f(static_cast<uint32_t>(static_cast<const uint16_t *>(w.scales[y])[at]) << 16) : static_cast<const float *>(w.scales[y])[at];
+        }
 #pragma unroll
       for (int t = 0; t < MT; ++t) {
         const i32x4 zero = {0, 0, 0, 0}, u = k < w.dim ? *reinterpret_cast<const i32x4 *>(x_row[t] + k) : zero,
@@ -661,51 +670,52 @@ __device__ __forceinline__ void few_sums(const FfnRows8 &x, const FfnWeights &w,
 #pragma unroll
     for (int p = 0; p < AHEAD; ++p) {
       if (b0 + p * stride >= x.blocks) break;
+      Wide gx[MT];
 #pragma unroll
-      for (int y = 0; y < MATRICES; ++y) {
-        const i32x8 fw = F::codes(raw[y][p]);
-        const f32x4 zero = {0.0f, 0.0f, 0.0f, 0.0f};
-        Wide gw;
-        if constexpr (EXACT) gw = widen(fw, 1.0f);
+      for (int t = 0; t < MT; ++t) gx[t] = widen(fx[p][t], power_of(sx[p][t]));
 #pragma unroll
-        for (int t = 0; t < MT; ++t) {
-          f32x4 v;
-          if constexpr (EXACT) v = multiply(widen(fx[p][t], power_of(sx[p][t])), gw, zero);
-          else v = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(fx[p][t], fw, zero, 0, 0, 0, static_cast<int>(sx[p][t]), 0, 127);
+      for (int y = 0; y < MATRICES; ++y)
 #pragma unroll
-          for (int r = 0; r < 4; ++r) acc[y][t][r] = fmaf(v[r], sw[y][p], acc[y][t][r]);
+        for (int u = 0; u < NT; ++u) {
+          const f32x4 zero = {0.0f, 0.0f, 0.0f, 0.0f};
+          const Wide gw = widen(F::codes(raw[y][p][u]), 1.0f);
+#pragma unroll
+          for (int t = 0; t < MT; ++t) {
+            const f32x4 v = multiply(gx[t], gw, zero);
+#pragma unroll
+            for (int r = 0; r < 4; ++r) acc[y][t][u][r] = fmaf(v[r], sw[y][p][u], acc[y][t][u][r]);
+          }
         }
-      }
     }
   }
 }
 
-// 16 columns to a workgroup, whose waves have blocks of the inner axis in turn; the waves' sums are added in their order.  Of the gated unit the results are h in
-// fp32, which rows of 8 bits are made of next: a block of 128 is the work of eight workgroups.
-template <int FMT, int MT, int END, int WAVES, bool EXACT>
-__global__ __launch_bounds__(WAVES * 64) void eco_ffn_few_kernel(ProductArgs a) {
-  constexpr int MATRICES = END == FFN_GATED ? 2 : 1, AHEAD = MT == 1 ? 4 / MATRICES : MT == 2 ? 2 : 1;
-  __shared__ float sums[WAVES][MATRICES * MT * 4][64];
+// 16 NT columns to a workgroup, whose waves have blocks of the inner axis in turn; the waves' sums are added in their order.  Of the gated unit the results are h in
+// fp32, which rows of 8 bits are made of next: a block of 128 is the work of several workgroups.
+constexpr int FEW_WAVES = 8;
+template <int FMT, int MT, int NT, int END>
+__global__ __launch_bounds__(FEW_WAVES * 64) void eco_ffn_few_kernel(ProductArgs a) {
+  constexpr int MATRICES = END == FFN_GATED ? 2 : 1, EACH = MT * NT, AHEAD = MATRICES * NT + MT >= 5 ? 1 : MATRICES * NT + MT >= 3 ? 2 : 4;
+  __shared__ float sums[FEW_WAVES][MATRICES * EACH * 4][64];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const uint32_t n0 = blockIdx.x * 16;
-  f32x4 acc[MATRICES][MT];
-  few_sums<FMT, MT, MATRICES, AHEAD, EXACT>(a.x, a.w, n0, wave, WAVES, lane, acc);
+  const uint32_t n0 = blockIdx.x * 16 * NT;
+  f32x4 acc[MATRICES][MT][NT];
+  few_sums<FMT, MT, NT, MATRICES, AHEAD>(a.x, a.w, n0, wave, FEW_WAVES, lane, acc);
 #pragma unroll
   for (int y = 0; y < MATRICES; ++y)
 #pragma unroll
-    for (int t = 0; t < MT; ++t)
+    for (int t = 0; t < EACH; ++t)
 #pragma unroll
-      for (int r = 0; r < 4; ++r) sums[wave][(y * MT + t) * 4 + r][lane] = acc[y][t][r];
+      for (int r = 0; r < 4; ++r) sums[wave][(y * EACH + t) * 4 + r][lane] = acc[y][t / NT][t % NT][r];
   __syncthreads();
-  const uint32_t n = n0 + (lane & 15);
-  for (int at = wave; at < MT * 4; at += WAVES) {
+  for (int at = wave; at < EACH * 4; at += FEW_WAVES) {
     float v = 0.0f, u = 0.0f;
 #pragma unroll
-    for (int w = 0; w < WAVES; ++w) {
+    for (int w = 0; w < FEW_WAVES; ++w) {
       v += sums[w][at][lane];
-      if (MATRICES == 2) u += sums[w][MT * 4 + at][lane];
+      if (MATRICES == 2) u += sums[w][EACH * 4 + at][lane];
     }
-    const uint32_t m = at / 4 * 16 + 4 * (lane >> 4) + at % 4;
+    const uint32_t n = n0 + at / 4 % NT * 16 + (lane & 15), m = at / 4 / NT * 16 + 4 * (lane >> 4) + at % 4;
     if (m >= a.x.rows || n >= a.w.rows) continue;
     if constexpr (END == FFN_GATED) {
       a.o.partial[static_cast<uint64_t>(m) * a.w.rows + n] = act_of(v, a.o.act) * u;
@@ -722,28 +732,36 @@ __global__ __launch_bounds__(WAVES * 64) void eco_ffn_few_kernel(ProductArgs a) 
   }
 }
 
-template <int FMT>
-hipError_t launch_few(const FfnPlan &p, const ProductArgs &a, hipStream_t s) {
-  const uint32_t grid = (a.w.rows + 15) / 16;
-  if (p.end == FFN_GATED) {
-    if (a.x.rows <= 16) eco_ffn_few_kernel<FMT, 1, FFN_GATED, 8, false><<<grid, 8 * 64, 0, s>>>(a);
-    else if (a.x.rows <= 32) eco_ffn_few_kernel<FMT, 2, FFN_GATED, 8, false><<<grid, 8 * 64, 0, s>>>(a);
-    else eco_ffn_few_kernel<FMT, 4, FFN_GATED, 8, false><<<grid, 8 * 64, 0, s>>>(a);
-    const hipError_t e = hipGetLastError();
-    if (e != hipSuccess) return e;
-    NormRows r = {};
-    r.input = a.o.partial; r.out = a.o.out; r.scales = a.o.scales; r.input_stride = r.dim = a.w.rows; r.out_stride = a.o.out_stride; r.rows = a.x.rows;
-    return launch_norm(r, s);
-  }
-  const auto go = [&](auto exact) {
-    constexpr bool E = decltype(exact)::value;
-    if (a.x.rows <= 16) eco_ffn_few_kernel<FMT, 1, FFN_LINEAR, 16, E><<<grid, 16 * 64, 0, s>>>(a);
-    else if (a.x.rows <= 32) eco_ffn_few_kernel<FMT, 2, FFN_LINEAR, 16, E><<<grid, 16 * 64, 0, s>>>(a);
-    else eco_ffn_few_kernel<FMT, 4, FFN_LINEAR, 16, E><<<grid, 16 * 64, 0, s>>>(a);
-  };
-  if (p.exact) go(std::true_type{});
-  else go(std::false_type{});
-  return hipGetLastError();
+template <int FMT, int MT, int NT, int END>
+void launch_few_of(const ProductArgs &a, hipStream_t s) {
+  eco_ffn_few_kernel<FMT, MT, NT, END><<<(a.w.rows + 16 * NT - 1) / (16 * NT), FEW_WAVES * 64, 0, s>>>(a);
+}
+// Columns of a workgroup, by 16: four, which read each row of x a quarter as often, where that leaves three workgroups to a compute unit, two where there would be one
+// and a half of one, and else one.  us with 16, 32 and 64: linear, 1 and 32 rows, 4096 x 14336 17.1, 16.2, 15.3 and 35.4, 27.5, 21.2; 14336 x 4096 15.2, 23.3, 42.8 and
+// 30.0, 37.9, 56.0; gated 1152 x 6912 9.3, 8.9, 11.9 and 13.9, 11.2, 14.7.
+constexpr int few_wide(int mt, bool gated) { return mt * (gated ? 2 : 1) <= 4 ? 4 : 2; }      // (what the sums' place in LDS holds)
+uint32_t few_columns(uint64_t width, int mt, bool gated) {
+  const uint64_t groups = (width + 15) / 16;
+  return groups >= 3 * FFN_UNITS ? few_wide(mt, gated) : groups >= FFN_UNITS * 3 / 2 ? 2 : 1;
+}
+template <int FMT, int MT, int END>
+void launch_few_rows(const ProductArgs &a, hipStream_t s) {
+  constexpr bool GATED = END == FFN_GATED;
+  const uint32_t columns = few_columns(a.w.rows, MT, GATED), grid = (a.w.rows + 16 * columns - 1) / (16 * columns);
+  if (columns == 1) eco_ffn_few_kernel<FMT, MT, 1, END><<<grid, FEW_WAVES * 64, 0, s>>>(a);
+  else if (columns == 2) eco_ffn_few_kernel<FMT, MT, 2, END><<<grid, FEW_WAVES * 64, 0, s>>>(a);
+  else eco_ffn_few_kernel<FMT, MT, few_wide(MT, GATED), END><<<grid, FEW_WAVES * 64, 0, s>>>(a);
+}
+template <int FMT, int END>
+hipError_t launch_few(const ProductArgs &a, hipStream_t s) {
+  if (a.x.rows <= 16) launch_few_rows<FMT, 1, END>(a, s);
+  else if (a.x.rows <= 32) launch_few_rows<FMT, 2, END>(a, s);
+  else launch_few_rows<FMT, 4, END>(a, s);
+  const hipError_t e = hipGetLastError();
+  if (END != FFN_GATED || e != hipSuccess) return e;
+  NormRows r = {};
+  r.input = a.o.partial; r.out = a.o.out; r.scales = a.o.scales; r.input_stride = r.dim = a.w.rows; r.out_stride = a.o.out_stride; r.rows = a.x.rows;
+  return launch_norm(r, s);
 }
 
 __global__ __launch_bounds__(256) void eco_ffn_expand_kernel(const uint32_t *first, const uint32_t *second, uint64_t words, uint2 *to_first, uint2 *to_second) {
@@ -787,16 +805,24 @@ double ffn_split(uint64_t tiles, uint64_t steps, uint64_t units, uint64_t least_
   return of_whole + least;
 }
 
+// Microseconds of the kernel for few rows: a block's loads and its share of products for each of a wave's fragments, or what the weights take, and for the gated unit the launch
+// that makes 8-bit rows.  Measured and by this rule, 32 and 64 rows: linear 6912 x 1152 13.3, 20.3 and 14.5, 19.4; 2048 x 1408 6.4, 8.9 and 6.0, 7.4; 4096 x 14336 20.9, 28.0
+// and 17.8, 29.0; gated 2048 x 1408 10.3, 12.9 and 9.8, 11.6; 4096 x 14336 37.3, 52.8 and 34, 43.
+double few_cost(const FfnWeights &w, uint64_t rows, bool gated) {
+  const int mt = rows <= 16 ? 1 : rows <= 32 ? 2 : 4, columns = static_cast<int>(few_columns(w.rows, mt, gated)), fragments = mt * columns * (gated ? 2 : 1);
+  const uint64_t blocks = (w.dim + FFN_BLOCK - 1) / FFN_BLOCK, each = (blocks + FEW_WAVES - 1) / FEW_WAVES, groups = (w.rows + 16 * columns - 1) / (16 * columns);
+  const uint64_t at_once = FFN_UNITS * (fragments > 8 ? 1 : 2);      // (by the sums' place in LDS)
+  const double work = static_cast<double>((groups + at_once - 1) / at_once * each) * (1.0 + (gated ? 0.228 : 0.35) * fragments);
+  const double bytes = static_cast<double>(w.rows) * w.dim * (gated ? 2 : 1) / 4.2e6;
+  return (work < bytes ? bytes : work) + (gated ? 6.0 : 2.6);
+}
+
 // Microseconds of a step of 128 and of a tile's ends (8192 x 6912 and 8192 x 1024 over widths that are whole rounds: 256 x 256 122 and 26 us, 256 x 128 73 and 18,
 // 128 x 128 46 and 11.5, 64 x 128 33 and 8.9; gated, tiles of 256, 128 and 64 rows, 120 and 27, 75 and 17, 57 and 12).  In bf16 products a step is of twice the work.
 FfnPlan ffn_plan(int end, const FfnWeights &w, uint64_t rows, bool exact) {
   const uint32_t steps = (w.dim + FFN_BLOCK - 1) / FFN_BLOCK;
   FfnPlan p = {end, 256, 256, exact, {0, 0, 1, steps, 0}};
   if (rows == 0) return p;
-  if (end != FFN_GATED_BACK && rows <= FFN_FEW_ROWS) {
-    p.rows_tile = p.width_tile = 0;
-    return p;
-  }
   const FfnTile linear[] = {{256, 256, 2.09, 4.5}, {128, 256, 1.2, 3.5}, {128, 128, 0.75, 2.0}, {128, 64, 0.51, 1.5}};
   const FfnTile gated[] = {{128, 256, 2.04, 5.5}, {128, 128, 1.25, 3.5}, {128, 64, 0.97, 2.0}};
   const FfnTile in_bf16[] = {{128, 256, 2.4, 3.5}, {128, 128, 1.4, 2.0}, {128, 64, 0.9, 1.5}};
@@ -815,13 +841,17 @@ FfnPlan ffn_plan(int end, const FfnWeights &w, uint64_t rows, bool exact) {
       p.split = split;
     }
   }
+  if (end != FFN_GATED_BACK && rows <= FFN_FEW_ROWS && (rows <= ffn_always_few(w.fmt) || few_cost(w, rows, !product) < least + 2.5)) p = {end, 0, 0, exact, {0, 0, 1, steps, 0}};
   return p;
 }
 
 hipError_t launch_ffn(const FfnPlan &p, const FfnRows8 &x, const FfnWeights &w, const FfnOut &o, hipStream_t s) {
   if (x.rows == 0) return hipSuccess;
   const ProductArgs a = args_of(p, x, w, o);
-  if (p.rows_tile == 0) return w.fmt == FMT_INT4 ? launch_few<FMT_INT4>(p, a, s) : launch_few<FMT_FP8>(p, a, s);
+  if (p.rows_tile == 0) {
+    if (p.end == FFN_GATED) return w.fmt == FMT_INT4 ? launch_few<FMT_INT4, FFN_GATED>(a, s) : launch_few<FMT_FP8, FFN_GATED>(a, s);
+    return w.fmt == FMT_INT4 ? launch_few<FMT_INT4, FFN_LINEAR>(a, s) : launch_few<FMT_FP8, FFN_LINEAR>(a, s);
+  }
   const auto by_rows = [&](auto of_256, auto of_128, auto of_64) { return p.rows_tile == 256 ? of_256(p, a, s) : p.rows_tile == 128 ? of_128(p, a, s) : of_64(p, a, s); };
   if (p.end == FFN_GATED) return by_rows(launch_tiles<4, 8, FFN_GATED, false>, launch_tiles<2, 8, FFN_GATED, false>, launch_tiles<1, 8, FFN_GATED, false>);
   if (p.end == FFN_GATED_BACK)

@@ -111,6 +111,9 @@ LINEARS = [
     (127, 1152, 300, 384, "fp8", "bf16"), (200, 272, 777, 272, "int4", "bf16"), (257, 640, 1153, 128, "fp8", "fp32"), (513, 48, 96, 10 ** 9, "fp8", "fp32"),
     (1025, 1152, 640, 1152, "fp8", "bf16"), (700, 2048, 1408, 2048, "int4", "fp32"),
     # one step of the inner axis, or a piece of one; tiles that are split along it, with odd widths; whole rounds of tiles and a rest
+    # few rows: each width of a workgroup with each number of rows
+    (9, 256, 12301, 128, "fp8", "fp32"), (30, 144, 12301, 144, "fp8", "bf16"), (20, 272, 6150, 272, "fp8", "fp32"), (50, 2048, 200, 128, "fp8", "fp32"),
+    (16, 400, 6150, 400, "int4", "fp32"), (2, 256, 12300, 256, "int4", "bf16"), (32, 256, 12301, 128, "int4", "fp32"), (60, 256, 12301, 256, "int4", "fp32"), (64, 144, 6150, 144, "int4", "bf16"),
     (100, 16, 40, 16, "fp8", "fp32"), (70, 6912, 301, 128, "fp8", "fp32"), (4100, 4096, 1030, 4096, "int4", "fp32"), (8200, 128, 2200, 128, "fp8", "bf16"),
 ]
 
@@ -152,6 +155,8 @@ GATED = [
     (16, 1024, 1024, 128, "fp8", "fp32", "silu"), (31, 2048, 1408, 128, "int4", "bf16", "silu"), (64, 320, 255, 320, "fp8", "fp32", "gelu"),
     (65, 512, 2048, 256, "fp8", "bf16", "silu"), (130, 1152, 391, 1152, "int4", "bf16", "gelu"), (300, 1024, 1000, 128, "fp8", "fp32", "silu"),
     (513, 144, 4100, 10 ** 9, "fp8", "fp32", "gelu"), (1030, 384, 640, 384, "fp8", "fp32", "silu"),
+    (9, 256, 12301, 128, "fp8", "fp32", "silu"), (30, 144, 12301, 144, "fp8", "bf16", "gelu"), (20, 272, 6150, 272, "fp8", "fp32", "silu"), (50, 1024, 200, 128, "fp8", "fp32", "silu"),
+    (2, 256, 6150, 256, "int4", "fp32", "gelu"), (32, 256, 12301, 128, "int4", "fp32", "silu"), (60, 256, 12301, 256, "int4", "fp32", "silu"), (64, 144, 6150, 144, "int4", "bf16", "silu"),
     (4100, 128, 2500, 128, "int4", "fp32", "gelu"), (66, 16, 7, 16, "fp8", "fp32", "silu"), (2100, 2048, 130, 256, "fp8", "bf16", "silu"),
 ]
 
