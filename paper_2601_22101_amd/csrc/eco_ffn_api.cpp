@@ -145,9 +145,10 @@ struct Places {
   uint64_t take(uint64_t n) { const uint64_t here = bytes; bytes += eco::ffn_round_up(n, 256); return here; }
 };
 
-// What the parts of a product of up to ny x nx results may take: split tiles are at most 256 x 256.
+// What the parts of a product of up to ny x nx results may take: split tiles have 64, 128 or 256 rows and 64, 128, 192 or 256 columns.
 uint64_t most_partial(uint64_t ny, uint64_t nx, uint64_t matrices) {
-  return least(eco::FFN_MOST_PARTIAL, eco::FFN_MOST_SPLITS * eco::ffn_round_up(ny, 256) * eco::ffn_round_up(nx, 256) * matrices);
+  const uint64_t by_256 = eco::ffn_round_up(nx, 256), by_192 = eco::ffn_round_up(nx, 192);
+  return least(eco::FFN_MOST_PARTIAL, eco::FFN_MOST_SPLITS * eco::ffn_round_up(ny, 256) * (by_256 < by_192 ? by_192 : by_256) * matrices);
 }
 
 // A product in 8 bits: INT4 weights as E4M3, and the parts of sums.

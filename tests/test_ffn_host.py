@@ -111,7 +111,7 @@ def test_a_workspace_is_enough_for_fewer_rows(eco, fmt):
         l, g = linear(eco, rows=most, in_dim=in_dim, out_dim=width, fmt=fmt), gated(eco, rows=most, in_dim=in_dim, width=width, fmt=fmt)
         sizes = [eco.eco_linear_workspace(l, b) for b in (False, True)] + [eco.eco_gated_workspace(g, b) for b in (False, True)]
         last = [0] * 4
-        for rows in [0, 1, 2, 63, 64, 65, 127, 128, 129, 255, 256, 257, 500, 640, 1000, 1025, 2047, 2049, most]:
+        for rows in [0, 1, 2, 16, 17, 32, 33, 63, 64, 65, 127, 128, 129, 255, 256, 257, 500, 640, 1000, 1025, 2047, 2049, most]:
             l.rows = g.rows = rows
             now = [eco.eco_linear_workspace(l, b) for b in (False, True)] + [eco.eco_gated_workspace(g, b) for b in (False, True)]
             assert all(a <= b for a, b in zip(last, now)), rows
@@ -121,6 +121,17 @@ def test_a_workspace_is_enough_for_fewer_rows(eco, fmt):
                     status(eco, call, d, 0x100000, now[n], 0)
                     assert "workspace" not in eco.eco_last_error(), (rows, n)
         assert last == sizes
+
+
+@pytest.mark.parametrize("kind,fmt,in_dim,width,rows", [("gated", 1, 1216, 7167, 169), ("gated", 0, 1280, 7162, 131), ("linear", 0, 1024, 211, 28608), ("linear", 1, 1184, 166, 17051)])
+def test_a_workspace_is_enough_for_tiles_of_192(eco, kind, fmt, in_dim, width, rows):
+    """Few tiles of 192 columns, split in fifteen or sixteen parts, which end further behind the last column than those of 256."""
+    make, size, back = {"linear": (linear, eco.eco_linear_workspace, eco.eco_linear_backward), "gated": (gated, eco.eco_gated_workspace, eco.eco_gated_backward)}[kind]
+    d = make(eco, rows=rows, in_dim=in_dim, group_size=in_dim, fmt=fmt, **{"out_dim" if kind == "linear" else "width": width})
+    if torch.cuda.is_available():
+        pytest.skip("the pointers are none")
+    status(eco, back, d, 0x100000, size(d, True), 0)
+    assert "workspace" not in eco.eco_last_error()
 
 
 def test_harness_refusals():
