@@ -58,6 +58,11 @@ eco_status_t check_rows(const char *what, const char *name, const void *p, uint6
   if (!aligned(p, align)) return fail(ECO_EALIGN, "%s: %s is not aligned to %llu bytes", what, name, (unsigned long long)align);
   return check_stride(what, name, stride, packed);
 }
+// Rows that are written where others are read, each after it was read: the two have to lie in the same places.
+eco_status_t check_in_place(const char *what, const char *out, const void *p, uint64_t stride, const char *in, const void *q, uint64_t in_stride, uint64_t packed) {
+  if (p && p == q && stride_or(stride, packed) != stride_or(in_stride, packed)) return fail(ECO_EINVAL, "%s: %s is %s with another stride", what, out, in);
+  return ECO_OK;
+}
 eco_status_t check_workspace(const char *what, const void *workspace, size_t bytes, uint64_t need) {
   if (need == 0) return ECO_OK;
   if (!workspace) return fail(ECO_EINVAL, "%s: null workspace", what);
@@ -323,6 +328,8 @@ eco_status_t eco_norm(const eco_norm_t *n, void *stream) {
   if (n->residual) {
     CHECK(check_rows("norm", "residual", n->residual, n->rows, n->residual_stride, n->dim, size));
     CHECK(check_rows("norm", "sum", n->sum, n->rows, n->sum_stride, n->dim, size));
+    CHECK(check_in_place("norm", "sum", n->sum, n->sum_stride, "input", n->input, n->input_stride, n->dim));
+    CHECK(check_in_place("norm", "sum", n->sum, n->sum_stride, "residual", n->residual, n->residual_stride, n->dim));
   } else if (n->sum && n->rows) {
     return fail(ECO_EINVAL, "norm: a sum without a residual");
   }
@@ -357,6 +364,8 @@ eco_status_t eco_norm_backward(const eco_norm_t *n, void *workspace, size_t work
   CHECK(check_rows("norm", "grad_out", n->grad_out, n->rows, n->grad_out_stride, n->dim, size));
   if (n->grad_sum) CHECK(check_rows("norm", "grad_sum", n->grad_sum, n->rows, n->grad_sum_stride, n->dim, size));
   if (n->grad_input) CHECK(check_rows("norm", "grad_input", n->grad_input, n->rows, n->grad_input_stride, n->dim, size));
+  CHECK(check_in_place("norm", "grad_input", n->grad_input, n->grad_input_stride, "grad_out", n->grad_out, n->grad_out_stride, n->dim));
+  CHECK(check_in_place("norm", "grad_input", n->grad_input, n->grad_input_stride, "grad_sum", n->grad_sum, n->grad_sum_stride, n->dim));
   CHECK(check_rows("norm", "rstd", n->rstd, n->rows, 0, 1, 4));
   if (n->grad_gain && !is_dtype(n->grad_gain_dtype)) return fail(ECO_EINVAL, "norm: unknown dtype of grad_gain");
   if (n->grad_gain && !aligned(n->grad_gain, size_of(n->grad_gain_dtype))) return fail(ECO_EALIGN, "norm: grad_gain is not aligned to its elements");
@@ -391,6 +400,7 @@ eco_status_t eco_linear(const eco_linear_t *l, void *workspace, size_t workspace
   const uintptr_t size = size_of(l->out_dtype);
   CHECK(check_rows("linear", "out", l->out, l->rows, l->out_stride, l->out_dim, size));
   if (l->add) CHECK(check_rows("linear", "add", l->add, l->rows, l->add_stride, l->out_dim, size));
+  CHECK(check_in_place("linear", "out", l->out, l->out_stride, "add", l->add, l->add_stride, l->out_dim));
   Places p;
   const Unit u = unit_of(l);
   const Forward f = forward_of(u, eco::FFN_LINEAR, EXACT, p, l->out_dtype == ECO_DT_FP32);

@@ -134,6 +134,19 @@ def test_a_workspace_is_enough_for_tiles_of_192(eco, kind, fmt, in_dim, width, r
     assert "workspace" not in eco.eco_last_error()
 
 
+def test_in_place_with_another_stride_is_refused(eco):
+    """A row would be written over others that are still to be read."""
+    for kw in (dict(sum=0x1000, sum_stride=600), dict(sum=0x2000, residual_stride=520), dict(sum=0x1000, input_stride=1024)):
+        assert status(eco, eco.eco_norm, norm(eco, **kw), 0) == eco.ECO_EINVAL and "stride" in eco.eco_last_error()
+    for kw in (dict(grad_input=0x8000, grad_out_stride=520), dict(grad_input=0x9000, grad_input_stride=600)):
+        assert status(eco, eco.eco_norm_backward, norm(eco, **kw), 0x10000, 1 << 30, 0) == eco.ECO_EINVAL and "stride" in eco.eco_last_error()
+    for kw in (dict(add=0x6000, add_stride=264), dict(add=0x6000, out_stride=512)):
+        assert status(eco, eco.eco_linear, linear(eco, **kw), 0x100000, 1 << 40, 0) == eco.ECO_EINVAL and "stride" in eco.eco_last_error()
+    if not torch.cuda.is_available():                         # (the same, given once as 0 and once as a number, gets past the checks)
+        for d, run in ((norm(eco, sum=0x1000, sum_stride=512), lambda d: eco.eco_norm(d, 0)), (linear(eco, add=0x6000, add_stride=256), lambda d: eco.eco_linear(d, 0x100000, 1 << 40, 0))):
+            assert status(eco, run, d) not in (eco.ECO_EINVAL, eco.ECO_EALIGN, eco.ECO_EUNSUPPORTED)
+
+
 def test_harness_refusals():
     from paper_2601_22101_amd import harness
     w, s = torch.zeros(256, 128, dtype=torch.uint8), torch.ones(256)
