@@ -90,13 +90,14 @@ hipError_t launch_ffn_expand(const FfnWeights &, void *const out[2], hipStream_t
 
 // ---- gradients, of bf16 operands
 // Weights as bf16 rows [matrices][padded_width][dim], zeros in the padding; x [padded_rows][dim] the same; the output's gradient copied to rows of grad_ld, zeros behind
-// them.  Those that are null are not made.
+// them; INT4 weights as E4M3 codes as well, as launch_ffn_expand makes them, where bf16 ones are made.  Those that are null are not made.
 struct FfnOperands {
   FfnWeights w;
   FfnRows8 x;
   const uint16_t *grad_from;
   uint64_t grad_stride;
   uint16_t *weights, *rows, *grad;
+  void *codes[2];
   uint32_t padded_width, padded_rows, grad_ld;
 };
 hipError_t launch_ffn_operands(const FfnOperands &, hipStream_t);

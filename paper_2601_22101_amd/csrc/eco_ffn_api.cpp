@@ -187,11 +187,12 @@ Forward forward_of(const Unit &u, int end, Room room, Places &p, bool exact = fa
   if (f.joins || f.rounds) f.partial = p.take(4 * (f.joins ? f.plan.split.partial : u.rows * u.width));
   return f;
 }
-eco_status_t product(const Unit &u, const Forward &f, eco::FfnOut o, char *ws, hipStream_t s) {
+// there: the E4M3 codes of INT4 weights are in the workspace.
+eco_status_t product(const Unit &u, const Forward &f, eco::FfnOut o, bool there, char *ws, hipStream_t s) {
   eco::FfnWeights w = weights_of(u);
   if (f.expands) {
     void *const codes[2] = {ws + f.expanded[0], ws + f.expanded[1]};
-    LAUNCH(u.what, eco::launch_ffn_expand(w, codes, s));
+    if (!there) LAUNCH(u.what, eco::launch_ffn_expand(w, codes, s));
     for (uint32_t m = 0; m < u.matrices; ++m) w.data[m] = codes[m];
     w.fmt = ECO_FMT_FP8_E4M3;
   }
@@ -229,7 +230,7 @@ Backward backward_of(const Unit &u, bool input, bool weights, bool copies, Room 
   if (of_weights) b.weights_partial = p.take(4 * of_weights);
   return b;
 }
-eco_status_t operands(const Unit &u, const Backward &b, const void *grad, uint64_t grad_stride, char *ws, hipStream_t s) {
+eco_status_t operands(const Unit &u, const Backward &b, const void *grad, uint64_t grad_stride, const Forward *f, char *ws, hipStream_t s) {
   eco::FfnOperands o;
   std::memset(&o, 0, sizeof o);
   o.w = weights_of(u); o.x = rows_of(u);
@@ -237,6 +238,8 @@ eco_status_t operands(const Unit &u, const Backward &b, const void *grad, uint64
   if (b.input) o.weights = reinterpret_cast<uint16_t *>(ws + b.w);
   if (b.weights) o.rows = reinterpret_cast<uint16_t *>(ws + b.x);
   if (grad) { o.grad = reinterpret_cast<uint16_t *>(ws + b.grad); o.grad_from = static_cast<const uint16_t *>(grad); o.grad_stride = grad_stride; o.grad_ld = static_cast<uint32_t>(b.half); }
+  if (f)
+    for (uint32_t m = 0; m < u.matrices; ++m) o.codes[m] = ws + f->expanded[m];
   LAUNCH(u.what, eco::launch_ffn_operands(o, s));
   return ECO_OK;
 }
@@ -411,7 +414,7 @@ eco_status_t eco_linear(const eco_linear_t *l, void *workspace, size_t workspace
   std::memset(&o, 0, sizeof o);
   o.add = l->add; o.out = l->out; o.add_stride = stride_or(l->add_stride, l->out_dim); o.out_stride = stride_or(l->out_stride, l->out_dim);
   o.bf16 = l->out_dtype == ECO_DT_BF16;
-  return product(u, f, o, static_cast<char *>(workspace), static_cast<hipStream_t>(stream));
+  return product(u, f, o, false, static_cast<char *>(workspace), static_cast<hipStream_t>(stream));
 }
 
 eco_status_t eco_linear_backward(const eco_linear_t *l, void *workspace, size_t workspace_bytes, void *stream) {
@@ -427,7 +430,7 @@ eco_status_t eco_linear_backward(const eco_linear_t *l, void *workspace, size_t 
   hipStream_t s = static_cast<hipStream_t>(stream);
   const void *grad = l->grad_out;
   uint64_t ldy = stride_or(l->grad_out_stride, l->out_dim);
-  CHECK(operands(u, b, copies ? grad : nullptr, ldy, ws, s));
+  CHECK(operands(u, b, copies ? grad : nullptr, ldy, nullptr, ws, s));
   if (copies) {
     grad = ws + b.grad;
     ldy = b.half;
@@ -459,7 +462,7 @@ eco_status_t eco_gated(const eco_gated_t *g, void *workspace, size_t workspace_b
   eco::FfnOut o;
   std::memset(&o, 0, sizeof o);
   o.out = g->out; o.out_stride = stride_or(g->out_stride, g->width); o.scales = static_cast<uint8_t *>(g->out_scales); o.act = g->act;
-  return product(u, f, o, static_cast<char *>(workspace), static_cast<hipStream_t>(stream));
+  return product(u, f, o, false, static_cast<char *>(workspace), static_cast<hipStream_t>(stream));
 }
 
 eco_status_t eco_gated_backward(const eco_gated_t *g, void *workspace, size_t workspace_bytes, void *stream) {
@@ -473,14 +476,16 @@ eco_status_t eco_gated_backward(const eco_gated_t *g, void *workspace, size_t wo
   (void)hipGetLastError();
   char *ws = static_cast<char *>(workspace);
   hipStream_t s = static_cast<hipStream_t>(stream);
+  // the operands are there before the products that are done again: INT4 weights are read once for both
+  const bool there = f.expands && b.input;
+  CHECK(operands(u, b, nullptr, 0, there ? &f : nullptr, ws, s));
   if (g->rows) {
     eco::FfnOut o;
     std::memset(&o, 0, sizeof o);
     o.out = ws + b.grad; o.out_stride = 2 * b.half; o.half = static_cast<uint32_t>(b.half); o.act = g->act;
     o.grad_out = static_cast<const uint16_t *>(g->grad_out); o.grad_out_stride = stride_or(g->grad_out_stride, g->width);
-    CHECK(product(u, f, o, ws, s));
+    CHECK(product(u, f, o, there, ws, s));
   }
-  CHECK(operands(u, b, nullptr, 0, ws, s));
   void *const to[2] = {g->grad_gate, g->grad_up};
   return gradients(u, b, ws + b.grad, 2 * b.half, g->grad_input, g->grad_input_stride, to, ws, s);
 }

@@ -12,6 +12,7 @@
 
 #include "eco_device.hpp"
 #include "eco_ffn.hpp"
+#include "eco_int4.hpp"
 #include "eco_product.hpp"
 
 namespace eco {
@@ -53,6 +54,8 @@ __device__ __forceinline__ void weights_bf16(const FfnOperands &a, uint64_t firs
       if constexpr (FMT == FMT_FP8) fp8_values(*reinterpret_cast<const uint2 *>(from + at), scale, v);
       else {
         const uint32_t u = *reinterpret_cast<const uint32_t *>(from + at / 2);
+        uint8_t *const codes = static_cast<uint8_t *>(matrix ? a.codes[1] : a.codes[0]);
+        if (codes) *reinterpret_cast<uint2 *>(codes + at) = e4m3_of_int4(u);
 #pragma unroll
         for (int j = 0; j < 8; ++j) v[j] = static_cast<float>(static_cast<int32_t>(u << (28 - 4 * j)) >> 28) * scale;
       }

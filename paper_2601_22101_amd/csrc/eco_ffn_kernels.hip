@@ -10,6 +10,7 @@
 
 #include "eco_device.hpp"
 #include "eco_ffn.hpp"
+#include "eco_int4.hpp"
 #include "eco_product.hpp"
 #include "eco_rows8.hpp"
 
@@ -41,20 +42,6 @@ __device__ __forceinline__ void act_both(float a, int act, float &f, float &df) 
   const float q = p * (1.0f - p);
   f = a * p;
   df = q == 0.0f ? p : fmaf(a * dt, q, p);         // (a dt may be infinite there)
-}
-
-// ------------------------------------------------------------------------------------------------ INT4 codes as E4M3
-
-// The E4M3 codes of 0 .. 7 and of -8 .. -1 (the second half's -8 is no code of the library's, and stands for itself).
-__device__ __forceinline__ uint32_t e4m3_of_nibbles(uint32_t n) {        // one nibble in each byte
-  const uint32_t low = __builtin_amdgcn_perm(0x4E4C4A48u, 0x44403800u, n & 0x07070707u);
-  const uint32_t high = __builtin_amdgcn_perm(0xB8C0C4C8u, 0xCACCCED0u, n & 0x07070707u);
-  const uint32_t mask = ((n >> 3) & 0x01010101u) * 255u;
-  return (low & ~mask) | (high & mask);
-}
-__device__ __forceinline__ uint2 e4m3_of_int4(uint32_t eight) {          // eight codes in their order
-  const uint32_t even = e4m3_of_nibbles(eight & 0x0F0F0F0Fu), odd = e4m3_of_nibbles((eight >> 4) & 0x0F0F0F0Fu);
-  return make_uint2(__builtin_amdgcn_perm(odd, even, 0x05010400u), __builtin_amdgcn_perm(odd, even, 0x07030602u));
 }
 
 // ------------------------------------------------------------------------------------------------ tiles
@@ -766,11 +753,15 @@ hipError_t launch_few(const ProductArgs &a, hipStream_t s) {
   return launch_norm(r, s);
 }
 
-__global__ __launch_bounds__(256) void eco_ffn_expand_kernel(const uint32_t *first, const uint32_t *second, uint64_t words, uint2 *to_first, uint2 *to_second) {
+// Sixteen codes a thread.
+__global__ __launch_bounds__(256) void eco_ffn_expand_kernel(const uint2 *first, const uint2 *second, uint64_t words, uint4 *to_first, uint4 *to_second) {
   const bool up = blockIdx.y;
-  const uint32_t *codes = up ? second : first;
-  uint2 *out = up ? to_second : to_first;
-  for (uint64_t i = static_cast<uint64_t>(blockIdx.x) * 256 + threadIdx.x; i < words; i += static_cast<uint64_t>(gridDim.x) * 256) out[i] = e4m3_of_int4(codes[i]);
+  const uint2 *codes = up ? second : first;
+  uint4 *out = up ? to_second : to_first;
+  for (uint64_t i = static_cast<uint64_t>(blockIdx.x) * 256 + threadIdx.x; i < words; i += static_cast<uint64_t>(gridDim.x) * 256) {
+    const uint2 u = codes[i], a = e4m3_of_int4(u.x), b = e4m3_of_int4(u.y);
+    out[i] = make_uint4(a.x, a.y, b.x, b.y);
+  }
 }
 
 template <int MI, int NJ, int END, bool EXACT>
@@ -869,9 +860,9 @@ hipError_t launch_ffn_join(const FfnPlan &p, const FfnRows8 &x, const FfnWeights
 }
 
 hipError_t launch_ffn_expand(const FfnWeights &w, void *const out[2], hipStream_t s) {
-  const uint64_t words = static_cast<uint64_t>(w.rows) * w.dim / 8, groups = ceil_div(words, 256);      // (rows are multiples of 16 codes)
+  const uint64_t words = static_cast<uint64_t>(w.rows) * w.dim / 16, groups = ceil_div(words, 256);      // (rows are multiples of 16 codes)
   eco_ffn_expand_kernel<<<dim3(static_cast<uint32_t>(groups < 4096 ? groups : 4096), w.matrices), 256, 0, s>>>(
-      static_cast<const uint32_t *>(w.data[0]), static_cast<const uint32_t *>(w.data[1]), words, static_cast<uint2 *>(out[0]), static_cast<uint2 *>(out[1]));
+      static_cast<const uint2 *>(w.data[0]), static_cast<const uint2 *>(w.data[1]), words, static_cast<uint4 *>(out[0]), static_cast<uint4 *>(out[1]));
   return hipGetLastError();
 }
 

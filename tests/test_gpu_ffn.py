@@ -180,6 +180,34 @@ def test_gated(harness, rows, in_dim, width, group, fmt, scales, act):
         hold(got, want[name], want[name + "_tol"], name)
 
 
+@pytest.mark.parametrize("rows,in_dim,width,fmt", [(40, 256, 133, "fp8"), (200, 256, 391, "int4"), (1100, 384, 640, "int4"), (700, 128, 2000, "fp8"), (20, 512, 100, "int4")])
+def test_one_gradient_alone(harness, rows, in_dim, width, fmt):
+    """The others are NULL in the descriptor: theirs are left alone."""
+    gen, codes, code_scales, x, gate, up = make_gated(rows, in_dim, width, 128, fmt, "fp32")
+    grad = torch.randn(rows, width, generator=gen).bfloat16().cuda()
+    unit = harness.GatedUnit(rows, in_dim, width, gate=gate[0], gate_scales=gate[1], up=up[0], up_scales=up[1], fmt=FMT[fmt], training=True)
+    line = harness.Linear(rows, in_dim, width, weights=gate[0], scales=gate[1], fmt=FMT[fmt], training=True)
+    of_unit = gated_exact(x, gate[2], up[2], "silu", grad)
+    of_line = gradients_exact([grad.double()], [gate[2]], x, [torch.zeros(rows, width, dtype=torch.float64, device="cuda")])
+    for u, d, want, names in ((unit, unit.gated, of_unit, ("grad_input", "grad_gate", "grad_up")), (line, line.linear, of_line, ("grad_input", "grad_weights"))):
+        u.forward(codes, code_scales)
+        for input_alone in (True, False):
+            keep = {n: getattr(d, n) for n in names}
+            for n in names:
+                getattr(u, n).fill_(77.0)
+                if (n == "grad_input") != input_alone:
+                    setattr(d, n, None)
+            u.backward(grad)
+            torch.cuda.synchronize()
+            for i, n in enumerate(names):
+                name = "grad_input" if i == 0 else f"grad_{i - 1}"
+                if (n == "grad_input") == input_alone:
+                    hold(getattr(u, n), want[name], want[name + "_tol"], n)
+                else:
+                    assert (getattr(u, n) == 77.0).all(), n
+                setattr(d, n, keep[n])
+
+
 def run_layer(harness, rows, device="cuda"):
     """The feed-forward half of a layer, forward and backward: a dict of everything that it makes."""
     dim, width = 576, 1152
