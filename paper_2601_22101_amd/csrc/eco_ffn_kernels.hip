@@ -567,8 +567,9 @@ __global__ __launch_bounds__(256) void eco_ffn_join_kernel(ProductArgs a, uint32
 // ------------------------------------------------------------------------------------------------ few rows
 
 // Few rows are bound by the reading of the weights: each wave reads 16 NT rows of them by itself, straight into the registers in which the matrix core takes
-// them, AHEAD blocks at a time, and INT4 codes become E4M3 there.  Nothing is kept in LDS but sums on their way from wave to wave.  The products are exact ones in
-// bf16: they cost nothing beside the loads (linear 1 x 6912 x 1152 7.4 us, 7.9 in 8 bits; gated 24 x 1152 x 6912 13.5 and 11.7).
+// them, AHEAD blocks at a time (twice as many: linear 1 x 4096 x 14336 15.9 us instead of 15.2, gated 1 x 1152 x 6912 9.6 instead of 9.1), and INT4 codes become E4M3 there.
+// Nothing is kept in LDS but sums on their way from wave to wave.  The products are exact ones in bf16: they cost little beside the loads (linear 1 x 6912 x 1152 7.4 us,
+// 7.9 in 8 bits; gated 24 x 1152 x 6912 13.5 and 11.7).
 template <class V>
 __device__ __forceinline__ V loose(const void *p) {            // at an address of any alignment
   V v;
