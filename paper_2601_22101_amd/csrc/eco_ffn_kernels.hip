@@ -243,9 +243,9 @@ __global__ __launch_bounds__(THREADS) void eco_ffn_kernel(ProductArgs a) {
 
   // ---- the products' place
   i32x8 fx[EXACT ? 1 : MI], fw[2];
-  Wide gx[EXACT ? MI : 1], gw[2];
+  Wide gx[EXACT ? MI : 1], gw[EXACT ? 2 : 1];
   uint32_t sx[MI];
-  float sw[2];
+  float sw[4];
   const uint32_t lane_at = lane_place(lane);
   const lds_char *x_at[2], *w_at[2];
   const lds_uint *scale_x, *scale_w;
@@ -259,12 +259,10 @@ __global__ __launch_bounds__(THREADS) void eco_ffn_kernel(ProductArgs a) {
     scale_w = (const lds_uint *)(step + T::X_BYTES + T::W_BYTES) + T::BM + wn * 16 * RUN + (lane & 15);
   };
   const auto read_w = [&](int j) {
-    const i32x8 f = operand(w_at[0], w_at[1], 16 * j);
-    if constexpr (EXACT) gw[j & 1] = widen(f, 1.0f);
-    else fw[j & 1] = f;
+    fw[j & 1] = operand(w_at[0], w_at[1], 16 * j);
     if constexpr (BLOCKS) {
       const uint32_t bits = scale_w[GATED ? j / RUN * T::COLUMNS + 16 * (j % RUN) : 16 * j];
-      sw[j & 1] = u2f(a.w.scale_bf16 ? bits << 16 : bits);
+      sw[j & 3] = u2f(a.w.scale_bf16 ? bits << 16 : bits);
     }
   };
   const auto read_x = [&]() {
@@ -278,25 +276,32 @@ __global__ __launch_bounds__(THREADS) void eco_ffn_kernel(ProductArgs a) {
   };
   constexpr int LOADS_EACH = (T::LOADS + NJ - 2) / (NJ - 1);       // loads beside a fragment's products
   uint32_t at = 0;
-  f32x4 acc[MI][NJ], part[2][MI];
+  constexpr int PARTS = EXACT ? 1 : 2;                         // (four instructions a sum leave time for the one before)
+  f32x4 acc[MI][NJ], part[PARTS][MI];
+  const auto add_one = [&](int j, int i) {
+#pragma unroll
+    for (int r = 0; r < 4; ++r) acc[i][j][r] = fmaf(part[j % PARTS][i][r], sw[j & 3], acc[i][j][r]);
+  };
+  const auto add = [&](int j) {
+    if constexpr (BLOCKS)
+#pragma unroll
+      for (int i = 0; i < MI; ++i) add_one(j, i);
+  };
   const auto products = [&](int j) {
     const f32x4 zero = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
     for (int i = 0; i < MI; ++i) {
       const f32x4 c = BLOCKS ? zero : acc[i][j];
       f32x4 v;
-      if constexpr (EXACT) v = multiply(gx[i], gw[j & 1], c);
-      else v = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(fx[i], fw[j & 1], c, 0, 0, 0, static_cast<int>(sx[i]), 0, 127);
-      if constexpr (BLOCKS) part[j & 1][i] = v;
+      if constexpr (EXACT) {
+        if (BLOCKS && j) add_one(j - 1, i);
+        v = multiply(gx[i], gw[j & 1], c);
+      } else {
+        v = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(fx[i], fw[j & 1], c, 0, 0, 0, static_cast<int>(sx[i]), 0, 127);
+      }
+      if constexpr (BLOCKS) part[j % PARTS][i] = v;
       else acc[i][j] = v;
     }
-  };
-  const auto add = [&](int j, float s) {
-    if constexpr (BLOCKS)
-#pragma unroll
-      for (int i = 0; i < MI; ++i)
-#pragma unroll
-        for (int r = 0; r < 4; ++r) acc[i][j][r] = fmaf(part[j & 1][i][r], s, acc[i][j][r]);
   };
 
   load_tile();
@@ -308,9 +313,14 @@ __global__ __launch_bounds__(THREADS) void eco_ffn_kernel(ProductArgs a) {
   }
   wait_loads<(DEPTH - 2) * T::LOADS>();
   barrier();
+  const auto read_first = [&]() {
+    read_w(0);
+    if constexpr (EXACT) read_w(1);
+    read_x();
+    if constexpr (EXACT) gw[0] = widen(fw[0], 1.0f);
+  };
   go_to(0);
-  read_x();
-  read_w(0);
+  read_first();
   for (uint32_t id = blockIdx.x; id < all_tiles; id += gridDim.x) {
     const Where w = where(id);
     const uint32_t m0 = w.m0, n0 = w.n0;
@@ -322,19 +332,36 @@ __global__ __launch_bounds__(THREADS) void eco_ffn_kernel(ProductArgs a) {
       next_step();                                             // into the last step's place, which every wave has read
       load_scale();
       __builtin_amdgcn_sched_barrier(0);                       // (from here on no branch, over which the compiler would carry the products)
-      float before = 0.0f;
+      if constexpr (EXACT) {
 #pragma unroll
-      for (int j = 0; j < NJ - 1; ++j) {
-        const float mine = sw[j & 1];
-        read_w(j + 1);
+        for (int j = 0; j < NJ; ++j) {
+          if (j + 2 < NJ) read_w(j + 2);
 #pragma unroll
-        for (int l = 0; l < T::LOADS - 1; ++l)
-          if (l / LOADS_EACH == j) load(l);
-        products(j);
-        if (j) add(j - 1, before);
-        before = mine;
-        // reads of LDS first, then a product and its share of the sums, and so on
-        if constexpr (!EXACT) {
+          for (int l = 0; l < T::LOADS - 1; ++l)
+            if (l / LOADS_EACH == j) load(l);
+          products(j);
+          if (j + 1 < NJ) gw[(j + 1) & 1] = widen(fw[(j + 1) & 1], 1.0f);
+          if (j + 2 < NJ) __builtin_amdgcn_sched_group_barrier(0x100, BLOCKS ? 3 : 2, 0);
+#pragma unroll
+          for (int i = 0; i < MI; ++i) {
+            if (BLOCKS && j) __builtin_amdgcn_sched_group_barrier(0x002, 4, 0);
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+              __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+              if (j + 1 < NJ) __builtin_amdgcn_sched_group_barrier(0x002, 16 / (4 * MI), 0);
+            }
+          }
+        }
+      } else {
+#pragma unroll
+        for (int j = 0; j < NJ - 1; ++j) {
+          read_w(j + 1);
+#pragma unroll
+          for (int l = 0; l < T::LOADS - 1; ++l)
+            if (l / LOADS_EACH == j) load(l);
+          products(j);
+          if (j) add(j - 1);
+          // reads of LDS first, then a product and its share of the sums, and so on
           __builtin_amdgcn_sched_group_barrier(0x100, BLOCKS ? 3 : 2, 0);
 #pragma unroll
           for (int i = 0; i < MI; ++i) {
@@ -342,18 +369,17 @@ __global__ __launch_bounds__(THREADS) void eco_ffn_kernel(ProductArgs a) {
             if (BLOCKS && j) __builtin_amdgcn_sched_group_barrier(0x002, 4, 0);
           }
         }
+        products(NJ - 1);
+        add(NJ - 2);
       }
-      const float last = sw[(NJ - 1) & 1];
-      products(NJ - 1);
-      add(NJ - 2, before);
       // the next step, of this tile or the next, is there once every wave's loads of it are
       wait_all_but<(DEPTH - 2) * T::LOADS>();
       barrier();
       at = at + 1 == DEPTH ? 0 : at + 1;
       go_to(at);
-      read_x();
-      read_w(0);
-      add(NJ - 1, last);
+      if constexpr (EXACT) add(NJ - 1);
+      read_first();
+      if constexpr (!EXACT) add(NJ - 1);
     }
 
     // ---- ends.  acc[i][j][r]: row m0 + wm + 16 i + 4 (end_lane >> 4) + r, column of fragment j and lane c = end_lane & 15 as above
