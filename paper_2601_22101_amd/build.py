@@ -13,6 +13,7 @@ from concurrent.futures import ThreadPoolExecutor
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
+CSRC_FFN = os.path.join(HERE, "csrc_ffn")
 BUILD = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libeco.so")
 
@@ -25,6 +26,9 @@ SOURCES = [
     "eco_step_int4_bf16.hip",
     "eco_head_api.cpp",
     "eco_head_kernels.hip",
+]
+# The feed-forward half of a layer, in a folder of its own: a record of the step's kernels is of the sources beside them.
+FFN_SOURCES = [
     "eco_norm_kernels.hip",
     "eco_ffn_api.cpp",
     "eco_ffn_kernels.hip",
@@ -49,14 +53,14 @@ def _hipcc() -> str:
 
 
 def _deps_mtime() -> float:
-    headers = [os.path.join(CSRC, f) for f in os.listdir(CSRC) if f.endswith((".hpp", ".h"))]
+    headers = [os.path.join(d, f) for d in (CSRC, CSRC_FFN) for f in os.listdir(d) if f.endswith((".hpp", ".h"))]
     headers.append(os.path.join(os.path.dirname(HERE), "include", "eco.h"))
     return max(os.path.getmtime(h) for h in headers)
 
 
-def _compile(src: str, force: bool, extra) -> str:
+def _compile(path: str, force: bool, extra) -> str:
+    src = os.path.basename(path)
     obj = os.path.join(BUILD, os.path.splitext(src)[0] + ".o")
-    path = os.path.join(CSRC, src)
     newest = max(os.path.getmtime(path), _deps_mtime())
     if not force and os.path.exists(obj) and os.path.getmtime(obj) >= newest:
         return obj
@@ -80,7 +84,7 @@ def build(force: bool = False, jobs: int = 6, defines=(), out: str = LIB) -> str
     os.makedirs(BUILD, exist_ok=True)
     extra = [f"-D{d}" for d in defines]
     with ThreadPoolExecutor(max_workers=jobs) as ex:
-        objs = list(ex.map(lambda s: _compile(s, force, extra), SOURCES))
+        objs = list(ex.map(lambda p: _compile(p, force, extra), [os.path.join(CSRC, s) for s in SOURCES] + [os.path.join(CSRC_FFN, s) for s in FFN_SOURCES]))
     if force or not os.path.exists(out) or any(os.path.getmtime(o) > os.path.getmtime(out) for o in objs):
         cmd = [_hipcc(), "--offload-arch=gfx950", "-shared", "-fPIC", *objs, "-o", out]
         subprocess.run(cmd, check=True)

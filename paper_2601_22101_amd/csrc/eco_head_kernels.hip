@@ -10,7 +10,7 @@
 
 #include "eco_device.hpp"
 #include "eco_head.hpp"
-#include "eco_product.hpp"
+#include "eco_head_product.hpp"
 
 namespace eco {
 namespace {

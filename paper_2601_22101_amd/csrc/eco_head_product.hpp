@@ -1,5 +1,5 @@
-// Device-side pieces of a matrix product through LDS: loads past the registers, the order of a step's pieces, the matrix cores' operands out of it, and results on
-// their way out in whole lines.
+// Device-side pieces of a matrix product through LDS, of the losses at the output projection and of the feed-forward half of a layer: loads past the registers, the order
+// of a step's pieces, the matrix cores' operands out of it, and results on their way out in whole lines.
 #pragma once
 #include <hip/hip_runtime.h>
 #include <stdint.h>

@@ -9,7 +9,7 @@
 
 #include "../../include/eco.h"
 #include "eco_ffn.hpp"
-#include "eco_internal.hpp"
+#include "../csrc/eco_internal.hpp"
 
 namespace {
 

@@ -8,10 +8,10 @@
 
 #include <type_traits>
 
-#include "eco_device.hpp"
+#include "../csrc/eco_device.hpp"
 #include "eco_ffn.hpp"
 #include "eco_int4.hpp"
-#include "eco_product.hpp"
+#include "../csrc/eco_head_product.hpp"
 #include "eco_rows8.hpp"
 
 namespace eco {

@@ -8,7 +8,7 @@
 // over the rows of each of 1024 workgroups, and those by a second kernel: 512, 1024, 1536 and 2048 of them take the backward pass 68.6, 50.6, 57.9 and 53.2 us.
 #include <hip/hip_runtime.h>
 
-#include "eco_device.hpp"
+#include "../csrc/eco_device.hpp"
 #include "eco_ffn.hpp"
 #include "eco_rows8.hpp"
 

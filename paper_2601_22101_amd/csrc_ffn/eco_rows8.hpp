@@ -5,7 +5,7 @@
 
 #include <type_traits>
 
-#include "eco_device.hpp"
+#include "../csrc/eco_device.hpp"
 
 namespace eco {
 namespace {
