@@ -106,6 +106,12 @@ struct GradArgs {
   uint32_t tiles_x, tiles_y, steps;
 };
 
+__device__ const uint4 grad_zeros = {0, 0, 0, 0};
+// As load_to_lds, from an address of each lane's own.
+__device__ __forceinline__ void lane_to_lds(uint32_t lds, const void *from) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds), "v"(from) : "memory");
+}
+
 constexpr int OWN = 4096;                         // of LDS, for a wave's results on their way out
 
 // D[y][x] = sum_k Y X.  x runs along a lane's registers, four neighbours in each group.  Workgroup `me` of `all` goes through tiles `all` apart; its loads do not stop
@@ -178,24 +184,19 @@ __device__ __forceinline__ void grad_product(const GradArgs &a, uint32_t me, uin
   const auto issue = [&]() {
     if (load_id >= all_tiles) return;
     const uint32_t lds = lds0 + place * T::STEP_BYTES + wave * 1024;
-    // the last step's end: X has zeros there, Y repeats what is there of the row, or the last row
-    const bool end = tail && load_first + at_step + 1 == a.steps;
 #pragma unroll
     for (int i = 0; i < T::X_LOADS; ++i) load_to_lds(lds + i * T::THREADS * 16, from_x, off_x[i]);
+    if (tail && load_first + at_step + 1 == a.steps) {         // past the last step's end both have zeros, X in memory: an infinity of Y times one would be NaN
 #pragma unroll
-    for (int i = 0; i < T::Y_LOADS; ++i) {
-      uint32_t off = off_y[i];
-      if (end) {
+      for (int i = 0; i < T::Y_LOADS; ++i) {
         uint32_t n, k;
-        if constexpr (Y_COLUMN) {
-          column_piece<T::BY>(threadIdx.x + i * T::THREADS, n, k);
-          if (k >= tail) off -= static_cast<uint32_t>((k - (tail - 1)) * p.ldy) * 2;
-        } else {
-          row_piece(threadIdx.x + i * T::THREADS, n, k);
-          if (k >= tail) off -= k * 2;
-        }
+        if constexpr (Y_COLUMN) column_piece<T::BY>(threadIdx.x + i * T::THREADS, n, k);
+        else row_piece(threadIdx.x + i * T::THREADS, n, k);
+        lane_to_lds(lds + T::X_BYTES + i * T::THREADS * 16, k >= tail ? reinterpret_cast<const char *>(&grad_zeros) : reinterpret_cast<const char *>(from_y) + off_y[i]);
       }
-      load_to_lds(lds + T::X_BYTES + i * T::THREADS * 16, from_y, off);
+    } else {
+#pragma unroll
+      for (int i = 0; i < T::Y_LOADS; ++i) load_to_lds(lds + T::X_BYTES + i * T::THREADS * 16, from_y, off_y[i]);
     }
     place = place + 1 == T::DEPTH ? 0 : place + 1;
     ++issued;

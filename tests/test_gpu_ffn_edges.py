@@ -1,0 +1,55 @@
+"""The feed-forward half at the edges of its values: infinities next to padding."""
+import pytest
+import torch
+
+from ffn_util import FMT, activations, rows8_values, weights
+from test_gpu_ffn import harness      # noqa: F401
+
+pytestmark = pytest.mark.gpu
+
+
+def as_formula(got, want, name):
+    """Infinities and NaN where the formula has them, with their signs."""
+    got = got.double()
+    assert torch.equal(got.isnan(), want.isnan()), f"{name}: {int((got.isnan() != want.isnan()).sum())} of {got.numel()} are NaN in one alone"
+    assert torch.equal(got.isinf(), want.isinf()) and torch.equal(got.isinf() * got.sign(), want.isinf() * want.sign()), f"{name}: infinities"
+
+
+# out_dim: of rows that are copied, and read where they lie; rows and out_dim leave the inner axes' last steps partly empty
+@pytest.mark.parametrize("rows,out_dim", [(70, 100), (70, 104), (6, 72), (190, 328), (700, 840)])
+@pytest.mark.parametrize("fmt", ["fp8", "int4"])
+def test_infinities_next_to_padding(harness, rows, out_dim, fmt):      # noqa: F811
+    """An infinite gradient in the last row and at the start of the last step: its products with the padding's zeros are no part of a sum."""
+    in_dim = 144
+    gen = torch.Generator().manual_seed(rows + out_dim)
+    codes, scales = activations(rows, in_dim, gen)
+    codes[codes & 0x7F == 0] = 0x38                           # (no zeros, whose product with an infinity is NaN in the formula too)
+    x = rows8_values(codes, scales)
+    w, ws, values = weights(out_dim, in_dim, fmt, 144, "fp32", gen)
+    unit = harness.Linear(rows, in_dim, out_dim, weights=w, scales=ws, fmt=FMT[fmt], group_size=144, training=True)
+    unit.forward(codes, scales)
+    grad = torch.randn(rows, out_dim, generator=gen).bfloat16().cuda()
+    grad[rows - 1, 7], grad[rows // 2, out_dim // 64 * 64], grad[1, out_dim - 1] = float("inf"), float("-inf"), float("inf")
+    grad_input, grad_weights = unit.backward(grad)
+    # products of an infinity with each term apart: a sum over the inner axis in a library's blocks has its own padding
+    as_formula(grad_input, (grad.double()[:, :, None] * values[None]).sum(1), "grad_input")
+    as_formula(grad_weights, (grad.double().t()[:, :, None] * x[None]).sum(1), "grad_weights")
+
+
+def test_infinities_next_to_padding_of_the_gated_unit(harness):      # noqa: F811
+    rows, in_dim, width = 70, 128, 100
+    gen = torch.Generator().manual_seed(1)
+    codes, scales = activations(rows, in_dim, gen)
+    codes[codes & 0x7F == 0] = 0x38
+    x = rows8_values(codes, scales)
+    gate, up = weights(width, in_dim, "fp8", 128, "fp32", gen), weights(width, in_dim, "fp8", 128, "fp32", gen)
+    unit = harness.GatedUnit(rows, in_dim, width, gate=gate[0], gate_scales=gate[1], up=up[0], up_scales=up[1], training=True)
+    unit.forward(codes, scales)
+    grad = torch.ones(rows, width, dtype=torch.bfloat16, device="cuda")
+    grad[rows - 1, 7] = float("inf")
+    _, grad_gate, grad_up = unit.backward(grad)
+    a, b = x[-1] @ gate[2][7], x[-1] @ up[2][7]
+    assert a != 0 and b != 0 and torch.isfinite(grad_gate[torch.arange(width) != 7]).all() and torch.isfinite(grad_up[torch.arange(width) != 7]).all()
+    s = torch.sigmoid(a)
+    assert torch.equal(grad_gate[7].double(), torch.sign(x[-1] * b * s * (1 + a * (1 - s))) * float("inf"))
+    assert torch.equal(grad_up[7].double(), torch.sign(x[-1] * a) * float("inf"))
