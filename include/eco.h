@@ -388,7 +388,8 @@ eco_status_t eco_rows_quantize(const void *src, int32_t src_dtype, uint64_t rows
  * backward, from grad_out = dL/dy (which passes the rounding to 8 bits straight through) and grad_sum = dL/ds from what else reads s (NULL: none):
  *     grad_input = rstd (u - s rstd mean(u s rstd)) + grad_sum,  u = grad_out gain     (the gradient of input and of residual alike)
  *     grad_gain  = sum over the rows of grad_out s rstd
- * Sums are fp32.  sum may be input or residual, grad_input may be grad_out or grad_sum: a row is read before it is written.
+ * Sums are fp32; of a finite row whose squares pass its range they are those of s 2^-80, so that any finite row is normalised.  sum may be input or residual, grad_input may
+ * be grad_out or grad_sum: a row is read before it is written.
  */
 typedef struct eco_norm {
   const void *input;          /* rows x dim of dtype; so residual, sum, grad_out, grad_sum, grad_input                            */

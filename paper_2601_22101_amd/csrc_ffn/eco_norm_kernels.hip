@@ -154,6 +154,9 @@ __device__ __forceinline__ void put_y(const NormRows &a, uint64_t row, uint32_t 
   else if (k < a.dim) write8<BF16>(const_cast<char *>(row_of(a.out, row, a.out_stride, BF16 ? 2 : 4)), k, a.dim, y);
 }
 
+// Rows whose squares pass fp32's range are summed as (s 2^-80)^2: the largest value's is 2^96, a row's of 2^16 2^112, and what takes the first sum past 2^128 leaves 2^-48 at least.
+constexpr float FAR = 0x1p-80f;
+
 // CHUNKS pieces of eight a lane, LANES * 8 columns apart; CHUNKS 0: as many as there are, read again for the second use, and rows of less than eight.
 template <bool BF16, int LANES, int CHUNKS>
 __global__ __launch_bounds__(LANES == 64 ? 256 : LANES) void eco_norm_kernel(NormRows a) {
@@ -196,7 +199,21 @@ __global__ __launch_bounds__(LANES == 64 ? 256 : LANES) void eco_norm_kernel(Nor
   }
   float rstd = 1.0f;
   if (a.norm) {
-    rstd = 1.0f / sqrtf(row_sum<LANES>(total, red) / static_cast<float>(a.dim) + a.eps);
+    float square = row_sum<LANES>(total, red) / static_cast<float>(a.dim) + a.eps, unit = 1.0f;
+    if (__builtin_expect(!(square < __builtin_inff()), 0)) {      // (the same in all of the row's lanes; rows that are not finite come out as they would have)
+      unit = FAR;
+      total = 0.0f;
+      for (uint32_t c = 0; c < chunks; ++c) {
+        if constexpr (CHUNKS == 0) read8<BF16, ANY>(residual ? sum : input, (c * LANES + lane) * 8, a.dim, s[0]);
+#pragma unroll
+        for (int k = 0; k < KEEP; ++k)
+          if (CHUNKS == 0 || c == static_cast<uint32_t>(k))
+#pragma unroll
+            for (int j = 0; j < 8; ++j) total = fmaf(s[k][j] * FAR, s[k][j] * FAR, total);
+      }
+      square = row_sum<LANES>(total, red) / static_cast<float>(a.dim) + a.eps * FAR * FAR;
+    }
+    rstd = unit / sqrtf(square);
     if (a.rstd && lane == 0) a.rstd[row] = rstd;
   }
   const auto leave = [&](int c, uint32_t k) {

@@ -1,8 +1,9 @@
-"""The feed-forward half at the edges of its values: infinities next to padding."""
+"""The feed-forward half at the edges of its values: infinities next to padding, norms of rows whose squares pass fp32's range."""
 import pytest
 import torch
 
-from ffn_util import FMT, activations, rows8_values, weights
+from ffn_checks import hold_rows8
+from ffn_util import DTYPE, FMT, activations, hold, norm_exact, rows8_values, weights
 from test_gpu_ffn import harness      # noqa: F401
 
 pytestmark = pytest.mark.gpu
@@ -53,3 +54,44 @@ def test_infinities_next_to_padding_of_the_gated_unit(harness):      # noqa: F81
     s = torch.sigmoid(a)
     assert torch.equal(grad_gate[7].double(), torch.sign(x[-1] * b * s * (1 + a * (1 - s))) * float("inf"))
     assert torch.equal(grad_up[7].double(), torch.sign(x[-1] * a) * float("inf"))
+
+
+@pytest.mark.parametrize("dim", [1, 7, 40, 512, 1000, 1152, 2048, 4100, 8192, 8200])
+@pytest.mark.parametrize("dtype,residual,quantize", [("bf16", False, False), ("bf16", True, True), ("fp32", True, False), ("fp32", False, True)])
+def test_norm_of_rows_whose_squares_pass_the_range(harness, dim, dtype, residual, quantize):      # noqa: F811
+    """The type's lowest value, values near its largest, and one such among small ones: normalised as any other row, next to rows of ordinary size and one that is infinite."""
+    t = DTYPE[dtype]
+    gen = torch.Generator().manual_seed(dim)
+    x = torch.randn(7, dim, generator=gen)
+    x[0] = torch.finfo(t).min
+    x[1] = torch.sign(x[1]) * (1 + torch.rand(dim, generator=gen)) * 1.5e38
+    x[2] *= 1e18                                              # sums past the range, of squares that are not
+    x[3, 1:], x[3, 0] = x[3, 1:] * 1e20, 3e38
+    x[5, dim // 2] = float("inf")
+    x = x.to(t).cuda()
+    gain, grad = (1 + 0.3 * torch.randn(dim, generator=gen)).cuda(), torch.randn(7, dim, generator=gen).to(t).cuda()
+    zeros = torch.zeros_like(x)
+    unit = harness.RowNorm(7, dim, gain=gain, dtype=t, eps=1e-6, residual=residual, quantize=quantize, training=True, grad_gain_dtype=torch.float32)
+    out, scales, total = unit.forward(x, zeros if residual else None)
+    if residual:
+        assert torch.equal(total, x)
+    rows = torch.tensor([0, 1, 2, 3, 4, 6], device="cuda")
+    want = norm_exact(x[rows].double(), gain.double(), 1e-6)
+    # 1 / 3.4e38 is held with 21 bits: 2^-22 of it, beside the sums'
+    tol = want["y_tol"] + want["y"].abs() * 2.0 ** -22
+    if quantize:
+        hold_rows8(out[rows], scales[rows], want["y"], tol, "y")
+    else:
+        hold(out[rows], want["y"], tol, "y")
+    assert ((unit.rstd[rows].double() / want["rstd"] - 1).abs() <= (want["rstd_tol"] / want["rstd"]) + 2.0 ** -22).all()
+    assert unit.rstd[5] == 0                                  # of an infinite row: zeros, and NaN where the infinity is (of 8 bits its block)
+    if not quantize:
+        assert out[5, dim // 2].isnan() and out[5].isnan().sum() == 1 and not out[5][~out[5].isnan()].any()
+    else:
+        assert (scales[5] == 255).sum() == 1
+    few = harness.RowNorm(6, dim, gain=gain, dtype=t, eps=1e-6, residual=residual, quantize=quantize, training=True, grad_gain_dtype=torch.float32)
+    few.forward(x[rows], zeros[rows] if residual else None)
+    grad_input, grad_gain = few.backward(grad[rows])
+    want = norm_exact(x[rows].double(), gain.double(), 1e-6, grad[rows])
+    hold(grad_gain, want["grad_gain"], want["grad_gain_tol"] + (grad[rows].double().abs() * x[rows].double().abs() * want["rstd"][:, None]).sum(0) * 2.0 ** -22, "grad_gain")
+    hold(grad_input, want["grad_input"], want["grad_input_tol"] + want["rstd"][:, None] * 2.0 ** -20 * (1 + grad[rows].double().abs()), "grad_input")
