@@ -63,6 +63,11 @@ eco_status_t check_in_place(const char *what, const char *out, const void *p, ui
   if (p && p == q && stride_or(stride, packed) != stride_or(in_stride, packed)) return fail(ECO_EINVAL, "%s: %s is %s with another stride", what, out, in);
   return ECO_OK;
 }
+// Rows that are written while other workgroups still read those in the same place.
+eco_status_t check_apart(const char *what, const char *out, const void *p, const char *in, const void *q) {
+  if (p && p == q) return fail(ECO_EINVAL, "%s: %s is %s", what, out, in);
+  return ECO_OK;
+}
 eco_status_t check_workspace(const char *what, const void *workspace, size_t bytes, uint64_t need) {
   if (need == 0) return ECO_OK;
   if (!workspace) return fail(ECO_EINVAL, "%s: null workspace", what);
@@ -280,6 +285,7 @@ eco_status_t check_linear_backward(const eco_linear_t *l) {
   CHECK(check_rows("linear", "grad_out", l->grad_out, l->rows, l->grad_out_stride, l->out_dim, 2));
   if (l->grad_input) CHECK(check_rows("linear", "grad_input", l->grad_input, l->rows, l->grad_input_stride, l->in_dim, 2));
   if (!aligned(l->grad_weights, 16)) return fail(ECO_EALIGN, "linear: grad_weights must be 16-byte aligned");
+  CHECK(check_apart("linear", "grad_input", l->grad_input, "grad_out", l->grad_out));
   return ECO_OK;
 }
 eco_status_t check_gated_backward(const eco_gated_t *g) {
@@ -314,6 +320,7 @@ eco_status_t eco_rows_quantize(const void *src, int32_t src_dtype, uint64_t rows
   CHECK(check_rows("rows_quantize", "src", src, rows, src_stride, dim, size_of(src_dtype)));
   CHECK(check_rows("rows_quantize", "codes", codes, rows, codes_stride, dim, 1));
   if (!scales && rows) return fail(ECO_EINVAL, "rows_quantize: null scales");
+  CHECK(check_apart("rows_quantize", "codes", codes, "src", src));
   (void)hipGetLastError();
   eco::NormRows a;
   std::memset(&a, 0, sizeof a);
@@ -337,6 +344,11 @@ eco_status_t eco_norm(const eco_norm_t *n, void *stream) {
     return fail(ECO_EINVAL, "norm: a sum without a residual");
   }
   CHECK(check_rows("norm", "out", n->out, n->rows, n->out_stride, n->dim, n->scales ? 1 : size));
+  if (n->scales) {                                // (8-bit rows lie at other places than those that they are made of)
+    CHECK(check_apart("norm", "out", n->out, "input", n->input));
+    CHECK(check_apart("norm", "out", n->out, "residual", n->residual));
+    CHECK(check_apart("norm", "out", n->out, "sum", n->sum));
+  }
   if (!aligned(n->rstd, 4)) return fail(ECO_EALIGN, "norm: rstd is not aligned to its elements");
   (void)hipGetLastError();
   eco::NormRows a;
@@ -404,6 +416,7 @@ eco_status_t eco_linear(const eco_linear_t *l, void *workspace, size_t workspace
   CHECK(check_rows("linear", "out", l->out, l->rows, l->out_stride, l->out_dim, size));
   if (l->add) CHECK(check_rows("linear", "add", l->add, l->rows, l->add_stride, l->out_dim, size));
   CHECK(check_in_place("linear", "out", l->out, l->out_stride, "add", l->add, l->add_stride, l->out_dim));
+  CHECK(check_apart("linear", "out", l->out, "codes", l->codes));
   Places p;
   const Unit u = unit_of(l);
   const Forward f = forward_of(u, eco::FFN_LINEAR, EXACT, p, l->out_dtype == ECO_DT_FP32);
@@ -453,6 +466,8 @@ eco_status_t eco_gated(const eco_gated_t *g, void *workspace, size_t workspace_b
   CHECK(check_gated(g));
   CHECK(check_rows("gated", "out", g->out, g->rows, g->out_stride, g->width, 1));
   if (!g->out_scales && g->rows) return fail(ECO_EINVAL, "gated: null out_scales");
+  CHECK(check_apart("gated", "out", g->out, "codes", g->codes));
+  CHECK(check_apart("gated", "out_scales", g->out_scales, "code_scales", g->code_scales));
   Places p;
   const Unit u = unit_of(g);
   const Forward f = forward_of(u, eco::FFN_GATED, EXACT, p);

@@ -623,6 +623,15 @@ class _RowUnit:
         self.workspace = torch.empty(self.workspace_bytes, dtype=torch.uint8, device=self.device) if self.workspace_bytes else None
 
 
+def _span(t: Optional[torch.Tensor]):
+    """The addresses of an array that a call writes: an input of it that begins there is refused, but for rows that lie where they are written and are read first."""
+    return (0, 0) if t is None else (t.data_ptr(), t.data_ptr() + t.nbytes)
+
+
+def _inside(name: str):
+    raise ValueError(f"{name}: it lies in what this call writes")
+
+
 def quantize_rows(x: torch.Tensor, codes: Optional[torch.Tensor] = None, scales: Optional[torch.Tensor] = None, stream=None):
     """(codes, scales) of the rows of ``x`` (fp32 or bf16): 8-bit rows as RowNorm and GatedUnit make them and Linear and GatedUnit take them.
     Both may be given, as uint8 arrays to write to; else they are new."""
@@ -652,7 +661,9 @@ class RowNorm(_RowUnit):
     """Root-mean-square norm with the residual's addition, its rows leaving in 8 bits or, with ``quantize=False``, in ``dtype`` (eco_norm, eco_norm_backward).
 
     Made for up to ``rows`` rows; a call brings as many or fewer.  The tensors that forward() and backward() return are the object's own, or views of them, and are
-    written again by its next call; both run on the current stream, or on ``stream``.  A call that refuses its arguments (ValueError) leaves the object as it was.
+    written again by its next call; both run on the current stream, or on ``stream``.  A call that refuses its arguments (ValueError) leaves the object as it was; an input that lies in
+    what the call writes is refused too, unless its rows lie where they are written (the sum or unquantized rows over x or the residual, grad_input over a gradient, of Linear the result over what
+    is added).
     """
 
     def __init__(self, rows: int, dim: int, *, gain: Optional[torch.Tensor] = None, dtype: torch.dtype = torch.bfloat16, eps: float = 1e-6, residual: bool = False,
@@ -674,6 +685,8 @@ class RowNorm(_RowUnit):
                                   grad_gain_dtype=_DTYPE[grad_gain_dtype], gain=gain, out=self.out, scales=self.scales, sum=self.sum, rstd=self.rstd,
                                   grad_input=self.grad_input, grad_gain=self.grad_gain)
         self._make_workspace([eco.eco_norm_backward_workspace(self.norm) if training else 0])
+        self._spans = [_span(t) for t in (self.sum, None if quantize else self.out) if t is not None]
+        self._grad_span = _span(self.grad_input)
         self._inputs = None                             # of the last forward()
 
     def forward(self, x: torch.Tensor, residual: Optional[torch.Tensor] = None, stream=None):
@@ -685,11 +698,17 @@ class RowNorm(_RowUnit):
         elif residual is not None:
             raise ValueError("residual: this RowNorm was made without residual=True")
         self._rows(n)
+        at, residual_at = x.data_ptr(), residual.data_ptr() if self.has_residual else 0
+        for lo, hi in self._spans:
+            if lo <= at < hi and (at != lo or stride not in (0, self.dim)):
+                _inside("x")
+            if lo <= residual_at < hi and (residual_at != lo or residual_stride not in (0, self.dim)):
+                _inside("residual")
         d = self.norm
         self._inputs = None
-        d.rows, d.input, d.input_stride = n, x.data_ptr(), stride
+        d.rows, d.input, d.input_stride = n, at, stride
         if self.has_residual:
-            d.residual, d.residual_stride = residual.data_ptr(), residual_stride
+            d.residual, d.residual_stride = residual_at, residual_stride
         self._run(eco.eco_norm, d, stream, () if stream is None else (x, residual, self.gain, self.out, self.scales, self.sum, self.rstd), workspace=False)
         self._inputs = x, n
         if n == self.rows:
@@ -706,9 +725,15 @@ class RowNorm(_RowUnit):
         x, n = self._inputs
         stride = self._takes("grad_out", grad_out, n, self.dim, self.dtype)
         sum_stride = self._takes("grad_sum", grad_sum, n, self.dim, self.dtype) if grad_sum is not None else 0
+        lo, hi = self._grad_span
+        at, sum_at = grad_out.data_ptr(), None if grad_sum is None else grad_sum.data_ptr()
+        if lo <= at < hi and (at != lo or stride not in (0, self.dim)):
+            _inside("grad_out")
+        if sum_at and lo <= sum_at < hi and (sum_at != lo or sum_stride not in (0, self.dim)):
+            _inside("grad_sum")
         d = self.norm
-        d.grad_out, d.grad_out_stride = grad_out.data_ptr(), stride
-        d.grad_sum, d.grad_sum_stride = None if grad_sum is None else grad_sum.data_ptr(), sum_stride
+        d.grad_out, d.grad_out_stride = at, stride
+        d.grad_sum, d.grad_sum_stride = sum_at, sum_stride
         self._run(eco.eco_norm_backward, d, stream, () if stream is None else (x, grad_out, grad_sum, self.gain, self.sum, self.rstd, self.grad_input, self.grad_gain))
         return self.grad_input if n == self.rows else self.grad_input[:n], self.grad_gain
 
@@ -737,6 +762,7 @@ class Linear(_RowUnit):
                                       grad_weights=self.grad_weights)
         self._make_workspace([eco.eco_linear_workspace(self.linear, b) for b in ([False, True] if training else [False])])
         self.linear.codes = self.linear.code_scales = None
+        self._span, self._grad_span = _span(self.out), _span(self.grad_input)
         self._inputs = None
 
     def forward(self, codes: torch.Tensor, scales: torch.Tensor, add: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
@@ -744,10 +770,15 @@ class Linear(_RowUnit):
         stride = self._takes_rows8(codes, scales, self.in_dim)
         n = codes.shape[0]
         add_stride = self._takes("add", add, n, self.out_dim, self.out_dtype) if add is not None else 0
+        add_at = None
+        if add is not None:
+            add_at, (lo, hi) = add.data_ptr(), self._span
+            if lo <= add_at < hi and (add_at != lo or add_stride not in (0, self.out_dim)):
+                _inside("add")
         d = self.linear
         self._inputs = None
         d.rows, d.codes, d.code_scales, d.codes_stride = n, codes.data_ptr(), scales.data_ptr(), stride
-        d.add, d.add_stride = None if add is None else add.data_ptr(), add_stride
+        d.add, d.add_stride = add_at, add_stride
         self._run(eco.eco_linear, d, stream, () if stream is None else (codes, scales, add, self.weights, self.scales, self.out))
         self._inputs = codes, scales, n
         return self.out if n == self.rows else self.out[:n]
@@ -760,8 +791,11 @@ class Linear(_RowUnit):
             raise RuntimeError("backward() needs a forward() before it")
         codes, scales, n = self._inputs
         stride = self._takes("grad_out", grad_out, n, self.out_dim, torch.bfloat16)
+        at, (lo, hi) = grad_out.data_ptr(), self._grad_span
+        if lo <= at < hi:
+            _inside("grad_out")
         d = self.linear
-        d.grad_out, d.grad_out_stride = grad_out.data_ptr(), stride
+        d.grad_out, d.grad_out_stride = at, stride
         self._run(eco.eco_linear_backward, d, stream, () if stream is None else (codes, scales, grad_out, self.weights, self.scales, self.grad_input, self.grad_weights))
         return self.grad_input if n == self.rows else self.grad_input[:n], self.grad_weights
 
@@ -795,15 +829,19 @@ class GatedUnit(_RowUnit):
                                     out_scales=self.scales, grad_input=self.grad_input, grad_gate=self.grad_gate, grad_up=self.grad_up)
         self._make_workspace([eco.eco_gated_workspace(self.gated, b) for b in ([False, True] if training else [False])])
         self.gated.codes = self.gated.code_scales = None
+        self._span, self._scales_span = _span(self.out), _span(self.scales)
         self._inputs = None
 
     def forward(self, codes: torch.Tensor, scales: torch.Tensor, stream=None):
         """(codes, scales) of the unit's rows."""
         stride = self._takes_rows8(codes, scales, self.in_dim)
         n = codes.shape[0]
+        at, scales_at, (lo, hi), (scales_lo, scales_hi) = codes.data_ptr(), scales.data_ptr(), self._span, self._scales_span
+        if lo <= at < hi or scales_lo <= scales_at < scales_hi:
+            _inside("codes or scales")
         d = self.gated
         self._inputs = None
-        d.rows, d.codes, d.code_scales, d.codes_stride = n, codes.data_ptr(), scales.data_ptr(), stride
+        d.rows, d.codes, d.code_scales, d.codes_stride = n, at, scales_at, stride
         self._run(eco.eco_gated, d, stream, () if stream is None else (codes, scales, self.gate, self.gate_scales, self.up, self.up_scales, self.out, self.scales))
         self._inputs = codes, scales, n
         return (self.out, self.scales) if n == self.rows else (self.out[:n], self.scales[:n])

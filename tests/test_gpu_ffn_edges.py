@@ -95,3 +95,54 @@ def test_norm_of_rows_whose_squares_pass_the_range(harness, dim, dtype, residual
     want = norm_exact(x[rows].double(), gain.double(), 1e-6, grad[rows])
     hold(grad_gain, want["grad_gain"], want["grad_gain_tol"] + (grad[rows].double().abs() * x[rows].double().abs() * want["rstd"][:, None]).sum(0) * 2.0 ** -22, "grad_gain")
     hold(grad_input, want["grad_input"], want["grad_input_tol"] + want["rstd"][:, None] * 2.0 ** -20 * (1 + grad[rows].double().abs()), "grad_input")
+
+
+def test_inputs_in_what_a_call_writes(harness):      # noqa: F811
+    """Refused where rows would be written that are still to be read, the object left as it was; as elsewhere where they are read first."""
+    gen = torch.Generator().manual_seed(6)
+    codes, scales = activations(300, 256, gen)
+    w, ws, _ = weights(256, 256, "fp8", 256, "fp32", gen)
+    unit = harness.GatedUnit(300, 256, 256, gate=w, gate_scales=ws, up=w, up_scales=ws, group_size=256, training=True)
+    first = [t.clone() for t in unit.forward(codes, scales)]
+    for c, s in ((unit.out, scales), (unit.out[1:], scales[1:]), (codes, unit.scales), (codes[:100], unit.scales[200:])):
+        with pytest.raises(ValueError, match="lies in"):
+            unit.forward(c, s)
+    unit.backward(torch.ones(300, 256, dtype=torch.bfloat16, device="cuda"))
+    again = unit.forward(*[t.clone() for t in first])
+    assert not torch.equal(again[0], first[0])
+    line = harness.Linear(300, 256, 256, weights=w, scales=ws, group_size=256, training=True)
+    out = line.forward(codes, scales).clone()
+    grad = torch.randn(300, 256, generator=gen).bfloat16().cuda()
+    want = line.backward(grad)[0].clone()
+    for bad in (line.grad_input, line.grad_input[:300]):
+        with pytest.raises(ValueError, match="lies in"):
+            line.backward(bad)
+    assert torch.equal(line.backward(grad)[0], want)
+    with pytest.raises(ValueError, match="lies in"):
+        line.forward(codes[1:], scales[1:], add=line.out[1:])
+    line.out.copy_(out)
+    assert torch.equal(line.forward(codes, scales, add=line.out), line.forward(codes, scales, add=out.clone()))
+    x, r = (torch.randn(300, 256, generator=gen).bfloat16().cuda() for _ in range(2))
+    for quantize in (True, False):
+        norm = harness.RowNorm(300, 256, residual=True, quantize=quantize, training=True, device=x.device)
+        want = [t.clone() for t in norm.forward(x, r) if t is not None]
+        for a, b in ((norm.sum[1:], r[1:]), (x[:9], norm.sum[3:12])):
+            with pytest.raises(ValueError, match="lies in"):
+                norm.forward(a, b)
+        norm.sum.copy_(x)
+        assert all(torch.equal(p, q) for p, q in zip([t for t in norm.forward(norm.sum, r) if t is not None], want))
+        if not quantize:
+            norm.out.copy_(r)
+            assert all(torch.equal(p, q) for p, q in zip([t for t in norm.forward(x, norm.out) if t is not None], want))
+            with pytest.raises(ValueError, match="lies in"):
+                norm.forward(norm.out[1:], r[1:])
+        norm.forward(x, r)
+        want = norm.backward(grad, r)[0].clone()
+        for a, b in ((norm.grad_input[:, :], r), (grad, norm.grad_input)):
+            norm.grad_input.copy_(grad if b is r else r)
+            assert torch.equal(norm.backward(a, b)[0], want)
+        norm.forward(x[1:], r[1:])
+        with pytest.raises(ValueError, match="lies in"):
+            norm.backward(norm.grad_input[1:], r[1:])
+        with pytest.raises(ValueError, match="lies in"):
+            norm.backward(grad[1:], norm.grad_input[1:])
