@@ -674,6 +674,8 @@ class RowNorm(_RowUnit):
         self.device = dev = dev if dev.index is not None else torch.device("cuda", torch.cuda.current_device())
         if dtype not in _DTYPE or gain is not None and (gain.shape != (dim,) or gain.dtype not in _DTYPE or not gain.is_contiguous()):
             raise ValueError(f"dtype and gain: {' or '.join(map(str, _DTYPE))}, and {dim} contiguous gains, are needed")
+        if grad_gain_dtype not in _DTYPE:
+            raise ValueError(f"grad_gain_dtype: {' or '.join(map(str, _DTYPE))} is needed")
         self.rows, self.dim, self.dtype, self.gain, self.has_residual, self.quantize, self.training = rows, dim, dtype, gain, residual, quantize, training
         self.out = torch.empty(rows, dim, dtype=torch.uint8 if quantize else dtype, device=dev)
         self.scales = torch.empty(rows, -(-dim // 128), dtype=torch.uint8, device=dev) if quantize else None

@@ -146,3 +146,8 @@ def test_inputs_in_what_a_call_writes(harness):      # noqa: F811
             norm.backward(norm.grad_input[1:], r[1:])
         with pytest.raises(ValueError, match="lies in"):
             norm.backward(grad[1:], norm.grad_input[1:])
+
+
+def test_types_of_the_gains_gradient(harness):      # noqa: F811
+    with pytest.raises(ValueError, match="grad_gain_dtype"):
+        harness.RowNorm(4, 128, gain=torch.ones(128, device="cuda"), training=True, grad_gain_dtype=torch.float16)
