@@ -373,8 +373,8 @@ eco_status_t eco_head_loss_backward(const eco_head_t *head, void *workspace, siz
  * kept between calls, and calls that may run at the same time have one each.  All run asynchronously on `stream`, allocate nothing and may be captured into a graph.  No atomics:
  * the same call on the same arrays gives the same bits.  At most 2^23 rows and 2^16 columns of anything, strides below 2^23.
  * Time: the reading of the weights bounds few rows (INT4 weights save a sixth to a fifth of FP8's time), products many: with a scale a row 8-bit products run up to a third faster
- * than with one a block of 128, and the gradients' are in bf16, at half the rate.  Calls with INT4 weights and more than 64 rows write the codes as E4M3 first (1.5 bytes
- * moved a weight).
+ * than with one a block of 128, and the gradients' are in bf16, at half the rate.  INT4 codes are written as E4M3 first (1.5 bytes moved a weight) by forward calls with more than
+ * 64 rows and by the gated unit's backward pass with any.
  */
 
 /* eco_rows_quantize — rows of src_dtype (ECO_DT_FP32 or ECO_DT_BF16) as 8-bit rows: an attention's output, say, on its way to eco_linear. */
@@ -415,8 +415,9 @@ eco_status_t eco_norm_backward(const eco_norm_t *norm, void *workspace, size_t w
 /*
  * Linear product of 8-bit rows with quantized weights:  out = x W^T (+ add), x = code 2^e, W = dec(code) * scale, out_dim x in_dim as eco_step keeps them.
  * in_dim is a multiple of 16.  Scale groups: the row (group_size = in_dim), the tensor (group_size >= its elements), or a multiple of 128 elements that divides in_dim.
- * Sums are fp32, of 128 at a time where groups are shorter than rows, times the weights' scale; out is rounded once.  INT4 codes are exact as E4M3.  For out in fp32, and for
- * up to 16 rows (INT4: 64), the sums are of exact products.  Otherwise the matrix instruction for 8 bits makes them, which of eight neighbouring products leaves out what is below
+ * Sums are fp32, of 128 at a time where groups are shorter than rows, times the weights' scale; out is rounded once.  INT4 codes are exact as E4M3.  The sums are of exact products
+ * for out in fp32, for up to 16 rows (INT4: 64) and, of 17 to 64 FP8 rows, where the kernel for few rows is estimated to be the faster one: the last bits of a row may differ with the
+ * number of rows beside it.  Otherwise the matrix instruction for 8 bits makes them, which of eight neighbouring products leaves out what is below
  * 2^-13 of the largest: up to 2^-14.4 of a result's size where some channels are far larger than others, a fiftieth of what rounding to bf16 leaves.  (Of the gated unit's 8-bit
  * rows one code in 400 to 1200 is then its neighbour: 0.0019 of a row's size, beside the 0.026 of the codes' own rounding.)  backward, from grad_out (bf16):
  *     grad_input = grad_out W   (of the values behind the 8-bit rows; W rounded to bf16, sums fp32, rounded once to bf16)
@@ -442,7 +443,8 @@ eco_status_t eco_linear_backward(const eco_linear_t *linear, void *workspace, si
 
 /*
  * Gated unit:  h = act(x G^T) * (x U^T) as 8-bit rows, x 8-bit rows, G and U width x in_dim as the weights of eco_linear.  Both projections, the activation, the
- * product and the rounding to 8 bits are one kernel; nothing else is kept, and the backward pass computes a = x G^T and b = x U^T again.  From grad_out = dL/dh (bf16):
+ * product and the rounding to 8 bits are one kernel (few rows: two); nothing else is kept, and the backward pass computes a = x G^T and b = x U^T again, with any number of rows by the
+ * instruction for 8 bits: with few, whose forward sums are of exact products, it takes the gradients at an a and b that are up to 2^-14.4 of their size away.  From grad_out = dL/dh (bf16):
  *     ga = grad_out b act'(a),  gb = grad_out act(a), each rounded once to bf16
  *     grad_input = ga G + gb U,  grad_gate = ga^T x,  grad_up = gb^T x     (as those of eco_linear)
  */
