@@ -14,9 +14,10 @@ constexpr uint32_t FFN_BLOCK = 128;               // elements of a row to a scal
 // of their own.  What the parts may take: a workspace is asked for once, for the most rows, and has to hold any call with fewer.
 constexpr uint32_t FFN_UNITS = 256;
 constexpr uint64_t FFN_MOST_SPLITS = 16, FFN_MOST_PARTIAL = 1ull << 24;      // elements
-// The most rows of the kernel for few rows, whose time grows with them, and those up to which it is always the faster: INT4 weights are wanted as E4M3 by tiles, a pass of its own.
-// us at 16, 32 and 64 rows and, from 17 on, of tiles: FP8 6912 x 1152 9.6, 13.3, 20.3 and 11.0 to 11.7; 14336 x 4096 20.7, 29.9, 44 and 18.1 to 18.6; gated 2048 x 1408 8.9, 10.3, 12.9
-// and 17.3; INT4 4096 x 14336 14.4, 17.8, 25.4 and 18.5 after 15 for the codes.
+// The most rows of the kernel for few rows, whose time grows with them, and those up to which it is taken whatever tiles cost: INT4 weights are wanted as E4M3 by tiles, a pass of its own,
+// and up to 16 FP8 rows it is the faster one but for long inner axes, where its exact sums cost up to a fifth.  us at 16, 32 and 64 rows, and of tiles: FP8 6912 x 1152 9.7, 13.3, 20.1
+// and 10.4 to 11.6; 14336 x 4096 21.4, 29.7, 43.5 and 17.5 to 18.1; gated 2048 x 1408 8.9, 10.4, 12.9 and 16.6 to 16.9; INT4 4096 x 14336 14.7, 17.6, 25.0 and 31, of which the codes
+// are 13.
 constexpr uint64_t FFN_FEW_ROWS = 64;
 constexpr uint64_t ffn_always_few(int fmt) { return fmt == ECO_FMT_INT4 ? FFN_FEW_ROWS : 16; }
 

@@ -125,11 +125,11 @@ struct Tile8 {
 // A workgroup goes through tiles gridDim.x apart; its loads do not stop between them: while a tile's results leave, the next tile's first steps are on their way.
 // EXACT: in bf16, whose instruction adds products as an fp32 sum does.  The one for 8 bits, twice as fast, leaves out of eight neighbouring products what is below 2^-13
 // of the largest of them: 2^-14.4 of a result of activations with outlying channels, far below its rounding to bf16 or 8 bits, but not to fp32.  Of the gated unit's 8-bit rows
-// one code in 400 to 1200 becomes its neighbour by it, 0.0019 of a row's size beside the 0.026 of their rounding; exact sums took it from 170 to 284 us at 8192 x 1152 x 6912.
+// one code in 400 to 1200 becomes its neighbour by it, 0.0019 of a row's size beside the 0.026 of their rounding; exact sums took it from 162 to 279 us at 8192 x 1152 x 6912.
 //
 // What bounds it: the matrix cores are busy for 31 % of the time of that product.  A step of a 256 x 256 tile takes 2.05 us, in which the matrix cores, the reads of LDS and the
-// loads to it have 0.9 us of work each, between two barriers; with a scale a row, without the multiplications by the blocks' scales, 1.6.  8192 x 6912 with 6912 columns 1904 TFLOP/s
-// (2482 with a scale a row); 8192 x 1152 x 6912, nine steps between a tile's ends, 1530.
+// loads to it have 0.9 us of work each, between two barriers; with a scale a row, without the multiplications by the blocks' scales, 1.6.  8192 x 6912 with 6912 columns 2000 TFLOP/s
+// (2330 with a scale a row; the same inputs again and again 2080 and 2520); gated 8192 x 1152 x 6912, nine steps between a tile's ends, 1630.
 // SCALES: of the weights, BY_BLOCK, or BY_ROW of rows that are whole blocks, or BY_ROW_CUT of others.
 enum : int { BY_BLOCK = 0, BY_ROW = 1, BY_ROW_CUT = 2 };
 template <int MI, int NJ, int END, int SCALES, bool EXACT>
@@ -593,9 +593,9 @@ __global__ __launch_bounds__(256) void eco_ffn_join_kernel(ProductArgs a, uint32
 // ------------------------------------------------------------------------------------------------ few rows
 
 // Few rows are bound by the reading of the weights: each wave reads 16 NT rows of them by itself, straight into the registers in which the matrix core takes
-// them, AHEAD blocks at a time (twice as many: linear 1 x 4096 x 14336 15.9 us instead of 15.2, gated 1 x 1152 x 6912 9.6 instead of 9.1), and INT4 codes become E4M3 there.
-// Nothing is kept in LDS but sums on their way from wave to wave.  The products are exact ones in bf16: they cost little beside the loads (linear 1 x 6912 x 1152 7.4 us,
-// 7.9 in 8 bits; gated 24 x 1152 x 6912 13.5 and 11.7).
+// them, AHEAD blocks at a time (twice as many: linear 1 x 4096 x 14336 16.0 us instead of 15.4, gated 1 x 1152 x 6912 9.5 instead of 8.9), and INT4 codes become E4M3 there.
+// Nothing is kept in LDS but sums on their way from wave to wave.  The products are exact ones in bf16: they cost little beside the loads (linear 1 x 6912 x 1152 7.5 us,
+// 7.0 in 8 bits; gated 24 x 1152 x 6912 11.0 and 11.1).
 template <class V>
 __device__ __forceinline__ V loose(const void *p) {            // at an address of any alignment
   V v;
@@ -753,8 +753,8 @@ __global__ __launch_bounds__(FEW_WAVES * 64) void eco_ffn_few_kernel(ProductArgs
 }
 
 // Columns of a workgroup, by 16: four, which read each row of x a quarter as often, where that leaves three workgroups to a compute unit, two where there would be one
-// and a half of one, and else one.  us with 16, 32 and 64: linear, 1 and 32 rows, 4096 x 14336 17.1, 16.2, 15.3 and 35.4, 27.5, 21.2; 14336 x 4096 15.2, 23.3, 42.8 and
-// 30.0, 37.9, 56.0; gated 1152 x 6912 9.3, 8.9, 11.9 and 13.9, 11.2, 14.7.
+// and a half of one, and else one.  us with 16, 32 and 64: linear, 1 and 32 rows, 4096 x 14336 17.1, 15.7, 15.0 and 35.5, 27.5, 20.8; 14336 x 4096 15.3, 23.3, 43.3 and
+// 30.6, 37.8, 55.6; gated 1152 x 6912 9.5, 9.0, 11.8 and 14.0, 11.2, 14.5.
 constexpr int few_wide(int mt, bool gated) { return mt * (gated ? 2 : 1) <= 4 ? 4 : 2; }      // (what the sums' place in LDS holds)
 uint32_t few_columns(uint64_t width, int mt, bool gated) {
   const uint64_t groups = (width + 15) / 16;
@@ -826,8 +826,8 @@ double ffn_split(uint64_t tiles, uint64_t steps, uint64_t units, uint64_t least_
 }
 
 // Microseconds of the kernel for few rows: a block's loads and its share of products for each of a wave's fragments, or what the weights take, and for the gated unit the launch
-// that makes 8-bit rows.  Measured and by this rule, 32 and 64 rows: linear 6912 x 1152 13.3, 20.3 and 14.5, 19.4; 2048 x 1408 6.4, 8.9 and 6.0, 7.4; 4096 x 14336 20.9, 28.0
-// and 17.8, 29.0; gated 2048 x 1408 10.3, 12.9 and 9.8, 11.6; 4096 x 14336 37.3, 52.8 and 34, 43.
+// that makes 8-bit rows.  Measured and by this rule, 32 and 64 rows: linear 6912 x 1152 13.3, 20.1 and 14.5, 19.4; 2048 x 1408 6.3, 8.8 and 6.0, 7.4; 4096 x 14336 20.5, 27.5
+// and 17.8, 29.0; gated 2048 x 1408 10.4, 12.9 and 9.8, 11.6; 4096 x 14336 37.7, 55.9 and 34, 43.
 double few_cost(const FfnWeights &w, uint64_t rows, bool gated) {
   const int mt = rows <= 16 ? 1 : rows <= 32 ? 2 : 4, columns = static_cast<int>(few_columns(w.rows, mt, gated)), fragments = mt * columns * (gated ? 2 : 1);
   const uint64_t blocks = (w.dim + FFN_BLOCK - 1) / FFN_BLOCK, each = (blocks + FEW_WAVES - 1) / FEW_WAVES, groups = (w.rows + 16 * columns - 1) / (16 * columns);
@@ -837,8 +837,9 @@ double few_cost(const FfnWeights &w, uint64_t rows, bool gated) {
   return (work < bytes ? bytes : work) + (gated ? 6.0 : 2.6);
 }
 
-// Microseconds of a step of 128 and of a tile's ends (8192 x 6912 and 8192 x 1024 over widths that are whole rounds: 256 x 256 122 and 26 us, 256 x 128 73 and 18,
-// 128 x 128 46 and 11.5, 64 x 128 33 and 8.9; gated, tiles of 256, 128 and 64 rows, 120 and 27, 75 and 17, 57 and 12).  In bf16 products a step is of twice the work.
+// Microseconds of a step of 128 and of a tile's ends (8192 x 6912 and 8192 x 1024 over widths that are whole rounds: 256 x 256 118 and 25 us, 256 x 128 71 and 17,
+// 128 x 128 45 and 11, 64 x 128 33 and 8.6; gated, tiles of 256, 128 and 64 rows, 115 and 27, 72 and 17.5, 49 and 12).  In bf16 products a step is of twice the work: 256 x 128 110 and
+// 27, 128 x 128 70 and 18, 64 x 128 50 and 12.5.
 FfnPlan ffn_plan(int end, const FfnWeights &w, uint64_t rows, bool exact) {
   const uint32_t steps = (w.dim + FFN_BLOCK - 1) / FFN_BLOCK;
   FfnPlan p = {end, 256, 256, exact, {0, 0, 1, steps, 0}};

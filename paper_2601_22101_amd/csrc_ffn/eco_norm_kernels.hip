@@ -4,8 +4,8 @@
 //   grad_input = rstd (u - n mean(u n)) + grad_sum,  grad_gain = sum over rows of grad_out n.
 // Bound by memory: each array is read or written once.  A row is held in registers: of a wave up to 512 elements, of two, three or four up to 1024, 1536 and 2048, of four with
 // two or four pieces a lane up to 8192; wider rows are read twice, the second time from the caches.  A workgroup for each row, so that many rows' loads are under way
-// at once (16384 x 2048 in bf16 with residual: forward 47 us, 5.0 TB/s, backward 52 us, 5.2 TB/s; with a wave a row for all sizes both take 121 us instead of 98).  The gain's gradient is summed
-// over the rows of each of 1024 workgroups, and those by a second kernel: 512, 1024, 1536 and 2048 of them take the backward pass 68.6, 50.6, 57.9 and 53.2 us.
+// at once (16384 x 2048 in bf16 with residual: forward 47 us, 5.0 TB/s, backward 52 us, 5.2 TB/s; with a wave a row both take 127 us instead of 101).  The gain's gradient is summed
+// over the rows of each of 1024 workgroups, and those by a second kernel: 512, 1024, 1536 and 2048 of them: 116, 101, 107 and 104 us both ways.
 #include <hip/hip_runtime.h>
 
 #include "../csrc/eco_device.hpp"
