@@ -4,7 +4,7 @@
 // grad_input averages: 0.0021 to 0.0024 of grad_input with the result's own rounding, 0.0027 to 0.0029 where G, the gated unit's, was rounded too; in two bf16 terms W would take
 // a second product).  Both products have the inner axis of their X operand, W or x, across memory, which the transposing reads of LDS turn.
 //
-// Bound by the matrix cores at large sizes: both products of two matrices of 6912 x 1152 with 8192 rows, 522 GFLOP, 458 us, the cores busy for 64 % of it at the 1.85 GHz that the
+// Bound by the matrix cores at large sizes: both products of two matrices of 6912 x 1152 with 8192 rows, 522 GFLOP, 455 us, the cores busy for 64 % of it at the 1.9 GHz that the
 // chip then runs at (torch's product of 8192^3 69 %).  The operands are 15 us of memory traffic beside them, the joining of split tiles 12.
 #include <hip/hip_runtime.h>
 
